@@ -44,7 +44,8 @@ typedef enum {
   DMM_ELD = -6,    /* a leading dimension is smaller than the tile's width, or a row pitch (leading
                       dimension times element size) of an A, B or C tile is 2^24 bytes or more */
   DMM_ELIMIT = -7  /* dmm_reduce_replicas_static: the work tables of this call do not fit the library's
-                      static device buffer (DMM_STATIC_SCRATCH_BYTES) */
+                      static device buffer (DMM_STATIC_SCRATCH_BYTES); dmm_mx_*: more than 2^30 workgroups or table
+                      entries */
 } dmm_status;
 
 /* Element type of the A and B tiles.  All partial sums are fp32, and so are the C tiles unless
@@ -270,6 +271,68 @@ int dmm_broadcast_replica(dmm_plan_t *p, void *const *c_tiles, const int64_t *c_
 int dmm_reduce_replicas_static(dmm_plan_t *p, void *const *c_tiles, const int64_t *c_ld,
                                int32_t origin_replica, void *hip_stream);
 
+/* ---- 4-bit microscaled floating point ------------------------------------------------------
+ *
+ * A form of a matrix that takes 4.25 bits an element: blocks of DMM_MX_BLOCK neighbouring elements along
+ * one axis of a tile share a scale 2^e, one byte e + 127, and an element is a 4-bit code: a sign and one of 0, 0.5, 1,
+ * 1.5, 2, 3, 4, 6 (codes 0 .. 7; the OCP microscaling formats' E2M1 elements and E8M0 scales).
+ *   e = floor(log2(largest magnitude of the block)) - 2, kept to [-127, 127]; -127 for a block of zeros
+ *   code = element / 2^e, rounded to nearest, half-way values to the even code, 6 beyond 6
+ *   a block that holds an infinity or a NaN has the scale byte 255 and stands for NaN throughout
+ * Blocks start at the tile's first element of the axis, so the last one may be shorter.
+ *
+ * A tile of h x w elements along its rows (DMM_MX_ROWS): h rows of codes, two a byte, the even one in the
+ * low half, and h rows of scale bytes.  Along its columns (DMM_MX_COLS): the same of the transposed tile, i.e. w rows that
+ * each run down a column.  Rows are filled up with zeros to whole chunks of DMM_MX_CHUNK elements: code_ld >=
+ * 64 bytes and scale_ld >= 4 bytes a chunk.  Codes are aligned to 16 bytes and code_ld is a multiple of 16, scales and
+ * scale_ld of 4 (DMM_EINVAL, DMM_ELD), and both leading dimensions stay below 2^24 bytes (DMM_ELD).  Bytes of a row behind
+ * its last chunk are neither read nor written.
+ *
+ * The rows of the transposed matrix are the columns of the matrix, so the form of X along its columns is the
+ * form of X^T along its rows: the same buffers serve both, with the tables in the order of the transposed tile
+ * grid.  A layer that is trained takes every matrix in both forms: C = A B needs A along its rows and B along its columns, dA =
+ * dC B^T needs dC along its rows and B along its rows (B^T along its columns), dB = A^T dC both along their columns. */
+#define DMM_MX_BLOCK 32
+#define DMM_MX_CHUNK 128
+#define DMM_MX_ROWS 1
+#define DMM_MX_COLS 2
+typedef struct {
+  void *const *codes;        /* host array of device pointers, one per (replica, tile) in table order */
+  const int64_t *code_ld;    /* bytes from one row of codes to the next */
+  void *const *scales;
+  const int64_t *scale_ld;   /* bytes */
+} dmm_mx_tiles;
+
+/* The tiles of X, bf16 or fp32 (`dtype`, x_ld in elements), to 4 bits: along their rows into `rows`, along their columns
+ * into `cols`; either may be null, not both.  Both take one pass over X.  Every replica is quantised from
+ * its own tiles; the process grid of X plays no part.  Writes whole chunks, zeros behind a tile's end included.  Pointers of empty
+ * tiles may be null.  Asynchronous on `hip_stream`; takes no memory and keeps nothing, so calls may overlap on any
+ * streams and be captured.  X and the outputs must not overlap. */
+int dmm_mx_quantize(const dmm_matrix_desc *X, int dtype, const void *const *x_tiles, const int64_t *x_ld,
+                    const dmm_mx_tiles *rows, const dmm_mx_tiles *cols, void *hip_stream);
+
+/* The values that the codes stand for, into the tiles of X (all are exact in bf16 and in fp32).  `along`: DMM_MX_ROWS or
+ * DMM_MX_COLS, whichever form `q` is.  Otherwise as dmm_mx_quantize. */
+int dmm_mx_dequantize(const dmm_matrix_desc *X, const dmm_mx_tiles *q, int along, int dtype, void *const *x_tiles,
+                      const int64_t *x_ld, void *hip_stream);
+
+/* dmm_execute for 4-bit operands: C = A B (overwrite) on a plan, A along its rows, B along its columns.
+ *   a, b      tables in the order of the plan's A and B
+ *   c_tiles   fp32 tiles (bf16 with DMM_C_BF16: C with one replica only), every element written once
+ *   flags     0 or any of DMM_NO_REDUCE, DMM_C_BF16
+ * Scales are applied by the matrix instructions, sums are fp32.  Blocks of A and of B must meet: every op's k range has
+ * to start at a multiple of DMM_MX_CHUNK inside its A tile and inside its B tile (DMM_EINVAL otherwise), which is so
+ * where A's column cuts, B's row cuts and the replicas' shares of k lie at such multiples.  Few rows run on
+ * kernels that stream B; where tiles are few they are cut along K into runs whose partial sums go through a
+ * scratch buffer and are added in ascending k (fixed cut and order: results are reproducible).
+ * Replicas of C, streams and ownership as for dmm_execute: replica 0 receives the sum unless DMM_NO_REDUCE, the call
+ * is asynchronous, the first call on a plan takes its work table (and, if needed, that scratch buffer) from a pool, later calls
+ * with the same arguments allocate nothing.  The plan's tables and scratch buffer serve all its calls: one that is to be
+ * captured is made once before, and while the graph is in use the plan is called with those arguments only, in stream order
+ * with the graph's launches.  dmm_plan_last_execute, dmm_plan_last_kernels and the elapsed times do not speak of these calls. */
+int dmm_mx_execute(dmm_plan_t *p, const dmm_mx_tiles *a, const dmm_mx_tiles *b, void *const *c_tiles, const int64_t *c_ld,
+                   uint32_t flags, void *hip_stream);
+
 /* ---- measurement and test aids (not steps of the method) ---------------------------------- */
 
 /* What the last dmm_execute on a plan did.
@@ -347,7 +410,7 @@ void dmm_plan_destroy(dmm_plan_t *p);
 
 const char *dmm_strerror(int status);
 int dmm_last_hip_error(void); /* hipError_t of the last failed HIP call on this thread, 0 if none */
-int dmm_version(void);         /* 5: dmm_plan_last_kernels (4: the replica sum is fused into the GEMM unless DMM_SEPARATE_REDUCE asks
+int dmm_version(void);         /* 6: dmm_mx_quantize, dmm_mx_dequantize, dmm_mx_execute (5: dmm_plan_last_kernels; 4: the replica sum is fused into the GEMM unless DMM_SEPARATE_REDUCE asks
                                   for the kernel of its own; dmm_plan_last_execute replaces the
                                   dmm_plan_ran_* accessors; 3: flag values of dmm_plan and dmm_execute disjoint,
                                   dmm_reduce_replicas_static) */

@@ -26,6 +26,8 @@ DMM_C_BF16 = 0x400
 DMM_NO_MERGE = 0x800
 DMM_SEPARATE_REDUCE = 0x1000
 DMM_STATIC_SCRATCH_BYTES = 1 << 20
+DMM_MX_BLOCK, DMM_MX_CHUNK = 32, 128
+DMM_MX_ROWS, DMM_MX_COLS = 1, 2
 STATIONARY_FLAGS = {"C": 0, "B": DMM_STATIONARY_B, "A": DMM_STATIONARY_A}
 STATUS_NAMES = {0: "OK", -1: "EINVAL", -2: "ESHAPE", -3: "EREPL", -4: "ENOMEM", -5: "EHIP", -6: "ELD", -7: "ELIMIT"}
 
@@ -69,6 +71,10 @@ class dmm_execute_report(C.Structure):
 
 class dmm_kernel_report(C.Structure):
     _fields_ = [("small_rows", C.c_int32), ("small_cols", C.c_int32), ("small_runs", C.c_int32), ("ran_dense", C.c_int32)]
+
+
+class dmm_mx_tiles(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("code_ld", C.c_void_p), ("scales", C.c_void_p), ("scale_ld", C.c_void_p)]
 
 
 class DmmError(RuntimeError):
@@ -127,6 +133,12 @@ def lib() -> C.CDLL:
         L.dmm_broadcast_replica.argtypes = [P, P, P, C.c_int32, P]
         L.dmm_reduce_replicas_static.restype = C.c_int
         L.dmm_reduce_replicas_static.argtypes = [P, P, P, C.c_int32, P]
+        L.dmm_mx_quantize.restype = C.c_int
+        L.dmm_mx_quantize.argtypes = [C.POINTER(dmm_matrix_desc), C.c_int, P, P, C.POINTER(dmm_mx_tiles), C.POINTER(dmm_mx_tiles), P]
+        L.dmm_mx_dequantize.restype = C.c_int
+        L.dmm_mx_dequantize.argtypes = [C.POINTER(dmm_matrix_desc), C.POINTER(dmm_mx_tiles), C.c_int, C.c_int, P, P, P]
+        L.dmm_mx_execute.restype = C.c_int
+        L.dmm_mx_execute.argtypes = [P, C.POINTER(dmm_mx_tiles), C.POINTER(dmm_mx_tiles), P, P, C.c_uint32, P]
         L.dmm_plan_elapsed_ms.restype = C.c_int
         L.dmm_plan_elapsed_ms.argtypes = [P, C.POINTER(C.c_float), C.POINTER(C.c_float)]
         L.dmm_plan_gemm_launch_ms.restype = C.c_int
@@ -146,7 +158,7 @@ def lib() -> C.CDLL:
 EXPORTS = ("dmm_plan", "dmm_plan_num_tasks", "dmm_plan_tasks", "dmm_plan_order", "dmm_plan_num_groups",
            "dmm_plan_group_offsets", "dmm_plan_num_items", "dmm_plan_items", "dmm_plan_macro_tile",
            "dmm_plan_num_merged_items", "dmm_plan_merged_items", "dmm_plan_last_execute", "dmm_plan_last_kernels",
-           "dmm_reduce_replicas_static",
+           "dmm_reduce_replicas_static", "dmm_mx_quantize", "dmm_mx_dequantize", "dmm_mx_execute",
            "dmm_execute", "dmm_reduce_replicas", "dmm_broadcast_replica", "dmm_plan_elapsed_ms", "dmm_plan_gemm_launch_ms", "dmm_plan_destroy", "dmm_strerror",
            "dmm_last_hip_error", "dmm_version", "dmm_measure_mfma_rate")
 
@@ -171,6 +183,27 @@ def _ptr(x) -> int:
 
 def _table(entries: Sequence, ctype):
     return (ctype * max(len(entries), 1))(*entries)
+
+
+def matrix_desc(d: Dict) -> dmm_matrix_desc:
+    """The C structure of a descriptor, for calls that take a matrix without a plan (reusable across calls)."""
+    keep: List = []
+    out = _desc(d, keep)
+    out.keep = keep
+    return out
+
+
+def tile_table(tiles: Sequence, ld: Sequence[int]):
+    """The pointer and leading-dimension arrays of a matrix' tiles (reusable across calls)."""
+    return _table([_ptr(t) for t in tiles], C.c_void_p), _table(list(ld), C.c_int64)
+
+
+def mx_tiles(codes: Sequence, code_ld: Sequence[int], scales: Sequence, scale_ld: Sequence[int]) -> dmm_mx_tiles:
+    """The tables of a matrix in 4 bits: codes and scales of every tile, leading dimensions in bytes (reusable across calls)."""
+    keep = [*tile_table(codes, code_ld), *tile_table(scales, scale_ld)]
+    out = dmm_mx_tiles(*[C.cast(x, C.c_void_p) for x in keep])
+    out.keep = keep
+    return out
 
 
 class Plan:
@@ -289,6 +322,12 @@ class Plan:
         if rc != DMM_OK:
             raise DmmError(rc, "dmm_execute")
 
+    def execute_mx(self, a: dmm_mx_tiles, b: dmm_mx_tiles, c, flags: int = 0, stream: Optional[int] = None) -> None:
+        """``dmm_mx_execute``: `a` along its rows and `b` along its columns (`mx_tiles`), `c` a `tile_table`."""
+        rc = lib().dmm_mx_execute(self._h, C.byref(a), C.byref(b), c[0], c[1], flags, C.c_void_p(stream or 0))
+        if rc != DMM_OK:
+            raise DmmError(rc, "dmm_mx_execute")
+
     def reduce_replicas(self, c_tiles: Sequence, c_ld: Sequence[int], origin: int = 0,
                         stream: Optional[int] = None) -> None:
         ct = _table([_ptr(t) for t in c_tiles], C.c_void_p)
@@ -357,6 +396,25 @@ def dmm_reduce_replicas(plan: Plan, c_tiles, c_ld, origin: int = 0, stream: Opti
 
 def dmm_reduce_replicas_static(plan: Plan, c_tiles, c_ld, origin: int = 0, stream: Optional[int] = None) -> None:
     plan.reduce_replicas_static(c_tiles, c_ld, origin, stream)
+
+
+def dmm_mx_quantize(desc: dmm_matrix_desc, dtype: int, x, rows: Optional[dmm_mx_tiles] = None, cols: Optional[dmm_mx_tiles] = None,
+                    stream: Optional[int] = None) -> None:
+    """`desc` a `matrix_desc`, `x` a `tile_table`, `rows` and `cols` `mx_tiles`."""
+    rc = lib().dmm_mx_quantize(C.byref(desc), dtype, x[0], x[1], None if rows is None else C.byref(rows), None if cols is None else C.byref(cols),
+                               C.c_void_p(stream or 0))
+    if rc != DMM_OK:
+        raise DmmError(rc, "dmm_mx_quantize")
+
+
+def dmm_mx_dequantize(desc: dmm_matrix_desc, q: dmm_mx_tiles, along: int, dtype: int, x, stream: Optional[int] = None) -> None:
+    rc = lib().dmm_mx_dequantize(C.byref(desc), C.byref(q), along, dtype, x[0], x[1], C.c_void_p(stream or 0))
+    if rc != DMM_OK:
+        raise DmmError(rc, "dmm_mx_dequantize")
+
+
+def dmm_mx_execute(plan: Plan, a: dmm_mx_tiles, b: dmm_mx_tiles, c, flags: int = 0, stream: Optional[int] = None) -> None:
+    plan.execute_mx(a, b, c, flags, stream)
 
 
 def dmm_plan_destroy(plan: Plan) -> None:

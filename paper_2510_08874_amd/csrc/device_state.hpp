@@ -558,7 +558,25 @@ struct ExecLayout {
   RedLaunch red;                // the replica-sum launch behind the GEMM (n_items == 0: none)
 };
 
+// Where the tables of a product of 4-bit operands sit in its buffer, and what it launches.
+struct MxLayout {
+  int shape = 0, n_items = 0, n_joins = 0;
+  size_t o_segs = 0, o_joins = 0;
+};
+
+// What a plan keeps for dmm_mx_execute: the tables of its last call, the inputs that they were made from, and
+// scratch memory for partial sums.
+struct MxState {
+  Uploader table;
+  char *buf = nullptr;
+  size_t cap = 0;
+  std::vector<char> key;
+  MxLayout layout;
+  bool cached = false;
+};
+
 struct DeviceState {
+  MxState mx;
   // A product that runs on dense copies of its operands: the plan it runs as, whose `uses` stand for these
   // calls, where the copies are, and the tables of the kernel that makes them.
   dmm_plan_t *dense = nullptr;
@@ -610,6 +628,8 @@ void destroy_device_state(DeviceState *d) {
     if (d->t_pack[i]) (void)hipEventDestroy(d->t_pack[i]);
   d->gemm_table.release();
   d->red_table.release();
+  d->mx.table.release();
+  scratch_pool().release(&d->mx.buf, &d->mx.cap);
   scratch_pool().release(&d->split_buf, &d->split_cap);
   d->uses.destroy();
   for (int i = 0; i < 2; ++i) {

@@ -17,6 +17,7 @@
 #include "device_state.hpp"
 #include "gemm_kernel.hpp"
 #include "gemm_launch.hpp"
+#include "mx_launch.hpp"
 #include "pack_kernel.hpp"
 #include "plan_internal.h"
 #include "ring_kernel.hpp"
@@ -109,6 +110,17 @@ int check_lds(const Grid &G, const int64_t *ld) {
       for (int32_t tj = 0; tj < G.gc; ++tj) {
         const int64_t w = G.cc[tj + 1] - G.cc[tj], h = G.rc[ti + 1] - G.rc[ti];
         if (w > 0 && h > 0 && ld[G.table_index(rep, ti, tj)] < w) return DMM_ELD;
+      }
+  return DMM_OK;
+}
+
+// a buffer, aligned to its elements, behind every non-empty tile
+int check_tiles(const Grid &G, const void *const *tiles, int es) {
+  for (int32_t rep = 0; rep < G.c; ++rep)
+    for (int32_t ti = 0; ti < G.gr; ++ti)
+      for (int32_t tj = 0; tj < G.gc; ++tj) {
+        const void *t = tiles[G.table_index(rep, ti, tj)];
+        if (G.cc[tj + 1] > G.cc[tj] && G.rc[ti + 1] > G.rc[ti] && (!t || ((uintptr_t)t & (uintptr_t)(es - 1)))) return DMM_EINVAL;
       }
   return DMM_OK;
 }
@@ -1892,3 +1904,5 @@ extern "C" int dmm_reduce_replicas_static(dmm_plan_t *P, void *const *c_tiles, c
   DMM_HIP(hipGetLastError());
   return DMM_OK;
 }
+
+#include "mx_exec.hpp"

@@ -1,0 +1,492 @@
+// Matrices in 4-bit microscaled floating point (gfx950, device code only): quantisation, its inverse, and
+// the products of two such matrices.
+//
+// A block of 32 elements along one axis has the scale 2^e, e = floor(log2(largest magnitude)) - 2 kept to [-127, 127],
+// stored as the byte e + 127 (255: the block holds an infinity or a NaN, all of it stands for NaN); an element
+// is a 4-bit code: sign, two bits of exponent, one of mantissa (0, 0.5, 1, 1.5, 2, 3, 4, 6).  The instruction that
+// converts rounds to nearest, half-way values to the even code, and keeps what is larger than 6 at 6: checked against
+// every bf16 value.
+#pragma once
+
+#include "gemm_launch.hpp"
+#include "mx_launch.hpp"
+#include "nt_kernel.hpp"
+
+namespace dmm {
+
+// ---- products -------------------------------------------------------------------------------------
+
+__device__ __forceinline__ unsigned short mx_bf16(float v) { return __builtin_bit_cast(unsigned short, (__bf16)v); }
+
+// (the host sees to it that a macro-tile's rows lie within 2^32 bytes)
+template <class SH, class E>
+__device__ __forceinline__ void mx_store(const NtTile<SH> &tile, const MxItem &it, int row0, int col0) {
+  const unsigned pitch = (unsigned)it.ldc * (unsigned)sizeof(E);
+  char *const c = (char *)nt_uniform(it.c);
+#pragma unroll
+  for (int i = 0; i < SH::MI; ++i)
+#pragma unroll
+    for (int j = 0; j < SH::NI; ++j) {
+      const int col = col0 + 32 * j;
+      if (col < it.n_ext) {
+#pragma unroll
+        for (int x = 0; x < 16; ++x) {
+          const int row = row0 + 32 * i + 8 * (x / 4) + x % 4;
+          if (row < it.m_ext) {
+            const float v = tile.acc[i][j][x];
+            E *const to = (E *)(c + ((unsigned)row * pitch + (unsigned)(col * (int)sizeof(E))));
+            if constexpr (sizeof(E) == 4) __builtin_nontemporal_store(v, to);
+            else __builtin_nontemporal_store(mx_bf16(v), to);
+          }
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
+// Macro-tiles.  Stores: half a wave writes 32 neighbouring columns of a row.
+template <class SH>
+__global__ __launch_bounds__(NT_THREADS, SH::TM == 256 ? 1 : 2) void mx_gemm_kernel(const MxItem *__restrict__ items, const NtSeg *__restrict__ segs) {
+  extern __shared__ char lds[];
+  const MxItem it = items[blockIdx.x];
+  NtTile<SH> tile;
+  tile.run(segs + it.seg, it.n_segs, it.first, it.steps, it.m_off, it.m_ext, it.n_off, it.n_ext, lds);
+  tile.pin();
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int row0 = (wave >> 1) * (SH::TM / 2) + 4 * (lane >> 5), col0 = (wave & 1) * (SH::TN / 2) + (lane & 31);
+  if (it.c_es == 4) mx_store<SH, float>(tile, it, row0, col0);
+  else mx_store<SH, unsigned short>(tile, it, row0, col0);
+}
+
+// Sums of partial tiles, in ascending k.
+__global__ __launch_bounds__(256) void mx_join_kernel(const MxJoin *__restrict__ joins, int blocks_per_join) {
+  const MxJoin jn = joins[blockIdx.x / blocks_per_join];
+  const int at = ((blockIdx.x % blocks_per_join) * 256 + threadIdx.x) * 4;
+  const int row = at / jn.tn, col = at % jn.tn;
+  if (row >= jn.m_ext || col >= jn.n_ext) return;
+  const int64_t slot = (int64_t)jn.tm * jn.tn;
+  const float *p = jn.parts + at;
+  nt_f32x4 sum = *(const nt_f32x4 *)p;
+  for (int r = 1; r < jn.runs; ++r) sum += *(const nt_f32x4 *)(p + r * slot);
+#pragma unroll
+  for (int x = 0; x < 4; ++x)
+    if (col + x < jn.n_ext) {
+      const int64_t o = (int64_t)row * jn.ldc + col + x;
+      if (jn.c_es == 4) ((float *)jn.c)[o] = sum[x];
+      else ((unsigned short *)jn.c)[o] = mx_bf16(sum[x]);
+    }
+}
+
+// A few rows against many columns: bound by the bytes of B, which every wave reads straight into registers.  A
+// workgroup owns 16 NT columns and 16 MT rows; its four waves take every fourth 512 elements of K each and add up
+// through LDS, so that there are enough waves on the way to memory without partial sums in memory.
+template <int MT, int NT>
+__global__ __launch_bounds__(NT_THREADS) void mx_skinny_kernel(const MxItem *__restrict__ items, const NtSeg *__restrict__ segs) {
+  constexpr int Q = 4;                                        // steps (128 of k) at a time
+  __shared__ nt_f32x4 sums[4][MT * NT][64];
+  const MxItem it = items[blockIdx.x];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 15, g = lane >> 4;
+  nt_f32x4 acc[MT][NT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[i][j] = nt_f32x4{0.f, 0.f, 0.f, 0.f};
+  int todo = it.steps, skip = it.first;
+  for (int sg = 0; todo > 0; ++sg) {
+    const NtSeg s = segs[it.seg + sg];
+    const int n = s.steps - skip < todo ? s.steps - skip : todo;
+    const char *pa[MT], *pb[NT], *sa[MT], *sb[NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const int64_t row = it.m_off + min(16 * i + r, it.m_ext - 1);
+      pa[i] = s.a + row * s.a_pitch + (int64_t)skip * NT_ROW + g * 16;
+      sa[i] = s.a_scale + row * s.a_scale_pitch + (int64_t)skip * 4;
+    }
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      const int64_t row = it.n_off + min(16 * j + r, it.n_ext - 1);
+      pb[j] = s.b + row * s.b_pitch + (int64_t)skip * NT_ROW + g * 16;
+      sb[j] = s.b_scale + row * s.b_scale_pitch + (int64_t)skip * 4;
+    }
+    auto multiply = [&](nt_i32x4 a, nt_i32x4 b, int as, int bs, nt_f32x4 c) {
+      const nt_i32x8 x = {b[0], b[1], b[2], b[3], 0, 0, 0, 0};
+      const nt_i32x8 y = {a[0], a[1], a[2], a[3], 0, 0, 0, 0};
+      return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, c, 4, 4, 0, (int)((unsigned)bs >> (8 * g)), 0, (int)((unsigned)as >> (8 * g)));
+    };
+    int t = wave * Q;
+    for (; t + Q <= n; t += 4 * Q) {
+      nt_i32x4 a[MT][Q], b[NT][Q], as[MT], bs[NT];
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        __builtin_memcpy(&bs[j], sb[j] + t * 4, 16);
+#pragma unroll
+        for (int q = 0; q < Q; ++q) b[j][q] = __builtin_nontemporal_load((const nt_i32x4 *)(pb[j] + (t + q) * NT_ROW));
+      }
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        __builtin_memcpy(&as[i], sa[i] + t * 4, 16);
+#pragma unroll
+        for (int q = 0; q < Q; ++q) a[i][q] = *(const nt_i32x4 *)(pa[i] + (t + q) * NT_ROW);
+      }
+#pragma unroll
+      for (int q = 0; q < Q; ++q)
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int j = 0; j < NT; ++j) acc[i][j] = multiply(a[i][q], b[j][q], as[i][q], bs[j][q], acc[i][j]);
+    }
+    // the last, incomplete 512 elements: one wave finds them
+    for (; t < n && t % Q == 0 && n - t < Q; ) {
+      for (; t < n; ++t)
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+            acc[i][j] = multiply(*(const nt_i32x4 *)(pa[i] + t * NT_ROW), *(const nt_i32x4 *)(pb[j] + t * NT_ROW), *(const int *)(sa[i] + t * 4),
+                                 *(const int *)(sb[j] + t * 4), acc[i][j]);
+    }
+    todo -= n;
+    skip = 0;
+  }
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) sums[wave][i * NT + j][lane] = acc[i][j];
+  __syncthreads();
+  for (int x = wave; x < MT * NT; x += 4) {
+    const nt_f32x4 v = ((sums[0][x][lane] + sums[1][x][lane]) + sums[2][x][lane]) + sums[3][x][lane];
+    // row r of A's tile x / NT, columns 4 g ... of B's tile x % NT
+    const int row = 16 * (x / NT) + r, col = 16 * (x % NT) + 4 * g;
+    if (row < it.m_ext) {
+#pragma unroll
+      for (int y = 0; y < 4; ++y)
+        if (col + y < it.n_ext) {
+          const int64_t at = (int64_t)row * it.ldc + col + y;
+          if (it.c_es == 4) ((float *)it.c)[at] = v[y];
+          else ((unsigned short *)it.c)[at] = mx_bf16(v[y]);
+        }
+    }
+  }
+}
+
+// ---- quantisation -----------------------------------------------------------------------------------
+
+typedef unsigned short mx_u16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 mx_bf16x2 __attribute__((ext_vector_type(2)));
+
+// Eight (2 N) neighbouring elements of a tile as they came: words of two bf16, or fp32.
+template <bool F32>
+struct MxVec {
+  static constexpr int WORDS = F32 ? 8 : 4;
+  unsigned w[WORDS];
+};
+
+// largest magnitude, as bits that compare like the values
+__device__ __forceinline__ unsigned mx_abs_max(const MxVec<true> &v) {
+  unsigned m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = max(m, v.w[i] & 0x7fffffffu);
+  return m;
+}
+__device__ __forceinline__ unsigned mx_abs_max(const MxVec<false> &v) {
+  mx_u16x2 m = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(mx_u16x2, v.w[i] & 0x7fff7fffu));
+  return (unsigned)max(m[0], m[1]) << 16;
+}
+// the scale's byte of a block whose largest magnitude has these bits
+__device__ __forceinline__ unsigned mx_scale(unsigned amax) {
+  const int e = (int)(amax >> 23);                            // 255: infinity or NaN; 0: below 2^-126
+  return e == 255 ? 255u : (unsigned)max(e - 2, 0);
+}
+// eight codes.  A scale of 2^-127 is no normal number: both sides 2^64 larger then.
+__device__ __forceinline__ unsigned mx_codes(const MxVec<true> &v, unsigned scale) {
+  if (scale == 255u) return 0;
+  unsigned r = 0;
+  if (scale == 0) {
+    const float s = __builtin_bit_cast(float, 64u << 23);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, ldexpf(__builtin_bit_cast(float, v.w[0]), 64), ldexpf(__builtin_bit_cast(float, v.w[1]), 64), s, 0);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, ldexpf(__builtin_bit_cast(float, v.w[2]), 64), ldexpf(__builtin_bit_cast(float, v.w[3]), 64), s, 1);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, ldexpf(__builtin_bit_cast(float, v.w[4]), 64), ldexpf(__builtin_bit_cast(float, v.w[5]), 64), s, 2);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, ldexpf(__builtin_bit_cast(float, v.w[6]), 64), ldexpf(__builtin_bit_cast(float, v.w[7]), 64), s, 3);
+    return r;
+  }
+  const float s = __builtin_bit_cast(float, scale << 23);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, __builtin_bit_cast(float, v.w[0]), __builtin_bit_cast(float, v.w[1]), s, 0);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, __builtin_bit_cast(float, v.w[2]), __builtin_bit_cast(float, v.w[3]), s, 1);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, __builtin_bit_cast(float, v.w[4]), __builtin_bit_cast(float, v.w[5]), s, 2);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, __builtin_bit_cast(float, v.w[6]), __builtin_bit_cast(float, v.w[7]), s, 3);
+  return r;
+}
+__device__ __forceinline__ unsigned mx_codes(const MxVec<false> &v, unsigned scale) {
+  if (scale == 0 || scale == 255u) {
+    MxVec<true> f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f.w[2 * i] = v.w[i] << 16;
+      f.w[2 * i + 1] = v.w[i] & 0xffff0000u;
+    }
+    return mx_codes(f, scale);
+  }
+  const float s = __builtin_bit_cast(float, scale << 23);
+  unsigned r = 0;
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(mx_bf16x2, v.w[0]), s, 0);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(mx_bf16x2, v.w[1]), s, 1);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(mx_bf16x2, v.w[2]), s, 2);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(mx_bf16x2, v.w[3]), s, 3);
+  return r;
+}
+
+// Eight elements of a row from column `col` on, zeros behind column w.  `wide`: rows are 16-byte aligned.
+template <bool F32>
+__device__ __forceinline__ MxVec<F32> mx_load8(const char *row, int col, int w, bool wide) {
+  MxVec<F32> v;
+  if (wide && col + 8 <= w) {
+    const nt_i32x4 *p = (const nt_i32x4 *)(row + (int64_t)col * (F32 ? 4 : 2));
+    const nt_i32x4 x = p[0];
+    v.w[0] = x[0], v.w[1] = x[1], v.w[2] = x[2], v.w[3] = x[3];
+    if constexpr (F32) {
+      const nt_i32x4 y = p[1];
+      v.w[4] = y[0], v.w[5] = y[1], v.w[6] = y[2], v.w[7] = y[3];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < MxVec<F32>::WORDS; ++i) {
+      if constexpr (F32) {
+        v.w[i] = col + i < w ? ((const unsigned *)row)[col + i] : 0u;
+      } else {
+        const unsigned lo = col + 2 * i < w ? ((const unsigned short *)row)[col + 2 * i] : 0u;
+        const unsigned hi = col + 2 * i + 1 < w ? ((const unsigned short *)row)[col + 2 * i + 1] : 0u;
+        v.w[i] = lo | hi << 16;
+      }
+    }
+  }
+  return v;
+}
+
+// the largest of four neighbouring lanes
+__device__ __forceinline__ unsigned mx_max4(unsigned v) {
+  v = max(v, (unsigned)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xF, 0xF, true));   // lane ^ 1
+  return max(v, (unsigned)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xF, 0xF, true));   // lane ^ 2
+}
+
+// the tile that workgroup `block` belongs to, and the workgroup's number inside it
+__device__ __forceinline__ const MxTile &mx_find(const MxTileArgs &args, int block, int *inside) {
+  int x = 0;
+  while (x + 1 < args.n && block >= args.tile[x + 1].first_block) ++x;
+  *inside = block - args.tile[x].first_block;
+  return args.tile[x];
+}
+
+// Along the rows alone: a wave takes 512 columns of R rows, all loads first.
+template <bool F32, int R>
+__global__ __launch_bounds__(256) void mx_rows_kernel(MxTileArgs) {
+  const auto &args = *(const MxTileArgs *)__builtin_amdgcn_kernarg_segment_ptr();
+  int block;
+  const MxTile &T = mx_find(args, blockIdx.x, &block);
+  const int lane = threadIdx.x & 63;
+  const int unit = block * 4 + (threadIdx.x >> 6), across = T.blocks_across;   // 512-column pieces of a row
+  const int col = (unit % across) * 512 + lane * 8, row0 = unit / across * R;
+  const int wide_cols = (T.w + 127) & ~127;
+  if (col >= wide_cols) return;
+  MxVec<F32> v[R];
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+    if (row0 + i < T.h) v[i] = mx_load8<F32>((const char *)T.x + (int64_t)(row0 + i) * T.x_pitch, col, T.w, T.wide);
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+    if (row0 + i < T.h) {
+      const unsigned scale = mx_scale(mx_max4(mx_abs_max(v[i])));
+      *(unsigned *)(T.row_codes + (int64_t)(row0 + i) * T.row_pitch + col / 2) = mx_codes(v[i], scale);
+      if ((lane & 3) == 0) T.row_scales[(int64_t)(row0 + i) * T.row_scale_pitch + col / 32] = (unsigned char)scale;
+    }
+}
+
+// Along the columns, and along the rows too if ROWS: a workgroup takes 128 rows of 128 columns, reads them along
+// the rows and leaves them in LDS, where each thread then finds its 32 rows of two columns.  Four threads make
+// the 64 bytes of a column's 128 codes.
+template <bool F32, bool ROWS>
+__global__ __launch_bounds__(256) void mx_cols_kernel(MxTileArgs) {
+  constexpr int ES = F32 ? 4 : 2;
+  constexpr int PITCH = 128 * ES + 4;                         // bytes (one word more: rows start in other banks)
+  extern __shared__ char lds[];
+  const auto &args = *(const MxTileArgs *)__builtin_amdgcn_kernarg_segment_ptr();
+  int block;
+  const MxTile &T = mx_find(args, blockIdx.x, &block);
+  const int col0 = (block % T.blocks_across) * 128, row0 = block / T.blocks_across * 128;
+  const int tid = threadIdx.x;
+  {
+    const int col = col0 + (tid & 15) * 8;
+#pragma unroll
+    for (int pass = 0; pass < 8; pass += 4) {
+      MxVec<F32> v[4];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const int row = row0 + (pass + x) * 16 + (tid >> 4);
+        v[x] = row < T.h ? mx_load8<F32>((const char *)T.x + (int64_t)row * T.x_pitch, col, T.w, T.wide) : MxVec<F32>{};
+      }
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const int r = (pass + x) * 16 + (tid >> 4);
+        unsigned *p = (unsigned *)(lds + r * PITCH + (tid & 15) * 8 * ES);
+#pragma unroll
+        for (int i = 0; i < MxVec<F32>::WORDS; ++i) p[i] = v[x].w[i];
+        if constexpr (ROWS) {
+          const unsigned scale = mx_scale(mx_max4(mx_abs_max(v[x])));
+          if (row0 + r < T.h) {
+            *(unsigned *)(T.row_codes + (int64_t)(row0 + r) * T.row_pitch + col / 2) = mx_codes(v[x], scale);
+            if ((tid & 3) == 0) T.row_scales[(int64_t)(row0 + r) * T.row_scale_pitch + col / 32] = (unsigned char)scale;
+          }
+        }
+      }
+    }
+  }
+  __syncthreads();
+  // thread: rows 32 b ..., columns 2 p and 2 p + 1
+  const int b = tid & 3, p = tid >> 2;
+  unsigned words[2][F32 ? 32 : 16];                           // the two columns: 32 fp32, or 32 bf16 in pairs
+#pragma unroll
+  for (int i = 0; i < 32; i += 2) {
+    const char *q = lds + (32 * b + i) * PITCH + p * 2 * ES;
+    if constexpr (F32) {
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        words[c][i] = *(const unsigned *)(q + 4 * c);
+        words[c][i + 1] = *(const unsigned *)(q + PITCH + 4 * c);
+      }
+    } else {
+      const unsigned x = *(const unsigned *)q, y = *(const unsigned *)(q + PITCH);
+      words[0][i / 2] = __builtin_amdgcn_perm(y, x, 0x05040100);   // low halves
+      words[1][i / 2] = __builtin_amdgcn_perm(y, x, 0x07060302);   // high halves
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const int col = col0 + 2 * p + c;
+    MxVec<F32> v[4];
+    unsigned amax = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+#pragma unroll
+      for (int i = 0; i < MxVec<F32>::WORDS; ++i) v[k].w[i] = words[c][k * MxVec<F32>::WORDS + i];
+      amax = max(amax, mx_abs_max(v[k]));
+    }
+    if (col < T.w) {
+      const unsigned scale = mx_scale(amax);
+      nt_i32x4 codes;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) codes[k] = (int)mx_codes(v[k], scale);
+      *(nt_i32x4 *)(T.col_codes + (int64_t)col * T.col_pitch + (row0 / 32 + b) * 16) = codes;
+      T.col_scales[(int64_t)col * T.col_scale_pitch + row0 / 32 + b] = (unsigned char)scale;
+    }
+  }
+}
+
+// ---- values -------------------------------------------------------------------------------------------
+
+// Eight values of a block as they are stored in the tile.
+template <bool F32>
+__device__ __forceinline__ MxVec<F32> mx_values(unsigned codes, unsigned scale) {
+  typedef float f2 __attribute__((ext_vector_type(2)));
+  const int e = (int)scale - 127;
+  float f[8];
+  const f2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.f, 1);
+  const f2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.f, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.f, 3);
+  f[0] = a[0], f[1] = a[1], f[2] = b[0], f[3] = b[1], f[4] = c[0], f[5] = c[1], f[6] = d[0], f[7] = d[1];
+  MxVec<F32> v;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    // (bf16 holds every such value: two significant bits, 2^-128 at least)
+    const unsigned bits = scale == 255u ? 0x7fc00000u : __builtin_bit_cast(unsigned, ldexpf(f[i], e));
+    if constexpr (F32) v.w[i] = bits;
+    else if (i & 1) v.w[i / 2] |= bits & 0xffff0000u;
+    else v.w[i / 2] = bits >> 16;
+  }
+  return v;
+}
+template <bool F32>
+__device__ __forceinline__ void mx_store8(char *row, int col, int w, bool wide, const MxVec<F32> &v) {
+  if (wide && col + 8 <= w) {
+    nt_i32x4 *p = (nt_i32x4 *)(row + (int64_t)col * (F32 ? 4 : 2));
+    p[0] = nt_i32x4{(int)v.w[0], (int)v.w[1], (int)v.w[2], (int)v.w[3]};
+    if constexpr (F32) p[1] = nt_i32x4{(int)v.w[4], (int)v.w[5], (int)v.w[6], (int)v.w[7]};
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (col + i < w) {
+        if constexpr (F32) ((unsigned *)row)[col + i] = v.w[i];
+        else ((unsigned short *)row)[col + i] = (unsigned short)(v.w[i / 2] >> (16 * (i & 1)));
+      }
+  }
+}
+
+template <bool F32, int R>
+__global__ __launch_bounds__(256) void mx_row_values_kernel(MxTileArgs) {
+  const auto &args = *(const MxTileArgs *)__builtin_amdgcn_kernarg_segment_ptr();
+  int block;
+  const MxTile &T = mx_find(args, blockIdx.x, &block);
+  const int lane = threadIdx.x & 63;
+  const int unit = block * 4 + (threadIdx.x >> 6), across = T.blocks_across;
+  const int col = (unit % across) * 512 + lane * 8, row0 = unit / across * R;
+  if (col >= T.w) return;
+  unsigned codes[R], scale[R];
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+    if (row0 + i < T.h) {
+      codes[i] = *(const unsigned *)(T.row_codes + (int64_t)(row0 + i) * T.row_pitch + col / 2);
+      scale[i] = T.row_scales[(int64_t)(row0 + i) * T.row_scale_pitch + col / 32];
+    }
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+    if (row0 + i < T.h) mx_store8<F32>((char *)T.x + (int64_t)(row0 + i) * T.x_pitch, col, T.w, T.wide, mx_values<F32>(codes[i], scale[i]));
+}
+
+// 128 rows of 128 columns, turned through LDS the other way.
+template <bool F32>
+__global__ __launch_bounds__(256) void mx_col_values_kernel(MxTileArgs) {
+  constexpr int ES = F32 ? 4 : 2;
+  constexpr int PITCH = 128 * ES + 4;
+  extern __shared__ char lds[];
+  const auto &args = *(const MxTileArgs *)__builtin_amdgcn_kernarg_segment_ptr();
+  int block;
+  const MxTile &T = mx_find(args, blockIdx.x, &block);
+  const int col0 = (block % T.blocks_across) * 128, row0 = block / T.blocks_across * 128;
+  const int tid = threadIdx.x, b = tid & 3, p = tid >> 2;
+  nt_i32x4 codes[2];
+  unsigned scale[2];
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const int col = min(col0 + 2 * p + c, T.w - 1);
+    codes[c] = *(const nt_i32x4 *)(T.col_codes + (int64_t)col * T.col_pitch + (row0 / 32 + b) * 16);
+    scale[c] = T.col_scales[(int64_t)col * T.col_scale_pitch + row0 / 32 + b];
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const MxVec<F32> x = mx_values<F32>((unsigned)codes[0][k], scale[0]), y = mx_values<F32>((unsigned)codes[1][k], scale[1]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      char *q = lds + (32 * b + 8 * k + i) * PITCH + p * 2 * ES;
+      if constexpr (F32) {
+        *(unsigned *)q = x.w[i];
+        *(unsigned *)(q + 4) = y.w[i];
+      } else {
+        *(unsigned *)q = __builtin_amdgcn_perm(y.w[i / 2], x.w[i / 2], i & 1 ? 0x07060302 : 0x05040100);
+      }
+    }
+  }
+  __syncthreads();
+  const int col = col0 + (tid & 15) * 8;
+#pragma unroll
+  for (int pass = 0; pass < 8; ++pass) {
+    const int r = pass * 16 + (tid >> 4);
+    if (row0 + r >= T.h) continue;
+    MxVec<F32> v;
+    const unsigned *q = (const unsigned *)(lds + r * PITCH + (tid & 15) * 8 * ES);
+#pragma unroll
+    for (int i = 0; i < MxVec<F32>::WORDS; ++i) v.w[i] = q[i];
+    mx_store8<F32>((char *)T.x + (int64_t)(row0 + r) * T.x_pitch, col, T.w, T.wide, v);
+  }
+}
+
+}  // namespace dmm

@@ -1,0 +1,378 @@
+"""GPU tests of the 4-bit microscaled matrices: codes, scales and values byte for byte against the
+oracle, products against the oracle's values multiplied in 64 bits."""
+import numpy as np
+import pytest
+
+import workloads
+from oracle import mx as oracle
+
+torch = pytest.importorskip("torch")
+binding = pytest.importorskip("paper_2510_08874_amd.binding")
+pytestmark = pytest.mark.gpu
+
+GUARD = 0xA5
+DT = {"bf16": (torch.bfloat16, 1), "f32": (torch.float32, 2)}
+
+
+class Form:
+    """Buffers of one form of a matrix, filled with a guard byte, rows longer than they have to be."""
+
+    def __init__(self, d, along, more=0):
+        self.d, self.along, self.codes, self.scales, self.size = d, along, [], [], []
+        for _ in range(d["replication"]):
+            for r0, r1 in zip(d["row_cuts"], d["row_cuts"][1:]):
+                for c0, c1 in zip(d["col_cuts"], d["col_cuts"][1:]):
+                    h, w = (r1 - r0, c1 - c0) if along == 1 else (c1 - c0, r1 - r0)
+                    chunks = -(-w // 128)
+                    self.size.append((h, w, chunks))
+                    empty = h == 0 or w == 0
+                    self.codes.append(None if empty else torch.full((h, 64 * chunks + 16 * more), GUARD, dtype=torch.uint8, device="cuda"))
+                    self.scales.append(None if empty else torch.full((h, 4 * chunks + 4 * more), GUARD, dtype=torch.uint8, device="cuda"))
+
+    def table(self):
+        return binding.mx_tiles(self.codes, [0 if c is None else c.shape[1] for c in self.codes], self.scales, [0 if s is None else s.shape[1] for s in self.scales])
+
+
+def tiles_of(x, d, dtype, ld_more=0, offset=0):
+    """Every tile a buffer of its own, `offset` elements into an allocation, rows `ld_more` elements longer; the rest NaN."""
+    out, ld = [], []
+    for _ in range(d["replication"]):
+        for r0, r1 in zip(d["row_cuts"], d["row_cuts"][1:]):
+            for c0, c1 in zip(d["col_cuts"], d["col_cuts"][1:]):
+                h, w = r1 - r0, c1 - c0
+                ld.append(w + ld_more)
+                if h == 0 or w == 0:
+                    out.append(None)
+                    continue
+                buf = torch.full((h * (w + ld_more) + offset,), float("nan"), dtype=dtype, device="cuda")
+                t = buf[offset:].view(h, w + ld_more)
+                t[:, :w] = x[r0:r1, c0:c1].to(dtype)
+                out.append(t)
+    return out, ld
+
+
+def bounds(d):
+    return [(r0, r1, c0, c1) for _ in range(d["replication"]) for r0, r1 in zip(d["row_cuts"], d["row_cuts"][1:])
+            for c0, c1 in zip(d["col_cuts"], d["col_cuts"][1:])]
+
+
+def check_form(form, x):
+    """Codes and scales of every tile, zeros to the end of the last chunk, the guard behind it."""
+    for (h, w, chunks), (r0, r1, c0, c1), codes, scales in zip(form.size, bounds(form.d), form.codes, form.scales):
+        if codes is None:
+            continue
+        t = x[r0:r1, c0:c1]
+        want_codes, want_scales = oracle.quantize(t if form.along == 1 else t.T)
+        got_codes, got_scales = codes.cpu().numpy(), scales.cpu().numpy()
+        bad = np.repeat(want_scales == 255, 32, axis=1)      # codes of blocks without a scale are anything
+        assert np.array_equal(got_scales[:, :4 * chunks], want_scales)
+        assert np.array_equal(np.where(bad, 0, oracle.unpack(got_codes[:, :64 * chunks])), np.where(bad, 0, want_codes))
+        assert (got_codes[:, 64 * chunks:] == GUARD).all() and (got_scales[:, 4 * chunks:] == GUARD).all()
+
+
+def quantize(d, x, dtype, forms=(1, 2), more=0, ld_more=0, offset=0):
+    tdt, code = DT[dtype]
+    xt, ld = tiles_of(x, d, tdt, ld_more, offset)
+    made = {f: Form(d, f, more) for f in forms}
+    tables = {f: m.table() for f, m in made.items()}
+    binding.dmm_mx_quantize(binding.matrix_desc(d), code, binding.tile_table(xt, ld), rows=tables.get(1), cols=tables.get(2),
+                            stream=torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    return made
+
+
+def whole(h, w):
+    return workloads.desc(h, w, [0, h], [0, w], 1, 1)
+
+
+def test_every_bf16_value_at_every_place_of_the_scale():
+    """Blocks that hold one bf16 value 31 times beside a largest one: all values against several exponents."""
+    bits = torch.arange(1 << 16, dtype=torch.int32).to(torch.int16).view(torch.bfloat16).cuda()
+    x = bits.float().repeat(1, 1).reshape(2048, 32)          # 32 neighbouring values a block
+    check_form(quantize(whole(2048, 32), x, "bf16", forms=(1,))[1], x.cpu().double().numpy())
+    # one value against a block maximum of the same exponent and up to four above it
+    vals = bits[(bits.float().abs() > 2.0 ** -100) & (bits.float().abs() < 2.0 ** 100)].float()
+    for up in range(5):
+        y = torch.zeros(len(vals), 32, device="cuda")
+        y[:, 1] = vals
+        y[:, 30] = torch.exp2(torch.floor(torch.log2(vals.abs())) + up)
+        y = y.bfloat16().float()
+        check_form(quantize(whole(len(vals), 32), y, "bf16", forms=(1,))[1], y.cpu().double().numpy())
+
+
+def test_fp32_values_next_to_the_borders():
+    """Half-way values of every code and their fp32 neighbours, in blocks of several exponents, largest and smallest included."""
+    half = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 7.0], dtype=torch.float32)
+    near = torch.cat([half, torch.nextafter(half, half * 0), torch.nextafter(half, half * 9)])
+    rows = []
+    for e in (-149, -140, -130, -127, -126, -125, -100, -1, 0, 1, 60, 124, 125):
+        row = torch.zeros(32, dtype=torch.float64)
+        row[:24] = near.double() * 2.0 ** e
+        row[25] = 4.0 * 2.0 ** e
+        rows += [row, -row]
+    x = torch.stack(rows).float().cuda()
+    for forms, y in (((1,), x), ((2,), x.T.contiguous())):
+        made = quantize(whole(*y.shape), y, "f32", forms=forms)
+        check_form(made[forms[0]], y.cpu().double().numpy())
+
+
+def test_infinities_and_nan_stay_in_their_block():
+    for dtype in ("bf16", "f32"):
+        g = torch.Generator(device="cuda").manual_seed(3)
+        x = torch.randn(96, 160, generator=g, device="cuda").to(DT[dtype][0]).float()
+        x[5, 40], x[6, 3], x[70, 159], x[33, 64:96] = float("inf"), float("nan"), float("-inf"), 0.0
+        x[40, :] = 0.0
+        made = quantize(whole(96, 160), x, dtype)
+        xd = x.cpu().double().numpy()
+        check_form(made[1], xd)
+        check_form(made[2], xd)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("h,w,more,ld_more,offset", [
+    (1, 1, 0, 0, 0), (1, 32, 0, 0, 0), (1, 4097, 1, 0, 0), (31, 33, 0, 1, 1), (128, 128, 0, 0, 0), (129, 127, 2, 8, 8),
+    (257, 640, 0, 3, 0), (640, 257, 1, 0, 3), (1000, 1, 0, 0, 0), (33, 8200, 0, 0, 0),
+], ids=str)
+def test_forms_of_a_tile(dtype, h, w, more, ld_more, offset):
+    g = torch.Generator(device="cuda").manual_seed(h * 131 + w)
+    x = torch.randn(h, w, generator=g, device="cuda") * torch.exp2(torch.randint(-30, 30, (h, 1), generator=g, device="cuda").float())
+    x = x.to(DT[dtype][0]).float()
+    xd = x.cpu().double().numpy()
+    for forms in ((1, 2), (1,), (2,)):
+        made = quantize(whole(h, w), x, dtype, forms, more, ld_more, offset)
+        for f in forms:
+            check_form(made[f], xd)
+            # and back
+            out, ld = tiles_of(torch.zeros(h, w, device="cuda"), whole(h, w), DT[dtype][0], ld_more, offset)
+            binding.dmm_mx_dequantize(binding.matrix_desc(whole(h, w)), made[f].table(), f, DT[dtype][1], binding.tile_table(out, ld),
+                                      torch.cuda.current_stream().cuda_stream)
+            got = out[0].float().cpu().numpy()
+            codes, scales = oracle.quantize(xd if f == 1 else xd.T)
+            want = oracle.values(codes, scales, w if f == 1 else h)
+            assert np.array_equal(got[:, :w], want if f == 1 else want.T)
+            assert np.isnan(got[:, w:]).all()
+
+
+def test_many_tiles_and_replicas():
+    """More tiles than a launch takes at once, empty ones among them; every replica from its own tiles."""
+    d = workloads.desc(300, 700, [0, 0, 7, 7, 130, 300], [0, 1, 33, 33, 170, 300, 431, 560, 700], 5, 8, replication=2)
+    g = torch.Generator(device="cuda").manual_seed(9)
+    x = torch.randn(300, 700, generator=g, device="cuda").bfloat16().float()
+    made = quantize(d, x, "bf16")
+    for f in (1, 2):
+        check_form(made[f], x.cpu().double().numpy())
+
+
+def test_values_of_the_smallest_and_largest_scales_and_of_nan():
+    scales = torch.tensor([[0, 1, 127, 252, 255, 254, 0, 0]], dtype=torch.uint8, device="cuda")
+    codes = torch.randint(0, 256, (1, 128), generator=torch.Generator().manual_seed(4), dtype=torch.int64).to(torch.uint8).cuda()
+    codes[0, 80:96] = 0x21                                  # (below 2: larger values times 2^127 are beyond fp32)
+    for dtype in ("bf16", "f32"):
+        out = torch.zeros(1, 256, dtype=DT[dtype][0], device="cuda")
+        binding.dmm_mx_dequantize(binding.matrix_desc(whole(1, 256)), binding.mx_tiles([codes], [128], [scales], [8]), 1, DT[dtype][1],
+                                  binding.tile_table([out], [256]), torch.cuda.current_stream().cuda_stream)
+        want = oracle.values(oracle.unpack(codes.cpu().numpy()), scales.cpu().numpy(), 256)
+        assert np.array_equal(out.double().cpu().numpy(), want, equal_nan=True)
+
+
+# ---- products -----------------------------------------------------------------------------------------
+
+def operand(d, along, seed, spread=3):
+    """Random codes and scales in every tile (the same in every replica), and the matrix that they stand for."""
+    form, rng = Form(d, along), np.random.default_rng(seed)
+    X = np.zeros((d["rows"], d["cols"]))
+    per = len(bounds(d)) // d["replication"]
+    for i, ((h, w, chunks), (r0, r1, c0, c1)) in enumerate(zip(form.size, bounds(d))):
+        if form.codes[i] is None:
+            continue
+        if i >= per:
+            form.codes[i].copy_(form.codes[i - per])
+            form.scales[i].copy_(form.scales[i - per])
+            continue
+        code = rng.integers(0, 16, (h, chunks * 128), dtype=np.uint8)
+        code[:, w:] = 0
+        scale = rng.integers(127 - spread, 128 + spread, (h, chunks * 4), dtype=np.uint8)
+        scale[:, -(-w // 32):] = 0
+        form.codes[i].copy_(torch.from_numpy(oracle.pack(code)))
+        form.scales[i].copy_(torch.from_numpy(scale))
+        v = oracle.values(code, scale, w)
+        X[r0:r1, c0:c1] = v if along == 1 else v.T
+    return form, X
+
+
+def gather(tiles, d, rep=0):
+    per = len(bounds(d)) // d["replication"]
+    out = np.zeros((d["rows"], d["cols"]))
+    for t, (r0, r1, c0, c1) in zip(tiles[rep * per:], bounds(d)[:per]):
+        if t is not None:
+            out[r0:r1, c0:c1] = t[:, :c1 - c0].float().cpu().numpy()
+    return out
+
+
+def multiply(da, db, dc, nranks, plan_flags=0, flags=0, c_dtype="f32", ld_more=0, offset=0, seed=1, plan=None, spread=3):
+    a, A = operand(da, 1, seed, spread)
+    b, B = operand(db, 2, seed + 1, spread)
+    c, ld = tiles_of(torch.full((dc["rows"], dc["cols"]), float("nan"), device="cuda"), dc, DT[c_dtype][0], ld_more, offset)
+    plan = plan or binding.Plan(da, db, dc, nranks, plan_flags)
+    plan.execute_mx(a.table(), b.table(), binding.tile_table(c, ld), flags | (binding.DMM_C_BF16 if c_dtype == "bf16" else 0),
+                    torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    for t, (_, _, c0, c1) in zip(c, bounds(dc)):
+        assert t is None or torch.isnan(t[:, c1 - c0:]).all(), "written behind a row's end"
+    return c, A, B
+
+
+def limit(A, B, c_dtype, terms):
+    """How far a product may be off: every term is exact in fp32, and so is a sum of a few of them; each of the
+    additions (of terms inside a matrix instruction, of instructions, of partial sums: no more than there are terms)
+    rounds by half a step, 2^-24, of a sum no larger than that of all magnitudes.  A rounding to bf16 adds 2^-8 of it."""
+    S = np.abs(A) @ np.abs(B)
+    out = terms * 2.0 ** -24 * S
+    if c_dtype == "bf16":
+        out = out + 2.0 ** -8 * (np.abs(A @ B) + out)
+    return out + 1e-300
+
+
+def block(*a, **k):
+    return workloads.block_desc(*a, **k)
+
+
+SHAPES = [(1, 1, 1), (1, 128, 1), (1, 129, 16), (3, 4096, 100), (16, 640, 513), (17, 1000, 33), (33, 2048, 65), (64, 513, 1000), (65, 128, 65),
+          (128, 384, 128), (130, 1153, 255), (257, 512, 300), (1, 20000, 48), (100, 9000, 70)]
+
+
+@pytest.mark.parametrize("c_dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,k,n", SHAPES, ids=str)
+def test_product_of_single_tiles(m, k, n, c_dtype):
+    ld_more, offset = (0, 0) if (m + n) % 2 else (3, 1)
+    c, A, B = multiply(whole(m, k), whole(k, n), whole(m, n), 1, c_dtype=c_dtype, ld_more=ld_more, offset=offset, seed=m + k + n)
+    err = np.abs(gather(c, whole(m, n)) - A @ B)
+    assert (err <= limit(A, B, c_dtype, k)).all()
+
+
+def test_product_on_large_macro_tiles():
+    m, k, n = 4100, 700, 3800
+    c, A, B = multiply(block(m, k, 4, 1), block(k, n, 1, 4), block(m, n, 2, 2), 4, seed=7)
+    assert (np.abs(gather(c, block(m, n, 2, 2)) - A @ B) <= limit(A, B, "f32", k)).all()
+
+
+def uneven(m, k, n):
+    return (workloads.desc(m, k, [0, m // 5, m // 2, m], [0, 128, 128, 512, k], 3, 4), workloads.desc(k, n, [0, 256, 384, k], [0, n // 3, n], 3, 2),
+            workloads.desc(m, n, [0, m // 7, m // 3, m - 1, m], [0, 0, n // 2, n], 4, 3))
+
+
+@pytest.mark.parametrize("stationary", ["C", "B", "A"])
+@pytest.mark.parametrize("m,k,n", [(61, 700, 77), (301, 1000, 259), (700, 640, 611)], ids=str)
+def test_product_of_uneven_tiles(m, k, n, stationary):
+    d = uneven(m, k, n)
+    c, A, B = multiply(*d, 12, plan_flags=binding.STATIONARY_FLAGS[stationary], seed=m)
+    assert (np.abs(gather(c, d[2]) - A @ B) <= limit(A, B, "f32", k)).all()
+
+
+@pytest.mark.parametrize("stationary,m,k,n", [("C", 500, 1024, 300), ("C", 40, 512, 300), ("B", 256, 512, 300), ("A", 300, 256, 256)], ids=str)
+def test_replicated_product(stationary, m, k, n):
+    """Every replica holds its partial sum, replica 0 the sum of all; Stationary B and A leave regions that no op of a replica writes."""
+    d = [block(m, k, 2, 2, replication=2), block(k, n, 2, 2, replication=2), block(m, n, 2, 2, replication=2)]
+    plan = binding.Plan(*d, 8, binding.STATIONARY_FLAGS[stationary])
+    c, A, B = multiply(*d, 8, flags=binding.DMM_NO_REDUCE, plan=plan, seed=11)
+    parts = [gather(c, d[2], r) for r in range(2)]
+    lim = limit(A, B, "f32", k)
+    assert (np.abs(parts[0] + parts[1] - A @ B) <= lim).all()
+    assert np.abs(parts[1]).max() > 0
+    c, _, _ = multiply(*d, 8, plan=plan, seed=11)
+    assert (np.abs(gather(c, d[2], 0) - A @ B) <= lim).all()
+    assert np.array_equal(gather(c, d[2], 1), parts[1])
+
+
+def test_scales_far_apart_and_blocks_that_are_nan():
+    m, k, n = 70, 512, 90
+    c, A, B = multiply(whole(m, k), whole(k, n), whole(m, n), 1, seed=5, spread=40)
+    assert (np.abs(gather(c, whole(m, n)) - A @ B) <= limit(A, B, "f32", k)).all()
+    for rows in (m, 8):
+        a, A = operand(whole(rows, k), 1, 5)
+        b, B = operand(whole(k, n), 2, 6)
+        a.scales[0][3, 7] = 255
+        b.scales[0][n - 1, 0] = 255
+        out = torch.zeros(rows, n, device="cuda")
+        binding.Plan(whole(rows, k), whole(k, n), whole(rows, n), 1).execute_mx(a.table(), b.table(), binding.tile_table([out], [n]),
+                                                                             stream=torch.cuda.current_stream().cuda_stream)
+        got = torch.isnan(out).cpu().numpy()
+        want = np.zeros((rows, n), bool)
+        want[3, :] = want[:, n - 1] = True
+        assert np.array_equal(got, want)
+        ok = ~want
+        assert (np.abs(out.cpu().numpy() - A @ B)[ok] <= limit(A, B, "f32", k)[ok]).all()
+
+
+def test_results_are_the_same_every_time_and_a_layer_is_trained_with_both_forms():
+    """Quantisation, C = A B, dA = dC B^T and dB = A^T dC of one layer in 2 x 2 blocks, against the oracle; twice, bit for bit."""
+    m, k, n = 300, 390, 520
+    cut = lambda x: [0, 256, x]
+    desc = lambda r, c: workloads.desc(r, c, cut(r), cut(c), 2, 2)
+    g = torch.Generator(device="cuda").manual_seed(21)
+    mats = [torch.randn(r, c, generator=g, device="cuda").bfloat16().float() for r, c in ((m, k), (k, n), (m, n))]
+    ds = [desc(*x.shape) for x in mats]
+    stream = torch.cuda.current_stream().cuda_stream
+
+    def turned(form):
+        gr, gc = len(form.d["row_cuts"]) - 1, len(form.d["col_cuts"]) - 1
+        at = [i * gc + j for j in range(gc) for i in range(gr)]
+        return binding.mx_tiles([form.codes[i] for i in at], [form.codes[i].shape[1] for i in at], [form.scales[i] for i in at],
+                                [form.scales[i].shape[1] for i in at])
+
+    runs = []
+    for _ in range(2):
+        q = [quantize(d, x, "bf16") for d, x in zip(ds, mats)]
+        got = []
+        for descs, left, right, d in (((ds[0], ds[1], ds[2]), q[0][1].table(), q[1][2].table(), ds[2]),
+                                      ((ds[2], desc(n, k), ds[0]), q[2][1].table(), turned(q[1][1]), ds[0]),
+                                      ((desc(k, m), ds[2], ds[1]), turned(q[0][2]), q[2][2].table(), ds[1])):
+            c, ld = tiles_of(torch.zeros(d["rows"], d["cols"], device="cuda"), d, torch.float32)
+            binding.Plan(*descs, 4).execute_mx(left, right, binding.tile_table(c, ld), stream=stream)
+            got.append(gather(c, d))
+        runs.append(got)
+    assert all(np.array_equal(x, y) for x, y in zip(*runs))
+
+    def along(x, d, axis):
+        out = np.zeros(x.shape)
+        for r0, r1, c0, c1 in bounds(d):
+            t = x[r0:r1, c0:c1]
+            codes, scales = oracle.quantize(t if axis == 1 else t.T)
+            v = oracle.values(codes, scales, t.shape[axis == 1])
+            out[r0:r1, c0:c1] = v if axis == 1 else v.T
+        return out
+
+    xs = [x.cpu().double().numpy() for x in mats]
+    rows, cols = [along(x, d, 1) for x, d in zip(xs, ds)], [along(x, d, 2) for x, d in zip(xs, ds)]
+    for c, (A, B) in zip(runs[0], ((rows[0], cols[1]), (rows[2], rows[1].T), (cols[0].T, cols[2]))):
+        assert (np.abs(c - A @ B) <= limit(A, B, "f32", A.shape[1])).all()
+
+
+def test_other_streams_and_a_captured_graph():
+    m, k, n = 100, 9000, 70                                  # cut along K: partial sums in the plan's scratch buffer
+    plan = binding.Plan(whole(m, k), whole(k, n), whole(m, n), 1)
+    a, A = operand(whole(m, k), 1, 3)
+    b, B = operand(whole(k, n), 2, 4)
+    ta, tb = a.table(), b.table()
+    out = torch.zeros(m, n, device="cuda")
+    tc = binding.tile_table([out], [n])
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    plan.execute_mx(ta, tb, tc, stream=side.cuda_stream)
+    side.synchronize()
+    want = out.clone()
+    assert (np.abs(want.cpu().numpy() - A @ B) <= limit(A, B, "f32", k)).all()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side, capture_error_mode="relaxed"):
+        plan.execute_mx(ta, tb, tc, stream=side.cuda_stream)
+    for _ in range(3):
+        out.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+        out.zero_()
+        plan.execute_mx(ta, tb, tc, stream=torch.cuda.current_stream().cuda_stream)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+    del graph
