@@ -44,8 +44,8 @@ typedef enum {
   DMM_ELD = -6,    /* a leading dimension is smaller than the tile's width, or a row pitch (leading
                       dimension times element size) of an A, B or C tile is 2^24 bytes or more */
   DMM_ELIMIT = -7  /* dmm_reduce_replicas_static: the work tables of this call do not fit the library's
-                      static device buffer (DMM_STATIC_SCRATCH_BYTES); dmm_mx_*: more than 2^30 workgroups or table
-                      entries */
+                      static device buffer (DMM_STATIC_SCRATCH_BYTES); dmm_mx_*, dmm_orthogonalize: more
+                      than 2^30 workgroups or table entries, a workspace that is too small */
 } dmm_status;
 
 /* Element type of the A and B tiles.  All partial sums are fp32, and so are the C tiles unless
@@ -333,6 +333,28 @@ int dmm_mx_dequantize(const dmm_matrix_desc *X, const dmm_mx_tiles *q, int along
 int dmm_mx_execute(dmm_plan_t *p, const dmm_mx_tiles *a, const dmm_mx_tiles *b, void *const *c_tiles, const int64_t *c_ld,
                    uint32_t flags, void *hip_stream);
 
+/* ---- orthogonalised updates --------------------------------------------------------------------
+ *
+ * Brings all singular values of `count` matrices of one shape and one tile grid near 1, as optimisers do with a weight's
+ * momentum before they apply it:
+ *   X = G / |G|  (Frobenius norm; a matrix of zeros stays zero, one with an infinity or a NaN comes out as NaN)
+ *   `steps` times:  S = X X^T,  X = a X + (b S + c S S) X       (with X^T in X's place where G has more rows than columns)
+ * coefficients: host, a, b, c of every step; null: (3.4445, -4.7750, 2.0315) for up to 5 steps, 5 of which take singular values from
+ * 0.002 |G| up to between 0.68 and 1.21.  Coefficients that let a singular value, or an eigenvalue of b S + c S S, pass
+ * 15 on the way are refused (DMM_EINVAL).
+ * Tables of the tiles: matrix * (grid_rows * grid_cols) + ti * grid_cols + tj; the descriptor's replication is 1 (DMM_EREPL).
+ * Elements bf16 or fp32 on either side; leading dimensions in elements.  Y may be X if both have the same type.
+ * Products are of pairs of fp16 numbers, 22 bits of a value, with fp32 sums: an fp32 result is off by no more than fp32
+ * products would leave it, a bf16 result is that rounded once.
+ * The workspace (device memory, aligned to 256 bytes, dmm_orthogonalize_workspace tells how much: DMM_ELIMIT if there is
+ * less) is the caller's: nothing else is allocated and nothing kept, so calls with workspaces of their own may overlap on any streams
+ * and be captured; calls that share one have to follow each other, replays of graphs included.  Sums are cut in a way that
+ * depends on the shape and the count alone.  A dimension is 2^20 at most (DMM_ELIMIT). */
+int dmm_orthogonalize_workspace(const dmm_matrix_desc *X, int32_t count, int64_t *bytes);
+int dmm_orthogonalize(const dmm_matrix_desc *X, int32_t count, int x_dtype, const void *const *x_tiles, const int64_t *x_ld,
+                      int y_dtype, void *const *y_tiles, const int64_t *y_ld, const float *coefficients, int32_t steps,
+                      void *workspace, int64_t workspace_bytes, void *hip_stream);
+
 /* ---- measurement and test aids (not steps of the method) ---------------------------------- */
 
 /* What the last dmm_execute on a plan did.
@@ -410,7 +432,8 @@ void dmm_plan_destroy(dmm_plan_t *p);
 
 const char *dmm_strerror(int status);
 int dmm_last_hip_error(void); /* hipError_t of the last failed HIP call on this thread, 0 if none */
-int dmm_version(void);         /* 6: dmm_mx_quantize, dmm_mx_dequantize, dmm_mx_execute (5: dmm_plan_last_kernels; 4: the replica sum is fused into the GEMM unless DMM_SEPARATE_REDUCE asks
+int dmm_version(void);         /* 6: dmm_mx_quantize, dmm_mx_dequantize, dmm_mx_execute,
+                                  dmm_orthogonalize (5: dmm_plan_last_kernels; 4: the replica sum is fused into the GEMM unless DMM_SEPARATE_REDUCE asks
                                   for the kernel of its own; dmm_plan_last_execute replaces the
                                   dmm_plan_ran_* accessors; 3: flag values of dmm_plan and dmm_execute disjoint,
                                   dmm_reduce_replicas_static) */

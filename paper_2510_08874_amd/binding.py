@@ -139,6 +139,10 @@ def lib() -> C.CDLL:
         L.dmm_mx_dequantize.argtypes = [C.POINTER(dmm_matrix_desc), C.POINTER(dmm_mx_tiles), C.c_int, C.c_int, P, P, P]
         L.dmm_mx_execute.restype = C.c_int
         L.dmm_mx_execute.argtypes = [P, C.POINTER(dmm_mx_tiles), C.POINTER(dmm_mx_tiles), P, P, C.c_uint32, P]
+        L.dmm_orthogonalize_workspace.restype = C.c_int
+        L.dmm_orthogonalize_workspace.argtypes = [C.POINTER(dmm_matrix_desc), C.c_int32, C.POINTER(C.c_int64)]
+        L.dmm_orthogonalize.restype = C.c_int
+        L.dmm_orthogonalize.argtypes = [C.POINTER(dmm_matrix_desc), C.c_int32, C.c_int, P, P, C.c_int, P, P, P, C.c_int32, P, C.c_int64, P]
         L.dmm_plan_elapsed_ms.restype = C.c_int
         L.dmm_plan_elapsed_ms.argtypes = [P, C.POINTER(C.c_float), C.POINTER(C.c_float)]
         L.dmm_plan_gemm_launch_ms.restype = C.c_int
@@ -158,7 +162,7 @@ def lib() -> C.CDLL:
 EXPORTS = ("dmm_plan", "dmm_plan_num_tasks", "dmm_plan_tasks", "dmm_plan_order", "dmm_plan_num_groups",
            "dmm_plan_group_offsets", "dmm_plan_num_items", "dmm_plan_items", "dmm_plan_macro_tile",
            "dmm_plan_num_merged_items", "dmm_plan_merged_items", "dmm_plan_last_execute", "dmm_plan_last_kernels",
-           "dmm_reduce_replicas_static", "dmm_mx_quantize", "dmm_mx_dequantize", "dmm_mx_execute",
+           "dmm_reduce_replicas_static", "dmm_mx_quantize", "dmm_mx_dequantize", "dmm_mx_execute", "dmm_orthogonalize", "dmm_orthogonalize_workspace",
            "dmm_execute", "dmm_reduce_replicas", "dmm_broadcast_replica", "dmm_plan_elapsed_ms", "dmm_plan_gemm_launch_ms", "dmm_plan_destroy", "dmm_strerror",
            "dmm_last_hip_error", "dmm_version", "dmm_measure_mfma_rate")
 
@@ -415,6 +419,29 @@ def dmm_mx_dequantize(desc: dmm_matrix_desc, q: dmm_mx_tiles, along: int, dtype:
 
 def dmm_mx_execute(plan: Plan, a: dmm_mx_tiles, b: dmm_mx_tiles, c, flags: int = 0, stream: Optional[int] = None) -> None:
     plan.execute_mx(a, b, c, flags, stream)
+
+
+def dmm_orthogonalize_workspace(desc: dmm_matrix_desc, count: int = 1) -> int:
+    """Bytes of device memory that ``dmm_orthogonalize`` needs."""
+    n = C.c_int64(0)
+    rc = lib().dmm_orthogonalize_workspace(C.byref(desc), count, C.byref(n))
+    if rc != DMM_OK:
+        raise DmmError(rc, "dmm_orthogonalize_workspace")
+    return int(n.value)
+
+
+def dmm_orthogonalize(desc: dmm_matrix_desc, count: int, x_dtype: int, x, y_dtype: int, y, workspace, workspace_bytes: int,
+                      coefficients: Optional[Sequence[Sequence[float]]] = None, steps: int = 5, stream: Optional[int] = None) -> None:
+    """`desc` a `matrix_desc`, `x` and `y` `tile_table`s of all matrices, `workspace` a tensor or an address, `coefficients` (a, b, c)
+    of every step (then `steps` is their number)."""
+    table = None
+    if coefficients is not None:
+        steps = len(coefficients)
+        table = (C.c_float * (3 * max(steps, 1)))(*[v for c in coefficients for v in c])
+    rc = lib().dmm_orthogonalize(C.byref(desc), count, x_dtype, x[0], x[1], y_dtype, y[0], y[1], table, steps, C.c_void_p(_ptr(workspace)),
+                                 workspace_bytes, C.c_void_p(stream or 0))
+    if rc != DMM_OK:
+        raise DmmError(rc, "dmm_orthogonalize")
 
 
 def dmm_plan_destroy(plan: Plan) -> None:

@@ -17,7 +17,7 @@ LIB = os.path.join(HERE, "libdmm.so")
 # (source, object name, extra flags): the grouped-GEMM kernels are compiled one instantiation per
 # object file (gemm_instance.hip, DMM_INSTANCE = 0 .. 5), side by side
 UNITS = [("plan.cpp", "plan", []), ("exec.hip", "exec", []), ("small_instance.hip", "small_instance", []),
-         ("mx_instance.hip", "mx_instance", [])] + \
+         ("mx_instance.hip", "mx_instance", []), ("ortho_instance.hip", "ortho_instance", [])] + \
         [("gemm_instance.hip", f"gemm_instance_{i}", [f"-DDMM_INSTANCE={i}"]) for i in range(6)]
 
 # packed-fp32 ops are switched off for all device code (a target feature of the
@@ -38,7 +38,7 @@ def check_resources(remarks: str, want_kernel: bool) -> None:
         name = b.split()[0]
         if "small_gemm_kernel" in name and re.search(r"(ScratchSize \[bytes/lane\]|VGPRs Spill): [1-9]", b):
             raise RuntimeError(f"{name}: scratch use or spills")
-        if "mx_gemm_kernel" in name and re.search(r"(ScratchSize \[bytes/lane\]|VGPRs Spill): [1-9]", b):
+        if re.search("mx_gemm_kernel|ortho_product_kernel", name) and re.search(r"(ScratchSize \[bytes/lane\]|VGPRs Spill): [1-9]", b):
             raise RuntimeError(f"{name}: scratch use or spills")
         if "grouped_gemm_kernel" not in name:
             continue

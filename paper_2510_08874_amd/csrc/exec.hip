@@ -18,6 +18,7 @@
 #include "gemm_kernel.hpp"
 #include "gemm_launch.hpp"
 #include "mx_launch.hpp"
+#include "ortho_launch.hpp"
 #include "pack_kernel.hpp"
 #include "plan_internal.h"
 #include "ring_kernel.hpp"
@@ -1906,3 +1907,4 @@ extern "C" int dmm_reduce_replicas_static(dmm_plan_t *P, void *const *c_tiles, c
 }
 
 #include "mx_exec.hpp"
+#include "ortho_exec.hpp"

@@ -18,33 +18,7 @@ namespace dmm {
 
 __device__ __forceinline__ unsigned short mx_bf16(float v) { return __builtin_bit_cast(unsigned short, (__bf16)v); }
 
-// (the host sees to it that a macro-tile's rows lie within 2^32 bytes)
-template <class SH, class E>
-__device__ __forceinline__ void mx_store(const NtTile<SH> &tile, const MxItem &it, int row0, int col0) {
-  const unsigned pitch = (unsigned)it.ldc * (unsigned)sizeof(E);
-  char *const c = (char *)nt_uniform(it.c);
-#pragma unroll
-  for (int i = 0; i < SH::MI; ++i)
-#pragma unroll
-    for (int j = 0; j < SH::NI; ++j) {
-      const int col = col0 + 32 * j;
-      if (col < it.n_ext) {
-#pragma unroll
-        for (int x = 0; x < 16; ++x) {
-          const int row = row0 + 32 * i + 8 * (x / 4) + x % 4;
-          if (row < it.m_ext) {
-            const float v = tile.acc[i][j][x];
-            E *const to = (E *)(c + ((unsigned)row * pitch + (unsigned)(col * (int)sizeof(E))));
-            if constexpr (sizeof(E) == 4) __builtin_nontemporal_store(v, to);
-            else __builtin_nontemporal_store(mx_bf16(v), to);
-          }
-        }
-      }
-      __builtin_amdgcn_sched_barrier(0);
-    }
-}
-
-// Macro-tiles.  Stores: half a wave writes 32 neighbouring columns of a row.
+// Macro-tiles.  The finished tile goes through LDS, so that a thread stores 16 bytes of a row.
 template <class SH>
 __global__ __launch_bounds__(NT_THREADS, SH::TM == 256 ? 1 : 2) void mx_gemm_kernel(const MxItem *__restrict__ items, const NtSeg *__restrict__ segs) {
   extern __shared__ char lds[];
@@ -52,10 +26,37 @@ __global__ __launch_bounds__(NT_THREADS, SH::TM == 256 ? 1 : 2) void mx_gemm_ker
   NtTile<SH> tile;
   tile.run(segs + it.seg, it.n_segs, it.first, it.steps, it.m_off, it.m_ext, it.n_off, it.n_ext, lds);
   tile.pin();
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int row0 = (wave >> 1) * (SH::TM / 2) + 4 * (lane >> 5), col0 = (wave & 1) * (SH::TN / 2) + (lane & 31);
-  if (it.c_es == 4) mx_store<SH, float>(tile, it, row0, col0);
-  else mx_store<SH, unsigned short>(tile, it, row0, col0);
+  const bool wide = !((uintptr_t)it.c & 15) && !(it.ldc * it.c_es & 15);
+  tile.slices(lds, [&](const float *values, int base) {
+    constexpr int PER = SH::TN / 8;                           // threads to a row: eight columns each
+    for (int x = threadIdx.x; x < 64 * PER; x += NT_THREADS) {
+      const int r = x / PER, col = x % PER * 8, row = base + (r & 31) + (r >> 5) * (SH::TM / 2);
+      if (row >= it.m_ext || col >= it.n_ext) continue;
+      const nt_f32x4 v = *(const nt_f32x4 *)(values + r * NtTile<SH>::PITCH + col), u = *(const nt_f32x4 *)(values + r * NtTile<SH>::PITCH + col + 4);
+      char *const to = it.c + ((int64_t)row * it.ldc + col) * it.c_es;
+      if (wide && col + 8 <= it.n_ext) {
+        if (it.c_es == 4) {
+          __builtin_nontemporal_store(v, (nt_f32x4 *)to);
+          __builtin_nontemporal_store(u, (nt_f32x4 *)to + 1);
+        } else {
+          nt_i32x4 w;
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            const nt_f32x4 &f = y < 2 ? v : u;
+            w[y] = (int)((unsigned)mx_bf16(f[2 * (y & 1)]) | (unsigned)mx_bf16(f[2 * (y & 1) + 1]) << 16);
+          }
+          __builtin_nontemporal_store(w, (nt_i32x4 *)to);
+        }
+      } else {
+#pragma unroll
+        for (int y = 0; y < 8; ++y)
+          if (col + y < it.n_ext) {
+            if (it.c_es == 4) ((float *)to)[y] = y < 4 ? v[y] : u[y - 4];
+            else ((unsigned short *)to)[y] = mx_bf16(y < 4 ? v[y] : u[y - 4]);
+          }
+      }
+    }
+  });
 }
 
 // Sums of partial tiles, in ascending k.

@@ -91,7 +91,32 @@ struct NtTile {
   }
 
   // `segs`: n_segs from the one that holds the first step; `first`: the first step in it; `steps`: in all
-  __device__ __forceinline__ void run(const NtSeg *__restrict__ segs, int n_segs, int first, int steps, int m_off, int m_ext, int n_off, int n_ext, char *lds) {
+  // The finished tile, 64 rows at a time through LDS, where `use(values, row)` finds rows row .. row + 31 of the tile in rows 0 .. 31
+  // of `values` and row + TM / 2 ... in rows 32 .. 63; PITCH floats from one to the next.  Every thread gets there between two barriers.
+  static constexpr int PITCH = SH::TN + 4;
+  static_assert(64 * PITCH * 4 <= SH::LDS, "a slice lies in the stages");
+  template <class F>
+  __device__ __forceinline__ void slices(char *lds, F &&use) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    float *const values = (float *)lds;
+    float *const mine = values + ((wave >> 1) * 32 + 4 * (lane >> 5)) * PITCH + (wave & 1) * (SH::TN / 2) + (lane & 31);
+    nt_for<SH::MI>([&](auto ic) {
+      constexpr int I = decltype(ic)::value;
+      __syncthreads();
+      nt_for<SH::NI>([&](auto jc) {
+        constexpr int J = decltype(jc)::value;
+#pragma unroll
+        for (int x = 0; x < 16; ++x) mine[(8 * (x / 4) + x % 4) * PITCH + 32 * J] = acc[I][J][x];
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      __syncthreads();
+      use(values, 32 * I);
+    });
+  }
+
+  // (`segs`: anything that has an NtSeg at an index)
+  template <class Segs>
+  __device__ __forceinline__ void run(const Segs &segs, int n_segs, int first, int steps, int m_off, int m_ext, int n_off, int n_ext, char *lds) {
     constexpr int MI = SH::MI, NI = SH::NI, LA = SH::LA, LB = SH::LB, LS = SH::LS;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);

@@ -1,0 +1,60 @@
+// Arguments and host-side doors of the kernels that orthogonalise a matrix (ortho_kernel.hpp), compiled in an
+// object file of their own (ortho_instance.hip).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace dmm {
+
+// A tile of an input or an output; travels with the launch.
+struct OrthoTile {
+  char *p;
+  int64_t pitch;                // bytes
+  int32_t row0, col0, h, w;     // where it lies in its matrix
+  int32_t matrix;
+  int32_t first_block, across;  // its workgroups begin here; as many side by side
+  int32_t pad;                  // the norm: workgroups of the matrix' tiles in front of this one
+};
+constexpr int ORTHO_TILES = 64;
+struct OrthoTiles {
+  int32_t n, f32;               // tiles; fp32 or bf16
+  int32_t rows, cols;
+  int32_t row_pitch, col_pitch; // elements of a row of the two layouts: columns (rows) up to a multiple of 32
+  int64_t stride;               // bytes from one matrix' buffers to the next
+  char *ws;
+  int64_t by_rows, by_cols;     // planes [rows][row_pitch] and [cols][col_pitch], the low parts right behind the high ones
+  double *sums;                 // of squares, so many per matrix
+  int32_t sums_of_launch, pad;
+  OrthoTile tile[ORTHO_TILES];
+};
+
+// out = alpha old + beta sum over k of A[m][k] B[n][k].  All matrices are pairs of fp16 planes.
+struct OrthoProduct {
+  char *ws;                     // what follows are byte offsets in a matrix' buffers
+  int64_t stride;
+  int64_t a, a_low, b, b_low;
+  int64_t old, old_low;         // out's rows and pitch; none: < 0
+  int64_t out, out_low;         // none: < 0
+  int64_t turned, turned_low;   // out transposed, none: < 0
+  int64_t y;                    // the last product: out goes here alone, in fp32; else < 0
+  uint32_t k_pitch_a, k_pitch_b;   // bytes
+  uint32_t out_pitch, turned_pitch;   // elements
+  int32_t m, n;                 // out: m x n (columns up to out_pitch are zero, and rows up to turned_pitch)
+  int32_t steps;                // 32 of k each
+  int32_t y_turned;             // ... transposed
+  int32_t symmetric;            // out is: tiles below the diagonal come from those above
+  int32_t count, tiles, tiles_m, tiles_n;   // matrices; tiles of each, in rows and columns
+  int32_t runs, per;            // every tile in so many ranges of K, steps of each (of 3 x steps)
+  float *parts;
+  float alpha, beta;
+};
+
+hipError_t ortho_allow_lds();
+void ortho_norm_launch(const OrthoTiles &args, int blocks, hipStream_t stream);
+void ortho_split_launch(const OrthoTiles &args, int blocks, hipStream_t stream);
+// y: fp32 matrices one behind another in by_rows' place -> the tiles
+void ortho_store_launch(const OrthoTiles &args, int blocks, hipStream_t stream);
+void ortho_product_launch(const OrthoProduct &args, int edge, hipStream_t stream);   // edge of a tile: 128 or 256
+
+}  // namespace dmm
