@@ -128,7 +128,7 @@ int over_tiles(const Grid &G, int es, char *const *x, const int64_t *x_ld, const
 // costs a tile's worth of partial sums written and read again.
 constexpr struct {
   int per_cu, min_steps;
-} kMxRun[MX_SHAPES] = {{1, 24}, {2, 12}, {4, 16}, {3, 16}, {2, 16}};
+} kMxRun[MX_SHAPES] = {{1, 12}, {2, 6}, {4, 8}, {3, 8}, {2, 8}};
 
 // Blocks of A and of B have to meet: every op starts at a whole chunk of both tiles.  (It then ends at one, or where
 // both tiles end: the next op starts there.)
@@ -173,9 +173,9 @@ int build_mx(dmm_plan_t *P, const dmm_mx_tiles *a, const dmm_mx_tiles *b, void *
       s.b_pitch = (uint32_t)b->code_ld[bi];
       s.a_scale_pitch = (uint32_t)a->scale_ld[ai];
       s.b_scale_pitch = (uint32_t)b->scale_ld[bi];
-      s.steps = (int32_t)((t.k1 - t.k0 + 127) / 128);
+      s.chunks = (int32_t)((t.k1 - t.k0 + 127) / 128);
       s.pad = 0;
-      steps += s.steps;
+      steps += (s.chunks + 1) / 2;
       segs.push_back(s);
     }
     if (steps > 0x3fffffff || segs.size() > 0x3fffffff) return DMM_ELIMIT;
@@ -239,7 +239,7 @@ int build_mx(dmm_plan_t *P, const dmm_mx_tiles *a, const dmm_mx_tiles *b, void *
             part.pad = 1;
             items.push_back(part);
             first += part.steps;
-            while (seg < group_seg[x + 1] && first >= segs[(size_t)seg].steps) first -= segs[(size_t)seg++].steps;
+            while (seg < group_seg[x + 1] && first >= (segs[(size_t)seg].chunks + 1) / 2) first -= (segs[(size_t)seg++].chunks + 1) / 2;
           }
         }
   }

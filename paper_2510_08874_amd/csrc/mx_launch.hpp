@@ -8,11 +8,11 @@
 namespace dmm {
 
 // A run of K on which both operands lie in one piece.  The pointers name row 0 of the product's rows (columns) at
-// the run's first step (64 bytes of a row); scales only where there are any (4 bytes of a row and step).
+// the run's first chunk (64 bytes of a row); scales only where there are any (4 bytes of a row and chunk).
 struct NtSeg {
   const char *a, *b, *a_scale, *b_scale;
   uint32_t a_pitch, b_pitch, a_scale_pitch, b_scale_pitch;   // bytes
-  int32_t steps;
+  int32_t chunks;
   int32_t pad;
 };
 
@@ -23,7 +23,7 @@ struct MxItem {
   int32_t m_off, n_off;         // first row and column inside the output sub-tile that the segments are given for
   int32_t m_ext, n_ext;
   int32_t seg, n_segs;          // from the segment that holds its first step; none: zeros
-  int32_t first, steps;         // first step (128 of k) in that segment; how many in all
+  int32_t first, steps;         // first step (two chunks, 256 of k) in that segment; how many in all
   int32_t c_es;                 // bytes of an element of C: 4, or 2 for bf16
   int32_t pad;
 };

@@ -1,16 +1,18 @@
 // Products of two operands that both lie along K (gfx950, device code only): D[m][n] = sum over k of
 // A[m][k] B[n][k], in macro-tiles that one workgroup of four waves accumulates in registers.  Shared by the
 // products of 4-bit microscaled operands (mx_kernel.hpp) and of fp16 pairs (ortho_kernel.hpp): both feed a matrix
-// instruction with 64 bytes of K a row, 16 in each lane, so a step, its stage in LDS and its loads are the same:
-//   fp4   16 x 16 x 128: a lane holds 32 codes of one row, which share one scale
-//   fp16  16 x 16 x 32:  a lane holds 8 values of one row
+// instruction with 32 bytes of K a row, 16 in each half of the lanes, so a step, its stage in LDS and its loads are the same:
+//   fp4   32 x 32 x 64: a lane holds 32 codes of one row, which share one scale
+//   fp16  32 x 32 x 16: a lane holds 8 values of one row
 //
-// What bounds a 256 x 256 tile: a step is 64 matrix instructions of 16 cycles on each of the four matrix
-// pipes (1024 cycles), 64 KB of LDS reads (512 cycles at 128 bytes), 32 KB written to LDS by the loads (256) and 32
-// KB from L2 (32 bytes a cycle and CU).  So the pipes can be kept busy if nothing waits: operands go straight into
-// a ring of four LDS stages, two steps ahead, and the fragments of a step are read during the step before it,
-// between its matrix instructions.  One barrier a step: behind it the next step's stage may be read, and the stage of
-// the step before, which every wave has read, may be filled.
+// What bounds a 256 x 256 tile: a step of 128 bytes a row is 64 matrix instructions of 32 cycles on each of the four
+// matrix pipes (2048 cycles), 128 KB of LDS reads (1024 cycles at 128 bytes), 64 KB written to LDS by the loads (512) and 64
+// KB from L2.  L2 answers requests of up to 128 bytes, 16 of them a cycle to the 32 CUs of an XCD: 512 rows
+// of 128 bytes take 1024 cycles, so the rows of a step are whole lines.  (With steps of 64 bytes, and four bytes of scales a row
+// and step, there were four times as many requests: 16384 x 8192 x 28672 in 4 bits 2.42 ms, matrix pipes busy 35 %.)
+// The pipes can be kept busy if nothing waits: operands go straight into two LDS stages, and the fragments of a
+// quarter of a step are read during the quarter before it, between its matrix instructions.  One barrier a step, in front of its last
+// quarter: behind it the next stage may be read, and the stage whose last fragments every wave holds may be filled.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -23,6 +25,7 @@
 
 namespace dmm {
 
+typedef int nt_i32x2 __attribute__((ext_vector_type(2)));
 typedef int nt_i32x4 __attribute__((ext_vector_type(4)));
 typedef int nt_i32x8 __attribute__((ext_vector_type(8)));
 typedef float nt_f32x4 __attribute__((ext_vector_type(4)));
@@ -32,12 +35,12 @@ typedef const __attribute__((address_space(1))) char *nt_gptr;
 typedef __attribute__((address_space(3))) char *nt_lptr;
 
 constexpr int NT_THREADS = 256;
-constexpr int NT_ROW = 64;                 // bytes of a row in one step
-constexpr int NT_STAGES = 4;
+constexpr int NT_ROW = 128;                // bytes of a row in one step
+constexpr int NT_CHUNK = 64;               // what a segment's length is given in: 128 codes, 32 fp16
 
-// 16-byte slots of a 64-byte row are exchanged by row, so that 16 lanes that read one slot of 16 rows fall
+// 16-byte slots of a 128-byte row are exchanged by row, so that 16 lanes that read one slot of 16 rows fall
 // into different banks.
-__device__ __forceinline__ int nt_swizzle(int row) { return ((row >> 1) & 3) ^ ((row >> 3) & 1); }
+__device__ __forceinline__ int nt_swizzle(int row) { return (row >> 1) & 7; }
 
 __device__ __forceinline__ void nt_load16(nt_gptr base, unsigned lane_off, unsigned lds) {
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(lane_off), "s"(base), "s"(lds) : "memory");
@@ -69,14 +72,14 @@ struct NtShape {
   static constexpr bool SCALED = SCALED_;
   static constexpr int TM = TM_, TN = TN_;
   static constexpr int MI = TM / 64, NI = TN / 64;           // 32 x 32 tiles of a wave
-  static constexpr int A_BYTES = TM * NT_ROW, B_BYTES = TN * NT_ROW;
-  static constexpr int S_BYTES = SCALED ? (TM + TN) * 4 : 0;
-  static constexpr int STAGE = A_BYTES + B_BYTES + S_BYTES;
-  static constexpr int LDS = NT_STAGES * STAGE;
-  static constexpr int LA = TM / 64, LB = TN / 64;           // 1 KB loads of a wave and step
-  static constexpr int LS = SCALED ? (TM + TN) / 256 : 0;    // 64-row loads of scales of a wave and step
-  static constexpr int LOADS = LA + LB + LS;
-  static_assert(TM % 128 == 0 && TN % 128 == 0, "a wave loads whole rows of scales");
+  static constexpr int A_BYTES = TM * NT_ROW, B_BYTES = TN * NT_ROW, STAGE = A_BYTES + B_BYTES;
+  // scales of two steps together, 16 bytes a row: a request fetches them once
+  static constexpr int S_ROW = 16, S_SLOT = SCALED ? (TM + TN) * S_ROW : 0;
+  static constexpr int LDS = 2 * STAGE + 3 * S_SLOT;
+  static constexpr int LA = TM / 32, LB = TN / 32;           // 1 KB loads of a wave and step, 8 rows each
+  static constexpr int LOADS = LA + LB, EARLY = LOADS / 2;   // half of them behind the barrier, half in the next step's first quarter
+  static constexpr int LS = SCALED ? (TM + TN) / 64 : 0;     // 16-row loads of scales of a wave, for two steps
+  static_assert(TM % 128 == 0 && TN % 128 == 0, "a wave loads whole rows of scales of one operand");
 };
 
 // Rows of a macro-tile past `ext` are read from its last row: they are never stored.
@@ -85,12 +88,12 @@ struct NtTile {
   // [i][j][x]: row 32 i + 8 (x / 4) + 4 (lane / 32) + x % 4, column 32 j + lane % 32 of the wave's quarter
   nt_f32x16 acc[SH::MI][SH::NI];
 
-  // The sums are in accumulator registers here: keeps the compiler from moving them about.
+  // The sums are in accumulator registers here: keeps the compiler from moving them about, and from moving matrix
+  // instructions behind a branch.
   __device__ __forceinline__ void pin() {
     nt_for<SH::MI * SH::NI>([&](auto tc) { asm volatile("" : "+a"(acc[decltype(tc)::value / SH::NI][decltype(tc)::value % SH::NI])); });
   }
 
-  // `segs`: n_segs from the one that holds the first step; `first`: the first step in it; `steps`: in all
   // The finished tile, 64 rows at a time through LDS, where `use(values, row)` finds rows row .. row + 31 of the tile in rows 0 .. 31
   // of `values` and row + TM / 2 ... in rows 32 .. 63; PITCH floats from one to the next.  Every thread gets there between two barriers.
   static constexpr int PITCH = SH::TN + 4;
@@ -114,7 +117,8 @@ struct NtTile {
     });
   }
 
-  // (`segs`: anything that has an NtSeg at an index)
+  // `segs`: n_segs from the one that holds the first step (anything that has an NtSeg at an index); `first`: the first
+  // step in it; `steps`: in all.  A segment of an odd number of chunks ends with half a step.
   template <class Segs>
   __device__ __forceinline__ void run(const Segs &segs, int n_segs, int first, int steps, int m_off, int m_ext, int n_off, int n_ext, char *lds) {
     constexpr int MI = SH::MI, NI = SH::NI, LA = SH::LA, LB = SH::LB, LS = SH::LS;
@@ -129,109 +133,150 @@ struct NtTile {
     if (steps <= 0) return;
 
     // ---- this lane's part of the loads -----------------------------------------------------
-    // load x of a wave: rows 16 (4 x + wave) ..., 16 bytes a lane, in the order of the stage
-    int arow[LA], brow[LB], srow[LS ? LS : 1];
-#pragma unroll
-    for (int x = 0; x < LA; ++x) arow[x] = min(16 * (4 * x + wave) + (lane >> 2), m_ext - 1);
-#pragma unroll
-    for (int x = 0; x < LB; ++x) brow[x] = min(16 * (4 * x + wave) + (lane >> 2), n_ext - 1);
-    // load x of scales: rows 64 (LS wave + x) ... of A's rows followed by B's
-#pragma unroll
-    for (int x = 0; x < LS; ++x) {
-      const int row = 64 * (LS * wave + x) + lane;
-      srow[x] = 64 * (LS * wave + x) < SH::TM ? min(row, m_ext - 1) : min(row - SH::TM, n_ext - 1);
-    }
-    const int slot = ((lane & 3) ^ nt_swizzle(lane >> 2)) * 16;
-    unsigned aoff[LA], boff[LB], soff[LS ? LS : 1];
-    nt_gptr a = nullptr, b = nullptr, as = nullptr, bs = nullptr;
-    int left = 0, on = NT_ROW;                                // steps to load in this run of K; bytes from one to the next
+    // load x of a wave: rows 8 (4 x + wave) ..., 16 bytes a lane, in the order of the stage
+    const int row8 = 8 * wave + (lane >> 3);
+    const int slot = (lane & 7) ^ nt_swizzle(row8);          // (load x is 32 rows on: the same)
+    unsigned aoff[LA], boff[LB];
+    nt_gptr a = nullptr, b = nullptr;
+    const char *as = nullptr, *bs = nullptr;                  // scales of row 0 at the segment's next step
+    unsigned as_pitch = 0, bs_pitch = 0;
+    int chunks = 0, on = NT_ROW;                              // chunks left to load in this segment; bytes from one step to the next
     auto enter = [&](const NtSeg &s, int skip) {
-      left = s.steps - skip;
+      chunks = s.chunks - 2 * skip;
       a = nt_uniform(s.a + (int64_t)m_off * s.a_pitch + (int64_t)skip * NT_ROW);
       b = nt_uniform(s.b + (int64_t)n_off * s.b_pitch + (int64_t)skip * NT_ROW);
 #pragma unroll
-      for (int x = 0; x < LA; ++x) aoff[x] = (unsigned)arow[x] * s.a_pitch + slot;
+      for (int x = 0; x < LA; ++x) aoff[x] = (unsigned)min(32 * x + row8, m_ext - 1) * s.a_pitch + slot * 16;
 #pragma unroll
-      for (int x = 0; x < LB; ++x) boff[x] = (unsigned)brow[x] * s.b_pitch + slot;
+      for (int x = 0; x < LB; ++x) boff[x] = (unsigned)min(32 * x + row8, n_ext - 1) * s.b_pitch + slot * 16;
       if constexpr (SH::SCALED) {
-        as = nt_uniform(s.a_scale + (int64_t)m_off * s.a_scale_pitch + (int64_t)skip * 4);
-        bs = nt_uniform(s.b_scale + (int64_t)n_off * s.b_scale_pitch + (int64_t)skip * 4);
-#pragma unroll
-        for (int x = 0; x < LS; ++x) soff[x] = (unsigned)srow[x] * (64 * (LS * wave + x) < SH::TM ? s.a_scale_pitch : s.b_scale_pitch);
+        as = s.a_scale + (int64_t)m_off * s.a_scale_pitch + (int64_t)skip * 8;
+        bs = s.b_scale + (int64_t)n_off * s.b_scale_pitch + (int64_t)skip * 8;
+        as_pitch = s.a_scale_pitch;
+        bs_pitch = s.b_scale_pitch;
       }
     };
-    int seg = 0;
-    enter(segs[0], first);
+    // The step that is loaded next is half a one: the lanes of what is missing read the half that is there, and count for nothing, since
+    // their scales are 2^-127 on both sides (fp16 operands are filled up with zeros).
+    auto halve = [&]() {
+      if (chunks == 1) {
+        const unsigned back = slot >= 4 ? 64 : 0;
+#pragma unroll
+        for (int x = 0; x < LA; ++x) aoff[x] -= back;
+#pragma unroll
+        for (int x = 0; x < LB; ++x) boff[x] -= back;
+      }
+    };
     // load x of a step, into the stage at byte `base` of LDS
     auto load = [&](auto xc, unsigned base) {
       constexpr int X = decltype(xc)::value;
       if constexpr (X < LA) nt_load16(a, aoff[X], base + (4 * X + wave) * 1024);
-      else if constexpr (X < LA + LB) nt_load16(b, boff[X - LA], base + SH::A_BYTES + (4 * (X - LA) + wave) * 1024);
-      else {
-        constexpr int Y = X - LA - LB;
-        nt_load4(64 * (LS * wave + Y) < SH::TM ? as : bs, soff[Y], base + SH::A_BYTES + SH::B_BYTES + (LS * wave + Y) * 256);
+      else nt_load16(b, boff[X - LA], base + SH::A_BYTES + (4 * (X - LA) + wave) * 1024);
+    };
+    // Scales of the next two steps of the segment, into the next slot: a wave's rows are of one operand.
+    int s_left = 0;                                           // steps whose scales are in the slot and that are yet to be loaded
+    unsigned s_at = 0, s_slot = 2 * SH::S_SLOT;               // ... of the step loaded next; the slot filled last
+    auto load_scales = [&]() {
+      if constexpr (SH::SCALED) {
+        // (of three: one is being read by waves that are late, one has the scales of the next step)
+        s_slot = s_slot == 2 * SH::S_SLOT ? 0 : s_slot + SH::S_SLOT;
+        s_at = s_slot;
+        s_left = chunks > 2 ? 2 : 1;
+        const bool is_a = wave < 2;
+        const int ext = is_a ? m_ext : n_ext, row0 = (wave & 1) * (SH::TM / 2) + (lane >> 2), n = chunks < 4 ? chunks : 4;
+        const unsigned pitch = is_a ? as_pitch : bs_pitch, d = lane & 3;
+        const nt_gptr p = nt_uniform(is_a ? as : bs);
+        const unsigned to = 2 * SH::STAGE + s_slot + wave * (LS * 16 * SH::S_ROW);
+        if (n == 4) {
+#pragma unroll
+          for (int x = 0; x < LS; ++x) nt_load4(p, (unsigned)min(row0 + 16 * x, ext - 1) * pitch + d * 4, lds0 + to + x * 256);
+        } else {
+          for (int x = 0; x < LS; ++x) {
+            int v = 0;
+            if ((int)d < n) v = *(const __attribute__((address_space(1))) int *)(p + ((unsigned)min(row0 + 16 * x, ext - 1) * pitch + d * 4));
+            *(__attribute__((address_space(3))) int *)((nt_lptr)lds + to + x * 256 + lane * 4) = v;
+          }
+        }
+        as += 16;
+        bs += 16;
       }
     };
-    // to the next step to load.  Past the last one its operands are loaded again, to be read by nobody: the loads under
-    // way stay countable, and the loop has no branches
-    auto advance = [&]() {
+    static_assert(SH::TM == SH::TN, "a wave's rows of scales");
+    int seg = 0;
+    enter(segs[0], first);
+    halve();
+    load_scales();
+    // to the next step to load.  Past the last one its operands are loaded again, to be read by nobody.
+    unsigned s_next_at = 0;                                   // where the scales of the step loaded last are
+    auto next = [&]() {
       a += on;
       b += on;
+      chunks -= 2;
       if constexpr (SH::SCALED) {
-        as += on >> 4;
-        bs += on >> 4;
+        s_next_at = s_at;
+        s_at += 8;
+        --s_left;
       }
-    };
-    auto turn = [&]() {                                       // behind the last step of a run
-      if (seg + 1 < n_segs) {
-        ++seg;
-        enter(segs[seg], 0);
-      } else {
-        a -= on;
-        b -= on;
-        as -= on >> 4;
-        bs -= on >> 4;
-        on = 0;
-        left = 1 << 30;
+      if (chunks <= 2 || (SH::SCALED && s_left == 0)) {
+        if (chunks <= 0) {
+          if (++seg < n_segs) {
+            enter(segs[seg], 0);
+            halve();
+            load_scales();
+          } else {
+            a -= on;
+            b -= on;
+            on = 0;
+            chunks = 1 << 30;
+            s_left = 1 << 30;
+            s_at = s_slot;
+          }
+        } else {
+          halve();
+          if (s_left == 0) load_scales();
+        }
       }
     };
 
     // ---- fragments ---------------------------------------------------------------------------
-    // half h of a step: 32 bytes of 32 rows, 16 in each lane; a row's scales (4 bytes a step) are shifted once so
-    // that byte 2 h is the one of the lane's codes
+    // quarter h of a step: 32 bytes of 32 rows, 16 in each lane.  A row's scales (8 bytes a step) are shifted once so that byte
+    // 2 (h % 2) of word h / 2 is the one of the lane's codes.
     const int r = lane & 31, g = lane >> 5;
     const nt_lptr fa = (nt_lptr)lds + wm * (SH::TM / 2) * NT_ROW + r * NT_ROW;
     const nt_lptr fb = (nt_lptr)lds + SH::A_BYTES + wn * (SH::TN / 2) * NT_ROW + r * NT_ROW;
-    const nt_lptr fs = (nt_lptr)lds + SH::A_BYTES + SH::B_BYTES + r * 4;
-    const int chunk[2] = {(g ^ nt_swizzle(r)) * 16, ((2 + g) ^ nt_swizzle(r)) * 16};
+    const nt_lptr fs = (nt_lptr)lds + 2 * SH::STAGE + r * SH::S_ROW;
+    const int turn = (g ^ nt_swizzle(r)) * 16;                // (slot 2 h + g, exchanged)
     struct Frag {
       nt_i32x4 a[MI], b[NI];
     };
     struct Scale {
-      int a[SH::SCALED ? MI : 1], b[SH::SCALED ? NI : 1];
+      nt_i32x2 a[SH::SCALED ? MI : 1], b[SH::SCALED ? NI : 1];
     };
-    // fragment x of a half: the rows of A, the columns of B
+    // fragment x of a quarter: the rows of A, the columns of B
     auto read = [&](Frag &f, auto xc, unsigned stage, auto hc) {
       constexpr int X = decltype(xc)::value;
-      const unsigned o = stage + chunk[decltype(hc)::value];
+      const unsigned o = stage + (turn ^ (decltype(hc)::value * 32));
       if constexpr (X < MI) f.a[X] = *(const __attribute__((address_space(3))) nt_i32x4 *)(fa + o + X * 32 * NT_ROW);
       else f.b[X - MI] = *(const __attribute__((address_space(3))) nt_i32x4 *)(fb + o + (X - MI) * 32 * NT_ROW);
     };
-    auto read_scales = [&](Scale &f, unsigned stage) {
+    auto read_scales = [&](Scale &f, unsigned at) {
       if constexpr (SH::SCALED) {
-        const nt_lptr p = fs + stage;
+        const nt_lptr p = fs + at;
 #pragma unroll
-        for (int i = 0; i < MI; ++i) f.a[i] = *(const __attribute__((address_space(3))) int *)(p + (wm * (SH::TM / 2) + 32 * i) * 4);
+        for (int i = 0; i < MI; ++i) f.a[i] = *(const __attribute__((address_space(3))) nt_i32x2 *)(p + (wm * (SH::TM / 2) + 32 * i) * SH::S_ROW);
 #pragma unroll
-        for (int j = 0; j < NI; ++j) f.b[j] = *(const __attribute__((address_space(3))) int *)(p + (SH::TM + wn * (SH::TN / 2) + 32 * j) * 4);
+        for (int j = 0; j < NI; ++j) f.b[j] = *(const __attribute__((address_space(3))) nt_i32x2 *)(p + (SH::TM + wn * (SH::TN / 2) + 32 * j) * SH::S_ROW);
       }
     };
     auto shift = [&](Scale &f) {
       if constexpr (SH::SCALED) {
 #pragma unroll
-        for (int i = 0; i < MI; ++i) f.a[i] = (int)((unsigned)f.a[i] >> (8 * g));
+        for (int w = 0; w < 2; ++w) {
 #pragma unroll
-        for (int j = 0; j < NI; ++j) f.b[j] = (int)((unsigned)f.b[j] >> (8 * g));
+          for (int i = 0; i < MI; ++i) f.a[i][w] = (int)((unsigned)f.a[i][w] >> (8 * g));
+#pragma unroll
+          for (int j = 0; j < NI; ++j) f.b[j][w] = (int)((unsigned)f.b[j][w] >> (8 * g));
+        }
       }
     };
     auto multiply = [&](const Frag &f, const Scale &s, auto tc, auto hc) {
@@ -239,67 +284,73 @@ struct NtTile {
       if constexpr (SH::SCALED) {
         const nt_i32x8 x = {f.a[I][0], f.a[I][1], f.a[I][2], f.a[I][3], 0, 0, 0, 0};
         const nt_i32x8 y = {f.b[J][0], f.b[J][1], f.b[J][2], f.b[J][3], 0, 0, 0, 0};
-        acc[I][J] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, acc[I][J], 4, 4, 2 * H, s.a[I], 2 * H, s.b[J]);
+        acc[I][J] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, acc[I][J], 4, 4, 2 * (H & 1), s.a[I][H >> 1], 2 * (H & 1), s.b[J][H >> 1]);
       } else {
         acc[I][J] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(nt_f16x8, f.a[I]), __builtin_bit_cast(nt_f16x8, f.b[J]), acc[I][J], 0, 0, 0);
       }
     };
+    constexpr int T = MI * NI, R = MI + NI;
+    // The order of the statements is the order of the instructions: what else a quarter needs (its `also`, by matrix instruction)
+    // is spread over its matrix instructions, which take the pipe 32 cycles each.
+    auto quarter = [&](const Frag &f, const Scale &s, auto hc, Frag &into, unsigned stage, auto also) {
+      constexpr int H = decltype(hc)::value;
+      nt_for<T>([&](auto tc) {
+        constexpr int I = decltype(tc)::value;
+        multiply(f, s, tc, hc);
+        nt_for<R>([&](auto xc) {
+          if constexpr (decltype(xc)::value * T / R == I) read(into, xc, stage, std::integral_constant<int, (H + 1) % 4>{});
+        });
+        also(tc);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    };
     std::integral_constant<int, 0> h0;
     std::integral_constant<int, 1> h1;
-    constexpr int T = MI * NI, R = MI + NI;
+    std::integral_constant<int, 2> h2;
+    std::integral_constant<int, 3> h3;
+    auto nothing = [](auto) {};
 
     // ---- the steps ---------------------------------------------------------------------------
-    // in front: stages 0, 1 and 2 under way, the first half of step 0 read
-#pragma unroll
-    for (int x = 0; x < 3; ++x) {
-      nt_for<SH::LOADS>([&](auto xc) { load(xc, lds0 + x * SH::STAGE); });
-      advance();
-      if (--left == 0) turn();
-    }
-    nt_wait_loads<2 * SH::LOADS>();
+    // in front: step 0 and half of step 1 under way, the first quarter of step 0 read
+    nt_for<SH::LOADS>([&](auto xc) { load(xc, lds0); });
+    next();
+    nt_for<SH::EARLY>([&](auto xc) { load(xc, lds0 + SH::STAGE); });
+    nt_wait_loads<SH::EARLY>();                               // (and the scales, older or behind a wait of their own)
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     Frag f0, f1;
     Scale s, s_next;
-    read_scales(s, 0);
+    read_scales(s, s_next_at);
     nt_for<R>([&](auto xc) { read(f0, xc, 0, h0); });
-    unsigned now = 0, fill = 3 * SH::STAGE;                   // stage of the current step; stage that is filled next
-    // The order of the statements is the order of the instructions: what else a step needs is spread over its
-    // matrix instructions, which take the pipe 32 cycles each.
+    unsigned now = 0;                                         // stage of the current step
 #pragma clang loop unroll(disable)
     for (int t = steps; t > 0; --t) {
       shift(s);
-      nt_for<T>([&](auto tc) {
-        constexpr int I = decltype(tc)::value;
-        multiply(f0, s, tc, h0);
-        nt_for<R>([&](auto xc) {
-          if constexpr (decltype(xc)::value * T / R == I) read(f1, xc, now, h1);
+      const unsigned other = SH::STAGE - now;
+      quarter(f0, s, h0, f1, now, [&](auto tc) {              // ... and the rest of the next step's loads
+        nt_for<SH::LOADS>([&](auto xc) {
+          constexpr int X = decltype(xc)::value - SH::EARLY;
+          if constexpr (X >= 0 && X * T / (SH::LOADS - SH::EARLY) == decltype(tc)::value) load(xc, lds0 + other);
         });
-        __builtin_amdgcn_sched_barrier(0);
       });
-      nt_wait_loads<SH::LOADS>();                           // the next step has landed
+      pin();
+      next();
+      quarter(f1, s, h1, f0, now, nothing);
+      quarter(f0, s, h2, f1, now, nothing);
+      nt_wait_loads<0>();                                     // the next step has landed,
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // and this one's last fragments are read
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
-      now = now == 3 * SH::STAGE ? 0 : now + SH::STAGE;
-      const unsigned base = lds0 + fill;
-      fill = fill == 3 * SH::STAGE ? 0 : fill + SH::STAGE;
-      read_scales(s_next, now);
+      read_scales(s_next, s_next_at);
       __builtin_amdgcn_sched_barrier(0);
-      nt_for<T>([&](auto tc) {
-        constexpr int I = decltype(tc)::value;
-        multiply(f1, s, tc, h1);
-        nt_for<R>([&](auto xc) {
-          if constexpr (decltype(xc)::value * T / R == I) read(f0, xc, now, h0);
+      quarter(f1, s, h3, f0, other, [&](auto tc) {            // ... and half of the loads of the step behind it
+        nt_for<SH::EARLY>([&](auto xc) {
+          if constexpr (decltype(xc)::value * T / SH::EARLY == decltype(tc)::value) load(xc, lds0 + now);
         });
-        nt_for<SH::LOADS>([&](auto xc) {
-          if constexpr (decltype(xc)::value * T / SH::LOADS == I) load(xc, base);
-        });
-        __builtin_amdgcn_sched_barrier(0);
       });
-      advance();
+      now = other;
       s = s_next;
-      pin();                                                  // (or the compiler moves matrix instructions behind the branch)
-      if (--left == 0) turn();
     }
     nt_wait_loads<0>();
   }

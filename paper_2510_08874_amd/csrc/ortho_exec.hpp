@@ -24,7 +24,7 @@ OrthoCut ortho_cut(int64_t m, int64_t n, bool symmetric, int64_t steps, int64_t 
   cut(256);
   if (c.tiles * count * 4 < kOrthoCus * 3) cut(128);
   const int64_t tiles = c.tiles * count, places = c.edge == 256 ? kOrthoCus : 2 * kOrthoCus;
-  int64_t runs = tiles * 2 <= places ? std::min<int64_t>(places / tiles, steps / 8) : 1;
+  int64_t runs = tiles * 2 <= places ? std::min<int64_t>(places / tiles, steps / 4) : 1;
   if (runs < 1) runs = 1;
   c.per = (int)((steps + runs - 1) / runs);
   c.runs = (int)((steps + c.per - 1) / c.per);
@@ -33,7 +33,7 @@ OrthoCut ortho_cut(int64_t m, int64_t n, bool symmetric, int64_t steps, int64_t 
 }
 
 struct OrthoLayout {
-  int64_t s, l, sp, lp;                // fewer rows, more columns; filled up to multiples of 32
+  int64_t s, l, sp, lp;                // fewer rows, more columns; filled up to multiples of 64
   bool flip;                           // the matrix has more rows than columns: its transpose is worked on
   // byte offsets in a matrix' buffers: two generations of X by rows and by columns, S, P
   int64_t wide[2], tall[2], S, P, stride;
@@ -50,8 +50,8 @@ int ortho_layout(const Grid &G, int32_t count, OrthoLayout *L) {
   L->flip = G.rows > G.cols;
   L->s = std::min(G.rows, G.cols);
   L->l = std::max(G.rows, G.cols);
-  L->sp = up(L->s, 32);
-  L->lp = up(L->l, 32);
+  L->sp = up(L->s, 64);
+  L->lp = up(L->l, 64);
   L->wide_plane = L->s * L->lp * 2;
   L->tall_plane = L->l * L->sp * 2;
   L->square_plane = L->s * L->sp * 2;
@@ -79,9 +79,9 @@ int ortho_layout(const Grid &G, int32_t count, OrthoLayout *L) {
   at *= count;
   L->sums = 256 + L->tiles;
   L->o_sums = take(count * L->sums * 8);
-  L->cut_s = ortho_cut(L->s, L->s, true, 3 * L->lp / 32, count);
-  L->cut_p = ortho_cut(L->s, L->s, true, 3 * L->sp / 32, count);
-  L->cut_x = ortho_cut(L->s, L->l, false, 3 * L->sp / 32, count);
+  L->cut_s = ortho_cut(L->s, L->s, true, 3 * L->lp / 64, count);
+  L->cut_p = ortho_cut(L->s, L->s, true, 3 * L->sp / 64, count);
+  L->cut_x = ortho_cut(L->s, L->l, false, 3 * L->sp / 64, count);
   L->o_parts = take((int64_t)std::max({L->cut_s.parts, L->cut_p.parts, L->cut_x.parts}));
   L->total = at;
   return DMM_OK;
@@ -265,7 +265,7 @@ int dmm_orthogonalize(const dmm_matrix_desc *X, int32_t count, int x_dtype, cons
       g.symmetric = symmetric;
       g.m = (int32_t)m;
       g.n = (int32_t)n;
-      g.steps = (int32_t)(kp / 32);
+      g.steps = (int32_t)(kp / 64);
       g.k_pitch_a = g.k_pitch_b = (uint32_t)(kp * 2);
       g.tiles_m = c.tiles_m;
       g.tiles_n = c.tiles_n;

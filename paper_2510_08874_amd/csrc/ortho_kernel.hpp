@@ -135,7 +135,7 @@ typedef _Float16 ortho_h8 __attribute__((ext_vector_type(8)));
 // row-wise planes; the values replace the sums.
 __device__ __forceinline__ void ortho_rows8(const OrthoProduct &g, char *ws, int row, int col, float *v) {
   const int64_t at = (int64_t)row * g.out_pitch + col;
-  if (row >= g.m || (unsigned)col >= g.out_pitch) {           // (out_pitch is a multiple of 32)
+  if (row >= g.m || (unsigned)col >= g.out_pitch) {           // (out_pitch is a multiple of 64)
 #pragma unroll
     for (int x = 0; x < 8; ++x) v[x] = 0.f;
     return;
@@ -245,7 +245,7 @@ __global__ __launch_bounds__(NT_THREADS, SH::TM == 256 ? 1 : 2) void ortho_produ
       s.a_pitch = g.k_pitch_a;
       s.b_pitch = g.k_pitch_b;
       s.a_scale_pitch = s.b_scale_pitch = 0;
-      s.steps = g.steps;
+      s.chunks = 2 * g.steps;
       s.pad = 0;
       return s;
     }

@@ -20,7 +20,7 @@ constexpr int ORTHO_TILES = 64;
 struct OrthoTiles {
   int32_t n, f32;               // tiles; fp32 or bf16
   int32_t rows, cols;
-  int32_t row_pitch, col_pitch; // elements of a row of the two layouts: columns (rows) up to a multiple of 32
+  int32_t row_pitch, col_pitch; // elements of a row of the two layouts: columns (rows) up to a multiple of 64
   int64_t stride;               // bytes from one matrix' buffers to the next
   char *ws;
   int64_t by_rows, by_cols;     // planes [rows][row_pitch] and [cols][col_pitch], the low parts right behind the high ones
@@ -41,7 +41,7 @@ struct OrthoProduct {
   uint32_t k_pitch_a, k_pitch_b;   // bytes
   uint32_t out_pitch, turned_pitch;   // elements
   int32_t m, n;                 // out: m x n (columns up to out_pitch are zero, and rows up to turned_pitch)
-  int32_t steps;                // 32 of k each
+  int32_t steps;                // 64 of k each
   int32_t y_turned;             // ... transposed
   int32_t symmetric;            // out is: tiles below the diagonal come from those above
   int32_t count, tiles, tiles_m, tiles_n;   // matrices; tiles of each, in rows and columns
