@@ -48,6 +48,12 @@ __device__ __forceinline__ void nt_load16(nt_gptr base, unsigned lane_off, unsig
 __device__ __forceinline__ void nt_load4(nt_gptr base, unsigned lane_off, unsigned lds) {
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" : : "v"(lane_off), "s"(base), "s"(lds) : "memory");
 }
+// (mask: all lanes or none)
+__device__ __forceinline__ void nt_load16_masked(nt_gptr base, unsigned lane_off, unsigned lds, unsigned mask) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_mov_b32 exec_lo, %3\n\ts_mov_b32 exec_hi, %3\n\t"
+               "global_load_lds_dwordx4 %0, %1\n\ts_mov_b64 exec, -1"
+               : : "v"(lane_off), "s"(base), "s"(lds), "s"(mask) : "memory");
+}
 template <int N>
 __device__ __forceinline__ void nt_wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
@@ -77,9 +83,9 @@ struct NtShape {
   static constexpr int S_ROW = 16, S_SLOT = SCALED ? (TM + TN) * S_ROW : 0;
   static constexpr int LDS = 2 * STAGE + 3 * S_SLOT;
   static constexpr int LA = TM / 32, LB = TN / 32;           // 1 KB loads of a wave and step, 8 rows each
-  static constexpr int LOADS = LA + LB, EARLY = LOADS / 2;   // half of them behind the barrier, half in the next step's first quarter
-  static constexpr int LS = SCALED ? (TM + TN) / 64 : 0;     // 16-row loads of scales of a wave, for two steps
-  static_assert(TM % 128 == 0 && TN % 128 == 0, "a wave loads whole rows of scales of one operand");
+  static constexpr int LOADS = LA + LB, EARLY = LOADS / 2;   // so many behind the barrier, the others in the next step's first quarter
+  static constexpr int S_ROWS = SCALED ? (TM + TN) / 4 : 0;  // rows whose scales a wave loads
+  static_assert(TM == TN && TM % 128 == 0, "a wave loads 64 or 128 rows of scales of one operand");
 };
 
 // Rows of a macro-tile past `ext` are read from its last row: they are never stored.
@@ -121,7 +127,7 @@ struct NtTile {
   // step in it; `steps`: in all.  A segment of an odd number of chunks ends with half a step.
   template <class Segs>
   __device__ __forceinline__ void run(const Segs &segs, int n_segs, int first, int steps, int m_off, int m_ext, int n_off, int n_ext, char *lds) {
-    constexpr int MI = SH::MI, NI = SH::NI, LA = SH::LA, LB = SH::LB, LS = SH::LS;
+    constexpr int MI = SH::MI, NI = SH::NI, LA = SH::LA, LB = SH::LB;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave >> 1, wn = wave & 1;
@@ -138,9 +144,13 @@ struct NtTile {
     const int slot = (lane & 7) ^ nt_swizzle(row8);          // (load x is 32 rows on: the same)
     unsigned aoff[LA], boff[LB];
     nt_gptr a = nullptr, b = nullptr;
-    const char *as = nullptr, *bs = nullptr;                  // scales of row 0 at the segment's next step
-    unsigned as_pitch = 0, bs_pitch = 0;
     int chunks = 0, on = NT_ROW;                              // chunks left to load in this segment; bytes from one step to the next
+    // scales: a wave loads those of rows row_s ... of one operand, at sp those of row 0 and the segment's next two steps
+    const bool s_is_a = wave < 2;
+    const int row_s = (wave & 1) * SH::S_ROWS, ext_s = (s_is_a ? m_ext : n_ext) - 1;
+    nt_gptr sp = nullptr;
+    unsigned s_pitch = 0, soff[2];
+    bool s_wide = false;                                      // 16 bytes of a row at a time
     auto enter = [&](const NtSeg &s, int skip) {
       chunks = s.chunks - 2 * skip;
       a = nt_uniform(s.a + (int64_t)m_off * s.a_pitch + (int64_t)skip * NT_ROW);
@@ -150,10 +160,11 @@ struct NtTile {
 #pragma unroll
       for (int x = 0; x < LB; ++x) boff[x] = (unsigned)min(32 * x + row8, n_ext - 1) * s.b_pitch + slot * 16;
       if constexpr (SH::SCALED) {
-        as = s.a_scale + (int64_t)m_off * s.a_scale_pitch + (int64_t)skip * 8;
-        bs = s.b_scale + (int64_t)n_off * s.b_scale_pitch + (int64_t)skip * 8;
-        as_pitch = s.a_scale_pitch;
-        bs_pitch = s.b_scale_pitch;
+        s_pitch = s_is_a ? s.a_scale_pitch : s.b_scale_pitch;
+        sp = nt_uniform((s_is_a ? s.a_scale : s.b_scale) + (int64_t)(s_is_a ? m_off : n_off) * s_pitch + (int64_t)skip * 8);
+        s_wide = (((unsigned)(uintptr_t)sp | s_pitch) & 15) == 0;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) soff[x] = (unsigned)min(row_s + 64 * x + lane, ext_s) * s_pitch;
       }
     };
     // The step that is loaded next is half a one: the lanes of what is missing read the half that is there, and count for nothing, since
@@ -173,41 +184,49 @@ struct NtTile {
       if constexpr (X < LA) nt_load16(a, aoff[X], base + (4 * X + wave) * 1024);
       else nt_load16(b, boff[X - LA], base + SH::A_BYTES + (4 * (X - LA) + wave) * 1024);
     };
-    // Scales of the next two steps of the segment, into the next slot: a wave's rows are of one operand.
-    int s_left = 0;                                           // steps whose scales are in the slot and that are yet to be loaded
-    unsigned s_at = 0, s_slot = 2 * SH::S_SLOT;               // ... of the step loaded next; the slot filled last
+    // Scales of two steps at a time, in one of three slots: one may be being read, one has those of the step behind.
+    int s_left = 0;                                           // steps that the slot has scales of and that are yet to be loaded
+    unsigned s_at = 0, s_slot = 2 * SH::S_SLOT;               // where those of the step loaded next are; the slot filled last
+    unsigned s_next_at = 0;                                   // ... of the step loaded last
+    auto s_behind = [&]() { return s_slot == 2 * SH::S_SLOT ? 0 : s_slot + SH::S_SLOT; };
+    // Of the two steps that follow, at once and word by word: in front of a segment, at its end, and where scales lie at
+    // odd places.  What is missing is 2^-127.
     auto load_scales = [&]() {
       if constexpr (SH::SCALED) {
-        // (of three: one is being read by waves that are late, one has the scales of the next step)
-        s_slot = s_slot == 2 * SH::S_SLOT ? 0 : s_slot + SH::S_SLOT;
-        s_at = s_slot;
-        s_left = chunks > 2 ? 2 : 1;
-        const bool is_a = wave < 2;
-        const int ext = is_a ? m_ext : n_ext, row0 = (wave & 1) * (SH::TM / 2) + (lane >> 2), n = chunks < 4 ? chunks : 4;
-        const unsigned pitch = is_a ? as_pitch : bs_pitch, d = lane & 3;
-        const nt_gptr p = nt_uniform(is_a ? as : bs);
-        const unsigned to = 2 * SH::STAGE + s_slot + wave * (LS * 16 * SH::S_ROW);
+        const int n = chunks < 4 ? chunks : 4;
+        const unsigned d = lane & 3, to = 2 * SH::STAGE + s_slot + wave * (SH::S_ROWS * SH::S_ROW);
         if (n == 4) {
 #pragma unroll
-          for (int x = 0; x < LS; ++x) nt_load4(p, (unsigned)min(row0 + 16 * x, ext - 1) * pitch + d * 4, lds0 + to + x * 256);
+          for (int x = 0; x < SH::S_ROWS / 16; ++x) nt_load4(sp, (unsigned)min(row_s + 16 * x + (lane >> 2), ext_s) * s_pitch + d * 4, lds0 + to + x * 256);
         } else {
-          for (int x = 0; x < LS; ++x) {
+          for (int x = 0; x < SH::S_ROWS / 16; ++x) {
             int v = 0;
-            if ((int)d < n) v = *(const __attribute__((address_space(1))) int *)(p + ((unsigned)min(row0 + 16 * x, ext - 1) * pitch + d * 4));
+            if ((int)d < n) v = *(const __attribute__((address_space(1))) int *)(sp + ((unsigned)min(row_s + 16 * x + (lane >> 2), ext_s) * s_pitch + d * 4));
             *(__attribute__((address_space(3))) int *)((nt_lptr)lds + to + x * 256 + lane * 4) = v;
           }
         }
-        as += 16;
-        bs += 16;
       }
     };
-    static_assert(SH::TM == SH::TN, "a wave's rows of scales");
+    auto new_slot = [&]() {
+      s_slot = s_behind();
+      s_at = s_slot;
+      s_left = chunks > 2 ? 2 : 1;
+    };
+    // Elsewhere those of the next two steps are loaded during these two, 64 rows of a wave with each.
+    auto load_scales_ahead = [&]() {
+      if constexpr (SH::SCALED) {
+        const bool second = s_left != 2;
+        const bool wanted = s_wide && chunks >= (second ? 6 : 8) && (!second || SH::S_ROWS > 64);
+        nt_load16_masked(sp, (second ? soff[1] : soff[0]) + 16, lds0 + 2 * SH::STAGE + s_behind() + (wave * SH::S_ROWS + (second ? 64 : 0)) * SH::S_ROW,
+                         (unsigned)__builtin_amdgcn_readfirstlane(wanted ? -1 : 0));
+      }
+    };
     int seg = 0;
     enter(segs[0], first);
     halve();
+    new_slot();
     load_scales();
     // to the next step to load.  Past the last one its operands are loaded again, to be read by nobody.
-    unsigned s_next_at = 0;                                   // where the scales of the step loaded last are
     auto next = [&]() {
       a += on;
       b += on;
@@ -218,22 +237,25 @@ struct NtTile {
         --s_left;
       }
       if (chunks <= 2 || (SH::SCALED && s_left == 0)) {
+        bool fresh = s_left == 0, front = false;
         if (chunks <= 0) {
           if (++seg < n_segs) {
             enter(segs[seg], 0);
-            halve();
-            load_scales();
+            fresh = front = true;
           } else {
             a -= on;
             b -= on;
             on = 0;
-            chunks = 1 << 30;
-            s_left = 1 << 30;
-            s_at = s_slot;
+            chunks = s_left = 1 << 30;
+            s_wide = fresh = false;
           }
-        } else {
-          halve();
-          if (s_left == 0) load_scales();
+        } else if (SH::SCALED && fresh) {
+          sp += 16;
+        }
+        halve();
+        if (SH::SCALED && fresh) {
+          new_slot();
+          if (front || !s_wide || chunks < 4) load_scales();
         }
       }
     };
@@ -259,24 +281,20 @@ struct NtTile {
       if constexpr (X < MI) f.a[X] = *(const __attribute__((address_space(3))) nt_i32x4 *)(fa + o + X * 32 * NT_ROW);
       else f.b[X - MI] = *(const __attribute__((address_space(3))) nt_i32x4 *)(fb + o + (X - MI) * 32 * NT_ROW);
     };
-    auto read_scales = [&](Scale &f, unsigned at) {
+    auto read_scale = [&](Scale &f, auto xc, unsigned at) {
       if constexpr (SH::SCALED) {
+        constexpr int X = decltype(xc)::value;
         const nt_lptr p = fs + at;
-#pragma unroll
-        for (int i = 0; i < MI; ++i) f.a[i] = *(const __attribute__((address_space(3))) nt_i32x2 *)(p + (wm * (SH::TM / 2) + 32 * i) * SH::S_ROW);
-#pragma unroll
-        for (int j = 0; j < NI; ++j) f.b[j] = *(const __attribute__((address_space(3))) nt_i32x2 *)(p + (SH::TM + wn * (SH::TN / 2) + 32 * j) * SH::S_ROW);
+        if constexpr (X < MI) f.a[X] = *(const __attribute__((address_space(3))) nt_i32x2 *)(p + (wm * (SH::TM / 2) + 32 * X) * SH::S_ROW);
+        else f.b[X - MI] = *(const __attribute__((address_space(3))) nt_i32x2 *)(p + (SH::TM + wn * (SH::TN / 2) + 32 * (X - MI)) * SH::S_ROW);
       }
     };
-    auto shift = [&](Scale &f) {
+    auto shift = [&](Scale &f, auto xc) {
       if constexpr (SH::SCALED) {
-#pragma unroll
-        for (int w = 0; w < 2; ++w) {
-#pragma unroll
-          for (int i = 0; i < MI; ++i) f.a[i][w] = (int)((unsigned)f.a[i][w] >> (8 * g));
-#pragma unroll
-          for (int j = 0; j < NI; ++j) f.b[j][w] = (int)((unsigned)f.b[j][w] >> (8 * g));
-        }
+        constexpr int X = decltype(xc)::value;
+        nt_i32x2 &v = X < MI ? f.a[X < MI ? X : 0] : f.b[X < MI ? 0 : X - MI];
+        v[0] = (int)((unsigned)v[0] >> (8 * g));
+        v[1] = (int)((unsigned)v[1] >> (8 * g));
       }
     };
     auto multiply = [&](const Frag &f, const Scale &s, auto tc, auto hc) {
@@ -313,6 +331,7 @@ struct NtTile {
     // ---- the steps ---------------------------------------------------------------------------
     // in front: step 0 and half of step 1 under way, the first quarter of step 0 read
     nt_for<SH::LOADS>([&](auto xc) { load(xc, lds0); });
+    load_scales_ahead();
     next();
     nt_for<SH::EARLY>([&](auto xc) { load(xc, lds0 + SH::STAGE); });
     nt_wait_loads<SH::EARLY>();                               // (and the scales, older or behind a wait of their own)
@@ -321,18 +340,19 @@ struct NtTile {
     asm volatile("" ::: "memory");
     Frag f0, f1;
     Scale s, s_next;
-    read_scales(s, s_next_at);
+    nt_for<R>([&](auto xc) { read_scale(s, xc, s_next_at); });
+    nt_for<R>([&](auto xc) { shift(s, xc); });
     nt_for<R>([&](auto xc) { read(f0, xc, 0, h0); });
     unsigned now = 0;                                         // stage of the current step
 #pragma clang loop unroll(disable)
     for (int t = steps; t > 0; --t) {
-      shift(s);
       const unsigned other = SH::STAGE - now;
       quarter(f0, s, h0, f1, now, [&](auto tc) {              // ... and the rest of the next step's loads
         nt_for<SH::LOADS>([&](auto xc) {
           constexpr int X = decltype(xc)::value - SH::EARLY;
           if constexpr (X >= 0 && X * T / (SH::LOADS - SH::EARLY) == decltype(tc)::value) load(xc, lds0 + other);
         });
+        if constexpr (decltype(tc)::value == T - 1) load_scales_ahead();
       });
       pin();
       next();
@@ -342,11 +362,13 @@ struct NtTile {
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // and this one's last fragments are read
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
-      read_scales(s_next, s_next_at);
-      __builtin_amdgcn_sched_barrier(0);
-      quarter(f1, s, h3, f0, other, [&](auto tc) {            // ... and half of the loads of the step behind it
+      quarter(f1, s, h3, f0, other, [&](auto tc) {            // ... and half of the loads of the step behind it, and the next scales
         nt_for<SH::EARLY>([&](auto xc) {
           if constexpr (decltype(xc)::value * T / SH::EARLY == decltype(tc)::value) load(xc, lds0 + now);
+        });
+        nt_for<R>([&](auto xc) {
+          if constexpr (decltype(xc)::value * T / 2 / R == decltype(tc)::value) read_scale(s_next, xc, s_next_at);
+          if constexpr (T / 2 + decltype(xc)::value * T / 2 / R == decltype(tc)::value) shift(s_next, xc);
         });
       });
       now = other;
