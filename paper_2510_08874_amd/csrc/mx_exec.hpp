@@ -405,7 +405,7 @@ int dmm_mx_execute(dmm_plan_t *P, const dmm_mx_tiles *a, const dmm_mx_tiles *b, 
     if ((rc = P->dev->uses.claim(stream, &behind))) return rc;
     const char *d = M.table.dev();
     bool marked = mx_launch(red.n_items ? nullptr : behind, L.shape, (const MxItem *)d, L.n_items, (const NtSeg *)(d + L.o_segs),
-                            (const MxJoin *)(d + L.o_joins), L.n_joins, stream);
+                            (const MxJoin *)(d + L.o_joins), L.n_joins, cus, stream);
     DMM_HIP(hipGetLastError());
     if (red.n_items && (rc = fire_reduce(P, red, stream, false, behind, &marked))) return rc;
     return marked ? DMM_OK : P->dev->uses.mark(stream);

@@ -4,8 +4,9 @@
 namespace dmm {
 namespace {
 
-using Mx256 = NtShape<true, 256, 256>;
-using Mx128 = NtShape<true, 128, 128>;
+using Mx256 = NtShape<true, 256>;
+using Mx128 = NtShape<true, 128>;            // two workgroups on a CU
+using Mx128Deep = NtShape<true, 128, 4>;     // one, which then has three steps on their way
 static_assert(kMxShape[MX_256].tm == Mx256::TM && kMxShape[MX_256].tn == Mx256::TN && kMxShape[MX_128].tm == Mx128::TM &&
                   kMxShape[MX_128].tn == Mx128::TN && kMxShape[MX_SKINNY_16].tn == 16 && kMxShape[MX_SKINNY_32].tn == 32 &&
                   kMxShape[MX_SKINNY_64].tn == 32,
@@ -24,6 +25,7 @@ constexpr int turn_lds() { return 128 * (128 * (F32 ? 4 : 2) + 4); }
 hipError_t mx_allow_lds() {
   hipError_t e = hipFuncSetAttribute((const void *)mx_gemm_kernel<Mx256>, hipFuncAttributeMaxDynamicSharedMemorySize, Mx256::LDS);
   if (e == hipSuccess) e = hipFuncSetAttribute((const void *)mx_gemm_kernel<Mx128>, hipFuncAttributeMaxDynamicSharedMemorySize, Mx128::LDS);
+  if (e == hipSuccess) e = hipFuncSetAttribute((const void *)mx_gemm_kernel<Mx128Deep>, hipFuncAttributeMaxDynamicSharedMemorySize, Mx128Deep::LDS);
   // (128 rows of fp32 with their extra words: 64.5 KB)
   const void *turn[3] = {(const void *)mx_cols_kernel<true, false>, (const void *)mx_cols_kernel<true, true>, (const void *)mx_col_values_kernel<true>};
   for (const void *f : turn)
@@ -31,12 +33,12 @@ hipError_t mx_allow_lds() {
   return e;
 }
 
-bool mx_launch(hipEvent_t behind, int shape, const MxItem *items, int n_items, const NtSeg *segs, const MxJoin *joins, int n_joins, hipStream_t stream) {
+bool mx_launch(hipEvent_t behind, int shape, const MxItem *items, int n_items, const NtSeg *segs, const MxJoin *joins, int n_joins, int cus, hipStream_t stream) {
   const hipEvent_t last = n_joins ? nullptr : behind;
   bool marked = false;
   switch (shape) {
     case MX_256: marked = launch<Mx256>(last, items, n_items, segs, stream); break;
-    case MX_128: marked = launch<Mx128>(last, items, n_items, segs, stream); break;
+    case MX_128: marked = n_items <= cus ? launch<Mx128Deep>(last, items, n_items, segs, stream) : launch<Mx128>(last, items, n_items, segs, stream); break;
     case MX_SKINNY_16: marked = launch_behind(last, mx_skinny_kernel<1, 1>, (unsigned)n_items, NT_THREADS, 0, stream, items, segs); break;
     case MX_SKINNY_32: marked = launch_behind(last, mx_skinny_kernel<2, 2>, (unsigned)n_items, NT_THREADS, 0, stream, items, segs); break;
     default: marked = launch_behind(last, mx_skinny_kernel<4, 2>, (unsigned)n_items, NT_THREADS, 0, stream, items, segs); break;

@@ -46,7 +46,7 @@ __device__ __forceinline__ void mx_store(const NtTile<SH> &tile, const MxItem &i
 
 // Macro-tiles.
 template <class SH>
-__global__ __launch_bounds__(NT_THREADS, SH::TM == 256 ? 1 : 2) void mx_gemm_kernel(const MxItem *__restrict__ items, const NtSeg *__restrict__ segs) {
+__global__ __launch_bounds__(NT_THREADS, SH::LDS > 80 * 1024 ? 1 : 2) void mx_gemm_kernel(const MxItem *__restrict__ items, const NtSeg *__restrict__ segs) {
   extern __shared__ char lds[];
   const MxItem it = items[blockIdx.x];
   NtTile<SH> tile;

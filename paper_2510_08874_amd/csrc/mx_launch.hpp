@@ -63,7 +63,7 @@ constexpr MxShape kMxShape[MX_SHAPES] = {{256, 256}, {128, 128}, {16, 16}, {32, 
 enum { MX_ALONG_ROWS = 1, MX_ALONG_COLS = 2 };
 
 hipError_t mx_allow_lds();
-bool mx_launch(hipEvent_t behind, int shape, const MxItem *items, int n_items, const NtSeg *segs, const MxJoin *joins, int n_joins, hipStream_t stream);
+bool mx_launch(hipEvent_t behind, int shape, const MxItem *items, int n_items, const NtSeg *segs, const MxJoin *joins, int n_joins, int cus, hipStream_t stream);
 // rows that a wave takes at a time, when there are `units` pieces of 512 columns of a row in all
 int mx_rows_per_unit(int64_t units);
 void mx_quantize_launch(const MxTileArgs &args, int blocks, bool f32, int along, int rows_per_unit, hipStream_t stream);

@@ -2,17 +2,20 @@
 // A[m][k] B[n][k], in macro-tiles that one workgroup of four waves accumulates in registers.  Shared by the
 // products of 4-bit microscaled operands (mx_kernel.hpp) and of fp16 pairs (ortho_kernel.hpp): both feed a matrix
 // instruction with 32 bytes of K a row, 16 in each half of the lanes, so a step, its stage in LDS and its loads are the same:
-//   fp4   32 x 32 x 64: a lane holds 32 codes of one row, which share one scale
-//   fp16  32 x 32 x 16: a lane holds 8 values of one row
+//   fp4    32 x 32 x 64: a lane holds 32 codes of one row, which share one scale; a step is 256 codes of a row
+//   pairs  32 x 32 x 16: a lane holds 8 values of one row; a step is 32 values as high parts (64 bytes) and low parts, whose
+//          three products (low high, high low, high high) use what is in LDS three times for two reads
 //
-// What bounds a 256 x 256 tile: a step of 128 bytes a row is 64 matrix instructions of 32 cycles on each of the four
-// matrix pipes (2048 cycles), 128 KB of LDS reads (1024 cycles at 128 bytes), 64 KB written to LDS by the loads (512) and 64
+// What bounds a 256 x 256 tile: a step of 128 bytes a row is 64 (pairs: 96) matrix instructions of 32 cycles on each of the four
+// matrix pipes (2048 or 3072 cycles), 128 KB of LDS reads (1024 cycles at 128 bytes), 64 KB written to LDS by the loads (512) and 64
 // KB from L2.  L2 answers requests of up to 128 bytes, 16 of them a cycle to the 32 CUs of an XCD: 512 rows
 // of 128 bytes take 1024 cycles, so the rows of a step are whole lines.  (With steps of 64 bytes, and four bytes of scales a row
 // and step, there were four times as many requests: 16384 x 8192 x 28672 in 4 bits 2.42 ms, matrix pipes busy 35 %.)
-// The pipes can be kept busy if nothing waits: operands go straight into two LDS stages, and the fragments of a
+// The pipes can be kept busy if nothing waits: operands go straight into LDS stages, and the fragments of a
 // quarter of a step are read during the quarter before it, between its matrix instructions.  One barrier a step, in front of its last
-// quarter: behind it the next stage may be read, and the stage whose last fragments every wave holds may be filled.
+// quarter (pairs: half): behind it the next stage may be read, and the stage whose last fragments every wave holds may be filled.
+// The part lowers its clock under matrix load: a loop of matrix instructions on registers alone makes 6.5 PFLOP/s in fp4
+// and 1.8 in fp16 with random operands (9.7 and 2.5 with zeros), and a kernel that also moves operands has less power left for it.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -36,7 +39,7 @@ typedef __attribute__((address_space(3))) char *nt_lptr;
 
 constexpr int NT_THREADS = 256;
 constexpr int NT_ROW = 128;                // bytes of a row in one step
-constexpr int NT_CHUNK = 64;               // what a segment's length is given in: 128 codes, 32 fp16
+constexpr int NT_CHUNK = 64;               // what a segment's length is given in: 128 codes, 16 pairs
 
 // 16-byte slots of a 128-byte row are exchanged by row, so that 16 lanes that read one slot of 16 rows fall
 // into different banks.
@@ -72,18 +75,21 @@ __device__ __forceinline__ void nt_for(F &&f) {
   nt_for_impl<N>(std::make_integer_sequence<int, N>{}, f);
 }
 
-// SCALED: 4-bit codes with scales; otherwise fp16.  TM x TN macro-tile over 2 x 2 waves.
-template <bool SCALED_, int TM_, int TN_>
+// SCALED: 4-bit codes with scales; otherwise pairs of fp16.  EDGE x EDGE macro-tile over 2 x 2 waves, NST stages.
+template <bool SCALED_, int EDGE, int NST_ = 2>
 struct NtShape {
   static constexpr bool SCALED = SCALED_;
-  static constexpr int TM = TM_, TN = TN_;
+  static constexpr int TM = EDGE, TN = EDGE, NST = NST_;
   static constexpr int MI = TM / 64, NI = TN / 64;           // 32 x 32 tiles of a wave
   static constexpr int A_BYTES = TM * NT_ROW, B_BYTES = TN * NT_ROW, STAGE = A_BYTES + B_BYTES;
   // scales of two steps together, 16 bytes a row: a request fetches them once
   static constexpr int S_ROW = 16, S_SLOT = SCALED ? (TM + TN) * S_ROW : 0;
-  static constexpr int LDS = 2 * STAGE + 3 * S_SLOT;
+  // slots: of the step whose scales are read, of those under way, and of the one behind them; every step may be a segment's last
+  static constexpr int SLOTS = NST + 1;
+  static constexpr int LDS = NST * STAGE + SLOTS * S_SLOT;
   static constexpr int LA = TM / 32, LB = TN / 32;           // 1 KB loads of a wave and step, 8 rows each
-  static constexpr int LOADS = LA + LB, EARLY = LOADS / 2;   // so many behind the barrier, the others in the next step's first quarter
+  static constexpr int LOADS = LA + LB;
+  static constexpr int EARLY = SCALED ? LOADS / 2 : LOADS;   // so many behind the barrier, the others in the next step's first quarter
   static constexpr int S_ROWS = SCALED ? (TM + TN) / 4 : 0;  // rows whose scales a wave loads
   static_assert(TM == TN && TM % 128 == 0, "a wave loads 64 or 128 rows of scales of one operand");
 };
@@ -184,17 +190,17 @@ struct NtTile {
       if constexpr (X < LA) nt_load16(a, aoff[X], base + (4 * X + wave) * 1024);
       else nt_load16(b, boff[X - LA], base + SH::A_BYTES + (4 * (X - LA) + wave) * 1024);
     };
-    // Scales of two steps at a time, in one of three slots: one may be being read, one has those of the step behind.
+    // Scales of two steps at a time, in the next slot.
     int s_left = 0;                                           // steps that the slot has scales of and that are yet to be loaded
-    unsigned s_at = 0, s_slot = 2 * SH::S_SLOT;               // where those of the step loaded next are; the slot filled last
-    unsigned s_next_at = 0;                                   // ... of the step loaded last
-    auto s_behind = [&]() { return s_slot == 2 * SH::S_SLOT ? 0 : s_slot + SH::S_SLOT; };
+    unsigned s_at = 0, s_slot = (SH::SLOTS - 1) * SH::S_SLOT; // where those of the step loaded next are; the slot filled last
+    unsigned s_loaded[SH::NST - 1] = {};                      // ... of the last NST - 1 steps loaded, in their order
+    auto s_behind = [&]() { return s_slot == (SH::SLOTS - 1) * SH::S_SLOT ? 0 : s_slot + SH::S_SLOT; };
     // Of the two steps that follow, at once and word by word: in front of a segment, at its end, and where scales lie at
     // odd places.  What is missing is 2^-127.
     auto load_scales = [&]() {
       if constexpr (SH::SCALED) {
         const int n = chunks < 4 ? chunks : 4;
-        const unsigned d = lane & 3, to = 2 * SH::STAGE + s_slot + wave * (SH::S_ROWS * SH::S_ROW);
+        const unsigned d = lane & 3, to = SH::NST * SH::STAGE + s_slot + wave * (SH::S_ROWS * SH::S_ROW);
         if (n == 4) {
 #pragma unroll
           for (int x = 0; x < SH::S_ROWS / 16; ++x) nt_load4(sp, (unsigned)min(row_s + 16 * x + (lane >> 2), ext_s) * s_pitch + d * 4, lds0 + to + x * 256);
@@ -217,7 +223,7 @@ struct NtTile {
       if constexpr (SH::SCALED) {
         const bool second = s_left != 2;
         const bool wanted = s_wide && chunks >= (second ? 6 : 8) && (!second || SH::S_ROWS > 64);
-        nt_load16_masked(sp, (second ? soff[1] : soff[0]) + 16, lds0 + 2 * SH::STAGE + s_behind() + (wave * SH::S_ROWS + (second ? 64 : 0)) * SH::S_ROW,
+        nt_load16_masked(sp, (second ? soff[1] : soff[0]) + 16, lds0 + SH::NST * SH::STAGE + s_behind() + (wave * SH::S_ROWS + (second ? 64 : 0)) * SH::S_ROW,
                          (unsigned)__builtin_amdgcn_readfirstlane(wanted ? -1 : 0));
       }
     };
@@ -232,7 +238,9 @@ struct NtTile {
       b += on;
       chunks -= 2;
       if constexpr (SH::SCALED) {
-        s_next_at = s_at;
+#pragma unroll
+        for (int x = 0; x + 1 < SH::NST - 1; ++x) s_loaded[x] = s_loaded[x + 1];
+        s_loaded[SH::NST - 2] = s_at;
         s_at += 8;
         --s_left;
       }
@@ -266,7 +274,7 @@ struct NtTile {
     const int r = lane & 31, g = lane >> 5;
     const nt_lptr fa = (nt_lptr)lds + wm * (SH::TM / 2) * NT_ROW + r * NT_ROW;
     const nt_lptr fb = (nt_lptr)lds + SH::A_BYTES + wn * (SH::TN / 2) * NT_ROW + r * NT_ROW;
-    const nt_lptr fs = (nt_lptr)lds + 2 * SH::STAGE + r * SH::S_ROW;
+    const nt_lptr fs = (nt_lptr)lds + SH::NST * SH::STAGE + r * SH::S_ROW;
     const int turn = (g ^ nt_swizzle(r)) * 16;                // (slot 2 h + g, exchanged)
     struct Frag {
       nt_i32x4 a[MI], b[NI];
@@ -298,13 +306,22 @@ struct NtTile {
       }
     };
     auto multiply = [&](const Frag &f, const Scale &s, auto tc, auto hc) {
-      constexpr int H = decltype(hc)::value, I = decltype(tc)::value / NI, J = decltype(tc)::value % NI;
       if constexpr (SH::SCALED) {
+        constexpr int H = decltype(hc)::value, I = decltype(tc)::value / NI, J = decltype(tc)::value % NI;
         const nt_i32x8 x = {f.a[I][0], f.a[I][1], f.a[I][2], f.a[I][3], 0, 0, 0, 0};
         const nt_i32x8 y = {f.b[J][0], f.b[J][1], f.b[J][2], f.b[J][3], 0, 0, 0, 0};
         acc[I][J] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, acc[I][J], 4, 4, 2 * (H & 1), s.a[I][H >> 1], 2 * (H & 1), s.b[J][H >> 1]);
-      } else {
-        acc[I][J] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(nt_f16x8, f.a[I]), __builtin_bit_cast(nt_f16x8, f.b[J]), acc[I][J], 0, 0, 0);
+      }
+    };
+    // of pairs: a's part times b's (0: high, 1: low)
+    struct Pair {
+      Frag part[SH::SCALED ? 1 : 2];
+    };
+    auto multiply_pair = [&](const Pair &f, auto tc, auto ac, auto bc) {
+      if constexpr (!SH::SCALED) {
+        constexpr int I = decltype(tc)::value / NI, J = decltype(tc)::value % NI;
+        acc[I][J] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(nt_f16x8, f.part[decltype(ac)::value].a[I]),
+                                                           __builtin_bit_cast(nt_f16x8, f.part[decltype(bc)::value].b[J]), acc[I][J], 0, 0, 0);
       }
     };
     constexpr int T = MI * NI, R = MI + NI;
@@ -322,6 +339,22 @@ struct NtTile {
         __builtin_amdgcn_sched_barrier(0);
       });
     };
+    // Half h of a step of pairs (values 16 h ...): the small products first.  Reads half 1 - h of `stage` into `into`.
+    auto half = [&](const Pair &f, auto hc, Pair &into, unsigned stage, auto also) {
+      constexpr int H = decltype(hc)::value;
+      nt_for<3 * T>([&](auto tc) {
+        constexpr int I = decltype(tc)::value;
+        multiply_pair(f, std::integral_constant<int, I % T>{}, std::integral_constant<int, I < T>{}, std::integral_constant<int, I / T == 1>{});
+        nt_for<2 * R>([&](auto xc) {
+          constexpr int X = decltype(xc)::value;
+          // (in the order of their use: low parts of A, high ones of B, ...)
+          if constexpr (X * 3 * T / (2 * R) == I) read(into.part[X < R ? (X < MI) : (X - R >= MI)], std::integral_constant<int, X % R>{}, stage,
+                                                       std::integral_constant<int, 1 - H + 2 * (X < R ? (X < MI) : (X - R >= MI))>{});
+        });
+        also(tc);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    };
     std::integral_constant<int, 0> h0;
     std::integral_constant<int, 1> h1;
     std::integral_constant<int, 2> h2;
@@ -329,50 +362,82 @@ struct NtTile {
     auto nothing = [](auto) {};
 
     // ---- the steps ---------------------------------------------------------------------------
-    // in front: step 0 and half of step 1 under way, the first quarter of step 0 read
-    nt_for<SH::LOADS>([&](auto xc) { load(xc, lds0); });
-    load_scales_ahead();
-    next();
-    nt_for<SH::EARLY>([&](auto xc) { load(xc, lds0 + SH::STAGE); });
-    nt_wait_loads<SH::EARLY>();                               // (and the scales, older or behind a wait of their own)
+    // in front: all stages but half of one under way, the first fragments of step 0 read
+    unsigned s_first = 0;
+#pragma unroll
+    for (int x = 0; x < SH::NST - 1; ++x) {
+      nt_for<SH::LOADS>([&](auto xc) { load(xc, lds0 + x * SH::STAGE); });
+      load_scales_ahead();
+      next();
+      if (x == 0) s_first = s_loaded[SH::NST - 2];
+    }
+    nt_for<SH::EARLY>([&](auto xc) { load(xc, lds0 + (SH::NST - 1) * SH::STAGE); });
+    nt_wait_loads<(SH::NST - 2) * SH::LOADS + SH::EARLY>();   // (and the step's scales, older or behind a wait of their own)
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    Frag f0, f1;
-    Scale s, s_next;
-    nt_for<R>([&](auto xc) { read_scale(s, xc, s_next_at); });
-    nt_for<R>([&](auto xc) { shift(s, xc); });
-    nt_for<R>([&](auto xc) { read(f0, xc, 0, h0); });
-    unsigned now = 0;                                         // stage of the current step
+    unsigned now = 0, before = (SH::NST - 1) * SH::STAGE;     // stages of the current step and of the one before it
+    if constexpr (SH::SCALED) {
+      Frag f0, f1;
+      Scale s, s_next;
+      nt_for<R>([&](auto xc) { read_scale(s, xc, s_first); });
+      nt_for<R>([&](auto xc) { shift(s, xc); });
+      nt_for<R>([&](auto xc) { read(f0, xc, 0, h0); });
 #pragma clang loop unroll(disable)
-    for (int t = steps; t > 0; --t) {
-      const unsigned other = SH::STAGE - now;
-      quarter(f0, s, h0, f1, now, [&](auto tc) {              // ... and the rest of the next step's loads
-        nt_for<SH::LOADS>([&](auto xc) {
-          constexpr int X = decltype(xc)::value - SH::EARLY;
-          if constexpr (X >= 0 && X * T / (SH::LOADS - SH::EARLY) == decltype(tc)::value) load(xc, lds0 + other);
+      for (int t = steps; t > 0; --t) {
+        const unsigned behind = now == (SH::NST - 1) * SH::STAGE ? 0 : now + SH::STAGE;
+        quarter(f0, s, h0, f1, now, [&](auto tc) {            // ... and the rest of the loads that the step before began
+          nt_for<SH::LOADS>([&](auto xc) {
+            constexpr int X = decltype(xc)::value - SH::EARLY;
+            if constexpr (X >= 0 && X * T / (SH::LOADS - SH::EARLY) == decltype(tc)::value) load(xc, lds0 + before);
+          });
+          if constexpr (decltype(tc)::value == T - 1) load_scales_ahead();
         });
-        if constexpr (decltype(tc)::value == T - 1) load_scales_ahead();
-      });
-      pin();
+        pin();
+        next();
+        quarter(f1, s, h1, f0, now, nothing);
+        quarter(f0, s, h2, f1, now, nothing);
+        nt_wait_loads<(SH::NST - 2) * SH::LOADS>();           // the next step has landed,
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");    // and this one's last fragments are read
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        quarter(f1, s, h3, f0, behind, [&](auto tc) {         // ... and half of the loads of the step that gets this one's stage
+          nt_for<SH::EARLY>([&](auto xc) {
+            if constexpr (decltype(xc)::value * T / SH::EARLY == decltype(tc)::value) load(xc, lds0 + now);
+          });
+          nt_for<R>([&](auto xc) {
+            if constexpr (decltype(xc)::value * T / 2 / R == decltype(tc)::value) read_scale(s_next, xc, s_loaded[0]);
+            if constexpr (T / 2 + decltype(xc)::value * T / 2 / R == decltype(tc)::value) shift(s_next, xc);
+          });
+        });
+        before = now;
+        now = behind;
+        s = s_next;
+      }
+    } else {
+      Pair f0, f1;
       next();
-      quarter(f1, s, h1, f0, now, nothing);
-      quarter(f0, s, h2, f1, now, nothing);
-      nt_wait_loads<0>();                                     // the next step has landed,
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // and this one's last fragments are read
-      __builtin_amdgcn_s_barrier();
-      asm volatile("" ::: "memory");
-      quarter(f1, s, h3, f0, other, [&](auto tc) {            // ... and half of the loads of the step behind it, and the next scales
-        nt_for<SH::EARLY>([&](auto xc) {
-          if constexpr (decltype(xc)::value * T / SH::EARLY == decltype(tc)::value) load(xc, lds0 + now);
-        });
-        nt_for<R>([&](auto xc) {
-          if constexpr (decltype(xc)::value * T / 2 / R == decltype(tc)::value) read_scale(s_next, xc, s_next_at);
-          if constexpr (T / 2 + decltype(xc)::value * T / 2 / R == decltype(tc)::value) shift(s_next, xc);
-        });
+      nt_for<R>([&](auto xc) {
+        read(f0.part[1], xc, 0, h2);
+        read(f0.part[0], xc, 0, h0);
       });
-      now = other;
-      s = s_next;
+#pragma clang loop unroll(disable)
+      for (int t = steps; t > 0; --t) {
+        const unsigned behind = now == (SH::NST - 1) * SH::STAGE ? 0 : now + SH::STAGE;
+        half(f0, h0, f1, now, nothing);
+        nt_wait_loads<(SH::NST - 2) * SH::LOADS>();
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        half(f1, h1, f0, behind, [&](auto tc) {               // ... and the loads of the step that gets this one's stage
+          nt_for<SH::LOADS>([&](auto xc) {
+            if constexpr (decltype(xc)::value * 3 * T / SH::LOADS == decltype(tc)::value) load(xc, lds0 + now);
+          });
+        });
+        now = behind;
+        pin();
+        next();
+      }
     }
     nt_wait_loads<0>();
   }

@@ -6,38 +6,58 @@
 namespace dmm {
 namespace {
 
-constexpr int kOrthoCus = 256;         // how products are cut along K, and so the workspace, does not depend on the device
+constexpr int kOrthoSums = 1024;       // workgroups that add up the squares of a matrix, about
+constexpr int kOrthoCus = 256;          // how products are cut along K, and so the workspace, does not depend on the device
 
 // How a symmetric (X X^T, S S) or plain (P X) product of m x n outputs and K steps is cut.
 struct OrthoCut {
   int edge, tiles_m, tiles_n, tiles, runs, per;
+  int whole;                           // tiles of all matrices that are not cut along K
   size_t parts;                        // bytes of partial sums
 };
+// Tiles that fill the device evenly are not cut; the others (all of them, where they are few) are cut along K if an
+// estimate finds that faster.
 OrthoCut ortho_cut(int64_t m, int64_t n, bool symmetric, int64_t steps, int64_t count) {
-  OrthoCut c;
-  auto cut = [&](int edge) {
+  OrthoCut best;
+  double best_us = 0.0;
+  for (int edge = 128; edge <= 256; edge += 128) {
+    OrthoCut c;
     c.edge = edge;
     c.tiles_m = (int)((m + edge - 1) / edge);
     c.tiles_n = (int)((n + edge - 1) / edge);
     c.tiles = symmetric ? c.tiles_m * (c.tiles_m + 1) / 2 : c.tiles_m * c.tiles_n;
-  };
-  cut(256);
-  if (c.tiles * count * 4 < kOrthoCus * 3) cut(128);
-  const int64_t tiles = c.tiles * count, places = c.edge == 256 ? kOrthoCus : 2 * kOrthoCus;
-  int64_t runs = tiles * 2 <= places ? std::min<int64_t>(places / tiles, steps / 4) : 1;
-  if (runs < 1) runs = 1;
-  c.per = (int)((steps + runs - 1) / runs);
-  c.runs = (int)((steps + c.per - 1) / c.per);
-  c.parts = c.runs > 1 ? (size_t)(tiles * c.runs) * (size_t)(c.edge * c.edge) * 4 : 0;
-  return c;
+    const int places = edge == 256 ? kOrthoCus : 2 * kOrthoCus;
+    const int64_t tiles = c.tiles * count, rest = tiles % places;
+    // us: a step of a tile of 256, of one of 128 that has its CU to itself (the more there are the longer L2 takes), of two; and a tile's ends
+    auto round = [&](int64_t n_tiles, int64_t n_steps) {
+      if (n_tiles == 0) return 0.0;
+      const double step = edge == 256 ? 2.2 : n_tiles > kOrthoCus ? 1.45 : 0.5 + 0.4 * (double)n_tiles / kOrthoCus;
+      return step * (double)n_steps + (edge == 256 ? 10.0 : 7.0);
+    };
+    const double whole_us = (tiles / places) * round(places, steps);
+    for (int64_t runs = 1; runs <= 32; ++runs) {
+      const int64_t per = (steps + runs - 1) / runs;
+      if (runs > 1 && (rest == 0 || rest * runs > places || per < 4 || (steps + per - 1) / per != runs)) continue;
+      const double bytes = runs > 1 ? 2.0 * rest * runs * edge * edge * 4 : 0.0;
+      const double us = whole_us + round(rest * runs, per) + (runs > 1 ? 5.0 + bytes / 3e6 : 0.0);
+      if (best_us == 0.0 || us < best_us) {
+        best_us = us;
+        best = c;
+        best.runs = (int)runs;
+        best.per = (int)per;
+        best.whole = (int)(runs > 1 ? tiles - rest : tiles);
+        best.parts = (size_t)(bytes / 2);
+      }
+    }
+  }
+  return best;
 }
 
 struct OrthoLayout {
-  int64_t s, l, sp, lp;                // fewer rows, more columns; filled up to multiples of 64
+  int64_t s, l, sp, lp;                // fewer rows, more columns; filled up to multiples of 32
   bool flip;                           // the matrix has more rows than columns: its transpose is worked on
   // byte offsets in a matrix' buffers: two generations of X by rows and by columns, S, P
   int64_t wide[2], tall[2], S, P, stride;
-  int64_t wide_plane, tall_plane, square_plane;
   int64_t tiles;                       // non-empty tiles of a matrix
   int64_t sums, o_sums, o_parts, total;
   OrthoCut cut_s, cut_p, cut_x;
@@ -50,11 +70,8 @@ int ortho_layout(const Grid &G, int32_t count, OrthoLayout *L) {
   L->flip = G.rows > G.cols;
   L->s = std::min(G.rows, G.cols);
   L->l = std::max(G.rows, G.cols);
-  L->sp = up(L->s, 64);
-  L->lp = up(L->l, 64);
-  L->wide_plane = L->s * L->lp * 2;
-  L->tall_plane = L->l * L->sp * 2;
-  L->square_plane = L->s * L->sp * 2;
+  L->sp = up(L->s, 32);
+  L->lp = up(L->l, 32);
   int64_t at = 0;
   auto take = [&](int64_t bytes) {
     const int64_t o = at;
@@ -62,11 +79,11 @@ int ortho_layout(const Grid &G, int32_t count, OrthoLayout *L) {
     return o;
   };
   for (int i = 0; i < 2; ++i) {
-    L->wide[i] = take(2 * L->wide_plane);
-    L->tall[i] = take(2 * L->tall_plane);
+    L->wide[i] = take(4 * L->s * L->lp);
+    L->tall[i] = take(4 * L->l * L->sp);
   }
-  L->S = take(2 * L->square_plane);
-  L->P = take(2 * L->square_plane);
+  L->S = take(4 * L->s * L->sp);
+  L->P = take(4 * L->s * L->sp);
   L->stride = at;
   L->tiles = 0;
   for (int32_t i = 0; i < G.gr; ++i)
@@ -77,11 +94,11 @@ int ortho_layout(const Grid &G, int32_t count, OrthoLayout *L) {
   }
   if (at > (int64_t)1 << 46 || (L->s + 127) / 128 * ((L->l + 127) / 128) > 0x3fffffff / count / 512) return DMM_ELIMIT;
   at *= count;
-  L->sums = 256 + L->tiles;
+  L->sums = kOrthoSums + L->tiles;
   L->o_sums = take(count * L->sums * 8);
-  L->cut_s = ortho_cut(L->s, L->s, true, 3 * L->lp / 64, count);
-  L->cut_p = ortho_cut(L->s, L->s, true, 3 * L->sp / 64, count);
-  L->cut_x = ortho_cut(L->s, L->l, false, 3 * L->sp / 64, count);
+  L->cut_s = ortho_cut(L->s, L->s, true, L->lp / 32, count);
+  L->cut_p = ortho_cut(L->s, L->s, true, L->sp / 32, count);
+  L->cut_x = ortho_cut(L->s, L->l, false, L->sp / 32, count);
   L->o_parts = take((int64_t)std::max({L->cut_s.parts, L->cut_p.parts, L->cut_x.parts}));
   L->total = at;
   return DMM_OK;
@@ -234,7 +251,7 @@ int dmm_orthogonalize(const dmm_matrix_desc *X, int32_t count, int x_dtype, cons
     args.by_rows = L.flip ? L.tall[0] : L.wide[0];
     args.by_cols = L.flip ? L.wide[0] : L.tall[0];
     args.sums = (double *)(ws + L.o_sums);
-    const int64_t share = std::max<int64_t>(1, 256 / L.tiles);
+    const int64_t share = std::max<int64_t>(1, kOrthoSums / L.tiles);
     int64_t sums = 0;
     for (int32_t i = 0; i < G.gr; ++i)
       for (int32_t j = 0; j < G.gc; ++j)
@@ -265,13 +282,14 @@ int dmm_orthogonalize(const dmm_matrix_desc *X, int32_t count, int x_dtype, cons
       g.symmetric = symmetric;
       g.m = (int32_t)m;
       g.n = (int32_t)n;
-      g.steps = (int32_t)(kp / 64);
-      g.k_pitch_a = g.k_pitch_b = (uint32_t)(kp * 2);
+      g.steps = (int32_t)(kp / 32);
+      g.k_pitch_a = g.k_pitch_b = (uint32_t)(kp * 4);
       g.tiles_m = c.tiles_m;
       g.tiles_n = c.tiles_n;
       g.tiles = c.tiles;
       g.runs = c.runs;
       g.per = c.per;
+      g.whole = c.whole;
       ortho_product_launch(g, c.edge, stream);
       DMM_HIP(hipGetLastError());
       return DMM_OK;
@@ -282,34 +300,25 @@ int dmm_orthogonalize(const dmm_matrix_desc *X, int32_t count, int x_dtype, cons
       const float *c = coefficients + 3 * i;
       // S = X X^T
       g.a = g.b = L.wide[now];
-      g.a_low = g.b_low = L.wide[now] + L.wide_plane;
-      g.old = g.old_low = g.y = -1;
+      g.old = g.y = -1;
       g.out = g.turned = L.S;
-      g.out_low = g.turned_low = L.S + L.square_plane;
       g.out_pitch = g.turned_pitch = (uint32_t)L.sp;
       g.alpha = 0.f;
       g.beta = unit;
       if ((rc = product(L.cut_s, true, L.s, L.s, L.lp))) return rc;
       // P = b S + c S S
       g.a = g.b = g.old = L.S;
-      g.a_low = g.b_low = g.old_low = L.S + L.square_plane;
       g.out = g.turned = L.P;
-      g.out_low = g.turned_low = L.P + L.square_plane;
       g.alpha = c[1];
       g.beta = c[2] * unit;
       if ((rc = product(L.cut_p, true, L.s, L.s, L.sp))) return rc;
       // X <- a X + P X
       g.a = L.P;
-      g.a_low = L.P + L.square_plane;
       g.b = L.tall[now];
-      g.b_low = L.tall[now] + L.tall_plane;
       g.old = L.wide[now];
-      g.old_low = L.wide[now] + L.wide_plane;
       g.out = L.wide[now ^ 1];
-      g.out_low = L.wide[now ^ 1] + L.wide_plane;
       g.out_pitch = (uint32_t)L.lp;
       g.turned = L.tall[now ^ 1];
-      g.turned_low = L.tall[now ^ 1] + L.tall_plane;
       g.turned_pitch = (uint32_t)L.sp;
       g.alpha = c[0];
       g.beta = unit;

@@ -4,14 +4,15 @@
 namespace dmm {
 namespace {
 
-using Ortho256 = NtShape<false, 256, 256>;
-using Ortho128 = NtShape<false, 128, 128>;
+using Ortho256 = NtShape<false, 256>;
+using Ortho128 = NtShape<false, 128>;            // two workgroups on a CU
+using Ortho128Deep = NtShape<false, 128, 4>;     // one, which then has three steps on their way
 
 template <class SH>
 void launch(const OrthoProduct &g, hipStream_t stream) {
-  const unsigned tiles = (unsigned)(g.count * g.tiles);
-  ortho_product_kernel<SH><<<dim3(tiles * (unsigned)g.runs), dim3(NT_THREADS), SH::LDS, stream>>>(g);
-  if (g.runs > 1) ortho_join_kernel<SH::TM><<<dim3(tiles * (SH::TM / 64)), dim3(256), 64 * (SH::TN + 4) * 4, stream>>>(g);
+  const int cut = g.count * g.tiles - g.whole;
+  ortho_product_kernel<SH><<<dim3((unsigned)(g.whole + cut * g.runs)), dim3(NT_THREADS), SH::LDS, stream>>>(g);
+  if (cut) ortho_join_kernel<SH::TM><<<dim3((unsigned)(cut * (SH::TM / 16))), dim3(256), 0, stream>>>(g);
 }
 
 }  // namespace
@@ -19,7 +20,7 @@ void launch(const OrthoProduct &g, hipStream_t stream) {
 hipError_t ortho_allow_lds() {
   hipError_t e = hipFuncSetAttribute((const void *)ortho_product_kernel<Ortho256>, hipFuncAttributeMaxDynamicSharedMemorySize, Ortho256::LDS);
   if (e == hipSuccess) e = hipFuncSetAttribute((const void *)ortho_product_kernel<Ortho128>, hipFuncAttributeMaxDynamicSharedMemorySize, Ortho128::LDS);
-  if (e == hipSuccess) e = hipFuncSetAttribute((const void *)ortho_join_kernel<256>, hipFuncAttributeMaxDynamicSharedMemorySize, 64 * 260 * 4);
+  if (e == hipSuccess) e = hipFuncSetAttribute((const void *)ortho_product_kernel<Ortho128Deep>, hipFuncAttributeMaxDynamicSharedMemorySize, Ortho128Deep::LDS);
   return e;
 }
 
@@ -28,6 +29,7 @@ void ortho_split_launch(const OrthoTiles &args, int blocks, hipStream_t stream) 
 void ortho_store_launch(const OrthoTiles &args, int blocks, hipStream_t stream) { ortho_store_kernel<<<dim3((unsigned)blocks), dim3(256), 0, stream>>>(args); }
 void ortho_product_launch(const OrthoProduct &g, int edge, hipStream_t stream) {
   if (edge == 256) launch<Ortho256>(g, stream);
+  else if (g.whole + (g.count * g.tiles - g.whole) * g.runs <= 256) launch<Ortho128Deep>(g, stream);
   else launch<Ortho128>(g, stream);
 }
 

@@ -20,32 +20,34 @@ constexpr int ORTHO_TILES = 64;
 struct OrthoTiles {
   int32_t n, f32;               // tiles; fp32 or bf16
   int32_t rows, cols;
-  int32_t row_pitch, col_pitch; // elements of a row of the two layouts: columns (rows) up to a multiple of 64
+  int32_t row_pitch, col_pitch; // elements of a row of the two layouts: columns (rows) up to a multiple of 32
   int64_t stride;               // bytes from one matrix' buffers to the next
   char *ws;
-  int64_t by_rows, by_cols;     // planes [rows][row_pitch] and [cols][col_pitch], the low parts right behind the high ones
+  int64_t by_rows, by_cols;     // byte offsets: pairs [rows][row_pitch] and [cols][col_pitch]
   double *sums;                 // of squares, so many per matrix
   int32_t sums_of_launch, pad;
   OrthoTile tile[ORTHO_TILES];
 };
 
-// out = alpha old + beta sum over k of A[m][k] B[n][k].  All matrices are pairs of fp16 planes.
+// out = alpha old + beta sum over k of A[m][k] B[n][k].  All matrices are pairs of fp16: 32 values of a row are 64 bytes
+// of high parts and 64 bytes of low parts.
 struct OrthoProduct {
   char *ws;                     // what follows are byte offsets in a matrix' buffers
   int64_t stride;
-  int64_t a, a_low, b, b_low;
-  int64_t old, old_low;         // out's rows and pitch; none: < 0
-  int64_t out, out_low;         // none: < 0
-  int64_t turned, turned_low;   // out transposed, none: < 0
+  int64_t a, b;
+  int64_t old;                  // out's rows and pitch; none: < 0
+  int64_t out;
+  int64_t turned;               // out transposed, none: < 0
   int64_t y;                    // the last product: out goes here alone, in fp32; else < 0
   uint32_t k_pitch_a, k_pitch_b;   // bytes
-  uint32_t out_pitch, turned_pitch;   // elements
+  uint32_t out_pitch, turned_pitch;   // elements (4 bytes)
   int32_t m, n;                 // out: m x n (columns up to out_pitch are zero, and rows up to turned_pitch)
-  int32_t steps;                // 64 of k each
+  int32_t steps;                // 32 of k each
   int32_t y_turned;             // ... transposed
   int32_t symmetric;            // out is: tiles below the diagonal come from those above
   int32_t count, tiles, tiles_m, tiles_n;   // matrices; tiles of each, in rows and columns
-  int32_t runs, per;            // every tile in so many ranges of K, steps of each (of 3 x steps)
+  int32_t whole;                // tiles (of all matrices) that are not cut; the others in `runs` ranges of K,
+  int32_t runs, per;            // steps of each
   float *parts;
   float alpha, beta;
 };
