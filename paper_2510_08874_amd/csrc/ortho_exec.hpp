@@ -6,6 +6,7 @@
 namespace dmm {
 namespace {
 
+static_assert(ORTHO_STEPS == DMM_ORTHOGONALIZE_STEPS, "coefficients travel with the launch");
 constexpr int kOrthoSums = 1024;       // workgroups that add up the squares of a matrix, about
 constexpr int kOrthoCus = 256;          // how products are cut along K, and so the workspace, does not depend on the device
 
@@ -61,6 +62,7 @@ struct OrthoLayout {
   int64_t tiles;                       // non-empty tiles of a matrix
   int64_t sums, o_sums, o_parts, total;
   OrthoCut cut_s, cut_p, cut_x;
+  bool small;                          // a workgroup a matrix, no workspace
 };
 
 int ortho_layout(const Grid &G, int32_t count, OrthoLayout *L) {
@@ -88,10 +90,10 @@ int ortho_layout(const Grid &G, int32_t count, OrthoLayout *L) {
   L->tiles = 0;
   for (int32_t i = 0; i < G.gr; ++i)
     for (int32_t j = 0; j < G.gc; ++j) L->tiles += G.rc[(size_t)i + 1] > G.rc[(size_t)i] && G.cc[(size_t)j + 1] > G.cc[(size_t)j];
-  if (L->s == 0 || count == 0) {
-    L->total = 0;
-    return DMM_OK;
-  }
+  // one tile, and no more than registers and LDS of a CU hold
+  L->small = G.gr == 1 && G.gc == 1 && L->l <= ORTHO_SMALL && L->s > 0 && count > 0;
+  L->total = 0;
+  if (L->small || L->s == 0 || count == 0) return DMM_OK;
   if (at > (int64_t)1 << 46 || (L->s + 127) / 128 * ((L->l + 127) / 128) > 0x3fffffff / count / 512) return DMM_ELIMIT;
   at *= count;
   L->sums = kOrthoSums + L->tiles;
@@ -184,6 +186,8 @@ int check_matrices(const Grid &G, int32_t count, const void *const *tiles, const
     const int64_t first = x * G.tiles_per_rep();
     int rc;
     if ((rc = check_lds(G, ld + first)) || (rc = check_tiles(G, tiles + first, es))) return rc;
+    for (int64_t i = first; i < first + G.tiles_per_rep(); ++i)
+      if (ld[i] > 0xffffffff) return DMM_ELD;
   }
   return DMM_OK;
 }
@@ -214,7 +218,7 @@ int dmm_orthogonalize(const dmm_matrix_desc *X, int32_t count, int x_dtype, cons
                       void *const *y_tiles, const int64_t *y_ld, const float *coefficients, int32_t steps, void *workspace,
                       int64_t workspace_bytes, void *hip_stream) {
   using namespace dmm;
-  if (!X || count < 0 || !x_tiles || !x_ld || !y_tiles || !y_ld || steps < 1) return DMM_EINVAL;
+  if (!X || count < 0 || !x_tiles || !x_ld || !y_tiles || !y_ld || steps < 1 || steps > ORTHO_STEPS) return DMM_EINVAL;
   if ((x_dtype != DMM_BF16 && x_dtype != DMM_F32) || (y_dtype != DMM_BF16 && y_dtype != DMM_F32)) return DMM_EINVAL;
   if (!coefficients) {
     if (steps > 5) return DMM_EINVAL;
@@ -231,11 +235,37 @@ int dmm_orthogonalize(const dmm_matrix_desc *X, int32_t count, int x_dtype, cons
     const int x_es = x_dtype == DMM_F32 ? 4 : 2, y_es = y_dtype == DMM_F32 ? 4 : 2;
     if ((rc = check_matrices(G, count, x_tiles, x_ld, x_es)) || (rc = check_matrices(G, count, y_tiles, y_ld, y_es))) return rc;
     if ((rc = ortho_layout(G, count, &L))) return rc;
+    hipStream_t stream = (hipStream_t)hip_stream;
+    if (L.small) {
+      if ((rc = allow_ortho_lds())) return rc;
+      OrthoSmall args;
+      std::memset(&args, 0, sizeof args);
+      args.rows = (int32_t)G.rows;
+      args.cols = (int32_t)G.cols;
+      args.steps = steps;
+      args.x_f32 = x_dtype == DMM_F32;
+      args.y_f32 = y_dtype == DMM_F32;
+      std::memcpy(args.coefficients, coefficients, (size_t)steps * 3 * sizeof(float));
+      bool even = count >= 2;
+      for (int32_t i = 2; i < count && even; ++i)
+        even = (const char *)x_tiles[i] - (const char *)x_tiles[i - 1] == (const char *)x_tiles[1] - (const char *)x_tiles[0] &&
+               (char *)y_tiles[i] - (char *)y_tiles[i - 1] == (char *)y_tiles[1] - (char *)y_tiles[0];
+      for (int32_t i = 1; i < count && even; ++i) even = x_ld[i] == x_ld[0] && y_ld[i] == y_ld[0];
+      args.even = even;
+      for (int32_t first = 0; first < count;) {
+        const int n = even ? count : std::min(count - first, ORTHO_MATRICES);
+        for (int i = 0; i < (even ? 2 : n); ++i)
+          args.matrix[i] = {(const char *)x_tiles[first + i], (char *)y_tiles[first + i], (uint32_t)x_ld[first + i], (uint32_t)y_ld[first + i]};
+        ortho_small_launch(args, n, stream);
+        DMM_HIP(hipGetLastError());
+        first += n;
+      }
+      return DMM_OK;
+    }
     if (L.total == 0) return DMM_OK;
     if (!workspace || ((uintptr_t)workspace & 255)) return DMM_EINVAL;
     if (workspace_bytes < L.total) return DMM_ELIMIT;
     if ((rc = allow_ortho_lds())) return rc;
-    hipStream_t stream = (hipStream_t)hip_stream;
     char *const ws = (char *)workspace;
 
     // ---- G / |G| as pairs ------------------------------------------------------------------

@@ -21,6 +21,7 @@ hipError_t ortho_allow_lds() {
   hipError_t e = hipFuncSetAttribute((const void *)ortho_product_kernel<Ortho256>, hipFuncAttributeMaxDynamicSharedMemorySize, Ortho256::LDS);
   if (e == hipSuccess) e = hipFuncSetAttribute((const void *)ortho_product_kernel<Ortho128>, hipFuncAttributeMaxDynamicSharedMemorySize, Ortho128::LDS);
   if (e == hipSuccess) e = hipFuncSetAttribute((const void *)ortho_product_kernel<Ortho128Deep>, hipFuncAttributeMaxDynamicSharedMemorySize, Ortho128Deep::LDS);
+  if (e == hipSuccess) e = hipFuncSetAttribute((const void *)ortho_small_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 2 * ORTHO_AREA);
   return e;
 }
 
@@ -31,6 +32,10 @@ void ortho_product_launch(const OrthoProduct &g, int edge, hipStream_t stream) {
   if (edge == 256) launch<Ortho256>(g, stream);
   else if (g.whole + (g.count * g.tiles - g.whole) * g.runs <= 256) launch<Ortho128Deep>(g, stream);
   else launch<Ortho128>(g, stream);
+}
+
+void ortho_small_launch(const OrthoSmall &args, int count, hipStream_t stream) {
+  ortho_small_kernel<<<dim3((unsigned)count), dim3(ORTHO_SMALL_THREADS), 2 * ORTHO_AREA, stream>>>(args);
 }
 
 }  // namespace dmm

@@ -309,4 +309,205 @@ __global__ __launch_bounds__(256) void ortho_join_kernel(const OrthoProduct g) {
                          g.turned >= 0 && !(g.symmetric && at.row == at.col));
 }
 
+// ---- small matrices ---------------------------------------------------------------------------------
+//
+// X stays in registers in fp32, eight waves of 32 x 64 elements each; what a product reads goes through LDS as pairs, two areas of
+// 128 rows: X by rows, then by columns, and S, then P.  Five barriers a step, no memory traffic between the first load and the
+// last store.  Bound by the matrix instructions of one CU: 3 x 384 of 32 cycles a step on its four pipes, 6 us for five steps
+// at 2.4 GHz, and by what waits in between (measured below).  In launches of the products above every one of the 18
+// took 8 to 15 us: 32 matrices of 128 x 128 200 us.
+constexpr int ORTHO_SMALL_THREADS = 512;
+constexpr int ORTHO_AREA = ORTHO_SMALL * ORTHO_SMALL * 4;    // bytes
+
+// Byte of an area that holds the high part of (row, k), the low part 64 further on (^ 64: it is the fourth bit of the slot's number);
+// 16-byte slots are exchanged by row so that 16 rows of one slot lie in different banks.
+__device__ __forceinline__ int ortho_area(int row, int k) {
+  const int slot = (k >> 5) * 8 + ((k & 31) >> 3);
+  return row * (ORTHO_SMALL * 4) + ((slot ^ (row & 15)) << 4) + (k & 7) * 2;
+}
+
+__global__ __launch_bounds__(ORTHO_SMALL_THREADS) void ortho_small_kernel(OrthoSmall) {
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  double *const part = (double *)lds;  // (for the norm, before the areas are used)
+  const auto &args = *(const OrthoSmall *)__builtin_amdgcn_kernarg_segment_ptr();
+  auto M = args.matrix[args.even ? 0 : blockIdx.x];
+  if (args.even) {
+    M.x += (int64_t)blockIdx.x * (args.matrix[1].x - M.x);
+    M.y += (int64_t)blockIdx.x * (args.matrix[1].y - M.y);
+  }
+  const int64_t x_pitch = (int64_t)M.x_ld * (args.x_f32 ? 4 : 2), y_pitch = (int64_t)M.y_ld * (args.y_f32 ? 4 : 2);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int r = lane & 31, g = lane >> 5;
+  const bool flip = args.rows > args.cols;
+  const int s = flip ? args.cols : args.rows, l = flip ? args.rows : args.cols;   // X is s x l
+  const int row0 = (wave >> 1) * 32, col0 = (wave & 1) * 64;
+  const unsigned area1 = (unsigned)(uintptr_t)(nt_lptr)lds, area2 = area1 + ORTHO_AREA;
+  auto row_of = [&](int x) { return row0 + 8 * (x / 4) + 4 * g + x % 4; };
+  nt_f32x16 X[2], S[2];
+
+  // ---- G / |G| -----------------------------------------------------------------------------
+  double sum = 0.0;
+  // (all loads first, whatever lies outside from the nearest element)
+  const char *const from = M.x;
+  const int64_t to_row = flip ? (args.x_f32 ? 4 : 2) : x_pitch, to_col = flip ? x_pitch : (args.x_f32 ? 4 : 2);
+  auto load = [&](auto fc) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int x = 0; x < 16; ++x)
+        X[j][x] = ortho_load(from + min(row_of(x), s - 1) * to_row + min(col0 + 32 * j + r, l - 1) * to_col, decltype(fc)::value, 0);
+  };
+  if (args.x_f32) load(std::true_type{});
+  else load(std::false_type{});
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+#pragma unroll
+    for (int x = 0; x < 16; ++x) X[j][x] = row_of(x) < s && col0 + 32 * j + r < l ? X[j][x] : 0.f;
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+#pragma unroll
+    for (int x = 0; x < 16; ++x) sum += (double)X[j][x] * (double)X[j][x];
+#pragma unroll
+  for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+  if (lane == 0) part[wave] = sum;
+  __syncthreads();
+  sum = 0.0;
+#pragma unroll
+  for (int w = 0; w < 8; ++w) sum += part[w];
+  __syncthreads();
+  const double inv = !(sum <= 1.7976931348623157e308) ? __builtin_nan("") : sum > 0.0 ? ORTHO_SCALE / sqrt(sum) : 0.0;
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+#pragma unroll
+    for (int x = 0; x < 16; ++x) X[j][x] = (float)((double)X[j][x] * inv);
+  asm volatile("" : "+v"(r), "+v"(g));
+  __builtin_amdgcn_sched_barrier(0);
+
+  // ---- between registers and areas -----------------------------------------------------------
+  // (addresses are written so that all but a few exclusive ors of constants are offsets of the instructions)
+  auto put_rows = [&](unsigned area, const nt_f32x16 (&v)[2]) {
+    const unsigned base = area + ortho_area(row0 + 4 * g, col0 + r);
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) {
+        const OrthoPair p = ortho_split(v[j][x]);
+        const int row = 8 * (x / 4) + x % 4, turn = ((row & 15) ^ (8 * j)) << 4;   // (32 columns on are 8 slots on)
+        *(__attribute__((address_space(3))) _Float16 *)((nt_lptr)(uintptr_t)(base ^ turn) + row * (ORTHO_SMALL * 4)) = p.high;
+        *(__attribute__((address_space(3))) _Float16 *)((nt_lptr)(uintptr_t)(base ^ turn ^ 64) + row * (ORTHO_SMALL * 4)) = p.low;
+        if (x % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+      }
+  };
+  // (the transpose; four neighbouring rows of a column at a time)
+  auto put_cols = [&](unsigned area, const nt_f32x16 (&v)[2]) {
+    typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+    const unsigned base = area + ortho_area(col0 + r, row0 + 4 * g);
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int x = 0; x < 16; x += 4) {
+        h4 high, low;
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          const OrthoPair p = ortho_split(v[j][x + y]);
+          high[y] = p.high;
+          low[y] = p.low;
+        }
+        *(__attribute__((address_space(3))) h4 *)((nt_lptr)(uintptr_t)(base ^ (x / 4 << 4)) + 32 * j * (ORTHO_SMALL * 4)) = high;
+        *(__attribute__((address_space(3))) h4 *)((nt_lptr)(uintptr_t)(base ^ (x / 4 << 4) ^ 64) + 32 * j * (ORTHO_SMALL * 4)) = low;
+        __builtin_amdgcn_sched_barrier(0);
+      }
+  };
+  // rows row0 ... of `a` times rows col0 ... of `b`, inner length 64 or 128
+  auto product = [&](unsigned a, unsigned b, int k, nt_f32x16 (&acc)[2]) {
+    acc[0] = nt_f32x16{};
+    acc[1] = nt_f32x16{};
+    const unsigned base_a = a + ortho_area(row0 + r, 8 * g), base_b = b + ortho_area(col0 + r, 8 * g);
+    auto get = [](unsigned at, int on) { return *(const __attribute__((address_space(3))) nt_f16x8 *)((nt_lptr)(uintptr_t)at + on); };
+    struct Frag {
+      nt_f16x8 ah, al, bh[2], bl[2];
+    };
+    auto read = [&](Frag &f, auto ac) {
+      constexpr int AT = decltype(ac)::value * 16, SLOT = (AT >> 5) * 8 + ((AT & 31) >> 3), TURN = (SLOT & 15) << 4, ON = (SLOT & 16) << 4;
+      f.al = get(base_a ^ TURN ^ 64, ON);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) f.bh[j] = get(base_b ^ TURN, ON + 32 * j * (ORTHO_SMALL * 4));
+      f.ah = get(base_a ^ TURN, ON);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) f.bl[j] = get(base_b ^ TURN ^ 64, ON + 32 * j * (ORTHO_SMALL * 4));
+    };
+    // the fragments of 16 k are read while those in front of them are multiplied
+    auto all = [&](auto nc) {
+      constexpr int N = decltype(nc)::value;
+      Frag f[2];
+      read(f[0], std::integral_constant<int, 0>{});
+      nt_for<N>([&](auto ac) {
+        constexpr int I = decltype(ac)::value;
+        const Frag &now = f[I & 1];
+        if constexpr (I + 1 < N) read(f[(I + 1) & 1], std::integral_constant<int, I + 1>{});
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(now.al, now.bh[j], acc[j], 0, 0, 0);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(now.ah, now.bl[j], acc[j], 0, 0, 0);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(now.ah, now.bh[j], acc[j], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    };
+    if (k > 64) all(std::integral_constant<int, 8>{});
+    else all(std::integral_constant<int, 4>{});
+  };
+
+  // ---- the steps -------------------------------------------------------------------------------
+  constexpr float UNIT = 1.f / ORTHO_SCALE;
+  for (int step = 0; step < args.steps; ++step) {
+    const float a = args.coefficients[3 * step], b = args.coefficients[3 * step + 1], c = args.coefficients[3 * step + 2];
+    nt_f32x16 acc[2];
+    // (behind every barrier the lane's number is new to the compiler, which else keeps 100 addresses from step to step)
+    auto sync = [&]() {
+      __syncthreads();
+      asm volatile("" : "+v"(r), "+v"(g));
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    put_rows(area1, X);
+    sync();
+    product(area1, area1, l, S);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) S[j] *= UNIT;
+    __builtin_amdgcn_sched_barrier(0);
+    put_cols(area2, S);                // (symmetric)
+    sync();
+    put_cols(area1, X);
+    product(area2, area2, s, acc);
+    sync();
+#pragma unroll
+    for (int j = 0; j < 2; ++j) S[j] = b * S[j] + c * UNIT * acc[j];
+    __builtin_amdgcn_sched_barrier(0);
+    put_cols(area2, S);
+    sync();
+    product(area2, area1, s, acc);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) X[j] = a * X[j] + UNIT * acc[j];
+    sync();
+  }
+  char *const out = M.y;
+  const int64_t out_row = flip ? (args.y_f32 ? 4 : 2) : y_pitch, out_col = flip ? y_pitch : (args.y_f32 ? 4 : 2);
+  auto store = [&](auto fc) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) {
+        const int row = row_of(x), col = col0 + 32 * j + r;
+        char *const to = out + row * out_row + col * out_col;
+        if (row < s && col < l) {
+          if constexpr (decltype(fc)::value) *(float *)to = X[j][x] * UNIT;
+          else *(__bf16 *)to = (__bf16)(X[j][x] * UNIT);
+        }
+      }
+  };
+  if (args.y_f32) store(std::true_type{});
+  else store(std::false_type{});
+}
+
 }  // namespace dmm

@@ -52,6 +52,22 @@ struct OrthoProduct {
   float alpha, beta;
 };
 
+// Matrices of up to 128 x 128, one workgroup each, whole in registers and LDS.
+constexpr int ORTHO_SMALL = 128;
+constexpr int ORTHO_MATRICES = 144, ORTHO_STEPS = 32;
+struct OrthoSmall {
+  int32_t rows, cols, steps;
+  int32_t x_f32, y_f32;
+  float coefficients[3 * ORTHO_STEPS];
+  int32_t even;                 // matrices lie at even distances: matrix[0] tells where the first is, matrix[1] the second
+  struct {
+    const char *x;
+    char *y;
+    uint32_t x_ld, y_ld;        // elements
+  } matrix[ORTHO_MATRICES];
+};
+void ortho_small_launch(const OrthoSmall &args, int count, hipStream_t stream);
+
 hipError_t ortho_allow_lds();
 void ortho_norm_launch(const OrthoTiles &args, int blocks, hipStream_t stream);
 void ortho_split_launch(const OrthoTiles &args, int blocks, hipStream_t stream);
