@@ -66,7 +66,7 @@ __global__ __launch_bounds__(NT_THREADS, SH::LDS > 80 * 1024 ? 1 : 2) void mx_ge
     for (int x = threadIdx.x; x < 64 * PER; x += NT_THREADS) {
       const int r = x / PER, col = x % PER * 8, row = base + (r & 31) + (r >> 5) * (SH::TM / 2);
       if (row >= it.m_ext || col >= it.n_ext) continue;
-      const nt_f32x4 v = *(const nt_f32x4 *)(values + r * NtTile<SH>::PITCH + col), u = *(const nt_f32x4 *)(values + r * NtTile<SH>::PITCH + col + 4);
+      const nt_f32x4 *const from = (const nt_f32x4 *)(values + nt_value(r, col, NtTile<SH>::PITCH)), v = from[0], u = from[1];
       char *const to = it.c + ((int64_t)row * it.ldc + col) * 2;
       if (col + 8 <= it.n_ext) {
         nt_i32x4 w;

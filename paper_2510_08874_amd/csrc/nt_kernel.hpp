@@ -75,6 +75,10 @@ __device__ __forceinline__ void nt_for(F &&f) {
   nt_for_impl<N>(std::make_integer_sequence<int, N>{}, f);
 }
 
+// Where a slice of 64 rows of a finished tile has an element: columns are exchanged eight at a time by row, so that eight rows
+// of a column, eight rows apart, lie in different banks (and eight neighbouring columns of a row stay together).
+__device__ __forceinline__ int nt_value(int row, int col, int pitch) { return row * pitch + (col ^ (row & 56)); }
+
 // SCALED: 4-bit codes with scales; otherwise pairs of fp16.  EDGE x EDGE macro-tile over 2 x 2 waves, NST stages.
 template <bool SCALED_, int EDGE, int NST_ = 2>
 struct NtShape {
@@ -107,21 +111,23 @@ struct NtTile {
   }
 
   // The finished tile, 64 rows at a time through LDS, where `use(values, row)` finds rows row .. row + 31 of the tile in rows 0 .. 31
-  // of `values` and row + TM / 2 ... in rows 32 .. 63; PITCH floats from one to the next.  Every thread gets there between two barriers.
+  // of `values` and row + TM / 2 ... in rows 32 .. 63, every element at nt_value(row, column, PITCH).  Every thread gets there between
+  // two barriers.
   static constexpr int PITCH = SH::TN + 4;
   static_assert(64 * PITCH * 4 <= SH::LDS, "a slice lies in the stages");
   template <class F>
   __device__ __forceinline__ void slices(char *lds, F &&use) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     float *const values = (float *)lds;
-    float *const mine = values + ((wave >> 1) * 32 + 4 * (lane >> 5)) * PITCH + (wave & 1) * (SH::TN / 2) + (lane & 31);
+    float *const mine = values + ((wave >> 1) * 32 + 4 * (lane >> 5)) * PITCH;
+    const int col = (wave & 1) * (SH::TN / 2) + (lane & 31), turn = (wave >> 1) * 32;
     nt_for<SH::MI>([&](auto ic) {
       constexpr int I = decltype(ic)::value;
       __syncthreads();
       nt_for<SH::NI>([&](auto jc) {
         constexpr int J = decltype(jc)::value;
 #pragma unroll
-        for (int x = 0; x < 16; ++x) mine[(8 * (x / 4) + x % 4) * PITCH + 32 * J] = acc[I][J][x];
+        for (int x = 0; x < 16; ++x) mine[(8 * (x / 4) + x % 4) * PITCH + ((col + 32 * J) ^ (turn + x / 4 * 8))] = acc[I][J][x];
         __builtin_amdgcn_sched_barrier(0);
       });
       __syncthreads();

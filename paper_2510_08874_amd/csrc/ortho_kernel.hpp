@@ -183,7 +183,7 @@ __device__ __forceinline__ void ortho_finish(const OrthoProduct &g, char *ws, fl
   auto row_of = [&](int r) { return row0 + r % HALF + r / HALF * apart; };
   for (int x = threadIdx.x; x < ROWS * PER; x += NT_THREADS) {
     const int r = x / PER, c = x % PER * 8;
-    float *const p = values + r * pitch + c;
+    float *const p = values + nt_value(r, c, pitch);
     float v[8];
 #pragma unroll
     for (int y = 0; y < 8; ++y) v[y] = p[y];
@@ -197,7 +197,7 @@ __device__ __forceinline__ void ortho_finish(const OrthoProduct &g, char *ws, fl
       // (lanes run along the rows of Y)
       const int r = g.y_turned ? x % ROWS : x / TN, c = g.y_turned ? x / ROWS : x % TN;
       const int row = row_of(r), col = col0 + c;
-      if (row < g.m && col < g.n) ((float *)(ws + g.y))[g.y_turned ? (int64_t)col * g.m + row : (int64_t)row * g.n + col] = values[r * pitch + c] * (1.f / ORTHO_SCALE);
+      if (row < g.m && col < g.n) ((float *)(ws + g.y))[g.y_turned ? (int64_t)col * g.m + row : (int64_t)row * g.n + col] = values[nt_value(r, c, pitch)] * (1.f / ORTHO_SCALE);
     }
   } else if (mirror) {
     __syncthreads();
@@ -205,7 +205,7 @@ __device__ __forceinline__ void ortho_finish(const OrthoProduct &g, char *ws, fl
       const int r = x % (ROWS / 8) * 8, c = x / (ROWS / 8);
       float v[8];
 #pragma unroll
-      for (int y = 0; y < 8; ++y) v[y] = values[(r + y) * pitch + c];
+      for (int y = 0; y < 8; ++y) v[y] = values[nt_value(r + y, c, pitch)];
       ortho_cols8(g, ws, row_of(r), col0 + c, v);
     }
   }
@@ -273,7 +273,7 @@ __global__ __launch_bounds__(NT_THREADS, SH::LDS > 80 * 1024 ? 1 : 2) void ortho
     tile.slices(lds, [&](const float *values, int base) {
       for (int x = threadIdx.x; x < 64 * SH::TN / 4; x += NT_THREADS) {
         const int r = x / (SH::TN / 4), c = x % (SH::TN / 4) * 4;
-        *(nt_f32x4 *)(part + (base + (r & 31) + (r >> 5) * (SH::TM / 2)) * SH::TN + c) = *(const nt_f32x4 *)(values + r * NtTile<SH>::PITCH + c);
+        *(nt_f32x4 *)(part + (base + (r & 31) + (r >> 5) * (SH::TM / 2)) * SH::TN + c) = *(const nt_f32x4 *)(values + nt_value(r, c, NtTile<SH>::PITCH));
       }
     });
   } else {
@@ -302,7 +302,7 @@ __global__ __launch_bounds__(256) void ortho_join_kernel(const OrthoProduct g) {
 #pragma unroll
   for (int y = 0; y < N; ++y) {
     const int x = y * 256 + threadIdx.x;
-    *(nt_f32x4 *)(values + x / (EDGE / 4) * PITCH + x % (EDGE / 4) * 4) = sum[y];
+    *(nt_f32x4 *)(values + nt_value(x / (EDGE / 4), x % (EDGE / 4) * 4, PITCH)) = sum[y];
   }
   __syncthreads();
   ortho_finish<EDGE, 16>(g, g.ws + at.matrix * g.stride, values, PITCH, at.row * EDGE + rows0, 8, at.col * EDGE,
