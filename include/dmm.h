@@ -340,8 +340,8 @@ int dmm_mx_execute(dmm_plan_t *p, const dmm_mx_tiles *a, const dmm_mx_tiles *b, 
  *   X = G / |G|  (Frobenius norm; a matrix of zeros stays zero, one with an infinity or a NaN comes out as NaN)
  *   `steps` times:  S = X X^T,  X = a X + (b S + c S S) X       (with X^T in X's place where G has more rows than columns)
  * coefficients: host, a, b, c of every step; null: (3.4445, -4.7750, 2.0315) for up to 5 steps, 5 of which take singular values from
- * 0.002 |G| up to between 0.68 and 1.21.  Coefficients that let a singular value, or an eigenvalue of b S + c S S, pass
- * 15 on the way are refused (DMM_EINVAL).
+ * 0.002 |G| up to between 0.68 and 1.21.  Coefficients that let a singular value, or an eigenvalue of S, of b S + c S S or of a I + b S + c S S,
+ * pass 15 on the way are refused (DMM_EINVAL).
  * Tables of the tiles: matrix * (grid_rows * grid_cols) + ti * grid_cols + tj; the descriptor's replication is 1 (DMM_EREPL).
  * Elements bf16 or fp32 on either side; leading dimensions in elements.  Y may be X if both have the same type.
  * Products are of pairs of fp16 numbers, 22 bits of a value, with fp32 sums: an fp32 result is off by no more than fp32

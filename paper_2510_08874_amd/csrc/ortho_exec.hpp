@@ -29,18 +29,19 @@ OrthoCut ortho_cut(int64_t m, int64_t n, bool symmetric, int64_t steps, int64_t 
     c.tiles = symmetric ? c.tiles_m * (c.tiles_m + 1) / 2 : c.tiles_m * c.tiles_n;
     const int places = edge == 256 ? kOrthoCus : 2 * kOrthoCus;
     const int64_t tiles = c.tiles * count, rest = tiles % places;
-    // us: a step of a tile of 256, of one of 128 that has its CU to itself (the more there are the longer L2 takes), of two; and a tile's ends
-    auto round = [&](int64_t n_tiles, int64_t n_steps) {
+    // us: a step of tiles of 256, of two of 128 on a CU, of one (the more there are the longer L2 takes, and the less power is
+    // left for each); and a tile's ends
+    auto round = [&](int64_t n_tiles, int64_t n_steps, bool cut) {
       if (n_tiles == 0) return 0.0;
-      const double step = edge == 256 ? 2.2 : n_tiles > kOrthoCus ? 1.45 : 0.5 + 0.4 * (double)n_tiles / kOrthoCus;
-      return step * (double)n_steps + (edge == 256 ? 10.0 : 7.0);
+      const double full = (double)n_tiles / kOrthoCus, step = edge == 256 ? 1.45 + 0.9 * full : full > 1.0 ? 1.35 : 0.4 + 0.2 * full;
+      return step * (double)n_steps + (edge == 256 ? 14.0 : cut ? 6.0 : 11.0);
     };
-    const double whole_us = (tiles / places) * round(places, steps);
+    const double whole_us = (tiles / places) * round(places, steps, false);
     for (int64_t runs = 1; runs <= 32; ++runs) {
       const int64_t per = (steps + runs - 1) / runs;
       if (runs > 1 && (rest == 0 || rest * runs > places || per < 4 || (steps + per - 1) / per != runs)) continue;
       const double bytes = runs > 1 ? 2.0 * rest * runs * edge * edge * 4 : 0.0;
-      const double us = whole_us + round(rest * runs, per) + (runs > 1 ? 5.0 + bytes / 3e6 : 0.0);
+      const double us = whole_us + round(rest * runs, per, runs > 1) + (runs > 1 ? 5.0 + bytes / 3e6 : 0.0);
       if (best_us == 0.0 || us < best_us) {
         best_us = us;
         best = c;
@@ -114,7 +115,7 @@ bool ortho_in_range(const float *c, int32_t steps) {
     double next = 0.0, poly = 0.0;
     for (int x = 0; x <= 4096; ++x) {
       const double v = top * x / 4096, q = v * v, p = c[1] * q + c[2] * q * q;
-      poly = std::max(poly, std::fabs(p));
+      poly = std::max(poly, std::max(std::fabs(p), std::fabs(c[0] + p)));
       next = std::max(next, std::fabs(v * (c[0] + p)));
     }
     if (!(top * top <= 15.0) || !(poly <= 15.0) || !(next <= 15.0)) return false;
@@ -336,22 +337,23 @@ int dmm_orthogonalize(const dmm_matrix_desc *X, int32_t count, int x_dtype, cons
       g.alpha = 0.f;
       g.beta = unit;
       if ((rc = product(L.cut_s, true, L.s, L.s, L.lp))) return rc;
-      // P = b S + c S S
+      // P = a I + b S + c S S
       g.a = g.b = g.old = L.S;
       g.out = g.turned = L.P;
       g.alpha = c[1];
       g.beta = c[2] * unit;
+      g.diagonal = c[0] / unit;
       if ((rc = product(L.cut_p, true, L.s, L.s, L.sp))) return rc;
-      // X <- a X + P X
+      // X <- P X
       g.a = L.P;
       g.b = L.tall[now];
-      g.old = L.wide[now];
+      g.old = -1;
       g.out = L.wide[now ^ 1];
       g.out_pitch = (uint32_t)L.lp;
       g.turned = L.tall[now ^ 1];
       g.turned_pitch = (uint32_t)L.sp;
-      g.alpha = c[0];
       g.beta = unit;
+      g.diagonal = 0.f;
       if (i + 1 == steps) {            // the result takes the place of the generation that it is not made from
         g.y = L.wide[now ^ 1];
         g.y_turned = L.flip;

@@ -1,12 +1,13 @@
 // Newton-Schulz steps that bring the singular values of a matrix near 1 (gfx950, device code only):
-//   X_0 = G / |G|,   S = X X^T,   X <- a X + (b S + c S S) X
-// with X the matrix or its transpose, whichever has fewer rows.
+//   X_0 = G / |G|,   S = X X^T,   X <- (a I + b S + c S S) X
+// with X the matrix or its transpose, whichever has fewer rows.  (a X is part of the last product: its own pass over X would
+// read as many bytes again as half of what that product writes.)
 //
 // Every matrix is kept as pairs of fp16, v 2^12 = high + low with low the rounded rest: 22 bits of a value, and
 // a product of two is low high + high low + high high, three matrix instructions (what is left out is 2^-22 of it).  Singular
 // values far below the largest grow by 3.4 each step, and so do errors: rounded to bf16 once per step a matrix with a few
 // strong directions comes out 28 % off (512 x 512, rank 16 over 1 % of noise), in fp16 4 %, in pairs 7e-6, in plain fp32 2e-5.
-// The factor 2^12: no value reaches 16 (|X| <= 1.2 and |b S + c S S| < 5 in every element, checked by the host for the coefficients
+// The factor 2^12: no value reaches 16 (|X| <= 1.2 and |a I + b S + c S S| < 5 in every element, checked by the host for the coefficients
 // given), and the low part of one of 2^-13, the size of an element of a normalised 8192 x 8192 matrix, still is
 // a multiple of 2^-24 / 2^12.
 #pragma once
@@ -152,7 +153,7 @@ __device__ __forceinline__ void ortho_rows8(const OrthoProduct &g, char *ws, int
   }
 #pragma unroll
   for (int x = 0; x < 8; ++x) {
-    v[x] = col + x < g.n ? g.alpha * ((float)high[x] + (float)low[x]) + g.beta * v[x] : 0.f;
+    v[x] = col + x < g.n ? g.alpha * ((float)high[x] + (float)low[x]) + g.beta * v[x] + (col + x == row ? g.diagonal : 0.f) : 0.f;
     const OrthoPair p = ortho_split(v[x]);
     high[x] = p.high;
     low[x] = p.low;
