@@ -103,13 +103,14 @@ int over_tiles(const Grid &G, int es, char *const *x, const int64_t *x_ld, const
         }
         t.h = (int32_t)h;
         t.w = (int32_t)w;
-        t.wide = !((uintptr_t)t.x & 15) && !(t.x_pitch & 15);
         int64_t n;
         if (along == MX_ALONG_ROWS) {
           t.blocks_across = (int32_t)((w + 511) / 512);
           n = ((h + per - 1) / per * t.blocks_across + 3) / 4;
         } else {
-          t.blocks_across = (int32_t)((w + 127) / 128);
+          // (with the rows too, down to the end of the last chunk)
+          const int64_t cols = mx_block_cols(es == 4), wide = rows ? (w + 127) / 128 * 128 : w;
+          t.blocks_across = (int32_t)((wide + cols - 1) / cols);
           n = (h + 127) / 128 * t.blocks_across;
         }
         if (n > 0x3fffffff) return DMM_ELIMIT;
@@ -317,7 +318,7 @@ int dmm_mx_quantize(const dmm_matrix_desc *X, int dtype, const void *const *x_ti
     if ((rc = load_matrix(X, &G)) || (rc = check_lds(G, x_ld))) return rc;
     if (rows && (rc = check_mx(G, rows, false))) return rc;
     if (cols && (rc = check_mx(G, cols, true))) return rc;
-    if ((rc = check_tiles(G, x_tiles, dtype == DMM_F32 ? 4 : 2)) || (rc = allow_mx_lds())) return rc;
+    if ((rc = check_tiles(G, x_tiles, dtype == DMM_F32 ? 4 : 2))) return rc;
     return over_tiles(G, dtype == DMM_F32 ? 4 : 2, (char *const *)x_tiles, x_ld, rows, cols, [&](const MxTileArgs &args, int blocks, int along, int per) {
       mx_quantize_launch(args, blocks, dtype == DMM_F32, along, per, (hipStream_t)hip_stream);
     });
@@ -336,7 +337,7 @@ int dmm_mx_dequantize(const dmm_matrix_desc *X, const dmm_mx_tiles *q, int along
     Grid G;
     int rc;
     if ((rc = load_matrix(X, &G)) || (rc = check_lds(G, x_ld)) || (rc = check_mx(G, q, along == DMM_MX_COLS))) return rc;
-    if ((rc = check_tiles(G, x_tiles, dtype == DMM_F32 ? 4 : 2)) || (rc = allow_mx_lds())) return rc;
+    if ((rc = check_tiles(G, x_tiles, dtype == DMM_F32 ? 4 : 2))) return rc;
     return over_tiles(G, dtype == DMM_F32 ? 4 : 2, (char *const *)x_tiles, x_ld, along == DMM_MX_ROWS ? q : nullptr, along == DMM_MX_COLS ? q : nullptr,
                       [&](const MxTileArgs &args, int blocks, int by, int per) {
                         mx_values_launch(args, blocks, dtype == DMM_F32, by, per, (hipStream_t)hip_stream);

@@ -17,8 +17,7 @@ bool launch(hipEvent_t behind, const MxItem *items, int n, const NtSeg *segs, hi
   return launch_behind(behind, mx_gemm_kernel<SH>, (unsigned)n, NT_THREADS, SH::LDS, stream, items, segs);
 }
 
-template <bool F32>
-constexpr int turn_lds() { return 128 * (128 * (F32 ? 4 : 2) + 4); }
+static_assert(MxBlock<false>::COLS == mx_block_cols(false) && MxBlock<true>::COLS == mx_block_cols(true), "blocks along the columns");
 
 }  // namespace
 
@@ -26,10 +25,6 @@ hipError_t mx_allow_lds() {
   hipError_t e = hipFuncSetAttribute((const void *)mx_gemm_kernel<Mx256>, hipFuncAttributeMaxDynamicSharedMemorySize, Mx256::LDS);
   if (e == hipSuccess) e = hipFuncSetAttribute((const void *)mx_gemm_kernel<Mx128>, hipFuncAttributeMaxDynamicSharedMemorySize, Mx128::LDS);
   if (e == hipSuccess) e = hipFuncSetAttribute((const void *)mx_gemm_kernel<Mx128Deep>, hipFuncAttributeMaxDynamicSharedMemorySize, Mx128Deep::LDS);
-  // (128 rows of fp32 with their extra words: 64.5 KB)
-  const void *turn[3] = {(const void *)mx_cols_kernel<true, false>, (const void *)mx_cols_kernel<true, true>, (const void *)mx_col_values_kernel<true>};
-  for (const void *f : turn)
-    if (e == hipSuccess) e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, turn_lds<true>());
   return e;
 }
 
@@ -56,11 +51,11 @@ void mx_quantize_launch(const MxTileArgs &args, int blocks, bool f32, int along,
     if (f32) rows_per_unit == 4 ? mx_rows_kernel<true, 4><<<grid, block, 0, stream>>>(args) : mx_rows_kernel<true, 1><<<grid, block, 0, stream>>>(args);
     else rows_per_unit == 4 ? mx_rows_kernel<false, 4><<<grid, block, 0, stream>>>(args) : mx_rows_kernel<false, 1><<<grid, block, 0, stream>>>(args);
   } else if (along == MX_ALONG_COLS) {
-    if (f32) mx_cols_kernel<true, false><<<grid, block, turn_lds<true>(), stream>>>(args);
-    else mx_cols_kernel<false, false><<<grid, block, turn_lds<false>(), stream>>>(args);
+    if (f32) mx_cols_kernel<true, false><<<grid, block, 0, stream>>>(args);
+    else mx_cols_kernel<false, false><<<grid, block, 0, stream>>>(args);
   } else {
-    if (f32) mx_cols_kernel<true, true><<<grid, block, turn_lds<true>(), stream>>>(args);
-    else mx_cols_kernel<false, true><<<grid, block, turn_lds<false>(), stream>>>(args);
+    if (f32) mx_cols_kernel<true, true><<<grid, block, 0, stream>>>(args);
+    else mx_cols_kernel<false, true><<<grid, block, 0, stream>>>(args);
   }
 }
 
@@ -70,8 +65,8 @@ void mx_values_launch(const MxTileArgs &args, int blocks, bool f32, int along, i
     if (f32) rows_per_unit == 4 ? mx_row_values_kernel<true, 4><<<grid, block, 0, stream>>>(args) : mx_row_values_kernel<true, 1><<<grid, block, 0, stream>>>(args);
     else rows_per_unit == 4 ? mx_row_values_kernel<false, 4><<<grid, block, 0, stream>>>(args) : mx_row_values_kernel<false, 1><<<grid, block, 0, stream>>>(args);
   } else {
-    if (f32) mx_col_values_kernel<true><<<grid, block, turn_lds<true>(), stream>>>(args);
-    else mx_col_values_kernel<false><<<grid, block, turn_lds<false>(), stream>>>(args);
+    if (f32) mx_col_values_kernel<true><<<grid, block, 0, stream>>>(args);
+    else mx_col_values_kernel<false><<<grid, block, 0, stream>>>(args);
   }
 }
 

@@ -16,12 +16,15 @@ namespace dmm {
 
 // ---- products -------------------------------------------------------------------------------------
 
+typedef int mx_i32x4_any __attribute__((ext_vector_type(4), aligned(2)));   // (16 bytes at any address of a bf16)
 __device__ __forceinline__ unsigned short mx_bf16(float v) { return __builtin_bit_cast(unsigned short, (__bf16)v); }
 
 // (the host sees to it that a macro-tile's rows lie within 2^32 bytes)
-template <class SH, class E>
-__device__ __forceinline__ void mx_store(const NtTile<SH> &tile, const MxItem &it, int row0, int col0) {
-  const unsigned pitch = (unsigned)it.ldc * (unsigned)sizeof(E);
+template <class SH>
+__device__ __forceinline__ void mx_store(const NtTile<SH> &tile, const MxItem &it) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int row0 = (wave >> 1) * (SH::TM / 2) + 4 * (lane >> 5), col0 = (wave & 1) * (SH::TN / 2) + (lane & 31);
+  const unsigned pitch = (unsigned)it.ldc * 4u;
   char *const c = (char *)nt_uniform(it.c);
 #pragma unroll
   for (int i = 0; i < SH::MI; ++i)
@@ -32,12 +35,7 @@ __device__ __forceinline__ void mx_store(const NtTile<SH> &tile, const MxItem &i
 #pragma unroll
         for (int x = 0; x < 16; ++x) {
           const int row = row0 + 32 * i + 8 * (x / 4) + x % 4;
-          if (row < it.m_ext) {
-            const float v = tile.acc[i][j][x];
-            E *const to = (E *)(c + ((unsigned)row * pitch + (unsigned)(col * (int)sizeof(E))));
-            if constexpr (sizeof(E) == 4) __builtin_nontemporal_store(v, to);
-            else __builtin_nontemporal_store(mx_bf16(v), to);
-          }
+          if (row < it.m_ext) __builtin_nontemporal_store(tile.acc[i][j][x], (float *)(c + ((unsigned)row * pitch + (unsigned)col * 4u)));
         }
       }
       __builtin_amdgcn_sched_barrier(0);
@@ -52,12 +50,9 @@ __global__ __launch_bounds__(NT_THREADS, SH::LDS > 80 * 1024 ? 1 : 2) void mx_ge
   NtTile<SH> tile;
   tile.run(segs + it.seg, it.n_segs, it.first, it.steps, it.m_off, it.m_ext, it.n_off, it.n_ext, lds);
   tile.pin();
-  // fp32, and rows that are not aligned: half a wave writes 32 neighbouring columns of a row
-  if (it.c_es == 4 || ((uintptr_t)it.c & 15) || (it.ldc & 7)) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int row0 = (wave >> 1) * (SH::TM / 2) + 4 * (lane >> 5), col0 = (wave & 1) * (SH::TN / 2) + (lane & 31);
-    if (it.c_es == 4) mx_store<SH, float>(tile, it, row0, col0);
-    else mx_store<SH, unsigned short>(tile, it, row0, col0);
+  // fp32: half a wave writes 32 neighbouring columns of a row
+  if (it.c_es == 4) {
+    mx_store(tile, it);
     return;
   }
   // bf16: through LDS, so that a thread stores 16 bytes of a row (16384 x 8192 x 28672: 2.54 -> 2.42 ms)
@@ -75,7 +70,7 @@ __global__ __launch_bounds__(NT_THREADS, SH::LDS > 80 * 1024 ? 1 : 2) void mx_ge
           const nt_f32x4 &f = y < 2 ? v : u;
           w[y] = (int)((unsigned)mx_bf16(f[2 * (y & 1)]) | (unsigned)mx_bf16(f[2 * (y & 1) + 1]) << 16);
         }
-        __builtin_nontemporal_store(w, (nt_i32x4 *)to);
+        __builtin_nontemporal_store(w, (mx_i32x4_any *)to);
       } else {
 #pragma unroll
         for (int y = 0; y < 8; ++y)
@@ -225,19 +220,11 @@ __device__ __forceinline__ unsigned mx_scale(unsigned amax) {
   const int e = (int)(amax >> 23);                            // 255: infinity or NaN; 0: below 2^-126
   return e == 255 ? 255u : (unsigned)max(e - 2, 0);
 }
-// eight codes.  A scale of 2^-127 is no normal number: both sides 2^64 larger then.
+// eight codes.  The instruction takes the scale from the exponent's bits alone, so 2^-127 (all of them zero) needs no care, nor
+// do elements below 2^-126; what it makes of a block without a scale counts for nothing.
 __device__ __forceinline__ unsigned mx_codes(const MxVec<true> &v, unsigned scale) {
-  if (scale == 255u) return 0;
-  unsigned r = 0;
-  if (scale == 0) {
-    const float s = __builtin_bit_cast(float, 64u << 23);
-    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, ldexpf(__builtin_bit_cast(float, v.w[0]), 64), ldexpf(__builtin_bit_cast(float, v.w[1]), 64), s, 0);
-    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, ldexpf(__builtin_bit_cast(float, v.w[2]), 64), ldexpf(__builtin_bit_cast(float, v.w[3]), 64), s, 1);
-    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, ldexpf(__builtin_bit_cast(float, v.w[4]), 64), ldexpf(__builtin_bit_cast(float, v.w[5]), 64), s, 2);
-    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, ldexpf(__builtin_bit_cast(float, v.w[6]), 64), ldexpf(__builtin_bit_cast(float, v.w[7]), 64), s, 3);
-    return r;
-  }
   const float s = __builtin_bit_cast(float, scale << 23);
+  unsigned r = 0;
   r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, __builtin_bit_cast(float, v.w[0]), __builtin_bit_cast(float, v.w[1]), s, 0);
   r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, __builtin_bit_cast(float, v.w[2]), __builtin_bit_cast(float, v.w[3]), s, 1);
   r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, __builtin_bit_cast(float, v.w[4]), __builtin_bit_cast(float, v.w[5]), s, 2);
@@ -245,15 +232,6 @@ __device__ __forceinline__ unsigned mx_codes(const MxVec<true> &v, unsigned scal
   return r;
 }
 __device__ __forceinline__ unsigned mx_codes(const MxVec<false> &v, unsigned scale) {
-  if (scale == 0 || scale == 255u) {
-    MxVec<true> f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      f.w[2 * i] = v.w[i] << 16;
-      f.w[2 * i + 1] = v.w[i] & 0xffff0000u;
-    }
-    return mx_codes(f, scale);
-  }
   const float s = __builtin_bit_cast(float, scale << 23);
   unsigned r = 0;
   r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(mx_bf16x2, v.w[0]), s, 0);
@@ -263,18 +241,13 @@ __device__ __forceinline__ unsigned mx_codes(const MxVec<false> &v, unsigned sca
   return r;
 }
 
-// Eight elements of a row from column `col` on, zeros behind column w.  `wide`: rows are 16-byte aligned.
+// Eight elements of a row from column `col` on, zeros behind column w.  Rows may begin anywhere: the loads and stores of 16
+// bytes take any address (element by element 4099 x 2731 fp32 took 29 us along the columns, and its values 32).
 template <bool F32>
-__device__ __forceinline__ MxVec<F32> mx_load8(const char *row, int col, int w, bool wide) {
+__device__ __forceinline__ MxVec<F32> mx_load8(const char *row, int col, int w) {
   MxVec<F32> v;
-  if (wide && col + 8 <= w) {
-    const nt_i32x4 *p = (const nt_i32x4 *)(row + (int64_t)col * (F32 ? 4 : 2));
-    const nt_i32x4 x = p[0];
-    v.w[0] = x[0], v.w[1] = x[1], v.w[2] = x[2], v.w[3] = x[3];
-    if constexpr (F32) {
-      const nt_i32x4 y = p[1];
-      v.w[4] = y[0], v.w[5] = y[1], v.w[6] = y[2], v.w[7] = y[3];
-    }
+  if (col + 8 <= w) {
+    __builtin_memcpy(v.w, row + (int64_t)col * (F32 ? 4 : 2), sizeof v.w);
   } else {
 #pragma unroll
     for (int i = 0; i < MxVec<F32>::WORDS; ++i) {
@@ -318,7 +291,7 @@ __global__ __launch_bounds__(256) void mx_rows_kernel(MxTileArgs) {
   MxVec<F32> v[R];
 #pragma unroll
   for (int i = 0; i < R; ++i)
-    if (row0 + i < T.h) v[i] = mx_load8<F32>((const char *)T.x + (int64_t)(row0 + i) * T.x_pitch, col, T.w, T.wide);
+    if (row0 + i < T.h) v[i] = mx_load8<F32>((const char *)T.x + (int64_t)(row0 + i) * T.x_pitch, col, T.w);
 #pragma unroll
   for (int i = 0; i < R; ++i)
     if (row0 + i < T.h) {
@@ -328,67 +301,71 @@ __global__ __launch_bounds__(256) void mx_rows_kernel(MxTileArgs) {
     }
 }
 
-// Along the columns, and along the rows too if ROWS: a workgroup takes 128 rows of 128 columns, reads them along
-// the rows and leaves them in LDS, where each thread then finds its 32 rows of two columns.  Four threads make
-// the 64 bytes of a column's 128 codes.
+// Along the columns, and along the rows too if ROWS: a workgroup takes 128 rows of 256 bytes, reads them along the rows and leaves
+// them in LDS (33 KB: four workgroups on a CU), where each thread then finds its 32 rows of one or two columns.  Four threads
+// make the 64 bytes of a column's 128 codes.
+// 8192 x 8192 bf16 both ways: 54 us for 205 MB (3.8 TB/s; 4.6 is what a large copy makes).  A workgroup that goes on to other blocks
+// and loads them ahead made 53, blocks ordered so that lines of codes and scales are completed in one L2 55.
+template <bool F32>
+struct MxBlock {
+  static constexpr int ES = F32 ? 4 : 2, COLS = 256 / ES;     // 64 or 128 columns
+  static constexpr int PITCH = 256 + 4;                       // bytes (one word more: rows start in other banks)
+  static constexpr int LDS = 128 * PITCH;
+  static constexpr int ACROSS = COLS / 8, DOWN = 256 / ACROSS, PASSES = 128 / DOWN;   // threads to a row of a pass, rows of a pass
+  static constexpr int OWN = COLS / 64;                       // columns of a thread
+};
 template <bool F32, bool ROWS>
 __global__ __launch_bounds__(256) void mx_cols_kernel(MxTileArgs) {
-  constexpr int ES = F32 ? 4 : 2;
-  constexpr int PITCH = 128 * ES + 4;                         // bytes (one word more: rows start in other banks)
-  extern __shared__ char lds[];
+  using B = MxBlock<F32>;
+  __shared__ __attribute__((aligned(16))) char lds[B::LDS];
   const auto &args = *(const MxTileArgs *)__builtin_amdgcn_kernarg_segment_ptr();
   int block;
   const MxTile &T = mx_find(args, blockIdx.x, &block);
-  const int col0 = (block % T.blocks_across) * 128, row0 = block / T.blocks_across * 128;
+  const int col0 = (block % T.blocks_across) * B::COLS, row0 = block / T.blocks_across * 128;
   const int tid = threadIdx.x;
   {
-    const int col = col0 + (tid & 15) * 8;
+    const int col = col0 + tid % B::ACROSS * 8, r0 = tid / B::ACROSS;
+    MxVec<F32> v[B::PASSES];
 #pragma unroll
-    for (int pass = 0; pass < 8; pass += 4) {
-      MxVec<F32> v[4];
+    for (int x = 0; x < B::PASSES; ++x) {
+      const int row = row0 + x * B::DOWN + r0;
+      v[x] = row < T.h ? mx_load8<F32>((const char *)T.x + (int64_t)row * T.x_pitch, col, T.w) : MxVec<F32>{};
+    }
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const int row = row0 + (pass + x) * 16 + (tid >> 4);
-        v[x] = row < T.h ? mx_load8<F32>((const char *)T.x + (int64_t)row * T.x_pitch, col, T.w, T.wide) : MxVec<F32>{};
-      }
+    for (int x = 0; x < B::PASSES; ++x) {
+      const int r = x * B::DOWN + r0;
+      unsigned *p = (unsigned *)(lds + r * B::PITCH + tid % B::ACROSS * 8 * B::ES);
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const int r = (pass + x) * 16 + (tid >> 4);
-        unsigned *p = (unsigned *)(lds + r * PITCH + (tid & 15) * 8 * ES);
-#pragma unroll
-        for (int i = 0; i < MxVec<F32>::WORDS; ++i) p[i] = v[x].w[i];
-        if constexpr (ROWS) {
-          const unsigned scale = mx_scale(mx_max4(mx_abs_max(v[x])));
-          if (row0 + r < T.h) {
-            *(unsigned *)(T.row_codes + (int64_t)(row0 + r) * T.row_pitch + col / 2) = mx_codes(v[x], scale);
-            if ((tid & 3) == 0) T.row_scales[(int64_t)(row0 + r) * T.row_scale_pitch + col / 32] = (unsigned char)scale;
-          }
+      for (int i = 0; i < MxVec<F32>::WORDS; ++i) p[i] = v[x].w[i];
+      if constexpr (ROWS) {
+        const unsigned scale = mx_scale(mx_max4(mx_abs_max(v[x])));
+        // (with 64 columns a block may lie behind the last chunk)
+        if (row0 + r < T.h && col < ((T.w + 127) & ~127)) {
+          *(unsigned *)(T.row_codes + (int64_t)(row0 + r) * T.row_pitch + col / 2) = mx_codes(v[x], scale);
+          if ((tid & 3) == 0) T.row_scales[(int64_t)(row0 + r) * T.row_scale_pitch + col / 32] = (unsigned char)scale;
         }
       }
     }
   }
   __syncthreads();
-  // thread: rows 32 b ..., columns 2 p and 2 p + 1
+  // thread: rows 32 b ..., its columns
   const int b = tid & 3, p = tid >> 2;
-  unsigned words[2][F32 ? 32 : 16];                           // the two columns: 32 fp32, or 32 bf16 in pairs
+  unsigned words[B::OWN][F32 ? 32 : 16];                      // a column: 32 fp32, or 32 bf16 in pairs
 #pragma unroll
   for (int i = 0; i < 32; i += 2) {
-    const char *q = lds + (32 * b + i) * PITCH + p * 2 * ES;
+    const char *q = lds + (32 * b + i) * B::PITCH + p * 4;
+    const unsigned x = *(const unsigned *)q, y = *(const unsigned *)(q + B::PITCH);
     if constexpr (F32) {
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        words[c][i] = *(const unsigned *)(q + 4 * c);
-        words[c][i + 1] = *(const unsigned *)(q + PITCH + 4 * c);
-      }
+      words[0][i] = x;
+      words[0][i + 1] = y;
     } else {
-      const unsigned x = *(const unsigned *)q, y = *(const unsigned *)(q + PITCH);
       words[0][i / 2] = __builtin_amdgcn_perm(y, x, 0x05040100);   // low halves
       words[1][i / 2] = __builtin_amdgcn_perm(y, x, 0x07060302);   // high halves
     }
   }
 #pragma unroll
-  for (int c = 0; c < 2; ++c) {
-    const int col = col0 + 2 * p + c;
+  for (int c = 0; c < B::OWN; ++c) {
+    const int col = col0 + B::OWN * p + c;
     MxVec<F32> v[4];
     unsigned amax = 0;
 #pragma unroll
@@ -431,11 +408,9 @@ __device__ __forceinline__ MxVec<F32> mx_values(unsigned codes, unsigned scale) 
   return v;
 }
 template <bool F32>
-__device__ __forceinline__ void mx_store8(char *row, int col, int w, bool wide, const MxVec<F32> &v) {
-  if (wide && col + 8 <= w) {
-    nt_i32x4 *p = (nt_i32x4 *)(row + (int64_t)col * (F32 ? 4 : 2));
-    p[0] = nt_i32x4{(int)v.w[0], (int)v.w[1], (int)v.w[2], (int)v.w[3]};
-    if constexpr (F32) p[1] = nt_i32x4{(int)v.w[4], (int)v.w[5], (int)v.w[6], (int)v.w[7]};
+__device__ __forceinline__ void mx_store8(char *row, int col, int w, const MxVec<F32> &v) {
+  if (col + 8 <= w) {
+    __builtin_memcpy(row + (int64_t)col * (F32 ? 4 : 2), v.w, sizeof v.w);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
@@ -464,53 +439,48 @@ __global__ __launch_bounds__(256) void mx_row_values_kernel(MxTileArgs) {
     }
 #pragma unroll
   for (int i = 0; i < R; ++i)
-    if (row0 + i < T.h) mx_store8<F32>((char *)T.x + (int64_t)(row0 + i) * T.x_pitch, col, T.w, T.wide, mx_values<F32>(codes[i], scale[i]));
+    if (row0 + i < T.h) mx_store8<F32>((char *)T.x + (int64_t)(row0 + i) * T.x_pitch, col, T.w, mx_values<F32>(codes[i], scale[i]));
 }
 
-// 128 rows of 128 columns, turned through LDS the other way.
+// 128 rows of 64 or 128 columns, turned through LDS the other way.
 template <bool F32>
 __global__ __launch_bounds__(256) void mx_col_values_kernel(MxTileArgs) {
-  constexpr int ES = F32 ? 4 : 2;
-  constexpr int PITCH = 128 * ES + 4;
-  extern __shared__ char lds[];
+  using B = MxBlock<F32>;
+  __shared__ __attribute__((aligned(16))) char lds[B::LDS];
   const auto &args = *(const MxTileArgs *)__builtin_amdgcn_kernarg_segment_ptr();
   int block;
   const MxTile &T = mx_find(args, blockIdx.x, &block);
-  const int col0 = (block % T.blocks_across) * 128, row0 = block / T.blocks_across * 128;
+  const int col0 = (block % T.blocks_across) * B::COLS, row0 = block / T.blocks_across * 128;
   const int tid = threadIdx.x, b = tid & 3, p = tid >> 2;
-  nt_i32x4 codes[2];
-  unsigned scale[2];
+  nt_i32x4 codes[B::OWN];
+  unsigned scale[B::OWN];
 #pragma unroll
-  for (int c = 0; c < 2; ++c) {
-    const int col = min(col0 + 2 * p + c, T.w - 1);
+  for (int c = 0; c < B::OWN; ++c) {
+    const int col = min(col0 + B::OWN * p + c, T.w - 1);
     codes[c] = *(const nt_i32x4 *)(T.col_codes + (int64_t)col * T.col_pitch + (row0 / 32 + b) * 16);
     scale[c] = T.col_scales[(int64_t)col * T.col_scale_pitch + row0 / 32 + b];
   }
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    const MxVec<F32> x = mx_values<F32>((unsigned)codes[0][k], scale[0]), y = mx_values<F32>((unsigned)codes[1][k], scale[1]);
+    const MxVec<F32> x = mx_values<F32>((unsigned)codes[0][k], scale[0]), y = mx_values<F32>((unsigned)codes[B::OWN - 1][k], scale[B::OWN - 1]);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      char *q = lds + (32 * b + 8 * k + i) * PITCH + p * 2 * ES;
-      if constexpr (F32) {
-        *(unsigned *)q = x.w[i];
-        *(unsigned *)(q + 4) = y.w[i];
-      } else {
-        *(unsigned *)q = __builtin_amdgcn_perm(y.w[i / 2], x.w[i / 2], i & 1 ? 0x07060302 : 0x05040100);
-      }
+      unsigned *const q = (unsigned *)(lds + (32 * b + 8 * k + i) * B::PITCH + p * 4);
+      if constexpr (F32) *q = x.w[i];
+      else *q = __builtin_amdgcn_perm(y.w[i / 2], x.w[i / 2], i & 1 ? 0x07060302 : 0x05040100);
     }
   }
   __syncthreads();
-  const int col = col0 + (tid & 15) * 8;
+  const int col = col0 + tid % B::ACROSS * 8, r0 = tid / B::ACROSS;
 #pragma unroll
-  for (int pass = 0; pass < 8; ++pass) {
-    const int r = pass * 16 + (tid >> 4);
+  for (int pass = 0; pass < B::PASSES; ++pass) {
+    const int r = pass * B::DOWN + r0;
     if (row0 + r >= T.h) continue;
     MxVec<F32> v;
-    const unsigned *q = (const unsigned *)(lds + r * PITCH + (tid & 15) * 8 * ES);
+    const unsigned *q = (const unsigned *)(lds + r * B::PITCH + tid % B::ACROSS * 8 * B::ES);
 #pragma unroll
     for (int i = 0; i < MxVec<F32>::WORDS; ++i) v.w[i] = q[i];
-    mx_store8<F32>((char *)T.x + (int64_t)(row0 + r) * T.x_pitch, col, T.w, T.wide, v);
+    mx_store8<F32>((char *)T.x + (int64_t)(row0 + r) * T.x_pitch, col, T.w, v);
   }
 }
 

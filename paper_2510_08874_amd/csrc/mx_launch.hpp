@@ -44,8 +44,6 @@ struct MxTile {
   int64_t row_pitch, col_pitch, row_scale_pitch, col_scale_pitch;
   int32_t h, w;
   int32_t first_block, blocks_across;   // its workgroups begin here; as many side by side
-  int32_t wide;                 // rows of x are 16-byte aligned
-  int32_t pad;
 };
 // Travels as the kernel's argument: the call needs no memory of its own and no copy.
 constexpr int MX_TILES = 32;
@@ -61,6 +59,7 @@ struct MxShape {
 constexpr MxShape kMxShape[MX_SHAPES] = {{256, 256}, {128, 128}, {16, 16}, {32, 32}, {64, 32}};
 
 enum { MX_ALONG_ROWS = 1, MX_ALONG_COLS = 2 };
+constexpr int mx_block_cols(bool f32) { return f32 ? 64 : 128; }   // 128 rows of so many columns a workgroup, along the columns
 
 hipError_t mx_allow_lds();
 bool mx_launch(hipEvent_t behind, int shape, const MxItem *items, int n_items, const NtSeg *segs, const MxJoin *joins, int n_joins, int cus, hipStream_t stream);
