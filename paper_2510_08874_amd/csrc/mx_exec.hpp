@@ -2,6 +2,8 @@
 // tiles to be quantised handed to the kernels with the launch, products run from a plan's op list.
 #pragma once
 
+#include <cmath>
+
 namespace dmm {
 namespace {
 
@@ -125,12 +127,6 @@ int over_tiles(const Grid &G, int es, char *const *x, const int64_t *x_ld, const
 
 // ---- products -----------------------------------------------------------------------------------------
 
-// Workgroups that a shape keeps on a CU, and the K steps that a run of a tile cut along K has at least: a run
-// costs a tile's worth of partial sums written and read again.
-constexpr struct {
-  int per_cu, min_steps;
-} kMxRun[MX_SHAPES] = {{1, 12}, {2, 6}, {4, 8}, {3, 8}, {2, 8}};
-
 // Blocks of A and of B have to meet: every op starts at a whole chunk of both tiles.  (It then ends at one, or where
 // both tiles end: the next op starts there.)
 int check_chunks(const dmm_plan_t *P) {
@@ -139,17 +135,69 @@ int check_chunks(const dmm_plan_t *P) {
   return DMM_OK;
 }
 
-// The shape whose tiles fill the device best.
-int choose_mx(const dmm_plan_t *P, int cus) {
-  int64_t most = 0, tiles256 = 0;
-  for (const Group &g : P->groups) {
+// Which kernel runs a plan's product, and into how many ranges of K its tiles are cut.
+struct MxChoice {
+  int shape = MX_256;
+  int64_t runs = 1;                    // of a tile of average length
+};
+
+// By an estimate in us.  A step (256 of k) of a tile costs its matrix instructions, or what L2 takes with many tiles at a time; few rows
+// wait for B from memory.  Measured on tiles alone: 256 x 256 1.25 to 1.78 a step (64 and 256 of them), 128 x 128 0.53 to 0.66
+// (36, 256), two on a CU 1.13; 32 rows against 117 MB of B 4.6 TB/s.  A tile cut along K costs its partial sums
+// and a launch that adds them up.
+MxChoice choose_mx(const dmm_plan_t *P, int cus) {
+  int64_t most = 0;                    // rows of a group
+  double cells = 0, k_steps = 0, b_bytes = 0;
+  for (size_t x = 0; x < P->groups.size(); ++x) {
+    const Group &g = P->groups[x];
     most = std::max(most, g.m1 - g.m0);
-    tiles256 += ((g.m1 - g.m0 + 255) / 256) * ((g.n1 - g.n0 + 255) / 256);
+    int64_t steps = 0;
+    for (int64_t y = g.first; y < g.first + g.count; ++y) {
+      const dmm_task &t = P->tasks[(size_t)P->order[(size_t)y]];
+      steps += (t.k1 - t.k0 + 255) / 256;
+    }
+    const double area = (double)(g.m1 - g.m0) * (double)(g.n1 - g.n0);
+    cells += area;
+    k_steps += area * (double)steps;
+    b_bytes += (double)(g.n1 - g.n0) * (double)steps * 136.0;
   }
-  if (most <= 16) return MX_SKINNY_16;
-  if (most <= 32) return MX_SKINNY_32;
-  if (most <= 64) return MX_SKINNY_64;
-  return tiles256 * 4 >= cus * 3 ? MX_256 : MX_128;
+  const double steps = cells > 0 ? k_steps / cells : 0;
+  MxChoice best;
+  double best_us = 0;
+  for (int shape = 0; shape < MX_SHAPES; ++shape) {
+    const int tm = kMxShape[shape].tm, tn = kMxShape[shape].tn;
+    if ((shape == MX_SKINNY && most > tm) || (shape == MX_32 && most > tm) || (shape == MX_64 && most > tm)) continue;
+    double tiles = 0;
+    for (const Group &g : P->groups) tiles += (double)(((g.m1 - g.m0 + tm - 1) / tm) * ((g.n1 - g.n0 + tn - 1) / tn));
+    if (tiles == 0) return best;
+    if (shape == MX_SKINNY) {
+      // (every eighth pair of chunks is a wave's next; 16 rows of A are read with every 16 columns of B)
+      const double us = 2.5 + std::max(0.8 * std::ceil(steps / 8) * std::ceil(tiles / (8.0 * cus)), b_bytes / (most <= 2 ? 4.2e6 : 3.0e6));
+      if (best_us == 0 || us < best_us) best_us = us, best.shape = shape, best.runs = 1;
+      continue;
+    }
+    const int places = shape == MX_256 ? cus : 2 * cus;
+    for (int64_t runs = 1; runs <= 32; ++runs) {
+      const double work = tiles * (double)runs, per = std::ceil(steps / (double)runs);
+      if (runs > 1 && (work > places || per < 3)) break;
+      // rounds of all places, and one of the rest
+      auto round = [&](double n) {
+        if (n <= 0) return 0.0;
+        const double full = n / cus;
+        switch (shape) {
+          case MX_256: return per * (1.2 + 0.55 * full) + 8.0;
+          case MX_128: return per * (full > 1 ? 1.13 : 0.5 + 0.16 * full) + 4.5;
+          default: return per * (full > 1 ? 0.75 : 0.45) + 3.5;
+        }
+      };
+      const double whole = std::floor(work / places);
+      double us = whole * round(places) + round(work - whole * places);
+      if (shape >= MX_64) us = std::max(us, b_bytes / 4.6e6);
+      if (runs > 1) us += 4.5 + 2.0 * work * tm * tn * 4 / 3e6;
+      if (best_us == 0 || us < best_us) best_us = us, best.shape = shape, best.runs = runs;
+    }
+  }
+  return best;
 }
 
 int build_mx(dmm_plan_t *P, const dmm_mx_tiles *a, const dmm_mx_tiles *b, void *const *c_tiles, const int64_t *c_ld, int c_es, int cus,
@@ -184,7 +232,8 @@ int build_mx(dmm_plan_t *P, const dmm_mx_tiles *a, const dmm_mx_tiles *b, void *
   }
   group_seg.push_back((int32_t)segs.size());
 
-  const int shape = choose_mx(P, cus);
+  const MxChoice choice = choose_mx(P, cus);
+  const int shape = choice.shape;
   const int tm = kMxShape[shape].tm, tn = kMxShape[shape].tn;
   auto corner = [&](int32_t rep, int32_t ti, int32_t tj, int64_t m0, int64_t n0, MxItem *it) {
     const int64_t i = C.table_index(rep, ti, tj);
@@ -194,55 +243,48 @@ int build_mx(dmm_plan_t *P, const dmm_mx_tiles *a, const dmm_mx_tiles *b, void *
     it->pad = 0;
     return c_tiles[i] != nullptr;
   };
-  int64_t tiles = 0;
-  for (const Group &g : P->groups) tiles += ((g.m1 - g.m0 + tm - 1) / tm) * ((g.n1 - g.n0 + tn - 1) / tn);
-  const int64_t places = (int64_t)cus * kMxRun[shape].per_cu;
   std::vector<MxItem> items;
   std::vector<MxJoin> joins;
   int64_t slots = 0;
   for (size_t x = 0; x < P->groups.size(); ++x) {
     const Group &g = P->groups[x];
     const int64_t rows = (g.m1 - g.m0 + tm - 1) / tm, cols = (g.n1 - g.n0 + tn - 1) / tn;
-    // cut along K where the tiles leave half of the device idle
-    int64_t runs = tiles * 2 <= places ? std::min<int64_t>(places / tiles, group_steps[x] / kMxRun[shape].min_steps) : 1;
-    if (runs < 1) runs = 1;
+    int64_t runs = std::min<int64_t>(choice.runs, std::max(1, group_steps[x] / 3));
     const int32_t per = (int32_t)((group_steps[x] + runs - 1) / runs);
     runs = (group_steps[x] + per - 1) / per;
-    // bands of eight tile rows, column by column: neighbours in the list share operands
-    for (int64_t r0 = 0; r0 < rows; r0 += 8)
-      for (int64_t c = 0; c < cols; ++c)
-        for (int64_t r = r0; r < std::min(r0 + 8, rows); ++r) {
-          MxItem it;
-          if (!corner(g.c_rep, g.c_ti, g.c_tj, g.m0 + r * tm, g.n0 + c * tn, &it)) return DMM_EINVAL;
-          it.m_off = (int32_t)(r * tm);
-          it.n_off = (int32_t)(c * tn);
-          it.m_ext = (int32_t)std::min<int64_t>(tm, g.m1 - g.m0 - r * tm);
-          it.n_ext = (int32_t)std::min<int64_t>(tn, g.n1 - g.n0 - c * tn);
-          if (runs == 1) {
-            it.seg = group_seg[x];
-            it.n_segs = group_seg[x + 1] - group_seg[x];
-            it.first = 0;
-            it.steps = group_steps[x];
+    // bands of eight tile rows, column by column: neighbours in the list share operands.  All first ranges of K, then all second ones, ...
+    const int64_t first_slot = slots;
+    int32_t seg = group_seg[x], first = 0;
+    for (int64_t run = 0; run < runs; ++run) {
+      const int32_t n_steps = std::min<int32_t>(per, group_steps[x] - (int32_t)run * per);
+      int64_t tile = 0;
+      for (int64_t r0 = 0; r0 < rows; r0 += 8)
+        for (int64_t c = 0; c < cols; ++c)
+          for (int64_t r = r0; r < std::min(r0 + 8, rows); ++r, ++tile) {
+            MxItem it;
+            if (!corner(g.c_rep, g.c_ti, g.c_tj, g.m0 + r * tm, g.n0 + c * tn, &it)) return DMM_EINVAL;
+            it.m_off = (int32_t)(r * tm);
+            it.n_off = (int32_t)(c * tn);
+            it.m_ext = (int32_t)std::min<int64_t>(tm, g.m1 - g.m0 - r * tm);
+            it.n_ext = (int32_t)std::min<int64_t>(tn, g.n1 - g.n0 - c * tn);
+            it.seg = seg;
+            it.n_segs = group_seg[x + 1] - seg;
+            it.first = first;
+            it.steps = n_steps;
+            if (runs > 1) {
+              const int64_t slot = first_slot + tile * runs;
+              if (run == 0) joins.push_back({it.c, it.ldc, (const float *)(uintptr_t)slot, (int32_t)runs, tm, tn, it.m_ext, it.n_ext, c_es});
+              it.c = (char *)(uintptr_t)(slot + run);
+              it.ldc = tn;
+              it.c_es = 4;
+              it.pad = 1;
+              ++slots;
+            }
             items.push_back(it);
-            continue;
           }
-          joins.push_back({it.c, it.ldc, (const float *)(uintptr_t)slots, (int32_t)runs, tm, tn, it.m_ext, it.n_ext, c_es});
-          int32_t seg = group_seg[x], first = 0;
-          for (int32_t at = 0; at < group_steps[x]; at += per) {
-            MxItem part = it;
-            part.seg = seg;
-            part.n_segs = group_seg[x + 1] - seg;
-            part.first = first;
-            part.steps = std::min(per, group_steps[x] - at);
-            part.c = (char *)(uintptr_t)slots++;
-            part.ldc = tn;
-            part.c_es = 4;
-            part.pad = 1;
-            items.push_back(part);
-            first += part.steps;
-            while (seg < group_seg[x + 1] && first >= (segs[(size_t)seg].chunks + 1) / 2) first -= (segs[(size_t)seg++].chunks + 1) / 2;
-          }
-        }
+      first += n_steps;
+      while (seg < group_seg[x + 1] && first >= (segs[(size_t)seg].chunks + 1) / 2) first -= (segs[(size_t)seg++].chunks + 1) / 2;
+    }
   }
   // regions of C that no op writes: zeros
   for (const dmm_work_item &w : P->items) {

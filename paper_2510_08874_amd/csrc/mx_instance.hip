@@ -6,11 +6,18 @@ namespace {
 
 using Mx256 = NtShape<true, 256>;
 using Mx128 = NtShape<true, 128>;            // two workgroups on a CU
-using Mx128Deep = NtShape<true, 128, 4>;     // one, which then has three steps on their way
-static_assert(kMxShape[MX_256].tm == Mx256::TM && kMxShape[MX_256].tn == Mx256::TN && kMxShape[MX_128].tm == Mx128::TM &&
-                  kMxShape[MX_128].tn == Mx128::TN && kMxShape[MX_SKINNY_16].tn == 16 && kMxShape[MX_SKINNY_32].tn == 32 &&
-                  kMxShape[MX_SKINNY_64].tn == 32,
+using Mx128Deep = NtShape<true, 128, 128, 4>;     // one, which then has three steps on their way
+using Mx64 = NtShape<true, 64, 128, 2>;          // few rows: bound by the bytes of B
+using Mx32 = NtShape<true, 32, 128, 3, 1>;
+template <class SH>
+constexpr bool same(int shape) { return kMxShape[shape].tm == SH::TM && kMxShape[shape].tn == SH::TN; }
+static_assert(same<Mx256>(MX_256) && same<Mx128>(MX_128) && same<Mx64>(MX_64) && same<Mx32>(MX_32) && kMxShape[MX_SKINNY].tn == 16,
               "the host cuts tiles as the kernels expect them");
+
+template <class SH>
+hipError_t allow() {
+  return hipFuncSetAttribute((const void *)mx_gemm_kernel<SH>, hipFuncAttributeMaxDynamicSharedMemorySize, SH::LDS);
+}
 
 template <class SH>
 bool launch(hipEvent_t behind, const MxItem *items, int n, const NtSeg *segs, hipStream_t stream) {
@@ -22,9 +29,11 @@ static_assert(MxBlock<false>::COLS == mx_block_cols(false) && MxBlock<true>::COL
 }  // namespace
 
 hipError_t mx_allow_lds() {
-  hipError_t e = hipFuncSetAttribute((const void *)mx_gemm_kernel<Mx256>, hipFuncAttributeMaxDynamicSharedMemorySize, Mx256::LDS);
-  if (e == hipSuccess) e = hipFuncSetAttribute((const void *)mx_gemm_kernel<Mx128>, hipFuncAttributeMaxDynamicSharedMemorySize, Mx128::LDS);
-  if (e == hipSuccess) e = hipFuncSetAttribute((const void *)mx_gemm_kernel<Mx128Deep>, hipFuncAttributeMaxDynamicSharedMemorySize, Mx128Deep::LDS);
+  hipError_t e = allow<Mx256>();
+  if (e == hipSuccess) e = allow<Mx128>();
+  if (e == hipSuccess) e = allow<Mx128Deep>();
+  if (e == hipSuccess) e = allow<Mx64>();
+  if (e == hipSuccess) e = allow<Mx32>();
   return e;
 }
 
@@ -34,9 +43,9 @@ bool mx_launch(hipEvent_t behind, int shape, const MxItem *items, int n_items, c
   switch (shape) {
     case MX_256: marked = launch<Mx256>(last, items, n_items, segs, stream); break;
     case MX_128: marked = n_items <= cus ? launch<Mx128Deep>(last, items, n_items, segs, stream) : launch<Mx128>(last, items, n_items, segs, stream); break;
-    case MX_SKINNY_16: marked = launch_behind(last, mx_skinny_kernel<1, 1>, (unsigned)n_items, NT_THREADS, 0, stream, items, segs); break;
-    case MX_SKINNY_32: marked = launch_behind(last, mx_skinny_kernel<2, 2>, (unsigned)n_items, NT_THREADS, 0, stream, items, segs); break;
-    default: marked = launch_behind(last, mx_skinny_kernel<4, 2>, (unsigned)n_items, NT_THREADS, 0, stream, items, segs); break;
+    case MX_64: marked = launch<Mx64>(last, items, n_items, segs, stream); break;
+    case MX_32: marked = launch<Mx32>(last, items, n_items, segs, stream); break;
+    default: marked = launch_behind(last, mx_skinny_kernel, (unsigned)n_items, NT_THREADS, 0, stream, items, segs); break;
   }
   if (!n_joins || hipPeekAtLastError() != hipSuccess) return marked;
   const int per = (kMxShape[shape].tm * kMxShape[shape].tn + 1023) / 1024;

@@ -19,12 +19,12 @@ namespace dmm {
 typedef int mx_i32x4_any __attribute__((ext_vector_type(4), aligned(2)));   // (16 bytes at any address of a bf16)
 __device__ __forceinline__ unsigned short mx_bf16(float v) { return __builtin_bit_cast(unsigned short, (__bf16)v); }
 
-// (the host sees to it that a macro-tile's rows lie within 2^32 bytes)
-template <class SH>
+// Half a wave stores 32 neighbouring columns of a row.  (The host sees to it that a macro-tile's rows lie within 2^32 bytes.)
+template <class SH, class E>
 __device__ __forceinline__ void mx_store(const NtTile<SH> &tile, const MxItem &it) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int row0 = (wave >> 1) * (SH::TM / 2) + 4 * (lane >> 5), col0 = (wave & 1) * (SH::TN / 2) + (lane & 31);
-  const unsigned pitch = (unsigned)it.ldc * 4u;
+  const int row0 = wave / SH::WN * (SH::TM / SH::WM) + 4 * (lane >> 5), col0 = wave % SH::WN * (SH::TN / SH::WN) + (lane & 31);
+  const unsigned pitch = (unsigned)it.ldc * (unsigned)sizeof(E);
   char *const c = (char *)nt_uniform(it.c);
 #pragma unroll
   for (int i = 0; i < SH::MI; ++i)
@@ -35,7 +35,11 @@ __device__ __forceinline__ void mx_store(const NtTile<SH> &tile, const MxItem &i
 #pragma unroll
         for (int x = 0; x < 16; ++x) {
           const int row = row0 + 32 * i + 8 * (x / 4) + x % 4;
-          if (row < it.m_ext) __builtin_nontemporal_store(tile.acc[i][j][x], (float *)(c + ((unsigned)row * pitch + (unsigned)col * 4u)));
+          if (row < it.m_ext) {
+            E *const to = (E *)(c + ((unsigned)row * pitch + (unsigned)col * (unsigned)sizeof(E)));
+            if constexpr (sizeof(E) == 4) __builtin_nontemporal_store(tile.acc[i][j][x], to);
+            else __builtin_nontemporal_store(mx_bf16(tile.acc[i][j][x]), to);
+          }
         }
       }
       __builtin_amdgcn_sched_barrier(0);
@@ -52,32 +56,38 @@ __global__ __launch_bounds__(NT_THREADS, SH::LDS > 80 * 1024 ? 1 : 2) void mx_ge
   tile.pin();
   // fp32: half a wave writes 32 neighbouring columns of a row
   if (it.c_es == 4) {
-    mx_store(tile, it);
+    mx_store<SH, float>(tile, it);
+    return;
+  }
+  if constexpr (SH::WM == 1) {
+    mx_store<SH, unsigned short>(tile, it);
     return;
   }
   // bf16: through LDS, so that a thread stores 16 bytes of a row (16384 x 8192 x 28672: 2.54 -> 2.42 ms)
-  tile.slices(lds, [&](const float *values, int base) {
-    constexpr int PER = SH::TN / 8;
-    for (int x = threadIdx.x; x < 64 * PER; x += NT_THREADS) {
-      const int r = x / PER, col = x % PER * 8, row = base + (r & 31) + (r >> 5) * (SH::TM / 2);
-      if (row >= it.m_ext || col >= it.n_ext) continue;
-      const nt_f32x4 *const from = (const nt_f32x4 *)(values + nt_value(r, col, NtTile<SH>::PITCH)), v = from[0], u = from[1];
-      char *const to = it.c + ((int64_t)row * it.ldc + col) * 2;
-      if (col + 8 <= it.n_ext) {
-        nt_i32x4 w;
+  if constexpr (SH::WM == 2) {
+    tile.slices(lds, [&](const float *values, int base) {
+      constexpr int PER = SH::TN / 8;
+      for (int x = threadIdx.x; x < 64 * PER; x += NT_THREADS) {
+        const int r = x / PER, col = x % PER * 8, row = base + (r & 31) + (r >> 5) * (SH::TM / 2);
+        if (row >= it.m_ext || col >= it.n_ext) continue;
+        const nt_f32x4 *const from = (const nt_f32x4 *)(values + nt_value(r, col, NtTile<SH>::PITCH)), v = from[0], u = from[1];
+        char *const to = it.c + ((int64_t)row * it.ldc + col) * 2;
+        if (col + 8 <= it.n_ext) {
+          nt_i32x4 w;
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          const nt_f32x4 &f = y < 2 ? v : u;
-          w[y] = (int)((unsigned)mx_bf16(f[2 * (y & 1)]) | (unsigned)mx_bf16(f[2 * (y & 1) + 1]) << 16);
+          for (int y = 0; y < 4; ++y) {
+            const nt_f32x4 &f = y < 2 ? v : u;
+            w[y] = (int)((unsigned)mx_bf16(f[2 * (y & 1)]) | (unsigned)mx_bf16(f[2 * (y & 1) + 1]) << 16);
+          }
+          __builtin_nontemporal_store(w, (mx_i32x4_any *)to);
+        } else {
+#pragma unroll
+          for (int y = 0; y < 8; ++y)
+            if (col + y < it.n_ext) ((unsigned short *)to)[y] = mx_bf16(y < 4 ? v[y] : u[y - 4]);
         }
-        __builtin_nontemporal_store(w, (mx_i32x4_any *)to);
-      } else {
-#pragma unroll
-        for (int y = 0; y < 8; ++y)
-          if (col + y < it.n_ext) ((unsigned short *)to)[y] = mx_bf16(y < 4 ? v[y] : u[y - 4]);
       }
-    }
-  });
+    });
+  }
 }
 
 // Sums of partial tiles, in ascending k.
@@ -99,94 +109,60 @@ __global__ __launch_bounds__(256) void mx_join_kernel(const MxJoin *__restrict__
     }
 }
 
-// A few rows against many columns: bound by the bytes of B, which every wave reads straight into registers.  A
-// workgroup owns 16 NT columns and 16 MT rows; its four waves take every fourth 512 elements of K each and add up
-// through LDS, so that there are enough waves on the way to memory without partial sums in memory.
-template <int MT, int NT>
+// Up to 16 rows against little B: every wave reads B straight into registers.  A workgroup owns 16 columns; its four waves take
+// every fourth 512 elements of K each and add up through LDS, so that there are enough waves on the way to memory without partial
+// sums in memory.  (1 x 4096 x 4096 4.6 us where tiles of 32 x 128 cut along K take 5.9 and the sum of their runs; B
+// of 117 MB that no cache holds at 4.0 TB/s with one row, 2.9 with 16, the tiles at 4.5 to 4.9.)
 __global__ __launch_bounds__(NT_THREADS) void mx_skinny_kernel(const MxItem *__restrict__ items, const NtSeg *__restrict__ segs) {
   constexpr int Q = 4;                                        // chunks (128 of k) at a time
-  __shared__ nt_f32x4 sums[4][MT * NT][64];
+  __shared__ nt_f32x4 sums[4][64];
   const MxItem it = items[blockIdx.x];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, g = lane >> 4;
-  nt_f32x4 acc[MT][NT];
-#pragma unroll
-  for (int i = 0; i < MT; ++i)
-#pragma unroll
-    for (int j = 0; j < NT; ++j) acc[i][j] = nt_f32x4{0.f, 0.f, 0.f, 0.f};
+  nt_f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   int todo = it.steps, skip = it.first;
   for (int sg = 0; todo > 0; ++sg) {
     const NtSeg s = segs[it.seg + sg];
     const int n = min(s.chunks - 2 * skip, 2 * todo);
-    const char *pa[MT], *pb[NT], *sa[MT], *sb[NT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      const int64_t row = it.m_off + min(16 * i + r, it.m_ext - 1);
-      pa[i] = s.a + row * s.a_pitch + (int64_t)skip * NT_ROW + g * 16;
-      sa[i] = s.a_scale + row * s.a_scale_pitch + (int64_t)skip * 8;
-    }
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      const int64_t row = it.n_off + min(16 * j + r, it.n_ext - 1);
-      pb[j] = s.b + row * s.b_pitch + (int64_t)skip * NT_ROW + g * 16;
-      sb[j] = s.b_scale + row * s.b_scale_pitch + (int64_t)skip * 8;
-    }
-    auto multiply = [&](nt_i32x4 a, nt_i32x4 b, int as, int bs, nt_f32x4 c) {
+    const int64_t row_a = it.m_off + min(r, it.m_ext - 1), row_b = it.n_off + min(r, it.n_ext - 1);
+    const char *const pa = s.a + row_a * s.a_pitch + (int64_t)skip * NT_ROW + g * 16, *const sa = s.a_scale + row_a * s.a_scale_pitch + (int64_t)skip * 8;
+    const char *const pb = s.b + row_b * s.b_pitch + (int64_t)skip * NT_ROW + g * 16, *const sb = s.b_scale + row_b * s.b_scale_pitch + (int64_t)skip * 8;
+    auto multiply = [&](nt_i32x4 a, nt_i32x4 b, int as, int bs) {
       const nt_i32x8 x = {b[0], b[1], b[2], b[3], 0, 0, 0, 0};
       const nt_i32x8 y = {a[0], a[1], a[2], a[3], 0, 0, 0, 0};
-      return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, c, 4, 4, 0, (int)((unsigned)bs >> (8 * g)), 0, (int)((unsigned)as >> (8 * g)));
+      acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, acc, 4, 4, 0, (int)((unsigned)bs >> (8 * g)), 0, (int)((unsigned)as >> (8 * g)));
     };
     int t = wave * Q;
     for (; t + Q <= n; t += 4 * Q) {
-      nt_i32x4 a[MT][Q], b[NT][Q], as[MT], bs[NT];
+      nt_i32x4 a[Q], b[Q], as, bs;
+      __builtin_memcpy(&bs, sb + t * 4, 16);
 #pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        __builtin_memcpy(&bs[j], sb[j] + t * 4, 16);
+      for (int q = 0; q < Q; ++q) b[q] = __builtin_nontemporal_load((const nt_i32x4 *)(pb + (t + q) * NT_CHUNK));
+      __builtin_memcpy(&as, sa + t * 4, 16);
 #pragma unroll
-        for (int q = 0; q < Q; ++q) b[j][q] = __builtin_nontemporal_load((const nt_i32x4 *)(pb[j] + (t + q) * NT_CHUNK));
-      }
+      for (int q = 0; q < Q; ++q) a[q] = *(const nt_i32x4 *)(pa + (t + q) * NT_CHUNK);
 #pragma unroll
-      for (int i = 0; i < MT; ++i) {
-        __builtin_memcpy(&as[i], sa[i] + t * 4, 16);
-#pragma unroll
-        for (int q = 0; q < Q; ++q) a[i][q] = *(const nt_i32x4 *)(pa[i] + (t + q) * NT_CHUNK);
-      }
-#pragma unroll
-      for (int q = 0; q < Q; ++q)
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-          for (int j = 0; j < NT; ++j) acc[i][j] = multiply(a[i][q], b[j][q], as[i][q], bs[j][q], acc[i][j]);
+      for (int q = 0; q < Q; ++q) multiply(a[q], b[q], as[q], bs[q]);
     }
     // the last, incomplete 512 elements: one wave's t ends in front of them, the others' behind
     for (; t < n; ++t)
-#pragma unroll
-      for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-          acc[i][j] = multiply(*(const nt_i32x4 *)(pa[i] + t * NT_CHUNK), *(const nt_i32x4 *)(pb[j] + t * NT_CHUNK), *(const int *)(sa[i] + t * 4),
-                               *(const int *)(sb[j] + t * 4), acc[i][j]);
+      multiply(*(const nt_i32x4 *)(pa + t * NT_CHUNK), *(const nt_i32x4 *)(pb + t * NT_CHUNK), *(const int *)(sa + t * 4), *(const int *)(sb + t * 4));
     todo -= (n + 1) >> 1;
     skip = 0;
   }
-#pragma unroll
-  for (int i = 0; i < MT; ++i)
-#pragma unroll
-    for (int j = 0; j < NT; ++j) sums[wave][i * NT + j][lane] = acc[i][j];
+  sums[wave][lane] = acc;
   __syncthreads();
-  for (int x = wave; x < MT * NT; x += 4) {
-    const nt_f32x4 v = ((sums[0][x][lane] + sums[1][x][lane]) + sums[2][x][lane]) + sums[3][x][lane];
-    // row r of A's tile x / NT, columns 4 g ... of B's tile x % NT
-    const int row = 16 * (x / NT) + r, col = 16 * (x % NT) + 4 * g;
-    if (row < it.m_ext) {
+  if (wave) return;
+  const nt_f32x4 v = ((sums[0][lane] + sums[1][lane]) + sums[2][lane]) + sums[3][lane];
+  const int col = 4 * g;                                      // row r, columns 4 g ...
+  if (r < it.m_ext) {
 #pragma unroll
-      for (int y = 0; y < 4; ++y)
-        if (col + y < it.n_ext) {
-          const int64_t at = (int64_t)row * it.ldc + col + y;
-          if (it.c_es == 4) ((float *)it.c)[at] = v[y];
-          else ((unsigned short *)it.c)[at] = mx_bf16(v[y]);
-        }
-    }
+    for (int y = 0; y < 4; ++y)
+      if (col + y < it.n_ext) {
+        const int64_t at = (int64_t)r * it.ldc + col + y;
+        if (it.c_es == 4) ((float *)it.c)[at] = v[y];
+        else ((unsigned short *)it.c)[at] = mx_bf16(v[y]);
+      }
   }
 }
 

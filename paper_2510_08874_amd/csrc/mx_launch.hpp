@@ -52,11 +52,11 @@ struct MxTileArgs {
   MxTile tile[MX_TILES];
 };
 
-enum { MX_256, MX_128, MX_SKINNY_16, MX_SKINNY_32, MX_SKINNY_64, MX_SHAPES };
+enum { MX_256, MX_128, MX_64, MX_32, MX_SKINNY, MX_SHAPES };
 struct MxShape {
   int tm, tn;
 };
-constexpr MxShape kMxShape[MX_SHAPES] = {{256, 256}, {128, 128}, {16, 16}, {32, 32}, {64, 32}};
+constexpr MxShape kMxShape[MX_SHAPES] = {{256, 256}, {128, 128}, {64, 128}, {32, 128}, {16, 16}};
 
 enum { MX_ALONG_ROWS = 1, MX_ALONG_COLS = 2 };
 constexpr int mx_block_cols(bool f32) { return f32 ? 64 : 128; }   // 128 rows of so many columns a workgroup, along the columns

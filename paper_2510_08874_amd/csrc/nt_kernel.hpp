@@ -79,29 +79,30 @@ __device__ __forceinline__ void nt_for(F &&f) {
 // of a column, eight rows apart, lie in different banks (and eight neighbouring columns of a row stay together).
 __device__ __forceinline__ int nt_value(int row, int col, int pitch) { return row * pitch + (col ^ (row & 56)); }
 
-// SCALED: 4-bit codes with scales; otherwise pairs of fp16.  EDGE x EDGE macro-tile over 2 x 2 waves, NST stages.
-template <bool SCALED_, int EDGE, int NST_ = 2>
+// SCALED: 4-bit codes with scales; otherwise pairs of fp16.  TM x TN macro-tile over WM x (4 / WM) waves, NST stages.
+template <bool SCALED_, int TM_, int TN_ = TM_, int NST_ = 2, int WM_ = 2>
 struct NtShape {
   static constexpr bool SCALED = SCALED_;
-  static constexpr int TM = EDGE, TN = EDGE, NST = NST_;
-  static constexpr int MI = TM / 64, NI = TN / 64;           // 32 x 32 tiles of a wave
+  static constexpr int TM = TM_, TN = TN_, NST = NST_, WM = WM_, WN = 4 / WM;
+  static constexpr int MI = TM / WM / 32, NI = TN / WN / 32; // 32 x 32 tiles of a wave
   static constexpr int A_BYTES = TM * NT_ROW, B_BYTES = TN * NT_ROW, STAGE = A_BYTES + B_BYTES;
-  // scales of two steps together, 16 bytes a row: a request fetches them once
-  static constexpr int S_ROW = 16, S_SLOT = SCALED ? (TM + TN) * S_ROW : 0;
+  // scales of two steps together, 16 bytes a row: a request fetches them once.  Units of 64 rows, A's in front of B's
+  static constexpr int S_ROW = 16, S_A = (TM + 63) / 64, S_UNITS = SCALED ? S_A + TN / 64 : 0, S_SLOT = S_UNITS * 64 * S_ROW;
   // slots: of the step whose scales are read, of those under way, and of the one behind them; every step may be a segment's last
   static constexpr int SLOTS = NST + 1;
   static constexpr int LDS = NST * STAGE + SLOTS * S_SLOT;
   static constexpr int LA = TM / 32, LB = TN / 32;           // 1 KB loads of a wave and step, 8 rows each
   static constexpr int LOADS = LA + LB;
   static constexpr int EARLY = SCALED ? LOADS / 2 : LOADS;   // so many behind the barrier, the others in the next step's first quarter
-  static constexpr int S_ROWS = SCALED ? (TM + TN) / 4 : 0;  // rows whose scales a wave loads
-  static_assert(TM == TN && TM % 128 == 0, "a wave loads 64 or 128 rows of scales of one operand");
+  static constexpr int LS = (S_UNITS + 3) / 4;               // units of a wave: one with the first of two steps, one with the second
+  static_assert(TM % (32 * WM) == 0 && TN % (32 * WN) == 0 && TN % 64 == 0 && LS <= 2, "whole matrix tiles and units of scales");
+  static_assert(NST >= 2 && (NST - 1) * LOADS < 64 && LDS <= 160 * 1024, "the counter of loads, the LDS of a CU");
 };
 
 // Rows of a macro-tile past `ext` are read from its last row: they are never stored.
 template <class SH>
 struct NtTile {
-  // [i][j][x]: row 32 i + 8 (x / 4) + 4 (lane / 32) + x % 4, column 32 j + lane % 32 of the wave's quarter
+  // [i][j][x]: row 32 i + 8 (x / 4) + 4 (lane / 32) + x % 4, column 32 j + lane % 32 of the wave's part
   nt_f32x16 acc[SH::MI][SH::NI];
 
   // The sums are in accumulator registers here: keeps the compiler from moving them about, and from moving matrix
@@ -114,9 +115,9 @@ struct NtTile {
   // of `values` and row + TM / 2 ... in rows 32 .. 63, every element at nt_value(row, column, PITCH).  Every thread gets there between
   // two barriers.
   static constexpr int PITCH = SH::TN + 4;
-  static_assert(64 * PITCH * 4 <= SH::LDS, "a slice lies in the stages");
   template <class F>
   __device__ __forceinline__ void slices(char *lds, F &&use) {
+    static_assert(SH::WM == 2 && 64 * PITCH * 4 <= SH::LDS, "a slice is 64 rows and lies in the stages");
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     float *const values = (float *)lds;
     float *const mine = values + ((wave >> 1) * 32 + 4 * (lane >> 5)) * PITCH;
@@ -142,7 +143,7 @@ struct NtTile {
     constexpr int MI = SH::MI, NI = SH::NI, LA = SH::LA, LB = SH::LB;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wm = wave >> 1, wn = wave & 1;
+    const int wm = wave / SH::WN, wn = wave % SH::WN;
     const unsigned lds0 = (unsigned)(uintptr_t)(nt_lptr)lds;
 #pragma unroll
     for (int i = 0; i < MI; ++i)
@@ -157,11 +158,12 @@ struct NtTile {
     unsigned aoff[LA], boff[LB];
     nt_gptr a = nullptr, b = nullptr;
     int chunks = 0, on = NT_ROW;                              // chunks left to load in this segment; bytes from one step to the next
-    // scales: a wave loads those of rows row_s ... of one operand, at sp those of row 0 and the segment's next two steps
-    const bool s_is_a = wave < 2;
-    const int row_s = (wave & 1) * SH::S_ROWS, ext_s = (s_is_a ? m_ext : n_ext) - 1;
-    nt_gptr sp = nullptr;
-    unsigned s_pitch = 0, soff[2];
+    // scales: this wave's units, at sp those of row 0 of the unit's operand and the segment's next two steps
+    const bool s_is_a[2] = {wave < SH::S_A, wave + 4 < SH::S_A};
+    const int s_row[2] = {64 * (s_is_a[0] ? wave : wave - SH::S_A), 64 * (s_is_a[1] ? wave + 4 : wave + 4 - SH::S_A)};
+    const int s_ext[2] = {(s_is_a[0] ? m_ext : n_ext) - 1, (s_is_a[1] ? m_ext : n_ext) - 1};
+    nt_gptr sp[2] = {nullptr, nullptr};
+    unsigned s_pitch[2] = {0, 0}, soff[2] = {0, 0};
     bool s_wide = false;                                      // 16 bytes of a row at a time
     auto enter = [&](const NtSeg &s, int skip) {
       chunks = s.chunks - 2 * skip;
@@ -172,11 +174,14 @@ struct NtTile {
 #pragma unroll
       for (int x = 0; x < LB; ++x) boff[x] = (unsigned)min(32 * x + row8, n_ext - 1) * s.b_pitch + slot * 16;
       if constexpr (SH::SCALED) {
-        s_pitch = s_is_a ? s.a_scale_pitch : s.b_scale_pitch;
-        sp = nt_uniform((s_is_a ? s.a_scale : s.b_scale) + (int64_t)(s_is_a ? m_off : n_off) * s_pitch + (int64_t)skip * 8);
-        s_wide = (((unsigned)(uintptr_t)sp | s_pitch) & 15) == 0;
+        s_wide = true;
 #pragma unroll
-        for (int x = 0; x < 2; ++x) soff[x] = (unsigned)min(row_s + 64 * x + lane, ext_s) * s_pitch;
+        for (int x = 0; x < SH::LS; ++x) {
+          s_pitch[x] = s_is_a[x] ? s.a_scale_pitch : s.b_scale_pitch;
+          sp[x] = nt_uniform((s_is_a[x] ? s.a_scale : s.b_scale) + (int64_t)(s_is_a[x] ? m_off : n_off) * s_pitch[x] + (int64_t)skip * 8);
+          s_wide = s_wide && (((unsigned)(uintptr_t)sp[x] | s_pitch[x]) & 15) == 0;
+          soff[x] = (unsigned)min(s_row[x] + lane, s_ext[x]) * s_pitch[x];
+        }
       }
     };
     // The step that is loaded next is half a one: the lanes of what is missing read the half that is there, and count for nothing, since
@@ -206,15 +211,21 @@ struct NtTile {
     auto load_scales = [&]() {
       if constexpr (SH::SCALED) {
         const int n = chunks < 4 ? chunks : 4;
-        const unsigned d = lane & 3, to = SH::NST * SH::STAGE + s_slot + wave * (SH::S_ROWS * SH::S_ROW);
-        if (n == 4) {
+        const unsigned d = lane & 3;
 #pragma unroll
-          for (int x = 0; x < SH::S_ROWS / 16; ++x) nt_load4(sp, (unsigned)min(row_s + 16 * x + (lane >> 2), ext_s) * s_pitch + d * 4, lds0 + to + x * 256);
-        } else {
-          for (int x = 0; x < SH::S_ROWS / 16; ++x) {
-            int v = 0;
-            if ((int)d < n) v = *(const __attribute__((address_space(1))) int *)(sp + ((unsigned)min(row_s + 16 * x + (lane >> 2), ext_s) * s_pitch + d * 4));
-            *(__attribute__((address_space(3))) int *)((nt_lptr)lds + to + x * 256 + lane * 4) = v;
+        for (int y = 0; y < SH::LS; ++y) {
+          if (wave + 4 * y >= SH::S_UNITS) break;
+          const unsigned to = SH::NST * SH::STAGE + s_slot + (wave + 4 * y) * (64 * SH::S_ROW);
+          if (n == 4) {
+#pragma unroll
+            for (int x = 0; x < 4; ++x) nt_load4(sp[y], (unsigned)min(s_row[y] + 16 * x + (lane >> 2), s_ext[y]) * s_pitch[y] + d * 4, lds0 + to + x * 256);
+          } else {
+            for (int x = 0; x < 4; ++x) {
+              int v = 0;
+              if ((int)d < n)
+                v = *(const __attribute__((address_space(1))) int *)(sp[y] + ((unsigned)min(s_row[y] + 16 * x + (lane >> 2), s_ext[y]) * s_pitch[y] + d * 4));
+              *(__attribute__((address_space(3))) int *)((nt_lptr)lds + to + x * 256 + lane * 4) = v;
+            }
           }
         }
       }
@@ -224,13 +235,14 @@ struct NtTile {
       s_at = s_slot;
       s_left = chunks > 2 ? 2 : 1;
     };
-    // Elsewhere those of the next two steps are loaded during these two, 64 rows of a wave with each.
+    // Elsewhere those of the next two steps are loaded during these two, a unit of a wave with each.
     auto load_scales_ahead = [&]() {
       if constexpr (SH::SCALED) {
         const bool second = s_left != 2;
-        const bool wanted = s_wide && chunks >= (second ? 6 : 8) && (!second || SH::S_ROWS > 64);
-        nt_load16_masked(sp, (second ? soff[1] : soff[0]) + 16, lds0 + SH::NST * SH::STAGE + s_behind() + (wave * SH::S_ROWS + (second ? 64 : 0)) * SH::S_ROW,
-                         (unsigned)__builtin_amdgcn_readfirstlane(wanted ? -1 : 0));
+        const int unit = second ? wave + 4 : wave;
+        const bool wanted = s_wide && chunks >= (second ? 6 : 8) && unit < SH::S_UNITS;
+        nt_load16_masked(SH::LS > 1 && second ? sp[1] : sp[0], (SH::LS > 1 && second ? soff[1] : soff[0]) + 16,
+                         lds0 + SH::NST * SH::STAGE + s_behind() + unit * (64 * SH::S_ROW), (unsigned)__builtin_amdgcn_readfirstlane(wanted ? -1 : 0));
       }
     };
     int seg = 0;
@@ -264,7 +276,8 @@ struct NtTile {
             s_wide = fresh = false;
           }
         } else if (SH::SCALED && fresh) {
-          sp += 16;
+#pragma unroll
+          for (int x = 0; x < 2; ++x) sp[x] += 16;
         }
         halve();
         if (SH::SCALED && fresh) {
@@ -278,8 +291,8 @@ struct NtTile {
     // quarter h of a step: 32 bytes of 32 rows, 16 in each lane.  A row's scales (8 bytes a step) are shifted once so that byte
     // 2 (h % 2) of word h / 2 is the one of the lane's codes.
     const int r = lane & 31, g = lane >> 5;
-    const nt_lptr fa = (nt_lptr)lds + wm * (SH::TM / 2) * NT_ROW + r * NT_ROW;
-    const nt_lptr fb = (nt_lptr)lds + SH::A_BYTES + wn * (SH::TN / 2) * NT_ROW + r * NT_ROW;
+    const nt_lptr fa = (nt_lptr)lds + wm * (SH::TM / SH::WM) * NT_ROW + r * NT_ROW;
+    const nt_lptr fb = (nt_lptr)lds + SH::A_BYTES + wn * (SH::TN / SH::WN) * NT_ROW + r * NT_ROW;
     const nt_lptr fs = (nt_lptr)lds + SH::NST * SH::STAGE + r * SH::S_ROW;
     const int turn = (g ^ nt_swizzle(r)) * 16;                // (slot 2 h + g, exchanged)
     struct Frag {
@@ -299,8 +312,8 @@ struct NtTile {
       if constexpr (SH::SCALED) {
         constexpr int X = decltype(xc)::value;
         const nt_lptr p = fs + at;
-        if constexpr (X < MI) f.a[X] = *(const __attribute__((address_space(3))) nt_i32x2 *)(p + (wm * (SH::TM / 2) + 32 * X) * SH::S_ROW);
-        else f.b[X - MI] = *(const __attribute__((address_space(3))) nt_i32x2 *)(p + (SH::TM + wn * (SH::TN / 2) + 32 * (X - MI)) * SH::S_ROW);
+        if constexpr (X < MI) f.a[X] = *(const __attribute__((address_space(3))) nt_i32x2 *)(p + (wm * (SH::TM / SH::WM) + 32 * X) * SH::S_ROW);
+        else f.b[X - MI] = *(const __attribute__((address_space(3))) nt_i32x2 *)(p + (64 * SH::S_A + wn * (SH::TN / SH::WN) + 32 * (X - MI)) * SH::S_ROW);
       }
     };
     auto shift = [&](Scale &f, auto xc) {
@@ -413,6 +426,8 @@ struct NtTile {
           });
           nt_for<R>([&](auto xc) {
             if constexpr (decltype(xc)::value * T / 2 / R == decltype(tc)::value) read_scale(s_next, xc, s_loaded[0]);
+          });
+          nt_for<R>([&](auto xc) {
             if constexpr (T / 2 + decltype(xc)::value * T / 2 / R == decltype(tc)::value) shift(s_next, xc);
           });
         });

@@ -6,7 +6,7 @@ namespace {
 
 using Ortho256 = NtShape<false, 256>;
 using Ortho128 = NtShape<false, 128>;            // two workgroups on a CU
-using Ortho128Deep = NtShape<false, 128, 4>;     // one, which then has three steps on their way
+using Ortho128Deep = NtShape<false, 128, 128, 4>;     // one, which then has three steps on their way
 
 template <class SH>
 void launch(const OrthoProduct &g, hipStream_t stream) {
