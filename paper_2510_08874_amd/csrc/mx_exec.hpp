@@ -166,13 +166,14 @@ MxChoice choose_mx(const dmm_plan_t *P, int cus) {
   double best_us = 0;
   for (int shape = 0; shape < MX_SHAPES; ++shape) {
     const int tm = kMxShape[shape].tm, tn = kMxShape[shape].tn;
-    if ((shape == MX_SKINNY && most > tm) || (shape == MX_32 && most > tm) || (shape == MX_64 && most > tm)) continue;
+    if ((shape == MX_SKINNY && most > 32) || (shape == MX_32 && most > tm) || (shape == MX_64 && most > tm)) continue;
     double tiles = 0;
     for (const Group &g : P->groups) tiles += (double)(((g.m1 - g.m0 + tm - 1) / tm) * ((g.n1 - g.n0 + tn - 1) / tn));
     if (tiles == 0) return best;
     if (shape == MX_SKINNY) {
-      // (every eighth pair of chunks is a wave's next; 16 rows of A are read with every 16 columns of B)
-      const double us = 2.5 + std::max(0.8 * std::ceil(steps / 8) * std::ceil(tiles / (8.0 * cus)), b_bytes / (most <= 2 ? 4.2e6 : 3.0e6));
+      // (every eighth pair of chunks is a wave's next; 16 rows of A are read with every 16 columns of B, and B again with 16 more rows)
+      const double us = 2.5 + std::max(0.8 * std::ceil(steps / 8) * std::ceil(tiles / (8.0 * cus)),
+                                       b_bytes / (most <= 2 ? 4.6e6 : 3.0e6) + (double)((most - 1) / 16) * b_bytes / 8e6);
       if (best_us == 0 || us < best_us) best_us = us, best.shape = shape, best.runs = 1;
       continue;
     }

@@ -170,9 +170,9 @@ struct NtTile {
       a = nt_uniform(s.a + (int64_t)m_off * s.a_pitch + (int64_t)skip * NT_ROW);
       b = nt_uniform(s.b + (int64_t)n_off * s.b_pitch + (int64_t)skip * NT_ROW);
 #pragma unroll
-      for (int x = 0; x < LA; ++x) aoff[x] = (unsigned)min(32 * x + row8, m_ext - 1) * s.a_pitch + slot * 16;
+      for (int x = 0; x < LA; ++x) aoff[x] = __umul24(min(32 * x + row8, m_ext - 1), s.a_pitch) + slot * 16;
 #pragma unroll
-      for (int x = 0; x < LB; ++x) boff[x] = (unsigned)min(32 * x + row8, n_ext - 1) * s.b_pitch + slot * 16;
+      for (int x = 0; x < LB; ++x) boff[x] = __umul24(min(32 * x + row8, n_ext - 1), s.b_pitch) + slot * 16;
       if constexpr (SH::SCALED) {
         s_wide = true;
 #pragma unroll
@@ -180,7 +180,7 @@ struct NtTile {
           s_pitch[x] = s_is_a[x] ? s.a_scale_pitch : s.b_scale_pitch;
           sp[x] = nt_uniform((s_is_a[x] ? s.a_scale : s.b_scale) + (int64_t)(s_is_a[x] ? m_off : n_off) * s_pitch[x] + (int64_t)skip * 8);
           s_wide = s_wide && (((unsigned)(uintptr_t)sp[x] | s_pitch[x]) & 15) == 0;
-          soff[x] = (unsigned)min(s_row[x] + lane, s_ext[x]) * s_pitch[x];
+          soff[x] = __umul24(min(s_row[x] + lane, s_ext[x]), s_pitch[x]);
         }
       }
     };
@@ -218,12 +218,12 @@ struct NtTile {
           const unsigned to = SH::NST * SH::STAGE + s_slot + (wave + 4 * y) * (64 * SH::S_ROW);
           if (n == 4) {
 #pragma unroll
-            for (int x = 0; x < 4; ++x) nt_load4(sp[y], (unsigned)min(s_row[y] + 16 * x + (lane >> 2), s_ext[y]) * s_pitch[y] + d * 4, lds0 + to + x * 256);
+            for (int x = 0; x < 4; ++x) nt_load4(sp[y], __umul24(min(s_row[y] + 16 * x + (lane >> 2), s_ext[y]), s_pitch[y]) + d * 4, lds0 + to + x * 256);
           } else {
             for (int x = 0; x < 4; ++x) {
               int v = 0;
               if ((int)d < n)
-                v = *(const __attribute__((address_space(1))) int *)(sp[y] + ((unsigned)min(s_row[y] + 16 * x + (lane >> 2), s_ext[y]) * s_pitch[y] + d * 4));
+                v = *(const __attribute__((address_space(1))) int *)(sp[y] + (__umul24(min(s_row[y] + 16 * x + (lane >> 2), s_ext[y]), s_pitch[y]) + d * 4));
               *(__attribute__((address_space(3))) int *)((nt_lptr)lds + to + x * 256 + lane * 4) = v;
             }
           }
