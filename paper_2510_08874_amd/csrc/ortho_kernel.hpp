@@ -1,7 +1,7 @@
 // Newton-Schulz steps that bring the singular values of a matrix near 1 (gfx950, device code only):
 //   X_0 = G / |G|,   S = X X^T,   X <- (a I + b S + c S S) X
-// with X the matrix or its transpose, whichever has fewer rows.  (a X is part of the last product: its own pass over X would
-// read as many bytes again as half of what that product writes.)
+// with X the matrix or its transpose, whichever has fewer rows.  (A result in bf16 has a X as part of the last product: the
+// epilogue that adds it otherwise reads as many bytes again as half of what it writes.)
 //
 // Every matrix is kept as pairs of fp16, v 2^12 = high + low with low the rounded rest: 22 bits of a value, and
 // a product of two is low high + high low + high high, three matrix instructions (what is left out is 2^-22 of it).  Singular

@@ -205,3 +205,19 @@ def test_streams_and_a_captured_graph():
         Y[1].zero_()
         torch.cuda.synchronize()
     del graph
+
+
+@pytest.mark.parametrize("rows,cols", [(1021, 2043), (700, 513), (120, 90), (129, 3000)], ids=str)
+def test_fp32_results_are_as_exact_as_fp32_arithmetic(rows, cols):
+    """Strong directions nearly cancel on the way: whatever rounds at the size of the cancelling parts shows in the others.  The same
+    steps in plain fp32 round as often at that size: no more than half as much again is lost."""
+    X = random(1, rows, cols, 21, "strong")
+    got, given = run(X, whole(rows, cols))
+    want = oracle.orthogonalize(given[0])
+    Y = X[0] / X[0].double().norm().float()
+    Y = Y.t().contiguous() if rows > cols else Y
+    for a, b, c in oracle.DEFAULT:
+        S = Y @ Y.t().contiguous()
+        Y = a * Y + (b * S + c * (S @ S)) @ Y
+    Y = (Y.t() if rows > cols else Y).double().cpu().numpy()
+    assert np.linalg.norm(got[0] - want) <= 1.5 * np.linalg.norm(Y - want)
