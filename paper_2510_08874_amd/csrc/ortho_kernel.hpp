@@ -248,7 +248,7 @@ __device__ __forceinline__ OrthoPlace ortho_place(const OrthoProduct &g, int t) 
 }
 
 template <class SH>
-__global__ __launch_bounds__(NT_THREADS, SH::LDS > 80 * 1024 ? 1 : 2) void ortho_product_kernel(const OrthoProduct g) {
+__global__ __launch_bounds__(NT_THREADS, SH::LDS > 80 * 1024 ? 1 : SH::TM == 64 ? 3 : 2) void ortho_product_kernel(const OrthoProduct g) {
   extern __shared__ char lds[];
   // workgroup w runs on XCD w % 8: every XCD gets a run of the whole tiles, and of the list of all first ranges of the others, all
   // second ones, ... (it then reads a range of K of all rows)
