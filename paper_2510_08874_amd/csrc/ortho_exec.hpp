@@ -297,11 +297,11 @@ int dmm_orthogonalize(const dmm_matrix_desc *X, int32_t count, int x_dtype, cons
       return (int64_t)t.across;
     }, [&](int blocks) { ortho_norm_launch(args, blocks, stream); });
     if (rc) return rc;
-    // (a matrix' last tiles also clear what fills its rows and columns up)
+    // (a matrix' last tiles also clear what fills its rows and columns up; workgroups begin at multiples of 8)
     auto blocks64 = [&](OrthoTile &t) {
       const int w = t.col0 + t.w == args.cols ? args.row_pitch - t.col0 : t.w, h = t.row0 + t.h == args.rows ? args.col_pitch - t.row0 : t.h;
-      t.across = (w + 63) / 64;
-      return (int64_t)t.across * ((h + 63) / 64);
+      t.across = (w + (t.col0 & 7) + 63) / 64;
+      return (int64_t)t.across * ((h + (t.row0 & 7) + 63) / 64);
     };
     if ((rc = over_ortho_tiles(G, count, args, x_es, (char *const *)x_tiles, x_ld, blocks64, [&](int blocks) { ortho_split_launch(args, blocks, stream); })))
       return rc;

@@ -81,40 +81,67 @@ __device__ __forceinline__ double ortho_inverse_norm(const double *sums, int n) 
   return s > 0.0 ? 1.0 / sqrt(s) : 0.0;
 }
 
-// G / |G| as pairs, by rows and by columns: 64 x 64 elements a workgroup, turned through LDS.
+typedef _Float16 ortho_h8 __attribute__((ext_vector_type(8)));
+
+// G / |G| as pairs, by rows and by columns: 64 x 64 elements a workgroup, turned through LDS, from multiples of 8 on so that eight
+// neighbours are stored together, 16 bytes high and 16 low parts; element by element where a tile begins or ends inside of
+// them.  (Stores of two bytes took 1021 x 4090 21 us, these take 17; 50 MB.)
 __global__ __launch_bounds__(256) void ortho_split_kernel(OrthoTiles) {
   __shared__ float turn[64][65];
   const auto &args = *(const OrthoTiles *)__builtin_amdgcn_kernarg_segment_ptr();
   int block;
   const OrthoTile &T = ortho_find(args, blockIdx.x, &block);
-  const double inv = ortho_inverse_norm(args.sums + (int64_t)T.matrix * args.sums_of_launch, args.sums_of_launch) * ORTHO_SCALE;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int col0 = (block % T.across) * 64, row0 = block / T.across * 64;
+  // rows and columns of the tile; those in front of it are negative
+  const int col0 = (block % T.across) * 64 - (T.col0 & 7), row0 = block / T.across * 64 - (T.row0 & 7);
+  float v[16];
+#pragma unroll
+  for (int x = 0; x < 16; ++x)
+    v[x] = ortho_load(T.p + (int64_t)min(max(row0 + 16 * wave + x, 0), T.h - 1) * T.pitch, args.f32, min(max(col0 + lane, 0), T.w - 1));
+  const double inv = ortho_inverse_norm(args.sums + (int64_t)T.matrix * args.sums_of_launch, args.sums_of_launch) * ORTHO_SCALE;
+#pragma unroll
+  for (int x = 0; x < 16; ++x) {
+    const int row = row0 + 16 * wave + x, col = col0 + lane;
+    turn[16 * wave + x][lane] = row >= 0 && row < T.h && col >= 0 && col < T.w ? (float)((double)v[x] * inv) : 0.f;
+  }
+  __syncthreads();
   // the last tiles of a matrix also clear what fills its rows and columns up
   const int w = T.col0 + T.w == args.cols ? args.row_pitch - T.col0 : T.w;
   const int h = T.row0 + T.h == args.rows ? args.col_pitch - T.row0 : T.h;
   char *const ws = args.ws + T.matrix * args.stride;
-  char *const by_rows = ws + args.by_rows, *const by_cols = ws + args.by_cols;
-  for (int r = wave; r < 64; r += 4) {
-    const int row = row0 + r, col = col0 + lane;
-    const float v = row < T.h && col < T.w ? (float)((double)ortho_load(T.p + (int64_t)row * T.pitch, args.f32, col) * inv) : 0.f;
-    turn[r][lane] = v;
-    if (row < T.h && col < w) {
-      const OrthoPair p = ortho_split(v);
-      char *const at = by_rows + ortho_at(T.row0 + row, T.col0 + col, args.row_pitch);
-      *(_Float16 *)at = p.high;
-      *(_Float16 *)(at + 64) = p.low;
+  // elements `line`, `at` ... at + 7 of a matrix whose tile has lines 0 ... lines - 1 and elements 0 ... n - 1 of them
+  auto put = [&](char *to, int line, int lines, int line0, int at, int n, int at0, unsigned pitch, const float *f) {
+    if (line < 0 || line >= lines) return;
+    ortho_h8 high, low;
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      const OrthoPair p = ortho_split(f[x]);
+      high[x] = p.high;
+      low[x] = p.low;
     }
-  }
-  __syncthreads();
-  for (int c = wave; c < 64; c += 4) {
-    const int row = row0 + lane, col = col0 + c;
-    if (col < T.w && row < h) {
-      const OrthoPair p = ortho_split(turn[lane][c]);
-      char *const at = by_cols + ortho_at(T.col0 + col, T.row0 + row, args.col_pitch);
-      *(_Float16 *)at = p.high;
-      *(_Float16 *)(at + 64) = p.low;
+    char *const out = to + ortho_at(line0 + line, at0 + at, pitch);
+    if (at >= 0 && at + 8 <= n) {
+      *(ortho_h8 *)out = high;
+      *(ortho_h8 *)(out + 64) = low;
+      return;
     }
+#pragma unroll
+    for (int x = 0; x < 8; ++x)
+      if (at + x >= 0 && at + x < n) {
+        ((_Float16 *)out)[x] = high[x];
+        ((_Float16 *)(out + 64))[x] = low[x];
+      }
+  };
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    const int line = 32 * x + 8 * wave + (lane >> 3), at = (lane & 7) * 8;
+    float f[8];
+#pragma unroll
+    for (int y = 0; y < 8; ++y) f[y] = turn[line][at + y];
+    put(ws + args.by_rows, row0 + line, T.h, T.row0, col0 + at, w, T.col0, args.row_pitch, f);
+#pragma unroll
+    for (int y = 0; y < 8; ++y) f[y] = turn[at + y][line];
+    put(ws + args.by_cols, col0 + line, T.w, T.col0, row0 + at, h, T.row0, args.col_pitch, f);
   }
 }
 
@@ -124,18 +151,20 @@ __global__ __launch_bounds__(256) void ortho_store_kernel(OrthoTiles) {
   int block;
   const OrthoTile &T = ortho_find(args, blockIdx.x, &block);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int col = (block % T.across) * 64 + lane, row0 = block / T.across * 64;
-  const float *const y = (const float *)(args.ws + T.matrix * args.stride + args.by_rows);
+  const int col = (block % T.across) * 64 + lane, row0 = block / T.across * 64 + wave * 16;
+  const float *const y = (const float *)(args.ws + T.matrix * args.stride + args.by_rows) + T.col0 + col;
   if (col >= T.w) return;
-  for (int r = row0 + wave; r < min(row0 + 64, T.h); r += 4) {
-    const float v = y[(int64_t)(T.row0 + r) * args.cols + T.col0 + col];
-    char *const row = T.p + (int64_t)r * T.pitch;
-    if (args.f32) ((float *)row)[col] = v;
-    else ((__bf16 *)row)[col] = (__bf16)v;
+  float v[16];
+#pragma unroll
+  for (int r = 0; r < 16; ++r) v[r] = y[(int64_t)(T.row0 + min(row0 + r, T.h - 1)) * args.cols];
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    if (row0 + r >= T.h) return;
+    char *const row = T.p + (int64_t)(row0 + r) * T.pitch;
+    if (args.f32) ((float *)row)[col] = v[r];
+    else ((__bf16 *)row)[col] = (__bf16)v[r];
   }
 }
-
-typedef _Float16 ortho_h8 __attribute__((ext_vector_type(8)));
 
 // Eight neighbouring elements of a row of out: their sums to what they hold (zero outside of the matrix), stored row by
 // row; the values replace the sums.
