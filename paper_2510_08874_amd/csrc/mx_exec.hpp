@@ -7,6 +7,8 @@
 namespace dmm {
 namespace {
 
+constexpr int64_t kMxBlocks = (1 << 24) - 1;                   // workgroups of a launch: 2^32 threads are too many
+
 // Pointers and pitches of one form of a matrix, checked: rows of codes hold whole chunks of 128 elements at multiples of 16
 // bytes, rows of scales four bytes a chunk at multiples of 4.  `by_cols`: a tile's rows of codes are its columns.
 int check_mx(const Grid &G, const dmm_mx_tiles *q, bool by_cols) {
@@ -115,9 +117,9 @@ int over_tiles(const Grid &G, int es, char *const *x, const int64_t *x_ld, const
           t.blocks_across = (int32_t)((wide + cols - 1) / cols);
           n = (h + 127) / 128 * t.blocks_across;
         }
-        if (n > 0x3fffffff) return DMM_ELIMIT;
+        if (n > kMxBlocks) return DMM_ELIMIT;
         int rc;
-        if ((args.n == MX_TILES || blocks + n > 0x3fffffff) && (rc = flush())) return rc;
+        if ((args.n == MX_TILES || blocks + n > kMxBlocks) && (rc = flush())) return rc;
         t.first_block = (int32_t)blocks;
         blocks += n;
         args.tile[args.n++] = t;
@@ -170,6 +172,7 @@ MxChoice choose_mx(const dmm_plan_t *P, int cus) {
     double tiles = 0;
     for (const Group &g : P->groups) tiles += (double)(((g.m1 - g.m0 + tm - 1) / tm) * ((g.n1 - g.n0 + tn - 1) / tn));
     if (tiles == 0) return best;
+    if (tiles > (double)kMxBlocks) continue;
     if (shape == MX_SKINNY) {
       // (every eighth pair of chunks is a wave's next; 16 rows of A are read with every 16 columns of B, and B again with 16 more rows)
       const double us = 2.5 + std::max(0.8 * std::ceil(steps / 8) * std::ceil(tiles / (8.0 * cus)),
@@ -304,7 +307,7 @@ int build_mx(dmm_plan_t *P, const dmm_mx_tiles *a, const dmm_mx_tiles *b, void *
     L->n_items = 0;
     return DMM_OK;
   }
-  if (items.size() > 0x3fffffff) return DMM_ELIMIT;
+  if ((int64_t)items.size() > kMxBlocks) return DMM_ELIMIT;
   // workgroup w runs on XCD w % 8: every XCD gets a run of the list
   std::vector<MxItem> ordered(items.size());
   {
@@ -406,7 +409,9 @@ int dmm_mx_execute(dmm_plan_t *P, const dmm_mx_tiles *a, const dmm_mx_tiles *b, 
   hipStream_t stream = (hipStream_t)hip_stream;
   TraceRange whole("dmm_mx_execute");
   try {
-    if (!(P->dev && P->dev->mx.cached) && ((rc = materialize(P)) || (rc = check_chunks(P)))) return rc;
+    const bool capturing = is_capturing(stream), known = P->dev && P->dev->mx.cached;
+    if (!known && ((rc = materialize(P)) || (rc = check_chunks(P)))) return rc;
+    if (capturing && !known) return DMM_EINVAL;                // (a graph cannot wait for tables that are on their way)
     if ((rc = ensure_state(P)) || (rc = allow_mx_lds())) return rc;
     int device = 0, cus = 0;
     DMM_HIP(hipGetDevice(&device));
@@ -433,6 +438,7 @@ int dmm_mx_execute(dmm_plan_t *P, const dmm_mx_tiles *a, const dmm_mx_tiles *b, 
       if ((rc = M.table.order_behind_copy(stream))) return rc;
       if (M.layout.n_joins && (rc = P->dev->uses.order(stream))) return rc;
     } else {
+      if (capturing) return DMM_EINVAL;
       M.cached = false;
       MxLayout L;
       if ((rc = build_mx(P, a, b, c_tiles, c_ld, c_es, cus, stream, &L))) return rc;

@@ -8,6 +8,7 @@ namespace {
 
 static_assert(ORTHO_STEPS == DMM_ORTHOGONALIZE_STEPS, "coefficients travel with the launch");
 constexpr int kOrthoSums = 1024;       // workgroups that add up the squares of a matrix, about
+constexpr int64_t kOrthoBlocks = (1 << 24) - 1;   // workgroups of a launch: 2^32 threads are too many
 constexpr int kOrthoCus = 256;          // how products are cut along K, and so the workspace, does not depend on the device
 
 // How a symmetric (X X^T, S S) or plain (P X) product of m x n outputs and K steps is cut.
@@ -99,7 +100,7 @@ int ortho_layout(const Grid &G, int32_t count, OrthoLayout *L) {
   L->small = G.gr == 1 && G.gc == 1 && L->l <= ORTHO_SMALL && L->s > 0 && count > 0;
   L->total = 0;
   if (L->small || L->s == 0 || count == 0) return DMM_OK;
-  if (at > (int64_t)1 << 46 || (L->s + 127) / 128 * ((L->l + 127) / 128) > 0x3fffffff / count / 512) return DMM_ELIMIT;
+  if (at > (int64_t)1 << 46 || (L->s + 127) / 128 * ((L->l + 127) / 128) > ((int64_t)1 << 21) / count) return DMM_ELIMIT;
   at *= count;
   L->sums = kOrthoSums + L->tiles;
   L->o_sums = take(count * L->sums * 8);
@@ -159,8 +160,9 @@ int over_ortho_tiles(const Grid &G, int32_t count, OrthoTiles &args, int es, cha
         t.pitch = ld[i] * es;
         t.matrix = x;
         const int64_t n = blocks_of(t);
+        if (n > kOrthoBlocks) return DMM_ELIMIT;
         int rc;
-        if ((args.n == ORTHO_TILES || blocks + n > 0x3fffffff) && (rc = flush())) return rc;
+        if ((args.n == ORTHO_TILES || blocks + n > kOrthoBlocks) && (rc = flush())) return rc;
         t.first_block = (int32_t)blocks;
         t.pad = (int32_t)before;
         blocks += n;
@@ -251,7 +253,7 @@ int dmm_orthogonalize(const dmm_matrix_desc *X, int32_t count, int x_dtype, cons
       args.x_f32 = x_dtype == DMM_F32;
       args.y_f32 = y_dtype == DMM_F32;
       std::memcpy(args.coefficients, coefficients, (size_t)steps * 3 * sizeof(float));
-      bool even = count >= 2;
+      bool even = count >= 2 && count <= 1 << 22;
       for (int32_t i = 2; i < count && even; ++i)
         even = (const char *)x_tiles[i] - (const char *)x_tiles[i - 1] == (const char *)x_tiles[1] - (const char *)x_tiles[0] &&
                (char *)y_tiles[i] - (char *)y_tiles[i - 1] == (char *)y_tiles[1] - (char *)y_tiles[0];

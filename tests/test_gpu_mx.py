@@ -376,3 +376,155 @@ def test_other_streams_and_a_captured_graph():
         torch.cuda.synchronize()
         assert torch.equal(out, want)
     del graph
+
+
+def made(h, w, along, seed, more=0):
+    """A random matrix in 4 bits along one axis, and its values (both by the library: checked against the oracle above)."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x = (torch.randn(h, w, generator=g, device="cuda") * torch.exp2(torch.randint(-3, 4, (h, 1), generator=g, device="cuda").float())).bfloat16()
+    d, stream = whole(h, w), torch.cuda.current_stream().cuda_stream
+    form, t = Form(d, along, more), binding.tile_table([x], [w])
+    binding.dmm_mx_quantize(binding.matrix_desc(d), 1, t, **{"rows" if along == 1 else "cols": form.table()}, stream=stream)
+    binding.dmm_mx_dequantize(binding.matrix_desc(d), form.table(), along, 1, t, stream=stream)
+    return form, x
+
+
+def check_product(c, A, B, c_dtype):
+    """On the device, a band of rows at a time."""
+    B, k = B.double(), A.shape[1]
+    for r in range(0, A.shape[0], 512):
+        a = A[r:r + 512].double()
+        want, far = a @ B, k * 2.0 ** -24 * (a.abs() @ B.abs())
+        if c_dtype == "bf16":
+            far = far + 2.0 ** -8 * (want.abs() + far)
+        assert ((c[r:r + 512].double() - want).abs() <= far + 1e-300).all()
+
+
+@pytest.mark.parametrize("m,k,n", [(1, 4096, 8192), (2, 1000, 60000), (16, 16384, 512), (17, 2048, 9000), (20, 4096, 28000), (32, 640, 20000), (31, 20000, 1000),
+                                   (50, 2048, 16000), (64, 8192, 4096), (63, 700, 300), (200, 1024, 9000), (700, 512, 6000), (1500, 256, 2600),
+                                   (129, 30000, 130), (2500, 640, 5000), (4500, 384, 4600), (4096, 130, 9000)], ids=str)
+def test_products_of_every_size(m, k, n):
+    """Few rows, tiles cut along K, less and more tiles than the device holds; rows of C at any address, scales at odd places."""
+    more = (m + n) // 4 % 3
+    (a, A), (b, B) = made(m, k, 1, m + k, more), made(k, n, 2, n, more)
+    plan = binding.Plan(whole(m, k), whole(k, n), whole(m, n), 1)
+    stream = torch.cuda.current_stream().cuda_stream
+    for c_dtype, offset, ld in (("f32", 0, n), ("bf16", 0, n), ("bf16", 3, n + 5), ("f32", 1, n + 3)):
+        buf = torch.full((m * ld + offset,), 7.0, dtype=DT[c_dtype][0], device="cuda")
+        c = buf[offset:].view(m, ld)
+        plan.execute_mx(a.table(), b.table(), binding.tile_table([c], [ld]), binding.DMM_C_BF16 if c_dtype == "bf16" else 0, stream)
+        check_product(c[:, :n], A, B, c_dtype)
+        assert (c[:, n:] == 7.0).all() and (buf[:offset] == 7.0).all()
+
+
+def test_offsets_past_32_bits():
+    """18 GB of bf16, 4.6 GB of codes: the last rows and columns, and a product that reads them."""
+    h, w = 70000, 131072 + 64
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x = torch.empty(h, w, dtype=torch.bfloat16, device="cuda")
+    for r in range(0, h, 1000):
+        x[r:r + 1000].normal_(generator=g)
+    stream = torch.cuda.current_stream().cuda_stream
+    rows = Form(whole(h, w), 1)
+    binding.dmm_mx_quantize(binding.matrix_desc(whole(h, w)), 1, binding.tile_table([x], [w]), rows=rows.table(), stream=stream)
+    few = x[-130:].contiguous()
+    part = quantize(whole(130, w), few, "bf16")[1]
+    assert torch.equal(rows.codes[0][-130:], part.codes[0]) and torch.equal(rows.scales[0][-130:], part.scales[0])
+    # ... whose rows are the columns of a matrix of w x h
+    a, A = made(1, w, 1, 3)
+    c = torch.zeros(1, h, device="cuda")
+    plan = binding.Plan(whole(1, w), whole(w, h), whole(1, h), 1)
+    plan.execute_mx(a.table(), rows.table(), binding.tile_table([c], [h]), 0, stream)
+    binding.dmm_mx_dequantize(binding.matrix_desc(whole(h, w)), rows.table(), 1, 1, binding.tile_table([x], [w]), stream=stream)
+    check_product(c[:, -130:], A, x[-130:].t(), "f32")
+    check_product(c[:, :130], A, x[:130].t(), "f32")
+    # ... and along the columns of what it is now, where the values are codes' values already
+    cols = Form(whole(h, w), 2)
+    binding.dmm_mx_quantize(binding.matrix_desc(whole(h, w)), 1, binding.tile_table([x], [w]), cols=cols.table(), stream=stream)
+    few = x[:, -70:].contiguous()
+    part = quantize(whole(h, 70), few, "bf16")[2]
+    assert torch.equal(cols.codes[0][-70:], part.codes[0]) and torch.equal(cols.scales[0][-70:], part.scales[0])
+
+
+def test_one_plan_on_two_streams_and_beside_other_products():
+    """Partial sums in the plan's scratch buffer, other outputs every time, dmm_execute on the same plan between."""
+    m, k, n = 100, 9000, 70
+    (a, A), (b, B) = made(m, k, 1, 8), made(k, n, 2, 9)
+    plan = binding.Plan(whole(m, k), whole(k, n), whole(m, n), 1)
+    ta, tb = a.table(), b.table()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    torch.cuda.synchronize()
+    outs = [torch.zeros(m, n, device="cuda") for _ in range(12)]
+    full = torch.zeros(m, n, device="cuda")
+    torch.cuda.synchronize()
+    for i, out in enumerate(outs):
+        plan.execute_mx(ta, tb, binding.tile_table([out], [n]), 0, streams[i % 3].cuda_stream)
+        if i % 4 == 1:
+            plan.execute_mx(ta, tb, binding.tile_table([out], [n]), 0, streams[(i + 1) % 3].cuda_stream)
+        if i % 3 == 2:
+            plan.execute(binding.DMM_BF16, [A], [k], [B], [n], [full], [n], 0, streams[i // 3 % 3].cuda_stream)
+    torch.cuda.synchronize()
+    for out in outs:
+        assert torch.equal(out, outs[0])
+    check_product(outs[0], A, B, "f32")
+    check_product(full, A, B, "f32")
+
+
+def test_a_graph_of_a_layer_and_captures_that_are_refused():
+    """Quantisation and a product captured together: every replay works on what the input holds then.  A product whose tables
+    are not on the device yet is refused, and the capture goes on."""
+    m, k, n = 40, 700, 300
+    b, B = made(k, n, 2, 11)
+    tb = b.table()
+    x = torch.zeros(m, k, dtype=torch.bfloat16, device="cuda")
+    form, d = Form(whole(m, k), 1), binding.matrix_desc(whole(m, k))
+    out, other = torch.zeros(m, n, device="cuda"), torch.zeros(m, n, device="cuda")
+    plan = binding.Plan(whole(m, k), whole(k, n), whole(m, n), 1)
+    ta, tx, tc = form.table(), binding.tile_table([x], [k]), binding.tile_table([out], [n])
+
+    def layer(stream):
+        binding.dmm_mx_quantize(d, 1, tx, rows=ta, stream=stream)
+        plan.execute_mx(ta, tb, tc, 0, stream)
+
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side, capture_error_mode="relaxed"):
+        with pytest.raises(binding.DmmError):
+            plan.execute_mx(ta, tb, tc, 0, side.cuda_stream)
+        binding.dmm_mx_quantize(d, 1, tx, rows=ta, stream=side.cuda_stream)
+    layer(side.cuda_stream)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side, capture_error_mode="relaxed"):
+        layer(side.cuda_stream)
+        with pytest.raises(binding.DmmError):
+            plan.execute_mx(ta, tb, binding.tile_table([other], [n]), 0, side.cuda_stream)
+    for i in range(4):
+        g = torch.Generator(device="cuda").manual_seed(i)
+        x.copy_(torch.randn(m, k, generator=g, device="cuda"))
+        torch.cuda.synchronize()
+        layer(torch.cuda.current_stream().cuda_stream)
+        torch.cuda.synchronize()
+        want = out.clone()
+        out.zero_()
+        form.codes[0].zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and out.any()
+    del graph
+
+
+def test_nothing_to_multiply():
+    """No K: zeros.  No rows or columns: nothing is written."""
+    stream = torch.cuda.current_stream().cuda_stream
+    for m, k, n in ((5, 0, 7), (0, 300, 7), (5, 300, 0)):
+        a, b = Form(whole(m, k), 1), Form(whole(k, n), 2)
+        for f in a.codes + a.scales + b.codes + b.scales:
+            if f is not None:
+                f.zero_()
+        out = torch.full((m, n), 3.0, device="cuda")
+        binding.Plan(whole(m, k), whole(k, n), whole(m, n), 1).execute_mx(a.table(), b.table(), binding.tile_table([out if out.numel() else None], [n]), 0, stream)
+        torch.cuda.synchronize()
+        assert not out.any()

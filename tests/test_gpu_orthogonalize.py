@@ -207,13 +207,24 @@ def test_streams_and_a_captured_graph():
     del graph
 
 
-@pytest.mark.parametrize("rows,cols", [(1021, 2043), (700, 513), (120, 90), (129, 3000)], ids=str)
+def exact(G):
+    X = G.double()
+    X = X / torch.linalg.vector_norm(X)
+    X = X.t().contiguous() if G.shape[0] > G.shape[1] else X
+    for a, b, c in oracle.DEFAULT:
+        S = X @ X.t().contiguous()
+        X = a * X + (b * S + c * (S @ S)) @ X
+    return X.t() if G.shape[0] > G.shape[1] else X
+
+
+@pytest.mark.parametrize("rows,cols", [(1021, 2043), (700, 513), (120, 90), (129, 3000), (2048, 2048), (4200, 4300)], ids=str)
 def test_fp32_results_are_as_exact_as_fp32_arithmetic(rows, cols):
     """Strong directions nearly cancel on the way: whatever rounds at the size of the cancelling parts shows in the others.  The same
     steps in plain fp32 round as often at that size: no more than half as much again is lost."""
     X = random(1, rows, cols, 21, "strong")
-    got, given = run(X, whole(rows, cols))
-    want = oracle.orthogonalize(given[0])
+    d = workloads.desc(rows, cols, [0, rows // 3, rows], [0, 1, cols], 2, 2)
+    got, _ = run(X, d)
+    want = exact(X[0]).cpu().numpy()
     Y = X[0] / X[0].double().norm().float()
     Y = Y.t().contiguous() if rows > cols else Y
     for a, b, c in oracle.DEFAULT:
@@ -221,3 +232,28 @@ def test_fp32_results_are_as_exact_as_fp32_arithmetic(rows, cols):
         Y = a * Y + (b * S + c * (S @ S)) @ Y
     Y = (Y.t() if rows > cols else Y).double().cpu().numpy()
     assert np.linalg.norm(got[0] - want) <= 1.5 * np.linalg.norm(Y - want)
+
+
+@pytest.mark.parametrize("even", [True, False])
+def test_many_small_matrices(even):
+    """More than a launch's argument names, evenly spaced in memory and not; the same matrix twice."""
+    count, rows, cols = 301, 30, 41
+    mats = random(count, rows, cols, 17)
+    at = np.arange(count) * rows * cols if even else np.cumsum(np.random.default_rng(3).integers(rows * cols, rows * cols + 50, count))
+    buf = torch.zeros(int(at[-1]) + rows * cols, device="cuda")
+    out = torch.zeros_like(buf)
+    view = lambda b, i: b[int(at[i]):int(at[i]) + rows * cols].view(rows, cols)
+    for i, M in enumerate(mats):
+        view(buf, i).copy_(M)
+    x = [view(buf, i) for i in range(count)]
+    if not even:
+        x[7] = x[8]
+    desc = binding.matrix_desc(whole(rows, cols))
+    binding.dmm_orthogonalize(desc, count, 2, binding.tile_table(x, [cols] * count), 2, binding.tile_table([view(out, i) for i in range(count)], [cols] * count),
+                              None, 0, stream=torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    for i in (0, 1, 7, 143, 144, 145, 299, 300):
+        G = x[i].double().cpu().numpy()
+        assert np.linalg.norm(view(out, i).double().cpu().numpy() - oracle.orthogonalize(G)) <= oracle.limit(G)
+    if not even:
+        assert torch.equal(view(out, 7), view(out, 8))
