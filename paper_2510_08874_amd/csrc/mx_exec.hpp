@@ -271,6 +271,7 @@ int build_mx(dmm_plan_t *P, const dmm_mx_tiles *a, const dmm_mx_tiles *b, void *
             it.n_off = (int32_t)(c * tn);
             it.m_ext = (int32_t)std::min<int64_t>(tm, g.m1 - g.m0 - r * tm);
             it.n_ext = (int32_t)std::min<int64_t>(tn, g.n1 - g.n0 - c * tn);
+            it.front = seg < group_seg[x + 1] ? segs[(size_t)seg] : NtSeg{};
             it.seg = seg;
             it.n_segs = group_seg[x + 1] - seg;
             it.first = first;

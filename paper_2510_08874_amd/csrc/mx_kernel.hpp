@@ -52,7 +52,7 @@ __global__ __launch_bounds__(NT_THREADS, SH::LDS > 80 * 1024 ? 1 : 2) void mx_ge
   extern __shared__ char lds[];
   const MxItem it = items[blockIdx.x];
   NtTile<SH> tile;
-  tile.run(segs + it.seg, it.n_segs, it.first, it.steps, it.m_off, it.m_ext, it.n_off, it.n_ext, lds);
+  tile.run(it.front, segs + it.seg, it.n_segs, it.first, it.steps, it.m_off, it.m_ext, it.n_off, it.n_ext, lds);
   tile.pin();
   // fp32: half a wave writes 32 neighbouring columns of a row
   if (it.c_es == 4) {
@@ -122,7 +122,7 @@ __global__ __launch_bounds__(NT_THREADS) void mx_skinny_kernel(const MxItem *__r
   nt_f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   int todo = it.steps, skip = it.first;
   for (int sg = 0; todo > 0; ++sg) {
-    const NtSeg s = segs[it.seg + sg];
+    const NtSeg s = sg ? segs[it.seg + sg] : it.front;
     const int n = min(s.chunks - 2 * skip, 2 * todo);
     const int64_t row_a = it.m_off + min(r, it.m_ext - 1), row_b = it.n_off + min(r, it.n_ext - 1);
     const char *const pa = s.a + row_a * s.a_pitch + (int64_t)skip * NT_ROW + g * 16, *const sa = s.a_scale + row_a * s.a_scale_pitch + (int64_t)skip * 8;

@@ -18,6 +18,7 @@ struct NtSeg {
 
 // A macro-tile of a product, or a run of its K whose partial sums go to a slot of scratch memory.
 struct MxItem {
+  NtSeg front;                  // segment `seg`, so that the first loads wait for one read of a table and not for two
   char *c;                      // its corner
   int64_t ldc;                  // elements
   int32_t m_off, n_off;         // first row and column inside the output sub-tile that the segments are given for

@@ -93,7 +93,7 @@ struct NtShape {
   static constexpr int LDS = NST * STAGE + SLOTS * S_SLOT;
   static constexpr int LA = TM / 32, LB = TN / 32;           // 1 KB loads of a wave and step, 8 rows each
   static constexpr int LOADS = LA + LB;
-  static constexpr int EARLY = SCALED ? LOADS / 2 : LOADS;   // so many behind the barrier, the others in the next step's first quarter
+  static constexpr int EARLY = LOADS / 2;                    // so many in the third quarter of a step, the others in the last
   static constexpr int LS = (S_UNITS + 3) / 4;               // units of a wave: one with the first of two steps, one with the second
   static_assert(TM % (32 * WM) == 0 && TN % (32 * WN) == 0 && TN % 64 == 0 && LS <= 2, "whole matrix tiles and units of scales");
   static_assert(NST >= 2 && (NST - 1) * LOADS < 64 && LDS <= 160 * 1024, "the counter of loads, the LDS of a CU");
@@ -136,10 +136,10 @@ struct NtTile {
     });
   }
 
-  // `segs`: n_segs from the one that holds the first step (anything that has an NtSeg at an index); `first`: the first
-  // step in it; `steps`: in all.  A segment of an odd number of chunks ends with half a step.
-  template <class Segs>
-  __device__ __forceinline__ void run(const Segs &segs, int n_segs, int first, int steps, int m_off, int m_ext, int n_off, int n_ext, char *lds) {
+  // `front`: the segment that holds the first step, step `first` of it; `segs`: n_segs from that one on (read from the second
+  // on); `steps`: in all.  A segment of an odd number of chunks ends with half a step.
+  __device__ __forceinline__ void run(const NtSeg &front, const NtSeg *segs, int n_segs, int first, int steps, int m_off, int m_ext, int n_off, int n_ext,
+                                      char *lds) {
     constexpr int MI = SH::MI, NI = SH::NI, LA = SH::LA, LB = SH::LB;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -216,7 +216,9 @@ struct NtTile {
         for (int y = 0; y < SH::LS; ++y) {
           if (wave + 4 * y >= SH::S_UNITS) break;
           const unsigned to = SH::NST * SH::STAGE + s_slot + (wave + 4 * y) * (64 * SH::S_ROW);
-          if (n == 4) {
+          if (n == 4 && s_wide) {
+            nt_load16(sp[y], soff[y], lds0 + to);
+          } else if (n == 4) {
 #pragma unroll
             for (int x = 0; x < 4; ++x) nt_load4(sp[y], __umul24(min(s_row[y] + 16 * x + (lane >> 2), s_ext[y]), s_pitch[y]) + d * 4, lds0 + to + x * 256);
           } else {
@@ -246,45 +248,61 @@ struct NtTile {
       }
     };
     int seg = 0;
-    enter(segs[0], first);
+    enter(front, first);
     halve();
     new_slot();
     load_scales();
-    // to the next step to load.  Past the last one its operands are loaded again, to be read by nobody.
-    auto next = [&]() {
-      a += on;
-      b += on;
-      chunks -= 2;
+    // To the next step to load, in two parts: what every step needs, which runs between matrix instructions, and the rest, seldom.
+    // Past the last step its operands are loaded again, to be read by nobody.
+    bool fresh = false;                                       // the next step's scales are the first of a slot
+    auto next_scales = [&]() {
       if constexpr (SH::SCALED) {
 #pragma unroll
         for (int x = 0; x + 1 < SH::NST - 1; ++x) s_loaded[x] = s_loaded[x + 1];
         s_loaded[SH::NST - 2] = s_at;
-        s_at += 8;
-        --s_left;
+        fresh = --s_left == 0;
+        s_slot = fresh ? s_behind() : s_slot;
+        s_at = fresh ? s_slot : s_at + 8;
+        s_left = fresh ? 2 : s_left;
+#pragma unroll
+        for (int x = 0; x < SH::LS; ++x) sp[x] += fresh ? 16 : 0;
       }
-      if (chunks <= 2 || (SH::SCALED && s_left == 0)) {
-        bool fresh = s_left == 0, front = false;
+    };
+    auto next_operands = [&]() {
+      a += on;
+      b += on;
+      chunks -= 2;
+    };
+    auto next_rest = [&]() {
+      if (chunks <= 2 || (SH::SCALED && fresh && (!s_wide || chunks < 4))) {
         if (chunks <= 0) {
           if (++seg < n_segs) {
             enter(segs[seg], 0);
-            fresh = front = true;
+            halve();
+            if (!fresh) s_slot = s_behind();
+            s_at = s_slot;
+            s_left = chunks > 2 ? 2 : 1;
+            load_scales();
           } else {
             a -= on;
             b -= on;
             on = 0;
             chunks = s_left = 1 << 30;
-            s_wide = fresh = false;
+            s_wide = false;
           }
-        } else if (SH::SCALED && fresh) {
-#pragma unroll
-          for (int x = 0; x < 2; ++x) sp[x] += 16;
-        }
-        halve();
-        if (SH::SCALED && fresh) {
-          new_slot();
-          if (front || !s_wide || chunks < 4) load_scales();
+        } else {
+          halve();
+          if (SH::SCALED && fresh) {
+            s_left = chunks > 2 ? 2 : 1;
+            load_scales();
+          }
         }
       }
+    };
+    auto next = [&]() {
+      next_scales();
+      next_operands();
+      next_rest();
     };
 
     // ---- fragments ---------------------------------------------------------------------------
@@ -298,8 +316,8 @@ struct NtTile {
     struct Frag {
       nt_i32x4 a[MI], b[NI];
     };
-    struct Scale {
-      nt_i32x2 a[SH::SCALED ? MI : 1], b[SH::SCALED ? NI : 1];
+    struct Scale {                                            // [word of a row's eight bytes][rows of A, columns of B]
+      int v[2][SH::SCALED ? MI + NI : 1];
     };
     // fragment x of a quarter: the rows of A, the columns of B
     auto read = [&](Frag &f, auto xc, unsigned stage, auto hc) {
@@ -308,28 +326,23 @@ struct NtTile {
       if constexpr (X < MI) f.a[X] = *(const __attribute__((address_space(3))) nt_i32x4 *)(fa + o + X * 32 * NT_ROW);
       else f.b[X - MI] = *(const __attribute__((address_space(3))) nt_i32x4 *)(fb + o + (X - MI) * 32 * NT_ROW);
     };
-    auto read_scale = [&](Scale &f, auto xc, unsigned at) {
+    auto read_scale = [&](Scale &f, auto xc, auto wc, unsigned at) {
       if constexpr (SH::SCALED) {
-        constexpr int X = decltype(xc)::value;
+        constexpr int X = decltype(xc)::value, W = decltype(wc)::value;
         const nt_lptr p = fs + at;
-        if constexpr (X < MI) f.a[X] = *(const __attribute__((address_space(3))) nt_i32x2 *)(p + (wm * (SH::TM / SH::WM) + 32 * X) * SH::S_ROW);
-        else f.b[X - MI] = *(const __attribute__((address_space(3))) nt_i32x2 *)(p + (64 * SH::S_A + wn * (SH::TN / SH::WN) + 32 * (X - MI)) * SH::S_ROW);
+        if constexpr (X < MI) f.v[W][X] = *(const __attribute__((address_space(3))) int *)(p + (wm * (SH::TM / SH::WM) + 32 * X) * SH::S_ROW + 4 * W);
+        else f.v[W][X] = *(const __attribute__((address_space(3))) int *)(p + (64 * SH::S_A + wn * (SH::TN / SH::WN) + 32 * (X - MI)) * SH::S_ROW + 4 * W);
       }
     };
-    auto shift = [&](Scale &f, auto xc) {
-      if constexpr (SH::SCALED) {
-        constexpr int X = decltype(xc)::value;
-        nt_i32x2 &v = X < MI ? f.a[X < MI ? X : 0] : f.b[X < MI ? 0 : X - MI];
-        v[0] = (int)((unsigned)v[0] >> (8 * g));
-        v[1] = (int)((unsigned)v[1] >> (8 * g));
-      }
+    auto shift = [&](Scale &f, auto xc, auto wc) {
+      if constexpr (SH::SCALED) f.v[decltype(wc)::value][decltype(xc)::value] = (int)((unsigned)f.v[decltype(wc)::value][decltype(xc)::value] >> (8 * g));
     };
     auto multiply = [&](const Frag &f, const Scale &s, auto tc, auto hc) {
       if constexpr (SH::SCALED) {
         constexpr int H = decltype(hc)::value, I = decltype(tc)::value / NI, J = decltype(tc)::value % NI;
         const nt_i32x8 x = {f.a[I][0], f.a[I][1], f.a[I][2], f.a[I][3], 0, 0, 0, 0};
         const nt_i32x8 y = {f.b[J][0], f.b[J][1], f.b[J][2], f.b[J][3], 0, 0, 0, 0};
-        acc[I][J] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, acc[I][J], 4, 4, 2 * (H & 1), s.a[I][H >> 1], 2 * (H & 1), s.b[J][H >> 1]);
+        acc[I][J] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, acc[I][J], 4, 4, 2 * (H & 1), s.v[H >> 1][I], 2 * (H & 1), s.v[H >> 1][MI + J]);
       }
     };
     // of pairs: a's part times b's (0: high, 1: low)
@@ -346,16 +359,18 @@ struct NtTile {
     constexpr int T = MI * NI, R = MI + NI;
     // The order of the statements is the order of the instructions: what else a quarter needs (its `also`, by matrix instruction)
     // is spread over its matrix instructions, which take the pipe 32 cycles each.
-    auto quarter = [&](const Frag &f, const Scale &s, auto hc, Frag &into, unsigned stage, auto also) {
-      constexpr int H = decltype(hc)::value;
+    auto quarter = [&](const Frag &f, const Scale &s, auto hc, auto also) {
       nt_for<T>([&](auto tc) {
-        constexpr int I = decltype(tc)::value;
         multiply(f, s, tc, hc);
-        nt_for<R>([&](auto xc) {
-          if constexpr (decltype(xc)::value * T / R == I) read(into, xc, stage, std::integral_constant<int, (H + 1) % 4>{});
-        });
         also(tc);
         __builtin_amdgcn_sched_barrier(0);
+      });
+    };
+    // calls f with those of 0 ... N - 1 that belong to matrix instruction `tc` of T
+    auto spread = [&](auto nc, auto tc, auto f) {
+      constexpr int N = decltype(nc)::value;
+      nt_for<N>([&](auto xc) {
+        if constexpr (decltype(xc)::value * T / N == decltype(tc)::value) f(xc);
       });
     };
     // Half h of a step of pairs (values 16 h ...): the small products first.  Reads half 1 - h of `stage` into `into`.
@@ -381,63 +396,76 @@ struct NtTile {
     auto nothing = [](auto) {};
 
     // ---- the steps ---------------------------------------------------------------------------
-    // in front: all stages but half of one under way, the first fragments of step 0 read
+    // in front: all stages under way, the first fragments of step 0 read
     unsigned s_first = 0;
 #pragma unroll
-    for (int x = 0; x < SH::NST - 1; ++x) {
+    for (int x = 0; x < SH::NST; ++x) {
       nt_for<SH::LOADS>([&](auto xc) { load(xc, lds0 + x * SH::STAGE); });
       load_scales_ahead();
       next();
       if (x == 0) s_first = s_loaded[SH::NST - 2];
     }
-    nt_for<SH::EARLY>([&](auto xc) { load(xc, lds0 + (SH::NST - 1) * SH::STAGE); });
-    nt_wait_loads<(SH::NST - 2) * SH::LOADS + SH::EARLY>();   // (and the step's scales, older or behind a wait of their own)
+    nt_wait_loads<(SH::NST - 1) * SH::LOADS>();               // (and the step's scales, older or behind a wait of their own)
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    unsigned now = 0, before = (SH::NST - 1) * SH::STAGE;     // stages of the current step and of the one before it
+    unsigned now = 0;                                         // stage of the current step
     if constexpr (SH::SCALED) {
-      Frag f0, f1;
-      Scale s, s_next;
-      nt_for<R>([&](auto xc) { read_scale(s, xc, s_first); });
-      nt_for<R>([&](auto xc) { shift(s, xc); });
+      constexpr int R2 = R / 2;
+      Frag f0, f1, f2, f3;
+      Scale s;
+      nt_for<R>([&](auto xc) { read_scale(s, xc, h0, s_first); });
+      nt_for<R>([&](auto xc) { shift(s, xc, h0); });
       nt_for<R>([&](auto xc) { read(f0, xc, 0, h0); });
+      unsigned s_now = s_first;
 #pragma clang loop unroll(disable)
       for (int t = steps; t > 0; --t) {
         const unsigned behind = now == (SH::NST - 1) * SH::STAGE ? 0 : now + SH::STAGE;
-        quarter(f0, s, h0, f1, now, [&](auto tc) {            // ... and the rest of the loads that the step before began
-          nt_for<SH::LOADS>([&](auto xc) {
-            constexpr int X = decltype(xc)::value - SH::EARLY;
-            if constexpr (X >= 0 && X * T / (SH::LOADS - SH::EARLY) == decltype(tc)::value) load(xc, lds0 + before);
+        // All of this step's fragments are read in three quarters: its stage may be filled a quarter before the next one
+        // has to have landed.  A scale's word is read where its last use is behind.
+        quarter(f0, s, h0, [&](auto tc) {
+          spread(std::integral_constant<int, R + R2>{}, tc, [&](auto xc) {
+            constexpr int X = decltype(xc)::value;
+            if constexpr (X < R) read(f1, xc, now, h1);
+            else read(f2, std::integral_constant<int, X - R>{}, now, h2);
           });
-          if constexpr (decltype(tc)::value == T - 1) load_scales_ahead();
+          spread(std::integral_constant<int, R>{}, tc, [&](auto xc) { read_scale(s, xc, h1, s_now); });
         });
-        pin();
-        next();
-        quarter(f1, s, h1, f0, now, nothing);
-        quarter(f0, s, h2, f1, now, nothing);
-        nt_wait_loads<(SH::NST - 2) * SH::LOADS>();           // the next step has landed,
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");    // and this one's last fragments are read
+        quarter(f1, s, h1, [&](auto tc) {
+          spread(std::integral_constant<int, 2 * R - R2>{}, tc, [&](auto xc) {
+            constexpr int X = decltype(xc)::value + R2;
+            if constexpr (X < R) read(f2, std::integral_constant<int, X>{}, now, h2);
+            else read(f3, std::integral_constant<int, X - R>{}, now, h3);
+          });
+          spread(std::integral_constant<int, R>{}, tc, [&](auto xc) { shift(s, xc, h1); });
+        });
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");    // every wave has read them
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        quarter(f1, s, h3, f0, behind, [&](auto tc) {         // ... and half of the loads of the step that gets this one's stage
-          nt_for<SH::EARLY>([&](auto xc) {
-            if constexpr (decltype(xc)::value * T / SH::EARLY == decltype(tc)::value) load(xc, lds0 + now);
-          });
-          nt_for<R>([&](auto xc) {
-            if constexpr (decltype(xc)::value * T / 2 / R == decltype(tc)::value) read_scale(s_next, xc, s_loaded[0]);
-          });
-          nt_for<R>([&](auto xc) {
-            if constexpr (T / 2 + decltype(xc)::value * T / 2 / R == decltype(tc)::value) shift(s_next, xc);
-          });
+        quarter(f2, s, h2, [&](auto tc) {
+          spread(std::integral_constant<int, SH::EARLY>{}, tc, [&](auto xc) { load(xc, lds0 + now); });
         });
-        before = now;
+        nt_wait_loads<(SH::NST - 2) * SH::LOADS + SH::EARLY>();   // the next step has landed
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        s_now = s_loaded[0];
+        quarter(f3, s, h3, [&](auto tc) {
+          spread(std::integral_constant<int, SH::LOADS - SH::EARLY>{}, tc, [&](auto xc) { load(std::integral_constant<int, decltype(xc)::value + SH::EARLY>{}, lds0 + now); });
+          spread(std::integral_constant<int, R>{}, tc, [&](auto xc) { read(f0, xc, behind, h0); });
+          nt_for<R>([&](auto xc) {
+            if constexpr (decltype(xc)::value * T / 2 / R == decltype(tc)::value) read_scale(s, xc, h0, s_now);
+            if constexpr (T / 2 + decltype(xc)::value * T / 2 / R == decltype(tc)::value) shift(s, xc, h0);
+          });
+          if constexpr (decltype(tc)::value == 0) load_scales_ahead();
+          if constexpr (decltype(tc)::value == T / 2) next_scales();
+          if constexpr (decltype(tc)::value == T - 1) next_operands();
+        });
+        pin();
+        next_rest();
         now = behind;
-        s = s_next;
       }
     } else {
       Pair f0, f1;
-      next();
       nt_for<R>([&](auto xc) {
         read(f0.part[1], xc, 0, h2);
         read(f0.part[0], xc, 0, h0);

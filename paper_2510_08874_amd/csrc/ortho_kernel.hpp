@@ -287,15 +287,11 @@ __global__ __launch_bounds__(NT_THREADS, SH::LDS > 80 * 1024 ? 1 : SH::TM == 64 
   const int run = cut ? in_list / rest : 0, piece = in_list - run * rest;
   const OrthoPlace at = ortho_place(g, cut ? g.whole + piece : in_list);
   char *const ws = g.ws + at.matrix * g.stride;
-  struct Seg {
-    NtSeg s;
-    __device__ __forceinline__ NtSeg operator[](int) const { return s; }
-  };
   const int begin = run * g.per, end = cut ? min(begin + g.per, g.steps) : g.steps;
   const int m0 = at.row * SH::TM, n0 = at.col * SH::TN;
   NtTile<SH> tile;
-  const Seg seg = {{ws + g.a, ws + g.b, nullptr, nullptr, g.k_pitch_a, g.k_pitch_b, 0, 0, 2 * g.steps, 0}};
-  tile.run(seg, 1, begin, end - begin, m0, min(SH::TM, g.m - m0), n0, min(SH::TN, g.n - n0), lds);
+  const NtSeg seg = {ws + g.a, ws + g.b, nullptr, nullptr, g.k_pitch_a, g.k_pitch_b, 0, 0, 2 * g.steps, 0};
+  tile.run(seg, nullptr, 1, begin, end - begin, m0, min(SH::TM, g.m - m0), n0, min(SH::TN, g.n - n0), lds);
   tile.pin();
   const bool mirror = g.turned >= 0 && !(g.symmetric && at.row == at.col);
   if (cut) {

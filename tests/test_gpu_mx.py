@@ -528,3 +528,18 @@ def test_nothing_to_multiply():
         binding.Plan(whole(m, k), whole(k, n), whole(m, n), 1).execute_mx(a.table(), b.table(), binding.tile_table([out if out.numel() else None], [n]), 0, stream)
         torch.cuda.synchronize()
         assert not out.any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_large_matrices_equal_their_parts(dtype):
+    h, w = 9001, 8200
+    x = torch.randn(h, w, generator=torch.Generator(device="cuda").manual_seed(31), device="cuda").to(DT[dtype][0])
+    stream, out = torch.cuda.current_stream().cuda_stream, torch.zeros(h, w, dtype=DT[dtype][0], device="cuda")
+    form = quantize(whole(h, w), x, dtype, forms=(1,))[1]
+    binding.dmm_mx_dequantize(binding.matrix_desc(whole(h, w)), form.table(), 1, DT[dtype][1], binding.tile_table([out], [w]), stream)
+    for r in (0, 4000, h - 60):
+        part = x[r:r + 60].contiguous()
+        one = quantize(whole(len(part), w), part, dtype, forms=(1,))[1]
+        assert torch.equal(form.codes[0][r:r + 60], one.codes[0]) and torch.equal(form.scales[0][r:r + 60], one.scales[0])
+        want = oracle.values(oracle.unpack(one.codes[0].cpu().numpy()), one.scales[0].cpu().numpy(), w)
+        assert np.array_equal(out[r:r + 60].double().cpu().numpy(), want)
