@@ -63,7 +63,7 @@ __global__ __launch_bounds__(NT_THREADS, SH::LDS > 80 * 1024 ? 1 : 2) void mx_ge
     mx_store<SH, unsigned short>(tile, it);
     return;
   }
-  // bf16: through LDS, so that a thread stores 16 bytes of a row (16384 x 8192 x 28672: 2.54 -> 2.42 ms)
+  // bf16: through LDS, so that a thread stores 16 bytes of a row (16384 x 8192 x 28672: 2.54 -> 2.42 ms; with stores that the caches keep 2 % slower)
   if constexpr (SH::WM == 2) {
     tile.slices(lds, [&](const float *values, int base) {
       constexpr int PER = SH::TN / 8;

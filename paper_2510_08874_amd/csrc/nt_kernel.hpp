@@ -7,15 +7,21 @@
 //          three products (low high, high low, high high) use what is in LDS three times for two reads
 //
 // What bounds a 256 x 256 tile: a step of 128 bytes a row is 64 (pairs: 96) matrix instructions of 32 cycles on each of the four
-// matrix pipes (2048 or 3072 cycles), 128 KB of LDS reads (1024 cycles at 128 bytes), 64 KB written to LDS by the loads (512) and 64
-// KB from L2.  L2 answers requests of up to 128 bytes, 16 of them a cycle to the 32 CUs of an XCD: 512 rows
-// of 128 bytes take 1024 cycles, so the rows of a step are whole lines.  (With steps of 64 bytes, and four bytes of scales a row
+// matrix pipes (2048 or 3072 cycles), 128 KB of LDS reads (1024 cycles at 128 bytes), and 64 KB that loads bring into LDS, which take
+// 1950 cycles by themselves (33 bytes a cycle and CU with all CUs at it; 17 TB/s from L2).  L2 answers requests of up to 128
+// bytes, so the rows of a step are whole lines.  (With steps of 64 bytes, and four bytes of scales a row
 // and step, there were four times as many requests: 16384 x 8192 x 28672 in 4 bits 2.42 ms, matrix pipes busy 35 %.)
-// The pipes can be kept busy if nothing waits: operands go straight into LDS stages, and the fragments of a
-// quarter of a step are read during the quarter before it, between its matrix instructions.  One barrier a step, in front of its last
-// quarter (pairs: half): behind it the next stage may be read, and the stage whose last fragments every wave holds may be filled.
+// So matrix instructions, LDS reads and loads have to run side by side all the time, from one wave on each SIMD, which issues an
+// instruction every four to five cycles: operands go straight into LDS stages, and every load, read and addition has its place between two matrix
+// instructions.  fp4: all fragments of a step are read in its first half and the quarter before; behind a barrier its stage is filled
+// again in the second half, a quarter before another barrier waits for the step behind it, so that loads of two steps overlap.  Pairs,
+// with half as much to load a cycle: fragments of a half are read during the half before it, one barrier a step.
+// fp4, 4096 x 4096 x 4096: 2660 cycles a step where one barrier in front of the last quarter, and 414 instructions a step instead
+// of 262, took 2900; matrix instructions and LDS reads alone take 2640, matrix instructions alone 2150.  A tile's ends come on top: 3 us
+// until the first step has landed, and 256 KB of fp32 from every CU at the same time take 11 us.
 // The part lowers its clock under matrix load: a loop of matrix instructions on registers alone makes 6.5 PFLOP/s in fp4
-// and 1.8 in fp16 with random operands (9.7 and 2.5 with zeros), and a kernel that also moves operands has less power left for it.
+// and 1.8 in fp16 with random operands (9.7 and 2.5 with zeros), and a kernel that also moves operands has less power left for it
+// (1.7 GHz in fp4, 1.58 with pairs, whose pipes are busy 83 % of the time).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -45,17 +51,19 @@ constexpr int NT_CHUNK = 64;               // what a segment's length is given i
 // into different banks.
 __device__ __forceinline__ int nt_swizzle(int row) { return (row >> 1) & 7; }
 
+// (to byte lds + ON)
+template <int ON>
 __device__ __forceinline__ void nt_load16(nt_gptr base, unsigned lane_off, unsigned lds) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(lane_off), "s"(base), "s"(lds) : "memory");
+  asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(lane_off), "s"(base), "s"(lds), "n"(ON) : "memory", "scc");
 }
 __device__ __forceinline__ void nt_load4(nt_gptr base, unsigned lane_off, unsigned lds) {
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" : : "v"(lane_off), "s"(base), "s"(lds) : "memory");
 }
-// (mask: all lanes or none)
-__device__ __forceinline__ void nt_load16_masked(nt_gptr base, unsigned lane_off, unsigned lds, unsigned mask) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_mov_b32 exec_lo, %3\n\ts_mov_b32 exec_hi, %3\n\t"
-               "global_load_lds_dwordx4 %0, %1\n\ts_mov_b64 exec, -1"
-               : : "v"(lane_off), "s"(base), "s"(lds), "s"(mask) : "memory");
+// (16 bytes on from lane_off, which counts for LDS as well; all lanes if `on` is negative, else none)
+__device__ __forceinline__ void nt_load16_if(nt_gptr base, unsigned lane_off, unsigned lds, int on) {
+  asm volatile("s_sub_u32 m0, %2, 16\n\ts_ashr_i32 exec_lo, %3, 31\n\ts_mov_b32 exec_hi, exec_lo\n\t"
+               "global_load_lds_dwordx4 %0, %1 offset:16\n\ts_mov_b64 exec, -1"
+               : : "v"(lane_off), "s"(base), "s"(lds), "s"(on) : "memory", "scc");
 }
 template <int N>
 __device__ __forceinline__ void nt_wait_loads() {
@@ -88,8 +96,8 @@ struct NtShape {
   static constexpr int A_BYTES = TM * NT_ROW, B_BYTES = TN * NT_ROW, STAGE = A_BYTES + B_BYTES;
   // scales of two steps together, 16 bytes a row: a request fetches them once.  Units of 64 rows, A's in front of B's
   static constexpr int S_ROW = 16, S_A = (TM + 63) / 64, S_UNITS = SCALED ? S_A + TN / 64 : 0, S_SLOT = S_UNITS * 64 * S_ROW;
-  // slots: of the step whose scales are read, of those under way, and of the one behind them; every step may be a segment's last
-  static constexpr int SLOTS = NST + 1;
+  // slots: of the step that is multiplied, of those under way, and of the one behind them; every step may be a segment's last
+  static constexpr int SLOTS = NST + 2;
   static constexpr int LDS = NST * STAGE + SLOTS * S_SLOT;
   static constexpr int LA = TM / 32, LB = TN / 32;           // 1 KB loads of a wave and step, 8 rows each
   static constexpr int LOADS = LA + LB;
@@ -198,8 +206,8 @@ struct NtTile {
     // load x of a step, into the stage at byte `base` of LDS
     auto load = [&](auto xc, unsigned base) {
       constexpr int X = decltype(xc)::value;
-      if constexpr (X < LA) nt_load16(a, aoff[X], base + (4 * X + wave) * 1024);
-      else nt_load16(b, boff[X - LA], base + SH::A_BYTES + (4 * (X - LA) + wave) * 1024);
+      if constexpr (X < LA) nt_load16<X * 4096>(a, aoff[X], base + wave * 1024);
+      else nt_load16<SH::A_BYTES + (X - LA) * 4096>(b, boff[X - LA], base + wave * 1024);
     };
     // Scales of two steps at a time, in the next slot.
     int s_left = 0;                                           // steps that the slot has scales of and that are yet to be loaded
@@ -217,7 +225,7 @@ struct NtTile {
           if (wave + 4 * y >= SH::S_UNITS) break;
           const unsigned to = SH::NST * SH::STAGE + s_slot + (wave + 4 * y) * (64 * SH::S_ROW);
           if (n == 4 && s_wide) {
-            nt_load16(sp[y], soff[y], lds0 + to);
+            nt_load16<0>(sp[y], soff[y], lds0 + to);
           } else if (n == 4) {
 #pragma unroll
             for (int x = 0; x < 4; ++x) nt_load4(sp[y], __umul24(min(s_row[y] + 16 * x + (lane >> 2), s_ext[y]), s_pitch[y]) + d * 4, lds0 + to + x * 256);
@@ -237,14 +245,19 @@ struct NtTile {
       s_at = s_slot;
       s_left = chunks > 2 ? 2 : 1;
     };
-    // Elsewhere those of the next two steps are loaded during these two, a unit of a wave with each.
+    // Elsewhere those of the next two steps are loaded during these two, a unit of a wave with each.  s_rest: chunks behind the steps
+    // of the slot, where 16 bytes of a row can be loaded at a time; little or nothing: word by word.
+    int s_rest = 0;
+    const unsigned s_mine = lds0 + SH::NST * SH::STAGE + wave * (64 * SH::S_ROW);
+    auto count_rest = [&]() { s_rest = s_wide ? chunks - 2 * s_left : 0; };
     auto load_scales_ahead = [&]() {
       if constexpr (SH::SCALED) {
-        const bool second = s_left != 2;
-        const int unit = second ? wave + 4 : wave;
-        const bool wanted = s_wide && chunks >= (second ? 6 : 8) && unit < SH::S_UNITS;
-        nt_load16_masked(SH::LS > 1 && second ? sp[1] : sp[0], (SH::LS > 1 && second ? soff[1] : soff[0]) + 16,
-                         lds0 + SH::NST * SH::STAGE + s_behind() + unit * (64 * SH::S_ROW), (unsigned)__builtin_amdgcn_readfirstlane(wanted ? -1 : 0));
+        const int left = s_left;
+        const bool second = SH::LS > 1 && left == 1;
+        int on = 3 - s_rest;
+        if constexpr (SH::S_UNITS < 4 * SH::LS) on = wave + (left == 1 ? 4 : 0) < SH::S_UNITS ? on : 0;
+        if constexpr (SH::LS == 1) on = left == 1 ? 0 : on;
+        nt_load16_if(second ? sp[1] : sp[0], second ? soff[1] : soff[0], s_mine + s_behind() + (second ? 4 * 64 * SH::S_ROW : 0), on);
       }
     };
     int seg = 0;
@@ -252,6 +265,7 @@ struct NtTile {
     halve();
     new_slot();
     load_scales();
+    count_rest();
     // To the next step to load, in two parts: what every step needs, which runs between matrix instructions, and the rest, seldom.
     // Past the last step its operands are loaded again, to be read by nobody.
     bool fresh = false;                                       // the next step's scales are the first of a slot
@@ -260,12 +274,15 @@ struct NtTile {
 #pragma unroll
         for (int x = 0; x + 1 < SH::NST - 1; ++x) s_loaded[x] = s_loaded[x + 1];
         s_loaded[SH::NST - 2] = s_at;
-        fresh = --s_left == 0;
+        int m = (s_left - 2) >> 31;                           // -1 behind the last step of a slot
+        asm("" : "+s"(m));                                    // (selects by one condition would become a branch, and all matrix instructions come behind it)
+        fresh = m != 0;
         s_slot = fresh ? s_behind() : s_slot;
         s_at = fresh ? s_slot : s_at + 8;
-        s_left = fresh ? 2 : s_left;
+        s_left += (m & 2) - 1;
+        s_rest += m & -4;
 #pragma unroll
-        for (int x = 0; x < SH::LS; ++x) sp[x] += fresh ? 16 : 0;
+        for (int x = 0; x < SH::LS; ++x) sp[x] += m & 16;
       }
     };
     auto next_operands = [&]() {
@@ -283,12 +300,13 @@ struct NtTile {
             s_at = s_slot;
             s_left = chunks > 2 ? 2 : 1;
             load_scales();
+            count_rest();
           } else {
             a -= on;
             b -= on;
             on = 0;
             chunks = s_left = 1 << 30;
-            s_wide = false;
+            s_rest = 0;
           }
         } else {
           halve();
@@ -335,7 +353,11 @@ struct NtTile {
       }
     };
     auto shift = [&](Scale &f, auto xc, auto wc) {
-      if constexpr (SH::SCALED) f.v[decltype(wc)::value][decltype(xc)::value] = (int)((unsigned)f.v[decltype(wc)::value][decltype(xc)::value] >> (8 * g));
+      if constexpr (SH::SCALED) {
+        int &v = f.v[decltype(wc)::value][decltype(xc)::value];
+        v = (int)((unsigned)v >> (8 * g));
+        asm volatile("" : "+v"(v));                           // here, not in front of its use
+      }
     };
     auto multiply = [&](const Frag &f, const Scale &s, auto tc, auto hc) {
       if constexpr (SH::SCALED) {
@@ -366,11 +388,11 @@ struct NtTile {
         __builtin_amdgcn_sched_barrier(0);
       });
     };
-    // calls f with those of 0 ... N - 1 that belong to matrix instruction `tc` of T
-    auto spread = [&](auto nc, auto tc, auto f) {
-      constexpr int N = decltype(nc)::value;
+    // calls f with those of 0 ... N - 1 that belong to matrix instruction `tc`, if they are spread over the first L of them
+    auto spread = [&](auto nc, auto lc, auto tc, auto f) {
+      constexpr int N = decltype(nc)::value, L = decltype(lc)::value;
       nt_for<N>([&](auto xc) {
-        if constexpr (decltype(xc)::value * T / N == decltype(tc)::value) f(xc);
+        if constexpr (decltype(xc)::value * L / N == decltype(tc)::value) f(xc);
       });
     };
     // Half h of a step of pairs (values 16 h ...): the small products first.  Reads half 1 - h of `stage` into `into`.
@@ -411,7 +433,12 @@ struct NtTile {
     asm volatile("" ::: "memory");
     unsigned now = 0;                                         // stage of the current step
     if constexpr (SH::SCALED) {
-      constexpr int R2 = R / 2;
+      // A wave issues an instruction every four or five cycles, so no more than six between two matrix instructions; what a barrier or
+      // the next quarter waits for is issued a few of these ahead.
+      constexpr int R2 = R * 3 / 4;
+      constexpr std::integral_constant<int, T> all;
+      constexpr std::integral_constant<int, (T * 11 + 15) / 16> most;
+      constexpr std::integral_constant<int, R> n_frags;
       Frag f0, f1, f2, f3;
       Scale s;
       nt_for<R>([&](auto xc) { read_scale(s, xc, h0, s_first); });
@@ -424,41 +451,44 @@ struct NtTile {
         // All of this step's fragments are read in three quarters: its stage may be filled a quarter before the next one
         // has to have landed.  A scale's word is read where its last use is behind.
         quarter(f0, s, h0, [&](auto tc) {
-          spread(std::integral_constant<int, R + R2>{}, tc, [&](auto xc) {
+          spread(std::integral_constant<int, R + R2>{}, all, tc, [&](auto xc) {
             constexpr int X = decltype(xc)::value;
             if constexpr (X < R) read(f1, xc, now, h1);
             else read(f2, std::integral_constant<int, X - R>{}, now, h2);
           });
-          spread(std::integral_constant<int, R>{}, tc, [&](auto xc) { read_scale(s, xc, h1, s_now); });
+          spread(n_frags, all, tc, [&](auto xc) { read_scale(s, xc, h1, s_now); });
+          if constexpr (decltype(tc)::value == T / 8) load_scales_ahead();
         });
         quarter(f1, s, h1, [&](auto tc) {
-          spread(std::integral_constant<int, 2 * R - R2>{}, tc, [&](auto xc) {
+          spread(std::integral_constant<int, 2 * R - R2>{}, most, tc, [&](auto xc) {
             constexpr int X = decltype(xc)::value + R2;
             if constexpr (X < R) read(f2, std::integral_constant<int, X>{}, now, h2);
             else read(f3, std::integral_constant<int, X - R>{}, now, h3);
           });
-          spread(std::integral_constant<int, R>{}, tc, [&](auto xc) { shift(s, xc, h1); });
+          spread(n_frags, all, tc, [&](auto xc) { shift(s, xc, h1); });
+          if constexpr (decltype(tc)::value == T * 12 / 16) {
+            s_now = s_loaded[0];                              // the next step's
+            next_scales();
+          }
         });
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");    // every wave has read them
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         quarter(f2, s, h2, [&](auto tc) {
-          spread(std::integral_constant<int, SH::EARLY>{}, tc, [&](auto xc) { load(xc, lds0 + now); });
+          spread(std::integral_constant<int, SH::EARLY>{}, all, tc, [&](auto xc) { load(xc, lds0 + now); });
         });
         nt_wait_loads<(SH::NST - 2) * SH::LOADS + SH::EARLY>();   // the next step has landed
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        s_now = s_loaded[0];
         quarter(f3, s, h3, [&](auto tc) {
-          spread(std::integral_constant<int, SH::LOADS - SH::EARLY>{}, tc, [&](auto xc) { load(std::integral_constant<int, decltype(xc)::value + SH::EARLY>{}, lds0 + now); });
-          spread(std::integral_constant<int, R>{}, tc, [&](auto xc) { read(f0, xc, behind, h0); });
+          constexpr int X = decltype(tc)::value;
+          spread(std::integral_constant<int, SH::LOADS - SH::EARLY>{}, most, tc, [&](auto xc) { load(std::integral_constant<int, decltype(xc)::value + SH::EARLY>{}, lds0 + now); });
+          spread(n_frags, most, tc, [&](auto xc) { read_scale(s, xc, h0, s_now); });
+          spread(n_frags, most, tc, [&](auto xc) { read(f0, xc, behind, h0); });
+          if constexpr (X == T * 13 / 16) next_operands();
           nt_for<R>([&](auto xc) {
-            if constexpr (decltype(xc)::value * T / 2 / R == decltype(tc)::value) read_scale(s, xc, h0, s_now);
-            if constexpr (T / 2 + decltype(xc)::value * T / 2 / R == decltype(tc)::value) shift(s, xc, h0);
+            if constexpr (T * 12 / 16 + decltype(xc)::value * (T - T * 12 / 16) / R == X) shift(s, xc, h0);
           });
-          if constexpr (decltype(tc)::value == 0) load_scales_ahead();
-          if constexpr (decltype(tc)::value == T / 2) next_scales();
-          if constexpr (decltype(tc)::value == T - 1) next_operands();
         });
         pin();
         next_rest();
