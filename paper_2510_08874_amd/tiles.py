@@ -94,6 +94,53 @@ class TileSet:
         return sum(t.numel() * t.element_size() for t in self.tensors if t is not None)
 
 
+class MxTileSet:
+    """The tiles of a matrix in 4 bits, along its rows or along its columns: codes and scales of every tile, in the
+    table order of the ABI.  ``table`` goes to ``dmm_mx_quantize``, ``dmm_mx_dequantize`` and ``Plan.execute_mx``."""
+
+    def __init__(self, desc: Dict, along: str, device="cuda"):
+        from . import binding
+        if along not in ("rows", "cols"):
+            raise ValueError(f"along: {along!r}, not 'rows' or 'cols'")
+        self.desc, self.along, self.binding = desc, along, binding
+        self.codes: List[Optional[torch.Tensor]] = []
+        self.scales: List[Optional[torch.Tensor]] = []
+        rc, cc = desc["row_cuts"], desc["col_cuts"]
+        for _ in range(desc["replication"]):
+            for r0, r1 in zip(rc, rc[1:]):
+                for c0, c1 in zip(cc, cc[1:]):
+                    n, k = (r1 - r0, c1 - c0) if along == "rows" else (c1 - c0, r1 - r0)
+                    chunks = _round_up(k, binding.DMM_MX_CHUNK) // binding.DMM_MX_CHUNK
+                    for made, size in ((self.codes, binding.DMM_MX_CHUNK // 2), (self.scales, binding.DMM_MX_CHUNK // binding.DMM_MX_BLOCK)):
+                        made.append(torch.empty((n, chunks * size), dtype=torch.uint8, device=device) if n and k else None)
+        self.table = self._table(range(len(self.codes)))
+
+    def _table(self, order):
+        def columns(made):
+            return [made[i] for i in order], [0 if made[i] is None else made[i].shape[1] for i in order]
+        order = list(order)
+        return self.binding.mx_tiles(*columns(self.codes), *columns(self.scales))
+
+    def transposed(self):
+        """The table of the transposed matrix, whose rows are this one's columns: the same buffers in another order."""
+        gr, gc = len(self.desc["row_cuts"]) - 1, len(self.desc["col_cuts"]) - 1
+        return self._table(rep * gr * gc + i * gc + j for rep in range(self.desc["replication"]) for j in range(gc) for i in range(gr))
+
+    def write_values(self, X: TileSet, stream: Optional[int] = None) -> None:
+        """The values that the codes stand for, into the tiles of ``X`` (bf16 or fp32)."""
+        b = self.binding
+        b.dmm_mx_dequantize(b.matrix_desc(self.desc), self.table, b.DMM_MX_ROWS if self.along == "rows" else b.DMM_MX_COLS,
+                            b.DMM_BF16 if X.dtype == torch.bfloat16 else b.DMM_F32, b.tile_table(X.tensors, X.ld),
+                            torch.cuda.current_stream().cuda_stream if stream is None else stream)
+
+
+def quantize(X: TileSet, rows: Optional[MxTileSet] = None, cols: Optional[MxTileSet] = None, stream: Optional[int] = None) -> None:
+    """``dmm_mx_quantize`` of the tiles of ``X`` along their rows, their columns or both, in one pass."""
+    from . import binding as b
+    b.dmm_mx_quantize(b.matrix_desc(X.desc), b.DMM_BF16 if X.dtype == torch.bfloat16 else b.DMM_F32, b.tile_table(X.tensors, X.ld),
+                      rows=rows and rows.table, cols=cols and cols.table, stream=torch.cuda.current_stream().cuda_stream if stream is None else stream)
+
+
 class DeviceProblem:
     """One partitioned product resident on the GPU: the plan, the three tile
     sets and the marshalled argument arrays of ``dmm_execute``."""

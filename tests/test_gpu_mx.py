@@ -543,3 +543,61 @@ def test_large_matrices_equal_their_parts(dtype):
         assert torch.equal(form.codes[0][r:r + 60], one.codes[0]) and torch.equal(form.scales[0][r:r + 60], one.scales[0])
         want = oracle.values(oracle.unpack(one.codes[0].cpu().numpy()), one.scales[0].cpu().numpy(), w)
         assert np.array_equal(out[r:r + 60].double().cpu().numpy(), want)
+
+
+def test_a_weight_is_trained():
+    """A layer's weight over two steps, all of it as a program would call it: forward, both gradients, the weight's gradient
+    orthogonalised and applied, everything quantised on the way.  Every part against the oracle on what it was given."""
+    from oracle import orthogonalize as ortho
+    from paper_2510_08874_amd.tiles import MxTileSet, TileSet, quantize as fill
+    m, k, n = 260, 384, 200
+    cut = lambda x: [0, 128, x]
+    desc = lambda r, c: workloads.desc(r, c, cut(r), cut(c), 2, 2)
+    dx, dw, dy = desc(m, k), desc(k, n), desc(m, n)
+    g = torch.Generator().manual_seed(77)
+    bits = lambda t: t.to(torch.bfloat16).view(torch.int16).numpy().view(np.uint16)
+    X, W, Y, DY, DX, DW, O = (TileSet(d, t) for d, t in ((dx, torch.bfloat16), (dw, torch.float32), (dy, torch.bfloat16), (dy, torch.bfloat16),
+                                                         (dx, torch.bfloat16), (dw, torch.float32), (dw, torch.float32)))
+    X.scatter(bits(torch.randn(m, k, generator=g)))
+    DY.scatter(bits(torch.randn(m, n, generator=g) * 1e-3))
+    W.scatter((torch.randn(k, n, generator=g) * k ** -0.5).numpy())
+    mx = {(t, a): MxTileSet(t.desc, a) for t in (X, W, DY) for a in ("rows", "cols")}
+    forward, to_x, to_w = binding.Plan(dx, dw, dy, 4), binding.Plan(dy, desc(n, k), dx, 4), binding.Plan(desc(k, m), dy, dw, 4)
+    matrix = binding.matrix_desc(dw)
+    size = binding.dmm_orthogonalize_workspace(matrix, 1)
+    ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+    table = lambda t: binding.tile_table(t.tensors, t.ld)
+    stream = torch.cuda.current_stream().cuda_stream
+
+    def along(x, d, axis):
+        out = np.zeros(x.shape)
+        for r0, r1, c0, c1 in bounds(d):
+            t = x[r0:r1, c0:c1].astype(np.float64)
+            codes, scales = oracle.quantize(t if axis == "rows" else t.T)
+            v = oracle.values(codes, scales, t.shape[axis == "rows"])
+            out[r0:r1, c0:c1] = v if axis == "rows" else v.T
+        return out
+
+    for _ in range(2):
+        for t in (X, W, DY):
+            fill(t, mx[t, "rows"], mx[t, "cols"])
+        forward.execute_mx(mx[X, "rows"].table, mx[W, "cols"].table, table(Y), binding.DMM_C_BF16, stream)
+        to_x.execute_mx(mx[DY, "rows"].table, mx[W, "rows"].transposed(), table(DX), binding.DMM_C_BF16, stream)
+        to_w.execute_mx(mx[X, "cols"].transposed(), mx[DY, "cols"].table, table(DW), 0, stream)
+        binding.dmm_orthogonalize(matrix, 1, binding.DMM_F32, table(DW), binding.DMM_F32, table(O), ws, size, stream=stream)
+        torch.cuda.synchronize()
+        x, w, d = (t.gather() for t in (X, W, DY))
+        for got, A, B, dtype in ((Y, along(x, dx, "rows"), along(w, dw, "cols"), "bf16"), (DX, along(d, dy, "rows"), along(w, dw, "rows").T, "bf16"),
+                                 (DW, along(x, dx, "cols").T, along(d, dy, "cols"), "f32")):
+            assert (np.abs(got.gather() - A @ B) <= limit(A, B, dtype, A.shape[1])).all()
+        G = DW.gather().astype(np.float64)
+        assert np.linalg.norm(O.gather() - ortho.orthogonalize(G)) <= ortho.limit(G)
+        # gradients against differences: Y is linear in each of its operands
+        E = np.random.default_rng(1).standard_normal((k, n))
+        A, C = along(x, dx, "cols"), along(d, dy, "cols")
+        assert abs(((A @ (E * 0.5) - A @ (E * -0.5)) * C).sum() - (G * E).sum()) <= 2.0 ** -24 * m * (np.abs(A.T) @ np.abs(C) * np.abs(E)).sum()
+        for t, o in zip(W.tensors, O.tensors):
+            t -= 0.02 * o
+    values = TileSet(dw, torch.bfloat16)
+    mx[W, "cols"].write_values(values)
+    assert np.array_equal(values.gather().astype(np.float64), along(w, dw, "cols"))
