@@ -344,18 +344,23 @@ struct NtTile {
       if constexpr (X < MI) f.a[X] = *(const __attribute__((address_space(3))) nt_i32x4 *)(fa + o + X * 32 * NT_ROW);
       else f.b[X - MI] = *(const __attribute__((address_space(3))) nt_i32x4 *)(fb + o + (X - MI) * 32 * NT_ROW);
     };
-    auto read_scale = [&](Scale &f, auto xc, auto wc, unsigned at) {
+    // both words of a row as they are (one by one they keep LDS busy for 400 cycles more a step)
+    struct RawScale {
+      nt_i32x2 v[SH::SCALED ? MI + NI : 1];
+    };
+    auto read_scale = [&](RawScale &f, auto xc, unsigned at) {
       if constexpr (SH::SCALED) {
-        constexpr int X = decltype(xc)::value, W = decltype(wc)::value;
+        constexpr int X = decltype(xc)::value;
         const nt_lptr p = fs + at;
-        if constexpr (X < MI) f.v[W][X] = *(const __attribute__((address_space(3))) int *)(p + (wm * (SH::TM / SH::WM) + 32 * X) * SH::S_ROW + 4 * W);
-        else f.v[W][X] = *(const __attribute__((address_space(3))) int *)(p + (64 * SH::S_A + wn * (SH::TN / SH::WN) + 32 * (X - MI)) * SH::S_ROW + 4 * W);
+        if constexpr (X < MI) f.v[X] = *(const __attribute__((address_space(3))) nt_i32x2 *)(p + (wm * (SH::TM / SH::WM) + 32 * X) * SH::S_ROW);
+        else f.v[X] = *(const __attribute__((address_space(3))) nt_i32x2 *)(p + (64 * SH::S_A + wn * (SH::TN / SH::WN) + 32 * (X - MI)) * SH::S_ROW);
       }
     };
-    auto shift = [&](Scale &f, auto xc, auto wc) {
+    // word W for the lane's half
+    auto shift = [&](Scale &f, const RawScale &raw, auto xc, auto wc) {
       if constexpr (SH::SCALED) {
         int &v = f.v[decltype(wc)::value][decltype(xc)::value];
-        v = (int)((unsigned)v >> (8 * g));
+        v = (int)((unsigned)raw.v[decltype(xc)::value][decltype(wc)::value] >> (8 * g));
         asm volatile("" : "+v"(v));                           // here, not in front of its use
       }
     };
@@ -441,22 +446,23 @@ struct NtTile {
       constexpr std::integral_constant<int, R> n_frags;
       Frag f0, f1, f2, f3;
       Scale s;
-      nt_for<R>([&](auto xc) { read_scale(s, xc, h0, s_first); });
-      nt_for<R>([&](auto xc) { shift(s, xc, h0); });
+      RawScale raw;
+      nt_for<R>([&](auto xc) { read_scale(raw, xc, s_first); });
+      nt_for<R>([&](auto xc) { shift(s, raw, xc, h0); });
       nt_for<R>([&](auto xc) { read(f0, xc, 0, h0); });
-      unsigned s_now = s_first;
 #pragma clang loop unroll(disable)
       for (int t = steps; t > 0; --t) {
         const unsigned behind = now == (SH::NST - 1) * SH::STAGE ? 0 : now + SH::STAGE;
+        unsigned s_next = 0;
         // All of this step's fragments are read in three quarters: its stage may be filled a quarter before the next one
-        // has to have landed.  A scale's word is read where its last use is behind.
+        // has to have landed.
         quarter(f0, s, h0, [&](auto tc) {
           spread(std::integral_constant<int, R + R2>{}, all, tc, [&](auto xc) {
             constexpr int X = decltype(xc)::value;
             if constexpr (X < R) read(f1, xc, now, h1);
             else read(f2, std::integral_constant<int, X - R>{}, now, h2);
           });
-          spread(n_frags, all, tc, [&](auto xc) { read_scale(s, xc, h1, s_now); });
+          spread(n_frags, all, tc, [&](auto xc) { shift(s, raw, xc, h1); });
           if constexpr (decltype(tc)::value == T / 8) load_scales_ahead();
         });
         quarter(f1, s, h1, [&](auto tc) {
@@ -465,9 +471,8 @@ struct NtTile {
             if constexpr (X < R) read(f2, std::integral_constant<int, X>{}, now, h2);
             else read(f3, std::integral_constant<int, X - R>{}, now, h3);
           });
-          spread(n_frags, all, tc, [&](auto xc) { shift(s, xc, h1); });
           if constexpr (decltype(tc)::value == T * 12 / 16) {
-            s_now = s_loaded[0];                              // the next step's
+            s_next = s_loaded[0];                             // where the next step's are
             next_scales();
           }
         });
@@ -483,11 +488,11 @@ struct NtTile {
         quarter(f3, s, h3, [&](auto tc) {
           constexpr int X = decltype(tc)::value;
           spread(std::integral_constant<int, SH::LOADS - SH::EARLY>{}, most, tc, [&](auto xc) { load(std::integral_constant<int, decltype(xc)::value + SH::EARLY>{}, lds0 + now); });
-          spread(n_frags, most, tc, [&](auto xc) { read_scale(s, xc, h0, s_now); });
+          spread(n_frags, most, tc, [&](auto xc) { read_scale(raw, xc, s_next); });
           spread(n_frags, most, tc, [&](auto xc) { read(f0, xc, behind, h0); });
           if constexpr (X == T * 13 / 16) next_operands();
           nt_for<R>([&](auto xc) {
-            if constexpr (T * 12 / 16 + decltype(xc)::value * (T - T * 12 / 16) / R == X) shift(s, xc, h0);
+            if constexpr (T * 12 / 16 + decltype(xc)::value * (T - T * 12 / 16) / R == X) shift(s, raw, xc, h0);
           });
         });
         pin();
