@@ -345,11 +345,12 @@ int dmm_mx_execute(dmm_plan_t *p, const dmm_mx_tiles *a, const dmm_mx_tiles *b, 
  * Tables of the tiles: matrix * (grid_rows * grid_cols) + ti * grid_cols + tj; the descriptor's replication is 1 (DMM_EREPL).
  * Elements bf16 or fp32 on either side; leading dimensions in elements.  Y may be X if both have the same type.
  * Products are of pairs of fp16 numbers, 22 bits of a value, with fp32 sums: an fp32 result is off by no more than fp32
- * products would leave it, a bf16 result is that rounded once.
- * At most DMM_ORTHOGONALIZE_STEPS steps (DMM_EINVAL).  The workspace (device memory, aligned to 256 bytes,
- * dmm_orthogonalize_workspace tells how much: DMM_ELIMIT if there is less; none for matrices of one tile of up to 128 x 128) is the caller's: nothing else is allocated and nothing kept, so calls with workspaces of their own may overlap on any streams
- * and be captured; calls that share one have to follow each other, replays of graphs included.  Sums are cut in a way that
- * depends on the shape and the count alone.  A dimension is 2^20 at most (DMM_ELIMIT). */
+ * products would leave it; a bf16 result is off by twice that, and rounded once.
+ * At most DMM_ORTHOGONALIZE_STEPS steps (DMM_EINVAL).  The workspace (device memory, aligned to 256 bytes;
+ * dmm_orthogonalize_workspace tells how much: DMM_ELIMIT if there is less; none for matrices of one tile of up to
+ * 128 x 128) is the caller's: nothing else is allocated and nothing kept, so calls with workspaces of their own may overlap
+ * on any streams and be captured; calls that share one have to follow each other, replays of graphs included.  Sums are cut
+ * in a way that depends on the shape and the count alone.  A dimension is 2^20 at most (DMM_ELIMIT). */
 #define DMM_ORTHOGONALIZE_STEPS 32
 int dmm_orthogonalize_workspace(const dmm_matrix_desc *X, int32_t count, int64_t *bytes);
 int dmm_orthogonalize(const dmm_matrix_desc *X, int32_t count, int x_dtype, const void *const *x_tiles, const int64_t *x_ld,

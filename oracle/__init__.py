@@ -9,6 +9,10 @@ This package is the slow, plain statement of what the path computes:
 * ``matmul``   -- ``C = A B`` by its definition (Section 2.1): an fp64 i-k-j
   triple loop in C (``matmul.c``), and the fp32 left-to-right replica sum
   (``reduce_replicas``, Table 1).
+* ``mx``       -- the 4-bit microscaled format: codes, scales and values of a
+  block from their definition.
+* ``orthogonalize`` -- Newton-Schulz steps in fp64, and a bound for what pairs
+  of fp16 numbers may be off.
 * ``execute``  -- runs a task list tile by tile in fp64 (Section 4.2, steps
   1-4 of direct execution) so that the plan's meaning can be checked on the
   CPU without any GPU.
