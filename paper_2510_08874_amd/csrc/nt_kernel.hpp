@@ -7,7 +7,7 @@
 //          three products (low high, high low, high high) use what is in LDS three times for two reads
 //
 // What bounds a 256 x 256 tile: a step of 128 bytes a row is 64 (pairs: 96) matrix instructions of 32 cycles on each of the four
-// matrix pipes (2048 or 3072 cycles), 128 KB of LDS reads (1024 cycles at 128 bytes), and 64 KB that loads bring into LDS, which take
+// matrix pipes (2048 cycles, pairs half as many again), 128 KB of LDS reads (1024 cycles at 128 bytes), and 64 KB that loads bring into LDS, which take
 // 1950 cycles by themselves (33 bytes a cycle and CU with all CUs at it; 17 TB/s from L2).  L2 answers requests of up to 128
 // bytes, so the rows of a step are whole lines.  (With steps of 64 bytes, and four bytes of scales a row
 // and step, there were four times as many requests: 16384 x 8192 x 28672 in 4 bits 2.42 ms, matrix pipes busy 35 %.)
@@ -16,12 +16,12 @@
 // instructions.  fp4: all fragments of a step are read in its first half and the quarter before; behind a barrier its stage is filled
 // again in the second half, a quarter before another barrier waits for the step behind it, so that loads of two steps overlap.  Pairs,
 // with half as much to load a cycle: fragments of a half are read during the half before it, one barrier a step.
-// fp4, 4096 x 4096 x 4096: 2660 cycles a step where one barrier in front of the last quarter, and 414 instructions a step instead
-// of 262, took 2900; matrix instructions and LDS reads alone take 2640, matrix instructions alone 2150.  A tile's ends come on top: 3 us
-// until the first step has landed, and 256 KB of fp32 from every CU at the same time take 11 us.
+// fp4, 4096 x 4096 x 4096: 2600 cycles a step with 187 instructions besides the matrix instructions.  Before, with 350 of them and one barrier in front of the
+// last quarter, 2900, of which matrix instructions and LDS reads alone took 2640, matrix instructions alone 2150.  A tile's ends come on top: 3
+// us until the first step has landed, and 256 KB of fp32 from every CU at the same time take 11 us.
 // The part lowers its clock under matrix load: a loop of matrix instructions on registers alone makes 6.5 PFLOP/s in fp4
 // and 1.8 in fp16 with random operands (9.7 and 2.5 with zeros), and a kernel that also moves operands has less power left for it
-// (1.7 GHz in fp4, 1.58 with pairs, whose pipes are busy 83 % of the time).
+// (1.6 to 1.7 GHz in fp4, 1.58 with pairs, whose pipes are busy 83 % of the time).
 #pragma once
 
 #include <hip/hip_runtime.h>

@@ -257,3 +257,40 @@ def test_many_small_matrices(even):
         assert np.linalg.norm(view(out, i).double().cpu().numpy() - oracle.orthogonalize(G)) <= oracle.limit(G)
     if not even:
         assert torch.equal(view(out, 7), view(out, 8))
+
+
+def test_calls_from_several_threads():
+    """Each with its own stream and buffers, on one shape of each kind; the same bits as one call alone."""
+    import threading
+    made = []
+    for rows, cols in ((90, 100), (200, 333)):
+        mats = random(3, rows, cols, rows)
+        d = binding.matrix_desc(whole(rows, cols))
+        size = binding.dmm_orthogonalize_workspace(d, 3)
+        want, _ = run(mats, whole(rows, cols))
+        made.append((mats, d, size, rows, cols, want))
+    jobs, errors = [], []
+    for i in range(6):
+        mats, d, size, rows, cols, want = made[i % 2]
+        out = [torch.zeros(rows, cols, device="cuda") for _ in mats]
+        jobs.append((d, binding.tile_table(mats, [cols] * 3), binding.tile_table(out, [cols] * 3), torch.empty(size + 256, dtype=torch.uint8, device="cuda"), size,
+                     torch.cuda.Stream(), out, want))
+    torch.cuda.synchronize()
+
+    def work(d, x, y, ws, size, stream, out, want):
+        try:
+            for _ in range(10):
+                binding.dmm_orthogonalize(d, 3, 2, x, 2, y, ws if size else None, size, stream=stream.cuda_stream)
+        except Exception as e:                                # (told by the test, not by the thread)
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=j) for j in jobs]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not errors
+    for j in jobs:
+        for got, want in zip(j[6], j[7]):
+            assert np.array_equal(got.double().cpu().numpy(), want)
