@@ -19,18 +19,36 @@ namespace dmm {
 
 constexpr float ORTHO_SCALE = 4096.f;
 
-struct OrthoPair {
-  _Float16 high, low;
-};
+typedef _Float16 ortho_h2 __attribute__((ext_vector_type(2)));
+typedef _Float16 ortho_h4 __attribute__((ext_vector_type(4)));
+typedef _Float16 ortho_h8 __attribute__((ext_vector_type(8)));
+typedef float ortho_f2 __attribute__((ext_vector_type(2)));
 // where the high part of an element lies in a matrix of `pitch` elements a row; the low part is 64 bytes on
 __device__ __forceinline__ int64_t ortho_at(int row, int col, unsigned pitch) {
   return (int64_t)row * (pitch * 4u) + (col >> 5) * 128 + (col & 31) * 2;
 }
-__device__ __forceinline__ OrthoPair ortho_split(float v) {
-  OrthoPair p;
-  p.high = (_Float16)v;
-  p.low = (_Float16)(v - (float)p.high);
+// Two values as pairs: four instructions (v - high in one, of a half that is not taken out first).
+struct OrthoPairs {
+  ortho_h2 high, low;
+};
+__device__ __forceinline__ OrthoPairs ortho_split(float v0, float v1) {
+  OrthoPairs p;
+  p.high = __builtin_convertvector((ortho_f2){v0, v1}, ortho_h2);
+  ortho_f2 rest;
+  float r0, r1;
+  asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(r0) : "v"(p.high), "v"(v0));
+  asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(r1) : "v"(p.high), "v"(v1));
+  rest = (ortho_f2){r0, r1};
+  p.low = __builtin_convertvector(rest, ortho_h2);
   return p;
+}
+__device__ __forceinline__ void ortho_split8(const float *v, ortho_h8 &high, ortho_h8 &low) {
+#pragma unroll
+  for (int x = 0; x < 8; x += 2) {
+    const OrthoPairs p = ortho_split(v[x], v[x + 1]);
+    high[x] = p.high[0], high[x + 1] = p.high[1];
+    low[x] = p.low[0], low[x + 1] = p.low[1];
+  }
 }
 
 __device__ __forceinline__ const OrthoTile &ortho_find(const OrthoTiles &args, int block, int *inside) {
@@ -81,8 +99,6 @@ __device__ __forceinline__ double ortho_inverse_norm(const double *sums, int n) 
   return s > 0.0 ? 1.0 / sqrt(s) : 0.0;
 }
 
-typedef _Float16 ortho_h8 __attribute__((ext_vector_type(8)));
-
 // G / |G| as pairs, by rows and by columns: 64 x 64 elements a workgroup, turned through LDS, from multiples of 8 on so that eight
 // neighbours are stored together, 16 bytes high and 16 low parts; element by element where a tile begins or ends inside of
 // them.  (Stores of two bytes took 1021 x 4090 21 us, these take 17; 50 MB.)
@@ -113,12 +129,7 @@ __global__ __launch_bounds__(256) void ortho_split_kernel(OrthoTiles) {
   auto put = [&](char *to, int line, int lines, int line0, int at, int n, int at0, unsigned pitch, const float *f) {
     if (line < 0 || line >= lines) return;
     ortho_h8 high, low;
-#pragma unroll
-    for (int x = 0; x < 8; ++x) {
-      const OrthoPair p = ortho_split(f[x]);
-      high[x] = p.high;
-      low[x] = p.low;
-    }
+    ortho_split8(f, high, low);
     char *const out = to + ortho_at(line0 + line, at0 + at, pitch);
     if (at >= 0 && at + 8 <= n) {
       *(ortho_h8 *)out = high;
@@ -181,13 +192,10 @@ __device__ __forceinline__ void ortho_rows8(const OrthoProduct &g, char *ws, int
     low = *(const ortho_h8 *)(ws + g.old + at + 64);
   }
 #pragma unroll
-  for (int x = 0; x < 8; ++x) {
+  for (int x = 0; x < 8; ++x)
     v[x] = col + x < g.n ? g.alpha * ((float)high[x] + (float)low[x]) + g.beta * v[x] + (col + x == row ? g.diagonal : 0.f) : 0.f;
-    const OrthoPair p = ortho_split(v[x]);
-    high[x] = p.high;
-    low[x] = p.low;
-  }
   if (g.y >= 0) return;
+  ortho_split8(v, high, low);
   *(ortho_h8 *)(ws + g.out + at) = high;
   *(ortho_h8 *)(ws + g.out + at + 64) = low;
 }
@@ -195,12 +203,7 @@ __device__ __forceinline__ void ortho_rows8(const OrthoProduct &g, char *ws, int
 __device__ __forceinline__ void ortho_cols8(const OrthoProduct &g, char *ws, int row, int col, const float *v) {
   if (col >= g.n || (unsigned)row >= g.turned_pitch) return;
   ortho_h8 high, low;
-#pragma unroll
-  for (int x = 0; x < 8; ++x) {
-    const OrthoPair p = ortho_split(v[x]);
-    high[x] = p.high;
-    low[x] = p.low;
-  }
+  ortho_split8(v, high, low);
   char *const at = ws + g.turned + ortho_at(col, row, g.turned_pitch);
   *(ortho_h8 *)at = high;
   *(ortho_h8 *)(at + 64) = low;
@@ -411,36 +414,41 @@ __global__ __launch_bounds__(ORTHO_SMALL_THREADS) void ortho_small_kernel(OrthoS
 
   // ---- between registers and areas -----------------------------------------------------------
   // (addresses are written so that all but a few exclusive ors of constants are offsets of the instructions)
-  auto put_rows = [&](unsigned area, const nt_f32x16 (&v)[2]) {
+  struct Pairs {
+    OrthoPairs p[2][8];                                       // of elements 2 x, 2 x + 1: neighbouring rows of a column
+  };
+  auto split = [&](const nt_f32x16 (&v)[2]) {
+    Pairs out;
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int x = 0; x < 8; ++x) out.p[j][x] = ortho_split(v[j][2 * x], v[j][2 * x + 1]);
+    return out;
+  };
+  auto put_rows = [&](unsigned area, const Pairs &v) {
     const unsigned base = area + ortho_area(row0 + 4 * g, col0 + r);
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int x = 0; x < 16; ++x) {
-        const OrthoPair p = ortho_split(v[j][x]);
+        const OrthoPairs &p = v.p[j][x / 2];
         const int row = 8 * (x / 4) + x % 4, turn = ((row & 15) ^ (8 * j)) << 4;   // (32 columns on are 8 slots on)
-        *(__attribute__((address_space(3))) _Float16 *)((nt_lptr)(uintptr_t)(base ^ turn) + row * (ORTHO_SMALL * 4)) = p.high;
-        *(__attribute__((address_space(3))) _Float16 *)((nt_lptr)(uintptr_t)(base ^ turn ^ 64) + row * (ORTHO_SMALL * 4)) = p.low;
+        *(__attribute__((address_space(3))) _Float16 *)((nt_lptr)(uintptr_t)(base ^ turn) + row * (ORTHO_SMALL * 4)) = p.high[x % 2];
+        *(__attribute__((address_space(3))) _Float16 *)((nt_lptr)(uintptr_t)(base ^ turn ^ 64) + row * (ORTHO_SMALL * 4)) = p.low[x % 2];
         if (x % 4 == 3) __builtin_amdgcn_sched_barrier(0);
       }
   };
   // (the transpose; four neighbouring rows of a column at a time)
-  auto put_cols = [&](unsigned area, const nt_f32x16 (&v)[2]) {
-    typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+  auto put_cols = [&](unsigned area, const Pairs &v) {
     const unsigned base = area + ortho_area(col0 + r, row0 + 4 * g);
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
-      for (int x = 0; x < 16; x += 4) {
-        h4 high, low;
-#pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          const OrthoPair p = ortho_split(v[j][x + y]);
-          high[y] = p.high;
-          low[y] = p.low;
-        }
-        *(__attribute__((address_space(3))) h4 *)((nt_lptr)(uintptr_t)(base ^ (x / 4 << 4)) + 32 * j * (ORTHO_SMALL * 4)) = high;
-        *(__attribute__((address_space(3))) h4 *)((nt_lptr)(uintptr_t)(base ^ (x / 4 << 4) ^ 64) + 32 * j * (ORTHO_SMALL * 4)) = low;
+      for (int x = 0; x < 4; ++x) {
+        const OrthoPairs &p = v.p[j][2 * x], &q = v.p[j][2 * x + 1];
+        const ortho_h4 high = {p.high[0], p.high[1], q.high[0], q.high[1]}, low = {p.low[0], p.low[1], q.low[0], q.low[1]};
+        *(__attribute__((address_space(3))) ortho_h4 *)((nt_lptr)(uintptr_t)(base ^ (x << 4)) + 32 * j * (ORTHO_SMALL * 4)) = high;
+        *(__attribute__((address_space(3))) ortho_h4 *)((nt_lptr)(uintptr_t)(base ^ (x << 4) ^ 64) + 32 * j * (ORTHO_SMALL * 4)) = low;
         __builtin_amdgcn_sched_barrier(0);
       }
   };
@@ -496,21 +504,22 @@ __global__ __launch_bounds__(ORTHO_SMALL_THREADS) void ortho_small_kernel(OrthoS
       asm volatile("" : "+v"(r), "+v"(g));
       __builtin_amdgcn_sched_barrier(0);
     };
-    put_rows(area1, X);
+    const Pairs x_pairs = split(X);
+    put_rows(area1, x_pairs);
     sync();
     product(area1, area1, l, S);
 #pragma unroll
     for (int j = 0; j < 2; ++j) S[j] *= UNIT;
     __builtin_amdgcn_sched_barrier(0);
-    put_cols(area2, S);                // (symmetric)
+    put_cols(area2, split(S));         // (symmetric)
     sync();
-    put_cols(area1, X);
+    put_cols(area1, x_pairs);
     product(area2, area2, s, acc);
     sync();
 #pragma unroll
     for (int j = 0; j < 2; ++j) S[j] = b * S[j] + c * UNIT * acc[j];
     __builtin_amdgcn_sched_barrier(0);
-    put_cols(area2, S);
+    put_cols(area2, split(S));
     sync();
     product(area2, area1, s, acc);
 #pragma unroll
