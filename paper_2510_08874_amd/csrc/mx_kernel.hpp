@@ -286,7 +286,9 @@ template <bool F32>
 struct MxBlock {
   static constexpr int ES = F32 ? 4 : 2, COLS = 256 / ES;     // 64 or 128 columns
   static constexpr int PITCH = 256 + 4;                       // bytes (one word more: rows start in other banks)
-  static constexpr int LDS = 128 * PITCH;
+  static constexpr int LDS = 128 * PITCH + 3 * 64;
+  // byte that a row starts at: 16 words further on every 32 rows, which four neighbouring threads have in hand at a time
+  static __device__ __forceinline__ int at(int row) { return row * PITCH + (row >> 5) * 64; }
   static constexpr int ACROSS = COLS / 8, DOWN = 256 / ACROSS, PASSES = 128 / DOWN;   // threads to a row of a pass, rows of a pass
   static constexpr int OWN = COLS / 64;                       // columns of a thread
 };
@@ -310,7 +312,7 @@ __global__ __launch_bounds__(256) void mx_cols_kernel(MxTileArgs) {
 #pragma unroll
     for (int x = 0; x < B::PASSES; ++x) {
       const int r = x * B::DOWN + r0;
-      unsigned *p = (unsigned *)(lds + r * B::PITCH + tid % B::ACROSS * 8 * B::ES);
+      unsigned *p = (unsigned *)(lds + B::at(r) + tid % B::ACROSS * 8 * B::ES);
 #pragma unroll
       for (int i = 0; i < MxVec<F32>::WORDS; ++i) p[i] = v[x].w[i];
       if constexpr (ROWS) {
@@ -329,7 +331,7 @@ __global__ __launch_bounds__(256) void mx_cols_kernel(MxTileArgs) {
   unsigned words[B::OWN][F32 ? 32 : 16];                      // a column: 32 fp32, or 32 bf16 in pairs
 #pragma unroll
   for (int i = 0; i < 32; i += 2) {
-    const char *q = lds + (32 * b + i) * B::PITCH + p * 4;
+    const char *q = lds + B::at(32 * b + i) + p * 4;
     const unsigned x = *(const unsigned *)q, y = *(const unsigned *)(q + B::PITCH);
     if constexpr (F32) {
       words[0][i] = x;
@@ -441,7 +443,7 @@ __global__ __launch_bounds__(256) void mx_col_values_kernel(MxTileArgs) {
     const MxVec<F32> x = mx_values<F32>((unsigned)codes[0][k], scale[0]), y = mx_values<F32>((unsigned)codes[B::OWN - 1][k], scale[B::OWN - 1]);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      unsigned *const q = (unsigned *)(lds + (32 * b + 8 * k + i) * B::PITCH + p * 4);
+      unsigned *const q = (unsigned *)(lds + B::at(32 * b + 8 * k + i) + p * 4);
       if constexpr (F32) *q = x.w[i];
       else *q = __builtin_amdgcn_perm(y.w[i / 2], x.w[i / 2], i & 1 ? 0x07060302 : 0x05040100);
     }
@@ -453,7 +455,7 @@ __global__ __launch_bounds__(256) void mx_col_values_kernel(MxTileArgs) {
     const int r = pass * B::DOWN + r0;
     if (row0 + r >= T.h) continue;
     MxVec<F32> v;
-    const unsigned *q = (const unsigned *)(lds + r * B::PITCH + tid % B::ACROSS * 8 * B::ES);
+    const unsigned *q = (const unsigned *)(lds + B::at(r) + tid % B::ACROSS * 8 * B::ES);
 #pragma unroll
     for (int i = 0; i < MxVec<F32>::WORDS; ++i) v.w[i] = q[i];
     mx_store8<F32>((char *)T.x + (int64_t)(row0 + r) * T.x_pitch, col, T.w, v);
