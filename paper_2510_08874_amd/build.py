@@ -38,7 +38,7 @@ def check_resources(remarks: str, want_kernel: bool) -> None:
         name = b.split()[0]
         if "small_gemm_kernel" in name and re.search(r"(ScratchSize \[bytes/lane\]|VGPRs Spill): [1-9]", b):
             raise RuntimeError(f"{name}: scratch use or spills")
-        if re.search("mx_gemm_kernel|ortho_product_kernel", name) and re.search(r"(ScratchSize \[bytes/lane\]|VGPRs Spill): [1-9]", b):
+        if re.search(r"mx_\w*kernel|ortho_\w*kernel", name) and re.search(r"(ScratchSize \[bytes/lane\]|VGPRs Spill): [1-9]", b):
             raise RuntimeError(f"{name}: scratch use or spills")
         if "grouped_gemm_kernel" not in name:
             continue

@@ -63,27 +63,35 @@ __global__ __launch_bounds__(NT_THREADS, SH::LDS > 80 * 1024 ? 1 : 2) void mx_ge
     mx_store<SH, unsigned short>(tile, it);
     return;
   }
-  // bf16: through LDS, so that a thread stores 16 bytes of a row (16384 x 8192 x 28672: 2.54 -> 2.42 ms; with stores that the caches keep 2 % slower)
+  // bf16: through LDS, so that a thread stores 16 bytes of a row (16384 x 8192 x 28672: 2.54 -> 2.42 ms; with stores that the caches keep 2 % slower).
+  // What a thread takes from a slice is read at once: with one wave on a SIMD every read by itself waits out the latency of LDS (a
+  // tile's end 19000 cycles).
   if constexpr (SH::WM == 2) {
     tile.slices(lds, [&](const float *values, int base) {
-      constexpr int PER = SH::TN / 8;
-      for (int x = threadIdx.x; x < 64 * PER; x += NT_THREADS) {
-        const int r = x / PER, col = x % PER * 8, row = base + (r & 31) + (r >> 5) * (SH::TM / 2);
+      constexpr int PER = SH::TN / 8, N = 64 * PER / NT_THREADS, ROWS = NT_THREADS / PER;
+      const int r0 = threadIdx.x / PER, col = threadIdx.x % PER * 8;
+      nt_f32x4 v[N][2];
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const nt_f32x4 *const from = (const nt_f32x4 *)(values + nt_value(r0 + i * ROWS, col, NtTile<SH>::PITCH));
+        v[i][0] = from[0];
+        v[i][1] = from[1];
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int r = r0 + i * ROWS, row = base + (r & 31) + (r >> 5) * (SH::TM / 2);
         if (row >= it.m_ext || col >= it.n_ext) continue;
-        const nt_f32x4 *const from = (const nt_f32x4 *)(values + nt_value(r, col, NtTile<SH>::PITCH)), v = from[0], u = from[1];
         char *const to = it.c + ((int64_t)row * it.ldc + col) * 2;
         if (col + 8 <= it.n_ext) {
           nt_i32x4 w;
 #pragma unroll
-          for (int y = 0; y < 4; ++y) {
-            const nt_f32x4 &f = y < 2 ? v : u;
-            w[y] = (int)((unsigned)mx_bf16(f[2 * (y & 1)]) | (unsigned)mx_bf16(f[2 * (y & 1) + 1]) << 16);
-          }
+          for (int y = 0; y < 4; ++y) w[y] = (int)((unsigned)mx_bf16(v[i][y / 2][2 * (y & 1)]) | (unsigned)mx_bf16(v[i][y / 2][2 * (y & 1) + 1]) << 16);
           __builtin_nontemporal_store(w, (mx_i32x4_any *)to);
         } else {
 #pragma unroll
           for (int y = 0; y < 8; ++y)
-            if (col + y < it.n_ext) ((unsigned short *)to)[y] = mx_bf16(y < 4 ? v[y] : u[y - 4]);
+            if (col + y < it.n_ext) ((unsigned short *)to)[y] = mx_bf16(v[i][y / 4][y % 4]);
         }
       }
     });
