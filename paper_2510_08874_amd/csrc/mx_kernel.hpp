@@ -16,6 +16,8 @@ namespace dmm {
 
 // ---- products -------------------------------------------------------------------------------------
 
+typedef __bf16 mx_bf16x2 __attribute__((ext_vector_type(2)));
+typedef float mx_f32x2 __attribute__((ext_vector_type(2)));
 typedef int mx_i32x4_any __attribute__((ext_vector_type(4), aligned(2)));   // (16 bytes at any address of a bf16)
 __device__ __forceinline__ unsigned short mx_bf16(float v) { return __builtin_bit_cast(unsigned short, (__bf16)v); }
 
@@ -46,11 +48,24 @@ __device__ __forceinline__ void mx_store(const NtTile<SH> &tile, const MxItem &i
     }
 }
 
+// A region of C that no op writes.
+__device__ __forceinline__ void mx_zeros(const MxItem &it) {
+  for (int x = threadIdx.x; x < it.m_ext * it.n_ext; x += NT_THREADS) {
+    const int64_t at = (int64_t)(x / it.n_ext) * it.ldc + x % it.n_ext;
+    if (it.c_es == 4) ((float *)it.c)[at] = 0.f;
+    else ((unsigned short *)it.c)[at] = 0;
+  }
+}
+
 // Macro-tiles.
 template <class SH>
 __global__ __launch_bounds__(NT_THREADS, SH::LDS > 80 * 1024 ? 1 : 2) void mx_gemm_kernel(const MxItem *__restrict__ items, const NtSeg *__restrict__ segs) {
   extern __shared__ char lds[];
   const MxItem it = items[blockIdx.x];
+  if (it.steps == 0) {
+    mx_zeros(it);
+    return;
+  }
   NtTile<SH> tile;
   tile.run(it.front, segs + it.seg, it.n_segs, it.first, it.steps, it.m_off, it.m_ext, it.n_off, it.n_ext, lds);
   tile.pin();
@@ -67,8 +82,10 @@ __global__ __launch_bounds__(NT_THREADS, SH::LDS > 80 * 1024 ? 1 : 2) void mx_ge
   // What a thread takes from a slice is read at once: with one wave on a SIMD every read by itself waits out the latency of LDS (a
   // tile's end 19000 cycles).
   if constexpr (SH::WM == 2) {
+    const unsigned pitch = (unsigned)it.ldc * 2u;
     tile.slices(lds, [&](const float *values, int base) {
       constexpr int PER = SH::TN / 8, N = 64 * PER / NT_THREADS, ROWS = NT_THREADS / PER;
+      static_assert(32 % ROWS == 0, "a thread's rows lie at the same distance in every half");
       const int r0 = threadIdx.x / PER, col = threadIdx.x % PER * 8;
       nt_f32x4 v[N][2];
 #pragma unroll
@@ -78,20 +95,26 @@ __global__ __launch_bounds__(NT_THREADS, SH::LDS > 80 * 1024 ? 1 : 2) void mx_ge
         v[i][1] = from[1];
       }
       __builtin_amdgcn_sched_barrier(0);
+      const unsigned mine = (unsigned)r0 * pitch + (unsigned)col * 2u;
+      const int rows = it.m_ext - base - r0;                  // below which the thread's rows are inside
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const int r = r0 + i * ROWS, row = base + (r & 31) + (r >> 5) * (SH::TM / 2);
-        if (row >= it.m_ext || col >= it.n_ext) continue;
-        char *const to = it.c + ((int64_t)row * it.ldc + col) * 2;
-        if (col + 8 <= it.n_ext) {
-          nt_i32x4 w;
+        const int down = (i * ROWS & 31) + (i * ROWS >> 5) * (SH::TM / 2);
+        char *const to = (char *)nt_uniform(it.c + (int64_t)(base + down) * pitch) + mine;
+        nt_i32x4 w;
 #pragma unroll
-          for (int y = 0; y < 4; ++y) w[y] = (int)((unsigned)mx_bf16(v[i][y / 2][2 * (y & 1)]) | (unsigned)mx_bf16(v[i][y / 2][2 * (y & 1) + 1]) << 16);
-          __builtin_nontemporal_store(w, (mx_i32x4_any *)to);
-        } else {
-#pragma unroll
-          for (int y = 0; y < 8; ++y)
-            if (col + y < it.n_ext) ((unsigned short *)to)[y] = mx_bf16(v[i][y / 4][y % 4]);
+        for (int y = 0; y < 4; ++y) {
+          const mx_f32x2 f = {v[i][y / 2][2 * (y & 1)], v[i][y / 2][2 * (y & 1) + 1]};
+          w[y] = __builtin_bit_cast(int, __builtin_convertvector(f, mx_bf16x2));
+        }
+        if (down < rows && col + 8 <= it.n_ext) __builtin_nontemporal_store(w, (mx_i32x4_any *)to);
+      }
+      // the columns behind the last whole eight
+      if (it.n_ext & 7) {
+        const int c0 = it.n_ext & ~7, n = it.n_ext & 7;
+        for (int x = threadIdx.x; x < 64 * n; x += NT_THREADS) {
+          const int r = x / n, c = c0 + x % n, row = base + (r & 31) + (r >> 5) * (SH::TM / 2);
+          if (row < it.m_ext) *(unsigned short *)(it.c + (int64_t)row * pitch + c * 2) = mx_bf16(values[nt_value(r, c, NtTile<SH>::PITCH)]);
         }
       }
     });
@@ -177,7 +200,6 @@ __global__ __launch_bounds__(NT_THREADS) void mx_skinny_kernel(const MxItem *__r
 // ---- quantisation -----------------------------------------------------------------------------------
 
 typedef unsigned short mx_u16x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 mx_bf16x2 __attribute__((ext_vector_type(2)));
 
 // Eight (2 N) neighbouring elements of a tile as they came: words of two bf16, or fp32.
 template <bool F32>

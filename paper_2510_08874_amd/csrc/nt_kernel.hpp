@@ -145,7 +145,7 @@ struct NtTile {
   }
 
   // `front`: the segment that holds the first step, step `first` of it; `segs`: n_segs from that one on (read from the second
-  // on); `steps`: in all.  A segment of an odd number of chunks ends with half a step.
+  // on); `steps`: in all, one at least.  A segment of an odd number of chunks ends with half a step.
   __device__ __forceinline__ void run(const NtSeg &front, const NtSeg *segs, int n_segs, int first, int steps, int m_off, int m_ext, int n_off, int n_ext,
                                       char *lds) {
     constexpr int MI = SH::MI, NI = SH::NI, LA = SH::LA, LB = SH::LB;
@@ -157,7 +157,6 @@ struct NtTile {
     for (int i = 0; i < MI; ++i)
 #pragma unroll
       for (int j = 0; j < NI; ++j) acc[i][j] = nt_f32x16{};
-    if (steps <= 0) return;
 
     // ---- this lane's part of the loads -----------------------------------------------------
     // load x of a wave: rows 8 (4 x + wave) ..., 16 bytes a lane, in the order of the stage
@@ -451,7 +450,7 @@ struct NtTile {
       nt_for<R>([&](auto xc) { shift(s, raw, xc, h0); });
       nt_for<R>([&](auto xc) { read(f0, xc, 0, h0); });
 #pragma clang loop unroll(disable)
-      for (int t = steps; t > 0; --t) {
+      do {
         const unsigned behind = now == (SH::NST - 1) * SH::STAGE ? 0 : now + SH::STAGE;
         unsigned s_next = 0;
         // All of this step's fragments are read in three quarters: its stage may be filled a quarter before the next one
@@ -498,7 +497,7 @@ struct NtTile {
         pin();
         next_rest();
         now = behind;
-      }
+      } while (--steps > 0);
     } else {
       Pair f0, f1;
       nt_for<R>([&](auto xc) {
@@ -506,7 +505,7 @@ struct NtTile {
         read(f0.part[0], xc, 0, h0);
       });
 #pragma clang loop unroll(disable)
-      for (int t = steps; t > 0; --t) {
+      do {
         const unsigned behind = now == (SH::NST - 1) * SH::STAGE ? 0 : now + SH::STAGE;
         half(f0, h0, f1, now, nothing);
         nt_wait_loads<(SH::NST - 2) * SH::LOADS>();
@@ -521,7 +520,7 @@ struct NtTile {
         now = behind;
         pin();
         next();
-      }
+      } while (--steps > 0);
     }
     nt_wait_loads<0>();
   }
