@@ -18,34 +18,62 @@ namespace dmm {
 
 typedef __bf16 mx_bf16x2 __attribute__((ext_vector_type(2)));
 typedef float mx_f32x2 __attribute__((ext_vector_type(2)));
-typedef int mx_i32x4_any __attribute__((ext_vector_type(4), aligned(2)));   // (16 bytes at any address of a bf16)
+typedef int mx_i32_any __attribute__((aligned(2)));           // (two bf16 at any address of one)
 __device__ __forceinline__ unsigned short mx_bf16(float v) { return __builtin_bit_cast(unsigned short, (__bf16)v); }
 
-// Half a wave stores 32 neighbouring columns of a row.  (The host sees to it that a macro-tile's rows lie within 2^32 bytes.)
-template <class SH, class E>
+// fp32: half a wave stores 32 neighbouring columns of a row.  bf16: the halves of a wave exchange two tiles of 32 columns, so that all lanes
+// have neighbouring columns of the same two rows, and lanes of an even and an odd column halves of these: a wave stores 64 columns of
+// two rows, whole lines.  Straight from the registers; by way of LDS, 64 rows at a time and 16 bytes a thread, the end of a tile took 11800 cycles
+// (19000 with one read of LDS after the other).  Addresses are a row's, the same for the wave, and a lane's, the same for
+// all rows.  INSIDE: the whole macro-tile is.  (The host sees to it that a macro-tile's rows lie within 2^32 bytes.)
+template <class SH, bool F32, bool INSIDE>
 __device__ __forceinline__ void mx_store(const NtTile<SH> &tile, const MxItem &it) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int row0 = wave / SH::WN * (SH::TM / SH::WM) + 4 * (lane >> 5), col0 = wave % SH::WN * (SH::TN / SH::WN) + (lane & 31);
-  const unsigned pitch = (unsigned)it.ldc * (unsigned)sizeof(E);
-  char *const c = (char *)nt_uniform(it.c);
-#pragma unroll
-  for (int i = 0; i < SH::MI; ++i)
-#pragma unroll
-    for (int j = 0; j < SH::NI; ++j) {
-      const int col = col0 + 32 * j;
-      if (col < it.n_ext) {
-#pragma unroll
-        for (int x = 0; x < 16; ++x) {
-          const int row = row0 + 32 * i + 8 * (x / 4) + x % 4;
-          if (row < it.m_ext) {
-            E *const to = (E *)(c + ((unsigned)row * pitch + (unsigned)col * (unsigned)sizeof(E)));
-            if constexpr (sizeof(E) == 4) __builtin_nontemporal_store(tile.acc[i][j][x], to);
-            else __builtin_nontemporal_store(mx_bf16(tile.acc[i][j][x]), to);
-          }
+  constexpr bool LINES = !F32 && SH::NI % 2 == 0;             // (of one tile of 32 columns: half of a line)
+  constexpr int ES = F32 ? 4 : 2;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wave_row = wave / SH::WN * (SH::TM / SH::WM), wave_col = wave % SH::WN * (SH::TN / SH::WN);
+  const unsigned pitch = (unsigned)it.ldc * (unsigned)ES;
+  const int row0 = (LINES ? 0 : 4 * (lane >> 5)) + (F32 ? 0 : lane & 1), col0 = F32 ? lane & 31 : LINES ? lane & 62 : lane & 30;
+  const unsigned mine = (unsigned)row0 * pitch + (unsigned)col0 * (unsigned)ES;
+  const unsigned pick = lane & 1 ? 0x07060302 : 0x01000504;   // bf16: the high halves of both lanes, or the low ones
+  const int rows = it.m_ext - wave_row - row0, cols = it.n_ext - wave_col - col0;   // below which the lane's are inside
+  const char *at = (const char *)nt_uniform(it.c + (int64_t)wave_row * pitch + wave_col * ES);
+  // two rows of a column in each lane, one column on in the other of two lanes: two columns of one row, from row `row` and column `col` on
+  auto pair = [&](unsigned own, const char *to, int row, int col) {
+    const unsigned other = (unsigned)__builtin_amdgcn_mov_dpp((int)own, 0xB1, 0xF, 0xF, true);   // lane ^ 1
+    const int both = (int)__builtin_amdgcn_perm(own, other, pick);
+    if (INSIDE || (row < rows && col + 1 < cols)) __builtin_nontemporal_store(both, (mx_i32_any *)(to + mine + col * 2));
+    else if (row < rows && col < cols) *(unsigned short *)(to + mine + col * 2) = (unsigned short)both;
+  };
+  nt_for<SH::MI>([&](auto ic) {
+    constexpr int I = decltype(ic)::value;
+    nt_for<16>([&](auto xc) {
+      constexpr int X = decltype(xc)::value, ROW = 32 * I + 8 * (X / 4) + X % 4;
+      if constexpr (F32) {
+        nt_for<SH::NI>([&](auto jc) {
+          constexpr int J = decltype(jc)::value;
+          if (INSIDE || (ROW < rows && 32 * J < cols)) __builtin_nontemporal_store(tile.acc[I][J][X], (float *)(at + mine) + 32 * J);
+        });
+      } else if constexpr (X % 2 == 0) {
+        auto two = [&](const nt_f32x16 &v) {
+          return __builtin_bit_cast(unsigned, __builtin_convertvector((mx_f32x2){v[X], v[X + 1]}, mx_bf16x2));
+        };
+        if constexpr (LINES) {
+          nt_for<SH::NI / 2>([&](auto jc) {
+            constexpr int J = 2 * decltype(jc)::value;
+            // {first's lower half, second's lower half}: rows ROW, ROW + 1; {the upper halves}: four rows on
+            const auto r = __builtin_amdgcn_permlane32_swap(two(tile.acc[I][J]), two(tile.acc[I][J + 1]), false, false);
+            pair(r[0], at, ROW, 32 * J);
+            pair(r[1], at + 4 * (int64_t)pitch, ROW + 4, 32 * J);
+          });
+        } else {
+          nt_for<SH::NI>([&](auto jc) { pair(two(tile.acc[I][decltype(jc)::value]), at, ROW, 32 * decltype(jc)::value); });
         }
       }
       __builtin_amdgcn_sched_barrier(0);
-    }
+      at += X % 4 == 3 ? 5 * (int64_t)pitch : (int64_t)pitch;
+    });
+  });
 }
 
 // A region of C that no op writes.
@@ -69,55 +97,13 @@ __global__ __launch_bounds__(NT_THREADS, SH::LDS > 80 * 1024 ? 1 : 2) void mx_ge
   NtTile<SH> tile;
   tile.run(it.front, segs + it.seg, it.n_segs, it.first, it.steps, it.m_off, it.m_ext, it.n_off, it.n_ext, lds);
   tile.pin();
-  // fp32: half a wave writes 32 neighbouring columns of a row
+  const bool inside = it.m_ext == SH::TM && it.n_ext == SH::TN;
   if (it.c_es == 4) {
-    mx_store<SH, float>(tile, it);
-    return;
-  }
-  if constexpr (SH::WM == 1) {
-    mx_store<SH, unsigned short>(tile, it);
-    return;
-  }
-  // bf16: through LDS, so that a thread stores 16 bytes of a row (16384 x 8192 x 28672: 2.54 -> 2.42 ms; with stores that the caches keep 2 % slower).
-  // What a thread takes from a slice is read at once: with one wave on a SIMD every read by itself waits out the latency of LDS (a
-  // tile's end 19000 cycles).
-  if constexpr (SH::WM == 2) {
-    const unsigned pitch = (unsigned)it.ldc * 2u;
-    tile.slices(lds, [&](const float *values, int base) {
-      constexpr int PER = SH::TN / 8, N = 64 * PER / NT_THREADS, ROWS = NT_THREADS / PER;
-      static_assert(32 % ROWS == 0, "a thread's rows lie at the same distance in every half");
-      const int r0 = threadIdx.x / PER, col = threadIdx.x % PER * 8;
-      nt_f32x4 v[N][2];
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const nt_f32x4 *const from = (const nt_f32x4 *)(values + nt_value(r0 + i * ROWS, col, NtTile<SH>::PITCH));
-        v[i][0] = from[0];
-        v[i][1] = from[1];
-      }
-      __builtin_amdgcn_sched_barrier(0);
-      const unsigned mine = (unsigned)r0 * pitch + (unsigned)col * 2u;
-      const int rows = it.m_ext - base - r0;                  // below which the thread's rows are inside
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const int down = (i * ROWS & 31) + (i * ROWS >> 5) * (SH::TM / 2);
-        char *const to = (char *)nt_uniform(it.c + (int64_t)(base + down) * pitch) + mine;
-        nt_i32x4 w;
-#pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          const mx_f32x2 f = {v[i][y / 2][2 * (y & 1)], v[i][y / 2][2 * (y & 1) + 1]};
-          w[y] = __builtin_bit_cast(int, __builtin_convertvector(f, mx_bf16x2));
-        }
-        if (down < rows && col + 8 <= it.n_ext) __builtin_nontemporal_store(w, (mx_i32x4_any *)to);
-      }
-      // the columns behind the last whole eight
-      if (it.n_ext & 7) {
-        const int c0 = it.n_ext & ~7, n = it.n_ext & 7;
-        for (int x = threadIdx.x; x < 64 * n; x += NT_THREADS) {
-          const int r = x / n, c = c0 + x % n, row = base + (r & 31) + (r >> 5) * (SH::TM / 2);
-          if (row < it.m_ext) *(unsigned short *)(it.c + (int64_t)row * pitch + c * 2) = mx_bf16(values[nt_value(r, c, NtTile<SH>::PITCH)]);
-        }
-      }
-    });
+    if (inside) mx_store<SH, true, true>(tile, it);
+    else mx_store<SH, true, false>(tile, it);
+  } else {
+    if (inside) mx_store<SH, false, true>(tile, it);
+    else mx_store<SH, false, false>(tile, it);
   }
 }
 
