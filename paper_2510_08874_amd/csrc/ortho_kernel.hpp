@@ -177,25 +177,27 @@ __global__ __launch_bounds__(256) void ortho_store_kernel(OrthoTiles) {
   }
 }
 
-// Eight neighbouring elements of a row of out: their sums to what they hold (zero outside of the matrix), stored row by
-// row; the values replace the sums.
-__device__ __forceinline__ void ortho_rows8(const OrthoProduct &g, char *ws, int row, int col, float *v) {
-  const int64_t at = ortho_at(row, col, g.out_pitch);
-  if (row >= g.m || (unsigned)col >= g.out_pitch) {           // (out_pitch is a multiple of 32)
+// What eight neighbouring elements of a row of out are added to.
+__device__ __forceinline__ void ortho_old8(const OrthoProduct &g, const char *ws, int row, int col, ortho_h8 &high, ortho_h8 &low) {
+  high = low = ortho_h8{};
+  if (g.old < 0 || row >= g.m || (unsigned)col >= g.out_pitch) return;   // (out_pitch is a multiple of 32)
+  const char *const at = ws + g.old + ortho_at(row, col, g.out_pitch);
+  high = *(const ortho_h8 *)at;
+  low = *(const ortho_h8 *)(at + 64);
+}
+// Their sums to what they hold (zero outside of the matrix), stored row by row; the values replace the sums.
+__device__ __forceinline__ void ortho_rows8(const OrthoProduct &g, char *ws, int row, int col, ortho_h8 high, ortho_h8 low, float *v) {
+  if (row >= g.m || (unsigned)col >= g.out_pitch) {
 #pragma unroll
     for (int x = 0; x < 8; ++x) v[x] = 0.f;
     return;
-  }
-  ortho_h8 high = {}, low = {};
-  if (g.old >= 0) {
-    high = *(const ortho_h8 *)(ws + g.old + at);
-    low = *(const ortho_h8 *)(ws + g.old + at + 64);
   }
 #pragma unroll
   for (int x = 0; x < 8; ++x)
     v[x] = col + x < g.n ? g.alpha * ((float)high[x] + (float)low[x]) + g.beta * v[x] + (col + x == row ? g.diagonal : 0.f) : 0.f;
   if (g.y >= 0) return;
   ortho_split8(v, high, low);
+  const int64_t at = ortho_at(row, col, g.out_pitch);
   *(ortho_h8 *)(ws + g.out + at) = high;
   *(ortho_h8 *)(ws + g.out + at + 64) = low;
 }
@@ -214,15 +216,32 @@ template <int TN, int ROWS>
 __device__ __forceinline__ void ortho_finish(const OrthoProduct &g, char *ws, float *values, int pitch, int row0, int apart, int col0, bool mirror) {
   constexpr int PER = TN / 8, HALF = ROWS / 2;
   auto row_of = [&](int r) { return row0 + r % HALF + r / HALF * apart; };
-  for (int x = threadIdx.x; x < ROWS * PER; x += NT_THREADS) {
-    const int r = x / PER, c = x % PER * 8;
+  // (what a thread reads is read at once: one after the other every read waits out its latency)
+  constexpr int N = (ROWS * PER + NT_THREADS - 1) / NT_THREADS;
+  float v[N][8];
+  ortho_h8 high[N], low[N];
+  const bool all = ROWS * PER % NT_THREADS == 0 || (int)threadIdx.x < ROWS * PER;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int x = i * NT_THREADS + threadIdx.x;
+    if (all) ortho_old8(g, ws, row_of(x / PER), col0 + x % PER * 8, high[i], low[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int x = i * NT_THREADS + threadIdx.x;
+    const float *const p = values + nt_value(all ? x / PER : 0, x % PER * 8, pitch);
+#pragma unroll
+    for (int y = 0; y < 8; ++y) v[i][y] = p[y];
+  }
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int x = i * NT_THREADS + threadIdx.x, r = x / PER, c = x % PER * 8;
+    if (!all) break;
+    ortho_rows8(g, ws, row_of(r), col0 + c, high[i], low[i], v[i]);
     float *const p = values + nt_value(r, c, pitch);
-    float v[8];
 #pragma unroll
-    for (int y = 0; y < 8; ++y) v[y] = p[y];
-    ortho_rows8(g, ws, row_of(r), col0 + c, v);
-#pragma unroll
-    for (int y = 0; y < 8; ++y) p[y] = v[y];
+    for (int y = 0; y < 8; ++y) p[y] = v[i][y];
   }
   if (g.y >= 0) {
     __syncthreads();
@@ -234,12 +253,20 @@ __device__ __forceinline__ void ortho_finish(const OrthoProduct &g, char *ws, fl
     }
   } else if (mirror) {
     __syncthreads();
-    for (int x = threadIdx.x; x < ROWS / 8 * TN; x += NT_THREADS) {
-      const int r = x % (ROWS / 8) * 8, c = x / (ROWS / 8);
-      float v[8];
+    constexpr int M = (ROWS / 8 * TN + NT_THREADS - 1) / NT_THREADS;
+    const bool some = ROWS / 8 * TN % NT_THREADS == 0 || (int)threadIdx.x < ROWS / 8 * TN;
+    float u[M][8];
 #pragma unroll
-      for (int y = 0; y < 8; ++y) v[y] = values[nt_value(r + y, c, pitch)];
-      ortho_cols8(g, ws, row_of(r), col0 + c, v);
+    for (int i = 0; i < M; ++i) {
+      const int x = i * NT_THREADS + threadIdx.x, r = some ? x % (ROWS / 8) * 8 : 0, c = some ? x / (ROWS / 8) : 0;
+#pragma unroll
+      for (int y = 0; y < 8; ++y) u[i][y] = values[nt_value(r + y, c, pitch)];
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < M; ++i) {
+      const int x = i * NT_THREADS + threadIdx.x;
+      if (some) ortho_cols8(g, ws, row_of(x % (ROWS / 8) * 8), col0 + x / (ROWS / 8), u[i]);
     }
   }
 }
