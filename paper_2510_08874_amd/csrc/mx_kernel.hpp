@@ -23,8 +23,8 @@ __device__ __forceinline__ unsigned short mx_bf16(float v) { return __builtin_bi
 
 // fp32: half a wave stores 32 neighbouring columns of a row.  bf16: the halves of a wave exchange two tiles of 32 columns, so that all lanes
 // have neighbouring columns of the same two rows, and lanes of an even and an odd column halves of these: a wave stores 64 columns of
-// two rows, whole lines.  Straight from the registers; by way of LDS, 64 rows at a time and 16 bytes a thread, the end of a tile took 11800 cycles
-// (19000 with one read of LDS after the other).  Addresses are a row's, the same for the wave, and a lane's, the same for
+// two rows, whole lines.  Straight from the registers, 9300 cycles; by way of LDS, 64 rows at a time and 16 bytes a thread, the end of a tile took
+// 11800 (19000 with one read of LDS after the other), half lines as many as whole ones but a layer's step 2 % more.  Addresses are a row's, the same for the wave, and a lane's, the same for
 // all rows.  INSIDE: the whole macro-tile is.  (The host sees to it that a macro-tile's rows lie within 2^32 bytes.)
 template <class SH, bool F32, bool INSIDE>
 __device__ __forceinline__ void mx_store(const NtTile<SH> &tile, const MxItem &it) {

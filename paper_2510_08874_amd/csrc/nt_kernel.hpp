@@ -17,11 +17,11 @@
 // again in the second half, a quarter before another barrier waits for the step behind it, so that loads of two steps overlap.  Pairs,
 // with half as much to load a cycle: fragments of a half are read during the half before it, one barrier a step.
 // fp4, 4096 x 4096 x 4096: 2600 cycles a step with 187 instructions besides the matrix instructions.  Before, with 350 of them and one barrier in front of the
-// last quarter, 2900, of which matrix instructions and LDS reads alone took 2640, matrix instructions alone 2150.  A tile's ends come on top: 3
-// us until the first step has landed, and 256 KB of fp32 from every CU at the same time take 11 us.
+// last quarter, 2900, of which matrix instructions and LDS reads alone took 2640, matrix instructions alone 2150.  A tile's ends come on top: 6300
+// cycles until the first step has landed, 9300 to store 128 KB of bf16, 19000 for 256 KB of fp32 from every CU at the same time (7 TB/s).
 // The part lowers its clock under matrix load: a loop of matrix instructions on registers alone makes 6.5 PFLOP/s in fp4
 // and 1.8 in fp16 with random operands (9.7 and 2.5 with zeros), and a kernel that also moves operands has less power left for it
-// (1.6 to 1.7 GHz in fp4, 1.58 with pairs, whose pipes are busy 83 % of the time).
+// (1.56 GHz in fp4, pipes busy 63 % of the time; 1.52 with pairs, 85 %).
 #pragma once
 
 #include <hip/hip_runtime.h>
