@@ -256,6 +256,22 @@ def test_product_on_large_macro_tiles():
     assert (np.abs(gather(c, block(m, n, 2, 2)) - A @ B) <= limit(A, B, "f32", k)).all()
 
 
+def test_large_macro_tiles_over_many_runs_of_k():
+    """Runs of K of one chunk and more, odd numbers of them, in tiles of 256 x 256; both types of C."""
+    m, k, n = 4093, 4100, 4091
+    da = workloads.desc(m, k, [0, 2048, m], [0, 128, 128, 512, k], 2, 4)
+    db = workloads.desc(k, n, [0, 256, 384, 1664, k], [0, 2048, n], 4, 2)
+    dc = workloads.desc(m, n, [0, 2048, m], [0, 2048, n], 2, 2)
+    for c_dtype in ("f32", "bf16"):
+        c, A, B = multiply(da, db, dc, 12, c_dtype=c_dtype, seed=19)
+        for r in range(0, m, 1024):                           # (on the device: 64-bit products of this size take the host a while)
+            a, b = (torch.from_numpy(x).cuda() for x in (A[r:r + 1024], B))
+            want, far = a @ b, k * 2.0 ** -24 * (a.abs() @ b.abs())
+            if c_dtype == "bf16":
+                far = far + 2.0 ** -8 * (want.abs() + far)
+            assert ((torch.from_numpy(gather(c, dc)[r:r + 1024]).cuda() - want).abs() <= far).all()
+
+
 def uneven(m, k, n):
     return (workloads.desc(m, k, [0, m // 5, m // 2, m], [0, 128, 128, 512, k], 3, 4), workloads.desc(k, n, [0, 256, 384, k], [0, n // 3, n], 3, 2),
             workloads.desc(m, n, [0, m // 7, m // 3, m - 1, m], [0, 0, n // 2, n], 4, 3))
