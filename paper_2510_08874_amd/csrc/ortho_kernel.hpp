@@ -452,17 +452,22 @@ __global__ __launch_bounds__(ORTHO_SMALL_THREADS) void ortho_small_kernel(OrthoS
       for (int x = 0; x < 8; ++x) out.p[j][x] = ortho_split(v[j][2 * x], v[j][2 * x + 1]);
     return out;
   };
+  // Lanes of an even and an odd column exchange halves of two rows, so that each stores two columns of one of them.
   auto put_rows = [&](unsigned area, const Pairs &v) {
-    const unsigned base = area + ortho_area(row0 + 4 * g, col0 + r);
+    const unsigned base = area + ortho_area(row0 + 4 * g + (r & 1), col0 + (r & 30)), pick = r & 1 ? 0x07060302 : 0x01000504;
+    auto turned = [&](ortho_h2 h) {
+      const unsigned own = __builtin_bit_cast(unsigned, h);
+      return __builtin_amdgcn_perm(own, (unsigned)__builtin_amdgcn_mov_dpp((int)own, 0xB1, 0xF, 0xF, true), pick);   // lane ^ 1
+    };
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
-      for (int x = 0; x < 16; ++x) {
+      for (int x = 0; x < 16; x += 2) {
         const OrthoPairs &p = v.p[j][x / 2];
         const int row = 8 * (x / 4) + x % 4, turn = ((row & 15) ^ (8 * j)) << 4;   // (32 columns on are 8 slots on)
-        *(__attribute__((address_space(3))) _Float16 *)((nt_lptr)(uintptr_t)(base ^ turn) + row * (ORTHO_SMALL * 4)) = p.high[x % 2];
-        *(__attribute__((address_space(3))) _Float16 *)((nt_lptr)(uintptr_t)(base ^ turn ^ 64) + row * (ORTHO_SMALL * 4)) = p.low[x % 2];
-        if (x % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+        *(__attribute__((address_space(3))) unsigned *)((nt_lptr)(uintptr_t)(base ^ turn) + row * (ORTHO_SMALL * 4)) = turned(p.high);
+        *(__attribute__((address_space(3))) unsigned *)((nt_lptr)(uintptr_t)(base ^ turn ^ 64) + row * (ORTHO_SMALL * 4)) = turned(p.low);
+        if (x % 4 == 2) __builtin_amdgcn_sched_barrier(0);
       }
   };
   // (the transpose; four neighbouring rows of a column at a time)
