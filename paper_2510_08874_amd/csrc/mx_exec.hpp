@@ -144,9 +144,9 @@ struct MxChoice {
 };
 
 // By an estimate in us.  A step (256 of k) of a tile costs its matrix instructions, or what L2 takes with many tiles at a time; few rows
-// wait for B from memory.  Measured on tiles alone: 256 x 256 1.25 to 1.78 a step (64 and 256 of them), 128 x 128 0.53 to 0.66
-// (36, 256), two on a CU 1.13; 32 rows against 117 MB of B 4.6 TB/s.  A tile cut along K costs its partial sums
-// and a launch that adds them up.
+// wait for B from memory.  Measured as what more of K costs: 256 x 256 1.4 to 2.0 a step with all CUs at it (random codes more than normal
+// data: power), 128 x 128 0.54 to 0.66 (64, 256 of them), two on a CU 1.1 to 1.4, 64 x 128 and 32 x 128 0.5 to 0.6; 32 rows against
+// 117 MB of B 4.6 TB/s.  A tile cut along K costs its partial sums and a launch that adds them up.
 MxChoice choose_mx(const dmm_plan_t *P, int cus) {
   int64_t most = 0;                    // rows of a group
   double cells = 0, k_steps = 0, b_bytes = 0;

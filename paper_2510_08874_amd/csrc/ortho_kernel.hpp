@@ -370,8 +370,8 @@ __global__ __launch_bounds__(256) void ortho_join_kernel(const OrthoProduct g) {
 // X stays in registers in fp32, eight waves of 32 x 64 elements each; what a product reads goes through LDS as pairs, two areas of
 // 128 rows: X by rows, then by columns, and S, then P.  Five barriers a step, no memory traffic between the first load and the
 // last store.  Bound by one CU: 3 x 384 matrix instructions of 32 cycles a step on its four pipes (9200 cycles), with LDS reads that
-// take as long (6 KB for every six of a wave); taking values apart and storing them between the barriers is the other half of 18000 cycles
-// a step, 43 us a call of five.  In launches of the products above every one of the 18 took 8 to 15 us: 32 matrices of 128 x 128 200 us.
+// take as long (6 KB for every six of a wave); taking values apart and storing them between the barriers is the other half of 17000 cycles
+// a step, 41.6 us a call of five.  In launches of the products above every one of the 18 took 8 to 15 us: 32 matrices of 128 x 128 200 us.
 constexpr int ORTHO_SMALL_THREADS = 512;
 constexpr int ORTHO_AREA = ORTHO_SMALL * ORTHO_SMALL * 4;    // bytes
 
