@@ -44,8 +44,8 @@ typedef enum {
   DMM_ELD = -6,    /* a leading dimension is smaller than the tile's width, or a row pitch (leading
                       dimension times element size) of an A, B or C tile is 2^24 bytes or more */
   DMM_ELIMIT = -7  /* dmm_reduce_replicas_static: the work tables of this call do not fit the library's
-                      static device buffer (DMM_STATIC_SCRATCH_BYTES); dmm_mx_*, dmm_orthogonalize: more
-                      than 2^30 workgroups or table entries, a workspace that is too small */
+                      static device buffer (DMM_STATIC_SCRATCH_BYTES); dmm_mx_*, dmm_orthogonalize: 2^24
+                      workgroups in a launch, 2^30 table entries, a workspace that is too small */
 } dmm_status;
 
 /* Element type of the A and B tiles.  All partial sums are fp32, and so are the C tiles unless
@@ -318,7 +318,8 @@ int dmm_mx_dequantize(const dmm_matrix_desc *X, const dmm_mx_tiles *q, int along
 
 /* dmm_execute for 4-bit operands: C = A B (overwrite) on a plan, A along its rows, B along its columns.
  *   a, b      tables in the order of the plan's A and B
- *   c_tiles   fp32 tiles (bf16 with DMM_C_BF16: C with one replica only), every element written once
+ *   c_tiles   fp32 tiles (bf16 with DMM_C_BF16: C with one replica only), every element written once; rows lie
+ *             less than 2^24 bytes apart (DMM_ELD)
  *   flags     0 or any of DMM_NO_REDUCE, DMM_C_BF16
  * Scales are applied by the matrix instructions, sums are fp32.  Blocks of A and of B must meet: every op's k range has
  * to start at a multiple of DMM_MX_CHUNK inside its A tile and inside its B tile (DMM_EINVAL otherwise), which is so
@@ -328,8 +329,8 @@ int dmm_mx_dequantize(const dmm_matrix_desc *X, const dmm_mx_tiles *q, int along
  * Replicas of C, streams and ownership as for dmm_execute: replica 0 receives the sum unless DMM_NO_REDUCE, the call
  * is asynchronous, the first call on a plan takes its work table (and, if needed, that scratch buffer) from a pool, later calls
  * with the same arguments allocate nothing.  The plan's tables and scratch buffer serve all its calls: one that is to be
- * captured is made once before (DMM_EINVAL otherwise), and while the graph is in use the plan is called with those arguments only, in stream order
- * with the graph's launches.  dmm_plan_last_execute, dmm_plan_last_kernels and the elapsed times do not speak of these calls. */
+ * captured is made once before (DMM_EINVAL otherwise; on any stream), and while the graph is in use the plan is called with
+ * those arguments only, in stream order with the graph's launches.  dmm_plan_last_execute, dmm_plan_last_kernels and the elapsed times do not speak of these calls. */
 int dmm_mx_execute(dmm_plan_t *p, const dmm_mx_tiles *a, const dmm_mx_tiles *b, void *const *c_tiles, const int64_t *c_ld,
                    uint32_t flags, void *hip_stream);
 

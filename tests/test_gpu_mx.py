@@ -617,3 +617,28 @@ def test_a_weight_is_trained():
     values = TileSet(dw, torch.bfloat16)
     mx[W, "cols"].write_values(values)
     assert np.array_equal(values.gather().astype(np.float64), along(w, dw, "cols"))
+
+
+@pytest.mark.parametrize("mode", ["global", "thread_local"])
+def test_captured_on_another_stream_than_called_before(mode):
+    m, k, n = 100, 9000, 70                                  # (cut along K)
+    (a, A), (b, B) = made(m, k, 1, 41), made(k, n, 2, 42)
+    plan = binding.Plan(whole(m, k), whole(k, n), whole(m, n), 1)
+    out = torch.zeros(m, n, device="cuda")
+    ta, tb, tc = a.table(), b.table(), binding.tile_table([out], [n])
+    first, side = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    plan.execute_mx(ta, tb, tc, 0, first.cuda_stream)
+    torch.cuda.synchronize()
+    want = out.clone()
+    check_product(want, A, B, "f32")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side, capture_error_mode=mode):
+        plan.execute_mx(ta, tb, tc, 0, side.cuda_stream)
+    for _ in range(3):
+        out.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+    del graph
