@@ -329,7 +329,7 @@ int dmm_mx_dequantize(const dmm_matrix_desc *X, const dmm_mx_tiles *q, int along
  * Replicas of C, streams and ownership as for dmm_execute: replica 0 receives the sum unless DMM_NO_REDUCE, the call
  * is asynchronous, the first call on a plan takes its work table (and, if needed, that scratch buffer) from a pool, later calls
  * with the same arguments allocate nothing.  The plan's tables and scratch buffer serve all its calls: one that is to be
- * captured is made once before (DMM_EINVAL otherwise; on any stream), and while the graph is in use the plan is called with
+ * captured is made once before (DMM_EINVAL otherwise; on any stream, with DMM_NO_REDUCE or without), and while the graph is in use the plan is called with
  * those arguments only, in stream order with the graph's launches.  dmm_plan_last_execute, dmm_plan_last_kernels and the elapsed times do not speak of these calls. */
 int dmm_mx_execute(dmm_plan_t *p, const dmm_mx_tiles *a, const dmm_mx_tiles *b, void *const *c_tiles, const int64_t *c_ld,
                    uint32_t flags, void *hip_stream);

@@ -562,6 +562,7 @@ struct ExecLayout {
 struct MxLayout {
   int shape = 0, n_items = 0, n_joins = 0;
   size_t o_segs = 0, o_joins = 0;
+  RedLaunch red;                // the replica-sum launch behind it (n_items == 0: C has one replica)
 };
 
 // What a plan keeps for dmm_mx_execute: the tables of its last call, the inputs that they were made from, and

@@ -345,7 +345,11 @@ int build_mx(dmm_plan_t *P, const dmm_mx_tiles *a, const dmm_mx_tiles *b, void *
   if (!segs.empty()) std::memcpy(h.data() + L->o_segs, segs.data(), segs.size() * sizeof(NtSeg));
   if (!joins.empty()) std::memcpy(h.data() + L->o_joins, joins.data(), joins.size() * sizeof(MxJoin));
   static_assert(sizeof(MxItem) % 8 == 0 && sizeof(NtSeg) % 8 == 0 && sizeof(MxJoin) % 8 == 0, "tables lie one behind another");
-  return M.table.upload(h.data(), h.size(), stream, P->dev->uses);
+  // those of the sum of C's replicas, also for a call without it: the next one with these arguments may be captured
+  if ((rc = build_reduce(P, c_tiles, c_ld, 0, &h, h.size(), &L->red))) return rc;
+  if ((rc = M.table.upload(h.data(), h.size(), stream, P->dev->uses))) return rc;
+  L->red.dev_base = M.table.dev();
+  return DMM_OK;
 }
 
 }  // namespace
@@ -449,16 +453,14 @@ int dmm_mx_execute(dmm_plan_t *P, const dmm_mx_tiles *a, const dmm_mx_tiles *b, 
     }
     const MxLayout &L = M.layout;
     if (L.n_items == 0) return DMM_OK;
-    RedLaunch red;
-    const bool sum = P->C.c > 1 && !(flags & DMM_NO_REDUCE);
-    if (sum && (rc = stage_reduce(P, c_tiles, c_ld, 0, stream, &red))) return rc;
+    const bool sum = L.red.n_items && !(flags & DMM_NO_REDUCE);
     hipEvent_t behind = nullptr;
     if ((rc = P->dev->uses.claim(stream, &behind))) return rc;
     const char *d = M.table.dev();
-    bool marked = mx_launch(red.n_items ? nullptr : behind, L.shape, (const MxItem *)d, L.n_items, (const NtSeg *)(d + L.o_segs),
+    bool marked = mx_launch(sum ? nullptr : behind, L.shape, (const MxItem *)d, L.n_items, (const NtSeg *)(d + L.o_segs),
                             (const MxJoin *)(d + L.o_joins), L.n_joins, cus, stream);
     DMM_HIP(hipGetLastError());
-    if (red.n_items && (rc = fire_reduce(P, red, stream, false, behind, &marked))) return rc;
+    if (sum && (rc = fire_reduce(P, L.red, stream, false, behind, &marked))) return rc;
     return marked ? DMM_OK : P->dev->uses.mark(stream);
   } catch (const std::bad_alloc &) {
     return DMM_ENOMEM;

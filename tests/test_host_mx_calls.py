@@ -1,0 +1,91 @@
+"""What `dmm_mx_execute` and the other entry points for 4-bit matrices and orthogonalised updates enqueue, without a
+GPU: scenarios on the stand-in for the HIP runtime, as in test_host_calls.py, every one in a process of its own."""
+import os
+import subprocess
+import sys
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+if ROOT not in sys.path:
+    sys.path.insert(0, ROOT)
+
+import workloads  # noqa: E402
+from tests.test_host_calls import Recorder, recorder, tables  # noqa: E402, F401
+
+
+# ---- inside the scenario's process --------------------------------------------------------------------
+
+def whole(h, w, replication=1):
+    return workloads.desc(h, w, [0, h], [0, w], 1, 1, replication=replication)
+
+
+def form(d, along, base):
+    """Made-up addresses of a matrix in 4 bits."""
+    from paper_2510_08874_amd import binding
+    codes, scales, cld, sld = [], [], [], []
+    for _ in range(d["replication"]):
+        for r0, r1 in zip(d["row_cuts"], d["row_cuts"][1:]):
+            for c0, c1 in zip(d["col_cuts"], d["col_cuts"][1:]):
+                h, w = (r1 - r0, c1 - c0) if along == 1 else (c1 - c0, r1 - r0)
+                chunks = -(-w // 128)
+                codes.append(base)
+                scales.append(base + h * 64 * chunks)
+                cld.append(64 * chunks)
+                sld.append(4 * chunks)
+                base += -(-h * 68 * chunks // 512) * 512 + 512
+    return binding.mx_tiles(codes, cld, scales, sld)
+
+
+class MxProduct:
+    """A plan and made-up 4-bit operands; outputs by `where`."""
+
+    def __init__(self, descs, nranks, flags=0):
+        from paper_2510_08874_amd import binding
+        self.b, self.descs, self.plan = binding, descs, binding.Plan(*descs, nranks, flags)
+        self.a, self.bt = form(descs[0], 1, 1 << 44), form(descs[1], 2, 3 << 43)
+
+    def c(self, where=0):
+        return tables(self.descs[2], (1 << 45) + (where << 40), 4)
+
+    def run(self, where=0, flags=0, stream=0):
+        self.plan.execute_mx(self.a, self.bt, self.b.tile_table(*self.c(where)), flags, stream)
+
+
+def replicated(m=500, k=1024, n=300):
+    block = workloads.block_desc
+    return MxProduct(tuple(block(r, c, 2, 2, replication=2) for r, c in ((m, k), (k, n), (m, n))), 8)
+
+
+def a_replicated_product_is_captured_after_other_calls(rec):
+    """The sum of C's replicas has its tables on the device with those of the product, whatever the plan did with replicas
+    before: a call that did not sum, sums and copies of other replicas.  While a stream is captured nothing is copied and no
+    memory is taken."""
+    p, s, other = replicated(), rec.stream(), rec.stream()
+    before = (lambda: p.run(0, p.b.DMM_NO_REDUCE, other), lambda: p.run(0, 0, s), lambda: p.plan.reduce_replicas(*p.c(3), 1, other),
+              lambda: p.plan.broadcast_replica(*p.c(0), 1, s))
+    for call in before:
+        call()
+        rec.so.rec_set_capturing(s, 1)
+        for flags, kernels in ((0, ["mx_gemm_kernel", "reduce_replicas_kernel"]), (p.b.DMM_NO_REDUCE, ["mx_gemm_kernel"])):
+            at, live = len(rec.ops()), rec.so.rec_live()
+            p.run(0, flags, s)
+            assert [o[1] for o in rec.ops(at) if o[1] != "event"] == kernels
+            assert rec.so.rec_live() == live
+        rec.so.rec_set_capturing(s, 0)
+        rec.check_tables()
+
+
+SCENARIOS = [a_replicated_product_is_captured_after_other_calls]
+
+
+# ---- the tests ----------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("scenario", [f.__name__ for f in SCENARIOS])
+def test_scenario(recorder, scenario):  # noqa: F811
+    run = subprocess.run([sys.executable, os.path.abspath(__file__), recorder, scenario], capture_output=True, text=True, cwd=ROOT, timeout=300)
+    assert run.returncode == 0, run.stdout[-2000:] + run.stderr[-4000:]
+
+
+if __name__ == "__main__":
+    {f.__name__: f for f in SCENARIOS}[sys.argv[2]](Recorder(sys.argv[1]))
