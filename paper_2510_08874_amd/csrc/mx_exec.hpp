@@ -72,6 +72,23 @@ int over_tiles(const Grid &G, int es, char *const *x, const int64_t *x_ld, const
     for (int32_t tj = 0; tj < G.gc; ++tj) units += G.c * (G.rc[ti + 1] - G.rc[ti]) * ((G.cc[tj + 1] - G.cc[tj] + 511) / 512);
   const int per = mx_rows_per_unit(units);
   const int along = (rows ? MX_ALONG_ROWS : 0) | (cols ? MX_ALONG_COLS : 0);
+  // workgroups of a tile, and how many of them side by side
+  auto blocks_of = [&](int64_t h, int64_t w, int32_t *across) -> int64_t {
+    if (along == MX_ALONG_ROWS) {
+      *across = (int32_t)((w + 511) / 512);
+      return ((h + per - 1) / per * *across + 3) / 4;
+    }
+    // (with the rows too, down to the end of the last chunk)
+    const int64_t cols = mx_block_cols(es == 4), wide = rows ? (w + 127) / 128 * 128 : w;
+    *across = (int32_t)((wide + cols - 1) / cols);
+    return (h + 127) / 128 * *across;
+  };
+  // (all tiles before the first launch: a call that is refused writes nothing)
+  for (int32_t ti = 0; ti < G.gr; ++ti)
+    for (int32_t tj = 0; tj < G.gc; ++tj) {
+      int32_t across;
+      if (blocks_of(G.rc[ti + 1] - G.rc[ti], G.cc[tj + 1] - G.cc[tj], &across) > kMxBlocks) return DMM_ELIMIT;
+    }
   MxTileArgs args;
   std::memset(&args, 0, sizeof args);
   int64_t blocks = 0;
@@ -107,17 +124,7 @@ int over_tiles(const Grid &G, int es, char *const *x, const int64_t *x_ld, const
         }
         t.h = (int32_t)h;
         t.w = (int32_t)w;
-        int64_t n;
-        if (along == MX_ALONG_ROWS) {
-          t.blocks_across = (int32_t)((w + 511) / 512);
-          n = ((h + per - 1) / per * t.blocks_across + 3) / 4;
-        } else {
-          // (with the rows too, down to the end of the last chunk)
-          const int64_t cols = mx_block_cols(es == 4), wide = rows ? (w + 127) / 128 * 128 : w;
-          t.blocks_across = (int32_t)((wide + cols - 1) / cols);
-          n = (h + 127) / 128 * t.blocks_across;
-        }
-        if (n > kMxBlocks) return DMM_ELIMIT;
+        const int64_t n = blocks_of(h, w, &t.blocks_across);
         int rc;
         if ((args.n == MX_TILES || blocks + n > kMxBlocks) && (rc = flush())) return rc;
         t.first_block = (int32_t)blocks;

@@ -76,7 +76,23 @@ def a_replicated_product_is_captured_after_other_calls(rec):
         rec.check_tables()
 
 
-SCENARIOS = [a_replicated_product_is_captured_after_other_calls]
+def a_refused_quantisation_launches_nothing(rec):
+    """A tile with too many workgroups for a launch behind tiles that would have been launched: no output is touched."""
+    from paper_2510_08874_amd import binding as b
+    high = workloads.desc((1 << 29) + 4000, 8, [i * 100 for i in range(41)] + [(1 << 29) + 4000], [0, 8], 41, 1)
+    wide = workloads.desc(600, 1 << 30, [0, 300, 600], [0, 8, 1 << 30], 2, 2)
+    for d, along in ((high, 1), (wide, 2)):
+        desc, q, t = b.matrix_desc(d), form(d, along, 1 << 44), b.tile_table(*tables(d, 1 << 45, 2))
+        for call in (lambda: b.dmm_mx_quantize(desc, 1, t, **{("rows", "cols")[along - 1]: q}), lambda: b.dmm_mx_dequantize(desc, q, along, 1, t)):
+            try:
+                call()
+                assert False, "not refused"
+            except b.DmmError as e:
+                assert e.kind == "ELIMIT"
+            assert not rec.ops()
+
+
+SCENARIOS = [a_replicated_product_is_captured_after_other_calls, a_refused_quantisation_launches_nothing]
 
 
 # ---- the tests ----------------------------------------------------------------------------------------
