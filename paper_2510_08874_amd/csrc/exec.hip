@@ -1619,11 +1619,11 @@ int dmm_execute(dmm_plan_t *P, int dtype, const void *const *a_tiles, const int6
   // multiply of (row, pitch): every row pitch has to stay below 2^24 bytes
   constexpr int64_t MAX_PITCH = (int64_t)1 << 24;
   for (int64_t i = 0; i < P->A.c * P->A.tiles_per_rep(); ++i)
-    if (a_ld[i] * es >= MAX_PITCH) return DMM_ELD;
+    if (a_ld[i] >= MAX_PITCH / es) return DMM_ELD;
   for (int64_t i = 0; i < P->B.c * P->B.tiles_per_rep(); ++i)
-    if (b_ld[i] * es >= MAX_PITCH) return DMM_ELD;
+    if (b_ld[i] >= MAX_PITCH / es) return DMM_ELD;
   for (int64_t i = 0; i < P->C.c * P->C.tiles_per_rep(); ++i)
-    if (c_ld[i] * c_es >= MAX_PITCH) return DMM_ELD;
+    if (c_ld[i] >= MAX_PITCH / c_es) return DMM_ELD;
   hipStream_t stream = (hipStream_t)hip_stream;
   TraceRange whole("dmm_execute");
   try {

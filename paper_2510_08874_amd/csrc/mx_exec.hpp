@@ -417,7 +417,7 @@ int dmm_mx_execute(dmm_plan_t *P, const dmm_mx_tiles *a, const dmm_mx_tiles *b, 
       (rc = check_tiles(P->C, c_tiles, c_es)))
     return rc;
   for (int64_t i = 0; i < P->C.c * P->C.tiles_per_rep(); ++i)
-    if (c_ld[i] * c_es >= (int64_t)1 << 24) return DMM_ELD;
+    if (c_ld[i] >= ((int64_t)1 << 24) / c_es) return DMM_ELD;
   hipStream_t stream = (hipStream_t)hip_stream;
   TraceRange whole("dmm_mx_execute");
   try {

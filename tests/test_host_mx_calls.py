@@ -103,5 +103,25 @@ def test_scenario(recorder, scenario):  # noqa: F811
     assert run.returncode == 0, run.stdout[-2000:] + run.stderr[-4000:]
 
 
+@pytest.mark.parametrize("ld", [1 << 22, 1 << 61, (1 << 62) + 77, (1 << 63) - 1], ids=str)
+def test_rows_that_lie_too_far_apart_are_refused(ld):
+    """2^24 bytes and more, also where the bytes would pass 64 bits."""
+    from paper_2510_08874_amd import binding as b
+    d = whole(130, 300), whole(300, 77), whole(130, 77)
+    plan, at = b.Plan(*d, 1), 3 << 40
+    for flags in (0, b.DMM_C_BF16):
+        if ld == 1 << 22 and flags:
+            continue                                          # (2^23 bytes are none too many)
+        with pytest.raises(b.DmmError) as e:
+            plan.execute_mx(form(d[0], 1, 1 << 44), form(d[1], 2, 3 << 43), b.tile_table([at], [ld]), flags)
+        assert e.value.kind == "ELD"
+    for x in range(3):
+        lds = [300, 77, 77]
+        lds[x] = ld
+        with pytest.raises(b.DmmError) as e:
+            plan.execute(b.DMM_F32, [at], [lds[0]], [at], [lds[1]], [at], [lds[2]])
+        assert e.value.kind == "ELD"
+
+
 if __name__ == "__main__":
     {f.__name__: f for f in SCENARIOS}[sys.argv[2]](Recorder(sys.argv[1]))
