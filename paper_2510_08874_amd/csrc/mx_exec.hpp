@@ -152,11 +152,20 @@ struct MxChoice {
 
 // By an estimate in us.  A step (256 of k) of a tile costs its matrix instructions, or what L2 takes with many tiles at a time; few rows
 // wait for B from memory.  Measured as what more of K costs: 256 x 256 1.4 to 2.0 a step with all CUs at it (random codes more than normal
-// data: power), 128 x 128 0.54 to 0.66 (64, 256 of them), two on a CU 1.1 to 1.4, 64 x 128 and 32 x 128 0.5 to 0.6; 32 rows against
-// 117 MB of B 4.6 TB/s.  A tile cut along K costs its partial sums and a launch that adds them up.
+// data: power), 128 x 128 0.54 to 0.66 (64, 256 of them), two on a CU 1.1 to 1.4; 64 x 128 0.5 (112) and 0.55 (224) of B that a cache holds, 0.8 and
+// 0.95 of B from memory, with two stages; 32 x 128 with three 0.35, 0.5; 0.55, 0.75; two of them on a CU 1.0 to 1.2.  Nothing is faster than memory: 570 MB of
+// B take 32 rows 113 us, 64 130, 128 131, 256 149; 125 MB 27, 34, 30, 50 (so up to 32 rows the tile of 32 is the best everywhere, from
+// 33 to 64 that of 64 but where there is one tile on almost every CU and K is long: 64 x 4096 x 14336 16.7, 128 rows 17.2; x 28000 20.9 and 18.8).  A tile cut
+// along K costs its partial sums and a launch that adds them up.  Of equal estimates the smaller tile's.
 MxChoice choose_mx(const dmm_plan_t *P, int cus) {
   int64_t most = 0;                    // rows of a group
-  double cells = 0, k_steps = 0, b_bytes = 0;
+  double cells = 0, k_steps = 0, b_bytes = 0, b_once = 0;
+  struct Columns {
+    int32_t rep;
+    int64_t n0;
+    double bytes;
+  };
+  std::vector<Columns> columns;        // of B, for every group that reads them
   for (size_t x = 0; x < P->groups.size(); ++x) {
     const Group &g = P->groups[x];
     most = std::max(most, g.m1 - g.m0);
@@ -165,15 +174,20 @@ MxChoice choose_mx(const dmm_plan_t *P, int cus) {
       const dmm_task &t = P->tasks[(size_t)P->order[(size_t)y]];
       steps += (t.k1 - t.k0 + 255) / 256;
     }
-    const double area = (double)(g.m1 - g.m0) * (double)(g.n1 - g.n0);
+    const double area = (double)(g.m1 - g.m0) * (double)(g.n1 - g.n0), bytes = (double)(g.n1 - g.n0) * (double)steps * 136.0;
     cells += area;
     k_steps += area * (double)steps;
-    b_bytes += (double)(g.n1 - g.n0) * (double)steps * 136.0;
+    b_bytes += bytes;
+    columns.push_back({g.c_rep, g.n0, bytes});
   }
+  std::sort(columns.begin(), columns.end(), [](const Columns &a, const Columns &b) { return a.rep != b.rep ? a.rep < b.rep : a.n0 < b.n0; });
+  for (size_t x = 0; x < columns.size(); ++x)
+    if (!x || columns[x].rep != columns[x - 1].rep || columns[x].n0 != columns[x - 1].n0) b_once += columns[x].bytes;
   const double steps = cells > 0 ? k_steps / cells : 0;
+  const double cold = b_bytes > 0 ? b_once / b_bytes : 0;   // of what is read of B, the part that comes from memory
   MxChoice best;
   double best_us = 0;
-  for (int shape = 0; shape < MX_SHAPES; ++shape) {
+  for (const int shape : {MX_SKINNY, MX_32, MX_64, MX_128, MX_256}) {
     const int tm = kMxShape[shape].tm, tn = kMxShape[shape].tn;
     if ((shape == MX_SKINNY && most > 32) || (shape == MX_32 && most > tm) || (shape == MX_64 && most > tm)) continue;
     double tiles = 0;
@@ -181,13 +195,15 @@ MxChoice choose_mx(const dmm_plan_t *P, int cus) {
     if (tiles == 0) return best;
     if (tiles > (double)kMxBlocks) continue;
     if (shape == MX_SKINNY) {
-      // (every eighth pair of chunks is a wave's next; 16 rows of A are read with every 16 columns of B, and B again with 16 more rows)
-      const double us = 2.5 + std::max(0.8 * std::ceil(steps / 8) * std::ceil(tiles / (8.0 * cus)),
+      // (every eighth pair of chunks is a wave's next; 16 rows of A are read with every 16 columns of B, and B again with 16 more rows.  Workgroups on
+      // one CU share its first cache, which takes 0.8 to 1.3 us for eight steps of each: 128 x 47936 x 532 on 8 blocks of rows, 360 tiles, 62 us)
+      const double us = 2.5 + std::max((most <= 2 ? 0.8 : 1.2) * std::ceil(steps / 8) * std::ceil(tiles / cus),
                                        b_bytes / (most <= 2 ? 4.6e6 : 3.0e6) + (double)((most - 1) / 16) * b_bytes / 8e6);
       if (best_us == 0 || us < best_us) best_us = us, best.shape = shape, best.runs = 1;
       continue;
     }
     const int places = shape == MX_256 ? cus : 2 * cus;
+    const double memory = 2.0 + b_once / (shape == MX_32 ? 5.0e6 : 4.4e6);
     for (int64_t runs = 1; runs <= 32; ++runs) {
       const double work = tiles * (double)runs, per = std::ceil(steps / (double)runs);
       if (runs > 1 && (work > places || per < 3)) break;
@@ -198,12 +214,12 @@ MxChoice choose_mx(const dmm_plan_t *P, int cus) {
         switch (shape) {
           case MX_256: return per * (1.2 + 0.55 * full) + 8.0;
           case MX_128: return per * (full > 1 ? 1.13 : 0.5 + 0.16 * full) + 4.5;
-          default: return per * (full > 1 ? 0.75 : 0.45) + 3.5;
+          case MX_64: return per * (full > 1 ? 1.15 : 0.33 + (0.25 + 0.37 * cold) * full) + 3.5;
+          default: return per * (full > 1 ? 1.05 : 0.3 + (0.22 + 0.28 * cold) * full) + 3.5;
         }
       };
       const double whole = std::floor(work / places);
-      double us = whole * round(places) + round(work - whole * places);
-      if (shape >= MX_64) us = std::max(us, b_bytes / 4.6e6);
+      double us = std::max(whole * round(places) + round(work - whole * places), memory);
       if (runs > 1) us += 4.5 + 2.0 * work * tm * tn * 4 / 3e6;
       if (best_us == 0 || us < best_us) best_us = us, best.shape = shape, best.runs = runs;
     }

@@ -126,10 +126,10 @@ __global__ __launch_bounds__(256) void mx_join_kernel(const MxJoin *__restrict__
     }
 }
 
-// Up to 16 rows against little B: every wave reads B straight into registers.  A workgroup owns 16 columns; its four waves take
-// every fourth 512 elements of K each and add up through LDS, so that there are enough waves on the way to memory without partial
-// sums in memory.  (1 x 4096 x 4096 4.6 us where tiles of 32 x 128 cut along K take 5.9 and the sum of their runs; B
-// of 117 MB that no cache holds at 4.0 TB/s with one row, 2.9 with 16, the tiles at 4.5 to 4.9.)
+// Up to 32 rows against little B, 16 a workgroup: every wave reads B straight into registers.  A workgroup owns 16 columns; its four waves
+// take every fourth 512 elements of K each and add up through LDS, so that there are enough waves on the way to memory without partial
+// sums in memory.  (Calls one after another, bf16: 1 x 4096 x 4096 5.7 us, tiles of 32 x 128 8.5; 1 x 16384 x 2048 9.8, those cut into eight 14.8.  125 MB
+// of B that no cache holds at 4.5 TB/s with one row, 3.2 with 16, the tiles at 4.6.)
 __global__ __launch_bounds__(NT_THREADS) void mx_skinny_kernel(const MxItem *__restrict__ items, const NtSeg *__restrict__ segs) {
   constexpr int Q = 4;                                        // chunks (128 of k) at a time
   __shared__ nt_f32x4 sums[4][64];

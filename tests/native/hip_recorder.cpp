@@ -22,6 +22,7 @@ struct Op {
   uint64_t arg, bytes;          // kernel: first eight bytes of its first argument; copy: destination and size
   uint64_t more[3] = {0, 0, 0}; // pack_kernel: its other arguments; copy: 1 if table_kernel makes it
   unsigned blocks = 0;
+  uint64_t lds = 0;
   std::vector<int> behind;
   int done_at = -1;             // known on the host to have finished before operation number done_at was enqueued
 };
@@ -115,6 +116,7 @@ uint64_t rec_arg(int i) { return ops[(size_t)i].arg; }
 uint64_t rec_bytes(int i) { return ops[(size_t)i].bytes; }
 uint64_t rec_more(int i, int k) { return ops[(size_t)i].more[k]; }
 unsigned rec_blocks(int i) { return ops[(size_t)i].blocks; }
+uint64_t rec_lds(int i) { return ops[(size_t)i].lds; }
 int rec_before(int a, int b) { return before(a, b); }
 uint64_t rec_new_stream() { return (uint64_t)fresh(); }
 void rec_finish_stream(uint64_t s) { finish(streams[(void *)s].last); }
@@ -161,7 +163,7 @@ hipError_t __hipPopCallConfiguration(dim3 *grid, dim3 *block, size_t *lds, hipSt
   *stream = cfg_stream;
   return hipSuccess;
 }
-hipError_t hipLaunchKernel(const void *f, dim3 grid, dim3, void **args, size_t, hipStream_t stream) {
+hipError_t hipLaunchKernel(const void *f, dim3 grid, dim3, void **args, size_t lds, hipStream_t stream) {
   stream = real(stream);
   if (kernels[f] == "table_kernel") {               // (table, where to, words): a copy on the caller's stream
     void *to = *(void **)args[1];
@@ -175,6 +177,7 @@ hipError_t hipLaunchKernel(const void *f, dim3 grid, dim3, void **args, size_t, 
   memcpy(&first, args[0], sizeof first);
   Op &o = ops[(size_t)enqueue(kernels[f], stream, first, 0)];
   o.blocks = grid.x;
+  o.lds = lds;
   if (o.name == "pack_kernel") {                    // (jobs, number of them, runs, tiles)
     o.more[0] = *(int *)args[1];
     memcpy(&o.more[1], args[2], 8);

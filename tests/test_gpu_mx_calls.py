@@ -1,9 +1,9 @@
-"""GPU tests of calls of `dmm_mx_execute` around each other: captures of replicated products."""
+"""GPU tests of calls of `dmm_mx_execute` around each other: captures of replicated products, few rows."""
 import numpy as np
 import pytest
 
 import workloads
-from tests.test_gpu_mx import gather, limit, operand, tiles_of
+from tests.test_gpu_mx import DT, check_product, gather, limit, made, operand, tiles_of, whole
 
 torch = pytest.importorskip("torch")
 binding = pytest.importorskip("paper_2510_08874_amd.binding")
@@ -48,3 +48,25 @@ def test_a_replicated_product_is_captured(mode):
         torch.cuda.synchronize()
         assert np.array_equal(gather(c, d[2], 1), part)
     del graph
+
+
+@pytest.mark.parametrize("c_dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("m,k,n", [(3, 2100, 9001), (31, 1157, 8897), (32, 700, 12865)], ids=str)
+def test_tiles_of_32_rows_are_stored_from_the_registers(m, k, n, c_dtype):
+    """Uncut: whole tiles and such that end inside of 32 columns (one column, the last bf16 by itself), rows at any address; in
+    row blocks, where every one of them has a tile of its own, too."""
+    (a, A), (b, B) = made(m, k, 1, m + n), made(k, n, 2, k + n)
+    flags, stream = binding.DMM_C_BF16 if c_dtype == "bf16" else 0, torch.cuda.current_stream().cuda_stream
+    for offset, ld in ((0, n), (1, n + 2)):
+        buf = torch.full((m * ld + offset,), 7.0, dtype=DT[c_dtype][0], device="cuda")
+        c = buf[offset:].view(m, ld)
+        binding.Plan(whole(m, k), whole(k, n), whole(m, n), 1).execute_mx(a.table(), b.table(), binding.tile_table([c], [ld]), flags, stream)
+        check_product(c[:, :n], A, B, c_dtype)
+        assert (c[:, n:] == 7.0).all() and (buf[:offset] == 7.0).all()
+    cut = [0, m // 2, m]
+    d = workloads.desc(m, k, cut, [0, k], 2, 1), whole(k, n), workloads.desc(m, n, cut, [0, n], 2, 1)
+    rows = [(a.codes[0][r0:r1], a.scales[0][r0:r1]) for r0, r1 in zip(cut, cut[1:])]
+    ta = binding.mx_tiles([x[0] for x in rows], [x[0].shape[1] for x in rows], [x[1] for x in rows], [x[1].shape[1] for x in rows])
+    out, want = torch.full((m, n), 7.0, dtype=DT[c_dtype][0], device="cuda"), c[:, :n]
+    binding.Plan(*d, 2).execute_mx(ta, b.table(), binding.tile_table([out[:m // 2], out[m // 2:]], [n, n]), flags, stream)
+    assert torch.equal(out, want)

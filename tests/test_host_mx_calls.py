@@ -1,5 +1,6 @@
 """What `dmm_mx_execute` and the other entry points for 4-bit matrices and orthogonalised updates enqueue, without a
 GPU: scenarios on the stand-in for the HIP runtime, as in test_host_calls.py, every one in a process of its own."""
+import ctypes
 import os
 import subprocess
 import sys
@@ -92,7 +93,30 @@ def a_refused_quantisation_launches_nothing(rec):
             assert not rec.ops()
 
 
-SCENARIOS = [a_replicated_product_is_captured_after_other_calls, a_refused_quantisation_launches_nothing]
+def few_rows_run_on_tiles_of_few_rows(rec):
+    """Up to 32 rows: the kernel without stages or, against much B, tiles of 32 rows; no estimate is below what it takes to
+    read B.  From 33 to 64 rows tiles of 64 or, with one on almost every CU, of 128."""
+    rec.so.rec_lds.restype = ctypes.c_uint64
+    rows_of = {76800: 32, 61440: 64, 81920: 128, 155648: 128, 163840: 256}    # bytes of LDS: stages and slots of scales
+    for m, k, n, want in ((1, 8192, 28672, 32), (8, 8192, 28672, 32), (32, 8192, 28672, 32), (1, 8192, 131072, 32), (32, 8192, 131072, 32),
+                          (20, 4096, 28000, 32), (32, 640, 20000, 32), (2, 1000, 60000, 32), (32, 12000, 10000, 32), (16, 4096, 14336, 32),
+                          (3, 2100, 9001, 32), (31, 1157, 8897, 32), (32, 700, 12865, 32),
+                          (1, 4096, 4096, 0), (16, 1024, 1024, 0), (2, 16384, 2048, 0),
+                          (64, 8192, 28672, 128), (48, 4096, 28000, 128), (33, 4096, 14336, 64), (64, 4096, 4096, 64), (64, 1024, 28672, 64)):
+        p, at = MxProduct((whole(m, k), whole(k, n), whole(m, n)), 1), len(rec.ops())
+        p.run()
+        first = rec.launches(at)[0]
+        got = 0 if first[1] == "mx_skinny_kernel" else rows_of[rec.so.rec_lds(first[0])]
+        assert got == want, (m, k, n, got, want)
+    # a few rows dealt to row blocks: every block reads all of B, from a cache but once
+    for m in (4, 16, 256):
+        block = workloads.block_desc
+        p, at = MxProduct((block(m, 8192, 8, 1), block(8192, 28672, 1, 8), block(m, 28672, 4, 2)), 8), len(rec.ops())
+        p.run()
+        assert rows_of[rec.so.rec_lds(rec.launches(at)[0][0])] == 32
+
+
+SCENARIOS = [few_rows_run_on_tiles_of_few_rows, a_replicated_product_is_captured_after_other_calls, a_refused_quantisation_launches_nothing]
 
 
 # ---- the tests ----------------------------------------------------------------------------------------
