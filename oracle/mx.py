@@ -52,3 +52,18 @@ def values(code: np.ndarray, scale: np.ndarray, w: int) -> np.ndarray:
     s = np.ldexp(1.0, scale.astype(np.int64) - 127)
     s = np.where(scale == 255, np.nan, s)
     return (v.reshape(*scale.shape, BLOCK) * s[:, :, None]).reshape(v.shape)[:, :w]
+
+
+def sum_limit(A: np.ndarray, B: np.ndarray) -> float:
+    """A bound for the Frobenius norm of the error of A B where every term is exact and sums are fp32: adding term t rounds by
+    at most half a step, 2^-24, of the sum so far.  Roundings of different additions are independent, so that their squares
+    add up.  Sums over ranges of k that are added up afterwards are differences of two sums from k = 0 on: at most
+    twice the largest so far; within a chunk these grow by no more than the magnitudes of its terms."""
+    total, top, S = 0.0, 0.0, np.zeros((A.shape[0], B.shape[1]))
+    for c in range(0, A.shape[1], CHUNK):
+        a, b = A[:, c:c + CHUNK], B[c:c + CHUNK]
+        inside = top + np.linalg.norm(np.abs(a) @ np.abs(b))
+        total += a.shape[1] * (2 * inside) ** 2
+        S = S + a @ b
+        top = max(top, np.linalg.norm(S))
+    return float(2.0 ** -24 * np.sqrt(total))

@@ -116,7 +116,16 @@ def few_rows_run_on_tiles_of_few_rows(rec):
         assert rows_of[rec.so.rec_lds(rec.launches(at)[0][0])] == 32
 
 
-SCENARIOS = [few_rows_run_on_tiles_of_few_rows, a_replicated_product_is_captured_after_other_calls, a_refused_quantisation_launches_nothing]
+def long_sums_are_cut(rec):
+    """The sizes at which sums over ranges of K are tested run in ranges of K."""
+    from tests.test_gpu_mx_sums import CUT, WHOLE
+    for m, k, n in CUT + WHOLE:
+        p, at = MxProduct((whole(m, k), whole(k, n), whole(m, n)), 1), len(rec.ops())
+        p.run()
+        assert ("mx_join_kernel" in [o[1] for o in rec.launches(at)]) == ((m, k, n) in CUT), (m, k, n)
+
+
+SCENARIOS = [long_sums_are_cut, few_rows_run_on_tiles_of_few_rows, a_replicated_product_is_captured_after_other_calls, a_refused_quantisation_launches_nothing]
 
 
 # ---- the tests ----------------------------------------------------------------------------------------
