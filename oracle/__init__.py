@@ -12,7 +12,7 @@ This package is the slow, plain statement of what the path computes:
 * ``mx``       -- the 4-bit microscaled format: codes, scales and values of a
   block from their definition.
 * ``orthogonalize`` -- Newton-Schulz steps in fp64, and a bound for what pairs
-  of fp16 numbers may be off.
+  of fp16 numbers may be off; the same steps as pairs and as fp32 round them.
 * ``execute``  -- runs a task list tile by tile in fp64 (Section 4.2, steps
   1-4 of direct execution) so that the plan's meaning can be checked on the
   CPU without any GPU.

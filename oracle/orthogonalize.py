@@ -66,3 +66,31 @@ def limit(G: np.ndarray, coefficients=DEFAULT) -> float:
         total += slopes[j + 1] * e_x
         X = new
     return float(total)
+
+
+def pair(x: np.ndarray) -> np.ndarray:
+    """Values as pairs of fp16 numbers hold them: x 2^12 = high + low.  22 bits, and no finer than steps of 2^-36."""
+    high = (x * 4096).astype(np.float16).astype(np.float64)
+    return (high + (x * 4096 - high).astype(np.float16)) / 4096
+
+
+def held(G: np.ndarray, hold, coefficients=DEFAULT) -> np.ndarray:
+    """The steps in 64 bits with every matrix on the way as `hold` leaves it: what that rounding by itself does to the result."""
+    X = np.asarray(G, dtype=np.float64)
+    X = hold(X / np.sqrt((X * X).sum()))
+    X = X.T if G.shape[0] > G.shape[1] else X
+    for a, b, c in coefficients:
+        S = hold(X @ X.T)
+        X = hold(a * X + hold(b * S + c * (S @ S)) @ X)
+    return X.T if G.shape[0] > G.shape[1] else X
+
+
+def in_fp32(G: np.ndarray, coefficients=DEFAULT) -> np.ndarray:
+    """The steps in fp32 throughout."""
+    X = np.asarray(G, dtype=np.float64)
+    X = (X / np.sqrt((X * X).sum())).astype(np.float32)
+    X = X.T if G.shape[0] > G.shape[1] else X
+    for a, b, c in np.asarray(coefficients, dtype=np.float32):
+        S = X @ X.T
+        X = a * X + (b * S + c * (S @ S)) @ X
+    return X.T if G.shape[0] > G.shape[1] else X
