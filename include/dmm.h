@@ -311,7 +311,8 @@ typedef struct {
 int dmm_mx_quantize(const dmm_matrix_desc *X, int dtype, const void *const *x_tiles, const int64_t *x_ld,
                     const dmm_mx_tiles *rows, const dmm_mx_tiles *cols, void *hip_stream);
 
-/* The values that the codes stand for, into the tiles of X (all are exact in bf16 and in fp32).  `along`: DMM_MX_ROWS or
+/* The values that the codes stand for, into the tiles of X (all that dmm_mx_quantize makes are exact in bf16 and in fp32; with scale bytes
+ * 253 and 254, which it does not make, those beyond the largest number become infinite).  `along`: DMM_MX_ROWS or
  * DMM_MX_COLS, whichever form `q` is.  Otherwise as dmm_mx_quantize. */
 int dmm_mx_dequantize(const dmm_matrix_desc *X, const dmm_mx_tiles *q, int along, int dtype, void *const *x_tiles,
                       const int64_t *x_ld, void *hip_stream);

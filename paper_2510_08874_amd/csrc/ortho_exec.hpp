@@ -334,7 +334,7 @@ int dmm_orthogonalize(const dmm_matrix_desc *X, int32_t count, int x_dtype, cons
     const float unit = 1.f / 4096.f;   // a product of two scaled matrices, scaled once
     // a X and b S X + ... nearly cancel in the strong directions.  As part of P, a is added up with the rest in the
     // matrix instructions, which round the sums so far twice for 16 values of K, at the size that they have on the way: a fp32 result is
-    // 1.3e-5 off instead of 6e-6 (1021 x 4090, a few strong directions; plain fp32 6e-6).  That is far below what bf16
+    // 1.3e-5 off instead of 4.1e-6 (1021 x 4090, a few strong directions; plain fp32 6.2e-6).  That is far below what bf16
     // rounds off, and spares reading X once more: 8192 x 8192 24.9 -> 24.4 ms.
     const bool fold = y_dtype == DMM_BF16;
     for (int32_t i = 0; i < steps; ++i) {

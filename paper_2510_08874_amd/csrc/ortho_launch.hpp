@@ -73,6 +73,6 @@ void ortho_norm_launch(const OrthoTiles &args, int blocks, hipStream_t stream);
 void ortho_split_launch(const OrthoTiles &args, int blocks, hipStream_t stream);
 // y: fp32 matrices one behind another in by_rows' place -> the tiles
 void ortho_store_launch(const OrthoTiles &args, int blocks, hipStream_t stream);
-void ortho_product_launch(const OrthoProduct &args, int edge, hipStream_t stream);   // edge of a tile: 128 or 256
+void ortho_product_launch(const OrthoProduct &args, int edge, hipStream_t stream);   // edge of a tile: 64, 128 or 256
 
 }  // namespace dmm

@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 
 import workloads
+from oracle import mx as oracle
 from tests.test_gpu_mx import DT, check_product, gather, limit, made, operand, tiles_of, whole
 
 torch = pytest.importorskip("torch")
@@ -70,3 +71,16 @@ def test_tiles_of_32_rows_are_stored_from_the_registers(m, k, n, c_dtype):
     out, want = torch.full((m, n), 7.0, dtype=DT[c_dtype][0], device="cuda"), c[:, :n]
     binding.Plan(*d, 2).execute_mx(ta, b.table(), binding.tile_table([out[:m // 2], out[m // 2:]], [n, n]), flags, stream)
     assert torch.equal(out, want)
+
+
+def test_values_of_scales_beyond_those_that_quantisation_makes():
+    """Bytes 253 and 254: values past the largest number become infinite, with their sign; the others are exact."""
+    codes = torch.arange(256, dtype=torch.int64).to(torch.uint8).repeat(2, 1).cuda()
+    scales = torch.tensor([[253] * 16, [254] * 16], dtype=torch.uint8, device="cuda")
+    want = oracle.values(oracle.unpack(codes.cpu().numpy()), scales.cpu().numpy(), 512)
+    want = np.where(np.abs(want) >= 2.0 ** 128, np.copysign(np.inf, want), want)
+    for dtype in ("bf16", "f32"):
+        out = torch.zeros(2, 512, dtype=DT[dtype][0], device="cuda")
+        binding.dmm_mx_dequantize(binding.matrix_desc(whole(2, 512)), binding.mx_tiles([codes], [256], [scales], [16]), 1, DT[dtype][1],
+                                  binding.tile_table([out], [512]), torch.cuda.current_stream().cuda_stream)
+        assert np.array_equal(out.double().cpu().numpy(), want) and np.isinf(want).any()
