@@ -129,14 +129,34 @@ class MxTileSet:
     def write_values(self, X: TileSet, stream: Optional[int] = None) -> None:
         """The values that the codes stand for, into the tiles of ``X`` (bf16 or fp32)."""
         b = self.binding
+        _check_form(X, self, self.along)
         b.dmm_mx_dequantize(b.matrix_desc(self.desc), self.table, b.DMM_MX_ROWS if self.along == "rows" else b.DMM_MX_COLS,
                             b.DMM_BF16 if X.dtype == torch.bfloat16 else b.DMM_F32, b.tile_table(X.tensors, X.ld),
                             torch.cuda.current_stream().cuda_stream if stream is None else stream)
 
 
+def _check_form(X: TileSet, form: MxTileSet, along: str) -> None:
+    """The library gets addresses alone: tiles and a form that do not belong together would be read or written out of range."""
+    if X.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError(f"tiles of {X.dtype}, not of bfloat16 or float32")
+    if form.along != along:
+        raise ValueError(f"a form along the {form.along} where one along the {along} is meant")
+    a, b = X.desc, form.desc
+    if a["replication"] != b["replication"] or any(tuple(a[c]) != tuple(b[c]) for c in ("row_cuts", "col_cuts")):
+        raise ValueError("the tiles and the form have different cuts or replicas")
+    for device in {t.device for t in (*X.tensors, *form.codes, *form.scales) if t is not None}:
+        if device.type != "cuda" or device.index != torch.cuda.current_device():
+            raise ValueError(f"tiles on {device}, not on the current device")
+
+
 def quantize(X: TileSet, rows: Optional[MxTileSet] = None, cols: Optional[MxTileSet] = None, stream: Optional[int] = None) -> None:
     """``dmm_mx_quantize`` of the tiles of ``X`` along their rows, their columns or both, in one pass."""
     from . import binding as b
+    if rows is None and cols is None:
+        raise ValueError("nothing to make: neither of rows, cols")
+    for form, along in ((rows, "rows"), (cols, "cols")):
+        if form is not None:
+            _check_form(X, form, along)
     b.dmm_mx_quantize(b.matrix_desc(X.desc), b.DMM_BF16 if X.dtype == torch.bfloat16 else b.DMM_F32, b.tile_table(X.tensors, X.ld),
                       rows=rows and rows.table, cols=cols and cols.table, stream=torch.cuda.current_stream().cuda_stream if stream is None else stream)
 
