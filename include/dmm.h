@@ -348,7 +348,7 @@ int dmm_mx_execute(dmm_plan_t *p, const dmm_mx_tiles *a, const dmm_mx_tiles *b, 
  * Elements bf16 or fp32 on either side; leading dimensions in elements.  Y may be X if both have the same type.
  * Products are of pairs of fp16 numbers with fp32 sums.  A pair holds 22 bits of a value, in steps of 2^-36 at least (X, S and what X is multiplied
  * with, |G| being 1).  In the Frobenius norm an fp32 result is off by at most half as much again as fp32 products would leave it (measured: 0.65 to 0.9
- * of that), a bf16 result by twice what these would, and rounded once.  Rows (columns where there are more rows) that are far smaller than
+ * of that); a bf16 result is that, rounded once.  Rows (columns where there are more rows) that are far smaller than
  * the matrix lose digits to the steps, where fp32 products would leave 1e-5 of them: of 256 x 1024, those of 10^-3 of the largest are off by
  * 1e-5 of themselves, 10^-6 by 4e-4, 10^-8 by 4e-2.  Matrices of one tile of up to 128 x 128 keep X in fp32: 10^-6 (60 x 90) 4e-6, 10^-8 (128 x 128) 7e-5.
  * At most DMM_ORTHOGONALIZE_STEPS steps (DMM_EINVAL).  The workspace (device memory, aligned to 256 bytes;

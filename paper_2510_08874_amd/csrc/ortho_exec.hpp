@@ -332,11 +332,10 @@ int dmm_orthogonalize(const dmm_matrix_desc *X, int32_t count, int x_dtype, cons
       return DMM_OK;
     };
     const float unit = 1.f / 4096.f;   // a product of two scaled matrices, scaled once
-    // a X and b S X + ... nearly cancel in the strong directions.  As part of P, a is added up with the rest in the
-    // matrix instructions, which round the sums so far twice for 16 values of K, at the size that they have on the way: a fp32 result is
-    // 1.3e-5 off instead of 4.1e-6 (1021 x 4090, a few strong directions; plain fp32 6.2e-6).  That is far below what bf16
-    // rounds off, and spares reading X once more: 8192 x 8192 24.9 -> 24.4 ms.
-    const bool fold = y_dtype == DMM_BF16;
+    // a X and b S X + ... nearly cancel in the strong directions: a X is added in the epilogue.  As a I in P it would be added up with
+    // the rest in the matrix instructions, which round the sums so far twice for 16 values of K, at the size that they have on the way: a fp32
+    // result is 1.3e-5 off then instead of 4.1e-6 (1021 x 4090, a few strong directions; plain fp32 6.2e-6), and of a bf16 one twice as many
+    // elements are not the nearest (8192 x 8192: 1.2 % instead of 0.54 %; plain fp32 0.77 %).  Reading X once more takes 1 % there, 3 % at 2048.
     for (int32_t i = 0; i < steps; ++i) {
       const int now = i & 1;
       const float *c = coefficients + 3 * i;
@@ -348,24 +347,22 @@ int dmm_orthogonalize(const dmm_matrix_desc *X, int32_t count, int x_dtype, cons
       g.alpha = 0.f;
       g.beta = unit;
       if ((rc = product(L.cut_s, true, L.s, L.s, L.lp))) return rc;
-      // P = b S + c S S, with a I for a result in bf16
+      // P = b S + c S S
       g.a = g.b = g.old = L.S;
       g.out = g.turned = L.P;
       g.alpha = c[1];
       g.beta = c[2] * unit;
-      g.diagonal = fold ? c[0] / unit : 0.f;
       if ((rc = product(L.cut_p, true, L.s, L.s, L.sp))) return rc;
-      // X <- P X, or a X + P X
+      // X <- a X + P X
       g.a = L.P;
       g.b = L.tall[now];
-      g.old = fold ? -1 : L.wide[now];
+      g.old = L.wide[now];
       g.alpha = c[0];
       g.out = L.wide[now ^ 1];
       g.out_pitch = (uint32_t)L.lp;
       g.turned = L.tall[now ^ 1];
       g.turned_pitch = (uint32_t)L.sp;
       g.beta = unit;
-      g.diagonal = 0.f;
       if (i + 1 == steps) {            // the result takes the place of the generation that it is not made from
         g.y = L.wide[now ^ 1];
         g.y_turned = L.flip;

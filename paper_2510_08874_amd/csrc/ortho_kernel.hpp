@@ -1,14 +1,13 @@
 // Newton-Schulz steps that bring the singular values of a matrix near 1 (gfx950, device code only):
 //   X_0 = G / |G|,   S = X X^T,   X <- (a I + b S + c S S) X
-// with X the matrix or its transpose, whichever has fewer rows.  (A result in bf16 has a X as part of the last product: the
-// epilogue that adds it otherwise reads as many bytes again as half of what it writes.)
+// with X the matrix or its transpose, whichever has fewer rows.
 //
 // Every matrix is kept as pairs of fp16, v 2^12 = high + low with low the rounded rest: 22 bits of a value, and
 // a product of two is low high + high low + high high, three matrix instructions (what is left out is 2^-22 of it).  Singular
 // values far below the largest grow by 3.4 each step, and so do errors: rounded to bf16 once per step a matrix with a few
 // strong directions comes out 28 % off (512 x 512, rank 16 over 1 % of noise), in fp16 4 %, in pairs 7e-6, in plain fp32 2e-5.
 // (Frobenius norms.)  The factor 2^12: no value reaches 16 (the host refuses coefficients with which one could pass 15; the default ones leave |X| <= 1.21
-// and |a I + b S + c S S| < 5), and the low part of one of 2^-13, the size of an element of a normalised 8192 x 8192 matrix, still is
+// and |b S + c S S| < 3), and the low part of one of 2^-13, the size of an element of a normalised 8192 x 8192 matrix, still is
 // a multiple of 2^-24 / 2^12.  Rows that are smaller than
 // the matrix by 10^6 and more lose digits to that step (256 x 1024: 10^6 4e-4 of themselves, 10^8 4e-2).
 #pragma once
@@ -195,7 +194,7 @@ __device__ __forceinline__ void ortho_rows8(const OrthoProduct &g, char *ws, int
   }
 #pragma unroll
   for (int x = 0; x < 8; ++x)
-    v[x] = col + x < g.n ? g.alpha * ((float)high[x] + (float)low[x]) + g.beta * v[x] + (col + x == row ? g.diagonal : 0.f) : 0.f;
+    v[x] = col + x < g.n ? g.alpha * ((float)high[x] + (float)low[x]) + g.beta * v[x] : 0.f;
   if (g.y >= 0) return;
   ortho_split8(v, high, low);
   const int64_t at = ortho_at(row, col, g.out_pitch);

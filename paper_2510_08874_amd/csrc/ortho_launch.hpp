@@ -29,7 +29,7 @@ struct OrthoTiles {
   OrthoTile tile[ORTHO_TILES];
 };
 
-// out = diagonal I + alpha old + beta sum over k of A[m][k] B[n][k].  All matrices are pairs of fp16: 32 values of a row are 64 bytes
+// out = alpha old + beta sum over k of A[m][k] B[n][k].  All matrices are pairs of fp16: 32 values of a row are 64 bytes
 // of high parts and 64 bytes of low parts.
 struct OrthoProduct {
   char *ws;                     // what follows are byte offsets in a matrix' buffers
@@ -49,7 +49,7 @@ struct OrthoProduct {
   int32_t whole;                // tiles (of all matrices) that are not cut; the others in `runs` ranges of K,
   int32_t runs, per;            // steps of each
   float *parts;
-  float alpha, beta, diagonal;
+  float alpha, beta;
 };
 
 // Matrices of up to 128 x 128, one workgroup each, whole in registers and LDS.

@@ -1,5 +1,5 @@
-"""GPU tests of ``dmm_orthogonalize`` on rows of very different size, and of small matrices in tile grids against the path
-that takes them in one tile."""
+"""GPU tests of ``dmm_orthogonalize`` on rows of very different size, of small matrices in tile grids against the path
+that takes them in one tile, and of results in bf16 against exact ones rounded."""
 import numpy as np
 import pytest
 
@@ -63,6 +63,34 @@ def test_small_matrices_in_tile_grids(rows, cols, row_cuts, col_cuts, dtype):
         exact = oracle.orthogonalize(G)
         if dtype == "f32" and min(rows, cols) > 64:
             assert (row_errors(x, exact) <= row_limits(G, exact)).all() and (row_errors(y, exact) <= row_limits(G, exact)).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("count,rows,cols", [(1, 1024, 2048), (8, 700, 600), (24, 300, 500), (1, 2048, 2048), (32, 128, 128)], ids=str)
+def test_bf16_results_are_as_near_as_those_of_fp32_arithmetic(count, rows, cols):
+    """How many elements fall on the other side of a border of the last rounding goes with the error in front of it: no more than
+    where the same steps are made in fp32, whose error a result in fp32 does not reach."""
+    from tests.test_gpu_orthogonalize import exact, random, tiles, whole
+    from paper_2510_08874_amd import binding
+    mats = [M.bfloat16() for M in random(count, rows, cols, rows + cols, "strong")]
+    d = whole(rows, cols)
+    y, ld = tiles([torch.zeros(rows, cols, device="cuda")] * count, d, torch.bfloat16)
+    desc = binding.matrix_desc(d)
+    size = binding.dmm_orthogonalize_workspace(desc, count)
+    ws = torch.empty(size + 256, dtype=torch.uint8, device="cuda")
+    binding.dmm_orthogonalize(desc, count, 1, binding.tile_table(mats, [cols] * count), 1, binding.tile_table(y, ld), ws if size else None, size,
+                              stream=torch.cuda.current_stream().cuda_stream)
+    own = plain = 0
+    for M, Y in zip(mats, y):
+        want = exact(M).float().bfloat16()
+        X = M.float() / M.double().norm().float()
+        X = X.t().contiguous() if rows > cols else X
+        for a, b, c in oracle.DEFAULT:
+            S = X @ X.t().contiguous()
+            X = a * X + (b * S + c * (S @ S)) @ X
+        own += int((Y != want).sum())
+        plain += int(((X.t() if rows > cols else X).bfloat16() != want).sum())
+    assert 0 < own <= plain, (own, plain)
 
 
 @pytest.mark.parametrize("rows,cols,decades", ROWS, ids=str)
