@@ -352,8 +352,8 @@ int dmm_mx_execute(dmm_plan_t *p, const dmm_mx_tiles *a, const dmm_mx_tiles *b, 
  * the matrix lose digits to the steps, where fp32 products would leave 1e-5 of them: of 256 x 1024, those of 10^-3 of the largest are off by
  * 1e-5 of themselves, 10^-6 by 4e-4, 10^-8 by 4e-2.  Matrices of one tile of up to 128 x 128 keep X in fp32: 10^-6 (60 x 90) 4e-6, 10^-8 (128 x 128) 7e-5.
  * At most DMM_ORTHOGONALIZE_STEPS steps (DMM_EINVAL).  The workspace (device memory, aligned to 256 bytes;
- * dmm_orthogonalize_workspace tells how much: DMM_ELIMIT if there is less; none for matrices of one tile of up to
- * 128 x 128) is the caller's: nothing else is allocated and nothing kept, so calls with workspaces of their own may overlap
+ * dmm_orthogonalize_workspace tells how much, about 16 bytes an element and 8 for the square of the shorter side: DMM_ELIMIT if there is less; none for
+ * matrices of one tile of up to 128 x 128) is the caller's: nothing else is allocated and nothing kept, so calls with workspaces of their own may overlap
  * on any streams and be captured; calls that share one have to follow each other, replays of graphs included.  Sums are cut
  * in a way that depends on the shape and the count alone.  A dimension is 2^20 at most (DMM_ELIMIT). */
 #define DMM_ORTHOGONALIZE_STEPS 32
