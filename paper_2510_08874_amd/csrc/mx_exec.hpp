@@ -150,13 +150,15 @@ struct MxChoice {
   int64_t runs = 1;                    // of a tile of average length
 };
 
-// By an estimate in us.  A step (256 of k) of a tile costs its matrix instructions, or what L2 takes with many tiles at a time; few rows
-// wait for B from memory.  Measured as what more of K costs: 256 x 256 1.4 to 2.0 a step with all CUs at it (random codes more than normal
-// data: power), 128 x 128 0.54 to 0.66 (64, 256 of them), two on a CU 1.1 to 1.4; 64 x 128 0.5 (112) and 0.55 (224) of B that a cache holds, 0.8 and
-// 0.95 of B from memory, with two stages; 32 x 128 with three 0.35, 0.5; 0.55, 0.75; two of them on a CU 1.0 to 1.2.  Nothing is faster than memory: 570 MB of
-// B take 32 rows 113 us, 64 130, 128 131, 256 149; 125 MB 27, 34, 30, 50 (so up to 32 rows the tile of 32 is the best everywhere, from
-// 33 to 64 that of 64 but where there is one tile on almost every CU and K is long: 64 x 4096 x 14336 16.7, 128 rows 17.2; x 28000 20.9 and 18.8).  A tile cut
-// along K costs its partial sums and a launch that adds them up.  Of equal estimates the smaller tile's.
+// By an estimate in us.  What a step (256 of k) of a tile costs, measured as what more of K costs:
+//   256 x 256  1.4 to 2.0 with all CUs at it (random codes more than normal data: power)
+//   128 x 128  0.54 (64 tiles) to 0.66 (256); two on a CU 1.1 to 1.4
+//   64 x 128   0.5 (112) and 0.55 (224) where a cache holds B, 0.8 and 0.95 where it comes from memory (two stages); two on a CU 1.1 to 1.25
+//   32 x 128   0.35 and 0.5, from memory 0.55 and 0.75 (three stages); two on a CU 1.0 to 1.1
+// and none is faster than memory: 570 MB of B take tiles of 32 113 us, of 64 130, of 128 131, of 256 149; 125 MB 27, 34, 30, 50.  Up to 32 rows the
+// tile of 32 is the best everywhere.  From 33 to 64 it is that of 64, or that of 128 where almost every CU has one and B comes from memory: 64 x 4096 x 14336 16.7
+// and 17.2, 64 x 4096 x 28000 20.9 and 18.8 (13.0 and 15.0 with B in the cache, which the choice does not know).  A tile cut along K costs its
+// partial sums and a launch that adds them up.  Of equal estimates the smaller tile's.
 MxChoice choose_mx(const dmm_plan_t *P, int cus) {
   int64_t most = 0;                    // rows of a group
   double cells = 0, k_steps = 0, b_bytes = 0, b_once = 0;

@@ -6,10 +6,11 @@
 // a product of two is low high + high low + high high, three matrix instructions (what is left out is 2^-22 of it).  Singular
 // values far below the largest grow by 3.4 each step, and so do errors: rounded to bf16 once per step a matrix with a few
 // strong directions comes out 28 % off (512 x 512, rank 16 over 1 % of noise), in fp16 4 %, in pairs 7e-6, in plain fp32 2e-5.
-// (Frobenius norms.)  The factor 2^12: no value reaches 16 (the host refuses coefficients with which one could pass 15; the default ones leave |X| <= 1.21
+// (Frobenius norms.)
+// The factor 2^12: no value reaches 16 (the host refuses coefficients with which one could pass 15; the default ones leave |X| <= 1.21
 // and |b S + c S S| < 3), and the low part of one of 2^-13, the size of an element of a normalised 8192 x 8192 matrix, still is
-// a multiple of 2^-24 / 2^12.  Rows that are smaller than
-// the matrix by 10^6 and more lose digits to that step (256 x 1024: 10^6 4e-4 of themselves, 10^8 4e-2).
+// a multiple of 2^-24 / 2^12.  Rows smaller than the matrix by 10^6 and more lose digits to that step (256 x 1024: 10^6 4e-4
+// of themselves, 10^8 4e-2).
 #pragma once
 
 #include "nt_kernel.hpp"

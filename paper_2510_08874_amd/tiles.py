@@ -152,8 +152,6 @@ def _check_form(X: TileSet, form: MxTileSet, along: str) -> None:
 def quantize(X: TileSet, rows: Optional[MxTileSet] = None, cols: Optional[MxTileSet] = None, stream: Optional[int] = None) -> None:
     """``dmm_mx_quantize`` of the tiles of ``X`` along their rows, their columns or both, in one pass."""
     from . import binding as b
-    if rows is None and cols is None:
-        raise ValueError("nothing to make: neither of rows, cols")
     for form, along in ((rows, "rows"), (cols, "cols")):
         if form is not None:
             _check_form(X, form, along)

@@ -57,8 +57,3 @@ def test_other_devices():
             quantize(tiles(device=x), rows=form(device=q))
         with pytest.raises(ValueError, match="current device"):
             form(device=q).write_values(tiles(device=x))
-
-
-def test_nothing_to_make():
-    with pytest.raises(ValueError, match="rows, cols"):
-        quantize(tiles())
