@@ -296,7 +296,7 @@ def _table(binding, tiles):
 
 
 def _i8_table(binding, x):
-    return binding.i8_tiles(x.q, [t.shape[1] for t in x.q], x.s)
+    return binding.int_tiles(x.q, [t.shape[1] for t in x.q], x.s)
 
 
 def _prepare_own(state):
@@ -310,7 +310,7 @@ def _prepare_own(state):
         s = [torch.empty(j - i, dtype=torch.float32, device="cuda") for i, j in zip(cuts, cuts[1:])]
         out = _empty_tiles(d, state["x"][0].dtype)
         state.update(desc=binding.matrix_desc(d), dtype=binding.DMM_BF16 if case["dtype"] == "bf16" else binding.DMM_F32, x_table=_table(binding, state["x"]),
-                     q=q, s=s, q_table=binding.i8_tiles(q, [t.shape[1] for t in q], s), out=out, out_table=_table(binding, out))
+                     q=q, s=s, q_table=binding.int_tiles(q, [t.shape[1] for t in q], s), out=out, out_table=_table(binding, out))
         return
     da, db, dc = state["descs"]
     state["plan"] = binding.Plan(da, db, dc, case["ranks"])
@@ -344,15 +344,15 @@ def _run_own(state):
     b, op, stream = state["binding"], state["op"], state["stream"]
     if op == "quantize":
         rows = state["case"]["along"] == "rows"
-        b.dmm_i8_quantize(state["desc"], state["dtype"], state["x_table"], rows=state["q_table"] if rows else None, cols=None if rows else state["q_table"],
+        b.dmm_int_quantize(state["desc"], state["dtype"], state["x_table"], rows=state["q_table"] if rows else None, cols=None if rows else state["q_table"],
                           stream=stream)
-        b.dmm_i8_dequantize(state["desc"], state["q_table"], b.DMM_MX_ROWS if rows else b.DMM_MX_COLS, state["dtype"], state["out_table"], stream=stream)
+        b.dmm_int_dequantize(state["desc"], state["q_table"], b.DMM_MX_ROWS if rows else b.DMM_MX_COLS, state["dtype"], state["out_table"], stream=stream)
         return state["out"]
     plan, tables = state["plan"], state["tables"]
     if op == "product":
-        plan.execute_i8(*tables, state["out_table"], state["flags"], stream)
+        plan.execute_int(*tables, state["out_table"], state["flags"], stream)
     elif op == "gated_i8":
-        plan.gated_i8(state["act"], *tables, state["out_table"], stream)
+        plan.gated_int(state["act"], *tables, state["out_table"], stream)
     elif op == "gated":
         h, *kept = state["out_tables"]
         plan.gated(state["act"], *tables, h, *kept, stream=stream)
