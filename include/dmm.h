@@ -44,8 +44,8 @@ typedef enum {
   DMM_ELD = -6,    /* a leading dimension is smaller than the tile's width, or a row pitch (leading
                       dimension times element size) of an A, B or C tile is 2^24 bytes or more */
   DMM_ELIMIT = -7  /* dmm_reduce_replicas_static: the work tables of this call do not fit the library's
-                      static device buffer (DMM_STATIC_SCRATCH_BYTES); dmm_mx_*, dmm_orthogonalize: 2^24
-                      workgroups in a launch, 2^30 table entries, a workspace that is too small */
+                      static device buffer (DMM_STATIC_SCRATCH_BYTES); dmm_mx_*, dmm_orthogonalize, dmm_int_*,
+                      dmm_gated_*, dmm_execute_backward: 2^24 workgroups in a launch, 2^30 table entries, a workspace that is too small */
 } dmm_status;
 
 /* Element type of the A and B tiles.  All partial sums are fp32, and so are the C tiles unless
@@ -362,6 +362,89 @@ int dmm_orthogonalize(const dmm_matrix_desc *X, int32_t count, int x_dtype, cons
                       int y_dtype, void *const *y_tiles, const int64_t *y_ld, const float *coefficients, int32_t steps,
                       void *workspace, int64_t workspace_bytes, void *hip_stream);
 
+/* ---- 8-bit integers with a scale for every row and column ----------------------------------------
+ *
+ * A form of a matrix for products of tokens with weights: a row (a token) or a column (a channel) has one scale s, over all tiles
+ * that it is cut into, and an element is an integer from -127 to 127.
+ *   s = largest magnitude of the row / 127, rounded to fp32
+ *   code = 127 element / (largest magnitude), taken exactly and rounded to nearest, half-way values to the even integer
+ *   a row of zeros has the scale 0; one that holds an infinity or a NaN has the scale NaN and codes of 0, and stands for NaN throughout
+ *
+ * A tile of h x w elements along its rows (DMM_MX_ROWS): h rows of w bytes.  Along its columns (DMM_MX_COLS): the same of the transposed
+ * tile, w rows of h bytes.  Rows may start at any address (multiples of 16 are read fastest) and lie less than 2^24 bytes apart (DMM_ELD).  As for 4-bit
+ * matrices, the form of X along its columns is that of X^T along its rows. */
+
+/* Tiles of a matrix: host arrays in table order.  Pointers of empty tiles may be null. */
+typedef struct {
+  void *const *tiles;        /* device pointers */
+  const int64_t *ld;         /* elements */
+} dmm_tiles;
+
+typedef struct {
+  void *const *codes;        /* host array of device pointers, one per (replica, tile) in table order */
+  const int64_t *code_ld;    /* bytes from one row of codes to the next */
+  float *const *scales;      /* along the rows: one per (replica, tile row), rep * grid_rows + ti, to as many scales as the tile has rows;
+                                along the columns: rep * grid_cols + tj, a scale per column */
+} dmm_int_tiles;
+
+/* The tiles of X, bf16 or fp32 (`dtype`), to integers: along their rows into `rows`, along their columns into `cols`; either may be null, not
+ * both.  Every replica is quantised from its own tiles; the process grid of X plays no part.  Asynchronous on `hip_stream`; takes no memory
+ * and keeps nothing, so calls may overlap on any streams and be captured.  X and the outputs must not overlap. */
+int dmm_int_quantize(const dmm_matrix_desc *X, int dtype, const dmm_tiles *x, const dmm_int_tiles *rows, const dmm_int_tiles *cols, void *hip_stream);
+
+/* The values that the integers stand for, code times scale in fp32, into the tiles of X (rounded once more where these are bf16).  `along`: DMM_MX_ROWS or
+ * DMM_MX_COLS, whichever form `q` is.  Otherwise as dmm_int_quantize. */
+int dmm_int_dequantize(const dmm_matrix_desc *X, const dmm_int_tiles *q, int along, int dtype, const dmm_tiles *x, void *hip_stream);
+
+/* dmm_execute for 8-bit operands: C = A B (overwrite) on a plan, A along its rows, B along its columns.
+ *   c         fp32 tiles (bf16 with DMM_C_BF16: C with one replica only), every element written once; rows lie less than 2^24 bytes apart (DMM_ELD)
+ *   flags     0 or any of DMM_NO_REDUCE, DMM_C_BF16
+ * An element is the sum of its products as an integer, without loss at any length (all codes from -128 to 127 may be there), rounded to fp32 once and
+ * multiplied with the scales of its row of A and its column of B.  Cuts of k may lie anywhere; a sum of more than 131071 products is taken in
+ * parts, and one part may meet so many at most (DMM_ELIMIT where thousands of cuts of k leave nothing longer than 127).  Where a replica of A or B is cut out of
+ * several, the scales are those of the replica that the plan's first op of the region reads: replicas are copies of each other.
+ * Replicas of C, streams, ownership and captures as for dmm_mx_execute; the plan's tables and scratch memory for this entry point are its own. */
+int dmm_int_execute(dmm_plan_t *p, const dmm_int_tiles *a, const dmm_int_tiles *b, const dmm_tiles *c, uint32_t flags, void *hip_stream);
+
+/* ---- the gated block ----------------------------------------------------------------------------
+ *
+ * H = act(G) * U element by element, with G = A Wg and U = A Wu: both projections, the activation and the product in one pass over A.  On a
+ * plan of A [m, k], a weight [k, n] (the plan's B, whose cuts both weights have) and H [m, n] (the plan's C, with one replica: DMM_EINVAL).
+ * Tiles are bf16; sums, the activation and the product are fp32, and each result is rounded once.  Rows of all tiles lie less than 2^24 bytes apart (DMM_ELD). */
+#define DMM_SILU 1           /* g / (1 + e^-g) */
+#define DMM_GELU 2           /* g (1 + erf(g / sqrt 2)) / 2 */
+#define DMM_GELU_TANH 3      /* g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2 */
+/* flag of the backward calls: weight gradients are fp32 tiles (else bf16) */
+#define DMM_DB_F32 0x2000u
+
+/* h; with g and u (either may be null) G and U as well, for the way back: bf16 tiles of the plan's C.
+ * Where tiles are few they are cut along K into runs whose partial sums go through a scratch buffer and are added in ascending k (fixed cut
+ * and order: results are reproducible).  Streams, ownership and captures as for dmm_mx_execute; the plan's tables and scratch memory for this entry
+ * point are its own. */
+int dmm_gated_execute(dmm_plan_t *p, int activation, const dmm_tiles *a, const dmm_tiles *gate, const dmm_tiles *up, const dmm_tiles *h,
+                      const dmm_tiles *g, const dmm_tiles *u, void *hip_stream);
+
+/* The same from 8-bit operands: A along its rows, both weights along their columns, H in bf16.  Sums as dmm_int_execute takes them. */
+int dmm_int_gated_execute(dmm_plan_t *p, int activation, const dmm_int_tiles *a, const dmm_int_tiles *gate, const dmm_int_tiles *up, const dmm_tiles *h,
+                         void *hip_stream);
+
+/* The gradients from dH, with G and U as dmm_gated_execute keeps them:
+ *   dg, du          dG = dH U act'(G), dU = dH act(G), bf16 tiles of the plan's C.  They may be the tiles of G and U.
+ *   da              dA = dG Wg^T + dU Wu^T, bf16, or null
+ *   dgate, dup      dWg = A^T dG, dWu = A^T dU, bf16 (fp32 with DMM_DB_F32), or null
+ * dA, dWg and dWu are products of dG and dU as they are stored, in bf16.  They are overwritten, and have one replica (grid_rows * grid_cols tiles in
+ * the cuts of A and B), whatever the operands have; of these replica 0 is read.  a may be null without dgate and dup, the weights without da.  Captures, streams and
+ * ownership as for dmm_gated_execute. */
+int dmm_gated_backward(dmm_plan_t *p, int activation, const dmm_tiles *a, const dmm_tiles *gate, const dmm_tiles *up, const dmm_tiles *g,
+                       const dmm_tiles *u, const dmm_tiles *dh, const dmm_tiles *dg, const dmm_tiles *du, const dmm_tiles *da, const dmm_tiles *dgate,
+                       const dmm_tiles *dup, uint32_t flags, void *hip_stream);
+
+/* The gradients of C = A B in bf16: dA = dC B^T and dB = A^T dC (either may be null), from tiles in the cuts of the plan's A, B and C.  All tables
+ * name one replica, whatever the plan has.  da is bf16, db bf16 (fp32 with DMM_DB_F32); both are overwritten.  a may be null without db, b
+ * without da.  Rows lie less than 2^24 bytes apart (DMM_ELD).  Captures, streams and ownership as for dmm_gated_execute. */
+int dmm_execute_backward(dmm_plan_t *p, const dmm_tiles *a, const dmm_tiles *b, const dmm_tiles *dc, const dmm_tiles *da, const dmm_tiles *db,
+                         uint32_t flags, void *hip_stream);
+
 /* ---- measurement and test aids (not steps of the method) ---------------------------------- */
 
 /* What the last dmm_execute on a plan did.
@@ -439,8 +522,9 @@ void dmm_plan_destroy(dmm_plan_t *p);
 
 const char *dmm_strerror(int status);
 int dmm_last_hip_error(void); /* hipError_t of the last failed HIP call on this thread, 0 if none */
-int dmm_version(void);         /* 6: dmm_mx_quantize, dmm_mx_dequantize, dmm_mx_execute,
-                                  dmm_orthogonalize (5: dmm_plan_last_kernels; 4: the replica sum is fused into the GEMM unless DMM_SEPARATE_REDUCE asks
+int dmm_version(void);         /* 7: dmm_int_quantize, dmm_int_dequantize, dmm_int_execute, dmm_gated_execute, dmm_int_gated_execute,
+                                  dmm_gated_backward, dmm_execute_backward (6: dmm_mx_quantize, dmm_mx_dequantize, dmm_mx_execute,
+                                  dmm_orthogonalize; 5: dmm_plan_last_kernels; 4: the replica sum is fused into the GEMM unless DMM_SEPARATE_REDUCE asks
                                   for the kernel of its own; dmm_plan_last_execute replaces the
                                   dmm_plan_ran_* accessors; 3: flag values of dmm_plan and dmm_execute disjoint,
                                   dmm_reduce_replicas_static) */

@@ -28,6 +28,8 @@ DMM_SEPARATE_REDUCE = 0x1000
 DMM_STATIC_SCRATCH_BYTES = 1 << 20
 DMM_MX_BLOCK, DMM_MX_CHUNK = 32, 128
 DMM_MX_ROWS, DMM_MX_COLS = 1, 2
+DMM_SILU, DMM_GELU, DMM_GELU_TANH = 1, 2, 3
+DMM_DB_F32 = 0x2000           # flag of the backward calls
 STATIONARY_FLAGS = {"C": 0, "B": DMM_STATIONARY_B, "A": DMM_STATIONARY_A}
 STATUS_NAMES = {0: "OK", -1: "EINVAL", -2: "ESHAPE", -3: "EREPL", -4: "ENOMEM", -5: "EHIP", -6: "ELD", -7: "ELIMIT"}
 
@@ -75,6 +77,14 @@ class dmm_kernel_report(C.Structure):
 
 class dmm_mx_tiles(C.Structure):
     _fields_ = [("codes", C.c_void_p), ("code_ld", C.c_void_p), ("scales", C.c_void_p), ("scale_ld", C.c_void_p)]
+
+
+class dmm_tiles(C.Structure):
+    _fields_ = [("tiles", C.c_void_p), ("ld", C.c_void_p)]
+
+
+class dmm_int_tiles(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("code_ld", C.c_void_p), ("scales", C.c_void_p)]
 
 
 class DmmError(RuntimeError):
@@ -143,6 +153,21 @@ def lib() -> C.CDLL:
         L.dmm_orthogonalize_workspace.argtypes = [C.POINTER(dmm_matrix_desc), C.c_int32, C.POINTER(C.c_int64)]
         L.dmm_orthogonalize.restype = C.c_int
         L.dmm_orthogonalize.argtypes = [C.POINTER(dmm_matrix_desc), C.c_int32, C.c_int, P, P, C.c_int, P, P, P, C.c_int32, P, C.c_int64, P]
+        T, Q = C.POINTER(dmm_tiles), C.POINTER(dmm_int_tiles)
+        L.dmm_int_quantize.restype = C.c_int
+        L.dmm_int_quantize.argtypes = [C.POINTER(dmm_matrix_desc), C.c_int, T, Q, Q, P]
+        L.dmm_int_dequantize.restype = C.c_int
+        L.dmm_int_dequantize.argtypes = [C.POINTER(dmm_matrix_desc), Q, C.c_int, C.c_int, T, P]
+        L.dmm_int_execute.restype = C.c_int
+        L.dmm_int_execute.argtypes = [P, Q, Q, T, C.c_uint32, P]
+        L.dmm_gated_execute.restype = C.c_int
+        L.dmm_gated_execute.argtypes = [P, C.c_int, T, T, T, T, T, T, P]
+        L.dmm_int_gated_execute.restype = C.c_int
+        L.dmm_int_gated_execute.argtypes = [P, C.c_int, Q, Q, Q, T, P]
+        L.dmm_gated_backward.restype = C.c_int
+        L.dmm_gated_backward.argtypes = [P, C.c_int] + [T] * 11 + [C.c_uint32, P]
+        L.dmm_execute_backward.restype = C.c_int
+        L.dmm_execute_backward.argtypes = [P, T, T, T, T, T, C.c_uint32, P]
         L.dmm_plan_elapsed_ms.restype = C.c_int
         L.dmm_plan_elapsed_ms.argtypes = [P, C.POINTER(C.c_float), C.POINTER(C.c_float)]
         L.dmm_plan_gemm_launch_ms.restype = C.c_int
@@ -163,6 +188,7 @@ EXPORTS = ("dmm_plan", "dmm_plan_num_tasks", "dmm_plan_tasks", "dmm_plan_order",
            "dmm_plan_group_offsets", "dmm_plan_num_items", "dmm_plan_items", "dmm_plan_macro_tile",
            "dmm_plan_num_merged_items", "dmm_plan_merged_items", "dmm_plan_last_execute", "dmm_plan_last_kernels",
            "dmm_reduce_replicas_static", "dmm_mx_quantize", "dmm_mx_dequantize", "dmm_mx_execute", "dmm_orthogonalize", "dmm_orthogonalize_workspace",
+           "dmm_int_quantize", "dmm_int_dequantize", "dmm_int_execute", "dmm_gated_execute", "dmm_int_gated_execute", "dmm_gated_backward", "dmm_execute_backward",
            "dmm_execute", "dmm_reduce_replicas", "dmm_broadcast_replica", "dmm_plan_elapsed_ms", "dmm_plan_gemm_launch_ms", "dmm_plan_destroy", "dmm_strerror",
            "dmm_last_hip_error", "dmm_version", "dmm_measure_mfma_rate")
 
@@ -208,6 +234,27 @@ def mx_tiles(codes: Sequence, code_ld: Sequence[int], scales: Sequence, scale_ld
     out = dmm_mx_tiles(*[C.cast(x, C.c_void_p) for x in keep])
     out.keep = keep
     return out
+
+
+def tiles(buffers: Sequence, ld: Sequence[int]) -> dmm_tiles:
+    """The tables of a matrix' tiles as a structure, for the calls that take one (reusable across calls; tensors live as long as it)."""
+    keep = tile_table(buffers, ld)
+    out = dmm_tiles(*[C.cast(x, C.c_void_p) for x in keep])
+    out.keep = [*keep, list(buffers)]
+    return out
+
+
+def int_tiles(codes: Sequence, code_ld: Sequence[int], scales: Sequence) -> dmm_int_tiles:
+    """The tables of a matrix in 8-bit integers: codes of every tile, leading dimensions in bytes, scales of every row (column) of tiles
+    (reusable across calls; tensors live as long as it)."""
+    keep = [*tile_table(codes, code_ld), _table([_ptr(s) for s in scales], C.c_void_p)]
+    out = dmm_int_tiles(*[C.cast(x, C.c_void_p) for x in keep])
+    out.keep = [*keep, list(codes), list(scales)]
+    return out
+
+
+def _ref(x):
+    return None if x is None else C.byref(x)
 
 
 class Plan:
@@ -332,6 +379,41 @@ class Plan:
         if rc != DMM_OK:
             raise DmmError(rc, "dmm_mx_execute")
 
+    def execute_int(self, a: dmm_int_tiles, b: dmm_int_tiles, c: dmm_tiles, flags: int = 0, stream: Optional[int] = None) -> None:
+        """``dmm_int_execute``: `a` along its rows and `b` along its columns (`int_tiles`), `c` from `tiles`."""
+        rc = lib().dmm_int_execute(self._h, C.byref(a), C.byref(b), C.byref(c), flags, C.c_void_p(stream or 0))
+        if rc != DMM_OK:
+            raise DmmError(rc, "dmm_int_execute")
+
+    def gated(self, activation: int, a: dmm_tiles, gate: dmm_tiles, up: dmm_tiles, h: dmm_tiles, g: Optional[dmm_tiles] = None,
+              u: Optional[dmm_tiles] = None, stream: Optional[int] = None) -> None:
+        """``dmm_gated_execute``; `g` and `u` receive what ``gated_backward`` needs."""
+        rc = lib().dmm_gated_execute(self._h, activation, C.byref(a), C.byref(gate), C.byref(up), C.byref(h), _ref(g), _ref(u), C.c_void_p(stream or 0))
+        if rc != DMM_OK:
+            raise DmmError(rc, "dmm_gated_execute")
+
+    def gated_int(self, activation: int, a: dmm_int_tiles, gate: dmm_int_tiles, up: dmm_int_tiles, h: dmm_tiles, stream: Optional[int] = None) -> None:
+        """``dmm_int_gated_execute``."""
+        rc = lib().dmm_int_gated_execute(self._h, activation, C.byref(a), C.byref(gate), C.byref(up), C.byref(h), C.c_void_p(stream or 0))
+        if rc != DMM_OK:
+            raise DmmError(rc, "dmm_int_gated_execute")
+
+    def gated_backward(self, activation: int, a: Optional[dmm_tiles], gate: Optional[dmm_tiles], up: Optional[dmm_tiles], g: dmm_tiles, u: dmm_tiles,
+                       dh: dmm_tiles, dg: dmm_tiles, du: dmm_tiles, da: Optional[dmm_tiles] = None, dgate: Optional[dmm_tiles] = None,
+                       dup: Optional[dmm_tiles] = None, flags: int = 0, stream: Optional[int] = None) -> None:
+        """``dmm_gated_backward``."""
+        rc = lib().dmm_gated_backward(self._h, activation, _ref(a), _ref(gate), _ref(up), C.byref(g), C.byref(u), C.byref(dh), C.byref(dg), C.byref(du),
+                                      _ref(da), _ref(dgate), _ref(dup), flags, C.c_void_p(stream or 0))
+        if rc != DMM_OK:
+            raise DmmError(rc, "dmm_gated_backward")
+
+    def execute_backward(self, a: Optional[dmm_tiles], b: Optional[dmm_tiles], dc: dmm_tiles, da: Optional[dmm_tiles] = None,
+                         db: Optional[dmm_tiles] = None, flags: int = 0, stream: Optional[int] = None) -> None:
+        """``dmm_execute_backward``: the gradients of a bf16 product."""
+        rc = lib().dmm_execute_backward(self._h, _ref(a), _ref(b), C.byref(dc), _ref(da), _ref(db), flags, C.c_void_p(stream or 0))
+        if rc != DMM_OK:
+            raise DmmError(rc, "dmm_execute_backward")
+
     def reduce_replicas(self, c_tiles: Sequence, c_ld: Sequence[int], origin: int = 0,
                         stream: Optional[int] = None) -> None:
         ct = _table([_ptr(t) for t in c_tiles], C.c_void_p)
@@ -419,6 +501,43 @@ def dmm_mx_dequantize(desc: dmm_matrix_desc, q: dmm_mx_tiles, along: int, dtype:
 
 def dmm_mx_execute(plan: Plan, a: dmm_mx_tiles, b: dmm_mx_tiles, c, flags: int = 0, stream: Optional[int] = None) -> None:
     plan.execute_mx(a, b, c, flags, stream)
+
+
+def dmm_int_quantize(desc: dmm_matrix_desc, dtype: int, x: dmm_tiles, rows: Optional[dmm_int_tiles] = None, cols: Optional[dmm_int_tiles] = None,
+                    stream: Optional[int] = None) -> None:
+    """`desc` a `matrix_desc`, `x` from `tiles`, `rows` and `cols` `int_tiles`."""
+    rc = lib().dmm_int_quantize(C.byref(desc), dtype, C.byref(x), _ref(rows), _ref(cols), C.c_void_p(stream or 0))
+    if rc != DMM_OK:
+        raise DmmError(rc, "dmm_int_quantize")
+
+
+def dmm_int_dequantize(desc: dmm_matrix_desc, q: dmm_int_tiles, along: int, dtype: int, x: dmm_tiles, stream: Optional[int] = None) -> None:
+    rc = lib().dmm_int_dequantize(C.byref(desc), C.byref(q), along, dtype, C.byref(x), C.c_void_p(stream or 0))
+    if rc != DMM_OK:
+        raise DmmError(rc, "dmm_int_dequantize")
+
+
+def dmm_int_execute(plan: Plan, a: dmm_int_tiles, b: dmm_int_tiles, c: dmm_tiles, flags: int = 0, stream: Optional[int] = None) -> None:
+    plan.execute_int(a, b, c, flags, stream)
+
+
+def dmm_gated_execute(plan: Plan, activation: int, a: dmm_tiles, gate: dmm_tiles, up: dmm_tiles, h: dmm_tiles, g: Optional[dmm_tiles] = None,
+                      u: Optional[dmm_tiles] = None, stream: Optional[int] = None) -> None:
+    plan.gated(activation, a, gate, up, h, g, u, stream)
+
+
+def dmm_int_gated_execute(plan: Plan, activation: int, a: dmm_int_tiles, gate: dmm_int_tiles, up: dmm_int_tiles, h: dmm_tiles,
+                         stream: Optional[int] = None) -> None:
+    plan.gated_int(activation, a, gate, up, h, stream)
+
+
+def dmm_gated_backward(plan: Plan, activation: int, a, gate, up, g, u, dh, dg, du, da=None, dgate=None, dup=None, flags: int = 0,
+                       stream: Optional[int] = None) -> None:
+    plan.gated_backward(activation, a, gate, up, g, u, dh, dg, du, da, dgate, dup, flags, stream)
+
+
+def dmm_execute_backward(plan: Plan, a, b, dc, da=None, db=None, flags: int = 0, stream: Optional[int] = None) -> None:
+    plan.execute_backward(a, b, dc, da, db, flags, stream)
 
 
 def dmm_orthogonalize_workspace(desc: dmm_matrix_desc, count: int = 1) -> int:

@@ -15,10 +15,11 @@ CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "_build")          # objects and the compiler's intermediate files
 LIB = os.path.join(HERE, "libdmm.so")
 # (source, object name, extra flags): the grouped-GEMM kernels are compiled one instantiation per
-# object file (gemm_instance.hip, DMM_INSTANCE = 0 .. 5), side by side
+# object file (gemm_instance.hip, DMM_INSTANCE = 0 .. 5), side by side, and so are the kinds of layer_instance.hip
 UNITS = [("plan.cpp", "plan", []), ("exec.hip", "exec", []), ("small_instance.hip", "small_instance", []),
          ("mx_instance.hip", "mx_instance", []), ("ortho_instance.hip", "ortho_instance", [])] + \
-        [("gemm_instance.hip", f"gemm_instance_{i}", [f"-DDMM_INSTANCE={i}"]) for i in range(6)]
+        [("gemm_instance.hip", f"gemm_instance_{i}", [f"-DDMM_INSTANCE={i}"]) for i in range(6)] + \
+        [("layer_instance.hip", f"layer_instance_{i}", [f"-DDMM_INSTANCE={i}"]) for i in range(6)]
 
 # packed-fp32 ops are switched off for all device code (a target feature of the
 # device pass; the host pass prints a harmless "not recognized" note).
@@ -38,7 +39,7 @@ def check_resources(remarks: str, want_kernel: bool) -> None:
         name = b.split()[0]
         if "small_gemm_kernel" in name and re.search(r"(ScratchSize \[bytes/lane\]|VGPRs Spill): [1-9]", b):
             raise RuntimeError(f"{name}: scratch use or spills")
-        if re.search(r"mx_\w*kernel|ortho_\w*kernel", name) and re.search(r"(ScratchSize \[bytes/lane\]|VGPRs Spill): [1-9]", b):
+        if re.search(r"mx_\w*kernel|ortho_\w*kernel|layer_\w*kernel|i8_\w*kernel", name) and re.search(r"(ScratchSize \[bytes/lane\]|VGPRs Spill): [1-9]", b):
             raise RuntimeError(f"{name}: scratch use or spills")
         if "grouped_gemm_kernel" not in name:
             continue

@@ -576,8 +576,27 @@ struct MxState {
   bool cached = false;
 };
 
+// Where the tables of a product around a layer (layer_launch.hpp) sit in its buffer, and what it launches.
+struct LayerLayout {
+  int kind = 0, shape = 0, act = 0, n_items = 0, n_joins = 0;
+  size_t o_items = 0, o_segs = 0, o_joins = 0;
+};
+
+// What a plan keeps for each entry point of these: as MxState.
+enum { LAYER_I8_EXECUTE, LAYER_I8_GATED_EXECUTE, LAYER_GATED_EXECUTE, LAYER_GATED_BACKWARD, LAYER_EXECUTE_BACKWARD, LAYER_ENTRIES };
+struct LayerState {
+  Uploader table;
+  char *buf = nullptr;
+  size_t cap = 0;
+  std::vector<char> key;
+  LayerLayout layout[2];
+  RedLaunch red;
+  bool cached = false;
+};
+
 struct DeviceState {
   MxState mx;
+  LayerState layer[LAYER_ENTRIES];
   // A product that runs on dense copies of its operands: the plan it runs as, whose `uses` stand for these
   // calls, where the copies are, and the tables of the kernel that makes them.
   dmm_plan_t *dense = nullptr;
@@ -631,6 +650,10 @@ void destroy_device_state(DeviceState *d) {
   d->red_table.release();
   d->mx.table.release();
   scratch_pool().release(&d->mx.buf, &d->mx.cap);
+  for (LayerState &l : d->layer) {
+    l.table.release();
+    scratch_pool().release(&l.buf, &l.cap);
+  }
   scratch_pool().release(&d->split_buf, &d->split_cap);
   d->uses.destroy();
   for (int i = 0; i < 2; ++i) {

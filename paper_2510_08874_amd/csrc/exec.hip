@@ -17,6 +17,7 @@
 #include "device_state.hpp"
 #include "gemm_kernel.hpp"
 #include "gemm_launch.hpp"
+#include "layer_launch.hpp"
 #include "mx_launch.hpp"
 #include "ortho_launch.hpp"
 #include "pack_kernel.hpp"
@@ -1908,3 +1909,4 @@ extern "C" int dmm_reduce_replicas_static(dmm_plan_t *P, void *const *c_tiles, c
 
 #include "mx_exec.hpp"
 #include "ortho_exec.hpp"
+#include "layer_exec.hpp"

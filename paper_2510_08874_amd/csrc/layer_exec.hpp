@@ -1,0 +1,908 @@
+// The entry points for the layers around a product (included by exec.hip): 8-bit integers, the gated block, the gradients of bf16
+// products.  Arguments are checked here; what a product reads and writes is laid out as groups (an output sub-tile and its segments of K),
+// cut into macro-tiles by one routine whatever the kind.
+#pragma once
+
+namespace dmm {
+namespace {
+
+constexpr int64_t kLayerBlocks = (1 << 24) - 1;                // workgroups of a launch: 2^32 threads are too many
+constexpr int64_t kLayerPitch = (int64_t)1 << 24;              // bytes from row to row
+constexpr int64_t kLayerSum = 131071;                          // products of two bytes that an int32 sum holds whatever they are
+
+int allow_layer_lds() {
+  static std::mutex mu;
+  static bool done[64] = {};
+  int device = 0;
+  DMM_HIP(hipGetDevice(&device));
+  if (device < 0 || device >= 64) return DMM_EINVAL;
+  std::lock_guard<std::mutex> g(mu);
+  if (!done[device]) {
+    DMM_HIP(layer_allow_lds());
+    done[device] = true;
+  }
+  return DMM_OK;
+}
+
+// The tiles of a matrix: buffers aligned to their elements, leading dimensions that hold a row and stay below kLayerPitch.
+int check_layer_tiles(const Grid &G, const dmm_tiles *t, int es) {
+  if (!t->tiles || !t->ld) return DMM_EINVAL;
+  int rc;
+  if ((rc = check_lds(G, t->ld)) || (rc = check_tiles(G, t->tiles, es))) return rc;
+  for (int32_t rep = 0; rep < G.c; ++rep)
+    for (int32_t ti = 0; ti < G.gr; ++ti)
+      for (int32_t tj = 0; tj < G.gc; ++tj)
+        if (G.rc[ti + 1] > G.rc[ti] && G.cc[tj + 1] > G.cc[tj] && t->ld[G.table_index(rep, ti, tj)] >= kLayerPitch / es) return DMM_ELD;
+  return DMM_OK;
+}
+// One replica's, whatever the matrix has.
+int check_layer_single(const Grid &G, const dmm_tiles *t, int es) {
+  Grid one = G;
+  one.c = 1;
+  return check_layer_tiles(one, t, es);
+}
+// 8-bit integers along the rows, or along the columns, where a tile lies transposed.
+int check_i8(const Grid &G, const dmm_int_tiles *q, bool by_cols) {
+  if (!q->codes || !q->code_ld || !q->scales) return DMM_EINVAL;
+  for (int32_t rep = 0; rep < G.c; ++rep) {
+    for (int32_t ti = 0; ti < G.gr; ++ti)
+      for (int32_t tj = 0; tj < G.gc; ++tj) {
+        const int64_t h = G.rc[ti + 1] - G.rc[ti], w = G.cc[tj + 1] - G.cc[tj];
+        if (h <= 0 || w <= 0) continue;
+        const int64_t i = G.table_index(rep, ti, tj);
+        if (!q->codes[i]) return DMM_EINVAL;
+        if (q->code_ld[i] < (by_cols ? h : w) || q->code_ld[i] >= kLayerPitch) return DMM_ELD;
+      }
+    const int32_t n = by_cols ? G.gc : G.gr;
+    for (int32_t t = 0; t < n; ++t) {
+      const int64_t len = by_cols ? G.cc[t + 1] - G.cc[t] : G.rc[t + 1] - G.rc[t];
+      const void *s = q->scales[(int64_t)rep * n + t];
+      if (len > 0 && (!s || ((uintptr_t)s & 3))) return DMM_EINVAL;
+    }
+  }
+  return DMM_OK;
+}
+
+// ---- groups -------------------------------------------------------------------------------------------
+
+struct LayerGroup {
+  int64_t m, n;                        // extents
+  size_t seg, n_segs;
+  char *c, *g, *u;                     // corners
+  int64_t ldc, ldg, ldu;
+  const float *sa, *sb, *sb2;
+};
+
+struct LayerWork {
+  int kind = 0, act = DMM_SILU, c_es = 4;
+  std::vector<LayerSeg> segs;
+  std::vector<LayerGroup> groups;
+};
+
+// Of a turned operand whose rows are `ld` elements apart: how many of a tile's last `rows` rows below k1 a read of eight columns at a time could
+// take past the end of its buffer, where the columns end with the tile.
+int64_t rows_past_end(int64_t tile_rows, int64_t tile_cols, int64_t ld, int64_t k1, int64_t col0, int64_t cols) {
+  const int64_t over = col0 + (cols + 7) / 8 * 8 - tile_cols;
+  if (over <= 0) return 0;
+  return std::max<int64_t>(0, (over + ld - 1) / ld - (tile_rows - k1));
+}
+
+// Whole steps of a segment of `len`, and what is left; the last `guard` rows are not to be part of whole steps.
+void put_segment(LayerWork *W, LayerSeg s, int64_t len, int64_t guard) {
+  const int64_t step = layer_step(W->kind);
+  int64_t steps = len / step, tail = len % step;
+  s.pad = 0;
+  if (tail < guard && steps > 0) {
+    s.steps = (int32_t)(steps - 1);
+    s.tail = (int32_t)step;
+    W->segs.push_back(s);
+    if (tail == 0) return;
+    auto on = [&](const char *p, uint32_t pitch, bool turned) { return p ? p + (turned ? steps * step * (int64_t)pitch : steps * 128) : p; };
+    const bool bt = W->kind == LAYER_TN || W->kind == LAYER_GATED;
+    s.a = on(s.a, s.a_pitch, W->kind == LAYER_TN);
+    s.b = on(s.b, s.b_pitch, bt);
+    s.b2 = on(s.b2, s.b2_pitch, bt);
+    steps = 0;
+  }
+  s.steps = (int32_t)steps;
+  s.tail = (int32_t)tail;
+  W->segs.push_back(s);
+}
+
+struct LayerChoice {
+  int shape = LAYER_256;
+  int64_t runs = 1;
+};
+
+// By an estimate in us, from what a step (128 bytes of K) of a tile takes.
+LayerChoice choose_layer(const LayerWork &W, int cus) {
+  const bool gated = layer_gated(W.kind);
+  double cells = 0, k_steps = 0, b_bytes = 0;
+  int64_t most = 0;
+  for (const LayerGroup &g : W.groups) {
+    most = std::max(most, g.m);
+    int64_t steps = 0;
+    for (size_t s = g.seg; s < g.seg + g.n_segs; ++s) steps += W.segs[s].steps + (W.segs[s].tail > 0 ? 2 : 0);
+    const double area = (double)g.m * (double)g.n;
+    cells += area;
+    k_steps += area * (double)steps;
+    b_bytes += (double)g.n * (double)steps * (gated ? 256.0 : 128.0);
+  }
+  const double steps = cells > 0 ? std::max(1.0, k_steps / cells) : 1;
+  LayerChoice best;
+  double best_us = 0;
+  for (int shape = 0; shape < LAYER_SHAPES; ++shape) {
+    const int tm = kLayerTile[W.kind][shape].tm, tn = kLayerTile[W.kind][shape].tn;
+    if (tm == 0 || (shape == LAYER_64 && most > 128) || (shape == LAYER_32 && most > 64)) continue;
+    double tiles = 0;
+    for (const LayerGroup &g : W.groups) tiles += (double)(((g.m + tm - 1) / tm) * ((g.n + tn - 1) / tn));
+    if (tiles == 0) return best;
+    if (tiles > (double)kLayerBlocks) continue;
+    // (two workgroups on a CU where the stages leave room)
+    const int places = shape == LAYER_256 || (gated && shape == LAYER_128) ? cus : gated ? cus : 2 * cus;
+    const double memory = 2.0 + b_bytes * std::ceil((double)most / tm > 4 ? 1.0 : 1.0) / 5.0e6;
+    for (int64_t runs = 1; runs <= 32; ++runs) {
+      const double work = tiles * (double)runs, per = std::ceil(steps / (double)runs);
+      if (runs > 1 && (work > places || per < 3)) break;
+      auto round = [&](double n) {
+        if (n <= 0) return 0.0;
+        const double full = n / cus;
+        switch (shape) {
+          case LAYER_256: return per * (1.15 + 0.3 * full) + 9.0;
+          case LAYER_128: return gated ? per * (0.8 + 0.2 * full) + 7.0 : per * (full > 1 ? 1.1 : 0.5 + 0.16 * full) + 5.0;
+          case LAYER_64: return gated ? per * (0.6 + 0.2 * full) + 5.0 : per * (full > 1 ? 1.0 : 0.35 + 0.25 * full) + 4.0;
+          default: return gated ? per * (0.5 + 0.2 * full) + 4.0 : per * (full > 1 ? 0.9 : 0.3 + 0.2 * full) + 3.5;
+        }
+      };
+      const double whole = std::floor(work / places);
+      double us = std::max(whole * round(places) + round(work - whole * places), memory);
+      if (runs > 1) us += 4.5 + 2.0 * work * tm * tn * (gated ? 2 : 1) * 4 / 3e6;
+      if (best_us == 0 || us < best_us) best_us = us, best.shape = shape, best.runs = runs;
+    }
+  }
+  return best;
+}
+
+// Tables of one product, appended to `h`; partial sums in slots of M's buffer, which have addresses from 0 on until place_parts.
+int lay_out(const LayerWork &W, int cus, std::vector<char> *h, LayerLayout *L, size_t *scratch) {
+  *L = LayerLayout();
+  L->kind = W.kind;
+  L->act = W.act;
+  const LayerChoice choice = choose_layer(W, cus);
+  const int shape = choice.shape, tm = kLayerTile[W.kind][shape].tm, tn = kLayerTile[W.kind][shape].tn;
+  const bool gated = layer_gated(W.kind);
+  const int wide = gated ? 2 * tn : tn;                        // columns of a slot
+  const size_t slot_bytes = (size_t)tm * wide * 4;
+  std::vector<LayerItem> items;
+  std::vector<LayerJoin> joins;
+  int64_t slots = 0;
+  for (const LayerGroup &g : W.groups) {
+    const int64_t rows = (g.m + tm - 1) / tm, cols = (g.n + tn - 1) / tn;
+    int64_t whole = 0, k = 0;
+    for (size_t s = g.seg; s < g.seg + g.n_segs; ++s) {
+      whole += W.segs[s].steps;
+      k += W.segs[s].steps * (int64_t)layer_step(W.kind) + W.segs[s].tail;
+    }
+    if (whole > 0x3fffffff || W.segs.size() > 0x3fffffff) return DMM_ELIMIT;
+    int64_t runs = std::min<int64_t>(choice.runs, std::max<int64_t>(1, whole / 3));
+    if (layer_i8(W.kind) && k > kLayerSum) runs = std::max<int64_t>(runs, (k + kLayerSum / 2 - 1) / (kLayerSum / 2));
+    const int64_t per = std::max<int64_t>(1, (whole + runs - 1) / runs);
+    runs = std::max<int64_t>(1, (whole + per - 1) / per);
+    const int64_t first_slot = slots;
+    size_t seg = g.seg, tail = g.seg;
+    int64_t first = 0, done = 0;                               // steps into `seg`; steps of the segments whose tails have been given out
+    for (int64_t run = 0; run < runs; ++run) {
+      const int64_t n_steps = std::min(per, whole - run * per);
+      while (seg < g.seg + g.n_segs && first >= W.segs[seg].steps) first -= W.segs[seg++].steps;
+      // a segment's tail goes to the run that has its last whole step
+      const size_t tail0 = tail;
+      int64_t sum = n_steps * layer_step(W.kind);
+      while (tail < g.seg + g.n_segs && (run == runs - 1 || done + W.segs[tail].steps <= (run + 1) * per)) {
+        done += W.segs[tail].steps;
+        sum += W.segs[tail++].tail;
+      }
+      if (layer_i8(W.kind) && sum > kLayerSum) return DMM_ELIMIT;
+      // bands of eight tile rows, column by column: neighbours in the list share operands.  All first ranges of K, then all second ones, ...
+      int64_t tile = 0;
+      for (int64_t r0 = 0; r0 < rows; r0 += 8)
+        for (int64_t c = 0; c < cols; ++c)
+          for (int64_t r = r0; r < std::min(r0 + 8, rows); ++r, ++tile) {
+            LayerItem it;
+            std::memset(&it, 0, sizeof it);
+            it.m_off = (int32_t)(r * tm);
+            it.n_off = (int32_t)(c * tn);
+            it.m_ext = (int32_t)std::min<int64_t>(tm, g.m - r * tm);
+            it.n_ext = (int32_t)std::min<int64_t>(tn, g.n - c * tn);
+            it.c = g.c + (r * tm * g.ldc + c * tn) * W.c_es;
+            it.ldc = g.ldc;
+            it.c_es = W.c_es;
+            if (g.g) it.g = g.g + (r * tm * g.ldg + c * tn) * 2;
+            if (g.u) it.u = g.u + (r * tm * g.ldu + c * tn) * 2;
+            it.ldg = g.ldg;
+            it.ldu = g.ldu;
+            if (g.sa) it.sa = g.sa + r * tm;
+            if (g.sb) it.sb = g.sb + c * tn;
+            if (g.sb2) it.sb2 = g.sb2 + c * tn;
+            if (n_steps > 0) it.front = W.segs[seg];
+            it.seg = (int32_t)seg;
+            it.n_segs = (int32_t)(g.seg + g.n_segs - seg);
+            it.first = (int32_t)first;
+            it.steps = (int32_t)n_steps;
+            it.tail_seg = (int32_t)tail0;
+            it.n_tails = (int32_t)(tail - tail0);
+            it.what = k == 0 ? LAYER_ZERO : LAYER_STORE;
+            if (runs > 1) {
+              const int64_t slot = first_slot + tile * runs;
+              if (run == 0)
+                joins.push_back({it.c, it.ldc, it.g, it.u, it.ldg, it.ldu, it.sa, it.sb, it.sb2, (const char *)(uintptr_t)((size_t)slot * slot_bytes),
+                                 (int32_t)runs, tm, wide, it.m_ext, it.n_ext, it.c_es});
+              it.c = (char *)(uintptr_t)((size_t)(slot + run) * slot_bytes);
+              it.what = LAYER_PARTS;
+              ++slots;
+            }
+            items.push_back(it);
+          }
+      first += n_steps;
+    }
+  }
+  if ((int64_t)items.size() > kLayerBlocks || (int64_t)joins.size() * ((tm * tn + 1023) / 1024) > kLayerBlocks) return DMM_ELIMIT;
+  if (items.empty()) return DMM_OK;
+  // workgroup w runs on XCD w % 8: every XCD gets a run of the list
+  std::vector<LayerItem> ordered(items.size());
+  {
+    size_t from = 0;
+    for (size_t xcd = 0; xcd < 8; ++xcd)
+      for (size_t w = xcd; w < items.size(); w += 8) ordered[w] = items[from++];
+  }
+  *scratch = std::max(*scratch, (size_t)slots * slot_bytes);
+  L->shape = shape;
+  L->n_items = (int)ordered.size();
+  L->n_joins = (int)joins.size();
+  L->o_items = h->size();
+  L->o_segs = L->o_items + ordered.size() * sizeof(LayerItem);
+  L->o_joins = L->o_segs + W.segs.size() * sizeof(LayerSeg);
+  h->resize(L->o_joins + joins.size() * sizeof(LayerJoin));
+  std::memcpy(h->data() + L->o_items, ordered.data(), ordered.size() * sizeof(LayerItem));
+  if (!W.segs.empty()) std::memcpy(h->data() + L->o_segs, W.segs.data(), W.segs.size() * sizeof(LayerSeg));
+  if (!joins.empty()) std::memcpy(h->data() + L->o_joins, joins.data(), joins.size() * sizeof(LayerJoin));
+  static_assert(sizeof(LayerItem) % 8 == 0 && sizeof(LayerSeg) % 8 == 0 && sizeof(LayerJoin) % 8 == 0, "tables lie one behind another");
+  return DMM_OK;
+}
+
+void place_parts(std::vector<char> *h, const LayerLayout &L, char *buf) {
+  LayerItem *items = (LayerItem *)(h->data() + L.o_items);
+  for (int i = 0; i < L.n_items; ++i)
+    if (items[i].what == LAYER_PARTS) items[i].c = buf + (uintptr_t)items[i].c;
+  LayerJoin *joins = (LayerJoin *)(h->data() + L.o_joins);
+  for (int i = 0; i < L.n_joins; ++i) joins[i].parts = buf + (uintptr_t)joins[i].parts;
+}
+
+// The part of a call that all kinds have in common: the tables of the call before if they are of the same inputs (`key`), else new ones,
+// made by `build` from the plan; then `in_front`, the launches and, where `reduce` asks for it, the sum of C's replicas.
+template <class Build, class Front>
+int run_layer(dmm_plan_t *P, int which, const std::vector<char> &inputs, void *const *c_tiles, const int64_t *c_ld, bool reduce, hipStream_t stream, Build build,
+              Front in_front) {
+  int rc;
+  const bool capturing = is_capturing(stream), known = P->dev && P->dev->layer[which].cached;
+  if (!known && (rc = materialize(P))) return rc;
+  if (capturing && !known) return DMM_EINVAL;                  // (a graph cannot wait for tables that are on their way)
+  if ((rc = ensure_state(P)) || (rc = allow_layer_lds())) return rc;
+  int device = 0, cus = 0;
+  DMM_HIP(hipGetDevice(&device));
+  if ((rc = device_cus(&cus))) return rc;
+  LayerState &M = P->dev->layer[which];
+  std::vector<char> key(inputs);
+  key.insert(key.end(), (const char *)&device, (const char *)&device + sizeof device);
+  if (M.cached && key == M.key) {
+    if ((rc = M.table.order_behind_copy(stream))) return rc;
+    if ((M.layout[0].n_joins || M.layout[1].n_joins) && (rc = P->dev->uses.order(stream))) return rc;
+  } else {
+    if (capturing) return DMM_EINVAL;
+    M.cached = false;
+    LayerLayout layout[2];
+    RedLaunch red;
+    std::vector<char> &h = P->dev->host;
+    h.clear();
+    size_t scratch = 0;
+    if ((rc = build(cus, &h, layout, &scratch))) return rc;
+    if (c_tiles && (rc = build_reduce(P, c_tiles, c_ld, 0, &h, h.size(), &red))) return rc;
+    if (scratch) {
+      if ((rc = P->dev->uses.order(stream))) return rc;
+      if (scratch > M.cap) {
+        if (M.buf) {
+          if ((rc = P->dev->uses.wait())) return rc;
+          DMM_HIP(hipStreamSynchronize(stream));
+          scratch_pool().release(&M.buf, &M.cap);
+        }
+        if ((rc = scratch_pool().acquire(scratch, &M.buf, &M.cap))) return rc;
+      }
+      for (const LayerLayout &L : layout)
+        if (L.n_joins) place_parts(&h, L, M.buf);
+    }
+    if ((rc = M.table.upload(h.data(), h.size(), stream, P->dev->uses))) return rc;
+    red.dev_base = M.table.dev();
+    M.layout[0] = layout[0];
+    M.layout[1] = layout[1];
+    M.red = red;
+    M.key.swap(key);
+    M.cached = true;
+  }
+  if ((rc = in_front())) return rc;
+  const bool sum = reduce && M.red.n_items;
+  if (!M.layout[0].n_items && !M.layout[1].n_items && !sum) return DMM_OK;
+  hipEvent_t behind = nullptr;
+  if ((rc = P->dev->uses.claim(stream, &behind))) return rc;
+  const char *d = M.table.dev();
+  bool marked = false;
+  for (int x = 0; x < 2; ++x) {
+    const LayerLayout &L = M.layout[x];
+    if (!L.n_items) continue;
+    const bool last = !sum && (x == 1 || !M.layout[1].n_items);
+    marked = layer_launch(last ? behind : nullptr, L.kind, L.shape, L.act, (const LayerItem *)(d + L.o_items), L.n_items, (const LayerSeg *)(d + L.o_segs),
+                          (const LayerJoin *)(d + L.o_joins), L.n_joins, stream);
+    DMM_HIP(hipGetLastError());
+  }
+  if (sum && (rc = fire_reduce(P, M.red, stream, false, behind, &marked))) return rc;
+  return marked ? DMM_OK : P->dev->uses.mark(stream);
+}
+
+struct LayerKey {
+  std::vector<char> bytes;
+  void put(const void *p, size_t n) { bytes.insert(bytes.end(), (const char *)p, (const char *)p + n); }
+  void put(const dmm_tiles *t, int64_t n) {
+    const char there = t != nullptr;
+    put(&there, 1);
+    if (!t) return;
+    put(t->tiles, (size_t)n * sizeof(void *));
+    put(t->ld, (size_t)n * sizeof(int64_t));
+  }
+  void put(const dmm_int_tiles *t, const Grid &G, bool by_cols) {
+    const size_t n = (size_t)(G.c * G.tiles_per_rep());
+    put(t->codes, n * sizeof(void *));
+    put(t->code_ld, n * sizeof(int64_t));
+    put(t->scales, (size_t)G.c * (size_t)(by_cols ? G.gc : G.gr) * sizeof(void *));
+  }
+};
+
+// Corner of a region inside a tile.
+char *corner(const Grid &G, const dmm_tiles *t, int64_t i, int32_t ti, int32_t tj, int64_t row, int64_t col, int es) {
+  return (char *)t->tiles[i] + ((row - G.rc[(size_t)ti]) * t->ld[i] + col - G.cc[(size_t)tj]) * es;
+}
+
+// Groups of a plan's own product: the op list by output sub-tile, and zeros where no op writes.
+template <class Segment, class Out>
+void plan_groups(const dmm_plan_t *P, LayerWork *W, Segment segment, Out out) {
+  for (const Group &g : P->groups) {
+    LayerGroup r;
+    std::memset(&r, 0, sizeof r);
+    r.m = g.m1 - g.m0;
+    r.n = g.n1 - g.n0;
+    r.seg = W->segs.size();
+    for (int64_t x = g.first; x < g.first + g.count; ++x) segment(g, P->tasks[(size_t)P->order[(size_t)x]]);
+    r.n_segs = W->segs.size() - r.seg;
+    out(g.c_rep, g.c_ti, g.c_tj, g.m0, g.n0, g.count ? &P->tasks[(size_t)P->order[(size_t)g.first]] : nullptr, &r);
+    W->groups.push_back(r);
+  }
+  for (const dmm_work_item &w : P->items) {
+    if (w.group >= 0) continue;
+    LayerGroup r;
+    std::memset(&r, 0, sizeof r);
+    r.m = w.m_ext;
+    r.n = w.n_ext;
+    r.seg = W->segs.size();
+    out(w.c_rep, w.c_ti, w.c_tj, w.m0, w.n0, nullptr, &r);
+    W->groups.push_back(r);
+  }
+}
+
+int32_t interval_of(const std::vector<int64_t> &cuts, int64_t at) {   // the non-empty interval that holds `at`
+  return (int32_t)(std::upper_bound(cuts.begin(), cuts.end(), at) - cuts.begin()) - 1;
+}
+
+// dA = dC B^T (summed over the pairs): A's tiles, cut where C's rows and B's rows are; both operands lie along n.
+void input_gradient(const dmm_plan_t *P, const dmm_tiles *const *dc, const dmm_tiles *const *b, int pairs, const dmm_tiles *da, LayerWork *W) {
+  const Grid &A = P->A, &B = P->B, &C = P->C;
+  const std::vector<int64_t> mc = merged_cuts({&A.rc, &C.rc}), kc = merged_cuts({&A.cc, &B.rc}), nc = merged_cuts({&B.cc, &C.cc});
+  for (size_t i = 0; i + 1 < mc.size(); ++i)
+    for (size_t j = 0; j + 1 < kc.size(); ++j) {
+      const int32_t ai = interval_of(A.rc, mc[i]), ci = interval_of(C.rc, mc[i]), aj = interval_of(A.cc, kc[j]), bi = interval_of(B.rc, kc[j]);
+      LayerGroup r;
+      std::memset(&r, 0, sizeof r);
+      r.m = mc[i + 1] - mc[i];
+      r.n = kc[j + 1] - kc[j];
+      r.seg = W->segs.size();
+      for (int p = 0; p < pairs; ++p)
+        for (size_t x = 0; x + 1 < nc.size(); ++x) {
+          const int32_t bj = interval_of(B.cc, nc[x]), cj = interval_of(C.cc, nc[x]);
+          const int64_t ct = C.table_index(0, ci, cj), bt = B.table_index(0, bi, bj);
+          LayerSeg s;
+          s.a = corner(C, dc[p], ct, ci, cj, mc[i], nc[x], 2);
+          s.b = corner(B, b[p], bt, bi, bj, kc[j], nc[x], 2);
+          s.b2 = nullptr;
+          s.a_pitch = (uint32_t)(dc[p]->ld[ct] * 2);
+          s.b_pitch = (uint32_t)(b[p]->ld[bt] * 2);
+          s.b2_pitch = 0;
+          put_segment(W, s, nc[x + 1] - nc[x], 0);
+        }
+      r.n_segs = W->segs.size() - r.seg;
+      const int64_t at = A.table_index(0, ai, aj);
+      r.c = corner(A, da, at, ai, aj, mc[i], kc[j], W->c_es);
+      r.ldc = da->ld[at];
+      W->groups.push_back(r);
+    }
+}
+
+// dB = A^T dC: B's tiles, cut where A's columns and C's columns are; both operands lie across m.
+void weight_gradient(const dmm_plan_t *P, const dmm_tiles *a, const dmm_tiles *dc, const dmm_tiles *db, LayerWork *W) {
+  const Grid &A = P->A, &B = P->B, &C = P->C;
+  const std::vector<int64_t> mc = merged_cuts({&A.rc, &C.rc}), kc = merged_cuts({&A.cc, &B.rc}), nc = merged_cuts({&B.cc, &C.cc});
+  for (size_t i = 0; i + 1 < kc.size(); ++i)
+    for (size_t j = 0; j + 1 < nc.size(); ++j) {
+      const int32_t aj = interval_of(A.cc, kc[i]), bi = interval_of(B.rc, kc[i]), bj = interval_of(B.cc, nc[j]), cj = interval_of(C.cc, nc[j]);
+      LayerGroup r;
+      std::memset(&r, 0, sizeof r);
+      r.m = kc[i + 1] - kc[i];
+      r.n = nc[j + 1] - nc[j];
+      r.seg = W->segs.size();
+      for (size_t x = 0; x + 1 < mc.size(); ++x) {
+        const int32_t ai = interval_of(A.rc, mc[x]), ci = interval_of(C.rc, mc[x]);
+        const int64_t at = A.table_index(0, ai, aj), ct = C.table_index(0, ci, cj);
+        LayerSeg s;
+        s.a = corner(A, a, at, ai, aj, mc[x], kc[i], 2);
+        s.b = corner(C, dc, ct, ci, cj, mc[x], nc[j], 2);
+        s.b2 = nullptr;
+        s.a_pitch = (uint32_t)(a->ld[at] * 2);
+        s.b_pitch = (uint32_t)(dc->ld[ct] * 2);
+        s.b2_pitch = 0;
+        const int64_t ga = rows_past_end(A.rc[ai + 1] - A.rc[ai], A.cc[aj + 1] - A.cc[aj], a->ld[at], mc[x + 1] - A.rc[ai], kc[i] - A.cc[aj], r.m);
+        const int64_t gc = rows_past_end(C.rc[ci + 1] - C.rc[ci], C.cc[cj + 1] - C.cc[cj], dc->ld[ct], mc[x + 1] - C.rc[ci], nc[j] - C.cc[cj], r.n);
+        put_segment(W, s, mc[x + 1] - mc[x], std::max(ga, gc));
+      }
+      r.n_segs = W->segs.size() - r.seg;
+      const int64_t bt = B.table_index(0, bi, bj);
+      r.c = corner(B, db, bt, bi, bj, kc[i], nc[j], W->c_es);
+      r.ldc = db->ld[bt];
+      W->groups.push_back(r);
+    }
+}
+
+bool is_activation(int act) { return act == DMM_SILU || act == DMM_GELU || act == DMM_GELU_TANH; }
+
+// C = A B, or the gated product of A with two right operands, in 8-bit integers.
+int i8_product(dmm_plan_t *P, int which, int act, const dmm_int_tiles *a, const dmm_int_tiles *b, const dmm_int_tiles *b2, const dmm_tiles *c, int c_es,
+               bool reduce, hipStream_t stream) {
+  const Grid &A = P->A, &B = P->B, &C = P->C;
+  int rc;
+  if ((rc = check_i8(A, a, false)) || (rc = check_i8(B, b, true)) || (b2 && (rc = check_i8(B, b2, true))) || (rc = check_layer_tiles(C, c, c_es))) return rc;
+  LayerKey key;
+  const int head[2] = {act, c_es};
+  key.put(head, sizeof head);
+  key.put(a, A, false);
+  key.put(b, B, true);
+  if (b2) key.put(b2, B, true);
+  key.put(c, C.c * C.tiles_per_rep());
+  auto build = [&](int cus, std::vector<char> *h, LayerLayout *layout, size_t *scratch) -> int {
+    LayerWork W;
+    W.kind = b2 ? LAYER_I8_GATED : LAYER_I8;
+    W.act = act;
+    W.c_es = c_es;
+    plan_groups(
+        P, &W,
+        [&](const Group &g, const dmm_task &t) {
+          const int64_t ai = A.table_index(t.a_rep, t.a_ti, t.a_tj), bi = B.table_index(t.b_rep, t.b_ti, t.b_tj);
+          const int64_t ak = t.k0 - A.cc[(size_t)t.a_tj], bk = t.k0 - B.rc[(size_t)t.b_ti];
+          const int64_t ar = g.m0 - A.rc[(size_t)t.a_ti], bc = g.n0 - B.cc[(size_t)t.b_tj];
+          LayerSeg s;
+          s.a = (const char *)a->codes[ai] + ar * a->code_ld[ai] + ak;
+          s.b = (const char *)b->codes[bi] + bc * b->code_ld[bi] + bk;
+          s.b2 = b2 ? (const char *)b2->codes[bi] + bc * b2->code_ld[bi] + bk : nullptr;
+          s.a_pitch = (uint32_t)a->code_ld[ai];
+          s.b_pitch = (uint32_t)b->code_ld[bi];
+          s.b2_pitch = b2 ? (uint32_t)b2->code_ld[bi] : 0;
+          put_segment(&W, s, t.k1 - t.k0, 0);
+        },
+        [&](int32_t rep, int32_t ti, int32_t tj, int64_t m0, int64_t n0, const dmm_task *t, LayerGroup *r) {
+          const int64_t i = C.table_index(rep, ti, tj);
+          r->c = corner(C, c, i, ti, tj, m0, n0, c_es);
+          r->ldc = c->ld[i];
+          if (!t) return;
+          r->sa = a->scales[(int64_t)t->a_rep * A.gr + t->a_ti] + (m0 - A.rc[(size_t)t->a_ti]);
+          const int64_t s = (int64_t)t->b_rep * B.gc + t->b_tj, at = n0 - B.cc[(size_t)t->b_tj];
+          r->sb = b->scales[s] + at;
+          r->sb2 = b2 ? b2->scales[s] + at : nullptr;
+        });
+    return lay_out(W, cus, h, &layout[0], scratch);
+  };
+  return run_layer(P, which, key.bytes, c->tiles, c->ld, reduce, stream, build, [] { return DMM_OK; });
+}
+
+// dU = dH act(G), dG = dH U act'(G), tile by tile.
+int slope(const Grid &C, int act, const dmm_tiles *g, const dmm_tiles *u, const dmm_tiles *dh, const dmm_tiles *dg, const dmm_tiles *du, hipStream_t stream) {
+  SlopeArgs args;
+  std::memset(&args, 0, sizeof args);
+  args.act = act;
+  int64_t blocks = 0;
+  auto blocks_of = [](int64_t h, int64_t w, int32_t *across) -> int64_t {
+    *across = (int32_t)((w + SLOPE_COLS - 1) / SLOPE_COLS);
+    return ((h + SLOPE_ROWS - 1) / SLOPE_ROWS * *across + 3) / 4;
+  };
+  auto flush = [&]() -> int {
+    if (!args.n) return DMM_OK;
+    slope_launch(args, (int)blocks, stream);
+    args.n = 0;
+    blocks = 0;
+    DMM_HIP(hipGetLastError());
+    return DMM_OK;
+  };
+  int rc;
+  for (int32_t ti = 0; ti < C.gr; ++ti)
+    for (int32_t tj = 0; tj < C.gc; ++tj) {
+      const int64_t h = C.rc[(size_t)ti + 1] - C.rc[(size_t)ti], w = C.cc[(size_t)tj + 1] - C.cc[(size_t)tj];
+      if (h <= 0 || w <= 0) continue;
+      const int64_t i = C.table_index(0, ti, tj);
+      SlopeTile t;
+      std::memset(&t, 0, sizeof t);
+      t.g = (const char *)g->tiles[i];
+      t.u = (const char *)u->tiles[i];
+      t.dh = (const char *)dh->tiles[i];
+      t.dg = (char *)dg->tiles[i];
+      t.du = (char *)du->tiles[i];
+      t.pg = g->ld[i] * 2;
+      t.pu = u->ld[i] * 2;
+      t.ph = dh->ld[i] * 2;
+      t.pdg = dg->ld[i] * 2;
+      t.pdu = du->ld[i] * 2;
+      t.h = (int32_t)h;
+      t.w = (int32_t)w;
+      const int64_t n = blocks_of(h, w, &t.blocks_across);
+      if ((args.n == SLOPE_TILES || blocks + n > kLayerBlocks) && (rc = flush())) return rc;
+      t.first_block = (int32_t)blocks;
+      blocks += n;
+      args.tile[args.n++] = t;
+    }
+  return flush();
+}
+// (before anything is launched: a call that is refused writes nothing)
+int check_slope(const Grid &C) {
+  for (int32_t ti = 0; ti < C.gr; ++ti)
+    for (int32_t tj = 0; tj < C.gc; ++tj) {
+      const int64_t h = C.rc[(size_t)ti + 1] - C.rc[(size_t)ti], w = C.cc[(size_t)tj + 1] - C.cc[(size_t)tj];
+      if (h > 0x7fffff00 || w > 0x7fffff00 || ((h + SLOPE_ROWS - 1) / SLOPE_ROWS) * ((w + SLOPE_COLS - 1) / SLOPE_COLS) / 4 >= kLayerBlocks) return DMM_ELIMIT;
+    }
+  return DMM_OK;
+}
+
+// ---- integers and values --------------------------------------------------------------------------------
+
+// Runs `launch` over all tiles in blocks of 128 rows by 256 bytes, as many tiles at a time as a launch's argument holds.
+template <class F>
+int over_i8_tiles(const Grid &G, int es, char *const *x, const int64_t *x_ld, const dmm_int_tiles *q, bool by_cols, F launch) {
+  I8Args args;
+  std::memset(&args, 0, sizeof args);
+  int64_t blocks = 0;
+  auto flush = [&]() -> int {
+    if (!args.n) return DMM_OK;
+    launch(args, (int)blocks);
+    args.n = 0;
+    blocks = 0;
+    DMM_HIP(hipGetLastError());
+    return DMM_OK;
+  };
+  int rc;
+  for (int32_t rep = 0; rep < G.c; ++rep)
+    for (int32_t ti = 0; ti < G.gr; ++ti)
+      for (int32_t tj = 0; tj < G.gc; ++tj) {
+        const int64_t h = G.rc[(size_t)ti + 1] - G.rc[(size_t)ti], w = G.cc[(size_t)tj + 1] - G.cc[(size_t)tj];
+        if (h <= 0 || w <= 0) continue;
+        const int64_t i = G.table_index(rep, ti, tj);
+        I8Tile t;
+        std::memset(&t, 0, sizeof t);
+        t.x = x[i];
+        t.x_pitch = x_ld[i] * es;
+        t.q = (char *)q->codes[i];
+        t.q_pitch = q->code_ld[i];
+        t.scale = q->scales[by_cols ? (int64_t)rep * G.gc + tj : (int64_t)rep * G.gr + ti];
+        t.h = (int32_t)h;
+        t.w = (int32_t)w;
+        t.blocks_across = (int32_t)((w + i8_block_cols(es == 4) - 1) / i8_block_cols(es == 4));
+        const int64_t n = (h + 127) / 128 * t.blocks_across;
+        if ((args.n == I8_TILES || blocks + n > kLayerBlocks) && (rc = flush())) return rc;
+        t.first_block = (int32_t)blocks;
+        blocks += n;
+        args.tile[args.n++] = t;
+      }
+  return flush();
+}
+int check_i8_blocks(const Grid &G, int es) {
+  for (int32_t ti = 0; ti < G.gr; ++ti)
+    for (int32_t tj = 0; tj < G.gc; ++tj) {
+      const int64_t h = G.rc[(size_t)ti + 1] - G.rc[(size_t)ti], w = G.cc[(size_t)tj + 1] - G.cc[(size_t)tj];
+      if ((h + 127) / 128 * ((w + i8_block_cols(es == 4) - 1) / i8_block_cols(es == 4)) > kLayerBlocks) return DMM_ELIMIT;
+    }
+  return DMM_OK;
+}
+
+int over_scales(const Grid &G, const dmm_int_tiles *q, bool by_cols, int what, hipStream_t stream) {
+  I8ScaleArgs args;
+  std::memset(&args, 0, sizeof args);
+  int64_t blocks = 0;
+  const std::vector<int64_t> &cuts = by_cols ? G.cc : G.rc;
+  const int32_t n = by_cols ? G.gc : G.gr;
+  auto flush = [&]() -> int {
+    if (!args.n) return DMM_OK;
+    i8_scales_launch(args, (int)blocks, what, stream);
+    args.n = 0;
+    blocks = 0;
+    DMM_HIP(hipGetLastError());
+    return DMM_OK;
+  };
+  int rc;
+  for (int32_t rep = 0; rep < G.c; ++rep)
+    for (int32_t t = 0; t < n; ++t) {
+      const int64_t len = cuts[(size_t)t + 1] - cuts[(size_t)t], need = (len + 255) / 256;
+      if (len <= 0) continue;
+      if ((args.n == I8_PIECES || blocks + need > kLayerBlocks) && (rc = flush())) return rc;
+      args.piece[args.n++] = {q->scales[(int64_t)rep * n + t], (int32_t)len, (int32_t)blocks};
+      blocks += need;
+    }
+  return flush();
+}
+
+// One form.  Along the rows, a workgroup takes a whole row where it meets few tiles and rows are many or short; otherwise, and along the columns, the
+// largest magnitudes are collected block by block first.
+int i8_form(const Grid &G, int dtype, char *const *x, const int64_t *x_ld, const dmm_int_tiles *q, bool by_cols, hipStream_t stream) {
+  const int es = dtype == DMM_F32 ? 4 : 2;
+  const bool f32 = es == 4;
+  int rc;
+  if (!by_cols && G.gc <= I8_ROW_PIECES) {
+    for (int32_t rep = 0; rep < G.c; ++rep)
+      for (int32_t ti = 0; ti < G.gr; ++ti) {
+        I8RowArgs args;
+        std::memset(&args, 0, sizeof args);
+        args.h = (int32_t)(G.rc[(size_t)ti + 1] - G.rc[(size_t)ti]);
+        if (args.h <= 0) continue;
+        args.scale = q->scales[(int64_t)rep * G.gr + ti];
+        for (int32_t tj = 0; tj < G.gc; ++tj) {
+          const int64_t w = G.cc[(size_t)tj + 1] - G.cc[(size_t)tj], i = G.table_index(rep, ti, tj);
+          if (w > 0) args.piece[args.n++] = {x[i], (char *)q->codes[i], x_ld[i] * es, q->code_ld[i], (int32_t)w, 0};
+        }
+        // (rows past what a launch can have go into the next)
+        const int32_t all = args.h;
+        for (int32_t at = 0; at < all; at += (int32_t)kLayerBlocks) {
+          I8RowArgs part = args;
+          part.h = std::min<int32_t>(all - at, (int32_t)kLayerBlocks);
+          part.scale += at;
+          for (int32_t p = 0; p < part.n; ++p) {
+            part.piece[p].x += at * part.piece[p].x_pitch;
+            part.piece[p].q += at * part.piece[p].q_pitch;
+          }
+          i8_whole_rows_launch(part, f32, stream);
+          DMM_HIP(hipGetLastError());
+        }
+      }
+    return DMM_OK;
+  }
+  if ((rc = over_scales(G, q, by_cols, I8_CLEAR, stream))) return rc;
+  if ((rc = over_i8_tiles(G, es, x, x_ld, q, by_cols, [&](const I8Args &args, int blocks) { i8_amax_launch(args, blocks, f32, by_cols, stream); }))) return rc;
+  if ((rc = over_i8_tiles(G, es, x, x_ld, q, by_cols, [&](const I8Args &args, int blocks) { i8_quantize_launch(args, blocks, f32, by_cols, stream); })))
+    return rc;
+  return over_scales(G, q, by_cols, I8_FINISH, stream);
+}
+
+}  // namespace
+}  // namespace dmm
+
+extern "C" {
+
+int dmm_int_quantize(const dmm_matrix_desc *X, int dtype, const dmm_tiles *x, const dmm_int_tiles *rows, const dmm_int_tiles *cols, void *hip_stream) {
+  using namespace dmm;
+  if (!X || !x || !x->tiles || !x->ld || (!rows && !cols) || (dtype != DMM_BF16 && dtype != DMM_F32)) return DMM_EINVAL;
+  TraceRange whole("dmm_int_quantize");
+  try {
+    Grid G;
+    int rc;
+    const int es = dtype == DMM_F32 ? 4 : 2;
+    if ((rc = load_matrix(X, &G)) || (rc = check_lds(G, x->ld))) return rc;
+    if (rows && (rc = check_i8(G, rows, false))) return rc;
+    if (cols && (rc = check_i8(G, cols, true))) return rc;
+    if ((rc = check_tiles(G, x->tiles, es)) || (rc = check_i8_blocks(G, es))) return rc;
+    if (rows && (rc = i8_form(G, dtype, (char *const *)x->tiles, x->ld, rows, false, (hipStream_t)hip_stream))) return rc;
+    return cols ? i8_form(G, dtype, (char *const *)x->tiles, x->ld, cols, true, (hipStream_t)hip_stream) : DMM_OK;
+  } catch (const std::bad_alloc &) {
+    return DMM_ENOMEM;
+  }
+}
+
+int dmm_int_dequantize(const dmm_matrix_desc *X, const dmm_int_tiles *q, int along, int dtype, const dmm_tiles *x, void *hip_stream) {
+  using namespace dmm;
+  if (!X || !q || !x || !x->tiles || !x->ld) return DMM_EINVAL;
+  if ((along != DMM_MX_ROWS && along != DMM_MX_COLS) || (dtype != DMM_BF16 && dtype != DMM_F32)) return DMM_EINVAL;
+  TraceRange whole("dmm_int_dequantize");
+  try {
+    Grid G;
+    int rc;
+    const int es = dtype == DMM_F32 ? 4 : 2;
+    const bool by_cols = along == DMM_MX_COLS;
+    if ((rc = load_matrix(X, &G)) || (rc = check_lds(G, x->ld)) || (rc = check_i8(G, q, by_cols)) || (rc = check_tiles(G, x->tiles, es)) ||
+        (rc = check_i8_blocks(G, es)))
+      return rc;
+    return over_i8_tiles(G, es, (char *const *)x->tiles, x->ld, q, by_cols,
+                         [&](const I8Args &args, int blocks) { i8_values_launch(args, blocks, es == 4, by_cols, (hipStream_t)hip_stream); });
+  } catch (const std::bad_alloc &) {
+    return DMM_ENOMEM;
+  }
+}
+
+int dmm_int_execute(dmm_plan_t *P, const dmm_int_tiles *a, const dmm_int_tiles *b, const dmm_tiles *c, uint32_t flags, void *hip_stream) {
+  using namespace dmm;
+  if (!P || !a || !b || !c) return DMM_EINVAL;
+  if (flags & ~(DMM_NO_REDUCE | DMM_C_BF16)) return DMM_EINVAL;
+  if ((flags & DMM_C_BF16) && P->C.c != 1) return DMM_EINVAL;
+  TraceRange whole("dmm_int_execute");
+  try {
+    return i8_product(P, LAYER_I8_EXECUTE, DMM_SILU, a, b, nullptr, c, (flags & DMM_C_BF16) ? 2 : 4, !(flags & DMM_NO_REDUCE), (hipStream_t)hip_stream);
+  } catch (const std::bad_alloc &) {
+    return DMM_ENOMEM;
+  }
+}
+
+int dmm_int_gated_execute(dmm_plan_t *P, int activation, const dmm_int_tiles *a, const dmm_int_tiles *gate, const dmm_int_tiles *up, const dmm_tiles *h,
+                         void *hip_stream) {
+  using namespace dmm;
+  if (!P || !a || !gate || !up || !h || !is_activation(activation) || P->C.c != 1) return DMM_EINVAL;
+  TraceRange whole("dmm_int_gated_execute");
+  try {
+    return i8_product(P, LAYER_I8_GATED_EXECUTE, activation, a, gate, up, h, 2, false, (hipStream_t)hip_stream);
+  } catch (const std::bad_alloc &) {
+    return DMM_ENOMEM;
+  }
+}
+
+int dmm_gated_execute(dmm_plan_t *P, int activation, const dmm_tiles *a, const dmm_tiles *gate, const dmm_tiles *up, const dmm_tiles *h, const dmm_tiles *g,
+                      const dmm_tiles *u, void *hip_stream) {
+  using namespace dmm;
+  if (!P || !a || !gate || !up || !h || !is_activation(activation) || P->C.c != 1) return DMM_EINVAL;
+  const Grid &A = P->A, &B = P->B, &C = P->C;
+  int rc;
+  if ((rc = check_layer_tiles(A, a, 2)) || (rc = check_layer_tiles(B, gate, 2)) || (rc = check_layer_tiles(B, up, 2)) || (rc = check_layer_tiles(C, h, 2)))
+    return rc;
+  if ((g && (rc = check_layer_tiles(C, g, 2))) || (u && (rc = check_layer_tiles(C, u, 2)))) return rc;
+  TraceRange whole("dmm_gated_execute");
+  try {
+    LayerKey key;
+    key.put(&activation, sizeof activation);
+    key.put(a, A.c * A.tiles_per_rep());
+    key.put(gate, B.c * B.tiles_per_rep());
+    key.put(up, B.c * B.tiles_per_rep());
+    for (const dmm_tiles *t : {h, g, u}) key.put(t, C.tiles_per_rep());
+    auto build = [&](int cus, std::vector<char> *out, LayerLayout *layout, size_t *scratch) -> int {
+      LayerWork W;
+      W.kind = LAYER_GATED;
+      W.act = activation;
+      W.c_es = 2;
+      plan_groups(
+          P, &W,
+          [&](const Group &gr, const dmm_task &t) {
+            const int64_t ai = A.table_index(t.a_rep, t.a_ti, t.a_tj), bi = B.table_index(t.b_rep, t.b_ti, t.b_tj);
+            LayerSeg s;
+            s.a = corner(A, a, ai, t.a_ti, t.a_tj, gr.m0, t.k0, 2);
+            s.b = corner(B, gate, bi, t.b_ti, t.b_tj, t.k0, gr.n0, 2);
+            s.b2 = corner(B, up, bi, t.b_ti, t.b_tj, t.k0, gr.n0, 2);
+            s.a_pitch = (uint32_t)(a->ld[ai] * 2);
+            s.b_pitch = (uint32_t)(gate->ld[bi] * 2);
+            s.b2_pitch = (uint32_t)(up->ld[bi] * 2);
+            int64_t guard = 0;
+            for (const dmm_tiles *w : {gate, up})
+              guard = std::max(guard, rows_past_end(B.rc[(size_t)t.b_ti + 1] - B.rc[(size_t)t.b_ti], B.cc[(size_t)t.b_tj + 1] - B.cc[(size_t)t.b_tj], w->ld[bi],
+                                                    t.k1 - B.rc[(size_t)t.b_ti], gr.n0 - B.cc[(size_t)t.b_tj], gr.n1 - gr.n0));
+            put_segment(&W, s, t.k1 - t.k0, guard);
+          },
+          [&](int32_t rep, int32_t ti, int32_t tj, int64_t m0, int64_t n0, const dmm_task *, LayerGroup *r) {
+            const int64_t i = C.table_index(rep, ti, tj);
+            r->c = corner(C, h, i, ti, tj, m0, n0, 2);
+            r->ldc = h->ld[i];
+            if (g) r->g = corner(C, g, i, ti, tj, m0, n0, 2), r->ldg = g->ld[i];
+            if (u) r->u = corner(C, u, i, ti, tj, m0, n0, 2), r->ldu = u->ld[i];
+          });
+      return lay_out(W, cus, out, &layout[0], scratch);
+    };
+    return run_layer(P, LAYER_GATED_EXECUTE, key.bytes, nullptr, nullptr, false, (hipStream_t)hip_stream, build, [] { return DMM_OK; });
+  } catch (const std::bad_alloc &) {
+    return DMM_ENOMEM;
+  }
+}
+
+int dmm_gated_backward(dmm_plan_t *P, int activation, const dmm_tiles *a, const dmm_tiles *gate, const dmm_tiles *up, const dmm_tiles *g, const dmm_tiles *u,
+                       const dmm_tiles *dh, const dmm_tiles *dg, const dmm_tiles *du, const dmm_tiles *da, const dmm_tiles *dgate, const dmm_tiles *dup,
+                       uint32_t flags, void *hip_stream) {
+  using namespace dmm;
+  if (!P || !g || !u || !dh || !dg || !du || !is_activation(activation) || P->C.c != 1 || (flags & ~DMM_DB_F32)) return DMM_EINVAL;
+  if ((da && (!gate || !up)) || ((dgate || dup) && !a)) return DMM_EINVAL;
+  const Grid &A = P->A, &B = P->B, &C = P->C;
+  const int es = (flags & DMM_DB_F32) ? 4 : 2;
+  int rc;
+  for (const dmm_tiles *t : {g, u, dh, dg, du})
+    if ((rc = check_layer_tiles(C, t, 2))) return rc;
+  if (da && ((rc = check_layer_tiles(B, gate, 2)) || (rc = check_layer_tiles(B, up, 2)) || (rc = check_layer_single(A, da, 2)))) return rc;
+  if ((dgate || dup) && (rc = check_layer_tiles(A, a, 2))) return rc;
+  if ((dgate && (rc = check_layer_single(B, dgate, es))) || (dup && (rc = check_layer_single(B, dup, es))) || (rc = check_slope(C))) return rc;
+  TraceRange whole("dmm_gated_backward");
+  try {
+    LayerKey key;
+    key.put(&flags, sizeof flags);
+    key.put(dgate || dup ? a : nullptr, A.tiles_per_rep());
+    for (const dmm_tiles *t : {da ? gate : nullptr, da ? up : nullptr, dgate, dup}) key.put(t, B.tiles_per_rep());
+    for (const dmm_tiles *t : {dg, du}) key.put(t, C.tiles_per_rep());
+    key.put(da, A.tiles_per_rep());
+    auto build = [&](int cus, std::vector<char> *out, LayerLayout *layout, size_t *scratch) -> int {
+      int rc2 = DMM_OK;
+      if (da) {
+        LayerWork W;
+        W.kind = LAYER_NT;
+        W.c_es = 2;
+        const dmm_tiles *const dcs[2] = {dg, du}, *const bs[2] = {gate, up};
+        input_gradient(P, dcs, bs, 2, da, &W);
+        if ((rc2 = lay_out(W, cus, out, &layout[0], scratch))) return rc2;
+      }
+      if (dgate || dup) {
+        LayerWork W;
+        W.kind = LAYER_TN;
+        W.c_es = es;
+        if (dgate) weight_gradient(P, a, dg, dgate, &W);
+        if (dup) weight_gradient(P, a, du, dup, &W);
+        rc2 = lay_out(W, cus, out, &layout[1], scratch);
+      }
+      return rc2;
+    };
+    hipStream_t stream = (hipStream_t)hip_stream;
+    return run_layer(P, LAYER_GATED_BACKWARD, key.bytes, nullptr, nullptr, false, stream, build,
+                     [&] { return slope(C, activation, g, u, dh, dg, du, stream); });
+  } catch (const std::bad_alloc &) {
+    return DMM_ENOMEM;
+  }
+}
+
+int dmm_execute_backward(dmm_plan_t *P, const dmm_tiles *a, const dmm_tiles *b, const dmm_tiles *dc, const dmm_tiles *da, const dmm_tiles *db, uint32_t flags,
+                         void *hip_stream) {
+  using namespace dmm;
+  if (!P || !dc || (!da && !db) || (da && !b) || (db && !a) || (flags & ~DMM_DB_F32)) return DMM_EINVAL;
+  const Grid &A = P->A, &B = P->B, &C = P->C;
+  const int es = (flags & DMM_DB_F32) ? 4 : 2;
+  int rc;
+  if ((rc = check_layer_single(C, dc, 2))) return rc;
+  if (da && ((rc = check_layer_single(B, b, 2)) || (rc = check_layer_single(A, da, 2)))) return rc;
+  if (db && ((rc = check_layer_single(A, a, 2)) || (rc = check_layer_single(B, db, es)))) return rc;
+  TraceRange whole("dmm_execute_backward");
+  try {
+    LayerKey key;
+    key.put(&flags, sizeof flags);
+    key.put(db ? a : nullptr, A.tiles_per_rep());
+    key.put(da, A.tiles_per_rep());
+    key.put(da ? b : nullptr, B.tiles_per_rep());
+    key.put(db, B.tiles_per_rep());
+    key.put(dc, C.tiles_per_rep());
+    auto build = [&](int cus, std::vector<char> *out, LayerLayout *layout, size_t *scratch) -> int {
+      int rc2 = DMM_OK;
+      if (da) {
+        LayerWork W;
+        W.kind = LAYER_NT;
+        W.c_es = 2;
+        input_gradient(P, &dc, &b, 1, da, &W);
+        if ((rc2 = lay_out(W, cus, out, &layout[0], scratch))) return rc2;
+      }
+      if (db) {
+        LayerWork W;
+        W.kind = LAYER_TN;
+        W.c_es = es;
+        weight_gradient(P, a, dc, db, &W);
+        rc2 = lay_out(W, cus, out, &layout[1], scratch);
+      }
+      return rc2;
+    };
+    return run_layer(P, LAYER_EXECUTE_BACKWARD, key.bytes, nullptr, nullptr, false, (hipStream_t)hip_stream, build, [] { return DMM_OK; });
+  } catch (const std::bad_alloc &) {
+    return DMM_ENOMEM;
+  }
+}
+
+}  // extern "C"

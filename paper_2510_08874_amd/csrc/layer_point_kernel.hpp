@@ -1,0 +1,434 @@
+// What the layers around a product do element by element (gfx950, device code only): the gated block's slopes, and
+// matrices to 8-bit integers and back.
+#pragma once
+
+#include "layer_kernel.hpp"
+
+namespace dmm {
+
+// the tile that workgroup `block` belongs to, and the workgroup's number inside it
+template <class Args>
+__device__ __forceinline__ const auto &layer_find(const Args &args, int block, int *inside) {
+  int x = 0;
+  while (x + 1 < args.n && block >= args.tile[x + 1].first_block) ++x;
+  *inside = block - args.tile[x].first_block;
+  return args.tile[x];
+}
+
+// Eight neighbouring elements of a row from column `col` on, zeros behind column w; rows may begin anywhere.
+template <bool F32>
+struct LayerVec {
+  static constexpr int WORDS = F32 ? 8 : 4;
+  unsigned w[WORDS];
+  __device__ __forceinline__ float at(int i) const {
+    if constexpr (F32) return __builtin_bit_cast(float, w[i]);
+    else return __builtin_bit_cast(float, i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+  }
+  __device__ __forceinline__ void set(int i, float v) {
+    if constexpr (F32) {
+      w[i] = __builtin_bit_cast(unsigned, v);
+    } else {
+      const unsigned b = layer_bf16(v);
+      w[i / 2] = i & 1 ? w[i / 2] | b << 16 : b;              // (in ascending order)
+    }
+  }
+};
+template <bool F32>
+__device__ __forceinline__ LayerVec<F32> layer_load8(const char *row, int col, int w) {
+  LayerVec<F32> v;
+  if (col + 8 <= w) {
+    __builtin_memcpy(v.w, row + (int64_t)col * (F32 ? 4 : 2), sizeof v.w);
+  } else {
+#pragma unroll
+    for (int i = 0; i < LayerVec<F32>::WORDS; ++i) {
+      if constexpr (F32) {
+        v.w[i] = col + i < w ? ((const unsigned *)row)[col + i] : 0u;
+      } else {
+        const unsigned lo = col + 2 * i < w ? ((const unsigned short *)row)[col + 2 * i] : 0u;
+        const unsigned hi = col + 2 * i + 1 < w ? ((const unsigned short *)row)[col + 2 * i + 1] : 0u;
+        v.w[i] = lo | hi << 16;
+      }
+    }
+  }
+  return v;
+}
+template <bool F32>
+__device__ __forceinline__ void layer_store8(char *row, int col, int w, const LayerVec<F32> &v) {
+  if (col + 8 <= w) {
+    __builtin_memcpy(row + (int64_t)col * (F32 ? 4 : 2), v.w, sizeof v.w);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (col + i < w) {
+        if constexpr (F32) ((unsigned *)row)[col + i] = v.w[i];
+        else ((unsigned short *)row)[col + i] = (unsigned short)(v.w[i / 2] >> (16 * (i & 1)));
+      }
+  }
+}
+
+// dU = dH act(G), dG = dH U act'(G): eight elements of SLOPE_ROWS rows a lane.  Every element is read before it is written, so dG and dU may
+// be G and U themselves.
+__global__ __launch_bounds__(256) void layer_slope_kernel(SlopeArgs) {
+  const auto &args = *(const SlopeArgs *)__builtin_amdgcn_kernarg_segment_ptr();
+  int block;
+  const SlopeTile &T = layer_find(args, blockIdx.x, &block);
+  const int unit = block * 4 + (threadIdx.x >> 6), across = T.blocks_across;
+  const int col = (unit % across) * SLOPE_COLS + (threadIdx.x & 63) * 8, row0 = unit / across * SLOPE_ROWS;
+  if (col >= T.w) return;
+  LayerVec<false> g[SLOPE_ROWS], u[SLOPE_ROWS], h[SLOPE_ROWS];
+#pragma unroll
+  for (int i = 0; i < SLOPE_ROWS; ++i)
+    if (row0 + i < T.h) {
+      g[i] = layer_load8<false>(T.g + (int64_t)(row0 + i) * T.pg, col, T.w);
+      u[i] = layer_load8<false>(T.u + (int64_t)(row0 + i) * T.pu, col, T.w);
+      h[i] = layer_load8<false>(T.dh + (int64_t)(row0 + i) * T.ph, col, T.w);
+    }
+#pragma unroll
+  for (int i = 0; i < SLOPE_ROWS; ++i)
+    if (row0 + i < T.h) {
+      LayerVec<false> dg, du;
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        float value, slope;
+        layer_slope(args.act, g[i].at(x), &value, &slope);
+        const float dh = h[i].at(x);
+        dg.set(x, dh * u[i].at(x) * slope);
+        du.set(x, dh * value);
+      }
+      layer_store8<false>(T.dg + (int64_t)(row0 + i) * T.pdg, col, T.w, dg);
+      layer_store8<false>(T.du + (int64_t)(row0 + i) * T.pdu, col, T.w, du);
+    }
+}
+
+// ---- 8-bit integers -------------------------------------------------------------------------------------
+//
+// A row's (column's) scale is its largest magnitude over 127, rounded to fp32; an element is the integer nearest to 127 x / (largest
+// magnitude), both taken exactly, half-way values to the even one.  A row with an infinity or a NaN has the scale NaN.
+
+// bits of |x|, which compare like the values (NaN above infinity)
+template <bool F32>
+__device__ __forceinline__ unsigned i8_abs_max(const LayerVec<F32> &v, unsigned m) {
+#pragma unroll
+  for (int i = 0; i < LayerVec<F32>::WORDS; ++i) {
+    if constexpr (F32) m = max(m, v.w[i] & 0x7fffffffu);
+    else m = max(m, max(v.w[i] << 16 & 0x7fffffffu, v.w[i] & 0x7fff0000u));
+  }
+  return m;
+}
+
+// What turns elements of a row into integers: |x| and the largest magnitude are brought to [1, 2) by a power of two, so that nothing leaves the
+// range of fp32 on the way.
+struct I8Row {
+  float top, over;              // the largest magnitude in [1, 2); 127 / top
+  int e;
+  unsigned bits;
+};
+__device__ __forceinline__ I8Row i8_row(unsigned bits) {
+  I8Row r;
+  r.bits = bits;
+  const float v = __builtin_bit_cast(float, bits);
+  r.e = 1 - __builtin_amdgcn_frexp_expf(v);
+  r.top = bits ? __builtin_amdgcn_ldexpf(v, r.e) : 1.f;
+  r.over = 127.f / r.top;
+  if (bits == 0 || bits >= 0x7f800000u) r.over = 0.f, r.e = 0;
+  return r;
+}
+__device__ __forceinline__ float i8_scale(unsigned bits) {
+  return bits >= 0x7f800000u ? __builtin_bit_cast(float, 0x7fc00000u) : __builtin_bit_cast(float, bits) / 127.f;
+}
+// x (127 / top) is off by less than 2^-16; where that could matter the exact products decide (they fit 53 bits).
+__device__ __forceinline__ int i8_code(const I8Row &r, float x) {
+  if (r.bits >= 0x7f800000u) return 0;
+  const float y = __builtin_amdgcn_ldexpf(x, r.e), q = y * r.over;
+  float t = __builtin_rintf(q);
+  const float off = q - t;
+  if (__builtin_fabsf(__builtin_fabsf(off) - 0.5f) < 0x1p-14f) {
+    const float low = off < 0.f ? t - 1.f : t;                // the integer below
+    const double twice = 254.0 * (double)y, border = (2.0 * (double)low + 1.0) * (double)r.top;
+    const bool odd = ((int)low & 1) != 0;
+    t = twice > border || (twice == border && odd) ? low + 1.f : low;
+  }
+  return (int)t;
+}
+__device__ __forceinline__ unsigned i8_four(const I8Row &r, float a, float b, float c, float d) {
+  return (unsigned)(i8_code(r, a) & 255) | (unsigned)(i8_code(r, b) & 255) << 8 | (unsigned)(i8_code(r, c) & 255) << 16 | (unsigned)i8_code(r, d) << 24;
+}
+// `n` of the bytes of N words, to any address
+template <int N>
+__device__ __forceinline__ void i8_put(char *p, const unsigned *w, int n) {
+  if (n >= 4 * N) {
+    __builtin_memcpy(p, w, 4 * N);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4 * N; ++i)
+      if (i < n) p[i] = (char)(w[i / 4] >> (8 * (i & 3)));
+  }
+}
+template <int N>
+__device__ __forceinline__ void i8_get(const char *p, unsigned *w, int n) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) w[i] = 0;
+  if (n >= 4 * N) {
+    __builtin_memcpy(w, p, 4 * N);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4 * N; ++i)
+      if (i < n) w[i / 4] |= (unsigned)*(const unsigned char *)(p + i) << (8 * (i & 3));
+  }
+}
+
+__device__ __forceinline__ unsigned i8_wave_max(unsigned v) {
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) v = max(v, (unsigned)__shfl_xor((int)v, d));
+  return v;
+}
+
+__global__ __launch_bounds__(256) void i8_scales_kernel(I8ScaleArgs, int what) {
+  const auto &args = *(const I8ScaleArgs *)__builtin_amdgcn_kernarg_segment_ptr();
+  int x = 0;
+  while (x + 1 < args.n && (int)blockIdx.x >= args.piece[x + 1].first_block) ++x;
+  const int i = ((int)blockIdx.x - args.piece[x].first_block) * 256 + threadIdx.x;
+  if (i >= args.piece[x].n) return;
+  float *const at = args.piece[x].at + i;
+  *at = what == I8_CLEAR ? 0.f : i8_scale(__builtin_bit_cast(unsigned, *at));
+}
+
+// A workgroup's 128 rows of 64 (128) columns: threads to a row of a pass, rows of a pass.
+template <bool F32>
+struct I8Block {
+  static constexpr int ES = F32 ? 4 : 2, COLS = i8_block_cols(F32), ACROSS = COLS / 8, DOWN = 256 / ACROSS, PASSES = 128 / DOWN;
+  static constexpr int PITCH = 256 + 4;                       // bytes of a row in LDS (one word more: rows start in other banks)
+};
+
+// Largest magnitudes of rows or columns so far, as bits, in the scales' place.  (The largest of integers does not depend on the order of the atomics.)
+template <bool F32, bool ALONG_COLS>
+__global__ __launch_bounds__(256) void i8_amax_kernel(I8Args) {
+  using B = I8Block<F32>;
+  __shared__ unsigned tops[128];
+  const auto &args = *(const I8Args *)__builtin_amdgcn_kernarg_segment_ptr();
+  int block;
+  const I8Tile &T = layer_find(args, blockIdx.x, &block);
+  const int col0 = (block % T.blocks_across) * B::COLS, row0 = block / T.blocks_across * 128;
+  const int tid = threadIdx.x, col = col0 + tid % B::ACROSS * 8, r0 = tid / B::ACROSS;
+  LayerVec<F32> v[B::PASSES];
+#pragma unroll
+  for (int x = 0; x < B::PASSES; ++x) {
+    const int row = row0 + x * B::DOWN + r0;
+    v[x] = row < T.h ? layer_load8<F32>(T.x + (int64_t)row * T.x_pitch, col, T.w) : LayerVec<F32>{};
+  }
+  if (tid < 128) tops[tid] = 0;
+  __syncthreads();
+  if constexpr (ALONG_COLS) {
+    unsigned m[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+    for (int x = 0; x < B::PASSES; ++x)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) m[i] = max(m[i], __builtin_bit_cast(unsigned, v[x].at(i)) & 0x7fffffffu);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+#pragma unroll
+      for (int d = B::ACROSS; d < 64; d *= 2) m[i] = max(m[i], (unsigned)__shfl_xor((int)m[i], d));
+      if ((tid & 63) < B::ACROSS) atomicMax(&tops[tid % B::ACROSS * 8 + i], m[i]);
+    }
+    __syncthreads();
+    if (tid < B::COLS && col0 + tid < T.w) atomicMax((unsigned *)T.scale + col0 + tid, tops[tid]);
+  } else {
+#pragma unroll
+    for (int x = 0; x < B::PASSES; ++x) {
+      unsigned m = i8_abs_max(v[x], 0);
+#pragma unroll
+      for (int d = 1; d < B::ACROSS; d *= 2) m = max(m, (unsigned)__shfl_xor((int)m, d));
+      if (tid % B::ACROSS == 0) tops[x * B::DOWN + r0] = m;
+    }
+    __syncthreads();
+    if (tid < 128 && row0 + tid < T.h) atomicMax((unsigned *)T.scale + row0 + tid, tops[tid]);
+  }
+}
+
+// Integers along the rows: the same blocks, eight bytes a thread and row.
+template <bool F32>
+__global__ __launch_bounds__(256) void i8_rows_kernel(I8Args) {
+  using B = I8Block<F32>;
+  const auto &args = *(const I8Args *)__builtin_amdgcn_kernarg_segment_ptr();
+  int block;
+  const I8Tile &T = layer_find(args, blockIdx.x, &block);
+  const int col0 = (block % T.blocks_across) * B::COLS, row0 = block / T.blocks_across * 128;
+  const int col = col0 + threadIdx.x % B::ACROSS * 8, r0 = threadIdx.x / B::ACROSS;
+#pragma unroll
+  for (int x = 0; x < B::PASSES; ++x) {
+    const int row = row0 + x * B::DOWN + r0;
+    if (row >= T.h || col >= T.w) continue;
+    const LayerVec<F32> v = layer_load8<F32>(T.x + (int64_t)row * T.x_pitch, col, T.w);
+    const I8Row r = i8_row(((const unsigned *)T.scale)[row]);
+    const unsigned w[2] = {i8_four(r, v.at(0), v.at(1), v.at(2), v.at(3)), i8_four(r, v.at(4), v.at(5), v.at(6), v.at(7))};
+    i8_put<2>(T.q + (int64_t)row * T.q_pitch + col, w, T.w - col);
+  }
+}
+
+// Integers along the columns: the block is left in LDS, where every thread finds 32 rows of one or two columns.
+template <bool F32>
+__global__ __launch_bounds__(256) void i8_cols_kernel(I8Args) {
+  using B = I8Block<F32>;
+  __shared__ __attribute__((aligned(16))) char lds[128 * B::PITCH + 3 * 64];
+  auto place = [](int row) { return row * B::PITCH + (row >> 5) * 64; };   // (16 words on every 32 rows: four threads read these side by side)
+  const auto &args = *(const I8Args *)__builtin_amdgcn_kernarg_segment_ptr();
+  int block;
+  const I8Tile &T = layer_find(args, blockIdx.x, &block);
+  const int col0 = (block % T.blocks_across) * B::COLS, row0 = block / T.blocks_across * 128;
+  const int tid = threadIdx.x;
+  {
+    const int col = col0 + tid % B::ACROSS * 8, r0 = tid / B::ACROSS;
+    LayerVec<F32> v[B::PASSES];
+#pragma unroll
+    for (int x = 0; x < B::PASSES; ++x) {
+      const int row = row0 + x * B::DOWN + r0;
+      v[x] = row < T.h ? layer_load8<F32>(T.x + (int64_t)row * T.x_pitch, col, T.w) : LayerVec<F32>{};
+    }
+#pragma unroll
+    for (int x = 0; x < B::PASSES; ++x) {
+      unsigned *p = (unsigned *)(lds + place(x * B::DOWN + r0) + tid % B::ACROSS * 8 * B::ES);
+#pragma unroll
+      for (int i = 0; i < LayerVec<F32>::WORDS; ++i) p[i] = v[x].w[i];
+    }
+  }
+  __syncthreads();
+  const int b = tid & 3, p = tid >> 2;                        // rows 32 b ..., a word of each row
+  constexpr int OWN = F32 ? 1 : 2;
+  I8Row r[OWN];
+#pragma unroll
+  for (int c = 0; c < OWN; ++c) {
+    const int col = col0 + OWN * p + c;
+    r[c] = i8_row(col < T.w ? ((const unsigned *)T.scale)[col] : 0u);
+  }
+  unsigned out[OWN][8];
+#pragma unroll
+  for (int i = 0; i < 32; i += 4) {
+    unsigned w[4];
+#pragma unroll
+    for (int y = 0; y < 4; ++y) w[y] = *(const unsigned *)(lds + place(32 * b + i + y) + p * 4);
+#pragma unroll
+    for (int c = 0; c < OWN; ++c) {
+      float f[4];
+#pragma unroll
+      for (int y = 0; y < 4; ++y) f[y] = __builtin_bit_cast(float, F32 ? w[y] : c ? w[y] & 0xffff0000u : w[y] << 16);
+      out[c][i / 4] = i8_four(r[c], f[0], f[1], f[2], f[3]);
+    }
+  }
+  const int row = row0 + 32 * b;
+#pragma unroll
+  for (int c = 0; c < OWN; ++c) {
+    const int col = col0 + OWN * p + c;
+    if (col < T.w && row < T.h) i8_put<8>(T.q + (int64_t)col * T.q_pitch + row, out[c], T.h - row);
+  }
+}
+
+// The rows of a row of tiles, a workgroup each, scales and integers: what fits is kept between the two passes over a row.
+template <bool F32>
+__global__ __launch_bounds__(256) void i8_whole_rows_kernel(I8RowArgs) {
+  constexpr int KEPT = F32 ? 4 : 8;
+  __shared__ unsigned tops[4];
+  const auto &args = *(const I8RowArgs *)__builtin_amdgcn_kernarg_segment_ptr();
+  const int row = blockIdx.x, tid = threadIdx.x;
+  LayerVec<F32> kept[KEPT];
+  unsigned m = 0;
+  int x = 0;                                                  // vectors of this thread so far
+  for (int p = 0; p < args.n; ++p) {
+    const I8RowPiece &P = args.piece[p];
+    const char *const at = P.x + (int64_t)row * P.x_pitch;
+    if (args.n == 1) {
+#pragma unroll
+      for (int y = 0; y < KEPT; ++y) kept[y] = layer_load8<F32>(at, min((y * 256 + tid) * 8, P.w), P.w);
+#pragma unroll
+      for (int y = 0; y < KEPT; ++y) m = i8_abs_max(kept[y], m);
+      x = KEPT;
+    }
+    for (int col = (x * 256 + tid) * 8; col < P.w; col += 2048) m = i8_abs_max(layer_load8<F32>(at, col, P.w), m);
+  }
+  m = i8_wave_max(m);
+  if ((tid & 63) == 0) tops[tid >> 6] = m;
+  __syncthreads();
+  m = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
+  if (tid == 0) args.scale[row] = i8_scale(m);
+  const I8Row r = i8_row(m);
+  auto codes = [&](const I8RowPiece &P, int col, const LayerVec<F32> &v) {
+    const unsigned w[2] = {i8_four(r, v.at(0), v.at(1), v.at(2), v.at(3)), i8_four(r, v.at(4), v.at(5), v.at(6), v.at(7))};
+    i8_put<2>(P.q + (int64_t)row * P.q_pitch + col, w, P.w - col);
+  };
+  for (int p = 0; p < args.n; ++p) {
+    const I8RowPiece &P = args.piece[p];
+    if (args.n == 1) {
+#pragma unroll
+      for (int y = 0; y < KEPT; ++y)
+        if ((y * 256 + tid) * 8 < P.w) codes(P, (y * 256 + tid) * 8, kept[y]);
+    }
+    for (int col = (x * 256 + tid) * 8; col < P.w; col += 2048) codes(P, col, layer_load8<F32>(P.x + (int64_t)row * P.x_pitch, col, P.w));
+  }
+}
+
+// Values, integer times scale, along the rows.
+template <bool F32>
+__global__ __launch_bounds__(256) void i8_row_values_kernel(I8Args) {
+  using B = I8Block<F32>;
+  const auto &args = *(const I8Args *)__builtin_amdgcn_kernarg_segment_ptr();
+  int block;
+  const I8Tile &T = layer_find(args, blockIdx.x, &block);
+  const int col = (block % T.blocks_across) * B::COLS + threadIdx.x % B::ACROSS * 8, row0 = block / T.blocks_across * 128 + threadIdx.x / B::ACROSS;
+  if (col >= T.w) return;
+#pragma unroll
+  for (int x = 0; x < B::PASSES; ++x) {
+    const int row = row0 + x * B::DOWN;
+    if (row >= T.h) continue;
+    unsigned w[2];
+    i8_get<2>(T.q + (int64_t)row * T.q_pitch + col, w, T.w - col);
+    const float s = T.scale[row];
+    LayerVec<F32> v;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v.set(i, (float)(signed char)(w[i / 4] >> (8 * (i & 3))) * s);
+    layer_store8<F32>(T.x + (int64_t)row * T.x_pitch, col, T.w, v);
+  }
+}
+
+// ... along the columns, turned through LDS the other way.
+template <bool F32>
+__global__ __launch_bounds__(256) void i8_col_values_kernel(I8Args) {
+  using B = I8Block<F32>;
+  __shared__ __attribute__((aligned(16))) char lds[128 * B::PITCH + 3 * 64];
+  auto place = [](int row) { return row * B::PITCH + (row >> 5) * 64; };
+  const auto &args = *(const I8Args *)__builtin_amdgcn_kernarg_segment_ptr();
+  int block;
+  const I8Tile &T = layer_find(args, blockIdx.x, &block);
+  const int col0 = (block % T.blocks_across) * B::COLS, row0 = block / T.blocks_across * 128;
+  const int tid = threadIdx.x, b = tid & 3, p = tid >> 2;
+  constexpr int OWN = F32 ? 1 : 2;
+  unsigned w[OWN][8];
+  float s[OWN];
+#pragma unroll
+  for (int c = 0; c < OWN; ++c) {
+    const int col = col0 + OWN * p + c, row = row0 + 32 * b;
+    i8_get<8>(T.q + (int64_t)col * T.q_pitch + row, w[c], col < T.w ? T.h - row : 0);
+    s[c] = col < T.w ? T.scale[col] : 0.f;
+  }
+#pragma unroll
+  for (int i = 0; i < 32; ++i) {
+    float f[OWN];
+#pragma unroll
+    for (int c = 0; c < OWN; ++c) f[c] = (float)(signed char)(w[c][i / 4] >> (8 * (i & 3))) * s[c];
+    *(unsigned *)(lds + place(32 * b + i) + p * 4) =
+        F32 ? __builtin_bit_cast(unsigned, f[0]) : (unsigned)layer_bf16(f[0]) | (unsigned)layer_bf16(f[OWN - 1]) << 16;
+  }
+  __syncthreads();
+  const int col = col0 + tid % B::ACROSS * 8, r0 = tid / B::ACROSS;
+  if (col >= T.w) return;
+#pragma unroll
+  for (int x = 0; x < B::PASSES; ++x) {
+    const int r = x * B::DOWN + r0;
+    if (row0 + r >= T.h) continue;
+    LayerVec<F32> v;
+    const unsigned *const q = (const unsigned *)(lds + place(r) + tid % B::ACROSS * 8 * B::ES);
+#pragma unroll
+    for (int i = 0; i < LayerVec<F32>::WORDS; ++i) v.w[i] = q[i];
+    layer_store8<F32>(T.x + (int64_t)(row0 + r) * T.x_pitch, col, T.w, v);
+  }
+}
+
+}  // namespace dmm

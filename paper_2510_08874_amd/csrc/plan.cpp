@@ -740,6 +740,6 @@ const char *dmm_strerror(int status) {
   }
 }
 
-int dmm_version(void) { return 6; }
+int dmm_version(void) { return 7; }
 
 }  // extern "C"
