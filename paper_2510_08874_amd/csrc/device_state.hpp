@@ -590,6 +590,8 @@ struct LayerState {
   size_t cap = 0;
   std::vector<char> key;
   LayerLayout layout[2];
+  int n_copies = 0, copy_blocks = 0;   // of operands, in front of the products
+  size_t o_copies = 0;
   RedLaunch red;
   bool cached = false;
 };

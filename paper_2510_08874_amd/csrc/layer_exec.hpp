@@ -112,7 +112,67 @@ void put_segment(LayerWork *W, LayerSeg s, int64_t len, int64_t guard) {
 struct LayerChoice {
   int shape = LAYER_256;
   int64_t runs = 1;
+  double us = 0;
 };
+
+// Dense copies of operands whose rows are misaligned or finely cut: every row starts at a multiple of 128 bytes, K is one segment of whole steps,
+// filled up with zeros.  Places are given out from 0 on; the buffer is known later.
+struct LayerCopies {
+  std::vector<LayerCopy> jobs;
+  size_t size = 0;
+  double bytes = 0;
+  int64_t blocks = 0;
+  bool fits = true;                    // rows are not too long for the kernels
+  struct Matrix {
+    size_t at;
+    int64_t pitch;
+  };
+
+  // rows x row_bytes bytes from `src` to place `dst`
+  void job(const void *src, int64_t src_pitch, size_t dst, int64_t dst_pitch, int64_t rows, int64_t row_bytes) {
+    if (rows <= 0 || row_bytes <= 0) return;
+    LayerCopy j;
+    std::memset(&j, 0, sizeof j);
+    j.src = (const char *)src;
+    j.dst = (char *)(uintptr_t)dst;
+    j.src_pitch = src_pitch;
+    j.dst_pitch = dst_pitch;
+    j.rows = (int32_t)rows;
+    j.bytes = (int32_t)row_bytes;
+    j.first_block = (int32_t)blocks;
+    blocks += ((row_bytes + 15) / 16 * rows + LAYER_COPY_CHUNKS - 1) / LAYER_COPY_CHUNKS;
+    jobs.push_back(j);
+    bytes += (double)rows * (double)row_bytes * (src ? 2 : 1);
+  }
+  // Replica 0 of a matrix, a row-major one with `rows` x `cols` elements to be there in the end; `turned`: its tiles lie transposed, and so does the copy.
+  Matrix matrix(const Grid &G, const void *const *tiles, const int64_t *ld, int es, bool turned, int64_t rows, int64_t cols) {
+    const int64_t have_rows = turned ? G.cols : G.rows, have_cols = turned ? G.rows : G.cols;
+    const int64_t pitch = (cols * es + 127) / 128 * 128 | 128;   // (an odd number of lines: rows start in different channels)
+    const Matrix m = {size, pitch};
+    if (pitch >= kLayerPitch || rows > 0x7fffff00) fits = false;
+    size += (size_t)(rows * pitch + 128 + 4095) / 4096 * 4096;   // (a read of eight columns may pass the last row's end)
+    for (int32_t ti = 0; ti < G.gr; ++ti)
+      for (int32_t tj = 0; tj < G.gc; ++tj) {
+        const int64_t r0 = turned ? G.cc[(size_t)tj] : G.rc[(size_t)ti], r1 = turned ? G.cc[(size_t)tj + 1] : G.rc[(size_t)ti + 1];
+        const int64_t c0 = turned ? G.rc[(size_t)ti] : G.cc[(size_t)tj], c1 = turned ? G.rc[(size_t)ti + 1] : G.cc[(size_t)tj + 1];
+        const int64_t i = G.table_index(0, ti, tj);
+        if (r1 > r0 && c1 > c0) job(tiles[i], ld[i] * es, m.at + (size_t)(r0 * pitch + c0 * es), pitch, r1 - r0, (c1 - c0) * es);
+      }
+    job(nullptr, 0, m.at + (size_t)(have_cols * es), pitch, have_rows, (cols - have_cols) * es);
+    job(nullptr, 0, m.at + (size_t)(have_rows * pitch), pitch, rows - have_rows, cols * es);
+    return m;
+  }
+  // scales of replica 0, one behind another
+  size_t scales(const std::vector<int64_t> &cuts, const float *const *s) {
+    const size_t at = size;
+    size += (size_t)(cuts.back() * 4 + 4095) / 4096 * 4096;
+    for (size_t i = 0; i + 1 < cuts.size(); ++i) job(s[i], 0, at + (size_t)cuts[i] * 4, 0, 1, (cuts[i + 1] - cuts[i]) * 4);
+    return at;
+  }
+  double us() const { return 4.0 + bytes / 4.0e6; }
+};
+constexpr size_t kLayerCopies = (size_t)1 << 30;               // of a call
+
 
 // By an estimate in us, from what a step (128 bytes of K) of a tile takes.
 LayerChoice choose_layer(const LayerWork &W, int cus) {
@@ -157,18 +217,18 @@ LayerChoice choose_layer(const LayerWork &W, int cus) {
       const double whole = std::floor(work / places);
       double us = std::max(whole * round(places) + round(work - whole * places), memory);
       if (runs > 1) us += 4.5 + 2.0 * work * tm * tn * (gated ? 2 : 1) * 4 / 3e6;
-      if (best_us == 0 || us < best_us) best_us = us, best.shape = shape, best.runs = runs;
+      // (of equal estimates, as where memory bounds all of them, the smaller tile's)
+      if (best_us == 0 || us < best_us || (us == best_us && shape != best.shape)) best_us = best.us = us, best.shape = shape, best.runs = runs;
     }
   }
   return best;
 }
 
 // Tables of one product, appended to `h`; partial sums in slots of M's buffer, which have addresses from 0 on until place_parts.
-int lay_out(const LayerWork &W, int cus, std::vector<char> *h, LayerLayout *L, size_t *scratch) {
+int lay_out(const LayerWork &W, const LayerChoice &choice, std::vector<char> *h, LayerLayout *L, size_t *scratch) {
   *L = LayerLayout();
   L->kind = W.kind;
   L->act = W.act;
-  const LayerChoice choice = choose_layer(W, cus);
   const int shape = choice.shape, tm = kLayerTile[W.kind][shape].tm, tn = kLayerTile[W.kind][shape].tn;
   const bool gated = layer_gated(W.kind);
   const int wide = gated ? 2 * tn : tn;                        // columns of a slot
@@ -269,18 +329,40 @@ int lay_out(const LayerWork &W, int cus, std::vector<char> *h, LayerLayout *L, s
   return DMM_OK;
 }
 
-void place_parts(std::vector<char> *h, const LayerLayout &L, char *buf) {
+// Partial sums and copies get their places in the buffer: the former at its front, the latter from `copies` on (none: null).
+void place_parts(std::vector<char> *h, const LayerLayout &L, char *buf, char *copies) {
+  auto move = [&](auto *&p) {
+    if (copies) p = (std::decay_t<decltype(p)>)(copies + (uintptr_t)p);
+  };
+  auto move_segment = [&](LayerSeg &s) {
+    move(s.a);
+    move(s.b);
+    move(s.b2);
+  };
   LayerItem *items = (LayerItem *)(h->data() + L.o_items);
-  for (int i = 0; i < L.n_items; ++i)
-    if (items[i].what == LAYER_PARTS) items[i].c = buf + (uintptr_t)items[i].c;
+  for (int i = 0; i < L.n_items; ++i) {
+    LayerItem &it = items[i];
+    if (it.what == LAYER_PARTS) it.c = buf + (uintptr_t)it.c;
+    move_segment(it.front);
+    move(it.sa);
+    move(it.sb);
+    move(it.sb2);
+  }
+  for (LayerSeg *s = (LayerSeg *)(h->data() + L.o_segs); s < (LayerSeg *)(h->data() + L.o_joins); ++s) move_segment(*s);
   LayerJoin *joins = (LayerJoin *)(h->data() + L.o_joins);
-  for (int i = 0; i < L.n_joins; ++i) joins[i].parts = buf + (uintptr_t)joins[i].parts;
+  for (int i = 0; i < L.n_joins; ++i) {
+    joins[i].parts = buf + (uintptr_t)joins[i].parts;
+    move(joins[i].sa);
+    move(joins[i].sb);
+    move(joins[i].sb2);
+  }
 }
 
 // The part of a call that all kinds have in common: the tables of the call before if they are of the same inputs (`key`), else new ones,
-// made by `build` from the plan; then `in_front`, the launches and, where `reduce` asks for it, the sum of C's replicas.
-template <class Build, class Front>
-int run_layer(dmm_plan_t *P, int which, const std::vector<char> &inputs, void *const *c_tiles, const int64_t *c_ld, bool reduce, hipStream_t stream, Build build,
+// made from the products that `make` describes (on the operands, or on copies); then `in_front`, the launches and, where `reduce` asks for it, the sum of
+// C's replicas.  A graph's launches are ordered with the plan's other calls by the caller, so nothing is waited for in a capture.
+template <class Make, class Front>
+int run_layer(dmm_plan_t *P, int which, const std::vector<char> &inputs, void *const *c_tiles, const int64_t *c_ld, bool reduce, hipStream_t stream, Make make,
               Front in_front) {
   int rc;
   const bool capturing = is_capturing(stream), known = P->dev && P->dev->layer[which].cached;
@@ -294,31 +376,67 @@ int run_layer(dmm_plan_t *P, int which, const std::vector<char> &inputs, void *c
   std::vector<char> key(inputs);
   key.insert(key.end(), (const char *)&device, (const char *)&device + sizeof device);
   if (M.cached && key == M.key) {
-    if ((rc = M.table.order_behind_copy(stream))) return rc;
-    if ((M.layout[0].n_joins || M.layout[1].n_joins) && (rc = P->dev->uses.order(stream))) return rc;
+    if (!capturing && (rc = M.table.order_behind_copy(stream))) return rc;
+    if (!capturing && (M.layout[0].n_joins || M.layout[1].n_joins || M.n_copies) && (rc = P->dev->uses.order(stream))) return rc;
   } else {
     if (capturing) return DMM_EINVAL;
     M.cached = false;
     LayerLayout layout[2];
+    LayerChoice choice[2];
     RedLaunch red;
     std::vector<char> &h = P->dev->host;
-    h.clear();
-    size_t scratch = 0;
-    if ((rc = build(cus, &h, layout, &scratch))) return rc;
-    if (c_tiles && (rc = build_reduce(P, c_tiles, c_ld, 0, &h, h.size(), &red))) return rc;
-    if (scratch) {
-      if ((rc = P->dev->uses.order(stream))) return rc;
-      if (scratch > M.cap) {
+    // on the operands as they lie, or on copies where that is estimated to be faster and there is room
+    LayerCopies copies;
+    std::vector<LayerWork> work = make(nullptr);
+    double us = 0;
+    for (size_t x = 0; x < work.size(); ++x) us += (choice[x] = choose_layer(work[x], cus)).us;
+    if (P->C.c == 1) {
+      std::vector<LayerWork> dense = make(&copies);
+      LayerChoice then[2];
+      double dense_us = copies.us();
+      for (size_t x = 0; x < dense.size(); ++x) dense_us += (then[x] = choose_layer(dense[x], cus)).us;
+      if (dense_us < us && copies.fits && copies.size <= kLayerCopies && copies.blocks <= kLayerBlocks) {
+        work.swap(dense);
+        std::copy(then, then + 2, choice);
+      } else {
+        copies = LayerCopies();
+      }
+    }
+    if ((rc = P->dev->uses.order(stream))) return rc;
+    for (;;) {
+      h.clear();
+      size_t scratch = 0;
+      for (size_t x = 0; x < work.size(); ++x)
+        if ((rc = lay_out(work[x], choice[x], &h, &layout[x], &scratch))) return rc;
+      scratch = (scratch + 4095) / 4096 * 4096;
+      const size_t need = scratch + copies.size;
+      if (need > M.cap) {
         if (M.buf) {
           if ((rc = P->dev->uses.wait())) return rc;
           DMM_HIP(hipStreamSynchronize(stream));
           scratch_pool().release(&M.buf, &M.cap);
         }
-        if ((rc = scratch_pool().acquire(scratch, &M.buf, &M.cap))) return rc;
+        rc = scratch_pool().acquire(need, &M.buf, &M.cap);
+        if (rc == DMM_ENOMEM && copies.size) {
+          (void)hipGetLastError();
+          copies = LayerCopies();
+          work = make(nullptr);
+          for (size_t x = 0; x < work.size(); ++x) choice[x] = choose_layer(work[x], cus);
+          continue;
+        }
+        if (rc) return rc;
       }
-      for (const LayerLayout &L : layout)
-        if (L.n_joins) place_parts(&h, L, M.buf);
+      char *const at = copies.size ? M.buf + scratch : nullptr;
+      for (const LayerLayout &L : layout) place_parts(&h, L, M.buf, at);
+      for (LayerCopy &j : copies.jobs) j.dst = at + (uintptr_t)j.dst;
+      break;
     }
+    M.n_copies = (int)copies.jobs.size();
+    M.copy_blocks = (int)copies.blocks;
+    M.o_copies = h.size();
+    h.insert(h.end(), (const char *)copies.jobs.data(), (const char *)(copies.jobs.data() + copies.jobs.size()));
+    static_assert(sizeof(LayerCopy) % 8 == 0, "tables lie one behind another");
+    if (c_tiles && (rc = build_reduce(P, c_tiles, c_ld, 0, &h, h.size(), &red))) return rc;
     if ((rc = M.table.upload(h.data(), h.size(), stream, P->dev->uses))) return rc;
     red.dev_base = M.table.dev();
     M.layout[0] = layout[0];
@@ -334,6 +452,10 @@ int run_layer(dmm_plan_t *P, int which, const std::vector<char> &inputs, void *c
   if ((rc = P->dev->uses.claim(stream, &behind))) return rc;
   const char *d = M.table.dev();
   bool marked = false;
+  if (M.n_copies) {
+    layer_copy_launch((const LayerCopy *)(d + M.o_copies), M.n_copies, M.copy_blocks, stream);
+    DMM_HIP(hipGetLastError());
+  }
   for (int x = 0; x < 2; ++x) {
     const LayerLayout &L = M.layout[x];
     if (!L.n_items) continue;
@@ -394,6 +516,39 @@ void plan_groups(const dmm_plan_t *P, LayerWork *W, Segment segment, Out out) {
     W->groups.push_back(r);
   }
 }
+
+// The same on copies (C has one replica): C's tiles, all of K in one segment.
+template <class Segment, class Out>
+void tile_groups(const Grid &G, LayerWork *W, Segment segment, Out out) {
+  for (int32_t ti = 0; ti < G.gr; ++ti)
+    for (int32_t tj = 0; tj < G.gc; ++tj) {
+      LayerGroup r;
+      std::memset(&r, 0, sizeof r);
+      r.m = G.rc[(size_t)ti + 1] - G.rc[(size_t)ti];
+      r.n = G.cc[(size_t)tj + 1] - G.cc[(size_t)tj];
+      if (r.m <= 0 || r.n <= 0) continue;
+      r.seg = W->segs.size();
+      segment(G.rc[(size_t)ti], G.cc[(size_t)tj]);
+      r.n_segs = W->segs.size() - r.seg;
+      out(0, ti, tj, G.rc[(size_t)ti], G.cc[(size_t)tj], &r);
+      W->groups.push_back(r);
+    }
+}
+// A segment on copies: places of the operands' first element, whole steps of K.
+LayerSeg dense_segment(size_t a, int64_t a_pitch, size_t b, int64_t b_pitch, size_t b2, int64_t b2_pitch, int64_t steps) {
+  LayerSeg s;
+  s.a = (const char *)(uintptr_t)a;
+  s.b = (const char *)(uintptr_t)b;
+  s.b2 = (const char *)(uintptr_t)b2;
+  s.a_pitch = (uint32_t)a_pitch;
+  s.b_pitch = (uint32_t)b_pitch;
+  s.b2_pitch = (uint32_t)b2_pitch;
+  s.steps = (int32_t)steps;
+  s.tail = 0;
+  s.pad = 0;
+  return s;
+}
+int64_t up_to(int64_t n, int64_t step) { return (n + step - 1) / step * step; }
 
 int32_t interval_of(const std::vector<int64_t> &cuts, int64_t at) {   // the non-empty interval that holds `at`
   return (int32_t)(std::upper_bound(cuts.begin(), cuts.end(), at) - cuts.begin()) - 1;
@@ -466,6 +621,60 @@ void weight_gradient(const dmm_plan_t *P, const dmm_tiles *a, const dmm_tiles *d
     }
 }
 
+// The products behind both backward calls: `pairs` of dC and B (and dB), from the operands or from copies of these.
+std::vector<LayerWork> gradients(const dmm_plan_t *P, const dmm_tiles *a, const dmm_tiles *const *b, const dmm_tiles *const *dc, int pairs, const dmm_tiles *da,
+                                 const dmm_tiles *const *db, int es, LayerCopies *copies) {
+  const Grid &A = P->A, &B = P->B, &C = P->C;
+  const bool any_db = db[0] || (pairs > 1 && db[1]);
+  std::vector<LayerWork> works((da != nullptr) + any_db);
+  if (da) works.front().kind = LAYER_NT, works.front().c_es = 2;
+  if (any_db) works.back().kind = LAYER_TN, works.back().c_es = es;
+  if (!copies) {
+    if (da) input_gradient(P, dc, b, pairs, da, &works.front());
+    for (int p = 0; p < pairs; ++p)
+      if (db[p]) weight_gradient(P, a, dc[p], db[p], &works.back());
+    return works;
+  }
+  // dC serves along n and across m
+  const int64_t m = up_to(C.rows, 64), n = up_to(C.cols, 64);
+  LayerCopies::Matrix cc[2];
+  for (int p = 0; p < pairs; ++p) cc[p] = copies->matrix(C, dc[p]->tiles, dc[p]->ld, 2, false, m, n);
+  if (da) {
+    LayerCopies::Matrix cb[2];
+    for (int p = 0; p < pairs; ++p) cb[p] = copies->matrix(B, b[p]->tiles, b[p]->ld, 2, false, B.rows, n);
+    LayerWork &W = works.front();
+    tile_groups(
+        A, &W,
+        [&](int64_t m0, int64_t k0) {
+          for (int p = 0; p < pairs; ++p)
+            W.segs.push_back(dense_segment(cc[p].at + (size_t)(m0 * cc[p].pitch), cc[p].pitch, cb[p].at + (size_t)(k0 * cb[p].pitch), cb[p].pitch, 0, 0, n / 64));
+        },
+        [&](int32_t, int32_t ti, int32_t tj, int64_t m0, int64_t k0, LayerGroup *r) {
+          const int64_t i = A.table_index(0, ti, tj);
+          r->c = corner(A, da, i, ti, tj, m0, k0, 2);
+          r->ldc = da->ld[i];
+        });
+  }
+  if (any_db) {
+    const LayerCopies::Matrix ca = copies->matrix(A, a->tiles, a->ld, 2, false, m, A.cols);
+    LayerWork &W = works.back();
+    for (int p = 0; p < pairs; ++p) {
+      if (!db[p]) continue;
+      tile_groups(
+          B, &W,
+          [&](int64_t k0, int64_t n0) {
+            W.segs.push_back(dense_segment(ca.at + (size_t)k0 * 2, ca.pitch, cc[p].at + (size_t)n0 * 2, cc[p].pitch, 0, 0, m / 64));
+          },
+          [&](int32_t, int32_t ti, int32_t tj, int64_t k0, int64_t n0, LayerGroup *r) {
+            const int64_t i = B.table_index(0, ti, tj);
+            r->c = corner(B, db[p], i, ti, tj, k0, n0, es);
+            r->ldc = db[p]->ld[i];
+          });
+    }
+  }
+  return works;
+}
+
 bool is_activation(int act) { return act == DMM_SILU || act == DMM_GELU || act == DMM_GELU_TANH; }
 
 // C = A B, or the gated product of A with two right operands, in 8-bit integers.
@@ -481,11 +690,37 @@ int i8_product(dmm_plan_t *P, int which, int act, const dmm_int_tiles *a, const 
   key.put(b, B, true);
   if (b2) key.put(b2, B, true);
   key.put(c, C.c * C.tiles_per_rep());
-  auto build = [&](int cus, std::vector<char> *h, LayerLayout *layout, size_t *scratch) -> int {
-    LayerWork W;
+  auto make = [&](LayerCopies *copies) {
+    std::vector<LayerWork> works(1);
+    LayerWork &W = works[0];
     W.kind = b2 ? LAYER_I8_GATED : LAYER_I8;
     W.act = act;
     W.c_es = c_es;
+    auto result = [&](int32_t rep, int32_t ti, int32_t tj, int64_t m0, int64_t n0, LayerGroup *r) {
+      const int64_t i = C.table_index(rep, ti, tj);
+      r->c = corner(C, c, i, ti, tj, m0, n0, c_es);
+      r->ldc = c->ld[i];
+    };
+    if (copies) {
+      const int64_t k = up_to(A.cols, layer_step(W.kind));
+      const LayerCopies::Matrix ca = copies->matrix(A, a->codes, a->code_ld, 1, false, A.rows, k), cb = copies->matrix(B, b->codes, b->code_ld, 1, true, B.cols, k);
+      LayerCopies::Matrix cb2 = {0, 0};
+      if (b2) cb2 = copies->matrix(B, b2->codes, b2->code_ld, 1, true, B.cols, k);
+      const size_t sa = copies->scales(A.rc, a->scales), sb = copies->scales(B.cc, b->scales), sb2 = b2 ? copies->scales(B.cc, b2->scales) : 0;
+      tile_groups(
+          C, &W,
+          [&](int64_t m0, int64_t n0) {
+            W.segs.push_back(dense_segment(ca.at + (size_t)(m0 * ca.pitch), ca.pitch, cb.at + (size_t)(n0 * cb.pitch), cb.pitch, cb2.at + (size_t)(n0 * cb2.pitch),
+                                           cb2.pitch, k / layer_step(W.kind)));
+          },
+          [&](int32_t rep, int32_t ti, int32_t tj, int64_t m0, int64_t n0, LayerGroup *r) {
+            result(rep, ti, tj, m0, n0, r);
+            r->sa = (const float *)(uintptr_t)(sa + (size_t)m0 * 4);
+            r->sb = (const float *)(uintptr_t)(sb + (size_t)n0 * 4);
+            r->sb2 = (const float *)(uintptr_t)(sb2 + (size_t)n0 * 4);
+          });
+      return works;
+    }
     plan_groups(
         P, &W,
         [&](const Group &g, const dmm_task &t) {
@@ -502,18 +737,16 @@ int i8_product(dmm_plan_t *P, int which, int act, const dmm_int_tiles *a, const 
           put_segment(&W, s, t.k1 - t.k0, 0);
         },
         [&](int32_t rep, int32_t ti, int32_t tj, int64_t m0, int64_t n0, const dmm_task *t, LayerGroup *r) {
-          const int64_t i = C.table_index(rep, ti, tj);
-          r->c = corner(C, c, i, ti, tj, m0, n0, c_es);
-          r->ldc = c->ld[i];
+          result(rep, ti, tj, m0, n0, r);
           if (!t) return;
           r->sa = a->scales[(int64_t)t->a_rep * A.gr + t->a_ti] + (m0 - A.rc[(size_t)t->a_ti]);
           const int64_t s = (int64_t)t->b_rep * B.gc + t->b_tj, at = n0 - B.cc[(size_t)t->b_tj];
           r->sb = b->scales[s] + at;
           r->sb2 = b2 ? b2->scales[s] + at : nullptr;
         });
-    return lay_out(W, cus, h, &layout[0], scratch);
+    return works;
   };
-  return run_layer(P, which, key.bytes, c->tiles, c->ld, reduce, stream, build, [] { return DMM_OK; });
+  return run_layer(P, which, key.bytes, c->tiles, c->ld, reduce, stream, make, [] { return DMM_OK; });
 }
 
 // dU = dH act(G), dG = dH U act'(G), tile by tile.
@@ -775,11 +1008,31 @@ int dmm_gated_execute(dmm_plan_t *P, int activation, const dmm_tiles *a, const d
     key.put(gate, B.c * B.tiles_per_rep());
     key.put(up, B.c * B.tiles_per_rep());
     for (const dmm_tiles *t : {h, g, u}) key.put(t, C.tiles_per_rep());
-    auto build = [&](int cus, std::vector<char> *out, LayerLayout *layout, size_t *scratch) -> int {
-      LayerWork W;
+    auto make = [&](LayerCopies *copies) {
+      std::vector<LayerWork> works(1);
+      LayerWork &W = works[0];
       W.kind = LAYER_GATED;
       W.act = activation;
       W.c_es = 2;
+      auto result = [&](int32_t rep, int32_t ti, int32_t tj, int64_t m0, int64_t n0, LayerGroup *r) {
+        const int64_t i = C.table_index(rep, ti, tj);
+        r->c = corner(C, h, i, ti, tj, m0, n0, 2);
+        r->ldc = h->ld[i];
+        if (g) r->g = corner(C, g, i, ti, tj, m0, n0, 2), r->ldg = g->ld[i];
+        if (u) r->u = corner(C, u, i, ti, tj, m0, n0, 2), r->ldu = u->ld[i];
+      };
+      if (copies) {
+        const int64_t k = up_to(A.cols, 64);
+        const LayerCopies::Matrix ca = copies->matrix(A, a->tiles, a->ld, 2, false, A.rows, k), cg = copies->matrix(B, gate->tiles, gate->ld, 2, false, k, B.cols),
+                                  cu = copies->matrix(B, up->tiles, up->ld, 2, false, k, B.cols);
+        tile_groups(
+            C, &W,
+            [&](int64_t m0, int64_t n0) {
+              W.segs.push_back(dense_segment(ca.at + (size_t)(m0 * ca.pitch), ca.pitch, cg.at + (size_t)n0 * 2, cg.pitch, cu.at + (size_t)n0 * 2, cu.pitch, k / 64));
+            },
+            result);
+        return works;
+      }
       plan_groups(
           P, &W,
           [&](const Group &gr, const dmm_task &t) {
@@ -797,16 +1050,10 @@ int dmm_gated_execute(dmm_plan_t *P, int activation, const dmm_tiles *a, const d
                                                     t.k1 - B.rc[(size_t)t.b_ti], gr.n0 - B.cc[(size_t)t.b_tj], gr.n1 - gr.n0));
             put_segment(&W, s, t.k1 - t.k0, guard);
           },
-          [&](int32_t rep, int32_t ti, int32_t tj, int64_t m0, int64_t n0, const dmm_task *, LayerGroup *r) {
-            const int64_t i = C.table_index(rep, ti, tj);
-            r->c = corner(C, h, i, ti, tj, m0, n0, 2);
-            r->ldc = h->ld[i];
-            if (g) r->g = corner(C, g, i, ti, tj, m0, n0, 2), r->ldg = g->ld[i];
-            if (u) r->u = corner(C, u, i, ti, tj, m0, n0, 2), r->ldu = u->ld[i];
-          });
-      return lay_out(W, cus, out, &layout[0], scratch);
+          [&](int32_t rep, int32_t ti, int32_t tj, int64_t m0, int64_t n0, const dmm_task *, LayerGroup *r) { result(rep, ti, tj, m0, n0, r); });
+      return works;
     };
-    return run_layer(P, LAYER_GATED_EXECUTE, key.bytes, nullptr, nullptr, false, (hipStream_t)hip_stream, build, [] { return DMM_OK; });
+    return run_layer(P, LAYER_GATED_EXECUTE, key.bytes, nullptr, nullptr, false, (hipStream_t)hip_stream, make, [] { return DMM_OK; });
   } catch (const std::bad_alloc &) {
     return DMM_ENOMEM;
   }
@@ -834,28 +1081,12 @@ int dmm_gated_backward(dmm_plan_t *P, int activation, const dmm_tiles *a, const 
     for (const dmm_tiles *t : {da ? gate : nullptr, da ? up : nullptr, dgate, dup}) key.put(t, B.tiles_per_rep());
     for (const dmm_tiles *t : {dg, du}) key.put(t, C.tiles_per_rep());
     key.put(da, A.tiles_per_rep());
-    auto build = [&](int cus, std::vector<char> *out, LayerLayout *layout, size_t *scratch) -> int {
-      int rc2 = DMM_OK;
-      if (da) {
-        LayerWork W;
-        W.kind = LAYER_NT;
-        W.c_es = 2;
-        const dmm_tiles *const dcs[2] = {dg, du}, *const bs[2] = {gate, up};
-        input_gradient(P, dcs, bs, 2, da, &W);
-        if ((rc2 = lay_out(W, cus, out, &layout[0], scratch))) return rc2;
-      }
-      if (dgate || dup) {
-        LayerWork W;
-        W.kind = LAYER_TN;
-        W.c_es = es;
-        if (dgate) weight_gradient(P, a, dg, dgate, &W);
-        if (dup) weight_gradient(P, a, du, dup, &W);
-        rc2 = lay_out(W, cus, out, &layout[1], scratch);
-      }
-      return rc2;
+    auto make = [&](LayerCopies *copies) {
+      const dmm_tiles *const bs[2] = {gate, up}, *const dcs[2] = {dg, du}, *const dbs[2] = {dgate, dup};
+      return gradients(P, a, bs, dcs, 2, da, dbs, es, copies);
     };
     hipStream_t stream = (hipStream_t)hip_stream;
-    return run_layer(P, LAYER_GATED_BACKWARD, key.bytes, nullptr, nullptr, false, stream, build,
+    return run_layer(P, LAYER_GATED_BACKWARD, key.bytes, nullptr, nullptr, false, stream, make,
                      [&] { return slope(C, activation, g, u, dh, dg, du, stream); });
   } catch (const std::bad_alloc &) {
     return DMM_ENOMEM;
@@ -881,25 +1112,8 @@ int dmm_execute_backward(dmm_plan_t *P, const dmm_tiles *a, const dmm_tiles *b, 
     key.put(da ? b : nullptr, B.tiles_per_rep());
     key.put(db, B.tiles_per_rep());
     key.put(dc, C.tiles_per_rep());
-    auto build = [&](int cus, std::vector<char> *out, LayerLayout *layout, size_t *scratch) -> int {
-      int rc2 = DMM_OK;
-      if (da) {
-        LayerWork W;
-        W.kind = LAYER_NT;
-        W.c_es = 2;
-        input_gradient(P, &dc, &b, 1, da, &W);
-        if ((rc2 = lay_out(W, cus, out, &layout[0], scratch))) return rc2;
-      }
-      if (db) {
-        LayerWork W;
-        W.kind = LAYER_TN;
-        W.c_es = es;
-        weight_gradient(P, a, dc, db, &W);
-        rc2 = lay_out(W, cus, out, &layout[1], scratch);
-      }
-      return rc2;
-    };
-    return run_layer(P, LAYER_EXECUTE_BACKWARD, key.bytes, nullptr, nullptr, false, (hipStream_t)hip_stream, build, [] { return DMM_OK; });
+    auto make = [&](LayerCopies *copies) { return gradients(P, a, &b, &dc, 1, da, &db, es, copies); };
+    return run_layer(P, LAYER_EXECUTE_BACKWARD, key.bytes, nullptr, nullptr, false, (hipStream_t)hip_stream, make, [] { return DMM_OK; });
   } catch (const std::bad_alloc &) {
     return DMM_ENOMEM;
   }

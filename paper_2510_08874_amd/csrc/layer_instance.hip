@@ -111,6 +111,9 @@ bool layer_launch(hipEvent_t behind, int kind, int shape, int act, const LayerIt
   }
 }
 
+void layer_copy_launch(const LayerCopy *jobs, int n, int blocks, hipStream_t stream) {
+  layer_copy_kernel<<<dim3((unsigned)blocks), dim3(256), 0, stream>>>(jobs, n);
+}
 void slope_launch(const SlopeArgs &args, int blocks, hipStream_t stream) { layer_slope_kernel<<<dim3((unsigned)blocks), dim3(256), 0, stream>>>(args); }
 void i8_scales_launch(const I8ScaleArgs &args, int blocks, int what, hipStream_t stream) {
   i8_scales_kernel<<<dim3((unsigned)blocks), dim3(256), 0, stream>>>(args, what);

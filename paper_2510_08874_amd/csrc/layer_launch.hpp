@@ -48,6 +48,17 @@ struct LayerJoin {
   int32_t runs, tm, tn, m_ext, n_ext, c_es;
 };
 
+// Rows of a tile on their way into a dense copy of its matrix; without a source, zeros.
+struct LayerCopy {
+  const char *src;
+  char *dst;
+  int64_t src_pitch, dst_pitch; // bytes
+  int32_t rows, bytes;          // of a row
+  int32_t first_block, pad;
+};
+constexpr int LAYER_COPY_CHUNKS = 2048;   // of 16 bytes, a workgroup
+void layer_copy_launch(const LayerCopy *jobs, int n, int blocks, hipStream_t stream);
+
 // Elements and operands of a product.
 enum {
   LAYER_I8,                     // C = A B, both direct

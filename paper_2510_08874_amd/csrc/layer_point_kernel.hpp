@@ -66,6 +66,46 @@ __device__ __forceinline__ void layer_store8(char *row, int col, int w, const La
   }
 }
 
+// Tiles whose rows are misaligned or finely cut, into dense rows: 16 bytes a thread at a time, eight of them on their way together.  The last 16 bytes
+// of a row are moved as such, over some of those in front of them: a part of 16 bytes would be moved one by one, and every wave meets one.
+__global__ __launch_bounds__(256) void layer_copy_kernel(const LayerCopy *__restrict__ jobs, int n) {
+  int lo = 0, hi = n - 1;                                     // the last job that does not begin behind this workgroup
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (jobs[mid].first_block <= (int)blockIdx.x) lo = mid;
+    else hi = mid - 1;
+  }
+  const LayerCopy j = jobs[lo];
+  const unsigned across = (unsigned)(j.bytes + 15) / 16;      // chunks of a row
+  const uint64_t all = (uint64_t)across * (unsigned)j.rows, first = (uint64_t)((int)blockIdx.x - j.first_block) * LAYER_COPY_CHUNKS;
+  constexpr int N = LAYER_COPY_CHUNKS / 256;
+  const unsigned row0 = (unsigned)(first / across), col0 = (unsigned)(first % across);
+  typedef __attribute__((address_space(1))) char *gptr;
+  typedef const __attribute__((address_space(1))) char *cgptr;
+  if (j.bytes < 16) {
+    for (int i = 0; i < N; ++i) {
+      const uint64_t row = first + i * 256 + threadIdx.x;     // (one chunk a row)
+      if (row >= all) break;
+      for (int b = 0; b < j.bytes; ++b) ((gptr)j.dst)[(int64_t)row * j.dst_pitch + b] = j.src ? ((cgptr)j.src)[(int64_t)row * j.src_pitch + b] : 0;
+    }
+    return;
+  }
+  nt_i32x4 v[N];
+  gptr to[N];
+  bool mine[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const unsigned on = col0 + i * 256 + threadIdx.x, row = row0 + on / across, at = min(on % across * 16, (unsigned)j.bytes - 16);
+    mine[i] = first + i * 256 + threadIdx.x < all;
+    to[i] = (gptr)j.dst + ((int64_t)row * j.dst_pitch + at);
+    v[i] = nt_i32x4{0, 0, 0, 0};
+    if (j.src && mine[i]) __builtin_memcpy(&v[i], (cgptr)j.src + ((int64_t)row * j.src_pitch + at), 16);
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (mine[i]) __builtin_memcpy(to[i], &v[i], 16);
+}
+
 // dU = dH act(G), dG = dH U act'(G): eight elements of SLOPE_ROWS rows a lane.  Every element is read before it is written, so dG and dU may
 // be G and U themselves.
 __global__ __launch_bounds__(256) void layer_slope_kernel(SlopeArgs) {

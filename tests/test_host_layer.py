@@ -29,7 +29,7 @@ class Space:
     """Made-up device buffers that end with a tile's last element, far from each other."""
 
     def __init__(self):
-        self.at, self.start, self.end = 1 << 44, [], []
+        self.at, self.start, self.end, self.copies = 1 << 44, [], [], None
 
     def take(self, size, align):
         self.at += align                                       # (at multiples of the element's size, not of more)
@@ -55,11 +55,14 @@ class Space:
         return b.int_tiles(ptr, ld, [self.take(4 * (j - i), 4) if j > i else None for _ in range(d["replication"]) for i, j in zip(cuts, cuts[1:])])
 
     def inside(self, first, last, what):
-        """Bytes first ... last - 1 lie in one buffer."""
+        """Bytes first ... last - 1 lie in one buffer (or in this call's copies)."""
+        if self.copies and self.copies[0] <= first and last <= self.copies[1]:
+            return
         i = bisect.bisect_right(self.start, first) - 1
         assert i >= 0 and first >= self.start[i] and last <= self.end[i], f"{what}: bytes {first:#x} to {last:#x}, the buffer ends at {self.end[i]:#x}"
 
 
+COPY = struct.Struct("<2Q2q4i")
 SEG, ITEM, JOIN = struct.Struct("<3Q3I3i"), struct.Struct("<3Q3I3i" + "Qq2Q2q3Q" + "12i"), struct.Struct("<Qq2Q2q3Q" + "Q6i")
 # kind of a launch: rows, columns of a right operand in its macro-tiles, by LDS; (A turned, B turned, two right operands, bytes of an element)
 KINDS = {"int": (False, False, False, 1), "int_gated": (False, False, True, 1), "gated": (False, True, True, 2), "nt": (False, False, False, 2), "tn": (True, True, False, 2)}
@@ -128,6 +131,21 @@ def follow(rec, space, op, kind):
 
 def follow_call(rec, space, at, kinds):
     """The launches of one call: [(corner, ld, bytes of an element, rows, columns, k)] of every kind."""
+    space.copies = None
+    for op in rec.launches(at):
+        if op[1] == "layer_copy_kernel":
+            blocks, x, low, high = 0, 0, 1 << 63, 0
+            while blocks < rec.so.rec_blocks(op[0]):
+                src, dst, src_pitch, dst_pitch, rows, size, first, _ = COPY.unpack(ctypes.string_at(op[3] + x * COPY.size, COPY.size))
+                assert first == blocks and rows > 0 and size > 0
+                if src:
+                    space.inside(src, src + (rows - 1) * src_pitch + size, "copied")
+                low, high = min(low, dst), max(high, dst + (rows - 1) * dst_pitch + size)
+                blocks += -(-(-(-size // 16) * rows) // 2048)
+                x += 1
+            assert blocks == rec.so.rec_blocks(op[0])
+            # (rows are filled up to 128 bytes, and so many lie behind the last: a read of eight columns may pass a row's end)
+            space.copies = (low, -(-high // 128) * 128 + 128)
     ops = [o for o in rec.launches(at) if o[1] in ("layer_gemm_kernel", "layer_join_kernel")]
     got, x = [], 0
     for kind in kinds:
@@ -154,9 +172,10 @@ def follow_call(rec, space, at, kinds):
     return got
 
 
-def covers(space, out, ptr, ld, d, es, k, replicas=1):
-    """Every element of the tiles is written once, with all of K."""
+def covers(space, out, ptr, ld, d, es, k, step, times=1, replicas=1):
+    """Every element of the tiles is written once, with all of K (on copies, filled up to whole steps)."""
     seen = {}
+    k = (-(-k // step) * step if space.copies else k) * times
     for c, ldc, c_es, h, w, k_sum in out:
         assert c_es == es and k_sum == k, (c_es, es, k_sum, k)
         i = bisect.bisect_right(space.start, c) - 1
@@ -214,25 +233,25 @@ def reads_and_writes_stay_inside(rec):
         a, w, v = space.integers(da, "rows", more), space.integers(db, "cols", more), space.integers(db, "cols", more + 2)
         c, h = space.tiles(dc, 4, more), space.tiles(dc, 2, more)
         (out,) = call(["int"], lambda: plan.execute_int(a, w, c[0], 0, 0))
-        covers(space, out, c[1], c[2], dc, 4, k)
+        covers(space, out, c[1], c[2], dc, 4, k, 128)
         (out,) = call(["int_gated"], lambda: plan.gated_int(b.DMM_SILU, a, w, v, h[0], 0))
-        covers(space, out, h[1], h[2], dc, 2, k)
+        covers(space, out, h[1], h[2], dc, 2, k, 128)
         if k > 10000:
             continue
         space = Space()
         a, w, v, h, g, u, dh, dg, du = [space.tiles(x, 2, more + y) for y, x in enumerate((da, db, db, dc, dc, dc, dc, dc, dc))]
         (out,) = call(["gated"], lambda: plan.gated(b.DMM_GELU, a[0], w[0], v[0], h[0], g[0], u[0], 0))
-        covers(space, out, h[1], h[2], dc, 2, k)
+        covers(space, out, h[1], h[2], dc, 2, k, 64)
         es = rng.choice((2, 4))
         ga, gw, gv = space.tiles(da, 2, more, 1), space.tiles(db, es, more, 1), space.tiles(db, es, more, 1)
         out = call(["nt", "tn"], lambda: plan.gated_backward(b.DMM_GELU, a[0], w[0], v[0], g[0], u[0], dh[0], dg[0], du[0], ga[0], gw[0], gv[0],
                                                              b.DMM_DB_F32 if es == 4 else 0, 0))
-        covers(space, out[0], ga[1], ga[2], da, 2, 2 * n)
-        covers(space, [o for o in out[1] if in_tiles(space, o[0], gw)], gw[1], gw[2], db, es, m)
-        covers(space, [o for o in out[1] if in_tiles(space, o[0], gv)], gv[1], gv[2], db, es, m)
+        covers(space, out[0], ga[1], ga[2], da, 2, n, 64, 2)
+        covers(space, [o for o in out[1] if in_tiles(space, o[0], gw)], gw[1], gw[2], db, es, m, 64)
+        covers(space, [o for o in out[1] if in_tiles(space, o[0], gv)], gv[1], gv[2], db, es, m, 64)
         out = call(["nt", "tn"], lambda: plan.execute_backward(a[0], w[0], dh[0], ga[0], gw[0], b.DMM_DB_F32 if es == 4 else 0, 0))
-        covers(space, out[0], ga[1], ga[2], da, 2, n)
-        covers(space, out[1], gw[1], gw[2], db, es, m)
+        covers(space, out[0], ga[1], ga[2], da, 2, n, 64)
+        covers(space, out[1], gw[1], gw[2], db, es, m, 64)
         rec.check_tables()
         plan.destroy()
 
@@ -256,13 +275,13 @@ def narrow_tiles(rec):
                 at = len(rec.ops())
                 plan.gated(b.DMM_SILU, a[0], w[0], v[0], h[0], None, None, 0)
                 (out,) = follow_call(rec, space, at, ["gated"])
-                covers(space, out, h[1], h[2], d[2], 2, k)
+                covers(space, out, h[1], h[2], d[2], 2, k, 64)
                 ga, gw = space.tiles(d[0], 2, more), space.tiles(d[1], 4, more)
                 at = len(rec.ops())
                 plan.execute_backward(a[0], w[0], h[0], ga[0], gw[0], b.DMM_DB_F32, 0)
                 out = follow_call(rec, space, at, ["nt", "tn"])
-                covers(space, out[0], ga[1], ga[2], d[0], 2, n)
-                covers(space, out[1], gw[1], gw[2], d[1], 4, m)
+                covers(space, out[0], ga[1], ga[2], d[0], 2, n, 64)
+                covers(space, out[1], gw[1], gw[2], d[1], 4, m, 64)
 
 
 SCENARIOS = [reads_and_writes_stay_inside, narrow_tiles]
