@@ -262,57 +262,66 @@ int lay_out(const LayerWork &W, const LayerChoice &choice, std::vector<char> *h,
         sum += W.segs[tail++].tail;
       }
       if (layer_i8(W.kind) && sum > kLayerSum) return DMM_ELIMIT;
-      // bands of eight tile rows, column by column: neighbours in the list share operands.  All first ranges of K, then all second ones, ...
+      // Blocks of 32 neighbours that share operands, eight tile rows by four tile columns, and the same columns of the eight rows below next, so that eight
+      // blocks are 16 by 16 tiles.  All first ranges of K, then all second ones, ...
       int64_t tile = 0;
-      for (int64_t r0 = 0; r0 < rows; r0 += 8)
-        for (int64_t c = 0; c < cols; ++c)
-          for (int64_t r = r0; r < std::min(r0 + 8, rows); ++r, ++tile) {
-            LayerItem it;
-            std::memset(&it, 0, sizeof it);
-            it.m_off = (int32_t)(r * tm);
-            it.n_off = (int32_t)(c * tn);
-            it.m_ext = (int32_t)std::min<int64_t>(tm, g.m - r * tm);
-            it.n_ext = (int32_t)std::min<int64_t>(tn, g.n - c * tn);
-            it.c = g.c + (r * tm * g.ldc + c * tn) * W.c_es;
-            it.ldc = g.ldc;
-            it.c_es = W.c_es;
-            if (g.g) it.g = g.g + (r * tm * g.ldg + c * tn) * 2;
-            if (g.u) it.u = g.u + (r * tm * g.ldu + c * tn) * 2;
-            it.ldg = g.ldg;
-            it.ldu = g.ldu;
-            if (g.sa) it.sa = g.sa + r * tm;
-            if (g.sb) it.sb = g.sb + c * tn;
-            if (g.sb2) it.sb2 = g.sb2 + c * tn;
-            if (n_steps > 0) it.front = W.segs[seg];
-            it.seg = (int32_t)seg;
-            it.n_segs = (int32_t)(g.seg + g.n_segs - seg);
-            it.first = (int32_t)first;
-            it.steps = (int32_t)n_steps;
-            it.tail_seg = (int32_t)tail0;
-            it.n_tails = (int32_t)(tail - tail0);
-            it.what = k == 0 ? LAYER_ZERO : LAYER_STORE;
-            if (runs > 1) {
-              const int64_t slot = first_slot + tile * runs;
-              if (run == 0)
-                joins.push_back({it.c, it.ldc, it.g, it.u, it.ldg, it.ldu, it.sa, it.sb, it.sb2, (const char *)(uintptr_t)((size_t)slot * slot_bytes),
-                                 (int32_t)runs, tm, wide, it.m_ext, it.n_ext, it.c_es});
-              it.c = (char *)(uintptr_t)((size_t)(slot + run) * slot_bytes);
-              it.what = LAYER_PARTS;
-              ++slots;
-            }
-            items.push_back(it);
-          }
+      for (int64_t r0 = 0; r0 < rows; r0 += 16) {
+        const int64_t wide_block = 32 / std::min<int64_t>(8, rows - r0);
+        for (int64_t c0 = 0; c0 < cols; c0 += wide_block)
+          for (int64_t band = r0; band < std::min(r0 + 16, rows); band += 8)
+            for (int64_t c = c0; c < std::min(c0 + wide_block, cols); ++c)
+              for (int64_t r = band; r < std::min(band + 8, rows); ++r, ++tile) {
+                LayerItem it;
+                std::memset(&it, 0, sizeof it);
+                it.m_off = (int32_t)(r * tm);
+                it.n_off = (int32_t)(c * tn);
+                it.m_ext = (int32_t)std::min<int64_t>(tm, g.m - r * tm);
+                it.n_ext = (int32_t)std::min<int64_t>(tn, g.n - c * tn);
+                it.c = g.c + (r * tm * g.ldc + c * tn) * W.c_es;
+                it.ldc = g.ldc;
+                it.c_es = W.c_es;
+                if (g.g) it.g = g.g + (r * tm * g.ldg + c * tn) * 2;
+                if (g.u) it.u = g.u + (r * tm * g.ldu + c * tn) * 2;
+                it.ldg = g.ldg;
+                it.ldu = g.ldu;
+                if (g.sa) it.sa = g.sa + r * tm;
+                if (g.sb) it.sb = g.sb + c * tn;
+                if (g.sb2) it.sb2 = g.sb2 + c * tn;
+                if (n_steps > 0) it.front = W.segs[seg];
+                it.seg = (int32_t)seg;
+                it.n_segs = (int32_t)(g.seg + g.n_segs - seg);
+                it.first = (int32_t)first;
+                it.steps = (int32_t)n_steps;
+                it.tail_seg = (int32_t)tail0;
+                it.n_tails = (int32_t)(tail - tail0);
+                it.what = k == 0 ? LAYER_ZERO : LAYER_STORE;
+                if (runs > 1) {
+                  const int64_t slot = first_slot + tile * runs;
+                  if (run == 0)
+                    joins.push_back({it.c, it.ldc, it.g, it.u, it.ldg, it.ldu, it.sa, it.sb, it.sb2, (const char *)(uintptr_t)((size_t)slot * slot_bytes),
+                                     (int32_t)runs, tm, wide, it.m_ext, it.n_ext, it.c_es});
+                  it.c = (char *)(uintptr_t)((size_t)(slot + run) * slot_bytes);
+                  it.what = LAYER_PARTS;
+                  ++slots;
+                }
+                items.push_back(it);
+              }
+      }
       first += n_steps;
     }
   }
   if ((int64_t)items.size() > kLayerBlocks || (int64_t)joins.size() * ((tm * tn + 1023) / 1024) > kLayerBlocks) return DMM_ELIMIT;
   if (items.empty()) return DMM_OK;
-  // workgroup w runs on XCD w % 8: every XCD gets a run of the list
+  // Workgroup w runs on XCD w % 8.  Blocks go to the XCDs in turn, so that all of them are in one region of one group, where what one brings into the
+  // last-level cache serves the others (8192 x 12288 x 49152 gated in column blocks, each with a replica of A of its own: 15.7 ms with a run of the
+  // list for every XCD); what is left of the list, a run of it for each.
   std::vector<LayerItem> ordered(items.size());
   {
-    size_t from = 0;
+    const size_t even = items.size() / 256 * 256;
+    for (size_t x = 0; x < even; ++x) ordered[x / 256 * 256 + x % 32 * 8 + x / 32 % 8] = items[x];
+    size_t from = even;
     for (size_t xcd = 0; xcd < 8; ++xcd)
-      for (size_t w = xcd; w < items.size(); w += 8) ordered[w] = items[from++];
+      for (size_t w = even + xcd; w < items.size(); w += 8) ordered[w] = items[from++];
   }
   *scratch = std::max(*scratch, (size_t)slots * slot_bytes);
   L->shape = shape;
