@@ -144,10 +144,27 @@ struct LayerCopies {
     jobs.push_back(j);
     bytes += (double)rows * (double)row_bytes * (src ? 2 : 1);
   }
-  // Replica 0 of a matrix, a row-major one with `rows` x `cols` elements to be there in the end; `turned`: its tiles lie transposed, and so does the copy.
-  Matrix matrix(const Grid &G, const void *const *tiles, const int64_t *ld, int es, bool turned, int64_t rows, int64_t cols) {
-    const int64_t have_rows = turned ? G.cols : G.rows, have_cols = turned ? G.rows : G.cols;
-    const int64_t pitch = (cols * es + 127) / 128 * 128 | 128;   // (an odd number of lines: rows start in different channels)
+  // Where the columns of a matrix lie in its copy: those from every cut on start at a multiple of 128 bytes, so that macro-tiles that begin there read
+  // aligned rows.
+  struct Axis {
+    std::vector<int64_t> cuts, at;
+    int64_t total = 0;                 // columns of the copy
+    Axis(const std::vector<int64_t> &c, int64_t step) : cuts(merged_cuts({&c})) {
+      for (size_t i = 0; i + 1 < cuts.size(); ++i) {
+        at.push_back(total);
+        total += (cuts[i + 1] - cuts[i] + step - 1) / step * step;
+      }
+    }
+    int64_t place(int64_t col) const {
+      const size_t i = (size_t)(std::upper_bound(cuts.begin(), cuts.end(), col) - cuts.begin()) - 1;
+      return at[i] + col - cuts[i];
+    }
+  };
+  // Replica 0 of a matrix, `rows` rows and the columns of `axis` to be there in the end, zeros where the matrix has none (`zeros`; otherwise what lies between the
+  // columns is left as it is).  `turned`: its tiles lie transposed, and so does the copy.
+  Matrix matrix(const Grid &G, const void *const *tiles, const int64_t *ld, int es, bool turned, int64_t rows, const Axis &axis, bool zeros) {
+    const int64_t have_rows = turned ? G.cols : G.rows;
+    const int64_t pitch = (axis.total * es + 127) / 128 * 128 | 128;   // (an odd number of lines: rows start in different channels)
     const Matrix m = {size, pitch};
     if (pitch >= kLayerPitch || rows > 0x7fffff00) fits = false;
     size += (size_t)(rows * pitch + 128 + 4095) / 4096 * 4096;   // (a read of eight columns may pass the last row's end)
@@ -156,10 +173,17 @@ struct LayerCopies {
         const int64_t r0 = turned ? G.cc[(size_t)tj] : G.rc[(size_t)ti], r1 = turned ? G.cc[(size_t)tj + 1] : G.rc[(size_t)ti + 1];
         const int64_t c0 = turned ? G.rc[(size_t)ti] : G.cc[(size_t)tj], c1 = turned ? G.rc[(size_t)ti + 1] : G.cc[(size_t)tj + 1];
         const int64_t i = G.table_index(0, ti, tj);
-        if (r1 > r0 && c1 > c0) job(tiles[i], ld[i] * es, m.at + (size_t)(r0 * pitch + c0 * es), pitch, r1 - r0, (c1 - c0) * es);
+        for (size_t x = 0; x + 1 < axis.cuts.size(); ++x) {
+          const int64_t lo = std::max(c0, axis.cuts[x]), hi = std::min(c1, axis.cuts[x + 1]);
+          if (r1 > r0 && hi > lo)
+            job((const char *)tiles[i] + (lo - c0) * es, ld[i] * es, m.at + (size_t)(r0 * pitch + axis.place(lo) * es), pitch, r1 - r0, (hi - lo) * es);
+        }
       }
-    job(nullptr, 0, m.at + (size_t)(have_cols * es), pitch, have_rows, (cols - have_cols) * es);
-    job(nullptr, 0, m.at + (size_t)(have_rows * pitch), pitch, rows - have_rows, cols * es);
+    for (size_t x = 0; zeros && x + 1 < axis.cuts.size(); ++x) {
+      const int64_t end = axis.at[x] + axis.cuts[x + 1] - axis.cuts[x], next = x + 1 < axis.at.size() ? axis.at[x + 1] : axis.total;
+      job(nullptr, 0, m.at + (size_t)(end * es), pitch, have_rows, (next - end) * es);
+    }
+    job(nullptr, 0, m.at + (size_t)(have_rows * pitch), pitch, rows - have_rows, axis.total * es);
     return m;
   }
   // scales of replica 0, one behind another
@@ -644,13 +668,14 @@ std::vector<LayerWork> gradients(const dmm_plan_t *P, const dmm_tiles *a, const 
       if (db[p]) weight_gradient(P, a, dc[p], db[p], &works.back());
     return works;
   }
-  // dC serves along n and across m
-  const int64_t m = up_to(C.rows, 64), n = up_to(C.cols, 64);
+  // dC serves along n and across m; its columns are those of dB's tiles
+  const LayerCopies::Axis cols(B.cc, 64), rows(B.rc, 64);
+  const int64_t m = up_to(C.rows, 64), n = cols.total;
   LayerCopies::Matrix cc[2];
-  for (int p = 0; p < pairs; ++p) cc[p] = copies->matrix(C, dc[p]->tiles, dc[p]->ld, 2, false, m, n);
+  for (int p = 0; p < pairs; ++p) cc[p] = copies->matrix(C, dc[p]->tiles, dc[p]->ld, 2, false, m, cols, da != nullptr);
   if (da) {
     LayerCopies::Matrix cb[2];
-    for (int p = 0; p < pairs; ++p) cb[p] = copies->matrix(B, b[p]->tiles, b[p]->ld, 2, false, B.rows, n);
+    for (int p = 0; p < pairs; ++p) cb[p] = copies->matrix(B, b[p]->tiles, b[p]->ld, 2, false, B.rows, cols, true);
     LayerWork &W = works.front();
     tile_groups(
         A, &W,
@@ -665,14 +690,14 @@ std::vector<LayerWork> gradients(const dmm_plan_t *P, const dmm_tiles *a, const 
         });
   }
   if (any_db) {
-    const LayerCopies::Matrix ca = copies->matrix(A, a->tiles, a->ld, 2, false, m, A.cols);
+    const LayerCopies::Matrix ca = copies->matrix(A, a->tiles, a->ld, 2, false, m, rows, false);
     LayerWork &W = works.back();
     for (int p = 0; p < pairs; ++p) {
       if (!db[p]) continue;
       tile_groups(
           B, &W,
           [&](int64_t k0, int64_t n0) {
-            W.segs.push_back(dense_segment(ca.at + (size_t)k0 * 2, ca.pitch, cc[p].at + (size_t)n0 * 2, cc[p].pitch, 0, 0, m / 64));
+            W.segs.push_back(dense_segment(ca.at + (size_t)rows.place(k0) * 2, ca.pitch, cc[p].at + (size_t)cols.place(n0) * 2, cc[p].pitch, 0, 0, m / 64));
           },
           [&](int32_t, int32_t ti, int32_t tj, int64_t k0, int64_t n0, LayerGroup *r) {
             const int64_t i = B.table_index(0, ti, tj);
@@ -711,10 +736,12 @@ int i8_product(dmm_plan_t *P, int which, int act, const dmm_int_tiles *a, const 
       r->ldc = c->ld[i];
     };
     if (copies) {
-      const int64_t k = up_to(A.cols, layer_step(W.kind));
-      const LayerCopies::Matrix ca = copies->matrix(A, a->codes, a->code_ld, 1, false, A.rows, k), cb = copies->matrix(B, b->codes, b->code_ld, 1, true, B.cols, k);
+      const LayerCopies::Axis along({0, A.cols}, layer_step(W.kind));
+      const int64_t k = along.total;
+      const LayerCopies::Matrix ca = copies->matrix(A, a->codes, a->code_ld, 1, false, A.rows, along, true),
+                                cb = copies->matrix(B, b->codes, b->code_ld, 1, true, B.cols, along, true);
       LayerCopies::Matrix cb2 = {0, 0};
-      if (b2) cb2 = copies->matrix(B, b2->codes, b2->code_ld, 1, true, B.cols, k);
+      if (b2) cb2 = copies->matrix(B, b2->codes, b2->code_ld, 1, true, B.cols, along, true);
       const size_t sa = copies->scales(A.rc, a->scales), sb = copies->scales(B.cc, b->scales), sb2 = b2 ? copies->scales(B.cc, b2->scales) : 0;
       tile_groups(
           C, &W,
@@ -759,15 +786,12 @@ int i8_product(dmm_plan_t *P, int which, int act, const dmm_int_tiles *a, const 
 }
 
 // dU = dH act(G), dG = dH U act'(G), tile by tile.
+int64_t slope_blocks(int64_t h, int64_t w) { return (h * ((w + 7) / 8) + SLOPE_CHUNKS - 1) / SLOPE_CHUNKS; }
 int slope(const Grid &C, int act, const dmm_tiles *g, const dmm_tiles *u, const dmm_tiles *dh, const dmm_tiles *dg, const dmm_tiles *du, hipStream_t stream) {
   SlopeArgs args;
   std::memset(&args, 0, sizeof args);
   args.act = act;
   int64_t blocks = 0;
-  auto blocks_of = [](int64_t h, int64_t w, int32_t *across) -> int64_t {
-    *across = (int32_t)((w + SLOPE_COLS - 1) / SLOPE_COLS);
-    return ((h + SLOPE_ROWS - 1) / SLOPE_ROWS * *across + 3) / 4;
-  };
   auto flush = [&]() -> int {
     if (!args.n) return DMM_OK;
     slope_launch(args, (int)blocks, stream);
@@ -796,7 +820,7 @@ int slope(const Grid &C, int act, const dmm_tiles *g, const dmm_tiles *u, const 
       t.pdu = du->ld[i] * 2;
       t.h = (int32_t)h;
       t.w = (int32_t)w;
-      const int64_t n = blocks_of(h, w, &t.blocks_across);
+      const int64_t n = slope_blocks(h, w);
       if ((args.n == SLOPE_TILES || blocks + n > kLayerBlocks) && (rc = flush())) return rc;
       t.first_block = (int32_t)blocks;
       blocks += n;
@@ -809,7 +833,7 @@ int check_slope(const Grid &C) {
   for (int32_t ti = 0; ti < C.gr; ++ti)
     for (int32_t tj = 0; tj < C.gc; ++tj) {
       const int64_t h = C.rc[(size_t)ti + 1] - C.rc[(size_t)ti], w = C.cc[(size_t)tj + 1] - C.cc[(size_t)tj];
-      if (h > 0x7fffff00 || w > 0x7fffff00 || ((h + SLOPE_ROWS - 1) / SLOPE_ROWS) * ((w + SLOPE_COLS - 1) / SLOPE_COLS) / 4 >= kLayerBlocks) return DMM_ELIMIT;
+      if (h > 0x7fffff00 || w > 0x7fffff00 || slope_blocks(h, w) > kLayerBlocks) return DMM_ELIMIT;
     }
   return DMM_OK;
 }
@@ -1031,13 +1055,16 @@ int dmm_gated_execute(dmm_plan_t *P, int activation, const dmm_tiles *a, const d
         if (u) r->u = corner(C, u, i, ti, tj, m0, n0, 2), r->ldu = u->ld[i];
       };
       if (copies) {
-        const int64_t k = up_to(A.cols, 64);
-        const LayerCopies::Matrix ca = copies->matrix(A, a->tiles, a->ld, 2, false, A.rows, k), cg = copies->matrix(B, gate->tiles, gate->ld, 2, false, k, B.cols),
-                                  cu = copies->matrix(B, up->tiles, up->ld, 2, false, k, B.cols);
+        const LayerCopies::Axis along({0, A.cols}, 64), cols(C.cc, 64);
+        const int64_t k = along.total;
+        const LayerCopies::Matrix ca = copies->matrix(A, a->tiles, a->ld, 2, false, A.rows, along, true),
+                                  cg = copies->matrix(B, gate->tiles, gate->ld, 2, false, k, cols, false),
+                                  cu = copies->matrix(B, up->tiles, up->ld, 2, false, k, cols, false);
         tile_groups(
             C, &W,
             [&](int64_t m0, int64_t n0) {
-              W.segs.push_back(dense_segment(ca.at + (size_t)(m0 * ca.pitch), ca.pitch, cg.at + (size_t)n0 * 2, cg.pitch, cu.at + (size_t)n0 * 2, cu.pitch, k / 64));
+              const size_t col = (size_t)cols.place(n0) * 2;
+              W.segs.push_back(dense_segment(ca.at + (size_t)(m0 * ca.pitch), ca.pitch, cg.at + col, cg.pitch, cu.at + col, cu.pitch, k / 64));
             },
             result);
         return works;

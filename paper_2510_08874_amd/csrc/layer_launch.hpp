@@ -107,14 +107,14 @@ struct SlopeTile {
   char *dg, *du;
   int64_t pg, pu, ph, pdg, pdu;  // bytes from row to row
   int32_t h, w;
-  int32_t first_block, blocks_across;
+  int32_t first_block, pad;
 };
 constexpr int SLOPE_TILES = 32;
 struct SlopeArgs {
   int32_t n, act;
   SlopeTile tile[SLOPE_TILES];
 };
-constexpr int SLOPE_ROWS = 4, SLOPE_COLS = 512;   // rows of so many columns a wave
+constexpr int SLOPE_CHUNKS = 1024;                // of eight elements of a row, a workgroup
 void slope_launch(const SlopeArgs &args, int blocks, hipStream_t stream);
 
 // ---- 8-bit integers -------------------------------------------------------------------------------------

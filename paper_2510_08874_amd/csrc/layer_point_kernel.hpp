@@ -106,26 +106,32 @@ __global__ __launch_bounds__(256) void layer_copy_kernel(const LayerCopy *__rest
     if (mine[i]) __builtin_memcpy(to[i], &v[i], 16);
 }
 
-// dU = dH act(G), dG = dH U act'(G): eight elements of SLOPE_ROWS rows a lane.  Every element is read before it is written, so dG and dU may
-// be G and U themselves.
+// dU = dH act(G), dG = dH U act'(G): a thread has four pieces of eight neighbouring elements, whatever rows they are of.  Every element is read and written
+// by one thread, in this order, so dG and dU may be G and U themselves.
 __global__ __launch_bounds__(256) void layer_slope_kernel(SlopeArgs) {
   const auto &args = *(const SlopeArgs *)__builtin_amdgcn_kernarg_segment_ptr();
+  constexpr int N = SLOPE_CHUNKS / 256;
   int block;
   const SlopeTile &T = layer_find(args, blockIdx.x, &block);
-  const int unit = block * 4 + (threadIdx.x >> 6), across = T.blocks_across;
-  const int col = (unit % across) * SLOPE_COLS + (threadIdx.x & 63) * 8, row0 = unit / across * SLOPE_ROWS;
-  if (col >= T.w) return;
-  LayerVec<false> g[SLOPE_ROWS], u[SLOPE_ROWS], h[SLOPE_ROWS];
+  const unsigned across = (unsigned)(T.w + 7) / 8;
+  const uint64_t first = (uint64_t)block * SLOPE_CHUNKS;
+  const unsigned row0 = (unsigned)(first / across), col0 = (unsigned)(first % across);
+  LayerVec<false> g[N], u[N], h[N];
+  int row[N], col[N];
 #pragma unroll
-  for (int i = 0; i < SLOPE_ROWS; ++i)
-    if (row0 + i < T.h) {
-      g[i] = layer_load8<false>(T.g + (int64_t)(row0 + i) * T.pg, col, T.w);
-      u[i] = layer_load8<false>(T.u + (int64_t)(row0 + i) * T.pu, col, T.w);
-      h[i] = layer_load8<false>(T.dh + (int64_t)(row0 + i) * T.ph, col, T.w);
+  for (int i = 0; i < N; ++i) {
+    const unsigned on = col0 + i * 256 + threadIdx.x;
+    row[i] = (int)(row0 + on / across);
+    col[i] = (int)(on % across) * 8;
+    if (row[i] < T.h) {
+      g[i] = layer_load8<false>(T.g + row[i] * T.pg, col[i], T.w);
+      u[i] = layer_load8<false>(T.u + row[i] * T.pu, col[i], T.w);
+      h[i] = layer_load8<false>(T.dh + row[i] * T.ph, col[i], T.w);
     }
+  }
 #pragma unroll
-  for (int i = 0; i < SLOPE_ROWS; ++i)
-    if (row0 + i < T.h) {
+  for (int i = 0; i < N; ++i)
+    if (row[i] < T.h) {
       LayerVec<false> dg, du;
 #pragma unroll
       for (int x = 0; x < 8; ++x) {
@@ -135,8 +141,8 @@ __global__ __launch_bounds__(256) void layer_slope_kernel(SlopeArgs) {
         dg.set(x, dh * u[i].at(x) * slope);
         du.set(x, dh * value);
       }
-      layer_store8<false>(T.dg + (int64_t)(row0 + i) * T.pdg, col, T.w, dg);
-      layer_store8<false>(T.du + (int64_t)(row0 + i) * T.pdu, col, T.w, du);
+      layer_store8<false>(T.dg + row[i] * T.pdg, col[i], T.w, dg);
+      layer_store8<false>(T.du + row[i] * T.pdu, col[i], T.w, du);
     }
 }
 
@@ -233,6 +239,22 @@ __global__ __launch_bounds__(256) void i8_scales_kernel(I8ScaleArgs, int what) {
   *at = what == I8_CLEAR ? 0.f : i8_scale(__builtin_bit_cast(unsigned, *at));
 }
 
+// A workgroup's place in a tile.  Neighbours share lines, of the matrix where rows are not aligned and of the integers along the columns, so every XCD (workgroup
+// w runs on XCD w % 8) has a run of the blocks, four side by side and then down the tile.  (`all` workgroups in the launch.)
+struct I8Place {
+  int row0, col0;
+};
+__device__ __forceinline__ int i8_in_order(int all) {
+  const int xcd = (int)blockIdx.x % 8, each = all / 8, more = all % 8;
+  return xcd * each + min(xcd, more) + (int)blockIdx.x / 8;
+}
+template <int ROWS, int COLS>
+__device__ __forceinline__ I8Place i8_place(const I8Tile &T, int block) {
+  const int down = (T.h + ROWS - 1) / ROWS, strip = block / (4 * down), in = block % (4 * down);
+  const int wide = min(4, T.blocks_across - 4 * strip);
+  return {in / wide * ROWS, (4 * strip + in % wide) * COLS};
+}
+
 // A workgroup's 128 rows of 64 (128) columns: threads to a row of a pass, rows of a pass.
 template <bool F32>
 struct I8Block {
@@ -247,8 +269,9 @@ __global__ __launch_bounds__(256) void i8_amax_kernel(I8Args) {
   __shared__ unsigned tops[128];
   const auto &args = *(const I8Args *)__builtin_amdgcn_kernarg_segment_ptr();
   int block;
-  const I8Tile &T = layer_find(args, blockIdx.x, &block);
-  const int col0 = (block % T.blocks_across) * B::COLS, row0 = block / T.blocks_across * 128;
+  const I8Tile &T = layer_find(args, i8_in_order(gridDim.x), &block);
+  const I8Place place0 = i8_place<128, B::COLS>(T, block);
+  const int col0 = place0.col0, row0 = place0.row0;
   const int tid = threadIdx.x, col = col0 + tid % B::ACROSS * 8, r0 = tid / B::ACROSS;
   LayerVec<F32> v[B::PASSES];
 #pragma unroll
@@ -291,8 +314,9 @@ __global__ __launch_bounds__(256) void i8_rows_kernel(I8Args) {
   using B = I8Block<F32>;
   const auto &args = *(const I8Args *)__builtin_amdgcn_kernarg_segment_ptr();
   int block;
-  const I8Tile &T = layer_find(args, blockIdx.x, &block);
-  const int col0 = (block % T.blocks_across) * B::COLS, row0 = block / T.blocks_across * 128;
+  const I8Tile &T = layer_find(args, i8_in_order(gridDim.x), &block);
+  const I8Place place0 = i8_place<128, B::COLS>(T, block);
+  const int col0 = place0.col0, row0 = place0.row0;
   const int col = col0 + threadIdx.x % B::ACROSS * 8, r0 = threadIdx.x / B::ACROSS;
 #pragma unroll
   for (int x = 0; x < B::PASSES; ++x) {
@@ -313,8 +337,9 @@ __global__ __launch_bounds__(256) void i8_cols_kernel(I8Args) {
   auto place = [](int row) { return row * B::PITCH + (row >> 5) * 64; };   // (16 words on every 32 rows: four threads read these side by side)
   const auto &args = *(const I8Args *)__builtin_amdgcn_kernarg_segment_ptr();
   int block;
-  const I8Tile &T = layer_find(args, blockIdx.x, &block);
-  const int col0 = (block % T.blocks_across) * B::COLS, row0 = block / T.blocks_across * 128;
+  const I8Tile &T = layer_find(args, i8_in_order(gridDim.x), &block);
+  const I8Place place0 = i8_place<128, B::COLS>(T, block);
+  const int col0 = place0.col0, row0 = place0.row0;
   const int tid = threadIdx.x;
   {
     const int col = col0 + tid % B::ACROSS * 8, r0 = tid / B::ACROSS;
@@ -411,8 +436,9 @@ __global__ __launch_bounds__(256) void i8_row_values_kernel(I8Args) {
   using B = I8Block<F32>;
   const auto &args = *(const I8Args *)__builtin_amdgcn_kernarg_segment_ptr();
   int block;
-  const I8Tile &T = layer_find(args, blockIdx.x, &block);
-  const int col = (block % T.blocks_across) * B::COLS + threadIdx.x % B::ACROSS * 8, row0 = block / T.blocks_across * 128 + threadIdx.x / B::ACROSS;
+  const I8Tile &T = layer_find(args, i8_in_order(gridDim.x), &block);
+  const I8Place place0 = i8_place<128, B::COLS>(T, block);
+  const int col = place0.col0 + threadIdx.x % B::ACROSS * 8, row0 = place0.row0 + threadIdx.x / B::ACROSS;
   if (col >= T.w) return;
 #pragma unroll
   for (int x = 0; x < B::PASSES; ++x) {
@@ -436,8 +462,9 @@ __global__ __launch_bounds__(256) void i8_col_values_kernel(I8Args) {
   auto place = [](int row) { return row * B::PITCH + (row >> 5) * 64; };
   const auto &args = *(const I8Args *)__builtin_amdgcn_kernarg_segment_ptr();
   int block;
-  const I8Tile &T = layer_find(args, blockIdx.x, &block);
-  const int col0 = (block % T.blocks_across) * B::COLS, row0 = block / T.blocks_across * 128;
+  const I8Tile &T = layer_find(args, i8_in_order(gridDim.x), &block);
+  const I8Place place0 = i8_place<128, B::COLS>(T, block);
+  const int col0 = place0.col0, row0 = place0.row0;
   const int tid = threadIdx.x, b = tid & 3, p = tid >> 2;
   constexpr int OWN = F32 ? 1 : 2;
   unsigned w[OWN][8];

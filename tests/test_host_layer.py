@@ -172,10 +172,11 @@ def follow_call(rec, space, at, kinds):
     return got
 
 
-def covers(space, out, ptr, ld, d, es, k, step, times=1, replicas=1):
-    """Every element of the tiles is written once, with all of K (on copies, filled up to whole steps)."""
+def covers(space, out, ptr, ld, d, es, k, step, times=1, cuts=None, replicas=1):
+    """Every element of the tiles is written once, with all of K (on copies, filled up to whole steps, every interval of `cuts`)."""
     seen = {}
-    k = (-(-k // step) * step if space.copies else k) * times
+    cuts = cuts or [0, k]
+    k = (sum(-(-(j - i) // step) * step for i, j in zip(cuts, cuts[1:])) if space.copies else k) * times
     for c, ldc, c_es, h, w, k_sum in out:
         assert c_es == es and k_sum == k, (c_es, es, k_sum, k)
         i = bisect.bisect_right(space.start, c) - 1
@@ -246,11 +247,11 @@ def reads_and_writes_stay_inside(rec):
         ga, gw, gv = space.tiles(da, 2, more, 1), space.tiles(db, es, more, 1), space.tiles(db, es, more, 1)
         out = call(["nt", "tn"], lambda: plan.gated_backward(b.DMM_GELU, a[0], w[0], v[0], g[0], u[0], dh[0], dg[0], du[0], ga[0], gw[0], gv[0],
                                                              b.DMM_DB_F32 if es == 4 else 0, 0))
-        covers(space, out[0], ga[1], ga[2], da, 2, n, 64, 2)
+        covers(space, out[0], ga[1], ga[2], da, 2, n, 64, 2, db["col_cuts"])
         covers(space, [o for o in out[1] if in_tiles(space, o[0], gw)], gw[1], gw[2], db, es, m, 64)
         covers(space, [o for o in out[1] if in_tiles(space, o[0], gv)], gv[1], gv[2], db, es, m, 64)
         out = call(["nt", "tn"], lambda: plan.execute_backward(a[0], w[0], dh[0], ga[0], gw[0], b.DMM_DB_F32 if es == 4 else 0, 0))
-        covers(space, out[0], ga[1], ga[2], da, 2, n, 64)
+        covers(space, out[0], ga[1], ga[2], da, 2, n, 64, 1, db["col_cuts"])
         covers(space, out[1], gw[1], gw[2], db, es, m, 64)
         rec.check_tables()
         plan.destroy()
@@ -280,7 +281,7 @@ def narrow_tiles(rec):
                 at = len(rec.ops())
                 plan.execute_backward(a[0], w[0], h[0], ga[0], gw[0], b.DMM_DB_F32, 0)
                 out = follow_call(rec, space, at, ["nt", "tn"])
-                covers(space, out[0], ga[1], ga[2], d[0], 2, n, 64)
+                covers(space, out[0], ga[1], ga[2], d[0], 2, n, 64, 1, d[1]["col_cuts"])
                 covers(space, out[1], gw[1], gw[2], d[1], 4, m, 64)
 
 
