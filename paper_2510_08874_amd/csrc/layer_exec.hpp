@@ -109,6 +109,8 @@ void put_segment(LayerWork *W, LayerSeg s, int64_t len, int64_t guard) {
   W->segs.push_back(s);
 }
 
+int64_t up_to(int64_t n, int64_t step) { return (n + step - 1) / step * step; }
+
 struct LayerChoice {
   int shape = LAYER_256;
   int64_t runs = 1;
@@ -581,7 +583,6 @@ LayerSeg dense_segment(size_t a, int64_t a_pitch, size_t b, int64_t b_pitch, siz
   s.pad = 0;
   return s;
 }
-int64_t up_to(int64_t n, int64_t step) { return (n + step - 1) / step * step; }
 
 int32_t interval_of(const std::vector<int64_t> &cuts, int64_t at) {   // the non-empty interval that holds `at`
   return (int32_t)(std::upper_bound(cuts.begin(), cuts.end(), at) - cuts.begin()) - 1;
@@ -932,6 +933,9 @@ int i8_form(const Grid &G, int dtype, char *const *x, const int64_t *x_ld, const
           const int64_t w = G.cc[(size_t)tj + 1] - G.cc[(size_t)tj], i = G.table_index(rep, ti, tj);
           if (w > 0) args.piece[args.n++] = {x[i], (char *)q->codes[i], x_ld[i] * es, q->code_ld[i], (int32_t)w, 0};
         }
+        int32_t widest = 0;
+        for (int32_t p = 0; p < args.n; ++p) widest = std::max(widest, args.piece[p].w);
+        const int threads = (int)std::min<int64_t>(I8_ROW_THREADS, up_to(std::max(widest, 512) / 8, 64));
         // (rows past what a launch can have go into the next)
         const int32_t all = args.h;
         for (int32_t at = 0; at < all; at += (int32_t)kLayerBlocks) {
@@ -942,7 +946,7 @@ int i8_form(const Grid &G, int dtype, char *const *x, const int64_t *x_ld, const
             part.piece[p].x += at * part.piece[p].x_pitch;
             part.piece[p].q += at * part.piece[p].q_pitch;
           }
-          i8_whole_rows_launch(part, f32, stream);
+          i8_whole_rows_launch(part, threads, f32, stream);
           DMM_HIP(hipGetLastError());
         }
       }

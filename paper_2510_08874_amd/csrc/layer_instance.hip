@@ -133,8 +133,8 @@ void i8_values_launch(const I8Args &args, int blocks, bool f32, bool cols, hipSt
   if (f32) cols ? i8_col_values_kernel<true><<<grid, block, 0, stream>>>(args) : i8_row_values_kernel<true><<<grid, block, 0, stream>>>(args);
   else cols ? i8_col_values_kernel<false><<<grid, block, 0, stream>>>(args) : i8_row_values_kernel<false><<<grid, block, 0, stream>>>(args);
 }
-void i8_whole_rows_launch(const I8RowArgs &args, bool f32, hipStream_t stream) {
-  const dim3 grid((unsigned)args.h), block(256);
+void i8_whole_rows_launch(const I8RowArgs &args, int threads, bool f32, hipStream_t stream) {
+  const dim3 grid((unsigned)args.h), block((unsigned)threads);
   if (f32) i8_whole_rows_kernel<true><<<grid, block, 0, stream>>>(args);
   else i8_whole_rows_kernel<false><<<grid, block, 0, stream>>>(args);
 }

@@ -17,8 +17,10 @@ __device__ __forceinline__ float layer_f32(unsigned short v) { return __builtin_
 
 // ---- activations ------------------------------------------------------------------------------------
 
-// 1 / (1 + e^-x)
-__device__ __forceinline__ float layer_sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.442695041f * x)); }
+// 16 / (1 + e^-x): the instruction for 1 / x gives zero instead of results below the normal range, and 1 / (1 + e^87.4) is one
+__device__ __forceinline__ float layer_sigmoid16(float x) {
+  return __builtin_amdgcn_rcpf(__builtin_fmaf(0.0625f, __builtin_amdgcn_exp2f(-1.442695041f * x), 0.0625f));
+}
 constexpr float kTanhIn = 1.595769122f, kTanhCube = 0.044715f;   // 2 sqrt(2 / pi): (1 + tanh y) / 2 = 1 / (1 + e^-2y)
 
 // The normal distribution's (1 + erf(g / sqrt 2)) / 2, to 5 units in the last place wherever it is (1 + erf would lose what is left of it where g
@@ -41,24 +43,24 @@ __device__ __forceinline__ float layer_normal(float g) {
 
 template <int ACT>
 __device__ __forceinline__ float layer_act(float g) {
-  if constexpr (ACT == DMM_SILU) return g * layer_sigmoid(g);
+  if constexpr (ACT == DMM_SILU) return 0.0625f * g * layer_sigmoid16(g);
   if constexpr (ACT == DMM_GELU) return g * layer_normal(g);
-  return g * layer_sigmoid(kTanhIn * (g + kTanhCube * g * g * g));
+  return 0.0625f * g * layer_sigmoid16(kTanhIn * (g + kTanhCube * g * g * g));
 }
 // act and its slope
 __device__ __forceinline__ void layer_slope(int act, float g, float *value, float *slope) {
   if (act == DMM_SILU) {
-    const float s = layer_sigmoid(g);
-    *value = g * s;
-    *slope = s * (1.f + g * (1.f - s));
+    const float s16 = layer_sigmoid16(g), s = 0.0625f * s16;
+    *value = 0.0625f * g * s16;
+    *slope = s16 * (0.0625f * (1.f + g * (1.f - s)));
   } else if (act == DMM_GELU) {
     const float p = layer_normal(g);
     *value = g * p;
     *slope = p + g * 0.3989422804f * __builtin_amdgcn_exp2f(-0.7213475204f * g * g);
   } else {
-    const float s = layer_sigmoid(kTanhIn * (g + kTanhCube * g * g * g));
-    *value = g * s;
-    *slope = s + g * s * (1.f - s) * kTanhIn * (1.f + 3.f * kTanhCube * g * g);
+    const float s16 = layer_sigmoid16(kTanhIn * (g + kTanhCube * g * g * g)), s = 0.0625f * s16;
+    *value = 0.0625f * g * s16;
+    *slope = s + *value * (1.f - s) * kTanhIn * (1.f + 3.f * kTanhCube * g * g);
   }
 }
 

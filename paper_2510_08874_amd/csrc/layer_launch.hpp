@@ -149,7 +149,7 @@ struct I8RowPiece {
   int64_t x_pitch, q_pitch;
   int32_t w, pad;
 };
-constexpr int I8_ROW_PIECES = 32;
+constexpr int I8_ROW_PIECES = 32, I8_ROW_THREADS = 1024, I8_ROW_KEPT = 2;   // eight elements of a row, so many a thread
 struct I8RowArgs {
   float *scale;
   int32_t h, n;
@@ -162,6 +162,6 @@ constexpr int i8_block_cols(bool f32) { return f32 ? 64 : 128; }
 void i8_amax_launch(const I8Args &args, int blocks, bool f32, bool cols, hipStream_t stream);
 void i8_quantize_launch(const I8Args &args, int blocks, bool f32, bool cols, hipStream_t stream);
 void i8_values_launch(const I8Args &args, int blocks, bool f32, bool cols, hipStream_t stream);
-void i8_whole_rows_launch(const I8RowArgs &args, bool f32, hipStream_t stream);
+void i8_whole_rows_launch(const I8RowArgs &args, int threads, bool f32, hipStream_t stream);
 
 }  // namespace dmm

@@ -6,16 +6,29 @@
 
 namespace dmm {
 
+// The last of `n` entries that does not begin behind workgroup `block`: 64 of them are looked at together (one after the other each costs the
+// workgroup a read that it waits for).
+template <class Entry>
+__device__ __forceinline__ int layer_last(const Entry *entries, int n, int block) {
+  int count = 0;
+  for (int x = 0; x < n; x += 64) {
+    const int i = x + (int)(threadIdx.x & 63);
+    const int mine = __builtin_popcountll(__ballot(i < n && entries[min(i, n - 1)].first_block <= block));
+    count += mine;
+    if (mine < 64) break;
+  }
+  return __builtin_amdgcn_readfirstlane(count) - 1;
+}
 // the tile that workgroup `block` belongs to, and the workgroup's number inside it
 template <class Args>
 __device__ __forceinline__ const auto &layer_find(const Args &args, int block, int *inside) {
-  int x = 0;
-  while (x + 1 < args.n && block >= args.tile[x + 1].first_block) ++x;
+  const int x = layer_last(args.tile, args.n, block);
   *inside = block - args.tile[x].first_block;
   return args.tile[x];
 }
 
-// Eight neighbouring elements of a row from column `col` on, zeros behind column w; rows may begin anywhere.
+// Eight neighbouring elements of a row from column `col` on, zeros behind column w; rows may begin anywhere.  (Where others write elements in front of
+// `col` at the same time, what is read of them counts for nothing.)
 template <bool F32>
 struct LayerVec {
   static constexpr int WORDS = F32 ? 8 : 4;
@@ -38,6 +51,13 @@ __device__ __forceinline__ LayerVec<F32> layer_load8(const char *row, int col, i
   LayerVec<F32> v;
   if (col + 8 <= w) {
     __builtin_memcpy(v.w, row + (int64_t)col * (F32 ? 4 : 2), sizeof v.w);
+  } else if (!F32 && w >= 8) {
+    // the row's last eight, moved to the front (one by one they keep the wave waiting eight times, and almost every wave meets a row's end)
+    unsigned __int128 all;
+    __builtin_memcpy(&all, row + (int64_t)(w - 8) * 2, 16);
+    const int back = min(col + 8 - w, 8);
+    all = back < 8 ? all >> (16 * back) : 0;
+    __builtin_memcpy(v.w, &all, sizeof v.w);
   } else {
 #pragma unroll
     for (int i = 0; i < LayerVec<F32>::WORDS; ++i) {
@@ -69,13 +89,7 @@ __device__ __forceinline__ void layer_store8(char *row, int col, int w, const La
 // Tiles whose rows are misaligned or finely cut, into dense rows: 16 bytes a thread at a time, eight of them on their way together.  The last 16 bytes
 // of a row are moved as such, over some of those in front of them: a part of 16 bytes would be moved one by one, and every wave meets one.
 __global__ __launch_bounds__(256) void layer_copy_kernel(const LayerCopy *__restrict__ jobs, int n) {
-  int lo = 0, hi = n - 1;                                     // the last job that does not begin behind this workgroup
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (jobs[mid].first_block <= (int)blockIdx.x) lo = mid;
-    else hi = mid - 1;
-  }
-  const LayerCopy j = jobs[lo];
+  const LayerCopy j = jobs[layer_last(jobs, n, (int)blockIdx.x)];
   const unsigned across = (unsigned)(j.bytes + 15) / 16;      // chunks of a row
   const uint64_t all = (uint64_t)across * (unsigned)j.rows, first = (uint64_t)((int)blockIdx.x - j.first_block) * LAYER_COPY_CHUNKS;
   constexpr int N = LAYER_COPY_CHUNKS / 256;
@@ -231,8 +245,7 @@ __device__ __forceinline__ unsigned i8_wave_max(unsigned v) {
 
 __global__ __launch_bounds__(256) void i8_scales_kernel(I8ScaleArgs, int what) {
   const auto &args = *(const I8ScaleArgs *)__builtin_amdgcn_kernarg_segment_ptr();
-  int x = 0;
-  while (x + 1 < args.n && (int)blockIdx.x >= args.piece[x + 1].first_block) ++x;
+  const int x = layer_last(args.piece, args.n, (int)blockIdx.x);
   const int i = ((int)blockIdx.x - args.piece[x].first_block) * 256 + threadIdx.x;
   if (i >= args.piece[x].n) return;
   float *const at = args.piece[x].at + i;
@@ -387,32 +400,36 @@ __global__ __launch_bounds__(256) void i8_cols_kernel(I8Args) {
   }
 }
 
-// The rows of a row of tiles, a workgroup each, scales and integers: what fits is kept between the two passes over a row.
+// The rows of a row of tiles, a workgroup each, scales and integers: what fits is kept between the two passes over a row.  (16 rows of 8192: 256 threads
+// with eight pieces each took 7 us, of which 2 went into turning 32 elements a thread into integers.)
 template <bool F32>
-__global__ __launch_bounds__(256) void i8_whole_rows_kernel(I8RowArgs) {
-  constexpr int KEPT = F32 ? 4 : 8;
-  __shared__ unsigned tops[4];
+__global__ __launch_bounds__(I8_ROW_THREADS) void i8_whole_rows_kernel(I8RowArgs) {
+  constexpr int KEPT = I8_ROW_KEPT;
+  __shared__ unsigned tops[I8_ROW_THREADS / 64];
   const auto &args = *(const I8RowArgs *)__builtin_amdgcn_kernarg_segment_ptr();
-  const int row = blockIdx.x, tid = threadIdx.x;
+  const int row = blockIdx.x, tid = threadIdx.x, threads = blockDim.x;
+  const bool one = args.n == 1;
   LayerVec<F32> kept[KEPT];
   unsigned m = 0;
-  int x = 0;                                                  // vectors of this thread so far
   for (int p = 0; p < args.n; ++p) {
     const I8RowPiece &P = args.piece[p];
     const char *const at = P.x + (int64_t)row * P.x_pitch;
-    if (args.n == 1) {
+    if (one) {
 #pragma unroll
-      for (int y = 0; y < KEPT; ++y) kept[y] = layer_load8<F32>(at, min((y * 256 + tid) * 8, P.w), P.w);
+      for (int y = 0; y < KEPT; ++y) {
+        kept[y] = LayerVec<F32>{};
+        if ((y * threads + tid) * 8 < P.w) kept[y] = layer_load8<F32>(at, (y * threads + tid) * 8, P.w);
+      }
 #pragma unroll
       for (int y = 0; y < KEPT; ++y) m = i8_abs_max(kept[y], m);
-      x = KEPT;
     }
-    for (int col = (x * 256 + tid) * 8; col < P.w; col += 2048) m = i8_abs_max(layer_load8<F32>(at, col, P.w), m);
+    for (int col = ((one ? KEPT * threads : 0) + tid) * 8; col < P.w; col += threads * 8) m = i8_abs_max(layer_load8<F32>(at, col, P.w), m);
   }
   m = i8_wave_max(m);
   if ((tid & 63) == 0) tops[tid >> 6] = m;
   __syncthreads();
-  m = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
+  m = 0;
+  for (int x = 0; x < threads / 64; ++x) m = max(m, tops[x]);
   if (tid == 0) args.scale[row] = i8_scale(m);
   const I8Row r = i8_row(m);
   auto codes = [&](const I8RowPiece &P, int col, const LayerVec<F32> &v) {
@@ -421,12 +438,13 @@ __global__ __launch_bounds__(256) void i8_whole_rows_kernel(I8RowArgs) {
   };
   for (int p = 0; p < args.n; ++p) {
     const I8RowPiece &P = args.piece[p];
-    if (args.n == 1) {
+    if (one) {
 #pragma unroll
       for (int y = 0; y < KEPT; ++y)
-        if ((y * 256 + tid) * 8 < P.w) codes(P, (y * 256 + tid) * 8, kept[y]);
+        if ((y * threads + tid) * 8 < P.w) codes(P, (y * threads + tid) * 8, kept[y]);
     }
-    for (int col = (x * 256 + tid) * 8; col < P.w; col += 2048) codes(P, col, layer_load8<F32>(P.x + (int64_t)row * P.x_pitch, col, P.w));
+    for (int col = ((one ? KEPT * threads : 0) + tid) * 8; col < P.w; col += threads * 8)
+      codes(P, col, layer_load8<F32>(P.x + (int64_t)row * P.x_pitch, col, P.w));
   }
 }
 
