@@ -200,19 +200,25 @@ struct LayerCopies {
 constexpr size_t kLayerCopies = (size_t)1 << 30;               // of a call
 
 
-// By an estimate in us, from what a step (128 bytes of K) of a tile takes.
+// By an estimate in us, from what a step (128 bytes of K) of a tile takes, measured as what more of K costs.  Where rows are not aligned to 16 bytes a step takes a
+// quarter more (integers: a third: 8191^3 direct 625 us, on copies 497; aligned 423), what is left of a segment as much as four steps.
 LayerChoice choose_layer(const LayerWork &W, int cus) {
   const bool gated = layer_gated(W.kind);
   double cells = 0, k_steps = 0, b_bytes = 0;
   int64_t most = 0;
   for (const LayerGroup &g : W.groups) {
     most = std::max(most, g.m);
-    int64_t steps = 0;
-    for (size_t s = g.seg; s < g.seg + g.n_segs; ++s) steps += W.segs[s].steps + (W.segs[s].tail > 0 ? 2 : 0);
+    double steps = 0, bytes = 0;
+    for (size_t x = g.seg; x < g.seg + g.n_segs; ++x) {
+      const LayerSeg &s = W.segs[x];
+      const bool odd = (((uintptr_t)s.a | (uintptr_t)s.b | (uintptr_t)s.b2 | s.a_pitch | s.b_pitch | s.b2_pitch) & 15) != 0;
+      steps += s.steps * (!odd ? 1.0 : layer_i8(W.kind) ? 1.35 : 1.25) + (s.tail > 0 ? 4 : 0);
+      bytes += s.steps + (s.tail > 0);
+    }
     const double area = (double)g.m * (double)g.n;
     cells += area;
-    k_steps += area * (double)steps;
-    b_bytes += (double)g.n * (double)steps * (gated ? 256.0 : 128.0);
+    k_steps += area * steps;
+    b_bytes += (double)g.n * bytes * (gated ? 256.0 : 128.0);
   }
   const double steps = cells > 0 ? std::max(1.0, k_steps / cells) : 1;
   LayerChoice best;
@@ -220,13 +226,15 @@ LayerChoice choose_layer(const LayerWork &W, int cus) {
   for (int shape = 0; shape < LAYER_SHAPES; ++shape) {
     const int tm = kLayerTile[W.kind][shape].tm, tn = kLayerTile[W.kind][shape].tn;
     if (tm == 0 || (shape == LAYER_64 && most > 128) || (shape == LAYER_32 && most > 64)) continue;
+    const double down = std::ceil((double)most / tm);
     double tiles = 0;
     for (const LayerGroup &g : W.groups) tiles += (double)(((g.m + tm - 1) / tm) * ((g.n + tn - 1) / tn));
     if (tiles == 0) return best;
     if (tiles > (double)kLayerBlocks) continue;
     // (two workgroups on a CU where the stages leave room)
     const int places = shape == LAYER_256 || (gated && shape == LAYER_128) ? cus : gated ? cus : 2 * cus;
-    const double memory = 2.0 + b_bytes * std::ceil((double)most / tm > 4 ? 1.0 : 1.0) / 5.0e6;
+    // B from memory; another row of tiles reads it from a cache (48 x 8192 x 28672 gated, integers: 85 us on tiles of 64 rows, 103 on those of 32)
+    const double memory = 2.0 + b_bytes * (1.0 + 0.2 * (down - 1)) / 5.4e6;
     for (int64_t runs = 1; runs <= 32; ++runs) {
       const double work = tiles * (double)runs, per = std::ceil(steps / (double)runs);
       if (runs > 1 && (work > places || per < 3)) break;
@@ -395,9 +403,9 @@ void place_parts(std::vector<char> *h, const LayerLayout &L, char *buf, char *co
 
 // The part of a call that all kinds have in common: the tables of the call before if they are of the same inputs (`key`), else new ones,
 // made from the products that `make` describes (on the operands, or on copies); then `in_front`, the launches and, where `reduce` asks for it, the sum of
-// C's replicas.  A graph's launches are ordered with the plan's other calls by the caller, so nothing is waited for in a capture.
+// C's replicas.
 template <class Make, class Front>
-int run_layer(dmm_plan_t *P, int which, const std::vector<char> &inputs, void *const *c_tiles, const int64_t *c_ld, bool reduce, hipStream_t stream, Make make,
+int run_layer_on(dmm_plan_t *P, int which, const std::vector<char> &inputs, void *const *c_tiles, const int64_t *c_ld, bool reduce, hipStream_t stream, Make make,
               Front in_front) {
   int rc;
   const bool capturing = is_capturing(stream), known = P->dev && P->dev->layer[which].cached;
@@ -411,8 +419,8 @@ int run_layer(dmm_plan_t *P, int which, const std::vector<char> &inputs, void *c
   std::vector<char> key(inputs);
   key.insert(key.end(), (const char *)&device, (const char *)&device + sizeof device);
   if (M.cached && key == M.key) {
-    if (!capturing && (rc = M.table.order_behind_copy(stream))) return rc;
-    if (!capturing && (M.layout[0].n_joins || M.layout[1].n_joins || M.n_copies) && (rc = P->dev->uses.order(stream))) return rc;
+    if ((rc = M.table.order_behind_copy(stream))) return rc;
+    if ((M.layout[0].n_joins || M.layout[1].n_joins || M.n_copies) && (rc = P->dev->uses.order(stream))) return rc;
   } else {
     if (capturing) return DMM_EINVAL;
     M.cached = false;
@@ -501,6 +509,14 @@ int run_layer(dmm_plan_t *P, int which, const std::vector<char> &inputs, void *c
   }
   if (sum && (rc = fire_reduce(P, M.red, stream, false, behind, &marked))) return rc;
   return marked ? DMM_OK : P->dev->uses.mark(stream);
+}
+
+template <class Make, class Front>
+int run_layer(dmm_plan_t *P, int which, const std::vector<char> &inputs, void *const *c_tiles, const int64_t *c_ld, bool reduce, hipStream_t stream, Make make,
+              Front in_front) {
+  const int rc = run_layer_on(P, which, inputs, c_tiles, c_ld, reduce, stream, make, in_front);
+  if (rc == DMM_ENOMEM) (void)hipGetLastError();               // (it would be the next call's)
+  return rc;
 }
 
 struct LayerKey {

@@ -48,12 +48,18 @@ struct LayerShape {
   static_assert(NST >= 2 && (NST - 1) * LOADS < 64 && LDS <= 160 * 1024, "the counter of loads, the LDS of a CU");
 };
 
-// `n` elements (at most 16 bytes' worth) at p, zeros behind them
+// `n` elements (at most 16 bytes' worth) at p, zeros behind them.  Where the row has 16 bytes up to there (`before` elements in front of p) these are read and
+// moved to the front: one by one, a row's end kept every wave waiting up to 15 times.
 template <int ES>
-__device__ __forceinline__ nt_i32x4 layer_some(const char *p, int n) {
+__device__ __forceinline__ nt_i32x4 layer_some(const char *p, int n, int before) {
   nt_i32x4 v = {0, 0, 0, 0};
   if (n >= 16 / ES) {
     __builtin_memcpy(&v, p, 16);
+  } else if (n > 0 && before + n >= 16 / ES) {
+    unsigned __int128 all;
+    const int back = 16 - n * ES;
+    __builtin_memcpy(&all, p - back, 16);
+    v = __builtin_bit_cast(nt_i32x4, all >> (8 * back));
   } else if (n > 0) {
     unsigned w[4] = {0, 0, 0, 0};
 #pragma unroll
@@ -307,10 +313,11 @@ struct LayerTileSums {
         const int off = of_b ? n_off : m_off, ext = of_b ? n_ext : m_ext, at = (second ? y - LB / 2 : y) * 256 + tid;
         if (is_turned) {
           const int k = at >> 4 & 63, col = (at >> 10) * LAYER_SUB + (at & 15) * 8;
-          return layer_some<SH::ES>(p + (int64_t)(off + col) * SH::ES + ((int64_t)s.steps * 64 + k) * pitch, k < s.tail ? ext - col : 0);
+          return layer_some<SH::ES>(p + (int64_t)(off + col) * SH::ES + ((int64_t)s.steps * 64 + k) * pitch, k < s.tail ? ext - col : 0, off + col);
         }
         const int row = at >> 3, k = (at & 7) * SH::CHUNK;
-        return layer_some<SH::ES>(p + (int64_t)(off + row) * pitch + ((int64_t)s.steps * SH::STEP + k) * SH::ES, row < ext ? s.tail - k : 0);
+        return layer_some<SH::ES>(p + (int64_t)(off + row) * pitch + ((int64_t)s.steps * SH::STEP + k) * SH::ES, row < ext ? s.tail - k : 0,
+                                  s.steps > 0 ? SH::CHUNK : k);
       };
       auto keep = [&](bool of_b, int y, nt_i32x4 v) {
         const int at = y * 256 + tid;

@@ -123,12 +123,9 @@ def scales_of(n, seed, spread=8):
 SIZES = [(1, 1, 1), (1, 127, 3), (2, 128, 130), (17, 129, 128), (33, 300, 257), (64, 1000, 64), (100, 640, 129), (130, 257, 131), (257, 1025, 300), (5, 9000, 70), (300, 5000, 500)]
 
 
-@pytest.mark.parametrize("c_dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("layout", [*LAYOUTS, "replicated"])
+@pytest.mark.parametrize("layout,c_dtype", [(x, t) for x in LAYOUTS for t in ("f32", "bf16")] + [("replicated", "f32")])
 @pytest.mark.parametrize("m,k,n", SIZES, ids=str)
 def test_products_of_integers(m, k, n, layout, c_dtype):
-    if layout == "replicated" and c_dtype == "bf16":
-        pytest.skip("bf16 results have one replica")
     (da, db, dc), ranks = descs(layout, m, k, n)
     qa, qb, sa, sb = integers(m, k, m + n), integers(k, n, k), scales_of(m, 1), scales_of(n, 2)
     t = torch.float32 if c_dtype == "f32" else torch.bfloat16

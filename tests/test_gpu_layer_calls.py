@@ -15,14 +15,15 @@ pytestmark = pytest.mark.gpu
 BF16 = torch.bfloat16
 
 # whole tiles; cut along K; on copies
-SIZES = [("blocks", 512, 384, 640), ("whole", 40, 8192, 300), ("uneven", 1301, 1103, 907)]
+SIZES = [("blocks", 512, 512, 768), ("whole", 40, 8192, 300), ("uneven", 1301, 1103, 907)]
 
 
 class Calls:
     """Every product around a layer on the same sizes: what is called, and the tiles that it writes."""
 
     def __init__(self, layout, m, k, n, seed=0):
-        (da, db, dc), ranks = self.descs = descs(layout, m, k, n)
+        self.descs, ranks = descs(layout, m, k, n)
+        da, db, dc = self.descs
         self.plan = binding.Plan(da, db, dc, ranks)
         qa, qg, qu = integers(m, k, seed + 1), integers(k, n, seed + 2), integers(k, n, seed + 3)
         sa, sg, su = scales_of(m, 1, 1) * (k ** -0.5 / 40), scales_of(n, 2, 1) / 40, scales_of(n, 3, 1) / 40

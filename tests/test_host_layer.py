@@ -28,11 +28,11 @@ def bounds(d, replicas):
 class Space:
     """Made-up device buffers that end with a tile's last element, far from each other."""
 
-    def __init__(self):
-        self.at, self.start, self.end, self.copies = 1 << 44, [], [], None
+    def __init__(self, aligned=False):
+        self.at, self.start, self.end, self.copies, self.aligned = 1 << 44, [], [], None, aligned
 
     def take(self, size, align):
-        self.at += align                                       # (at multiples of the element's size, not of more)
+        self.at += 0 if self.aligned else align                # (at multiples of the element's size, not of more)
         start = self.at
         self.start.append(start)
         self.end.append(start + size)
@@ -285,7 +285,144 @@ def narrow_tiles(rec):
                 covers(space, out[1], gw[1], gw[2], d[1], 4, m, 64)
 
 
-SCENARIOS = [reads_and_writes_stay_inside, narrow_tiles]
+def sizes_under_test_take_the_ways_they_are_meant_for(rec):
+    """The sizes of the GPU tests of calls: whole tiles as they lie, tiles cut along K, copies of the operands."""
+    from paper_2510_08874_amd import binding as b
+    for layout, m, k, n, kernels in (("blocks", 512, 512, 768, {"layer_gemm_kernel"}), ("whole", 40, 8192, 300, {"layer_gemm_kernel", "layer_join_kernel"}),
+                                     ("uneven", 1301, 1103, 907, {"layer_gemm_kernel", "layer_copy_kernel"})):
+        d = made(layout, m, k, n)
+        plan, space = b.Plan(*d, 12), Space(True)
+        a, w, v = space.integers(d[0], "rows"), space.integers(d[1], "cols"), space.integers(d[1], "cols")
+        t = [space.tiles(x, 2)[0] for x in (d[0], d[1], d[1], d[2], d[2], d[2], d[2], d[0], d[1])]
+        c = space.tiles(d[2], 4)[0]
+        for call, at_least in ((lambda: plan.execute_int(a, w, c, 0, 0), kernels), (lambda: plan.gated_int(b.DMM_GELU, a, w, v, t[3], 0), kernels),
+                               (lambda: plan.gated(b.DMM_SILU, *t[:4], None, None, 0), kernels), (lambda: plan.execute_backward(t[0], t[1], t[3], t[7], t[8]), set())):
+            at = len(rec.ops())
+            call()
+            got = {o[1] for o in rec.launches(at)}
+            assert got >= at_least and (not at_least or "layer_copy_kernel" in at_least or "layer_copy_kernel" not in got), (layout, got)
+
+
+def made(layout, m, k, n):
+    """As in layer_tiles.py, which needs a GPU."""
+    def uneven(n, parts):
+        cuts = [0] + sorted((n * (i * i + 2 * i) // (parts * parts + 2 * parts)) for i in range(1, parts)) + [n]
+        if parts >= 3:
+            cuts[2] = cuts[1]
+        return cuts
+    D, block = workloads.desc, workloads.block_desc
+    if layout == "whole":
+        return D(m, k, [0, m], [0, k], 1, 1), D(k, n, [0, k], [0, n], 1, 1), D(m, n, [0, m], [0, n], 1, 1)
+    if layout == "blocks":
+        return block(m, k, 2, 2), block(k, n, 2, 2), block(m, n, 2, 2)
+    return D(m, k, uneven(m, 3), uneven(k, 4), 3, 4), D(k, n, uneven(k, 3), uneven(n, 2), 3, 2), D(m, n, uneven(m, 2), uneven(n, 3), 2, 3)
+
+
+def few_rows_run_on_few_rows(rec):
+    """Up to 32 rows on tiles of 32 and up to 64 on tiles of 64 or 32 wherever memory bounds them, whole along K where tiles fill the device."""
+    from paper_2510_08874_amd import binding as b
+    rec.so.rec_lds.restype = ctypes.c_uint64
+    for m, want in ((1, 32), (17, 32), (32, 32), (48, 64), (64, 64)):
+        d = made("whole", m, 8192, 28672)
+        plan, space = b.Plan(*d, 1), Space(True)
+        a, w, v = space.integers(d[0], "rows"), space.integers(d[1], "cols"), space.integers(d[1], "cols")
+        t = [space.tiles(x, 2)[0] for x in (d[0], d[1], d[1], d[2])]
+        # (bytes of LDS: stages)
+        for call, rows in ((lambda: plan.execute_int(a, w, t[3], b.DMM_C_BF16, 0), {3 * 160 * 128: 32, 3 * 192 * 128: 64}),
+                           (lambda: plan.gated_int(b.DMM_GELU, a, w, v, t[3], 0), {4 * 288 * 128: 32, 3 * 320 * 128: 64}),
+                           (lambda: plan.gated(b.DMM_SILU, *t, None, None, 0), {4 * 288 * 128: 32, 3 * 320 * 128: 64})):
+            at = len(rec.ops())
+            call()
+            ops = rec.launches(at)
+            assert [o[1] for o in ops] == ["layer_gemm_kernel"] and rows.get(rec.so.rec_lds(ops[0][0])) == want, (m, want, rec.so.rec_lds(ops[0][0]))
+
+
+def a_call_without_memory_for_copies_runs_on_the_operands(rec):
+    from paper_2510_08874_amd import binding as b
+    d = made("uneven", 1301, 1103, 907)
+    plan, space = b.Plan(*d, 12), Space(True)
+    t = [space.tiles(x, 2)[0] for x in (d[0], d[1], d[1], d[2])]
+    rec.so.rec_fail_allocations(3, 1)                          # (behind the tables' buffers, if these come first)
+    for _ in range(3):
+        at = len(rec.ops())
+        plan.gated(b.DMM_SILU, *t, None, None, 0)
+        assert "layer_gemm_kernel" in [o[1] for o in rec.launches(at)]
+        rec.check_tables()
+    rec.so.rec_set_limit(0)                                    # no memory at all: refused, and as before when there is some again
+    other = b.Plan(*d, 12)
+    at = len(rec.ops())
+    try:
+        other.gated(b.DMM_SILU, *t, None, None, 0)
+        assert "layer_gemm_kernel" in [o[1] for o in rec.launches(at)]     # (on buffers that are there)
+    except b.DmmError as e:
+        assert e.kind == "ENOMEM" and not rec.launches(at)
+    rec.so.rec_set_limit(1 << 40)
+    other.gated(b.DMM_SILU, *t, None, None, 0)
+
+
+def captures_take_what_is_there(rec):
+    """A first call is refused while a stream is captured; a call with the tables of the call before takes no memory, copies nothing and waits for nothing, on
+    any stream; one with others is refused."""
+    from paper_2510_08874_amd import binding as b
+    for layout, m, k, n in (("blocks", 512, 512, 768), ("whole", 40, 8192, 300), ("uneven", 1301, 1103, 907)):
+        d = made(layout, m, k, n)
+        plan, space = b.Plan(*d, 12), Space(True)
+        a, w, v = space.integers(d[0], "rows"), space.integers(d[1], "cols"), space.integers(d[1], "cols")
+        t = [space.tiles(x, 2)[0] for x in (d[0], d[1], d[1], d[2], d[2], d[2], d[2], d[2], d[0], d[1], d[1])]
+        c = [space.tiles(d[2], 4)[0] for _ in range(2)]
+        s, side = rec.stream(), rec.stream()
+        calls = [lambda x, st: plan.execute_int(a, w, c[x], 0, st), lambda x, st: plan.gated_int(b.DMM_GELU, a, w, v, t[3 + x], st),
+                 lambda x, st: plan.gated(b.DMM_SILU, *t[:3], t[3 + x], None, None, st),
+                 lambda x, st: plan.gated_backward(b.DMM_SILU, *t[:6], t[6 - x], t[7 - x], *t[8:], stream=st),
+                 lambda x, st: plan.execute_backward(t[0], t[1], t[3 + x], t[8], t[9], 0, st)]
+        for call in calls:
+            rec.so.rec_set_capturing(side, 1)
+            at = len(rec.ops())
+            try:
+                call(0, side)
+                assert False, "not refused"
+            except b.DmmError as e:
+                assert e.kind == "EINVAL" and not rec.launches(at)
+            rec.so.rec_set_capturing(side, 0)
+            call(0, s)
+            want = [o[1] for o in rec.launches(at)]
+            rec.so.rec_set_capturing(side, 1)
+            at, live = len(rec.ops()), rec.so.rec_live()
+            call(0, side)
+            assert [o[1] for o in rec.launches(at)] == want and rec.so.rec_live() == live and not [o for o in rec.ops(at) if o[1] == "copy"]
+            at = len(rec.ops())
+            try:
+                call(1, side)
+                assert False, "not refused"
+            except b.DmmError as e:
+                assert e.kind == "EINVAL" and not rec.launches(at)
+            rec.so.rec_set_capturing(side, 0)
+        rec.check_tables()
+        plan.destroy()
+
+
+def partial_sums_and_copies_wait_for_each_other(rec):
+    """Calls on two streams whose partial sums or copies lie in one buffer: each behind the one before; with whole tiles they need not wait."""
+    from paper_2510_08874_amd import binding as b
+    for layout, m, k, n, shared in (("blocks", 512, 512, 768, False), ("whole", 40, 8192, 300, True), ("uneven", 1301, 1103, 907, True)):
+        d = made(layout, m, k, n)
+        plan, space = b.Plan(*d, 12), Space(True)
+        t = [space.tiles(x, 2)[0] for x in (d[0], d[1], d[1], d[2])]
+        streams = [rec.stream(), rec.stream()]
+        last = None
+        for turn in range(4):
+            at = len(rec.ops())
+            plan.gated(b.DMM_SILU, *t, None, None, streams[turn % 2])
+            ops = [o[0] for o in rec.launches(at)]
+            if last is not None:
+                assert rec.before(last, ops[0]) or not shared
+            last = ops[-1]
+        rec.check_tables()
+        plan.destroy()
+
+
+SCENARIOS = [reads_and_writes_stay_inside, narrow_tiles, sizes_under_test_take_the_ways_they_are_meant_for, few_rows_run_on_few_rows,
+             a_call_without_memory_for_copies_runs_on_the_operands, captures_take_what_is_there, partial_sums_and_copies_wait_for_each_other]
 
 
 # ---- the tests ----------------------------------------------------------------------------------------
@@ -294,6 +431,110 @@ SCENARIOS = [reads_and_writes_stay_inside, narrow_tiles]
 def test_scenario(recorder, scenario):  # noqa: F811
     run = subprocess.run([sys.executable, os.path.abspath(__file__), recorder, scenario], capture_output=True, text=True, cwd=ROOT, timeout=300)
     assert run.returncode == 0, run.stdout[-2000:] + run.stderr[-4000:]
+
+
+BASE = 1 << 44
+
+
+def refused(kind, call, *args, **kw):
+    from paper_2510_08874_amd import binding as b
+    with pytest.raises(b.DmmError) as e:
+        call(*args, **kw)
+    assert e.value.kind == kind, e.value
+
+
+def a_plan(m=100, k=60, n=80, replication=1):
+    from paper_2510_08874_amd import binding as b
+    d = [workloads.desc(r, c, [0, r], [0, c], 1, 1, replication=replication) for r, c in ((m, k), (k, n), (m, n))]
+    return b, d, b.Plan(*d, replication)
+
+
+def good(b, d, ld=None, at=BASE, replicas=1):
+    return b.tiles([at + (i << 30) for i in range(replicas)], [ld or d["cols"]] * replicas)
+
+
+def good_int(b, d, along, ld=None, at=BASE, scales=BASE + (1 << 40), replicas=1):
+    w = d["cols"] if along == "rows" else d["rows"]
+    return b.int_tiles([at and at + (i << 30) for i in range(replicas)], [ld or w] * replicas, [scales] * replicas)
+
+
+def test_refusals_of_integers():
+    b, (da, db, dc), plan = a_plan()
+    desc = b.matrix_desc(da)
+    x, rows, cols = good(b, da), good_int(b, da, "rows"), good_int(b, da, "cols")
+    refused("EINVAL", b.dmm_int_quantize, desc, b.DMM_BF16, x)                                  # no form
+    refused("EINVAL", b.dmm_int_quantize, desc, 3, x, rows=rows)                                # no such type
+    refused("ELD", b.dmm_int_quantize, desc, b.DMM_BF16, good(b, da, 59), rows=rows)
+    refused("ELD", b.dmm_int_quantize, desc, b.DMM_BF16, x, rows=good_int(b, da, "rows", 59))
+    refused("ELD", b.dmm_int_quantize, desc, b.DMM_BF16, x, cols=good_int(b, da, "cols", 99))
+    refused("ELD", b.dmm_int_quantize, desc, b.DMM_BF16, x, rows=good_int(b, da, "rows", 1 << 24))
+    refused("EINVAL", b.dmm_int_quantize, desc, b.DMM_BF16, good(b, da, at=BASE + 1), rows=rows)   # not aligned to its elements
+    refused("EINVAL", b.dmm_int_quantize, desc, b.DMM_F32, good(b, da, at=BASE + 2), rows=rows)
+    refused("EINVAL", b.dmm_int_quantize, desc, b.DMM_BF16, x, rows=good_int(b, da, "rows", at=None))
+    refused("EINVAL", b.dmm_int_quantize, desc, b.DMM_BF16, x, rows=good_int(b, da, "rows", scales=None))
+    refused("EINVAL", b.dmm_int_quantize, desc, b.DMM_BF16, x, rows=good_int(b, da, "rows", scales=BASE + 2))
+    refused("EINVAL", b.dmm_int_dequantize, desc, rows, 3, b.DMM_BF16, x)
+    refused("EINVAL", b.dmm_int_dequantize, desc, rows, b.DMM_MX_ROWS, 0, x)
+    refused("ELD", b.dmm_int_dequantize, desc, rows, b.DMM_MX_COLS, b.DMM_BF16, x)              # rows of 60 bytes where a column has 100
+    bad = b.matrix_desc(dict(da, col_cuts=[0, 59]))
+    refused("EINVAL", b.dmm_int_quantize, bad, b.DMM_BF16, x, rows=rows)
+    a, w = good_int(b, da, "rows"), good_int(b, db, "cols")
+    refused("EINVAL", plan.execute_int, a, w, good(b, dc), b.DMM_TIMING)
+    refused("EINVAL", plan.execute_int, a, w, good(b, dc), b.DMM_DB_F32)
+    refused("EINVAL", plan.execute_int, a, w, good(b, dc, at=BASE + 2), 0)                      # fp32 tiles
+    refused("ELD", plan.execute_int, a, w, good(b, dc, 79), 0)
+    refused("ELD", plan.execute_int, a, w, good(b, dc, 1 << 22), 0)
+    refused("ELD", plan.execute_int, a, w, good(b, dc, 1 << 23), b.DMM_C_BF16)
+    refused("ELD", plan.execute_int, good_int(b, da, "rows", 59), w, good(b, dc), 0)
+    refused("ELD", plan.execute_int, a, good_int(b, db, "cols", 59), good(b, dc), 0)
+    refused("EINVAL", plan.execute_int, a, good_int(b, db, "cols", scales=None), good(b, dc), 0)
+    for act in (0, 4, -1):
+        refused("EINVAL", plan.gated_int, act, a, w, w, good(b, dc))
+    refused("ELD", plan.gated_int, b.DMM_SILU, a, w, good_int(b, db, "cols", 59), good(b, dc))
+    refused("EINVAL", plan.gated_int, b.DMM_SILU, a, w, w, good(b, dc, at=BASE + 1))
+    b, (ra, rb, rc), replicated = a_plan(replication=2)
+    a, w = good_int(b, ra, "rows", replicas=2), good_int(b, rb, "cols", replicas=2)
+    refused("EINVAL", replicated.execute_int, a, w, good(b, rc, replicas=2), b.DMM_C_BF16)
+    refused("EINVAL", replicated.gated_int, b.DMM_SILU, a, w, w, good(b, rc, replicas=2))
+
+
+def test_refusals_of_bf16_layers():
+    b, (da, db, dc), plan = a_plan()
+    a, w, h = good(b, da), good(b, db), good(b, dc)
+    for act in (0, 4, -1):
+        refused("EINVAL", plan.gated, act, a, w, w, h)
+        refused("EINVAL", plan.gated_backward, act, a, w, w, h, h, h, h, h)
+    for x in range(6):
+        args = [good(b, d, d["cols"] - 1 if x == y else None) for y, d in enumerate((da, db, db, dc, dc, dc))]
+        refused("ELD", plan.gated, b.DMM_SILU, *args)
+        args = [good(b, d, 1 << 23 if x == y else None) for y, d in enumerate((da, db, db, dc, dc, dc))]
+        refused("ELD", plan.gated, b.DMM_SILU, *args)
+        args = [good(b, d, at=BASE + (x == y)) for y, d in enumerate((da, db, db, dc, dc, dc))]
+        refused("EINVAL", plan.gated, b.DMM_SILU, *args)
+    everything = (da, db, db, dc, dc, dc, dc, dc, da, db, db)
+    for x in range(11):
+        args = [good(b, d, d["cols"] - 1 if x == y else None) for y, d in enumerate(everything)]
+        refused("ELD", plan.gated_backward, b.DMM_SILU, *args)
+        args = [good(b, d, at=BASE + (x == y)) for y, d in enumerate(everything)]
+        refused("EINVAL", plan.gated_backward, b.DMM_SILU, *args)
+    full = [good(b, d) for d in everything]
+    refused("EINVAL", plan.gated_backward, b.DMM_SILU, *full, b.DMM_C_BF16)                     # no such flag here
+    for x in (9, 10):                                                                           # fp32 where bf16 alone is aligned
+        refused("EINVAL", plan.gated_backward, b.DMM_SILU, *[t if y != x else good(b, db, at=BASE + 2) for y, t in enumerate(full)], b.DMM_DB_F32)
+    refused("EINVAL", plan.gated_backward, b.DMM_SILU, None, *full[1:])                         # a weight's gradient without A
+    refused("EINVAL", plan.gated_backward, b.DMM_SILU, full[0], None, *full[2:])                # A's without a weight
+    refused("EINVAL", plan.gated_backward, b.DMM_SILU, full[0], full[1], None, *full[3:])
+    refused("EINVAL", plan.execute_backward, a, w, h, None, None)                               # nothing to do
+    refused("EINVAL", plan.execute_backward, None, w, h, a, w)
+    refused("EINVAL", plan.execute_backward, a, None, h, a, w)
+    refused("EINVAL", plan.execute_backward, a, w, h, a, w, b.DMM_NO_REDUCE)
+    refused("ELD", plan.execute_backward, a, w, good(b, dc, 79), a, w)
+    refused("ELD", plan.execute_backward, a, w, h, a, good(b, db, 1 << 22), b.DMM_DB_F32)
+    refused("EINVAL", plan.execute_backward, a, w, h, a, good(b, db, at=BASE + 2), b.DMM_DB_F32)
+    b, (ra, rb, rc), replicated = a_plan(replication=2)
+    a, w, h = (good(b, d, replicas=2) for d in (ra, rb, rc))
+    refused("EINVAL", replicated.gated, b.DMM_SILU, a, w, w, h)
+    refused("EINVAL", replicated.gated_backward, b.DMM_SILU, a, w, w, h, h, h, h, h)
 
 
 if __name__ == "__main__":
