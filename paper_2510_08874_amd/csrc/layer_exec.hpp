@@ -129,6 +129,12 @@ struct LayerCopies {
     size_t at;
     int64_t pitch;
   };
+  struct Made {
+    const void *tiles;
+    const Grid *grid;
+    Matrix m;
+  };
+  std::vector<Made> made;              // two products may read one copy
 
   // rows x row_bytes bytes from `src` to place `dst`
   void job(const void *src, int64_t src_pitch, size_t dst, int64_t dst_pitch, int64_t rows, int64_t row_bytes) {
@@ -165,6 +171,8 @@ struct LayerCopies {
   // Replica 0 of a matrix, `rows` rows and the columns of `axis` to be there in the end, zeros where the matrix has none (`zeros`; otherwise what lies between the
   // columns is left as it is).  `turned`: its tiles lie transposed, and so does the copy.
   Matrix matrix(const Grid &G, const void *const *tiles, const int64_t *ld, int es, bool turned, int64_t rows, const Axis &axis, bool zeros) {
+    for (const Made &other : made)
+      if (other.tiles == tiles && other.grid == &G) return other.m;
     const int64_t have_rows = turned ? G.cols : G.rows;
     const int64_t pitch = (axis.total * es + 127) / 128 * 128 | 128;   // (an odd number of lines: rows start in different channels)
     const Matrix m = {size, pitch};
@@ -186,6 +194,7 @@ struct LayerCopies {
       job(nullptr, 0, m.at + (size_t)(end * es), pitch, have_rows, (next - end) * es);
     }
     job(nullptr, 0, m.at + (size_t)(have_rows * pitch), pitch, rows - have_rows, axis.total * es);
+    made.push_back({tiles, &G, m});
     return m;
   }
   // scales of replica 0, one behind another
@@ -402,11 +411,11 @@ void place_parts(std::vector<char> *h, const LayerLayout &L, char *buf, char *co
 }
 
 // The part of a call that all kinds have in common: the tables of the call before if they are of the same inputs (`key`), else new ones,
-// made from the products that `make` describes (on the operands, or on copies); then `in_front`, the launches and, where `reduce` asks for it, the sum of
+// made from what `make` tells of each product (on the operands, or on copies); then `in_front`, the launches and, where `reduce` asks for it, the sum of
 // C's replicas.
 template <class Make, class Front>
-int run_layer_on(dmm_plan_t *P, int which, const std::vector<char> &inputs, void *const *c_tiles, const int64_t *c_ld, bool reduce, hipStream_t stream, Make make,
-              Front in_front) {
+int run_layer_on(dmm_plan_t *P, int which, const std::vector<char> &inputs, void *const *c_tiles, const int64_t *c_ld, bool reduce, hipStream_t stream, int products,
+              Make make, Front in_front) {
   int rc;
   const bool capturing = is_capturing(stream), known = P->dev && P->dev->layer[which].cached;
   if (!known && (rc = materialize(P))) return rc;
@@ -428,28 +437,27 @@ int run_layer_on(dmm_plan_t *P, int which, const std::vector<char> &inputs, void
     LayerChoice choice[2];
     RedLaunch red;
     std::vector<char> &h = P->dev->host;
-    // on the operands as they lie, or on copies where that is estimated to be faster and there is room
-    LayerCopies copies;
-    std::vector<LayerWork> work = make(nullptr);
-    double us = 0;
-    for (size_t x = 0; x < work.size(); ++x) us += (choice[x] = choose_layer(work[x], cus)).us;
-    if (P->C.c == 1) {
-      std::vector<LayerWork> dense = make(&copies);
-      LayerChoice then[2];
-      double dense_us = copies.us();
-      for (size_t x = 0; x < dense.size(); ++x) dense_us += (then[x] = choose_layer(dense[x], cus)).us;
-      if (dense_us < us && copies.fits && copies.size <= kLayerCopies && copies.blocks <= kLayerBlocks) {
-        work.swap(dense);
-        std::copy(then, then + 2, choice);
-      } else {
-        copies = LayerCopies();
-      }
+    // each product on its operands as they lie, or on copies where that is estimated to be faster and there is room (by itself: what it is asked for with
+    // does not change its bits)
+    LayerWork work[2];
+    bool dense[2] = {false, false};
+    for (int x = 0; x < products; ++x) {
+      work[x] = make(x, nullptr);
+      choice[x] = choose_layer(work[x], cus);
+      if (P->C.c != 1) continue;
+      LayerCopies copies;
+      const LayerWork then = make(x, &copies);
+      const LayerChoice c = choose_layer(then, cus);
+      if (c.us + copies.us() < choice[x].us && copies.fits && copies.size <= kLayerCopies && copies.blocks <= kLayerBlocks) dense[x] = true, choice[x] = c;
     }
+    LayerCopies copies;
+    for (int x = 0; x < products; ++x)
+      if (dense[x]) work[x] = make(x, &copies);
     if ((rc = P->dev->uses.order(stream))) return rc;
     for (;;) {
       h.clear();
       size_t scratch = 0;
-      for (size_t x = 0; x < work.size(); ++x)
+      for (int x = 0; x < products; ++x)
         if ((rc = lay_out(work[x], choice[x], &h, &layout[x], &scratch))) return rc;
       scratch = (scratch + 4095) / 4096 * 4096;
       const size_t need = scratch + copies.size;
@@ -463,14 +471,18 @@ int run_layer_on(dmm_plan_t *P, int which, const std::vector<char> &inputs, void
         if (rc == DMM_ENOMEM && copies.size) {
           (void)hipGetLastError();
           copies = LayerCopies();
-          work = make(nullptr);
-          for (size_t x = 0; x < work.size(); ++x) choice[x] = choose_layer(work[x], cus);
+          for (int x = 0; x < products; ++x) {
+            if (!dense[x]) continue;
+            dense[x] = false;
+            work[x] = make(x, nullptr);
+            choice[x] = choose_layer(work[x], cus);
+          }
           continue;
         }
         if (rc) return rc;
       }
       char *const at = copies.size ? M.buf + scratch : nullptr;
-      for (const LayerLayout &L : layout) place_parts(&h, L, M.buf, at);
+      for (int x = 0; x < products; ++x) place_parts(&h, layout[x], M.buf, dense[x] ? at : nullptr);
       for (LayerCopy &j : copies.jobs) j.dst = at + (uintptr_t)j.dst;
       break;
     }
@@ -512,9 +524,9 @@ int run_layer_on(dmm_plan_t *P, int which, const std::vector<char> &inputs, void
 }
 
 template <class Make, class Front>
-int run_layer(dmm_plan_t *P, int which, const std::vector<char> &inputs, void *const *c_tiles, const int64_t *c_ld, bool reduce, hipStream_t stream, Make make,
-              Front in_front) {
-  const int rc = run_layer_on(P, which, inputs, c_tiles, c_ld, reduce, stream, make, in_front);
+int run_layer(dmm_plan_t *P, int which, const std::vector<char> &inputs, void *const *c_tiles, const int64_t *c_ld, bool reduce, hipStream_t stream, int products,
+              Make make, Front in_front) {
+  const int rc = run_layer_on(P, which, inputs, c_tiles, c_ld, reduce, stream, products, make, in_front);
   if (rc == DMM_ENOMEM) (void)hipGetLastError();               // (it would be the next call's)
   return rc;
 }
@@ -671,29 +683,27 @@ void weight_gradient(const dmm_plan_t *P, const dmm_tiles *a, const dmm_tiles *d
     }
 }
 
-// The products behind both backward calls: `pairs` of dC and B (and dB), from the operands or from copies of these.
-std::vector<LayerWork> gradients(const dmm_plan_t *P, const dmm_tiles *a, const dmm_tiles *const *b, const dmm_tiles *const *dc, int pairs, const dmm_tiles *da,
-                                 const dmm_tiles *const *db, int es, LayerCopies *copies) {
+// The products behind both backward calls, from the operands or from copies of these: dA (`input`) or all dB, of `pairs` of dC and B.
+LayerWork gradients(const dmm_plan_t *P, bool input, const dmm_tiles *a, const dmm_tiles *const *b, const dmm_tiles *const *dc, int pairs, const dmm_tiles *da,
+                    const dmm_tiles *const *db, int es, LayerCopies *copies) {
   const Grid &A = P->A, &B = P->B, &C = P->C;
-  const bool any_db = db[0] || (pairs > 1 && db[1]);
-  std::vector<LayerWork> works((da != nullptr) + any_db);
-  if (da) works.front().kind = LAYER_NT, works.front().c_es = 2;
-  if (any_db) works.back().kind = LAYER_TN, works.back().c_es = es;
+  LayerWork W;
+  W.kind = input ? LAYER_NT : LAYER_TN;
+  W.c_es = input ? 2 : es;
   if (!copies) {
-    if (da) input_gradient(P, dc, b, pairs, da, &works.front());
-    for (int p = 0; p < pairs; ++p)
-      if (db[p]) weight_gradient(P, a, dc[p], db[p], &works.back());
-    return works;
+    if (input) input_gradient(P, dc, b, pairs, da, &W);
+    for (int p = 0; p < pairs && !input; ++p)
+      if (db[p]) weight_gradient(P, a, dc[p], db[p], &W);
+    return W;
   }
   // dC serves along n and across m; its columns are those of dB's tiles
   const LayerCopies::Axis cols(B.cc, 64), rows(B.rc, 64);
   const int64_t m = up_to(C.rows, 64), n = cols.total;
-  LayerCopies::Matrix cc[2];
-  for (int p = 0; p < pairs; ++p) cc[p] = copies->matrix(C, dc[p]->tiles, dc[p]->ld, 2, false, m, cols, da != nullptr);
-  if (da) {
-    LayerCopies::Matrix cb[2];
+  LayerCopies::Matrix cc[2], cb[2];
+  for (int p = 0; p < pairs; ++p)
+    if (input || db[p]) cc[p] = copies->matrix(C, dc[p]->tiles, dc[p]->ld, 2, false, m, cols, true);
+  if (input) {
     for (int p = 0; p < pairs; ++p) cb[p] = copies->matrix(B, b[p]->tiles, b[p]->ld, 2, false, B.rows, cols, true);
-    LayerWork &W = works.front();
     tile_groups(
         A, &W,
         [&](int64_t m0, int64_t k0) {
@@ -705,25 +715,23 @@ std::vector<LayerWork> gradients(const dmm_plan_t *P, const dmm_tiles *a, const 
           r->c = corner(A, da, i, ti, tj, m0, k0, 2);
           r->ldc = da->ld[i];
         });
+    return W;
   }
-  if (any_db) {
-    const LayerCopies::Matrix ca = copies->matrix(A, a->tiles, a->ld, 2, false, m, rows, false);
-    LayerWork &W = works.back();
-    for (int p = 0; p < pairs; ++p) {
-      if (!db[p]) continue;
-      tile_groups(
-          B, &W,
-          [&](int64_t k0, int64_t n0) {
-            W.segs.push_back(dense_segment(ca.at + (size_t)rows.place(k0) * 2, ca.pitch, cc[p].at + (size_t)cols.place(n0) * 2, cc[p].pitch, 0, 0, m / 64));
-          },
-          [&](int32_t, int32_t ti, int32_t tj, int64_t k0, int64_t n0, LayerGroup *r) {
-            const int64_t i = B.table_index(0, ti, tj);
-            r->c = corner(B, db[p], i, ti, tj, k0, n0, es);
-            r->ldc = db[p]->ld[i];
-          });
-    }
+  const LayerCopies::Matrix ca = copies->matrix(A, a->tiles, a->ld, 2, false, m, rows, false);
+  for (int p = 0; p < pairs; ++p) {
+    if (!db[p]) continue;
+    tile_groups(
+        B, &W,
+        [&](int64_t k0, int64_t n0) {
+          W.segs.push_back(dense_segment(ca.at + (size_t)rows.place(k0) * 2, ca.pitch, cc[p].at + (size_t)cols.place(n0) * 2, cc[p].pitch, 0, 0, m / 64));
+        },
+        [&](int32_t, int32_t ti, int32_t tj, int64_t k0, int64_t n0, LayerGroup *r) {
+          const int64_t i = B.table_index(0, ti, tj);
+          r->c = corner(B, db[p], i, ti, tj, k0, n0, es);
+          r->ldc = db[p]->ld[i];
+        });
   }
-  return works;
+  return W;
 }
 
 bool is_activation(int act) { return act == DMM_SILU || act == DMM_GELU || act == DMM_GELU_TANH; }
@@ -741,9 +749,8 @@ int i8_product(dmm_plan_t *P, int which, int act, const dmm_int_tiles *a, const 
   key.put(b, B, true);
   if (b2) key.put(b2, B, true);
   key.put(c, C.c * C.tiles_per_rep());
-  auto make = [&](LayerCopies *copies) {
-    std::vector<LayerWork> works(1);
-    LayerWork &W = works[0];
+  auto make = [&](int, LayerCopies *copies) {
+    LayerWork W;
     W.kind = b2 ? LAYER_I8_GATED : LAYER_I8;
     W.act = act;
     W.c_es = c_es;
@@ -772,7 +779,7 @@ int i8_product(dmm_plan_t *P, int which, int act, const dmm_int_tiles *a, const 
             r->sb = (const float *)(uintptr_t)(sb + (size_t)n0 * 4);
             r->sb2 = (const float *)(uintptr_t)(sb2 + (size_t)n0 * 4);
           });
-      return works;
+      return W;
     }
     plan_groups(
         P, &W,
@@ -797,9 +804,9 @@ int i8_product(dmm_plan_t *P, int which, int act, const dmm_int_tiles *a, const 
           r->sb = b->scales[s] + at;
           r->sb2 = b2 ? b2->scales[s] + at : nullptr;
         });
-    return works;
+    return W;
   };
-  return run_layer(P, which, key.bytes, c->tiles, c->ld, reduce, stream, make, [] { return DMM_OK; });
+  return run_layer(P, which, key.bytes, c->tiles, c->ld, reduce, stream, 1, make, [] { return DMM_OK; });
 }
 
 // dU = dH act(G), dG = dH U act'(G), tile by tile.
@@ -1061,9 +1068,8 @@ int dmm_gated_execute(dmm_plan_t *P, int activation, const dmm_tiles *a, const d
     key.put(gate, B.c * B.tiles_per_rep());
     key.put(up, B.c * B.tiles_per_rep());
     for (const dmm_tiles *t : {h, g, u}) key.put(t, C.tiles_per_rep());
-    auto make = [&](LayerCopies *copies) {
-      std::vector<LayerWork> works(1);
-      LayerWork &W = works[0];
+    auto make = [&](int, LayerCopies *copies) {
+      LayerWork W;
       W.kind = LAYER_GATED;
       W.act = activation;
       W.c_es = 2;
@@ -1087,7 +1093,7 @@ int dmm_gated_execute(dmm_plan_t *P, int activation, const dmm_tiles *a, const d
               W.segs.push_back(dense_segment(ca.at + (size_t)(m0 * ca.pitch), ca.pitch, cg.at + col, cg.pitch, cu.at + col, cu.pitch, k / 64));
             },
             result);
-        return works;
+        return W;
       }
       plan_groups(
           P, &W,
@@ -1107,9 +1113,9 @@ int dmm_gated_execute(dmm_plan_t *P, int activation, const dmm_tiles *a, const d
             put_segment(&W, s, t.k1 - t.k0, guard);
           },
           [&](int32_t rep, int32_t ti, int32_t tj, int64_t m0, int64_t n0, const dmm_task *, LayerGroup *r) { result(rep, ti, tj, m0, n0, r); });
-      return works;
+      return W;
     };
-    return run_layer(P, LAYER_GATED_EXECUTE, key.bytes, nullptr, nullptr, false, (hipStream_t)hip_stream, make, [] { return DMM_OK; });
+    return run_layer(P, LAYER_GATED_EXECUTE, key.bytes, nullptr, nullptr, false, (hipStream_t)hip_stream, 1, make, [] { return DMM_OK; });
   } catch (const std::bad_alloc &) {
     return DMM_ENOMEM;
   }
@@ -1137,12 +1143,11 @@ int dmm_gated_backward(dmm_plan_t *P, int activation, const dmm_tiles *a, const 
     for (const dmm_tiles *t : {da ? gate : nullptr, da ? up : nullptr, dgate, dup}) key.put(t, B.tiles_per_rep());
     for (const dmm_tiles *t : {dg, du}) key.put(t, C.tiles_per_rep());
     key.put(da, A.tiles_per_rep());
-    auto make = [&](LayerCopies *copies) {
-      const dmm_tiles *const bs[2] = {gate, up}, *const dcs[2] = {dg, du}, *const dbs[2] = {dgate, dup};
-      return gradients(P, a, bs, dcs, 2, da, dbs, es, copies);
-    };
+    const dmm_tiles *const bs[2] = {gate, up}, *const dcs[2] = {dg, du}, *const dbs[2] = {dgate, dup};
+    const int first = da ? 0 : 1, last = dgate || dup ? 1 : 0;
+    auto make = [&](int x, LayerCopies *copies) { return gradients(P, first + x == 0, a, bs, dcs, 2, da, dbs, es, copies); };
     hipStream_t stream = (hipStream_t)hip_stream;
-    return run_layer(P, LAYER_GATED_BACKWARD, key.bytes, nullptr, nullptr, false, stream, make,
+    return run_layer(P, LAYER_GATED_BACKWARD, key.bytes, nullptr, nullptr, false, stream, std::max(0, last - first + 1), make,
                      [&] { return slope(C, activation, g, u, dh, dg, du, stream); });
   } catch (const std::bad_alloc &) {
     return DMM_ENOMEM;
@@ -1168,8 +1173,9 @@ int dmm_execute_backward(dmm_plan_t *P, const dmm_tiles *a, const dmm_tiles *b, 
     key.put(da ? b : nullptr, B.tiles_per_rep());
     key.put(db, B.tiles_per_rep());
     key.put(dc, C.tiles_per_rep());
-    auto make = [&](LayerCopies *copies) { return gradients(P, a, &b, &dc, 1, da, &db, es, copies); };
-    return run_layer(P, LAYER_EXECUTE_BACKWARD, key.bytes, nullptr, nullptr, false, (hipStream_t)hip_stream, make, [] { return DMM_OK; });
+    const int first = da ? 0 : 1;
+    auto make = [&](int x, LayerCopies *copies) { return gradients(P, first + x == 0, a, &b, &dc, 1, da, &db, es, copies); };
+    return run_layer(P, LAYER_EXECUTE_BACKWARD, key.bytes, nullptr, nullptr, false, (hipStream_t)hip_stream, (da != nullptr) + (db != nullptr), make, [] { return DMM_OK; });
   } catch (const std::bad_alloc &) {
     return DMM_ENOMEM;
   }

@@ -63,6 +63,11 @@ class Space:
 
 
 COPY = struct.Struct("<2Q2q4i")
+class Results(list):
+    """Regions of results; `copies`: the operands lie in copies."""
+    copies = False
+
+
 SEG, ITEM, JOIN = struct.Struct("<3Q3I3i"), struct.Struct("<3Q3I3i" + "Qq2Q2q3Q" + "12i"), struct.Struct("<Qq2Q2q3Q" + "Q6i")
 # kind of a launch: rows, columns of a right operand in its macro-tiles, by LDS; (A turned, B turned, two right operands, bytes of an element)
 KINDS = {"int": (False, False, False, 1), "int_gated": (False, False, True, 1), "gated": (False, True, True, 2), "nt": (False, False, False, 2), "tn": (True, True, False, 2)}
@@ -91,11 +96,13 @@ def follow(rec, space, op, kind):
             first = p + off * pitch + k0 * es
             space.inside(first, first + (ext - 1) * pitch + k * es, f"{kind}, along K, {'whole steps' if whole else 'a tail'}")
 
-    out, parts = [], {}
+    out, parts = Results(), {}
     for x in range(n):
         v = ITEM.unpack(raw[x * ITEM.size:(x + 1) * ITEM.size])
         front, (c, ldc, g, u, ldg, ldu, sa, sb, sb2), (m_off, n_off, m_ext, n_ext, seg, n_segs, first, steps, tail_seg, n_tails, c_es, what) = v[:9], v[9:18], v[18:]
         k_sum, left, s, skip = 0, steps, 0, first
+        if steps and space.copies and space.copies[0] <= front[0] < space.copies[1]:
+            out.copies = True
         while left > 0:
             rec_seg = front if s == 0 else seg_at(seg + s)
             assert s < n_segs
@@ -176,7 +183,7 @@ def covers(space, out, ptr, ld, d, es, k, step, times=1, cuts=None, replicas=1):
     """Every element of the tiles is written once, with all of K (on copies, filled up to whole steps, every interval of `cuts`)."""
     seen = {}
     cuts = cuts or [0, k]
-    k = (sum(-(-(j - i) // step) * step for i, j in zip(cuts, cuts[1:])) if space.copies else k) * times
+    k = (sum(-(-(j - i) // step) * step for i, j in zip(cuts, cuts[1:])) if out.copies else k) * times
     for c, ldc, c_es, h, w, k_sum in out:
         assert c_es == es and k_sum == k, (c_es, es, k_sum, k)
         i = bisect.bisect_right(space.start, c) - 1
@@ -248,8 +255,8 @@ def reads_and_writes_stay_inside(rec):
         out = call(["nt", "tn"], lambda: plan.gated_backward(b.DMM_GELU, a[0], w[0], v[0], g[0], u[0], dh[0], dg[0], du[0], ga[0], gw[0], gv[0],
                                                              b.DMM_DB_F32 if es == 4 else 0, 0))
         covers(space, out[0], ga[1], ga[2], da, 2, n, 64, 2, db["col_cuts"])
-        covers(space, [o for o in out[1] if in_tiles(space, o[0], gw)], gw[1], gw[2], db, es, m, 64)
-        covers(space, [o for o in out[1] if in_tiles(space, o[0], gv)], gv[1], gv[2], db, es, m, 64)
+        covers(space, those(space, out[1], gw), gw[1], gw[2], db, es, m, 64)
+        covers(space, those(space, out[1], gv), gv[1], gv[2], db, es, m, 64)
         out = call(["nt", "tn"], lambda: plan.execute_backward(a[0], w[0], dh[0], ga[0], gw[0], b.DMM_DB_F32 if es == 4 else 0, 0))
         covers(space, out[0], ga[1], ga[2], da, 2, n, 64, 1, db["col_cuts"])
         covers(space, out[1], gw[1], gw[2], db, es, m, 64)
@@ -257,8 +264,11 @@ def reads_and_writes_stay_inside(rec):
         plan.destroy()
 
 
-def in_tiles(space, p, t):
-    return space.start[bisect.bisect_right(space.start, p) - 1] in t[1]
+def those(space, out, t):
+    """The results that lie in the tiles `t`."""
+    got = Results(o for o in out if space.start[bisect.bisect_right(space.start, o[0]) - 1] in t[1])
+    got.copies = out.copies
+    return got
 
 
 def narrow_tiles(rec):
