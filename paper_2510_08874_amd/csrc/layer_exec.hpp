@@ -253,8 +253,8 @@ LayerChoice choose_layer(const LayerWork &W, int cus) {
         switch (shape) {
           case LAYER_256: return per * (1.15 + 0.3 * full) + 9.0;
           case LAYER_128: return gated ? per * (0.8 + 0.2 * full) + 7.0 : per * (full > 1 ? 1.1 : 0.5 + 0.16 * full) + 5.0;
-          case LAYER_64: return gated ? per * (0.6 + 0.2 * full) + 5.0 : per * (full > 1 ? 1.0 : 0.35 + 0.25 * full) + 4.0;
-          default: return gated ? per * (0.5 + 0.2 * full) + 4.0 : per * (full > 1 ? 0.9 : 0.3 + 0.2 * full) + 3.5;
+          case LAYER_64: return gated ? per * (0.7 + 0.2 * full) + 5.0 : per * (full > 1 ? 1.0 : 0.35 + 0.25 * full) + 4.0;
+          default: return gated ? per * (0.65 + 0.2 * full) + 4.0 : per * (full > 1 ? 0.9 : 0.3 + 0.2 * full) + 3.5;
         }
       };
       const double whole = std::floor(work / places);
@@ -515,7 +515,7 @@ int run_layer_on(dmm_plan_t *P, int which, const std::vector<char> &inputs, void
     const LayerLayout &L = M.layout[x];
     if (!L.n_items) continue;
     const bool last = !sum && (x == 1 || !M.layout[1].n_items);
-    marked = layer_launch(last ? behind : nullptr, L.kind, L.shape, L.act, (const LayerItem *)(d + L.o_items), L.n_items, (const LayerSeg *)(d + L.o_segs),
+    marked = layer_launch(last ? behind : nullptr, L.kind, L.shape, L.act, cus, (const LayerItem *)(d + L.o_items), L.n_items, (const LayerSeg *)(d + L.o_segs),
                           (const LayerJoin *)(d + L.o_joins), L.n_joins, stream);
     DMM_HIP(hipGetLastError());
   }
@@ -864,9 +864,9 @@ int check_slope(const Grid &C) {
 
 // ---- integers and values --------------------------------------------------------------------------------
 
-// Runs `launch` over all tiles in blocks of 128 rows by 256 bytes, as many tiles at a time as a launch's argument holds.
+// Runs `launch` over all tiles in blocks of `rows` by `cols`, as many tiles at a time as a launch's argument holds.
 template <class F>
-int over_i8_tiles(const Grid &G, int es, char *const *x, const int64_t *x_ld, const dmm_int_tiles *q, bool by_cols, F launch) {
+int over_i8_tiles(const Grid &G, int es, char *const *x, const int64_t *x_ld, const dmm_int_tiles *q, bool by_cols, int64_t rows, int64_t cols, F launch) {
   I8Args args;
   std::memset(&args, 0, sizeof args);
   int64_t blocks = 0;
@@ -894,8 +894,8 @@ int over_i8_tiles(const Grid &G, int es, char *const *x, const int64_t *x_ld, co
         t.scale = q->scales[by_cols ? (int64_t)rep * G.gc + tj : (int64_t)rep * G.gr + ti];
         t.h = (int32_t)h;
         t.w = (int32_t)w;
-        t.blocks_across = (int32_t)((w + i8_block_cols(es == 4) - 1) / i8_block_cols(es == 4));
-        const int64_t n = (h + 127) / 128 * t.blocks_across;
+        t.blocks_across = (int32_t)((w + cols - 1) / cols);
+        const int64_t n = (h + rows - 1) / rows * t.blocks_across;
         if ((args.n == I8_TILES || blocks + n > kLayerBlocks) && (rc = flush())) return rc;
         t.first_block = (int32_t)blocks;
         blocks += n;
@@ -976,8 +976,11 @@ int i8_form(const Grid &G, int dtype, char *const *x, const int64_t *x_ld, const
     return DMM_OK;
   }
   if ((rc = over_scales(G, q, by_cols, I8_CLEAR, stream))) return rc;
-  if ((rc = over_i8_tiles(G, es, x, x_ld, q, by_cols, [&](const I8Args &args, int blocks) { i8_amax_launch(args, blocks, f32, by_cols, stream); }))) return rc;
-  if ((rc = over_i8_tiles(G, es, x, x_ld, q, by_cols, [&](const I8Args &args, int blocks) { i8_quantize_launch(args, blocks, f32, by_cols, stream); })))
+  if ((rc = over_i8_tiles(G, es, x, x_ld, q, by_cols, 128, i8_block_cols(f32),
+                          [&](const I8Args &args, int blocks) { i8_amax_launch(args, blocks, f32, by_cols, stream); })))
+    return rc;
+  if ((rc = over_i8_tiles(G, es, x, x_ld, q, by_cols, 128, i8_block_cols(f32),
+                          [&](const I8Args &args, int blocks) { i8_quantize_launch(args, blocks, f32, by_cols, stream); })))
     return rc;
   return over_scales(G, q, by_cols, I8_FINISH, stream);
 }
@@ -1019,7 +1022,7 @@ int dmm_int_dequantize(const dmm_matrix_desc *X, const dmm_int_tiles *q, int alo
     if ((rc = load_matrix(X, &G)) || (rc = check_lds(G, x->ld)) || (rc = check_i8(G, q, by_cols)) || (rc = check_tiles(G, x->tiles, es)) ||
         (rc = check_i8_blocks(G, es)))
       return rc;
-    return over_i8_tiles(G, es, (char *const *)x->tiles, x->ld, q, by_cols,
+    return over_i8_tiles(G, es, (char *const *)x->tiles, x->ld, q, by_cols, 128, i8_block_cols(es == 4),
                          [&](const I8Args &args, int blocks) { i8_values_launch(args, blocks, es == 4, by_cols, (hipStream_t)hip_stream); });
   } catch (const std::bad_alloc &) {
     return DMM_ENOMEM;

@@ -21,6 +21,10 @@ using L128 = LayerShape<KIND, 128, DUAL ? 256 : 128, DUAL ? 3 : 2, 2>;   // (not
 using L64 = LayerShape<KIND == LAYER_TN ? LAYER_NT : KIND, 64, DUAL ? 256 : 128, 3, 2>;
 using L32 = LayerShape<KIND == LAYER_TN ? LAYER_NT : KIND, 32, DUAL ? 256 : 128, DUAL ? 4 : 3, 1>;
 constexpr bool SMALL = KIND != LAYER_TN;
+// not gated, where every workgroup has a CU to itself: more steps on their way
+using D128 = LayerShape<DUAL ? LAYER_NT : KIND, 128, 128, 4, 2>;
+using D64 = LayerShape<SMALL && !DUAL ? KIND : LAYER_NT, 64, 128, 6, 2>;
+using D32 = LayerShape<SMALL && !DUAL ? KIND : LAYER_NT, 32, 128, 7, 1>;
 template <class SH>
 constexpr bool same(int shape) { return kLayerTile[KIND][shape].tm == SH::TM && kLayerTile[KIND][shape].tn == SH::OUT; }
 static_assert(same<L256>(LAYER_256) && same<L128>(LAYER_128) && (!SMALL || (same<L64>(LAYER_64) && same<L32>(LAYER_32))),
@@ -38,16 +42,35 @@ hipError_t allow_all() {
     if (e == hipSuccess) e = allow<L64, ACT>();
     if (e == hipSuccess) e = allow<L32, ACT>();
   }
+  if constexpr (!DUAL) {
+    if (e == hipSuccess) e = allow<D128, ACT>();
+    if constexpr (SMALL) {
+      if (e == hipSuccess) e = allow<D64, ACT>();
+      if (e == hipSuccess) e = allow<D32, ACT>();
+    }
+  }
   return e;
 }
+template <class SH, int ACT>
+bool launch_as(hipEvent_t behind, const LayerItem *items, int n, const LayerSeg *segs, hipStream_t stream) {
+  return launch_behind(behind, layer_gemm_kernel<SH, ACT>, (unsigned)n, LAYER_THREADS, SH::LDS, stream, items, segs);
+}
 template <int ACT>
-bool launch(hipEvent_t behind, int shape, const LayerItem *items, int n, const LayerSeg *segs, hipStream_t stream) {
+bool launch(hipEvent_t behind, int shape, int cus, const LayerItem *items, int n, const LayerSeg *segs, hipStream_t stream) {
+  if (shape == LAYER_256) return launch_as<L256, ACT>(behind, items, n, segs, stream);
+  if constexpr (!DUAL)
+    if (n <= cus) {
+      if constexpr (SMALL) {
+        if (shape == LAYER_64) return launch_as<D64, ACT>(behind, items, n, segs, stream);
+        if (shape == LAYER_32) return launch_as<D32, ACT>(behind, items, n, segs, stream);
+      }
+      return launch_as<D128, ACT>(behind, items, n, segs, stream);
+    }
   if constexpr (SMALL) {
-    if (shape == LAYER_64) return launch_behind(behind, layer_gemm_kernel<L64, ACT>, (unsigned)n, LAYER_THREADS, L64::LDS, stream, items, segs);
-    if (shape == LAYER_32) return launch_behind(behind, layer_gemm_kernel<L32, ACT>, (unsigned)n, LAYER_THREADS, L32::LDS, stream, items, segs);
+    if (shape == LAYER_64) return launch_as<L64, ACT>(behind, items, n, segs, stream);
+    if (shape == LAYER_32) return launch_as<L32, ACT>(behind, items, n, segs, stream);
   }
-  if (shape == LAYER_256) return launch_behind(behind, layer_gemm_kernel<L256, ACT>, (unsigned)n, LAYER_THREADS, L256::LDS, stream, items, segs);
-  return launch_behind(behind, layer_gemm_kernel<L128, ACT>, (unsigned)n, LAYER_THREADS, L128::LDS, stream, items, segs);
+  return launch_as<L128, ACT>(behind, items, n, segs, stream);
 }
 
 }  // namespace
@@ -60,12 +83,13 @@ hipError_t DMM_CAT(layer_allow_lds_, DMM_INSTANCE)() {
   }
   return e;
 }
-bool DMM_CAT(layer_launch_, DMM_INSTANCE)(hipEvent_t behind, int shape, int act, const LayerItem *items, int n, const LayerSeg *segs, hipStream_t stream) {
+bool DMM_CAT(layer_launch_, DMM_INSTANCE)(hipEvent_t behind, int shape, int act, int cus, const LayerItem *items, int n, const LayerSeg *segs,
+                                          hipStream_t stream) {
   if constexpr (DUAL) {
-    if (act == DMM_GELU) return launch<DMM_GELU>(behind, shape, items, n, segs, stream);
-    if (act == DMM_GELU_TANH) return launch<DMM_GELU_TANH>(behind, shape, items, n, segs, stream);
+    if (act == DMM_GELU) return launch<DMM_GELU>(behind, shape, cus, items, n, segs, stream);
+    if (act == DMM_GELU_TANH) return launch<DMM_GELU_TANH>(behind, shape, cus, items, n, segs, stream);
   }
-  return launch<DMM_SILU>(behind, shape, items, n, segs, stream);
+  return launch<DMM_SILU>(behind, shape, cus, items, n, segs, stream);
 }
 
 #else
@@ -90,16 +114,16 @@ bool join(hipEvent_t behind, int act, const LayerJoin *joins, int n, int per, hi
 }
 }  // namespace
 
-bool layer_launch(hipEvent_t behind, int kind, int shape, int act, const LayerItem *items, int n_items, const LayerSeg *segs, const LayerJoin *joins,
+bool layer_launch(hipEvent_t behind, int kind, int shape, int act, int cus, const LayerItem *items, int n_items, const LayerSeg *segs, const LayerJoin *joins,
                   int n_joins, hipStream_t stream) {
   const hipEvent_t last = n_joins ? nullptr : behind;
   bool marked = false;
   switch (kind) {
-    case LAYER_I8: marked = layer_launch_0(last, shape, act, items, n_items, segs, stream); break;
-    case LAYER_I8_GATED: marked = layer_launch_1(last, shape, act, items, n_items, segs, stream); break;
-    case LAYER_GATED: marked = layer_launch_2(last, shape, act, items, n_items, segs, stream); break;
-    case LAYER_NT: marked = layer_launch_3(last, shape, act, items, n_items, segs, stream); break;
-    default: marked = layer_launch_4(last, shape, act, items, n_items, segs, stream); break;
+    case LAYER_I8: marked = layer_launch_0(last, shape, act, cus, items, n_items, segs, stream); break;
+    case LAYER_I8_GATED: marked = layer_launch_1(last, shape, act, cus, items, n_items, segs, stream); break;
+    case LAYER_GATED: marked = layer_launch_2(last, shape, act, cus, items, n_items, segs, stream); break;
+    case LAYER_NT: marked = layer_launch_3(last, shape, act, cus, items, n_items, segs, stream); break;
+    default: marked = layer_launch_4(last, shape, act, cus, items, n_items, segs, stream); break;
   }
   if (!n_joins || hipPeekAtLastError() != hipSuccess) return marked;
   const int per = (kLayerTile[kind][shape].tm * kLayerTile[kind][shape].tn + 1023) / 1024;

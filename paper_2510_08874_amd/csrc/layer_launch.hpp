@@ -85,13 +85,13 @@ constexpr bool layer_i8(int kind) { return kind == LAYER_I8 || kind == LAYER_I8_
 constexpr int layer_step(int kind) { return layer_i8(kind) ? 128 : 64; }   // of K
 
 hipError_t layer_allow_lds();
-bool layer_launch(hipEvent_t behind, int kind, int shape, int act, const LayerItem *items, int n_items, const LayerSeg *segs, const LayerJoin *joins,
+bool layer_launch(hipEvent_t behind, int kind, int shape, int act, int cus, const LayerItem *items, int n_items, const LayerSeg *segs, const LayerJoin *joins,
                   int n_joins, hipStream_t stream);
 
 // per kind, in object files of their own
 #define DMM_DECLARE_LAYER(n)      \
   hipError_t layer_allow_lds_##n(); \
-  bool layer_launch_##n(hipEvent_t behind, int shape, int act, const LayerItem *items, int n_items, const LayerSeg *segs, hipStream_t stream);
+  bool layer_launch_##n(hipEvent_t behind, int shape, int act, int cus, const LayerItem *items, int n_items, const LayerSeg *segs, hipStream_t stream);
 DMM_DECLARE_LAYER(0)
 DMM_DECLARE_LAYER(1)
 DMM_DECLARE_LAYER(2)

@@ -404,26 +404,32 @@ __global__ __launch_bounds__(256) void i8_cols_kernel(I8Args) {
 // with eight pieces each took 7 us, of which 2 went into turning 32 elements a thread into integers.)
 template <bool F32>
 __global__ __launch_bounds__(I8_ROW_THREADS) void i8_whole_rows_kernel(I8RowArgs) {
-  constexpr int KEPT = I8_ROW_KEPT;
+  constexpr int KEPT = I8_ROW_KEPT, PIECES = 4;               // pieces of eight elements of each of the first tiles of the row that stay in registers
   __shared__ unsigned tops[I8_ROW_THREADS / 64];
   const auto &args = *(const I8RowArgs *)__builtin_amdgcn_kernarg_segment_ptr();
   const int row = blockIdx.x, tid = threadIdx.x, threads = blockDim.x;
-  const bool one = args.n == 1;
-  LayerVec<F32> kept[KEPT];
+  LayerVec<F32> kept[PIECES][KEPT];
   unsigned m = 0;
+#pragma unroll
+  for (int p = 0; p < PIECES; ++p) {
+    if (p >= args.n) break;
+    const I8RowPiece &P = args.piece[p];
+#pragma unroll
+    for (int y = 0; y < KEPT; ++y) {
+      kept[p][y] = LayerVec<F32>{};
+      if ((y * threads + tid) * 8 < P.w) kept[p][y] = layer_load8<F32>(P.x + (int64_t)row * P.x_pitch, (y * threads + tid) * 8, P.w);
+    }
+  }
+#pragma unroll
+  for (int p = 0; p < PIECES; ++p) {
+    if (p >= args.n) break;
+#pragma unroll
+    for (int y = 0; y < KEPT; ++y) m = i8_abs_max(kept[p][y], m);
+  }
   for (int p = 0; p < args.n; ++p) {
     const I8RowPiece &P = args.piece[p];
-    const char *const at = P.x + (int64_t)row * P.x_pitch;
-    if (one) {
-#pragma unroll
-      for (int y = 0; y < KEPT; ++y) {
-        kept[y] = LayerVec<F32>{};
-        if ((y * threads + tid) * 8 < P.w) kept[y] = layer_load8<F32>(at, (y * threads + tid) * 8, P.w);
-      }
-#pragma unroll
-      for (int y = 0; y < KEPT; ++y) m = i8_abs_max(kept[y], m);
-    }
-    for (int col = ((one ? KEPT * threads : 0) + tid) * 8; col < P.w; col += threads * 8) m = i8_abs_max(layer_load8<F32>(at, col, P.w), m);
+    for (int col = ((p < PIECES ? KEPT * threads : 0) + tid) * 8; col < P.w; col += threads * 8)
+      m = i8_abs_max(layer_load8<F32>(P.x + (int64_t)row * P.x_pitch, col, P.w), m);
   }
   m = i8_wave_max(m);
   if ((tid & 63) == 0) tops[tid >> 6] = m;
@@ -436,14 +442,17 @@ __global__ __launch_bounds__(I8_ROW_THREADS) void i8_whole_rows_kernel(I8RowArgs
     const unsigned w[2] = {i8_four(r, v.at(0), v.at(1), v.at(2), v.at(3)), i8_four(r, v.at(4), v.at(5), v.at(6), v.at(7))};
     i8_put<2>(P.q + (int64_t)row * P.q_pitch + col, w, P.w - col);
   };
+#pragma unroll
+  for (int p = 0; p < PIECES; ++p) {
+    if (p >= args.n) break;
+    const I8RowPiece &P = args.piece[p];
+#pragma unroll
+    for (int y = 0; y < KEPT; ++y)
+      if ((y * threads + tid) * 8 < P.w) codes(P, (y * threads + tid) * 8, kept[p][y]);
+  }
   for (int p = 0; p < args.n; ++p) {
     const I8RowPiece &P = args.piece[p];
-    if (one) {
-#pragma unroll
-      for (int y = 0; y < KEPT; ++y)
-        if ((y * threads + tid) * 8 < P.w) codes(P, (y * threads + tid) * 8, kept[y]);
-    }
-    for (int col = ((one ? KEPT * threads : 0) + tid) * 8; col < P.w; col += threads * 8)
+    for (int col = ((p < PIECES ? KEPT * threads : 0) + tid) * 8; col < P.w; col += threads * 8)
       codes(P, col, layer_load8<F32>(P.x + (int64_t)row * P.x_pitch, col, P.w));
   }
 }

@@ -65,7 +65,7 @@ __device__ __forceinline__ nt_i32x4 layer_some(const char *p, int n, int before)
 #pragma unroll
     for (int i = 0; i < 16 / ES; ++i)
       if (i < n) {
-        const unsigned e = ES == 1 ? (unsigned)*(const unsigned char *)(p + i) : (unsigned)*(const unsigned short *)(p + 2 * i);
+        const unsigned e = ES == 1 ? (unsigned)*(const unsigned char *)(p + i) : ES == 2 ? (unsigned)*(const unsigned short *)(p + 2 * i) : *(const unsigned *)(p + 4 * i);
         w[i * ES / 4] |= e << (i * ES % 4 * 8);
       }
     v = nt_i32x4{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
