@@ -3,7 +3,7 @@ own torch allocation, as every virtual rank's tile is its own HBM buffer.
 Allocation, host<->device copies and slicing by cut points only."""
 from __future__ import annotations
 
-from typing import Dict, List, Optional, Tuple
+from typing import Dict, List, Optional, Tuple, Union
 
 import numpy as np
 import torch
@@ -135,7 +135,47 @@ class MxTileSet:
                             torch.cuda.current_stream().cuda_stream if stream is None else stream)
 
 
-def _check_form(X: TileSet, form: MxTileSet, along: str) -> None:
+class IntTileSet:
+    """The tiles of a matrix in 8-bit integers, along its rows or along its columns: codes of every tile and scales of every row (column) of tiles, in
+    the table order of the ABI.  ``table`` goes to ``dmm_int_quantize``, ``dmm_int_dequantize``, ``Plan.execute_int`` and ``Plan.gated_int``."""
+
+    def __init__(self, desc: Dict, along: str, device="cuda"):
+        from . import binding
+        if along not in ("rows", "cols"):
+            raise ValueError(f"along: {along!r}, not 'rows' or 'cols'")
+        self.desc, self.along, self.binding = desc, along, binding
+        self.codes: List[Optional[torch.Tensor]] = []
+        self.scales: List[Optional[torch.Tensor]] = []
+        rc, cc = desc["row_cuts"], desc["col_cuts"]
+        for _ in range(desc["replication"]):
+            for r0, r1 in zip(rc, rc[1:]):
+                for c0, c1 in zip(cc, cc[1:]):
+                    n, k = (r1 - r0, c1 - c0) if along == "rows" else (c1 - c0, r1 - r0)
+                    self.codes.append(torch.empty((n, _round_up(k, 16)), dtype=torch.int8, device=device) if n and k else None)
+            cuts = rc if along == "rows" else cc
+            for i, j in zip(cuts, cuts[1:]):
+                self.scales.append(torch.empty(j - i, dtype=torch.float32, device=device) if j > i else None)
+        self.table = self._table(range(len(self.codes)))
+
+    def _table(self, order):
+        order = list(order)
+        return self.binding.int_tiles([self.codes[i] for i in order], [0 if self.codes[i] is None else self.codes[i].shape[1] for i in order], self.scales)
+
+    def transposed(self):
+        """The table of the transposed matrix, whose rows are this one's columns: the same buffers, the codes in another order."""
+        gr, gc = len(self.desc["row_cuts"]) - 1, len(self.desc["col_cuts"]) - 1
+        return self._table(rep * gr * gc + i * gc + j for rep in range(self.desc["replication"]) for j in range(gc) for i in range(gr))
+
+    def write_values(self, X: TileSet, stream: Optional[int] = None) -> None:
+        """The values that the integers stand for, into the tiles of ``X`` (bf16 or fp32)."""
+        b = self.binding
+        _check_form(X, self, self.along)
+        b.dmm_int_dequantize(b.matrix_desc(self.desc), self.table, b.DMM_MX_ROWS if self.along == "rows" else b.DMM_MX_COLS,
+                             b.DMM_BF16 if X.dtype == torch.bfloat16 else b.DMM_F32, b.tiles(X.tensors, X.ld),
+                             torch.cuda.current_stream().cuda_stream if stream is None else stream)
+
+
+def _check_form(X: TileSet, form: Union[MxTileSet, IntTileSet], along: str) -> None:
     """The library gets addresses alone: tiles and a form that do not belong together would be read or written out of range."""
     if X.dtype not in (torch.bfloat16, torch.float32):
         raise ValueError(f"tiles of {X.dtype}, not of bfloat16 or float32")
@@ -149,14 +189,22 @@ def _check_form(X: TileSet, form: MxTileSet, along: str) -> None:
             raise ValueError(f"tiles on {device}, not on the current device")
 
 
-def quantize(X: TileSet, rows: Optional[MxTileSet] = None, cols: Optional[MxTileSet] = None, stream: Optional[int] = None) -> None:
-    """``dmm_mx_quantize`` of the tiles of ``X`` along their rows, their columns or both, in one pass."""
+def quantize(X: TileSet, rows: Union[MxTileSet, IntTileSet, None] = None, cols: Union[MxTileSet, IntTileSet, None] = None,
+             stream: Optional[int] = None) -> None:
+    """``dmm_mx_quantize`` or, into an ``IntTileSet``, ``dmm_int_quantize`` of the tiles of ``X`` along their rows, their columns or both."""
     from . import binding as b
     for form, along in ((rows, "rows"), (cols, "cols")):
         if form is not None:
             _check_form(X, form, along)
-    b.dmm_mx_quantize(b.matrix_desc(X.desc), b.DMM_BF16 if X.dtype == torch.bfloat16 else b.DMM_F32, b.tile_table(X.tensors, X.ld),
-                      rows=rows and rows.table, cols=cols and cols.table, stream=torch.cuda.current_stream().cuda_stream if stream is None else stream)
+    kinds = {type(form) for form in (rows, cols) if form is not None}
+    if len(kinds) > 1:
+        raise ValueError("one form in 4 bits and one in 8-bit integers: two calls")
+    desc, dtype, forms = b.matrix_desc(X.desc), b.DMM_BF16 if X.dtype == torch.bfloat16 else b.DMM_F32, dict(rows=rows and rows.table, cols=cols and cols.table)
+    on = torch.cuda.current_stream().cuda_stream if stream is None else stream
+    if kinds == {IntTileSet}:
+        b.dmm_int_quantize(desc, dtype, b.tiles(X.tensors, X.ld), **forms, stream=on)
+    else:
+        b.dmm_mx_quantize(desc, dtype, b.tile_table(X.tensors, X.ld), **forms, stream=on)
 
 
 class DeviceProblem:
