@@ -372,7 +372,9 @@ int dmm_orthogonalize(const dmm_matrix_desc *X, int32_t count, int x_dtype, cons
  *
  * A tile of h x w elements along its rows (DMM_MX_ROWS): h rows of w bytes.  Along its columns (DMM_MX_COLS): the same of the transposed
  * tile, w rows of h bytes.  Rows may start at any address (multiples of 16 are read fastest) and lie less than 2^24 bytes apart (DMM_ELD).  As for 4-bit
- * matrices, the form of X along its columns is that of X^T along its rows. */
+ * matrices, the form of X along its columns is that of X^T along its rows.
+ *
+ * These calls, the gated block and the gradients take matrices of up to 2^31 - 2^16 rows and columns (DMM_ELIMIT). */
 
 /* Tiles of a matrix: host arrays in table order.  Pointers of empty tiles may be null. */
 typedef struct {
@@ -401,9 +403,14 @@ int dmm_int_dequantize(const dmm_matrix_desc *X, const dmm_int_tiles *q, int alo
  *   flags     0 or any of DMM_NO_REDUCE, DMM_C_BF16
  * An element is the sum of its products as an integer, without loss at any length (all codes from -128 to 127 may be there), rounded to fp32 once and
  * multiplied with the scales of its row of A and its column of B.  Cuts of k may lie anywhere; a sum of more than 131071 products is taken in
- * parts, and one part may meet so many at most (DMM_ELIMIT where thousands of cuts of k leave nothing longer than 127).  Where a replica of A or B is cut out of
- * several, the scales are those of the replica that the plan's first op of the region reads: replicas are copies of each other.
- * Replicas of C, streams, ownership and captures as for dmm_mx_execute; the plan's tables and scratch memory for this entry point are its own. */
+ * parts, and one part may meet so many at most (DMM_ELIMIT where thousands of cuts of k leave nothing longer than 127).  Replicas of A and B are taken to be
+ * copies of each other: which of them an element and its scale are read from is not said.
+ * Operands whose rows are misaligned or finely cut may be copied to dense rows first, into the plan's scratch memory (at most 1 GiB a call; without so much the call
+ * runs on the operands).  Whether they are is decided from cuts, leading dimensions and addresses; integer sums do not depend on it, those of bf16 in the
+ * calls below are rounded in another order on copies.
+ * Replicas of C, streams, ownership and captures as for dmm_mx_execute; the plan's tables and scratch memory for this entry point are its own.  (With
+ * copies or partial sums a call waits for the plan's calls before it, on whichever stream.)  dmm_plan_last_execute, dmm_plan_last_kernels and
+ * the elapsed times do not speak of these calls, of the gated block's or of the gradients'. */
 int dmm_int_execute(dmm_plan_t *p, const dmm_int_tiles *a, const dmm_int_tiles *b, const dmm_tiles *c, uint32_t flags, void *hip_stream);
 
 /* ---- the gated block ----------------------------------------------------------------------------
@@ -419,8 +426,8 @@ int dmm_int_execute(dmm_plan_t *p, const dmm_int_tiles *a, const dmm_int_tiles *
 
 /* h; with g and u (either may be null) G and U as well, for the way back: bf16 tiles of the plan's C.
  * Where tiles are few they are cut along K into runs whose partial sums go through a scratch buffer and are added in ascending k (fixed cut
- * and order: results are reproducible).  Streams, ownership and captures as for dmm_mx_execute; the plan's tables and scratch memory for this entry
- * point are its own. */
+ * and order: results are reproducible).  Copies of operands as for dmm_int_execute; streams, ownership and captures as for dmm_mx_execute; the plan's
+ * tables and scratch memory for this entry point are its own. */
 int dmm_gated_execute(dmm_plan_t *p, int activation, const dmm_tiles *a, const dmm_tiles *gate, const dmm_tiles *up, const dmm_tiles *h,
                       const dmm_tiles *g, const dmm_tiles *u, void *hip_stream);
 
@@ -433,15 +440,15 @@ int dmm_int_gated_execute(dmm_plan_t *p, int activation, const dmm_int_tiles *a,
  *   da              dA = dG Wg^T + dU Wu^T, bf16, or null
  *   dgate, dup      dWg = A^T dG, dWu = A^T dU, bf16 (fp32 with DMM_DB_F32), or null
  * dA, dWg and dWu are products of dG and dU as they are stored, in bf16.  They are overwritten, and have one replica (grid_rows * grid_cols tiles in
- * the cuts of A and B), whatever the operands have; of these replica 0 is read.  a may be null without dgate and dup, the weights without da.  Captures, streams and
- * ownership as for dmm_gated_execute. */
+ * the cuts of A and B), whatever the operands have; of these replica 0 is read.  a may be null without dgate and dup, the weights without da.  Bits of each result do
+ * not depend on which others are asked for.  Copies, captures, streams and ownership as for dmm_gated_execute. */
 int dmm_gated_backward(dmm_plan_t *p, int activation, const dmm_tiles *a, const dmm_tiles *gate, const dmm_tiles *up, const dmm_tiles *g,
                        const dmm_tiles *u, const dmm_tiles *dh, const dmm_tiles *dg, const dmm_tiles *du, const dmm_tiles *da, const dmm_tiles *dgate,
                        const dmm_tiles *dup, uint32_t flags, void *hip_stream);
 
 /* The gradients of C = A B in bf16: dA = dC B^T and dB = A^T dC (either may be null), from tiles in the cuts of the plan's A, B and C.  All tables
  * name one replica, whatever the plan has.  da is bf16, db bf16 (fp32 with DMM_DB_F32); both are overwritten.  a may be null without db, b
- * without da.  Rows lie less than 2^24 bytes apart (DMM_ELD).  Captures, streams and ownership as for dmm_gated_execute. */
+ * without da.  Rows lie less than 2^24 bytes apart (DMM_ELD).  Copies, captures, streams and ownership as for dmm_gated_execute. */
 int dmm_execute_backward(dmm_plan_t *p, const dmm_tiles *a, const dmm_tiles *b, const dmm_tiles *dc, const dmm_tiles *da, const dmm_tiles *db,
                          uint32_t flags, void *hip_stream);
 

@@ -8,6 +8,7 @@ namespace {
 
 constexpr int64_t kLayerBlocks = (1 << 24) - 1;                // workgroups of a launch: 2^32 threads are too many
 constexpr int64_t kLayerPitch = (int64_t)1 << 24;              // bytes from row to row
+constexpr int64_t kLayerRows = 0x7fff0000;                     // kernels count rows and columns in 32 bits, a workgroup's past the last among them
 constexpr int64_t kLayerSum = 131071;                          // products of two bytes that an int32 sum holds whatever they are
 
 int allow_layer_lds() {
@@ -41,6 +42,7 @@ int check_layer_single(const Grid &G, const dmm_tiles *t, int es) {
   one.c = 1;
   return check_layer_tiles(one, t, es);
 }
+int check_sizes(const dmm_plan_t *P) { return std::max({P->A.rows, P->A.cols, P->B.cols}) > kLayerRows ? DMM_ELIMIT : DMM_OK; }
 // 8-bit integers along the rows, or along the columns, where a tile lies transposed.
 int check_i8(const Grid &G, const dmm_int_tiles *q, bool by_cols) {
   if (!q->codes || !q->code_ld || !q->scales) return DMM_EINVAL;
@@ -130,7 +132,7 @@ struct LayerCopies {
     int64_t pitch;
   };
   struct Made {
-    const void *tiles;
+    const void *tiles, *ld;
     const Grid *grid;
     Matrix m;
   };
@@ -172,7 +174,7 @@ struct LayerCopies {
   // columns is left as it is).  `turned`: its tiles lie transposed, and so does the copy.
   Matrix matrix(const Grid &G, const void *const *tiles, const int64_t *ld, int es, bool turned, int64_t rows, const Axis &axis, bool zeros) {
     for (const Made &other : made)
-      if (other.tiles == tiles && other.grid == &G) return other.m;
+      if (other.tiles == tiles && other.ld == ld && other.grid == &G) return other.m;
     const int64_t have_rows = turned ? G.cols : G.rows;
     const int64_t pitch = (axis.total * es + 127) / 128 * 128 | 128;   // (an odd number of lines: rows start in different channels)
     const Matrix m = {size, pitch};
@@ -194,7 +196,7 @@ struct LayerCopies {
       job(nullptr, 0, m.at + (size_t)(end * es), pitch, have_rows, (next - end) * es);
     }
     job(nullptr, 0, m.at + (size_t)(have_rows * pitch), pitch, rows - have_rows, axis.total * es);
-    made.push_back({tiles, &G, m});
+    made.push_back({tiles, ld, &G, m});
     return m;
   }
   // scales of replica 0, one behind another
@@ -741,7 +743,9 @@ int i8_product(dmm_plan_t *P, int which, int act, const dmm_int_tiles *a, const 
                bool reduce, hipStream_t stream) {
   const Grid &A = P->A, &B = P->B, &C = P->C;
   int rc;
-  if ((rc = check_i8(A, a, false)) || (rc = check_i8(B, b, true)) || (b2 && (rc = check_i8(B, b2, true))) || (rc = check_layer_tiles(C, c, c_es))) return rc;
+  if ((rc = check_i8(A, a, false)) || (rc = check_i8(B, b, true)) || (b2 && (rc = check_i8(B, b2, true))) || (rc = check_layer_tiles(C, c, c_es)) ||
+      (rc = check_sizes(P)))
+    return rc;
   LayerKey key;
   const int head[2] = {act, c_es};
   key.put(head, sizeof head);
@@ -857,7 +861,7 @@ int check_slope(const Grid &C) {
   for (int32_t ti = 0; ti < C.gr; ++ti)
     for (int32_t tj = 0; tj < C.gc; ++tj) {
       const int64_t h = C.rc[(size_t)ti + 1] - C.rc[(size_t)ti], w = C.cc[(size_t)tj + 1] - C.cc[(size_t)tj];
-      if (h > 0x7fffff00 || w > 0x7fffff00 || slope_blocks(h, w) > kLayerBlocks) return DMM_ELIMIT;
+      if (slope_blocks(h, w) > kLayerBlocks) return DMM_ELIMIT;
     }
   return DMM_OK;
 }
@@ -907,7 +911,7 @@ int check_i8_blocks(const Grid &G, int es) {
   for (int32_t ti = 0; ti < G.gr; ++ti)
     for (int32_t tj = 0; tj < G.gc; ++tj) {
       const int64_t h = G.rc[(size_t)ti + 1] - G.rc[(size_t)ti], w = G.cc[(size_t)tj + 1] - G.cc[(size_t)tj];
-      if ((h + 127) / 128 * ((w + i8_block_cols(es == 4) - 1) / i8_block_cols(es == 4)) > kLayerBlocks) return DMM_ELIMIT;
+      if (h > kLayerRows || w > kLayerRows || (h + 127) / 128 * ((w + i8_block_cols(es == 4) - 1) / i8_block_cols(es == 4)) > kLayerBlocks) return DMM_ELIMIT;
     }
   return DMM_OK;
 }
@@ -959,11 +963,11 @@ int i8_form(const Grid &G, int dtype, char *const *x, const int64_t *x_ld, const
         int32_t widest = 0;
         for (int32_t p = 0; p < args.n; ++p) widest = std::max(widest, args.piece[p].w);
         const int threads = (int)std::min<int64_t>(I8_ROW_THREADS, up_to(std::max(widest, 512) / 8, 64));
-        // (rows past what a launch can have go into the next)
-        const int32_t all = args.h;
-        for (int32_t at = 0; at < all; at += (int32_t)kLayerBlocks) {
+        // (rows past the 2^32 threads that a launch can have go into the next)
+        const int64_t all = args.h, most = ((int64_t)1 << 32) / threads - 1;
+        for (int64_t at = 0; at < all; at += most) {
           I8RowArgs part = args;
-          part.h = std::min<int32_t>(all - at, (int32_t)kLayerBlocks);
+          part.h = (int32_t)std::min(all - at, most);
           part.scale += at;
           for (int32_t p = 0; p < part.n; ++p) {
             part.piece[p].x += at * part.piece[p].x_pitch;
@@ -1062,7 +1066,7 @@ int dmm_gated_execute(dmm_plan_t *P, int activation, const dmm_tiles *a, const d
   int rc;
   if ((rc = check_layer_tiles(A, a, 2)) || (rc = check_layer_tiles(B, gate, 2)) || (rc = check_layer_tiles(B, up, 2)) || (rc = check_layer_tiles(C, h, 2)))
     return rc;
-  if ((g && (rc = check_layer_tiles(C, g, 2))) || (u && (rc = check_layer_tiles(C, u, 2)))) return rc;
+  if ((g && (rc = check_layer_tiles(C, g, 2))) || (u && (rc = check_layer_tiles(C, u, 2))) || (rc = check_sizes(P))) return rc;
   TraceRange whole("dmm_gated_execute");
   try {
     LayerKey key;
@@ -1137,7 +1141,8 @@ int dmm_gated_backward(dmm_plan_t *P, int activation, const dmm_tiles *a, const 
     if ((rc = check_layer_tiles(C, t, 2))) return rc;
   if (da && ((rc = check_layer_tiles(B, gate, 2)) || (rc = check_layer_tiles(B, up, 2)) || (rc = check_layer_single(A, da, 2)))) return rc;
   if ((dgate || dup) && (rc = check_layer_tiles(A, a, 2))) return rc;
-  if ((dgate && (rc = check_layer_single(B, dgate, es))) || (dup && (rc = check_layer_single(B, dup, es))) || (rc = check_slope(C))) return rc;
+  if ((dgate && (rc = check_layer_single(B, dgate, es))) || (dup && (rc = check_layer_single(B, dup, es))) || (rc = check_sizes(P)) || (rc = check_slope(C)))
+    return rc;
   TraceRange whole("dmm_gated_backward");
   try {
     LayerKey key;
@@ -1167,6 +1172,7 @@ int dmm_execute_backward(dmm_plan_t *P, const dmm_tiles *a, const dmm_tiles *b, 
   if ((rc = check_layer_single(C, dc, 2))) return rc;
   if (da && ((rc = check_layer_single(B, b, 2)) || (rc = check_layer_single(A, da, 2)))) return rc;
   if (db && ((rc = check_layer_single(A, a, 2)) || (rc = check_layer_single(B, db, es)))) return rc;
+  if ((rc = check_sizes(P))) return rc;
   TraceRange whole("dmm_execute_backward");
   try {
     LayerKey key;

@@ -329,16 +329,18 @@ def made(layout, m, k, n):
 
 
 def few_rows_run_on_few_rows(rec):
-    """Up to 32 rows on tiles of 32 and up to 64 on tiles of 64 or 32 wherever memory bounds them, whole along K where tiles fill the device."""
+    """Up to 32 rows on tiles of 32 and up to 64 on tiles of 64 or 32 wherever memory bounds them, whole along K where tiles fill the device,
+    with more steps in flight where every workgroup has a CU to itself."""
     from paper_2510_08874_amd import binding as b
     rec.so.rec_lds.restype = ctypes.c_uint64
-    for m, want in ((1, 32), (17, 32), (32, 32), (48, 64), (64, 64)):
-        d = made("whole", m, 8192, 28672)
+    for m, want, n, deep in ((1, 32, 28672, True), (17, 32, 28672, True), (32, 32, 28672, True), (48, 64, 28672, True), (64, 64, 28672, True), (32, 32, 40960, False),
+                             (64, 64, 40960, False)):
+        d = made("whole", m, 8192, n)
         plan, space = b.Plan(*d, 1), Space(True)
         a, w, v = space.integers(d[0], "rows"), space.integers(d[1], "cols"), space.integers(d[1], "cols")
         t = [space.tiles(x, 2)[0] for x in (d[0], d[1], d[1], d[2])]
         # (bytes of LDS: stages)
-        for call, rows in ((lambda: plan.execute_int(a, w, t[3], b.DMM_C_BF16, 0), {3 * 160 * 128: 32, 3 * 192 * 128: 64}),
+        for call, rows in ((lambda: plan.execute_int(a, w, t[3], b.DMM_C_BF16, 0), {7 * 160 * 128: 32, 6 * 192 * 128: 64} if deep else {3 * 160 * 128: 32, 3 * 192 * 128: 64}),
                            (lambda: plan.gated_int(b.DMM_GELU, a, w, v, t[3], 0), {4 * 288 * 128: 32, 3 * 320 * 128: 64}),
                            (lambda: plan.gated(b.DMM_SILU, *t, None, None, 0), {4 * 288 * 128: 32, 3 * 320 * 128: 64})):
             at = len(rec.ops())
@@ -431,7 +433,20 @@ def partial_sums_and_copies_wait_for_each_other(rec):
         plan.destroy()
 
 
-SCENARIOS = [reads_and_writes_stay_inside, narrow_tiles, sizes_under_test_take_the_ways_they_are_meant_for, few_rows_run_on_few_rows,
+def many_rows_take_several_launches(rec):
+    """A launch has less than 2^32 threads, and no row is left out or quantised twice."""
+    from paper_2510_08874_amd import binding as b
+    rec.so.rec_blocks.restype = ctypes.c_uint
+    for m, n, threads in (((1 << 23) + 5, 8192, 1024), ((1 << 31) - (1 << 17), 1, 64), (1 << 22, 2000, 256)):
+        d, space = workloads.desc(m, n, [0, m], [0, n], 1, 1), Space(True)
+        at = len(rec.ops())
+        b.dmm_int_quantize(b.matrix_desc(d), b.DMM_BF16, space.tiles(d, 2)[0], rows=space.integers(d, "rows"))
+        ops = rec.launches(at)
+        blocks = [int(rec.so.rec_blocks(o[0])) for o in ops]
+        assert {o[1] for o in ops} == {"i8_whole_rows_kernel"} and sum(blocks) == m and max(blocks) * threads < 1 << 32, (m, n, blocks)
+
+
+SCENARIOS = [many_rows_take_several_launches, reads_and_writes_stay_inside, narrow_tiles, sizes_under_test_take_the_ways_they_are_meant_for, few_rows_run_on_few_rows,
              a_call_without_memory_for_copies_runs_on_the_operands, captures_take_what_is_there, partial_sums_and_copies_wait_for_each_other]
 
 
@@ -506,6 +521,22 @@ def test_refusals_of_integers():
     a, w = good_int(b, ra, "rows", replicas=2), good_int(b, rb, "cols", replicas=2)
     refused("EINVAL", replicated.execute_int, a, w, good(b, rc, replicas=2), b.DMM_C_BF16)
     refused("EINVAL", replicated.gated_int, b.DMM_SILU, a, w, w, good(b, rc, replicas=2))
+
+
+def test_sizes_that_do_not_fit_32_bits():
+    most = (1 << 31) - (1 << 16)
+    b, (da, db, dc), plan = a_plan(most + 1, 1, 1)
+    a, w, h = good(b, da), good(b, db), good(b, dc)
+    refused("ELIMIT", plan.gated, b.DMM_SILU, a, w, w, h)
+    refused("ELIMIT", plan.gated_backward, b.DMM_SILU, a, w, w, h, h, h, h, h, a, w, w)
+    refused("ELIMIT", plan.execute_backward, a, w, h, a, w)
+    refused("ELIMIT", plan.execute_int, good_int(b, da, "rows"), good_int(b, db, "cols"), h, 0)
+    refused("ELIMIT", plan.gated_int, b.DMM_SILU, good_int(b, da, "rows"), good_int(b, db, "cols"), good_int(b, db, "cols"), h)
+    for rows, cols in ((most + 1, 1), (1, most + 1)):
+        d = workloads.desc(rows, cols, [0, rows], [0, cols], 1, 1)
+        form, along = (good_int(b, d, "rows"), "rows") if cols == 1 else (good_int(b, d, "cols"), "cols")
+        refused("ELIMIT", b.dmm_int_quantize, b.matrix_desc(d), b.DMM_BF16, good(b, d), **{along: form})
+        refused("ELIMIT", b.dmm_int_dequantize, b.matrix_desc(d), form, b.DMM_MX_ROWS if along == "rows" else b.DMM_MX_COLS, b.DMM_BF16, good(b, d))
 
 
 def test_refusals_of_bf16_layers():
