@@ -243,7 +243,7 @@ LayerChoice choose_layer(const LayerWork &W, int cus) {
     if (tiles == 0) return best;
     if (tiles > (double)kLayerBlocks) continue;
     // (two workgroups on a CU where the stages leave room)
-    const int places = shape == LAYER_256 || (gated && shape == LAYER_128) ? cus : gated ? cus : 2 * cus;
+    const int places = shape == LAYER_TWO || (!gated && shape != LAYER_256) ? 2 * cus : cus;
     // B from memory; another row of tiles reads it from a cache (48 x 8192 x 28672 gated, integers: 85 us on tiles of 64 rows, 103 on those of 32)
     const double memory = 2.0 + b_bytes * (1.0 + 0.2 * (down - 1)) / 5.4e6;
     for (int64_t runs = 1; runs <= 32; ++runs) {
@@ -253,10 +253,11 @@ LayerChoice choose_layer(const LayerWork &W, int cus) {
         if (n <= 0) return 0.0;
         const double full = n / cus;
         switch (shape) {
-          case LAYER_256: return per * (1.15 + 0.3 * full) + 9.0;
-          case LAYER_128: return gated ? per * (0.8 + 0.2 * full) + 7.0 : per * (full > 1 ? 1.1 : 0.5 + 0.16 * full) + 5.0;
-          case LAYER_64: return gated ? per * (0.7 + 0.2 * full) + 5.0 : per * (full > 1 ? 1.0 : 0.35 + 0.25 * full) + 4.0;
-          default: return gated ? per * (0.65 + 0.2 * full) + 4.0 : per * (full > 1 ? 0.9 : 0.3 + 0.2 * full) + 3.5;
+          case LAYER_256: return per * (1.15 + 0.3 * full) + (W.kind == LAYER_I8_GATED ? 12.0 : 9.0);
+          case LAYER_128: return gated ? per * ((layer_i8(W.kind) ? 0.62 : 0.5) + 0.3 * full) + 6.5 : per * (full > 1 ? 1.1 : 0.5 + 0.16 * full) + 5.0;
+          case LAYER_TWO: return per * (full > 1 ? (layer_i8(W.kind) ? 0.93 : 1.07) : 0.36 + 0.18 * full) + 4.5;
+          case LAYER_64: return gated ? per * (0.42 + 0.2 * full) + 5.0 : per * (full > 1 ? 1.0 : 0.35 + 0.25 * full) + 4.0;
+          default: return gated ? per * (0.38 + 0.15 * full) + 4.0 : per * (full > 1 ? 0.9 : 0.3 + 0.2 * full) + 3.5;
         }
       };
       const double whole = std::floor(work / places);

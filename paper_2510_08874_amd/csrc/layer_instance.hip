@@ -25,9 +25,11 @@ constexpr bool SMALL = KIND != LAYER_TN;
 using D128 = LayerShape<DUAL ? LAYER_NT : KIND, 128, 128, 4, 2>;
 using D64 = LayerShape<SMALL && !DUAL ? KIND : LAYER_NT, 64, 128, 6, 2>;
 using D32 = LayerShape<SMALL && !DUAL ? KIND : LAYER_NT, 32, 128, 7, 1>;
+// gated, two workgroups on a CU
+using L2 = LayerShape<DUAL ? KIND : LAYER_I8_GATED, KIND == LAYER_GATED ? 64 : 128, KIND == LAYER_GATED ? 256 : 128, 2, 2>;
 template <class SH>
 constexpr bool same(int shape) { return kLayerTile[KIND][shape].tm == SH::TM && kLayerTile[KIND][shape].tn == SH::OUT; }
-static_assert(same<L256>(LAYER_256) && same<L128>(LAYER_128) && (!SMALL || (same<L64>(LAYER_64) && same<L32>(LAYER_32))),
+static_assert(same<L256>(LAYER_256) && same<L128>(LAYER_128) && (!SMALL || (same<L64>(LAYER_64) && same<L32>(LAYER_32))) && (!DUAL || same<L2>(LAYER_TWO)),
               "the host cuts tiles as the kernels expect them");
 
 template <class SH, int ACT>
@@ -42,6 +44,8 @@ hipError_t allow_all() {
     if (e == hipSuccess) e = allow<L64, ACT>();
     if (e == hipSuccess) e = allow<L32, ACT>();
   }
+  if constexpr (DUAL)
+    if (e == hipSuccess) e = allow<L2, ACT>();
   if constexpr (!DUAL) {
     if (e == hipSuccess) e = allow<D128, ACT>();
     if constexpr (SMALL) {
@@ -58,6 +62,8 @@ bool launch_as(hipEvent_t behind, const LayerItem *items, int n, const LayerSeg 
 template <int ACT>
 bool launch(hipEvent_t behind, int shape, int cus, const LayerItem *items, int n, const LayerSeg *segs, hipStream_t stream) {
   if (shape == LAYER_256) return launch_as<L256, ACT>(behind, items, n, segs, stream);
+  if constexpr (DUAL)
+    if (shape == LAYER_TWO) return launch_as<L2, ACT>(behind, items, n, segs, stream);
   if constexpr (!DUAL)
     if (n <= cus) {
       if constexpr (SMALL) {

@@ -69,16 +69,16 @@ enum {
   LAYER_KINDS
 };
 // Macro-tiles of a kind: rows by columns of the result.
-enum { LAYER_256, LAYER_128, LAYER_64, LAYER_32, LAYER_SHAPES };
+enum { LAYER_256, LAYER_128, LAYER_TWO, LAYER_64, LAYER_32, LAYER_SHAPES };   // (TWO: gated, small enough for two on a CU)
 struct LayerTile {
   int tm, tn;
 };
 constexpr LayerTile kLayerTile[LAYER_KINDS][LAYER_SHAPES] = {
-    {{256, 256}, {128, 128}, {64, 128}, {32, 128}},
-    {{256, 128}, {128, 128}, {64, 128}, {32, 128}},
-    {{256, 128}, {128, 128}, {64, 128}, {32, 128}},
-    {{256, 256}, {128, 128}, {64, 128}, {32, 128}},
-    {{256, 256}, {128, 128}, {0, 0}, {0, 0}},
+    {{256, 256}, {128, 128}, {0, 0}, {64, 128}, {32, 128}},
+    {{256, 128}, {128, 128}, {128, 64}, {64, 128}, {32, 128}},
+    {{256, 128}, {128, 128}, {64, 128}, {64, 128}, {32, 128}},
+    {{256, 256}, {128, 128}, {0, 0}, {64, 128}, {32, 128}},
+    {{256, 256}, {128, 128}, {0, 0}, {0, 0}, {0, 0}},
 };
 constexpr bool layer_gated(int kind) { return kind == LAYER_I8_GATED || kind == LAYER_GATED; }
 constexpr bool layer_i8(int kind) { return kind == LAYER_I8 || kind == LAYER_I8_GATED; }

@@ -44,7 +44,7 @@ struct LayerShape {
   static constexpr int LA = TM / 32, LB = TN / 32, LOADS = LA + LB;   // 1 KB loads of a wave and step
   static constexpr int EARLY = LOADS / 2;                     // so many in the third quarter of a step, the others in the last
   static_assert(TM % (32 * WM) == 0 && TN % (32 * WN) == 0 && (!DUAL || NI % 2 == 0), "whole matrix tiles");
-  static_assert((!A_TURNED || TM % LAYER_SUB == 0) && (!B_TURNED || TN % LAYER_SUB == 0) && (!DUAL || TN == 2 * LAYER_SUB), "whole blocks of columns");
+  static_assert((!A_TURNED || TM % LAYER_SUB == 0) && (!B_TURNED || TN % LAYER_SUB == 0) && (!DUAL || !B_TURNED || TN == 2 * LAYER_SUB), "whole blocks of columns");
   static_assert(NST >= 2 && (NST - 1) * LOADS < 64 && LDS <= 160 * 1024, "the counter of loads, the LDS of a CU");
 };
 
