@@ -591,7 +591,8 @@ struct LayerState {
   std::vector<char> key;
   LayerLayout layout[2];
   int n_copies = 0, copy_blocks = 0;   // of operands, in front of the products
-  size_t o_copies = 0;
+  int n_back = 0, back_blocks = 0;     // of results, behind them
+  size_t o_copies = 0, o_back = 0;
   RedLaunch red;
   bool cached = false;
 };

@@ -77,6 +77,7 @@ struct LayerGroup {
 
 struct LayerWork {
   int kind = 0, act = DMM_SILU, c_es = 4;
+  int64_t rows = 1;                    // of the whole result
   std::vector<LayerSeg> segs;
   std::vector<LayerGroup> groups;
 };
@@ -119,13 +120,16 @@ struct LayerChoice {
   double us = 0;
 };
 
+// Which operands of a product are read from copies; LAYER_ROWS: the left one, and results go through scratch memory as well.
+enum LayerDense { LAYER_IN_PLACE, LAYER_BOTH, LAYER_LEFT, LAYER_ROWS };
+
 // Dense copies of operands whose rows are misaligned or finely cut: every row starts at a multiple of 128 bytes, K is one segment of whole steps,
 // filled up with zeros.  Places are given out from 0 on; the buffer is known later.
 struct LayerCopies {
-  std::vector<LayerCopy> jobs;
+  std::vector<LayerCopy> jobs, back;   // in front of the product, behind it
   size_t size = 0;
   double bytes = 0;
-  int64_t blocks = 0;
+  int64_t blocks = 0, back_blocks = 0;
   bool fits = true;                    // rows are not too long for the kernels
   struct Matrix {
     size_t at;
@@ -153,6 +157,30 @@ struct LayerCopies {
     blocks += ((row_bytes + 15) / 16 * rows + LAYER_COPY_CHUNKS - 1) / LAYER_COPY_CHUNKS;
     jobs.push_back(j);
     bytes += (double)rows * (double)row_bytes * (src ? 2 : 1);
+  }
+  // Results of `es` bytes in dense rows, and their way into the tiles from there.
+  Matrix results(const Grid &G, const dmm_tiles *t, int es) {
+    const Matrix m = {size, (G.cols * es + 127) / 128 * 128 | 128};
+    if (m.pitch >= kLayerPitch) fits = false;
+    size += (size_t)(G.rows * m.pitch + 4095) / 4096 * 4096;
+    for (int32_t ti = 0; ti < G.gr; ++ti)
+      for (int32_t tj = 0; tj < G.gc; ++tj) {
+        const int64_t i = G.table_index(0, ti, tj), r0 = G.rc[(size_t)ti], c0 = G.cc[(size_t)tj], rows = G.rc[(size_t)ti + 1] - r0, w = G.cc[(size_t)tj + 1] - c0;
+        if (rows <= 0 || w <= 0) continue;
+        LayerCopy j;
+        std::memset(&j, 0, sizeof j);
+        j.src = (const char *)(uintptr_t)(m.at + (size_t)(r0 * m.pitch + c0 * es));
+        j.dst = (char *)t->tiles[i];
+        j.src_pitch = m.pitch;
+        j.dst_pitch = t->ld[i] * es;
+        j.rows = (int32_t)rows;
+        j.bytes = (int32_t)(w * es);
+        j.first_block = (int32_t)back_blocks;
+        back_blocks += ((w * es + 15) / 16 * rows + LAYER_COPY_CHUNKS - 1) / LAYER_COPY_CHUNKS;
+        back.push_back(j);
+        bytes += 2.0 * (double)rows * (double)w * es;
+      }
+    return m;
   }
   // Where the columns of a matrix lie in its copy: those from every cut on start at a multiple of 128 bytes, so that macro-tiles that begin there read
   // aligned rows.
@@ -206,58 +234,66 @@ struct LayerCopies {
     for (size_t i = 0; i + 1 < cuts.size(); ++i) job(s[i], 0, at + (size_t)cuts[i] * 4, 0, 1, (cuts[i + 1] - cuts[i]) * 4);
     return at;
   }
-  double us() const { return 4.0 + bytes / 4.0e6; }
+  double us() const { return (back.empty() ? 4.0 : 8.0) + bytes / 4.0e6; }
+  bool possible() const;
 };
+constexpr double kTail = 5;                                    // us, see choose_layer
 constexpr size_t kLayerCopies = (size_t)1 << 30;               // of a call
+bool LayerCopies::possible() const { return fits && size <= kLayerCopies && blocks <= kLayerBlocks && back_blocks <= kLayerBlocks; }
 
 
 // By an estimate in us, from what a step (128 bytes of K) of a tile takes, measured as what more of K costs.  Where rows are not aligned to 16 bytes a step takes a
 // quarter more (integers: a third: 8191^3 direct 625 us, on copies 497; aligned 423), what is left of a segment as much as four steps.
 LayerChoice choose_layer(const LayerWork &W, int cus) {
   const bool gated = layer_gated(W.kind);
-  double cells = 0, k_steps = 0, b_bytes = 0;
+  double cells = 0, k_steps = 0, k_tails = 0, b_once = 0;
   int64_t most = 0;
   for (const LayerGroup &g : W.groups) {
     most = std::max(most, g.m);
-    double steps = 0, bytes = 0;
+    double steps = 0, tails = 0, bytes = 0;
     for (size_t x = g.seg; x < g.seg + g.n_segs; ++x) {
       const LayerSeg &s = W.segs[x];
       const bool odd = (((uintptr_t)s.a | (uintptr_t)s.b | (uintptr_t)s.b2 | s.a_pitch | s.b_pitch | s.b2_pitch) & 15) != 0;
-      steps += s.steps * (!odd ? 1.0 : layer_i8(W.kind) ? 1.35 : 1.25) + (s.tail > 0 ? 4 : 0);
+      steps += s.steps * (!odd ? 1.0 : gated ? (layer_i8(W.kind) ? 1.45 : 1.4) : layer_i8(W.kind) ? 1.35 : 1.25);
+      tails += s.tail > 0;
       bytes += s.steps + (s.tail > 0);
     }
     const double area = (double)g.m * (double)g.n;
     cells += area;
     k_steps += area * steps;
-    b_bytes += (double)g.n * bytes * (gated ? 256.0 : 128.0);
+    k_tails += area * tails;
+    b_once += area / (double)W.rows * bytes * (gated ? 256.0 : 128.0);
   }
-  const double steps = cells > 0 ? std::max(1.0, k_steps / cells) : 1;
+  const double steps = cells > 0 ? std::max(1.0, k_steps / cells) : 1, tails = cells > 0 ? k_tails / cells : 0;
   LayerChoice best;
   double best_us = 0;
   for (int shape = 0; shape < LAYER_SHAPES; ++shape) {
     const int tm = kLayerTile[W.kind][shape].tm, tn = kLayerTile[W.kind][shape].tn;
     if (tm == 0 || (shape == LAYER_64 && most > 128) || (shape == LAYER_32 && most > 64)) continue;
-    const double down = std::ceil((double)most / tm);
-    double tiles = 0;
-    for (const LayerGroup &g : W.groups) tiles += (double)(((g.m + tm - 1) / tm) * ((g.n + tn - 1) / tn));
+    double tiles = 0, strips = 0;                              // strips: columns of B that rows of tiles read, in all
+    for (const LayerGroup &g : W.groups) {
+      tiles += (double)(((g.m + tm - 1) / tm) * ((g.n + tn - 1) / tn));
+      strips += (double)((g.m + tm - 1) / tm) * (double)g.n;
+    }
     if (tiles == 0) return best;
     if (tiles > (double)kLayerBlocks) continue;
     // (two workgroups on a CU where the stages leave room)
     const int places = shape == LAYER_TWO || (!gated && shape != LAYER_256) ? 2 * cus : cus;
     // B from memory; another row of tiles reads it from a cache (48 x 8192 x 28672 gated, integers: 85 us on tiles of 64 rows, 103 on those of 32)
-    const double memory = 2.0 + b_bytes * (1.0 + 0.2 * (down - 1)) / 5.4e6;
+    const double down = strips * (double)W.rows / std::max(cells, 1.0);
+    const double memory = 2.0 + b_once * (0.8 + 0.2 * down) / 5.4e6;
     for (int64_t runs = 1; runs <= 32; ++runs) {
       const double work = tiles * (double)runs, per = std::ceil(steps / (double)runs);
       if (runs > 1 && (work > places || per < 3)) break;
       auto round = [&](double n) {
         if (n <= 0) return 0.0;
-        const double full = n / cus;
+        const double full = n / cus, ends = kTail * tails / (double)runs;
         switch (shape) {
-          case LAYER_256: return per * (1.15 + 0.3 * full) + (W.kind == LAYER_I8_GATED ? 12.0 : 9.0);
-          case LAYER_128: return gated ? per * ((layer_i8(W.kind) ? 0.62 : 0.5) + 0.3 * full) + 6.5 : per * (full > 1 ? 1.1 : 0.5 + 0.16 * full) + 5.0;
-          case LAYER_TWO: return per * (full > 1 ? (layer_i8(W.kind) ? 0.93 : 1.07) : 0.36 + 0.18 * full) + 4.5;
-          case LAYER_64: return gated ? per * (0.42 + 0.2 * full) + 5.0 : per * (full > 1 ? 1.0 : 0.35 + 0.25 * full) + 4.0;
-          default: return gated ? per * (0.38 + 0.15 * full) + 4.0 : per * (full > 1 ? 0.9 : 0.3 + 0.2 * full) + 3.5;
+          case LAYER_256: return ends + per * (1.15 + 0.3 * full) + (W.kind == LAYER_I8_GATED ? 12.0 : 9.0);
+          case LAYER_128: return ends + (gated ? per * ((layer_i8(W.kind) ? 0.62 : 0.5) + 0.3 * full) + 6.5 : per * (full > 1 ? 1.1 : 0.5 + 0.16 * full) + 5.0);
+          case LAYER_TWO: return ends + per * (full > 1 ? (layer_i8(W.kind) ? 0.93 : 1.07) : 0.36 + 0.18 * full) + 4.5;
+          case LAYER_64: return ends + (gated ? per * (0.42 + 0.2 * full) + 5.0 : per * (full > 1 ? 1.0 : 0.35 + 0.25 * full) + 4.0);
+          default: return ends + (gated ? per * (0.38 + 0.15 * full) + 4.0 : per * (full > 1 ? 0.9 : 0.3 + 0.2 * full) + 3.5);
         }
       };
       const double whole = std::floor(work / places);
@@ -384,32 +420,39 @@ int lay_out(const LayerWork &W, const LayerChoice &choice, std::vector<char> *h,
   return DMM_OK;
 }
 
-// Partial sums and copies get their places in the buffer: the former at its front, the latter from `copies` on (none: null).
-void place_parts(std::vector<char> *h, const LayerLayout &L, char *buf, char *copies) {
-  auto move = [&](auto *&p) {
-    if (copies) p = (std::decay_t<decltype(p)>)(copies + (uintptr_t)p);
+// Partial sums and copies get their places in the buffer: the former at its front, the latter from `copies` on.
+void place_parts(std::vector<char> *h, const LayerLayout &L, char *buf, char *copies, LayerDense dense) {
+  auto move = [&](auto *&p, bool copied) {
+    if (copied) p = (std::decay_t<decltype(p)>)(copies + (uintptr_t)p);
   };
+  const bool left = dense != LAYER_IN_PLACE, right = dense == LAYER_BOTH, out = dense == LAYER_ROWS;
   auto move_segment = [&](LayerSeg &s) {
-    move(s.a);
-    move(s.b);
-    move(s.b2);
+    move(s.a, left);
+    move(s.b, right);
+    move(s.b2, right);
   };
   LayerItem *items = (LayerItem *)(h->data() + L.o_items);
   for (int i = 0; i < L.n_items; ++i) {
     LayerItem &it = items[i];
     if (it.what == LAYER_PARTS) it.c = buf + (uintptr_t)it.c;
+    else move(it.c, out);
+    move(it.g, out && it.ldg);
+    move(it.u, out && it.ldu);
     move_segment(it.front);
-    move(it.sa);
-    move(it.sb);
-    move(it.sb2);
+    move(it.sa, left);
+    move(it.sb, right);
+    move(it.sb2, right);
   }
   for (LayerSeg *s = (LayerSeg *)(h->data() + L.o_segs); s < (LayerSeg *)(h->data() + L.o_joins); ++s) move_segment(*s);
   LayerJoin *joins = (LayerJoin *)(h->data() + L.o_joins);
   for (int i = 0; i < L.n_joins; ++i) {
     joins[i].parts = buf + (uintptr_t)joins[i].parts;
-    move(joins[i].sa);
-    move(joins[i].sb);
-    move(joins[i].sb2);
+    move(joins[i].c, out);
+    move(joins[i].g, out && joins[i].ldg);
+    move(joins[i].u, out && joins[i].ldu);
+    move(joins[i].sa, left);
+    move(joins[i].sb, right);
+    move(joins[i].sb2, right);
   }
 }
 
@@ -418,7 +461,7 @@ void place_parts(std::vector<char> *h, const LayerLayout &L, char *buf, char *co
 // C's replicas.
 template <class Make, class Front>
 int run_layer_on(dmm_plan_t *P, int which, const std::vector<char> &inputs, void *const *c_tiles, const int64_t *c_ld, bool reduce, hipStream_t stream, int products,
-              Make make, Front in_front) {
+              bool left, Make make, Front in_front) {
   int rc;
   const bool capturing = is_capturing(stream), known = P->dev && P->dev->layer[which].cached;
   if (!known && (rc = materialize(P))) return rc;
@@ -443,19 +486,23 @@ int run_layer_on(dmm_plan_t *P, int which, const std::vector<char> &inputs, void
     // each product on its operands as they lie, or on copies where that is estimated to be faster and there is room (by itself: what it is asked for with
     // does not change its bits)
     LayerWork work[2];
-    bool dense[2] = {false, false};
+    LayerDense dense[2] = {LAYER_IN_PLACE, LAYER_IN_PLACE};
     for (int x = 0; x < products; ++x) {
-      work[x] = make(x, nullptr);
+      work[x] = make(x, LAYER_IN_PLACE, nullptr);
       choice[x] = choose_layer(work[x], cus);
-      if (P->C.c != 1) continue;
-      LayerCopies copies;
-      const LayerWork then = make(x, &copies);
-      const LayerChoice c = choose_layer(then, cus);
-      if (c.us + copies.us() < choice[x].us && copies.fits && copies.size <= kLayerCopies && copies.blocks <= kLayerBlocks) dense[x] = true, choice[x] = c;
+      double best = choice[x].us;
+      for (LayerDense d : {LAYER_BOTH, LAYER_LEFT, LAYER_ROWS}) {
+        if (P->C.c != 1 || (d != LAYER_BOTH && !left)) continue;
+        LayerCopies copies;
+        const LayerWork then = make(x, d, &copies);
+        const LayerChoice c = choose_layer(then, cus);
+        if (c.us + copies.us() < best && copies.possible())
+          best = c.us + copies.us(), dense[x] = d, choice[x] = c;
+      }
     }
     LayerCopies copies;
     for (int x = 0; x < products; ++x)
-      if (dense[x]) work[x] = make(x, &copies);
+      if (dense[x]) work[x] = make(x, dense[x], &copies);
     if ((rc = P->dev->uses.order(stream))) return rc;
     for (;;) {
       h.clear();
@@ -476,8 +523,8 @@ int run_layer_on(dmm_plan_t *P, int which, const std::vector<char> &inputs, void
           copies = LayerCopies();
           for (int x = 0; x < products; ++x) {
             if (!dense[x]) continue;
-            dense[x] = false;
-            work[x] = make(x, nullptr);
+            dense[x] = LAYER_IN_PLACE;
+            work[x] = make(x, LAYER_IN_PLACE, nullptr);
             choice[x] = choose_layer(work[x], cus);
           }
           continue;
@@ -485,14 +532,18 @@ int run_layer_on(dmm_plan_t *P, int which, const std::vector<char> &inputs, void
         if (rc) return rc;
       }
       char *const at = copies.size ? M.buf + scratch : nullptr;
-      for (int x = 0; x < products; ++x) place_parts(&h, layout[x], M.buf, dense[x] ? at : nullptr);
+      for (int x = 0; x < products; ++x) place_parts(&h, layout[x], M.buf, at, dense[x]);
       for (LayerCopy &j : copies.jobs) j.dst = at + (uintptr_t)j.dst;
+      for (LayerCopy &j : copies.back) j.src = at + (uintptr_t)j.src;
       break;
     }
     M.n_copies = (int)copies.jobs.size();
     M.copy_blocks = (int)copies.blocks;
+    M.n_back = (int)copies.back.size();
+    M.back_blocks = (int)copies.back_blocks;
     M.o_copies = h.size();
-    h.insert(h.end(), (const char *)copies.jobs.data(), (const char *)(copies.jobs.data() + copies.jobs.size()));
+    M.o_back = M.o_copies + copies.jobs.size() * sizeof(LayerCopy);
+    for (const std::vector<LayerCopy> *v : {&copies.jobs, &copies.back}) h.insert(h.end(), (const char *)v->data(), (const char *)(v->data() + v->size()));
     static_assert(sizeof(LayerCopy) % 8 == 0, "tables lie one behind another");
     if (c_tiles && (rc = build_reduce(P, c_tiles, c_ld, 0, &h, h.size(), &red))) return rc;
     if ((rc = M.table.upload(h.data(), h.size(), stream, P->dev->uses))) return rc;
@@ -517,9 +568,13 @@ int run_layer_on(dmm_plan_t *P, int which, const std::vector<char> &inputs, void
   for (int x = 0; x < 2; ++x) {
     const LayerLayout &L = M.layout[x];
     if (!L.n_items) continue;
-    const bool last = !sum && (x == 1 || !M.layout[1].n_items);
+    const bool last = !sum && !M.n_back && (x == 1 || !M.layout[1].n_items);
     marked = layer_launch(last ? behind : nullptr, L.kind, L.shape, L.act, cus, (const LayerItem *)(d + L.o_items), L.n_items, (const LayerSeg *)(d + L.o_segs),
                           (const LayerJoin *)(d + L.o_joins), L.n_joins, stream);
+    DMM_HIP(hipGetLastError());
+  }
+  if (M.n_back) {
+    layer_copy_launch((const LayerCopy *)(d + M.o_back), M.n_back, M.back_blocks, stream);
     DMM_HIP(hipGetLastError());
   }
   if (sum && (rc = fire_reduce(P, M.red, stream, false, behind, &marked))) return rc;
@@ -528,8 +583,8 @@ int run_layer_on(dmm_plan_t *P, int which, const std::vector<char> &inputs, void
 
 template <class Make, class Front>
 int run_layer(dmm_plan_t *P, int which, const std::vector<char> &inputs, void *const *c_tiles, const int64_t *c_ld, bool reduce, hipStream_t stream, int products,
-              Make make, Front in_front) {
-  const int rc = run_layer_on(P, which, inputs, c_tiles, c_ld, reduce, stream, products, make, in_front);
+              bool left, Make make, Front in_front) {
+  const int rc = run_layer_on(P, which, inputs, c_tiles, c_ld, reduce, stream, products, left, make, in_front);
   if (rc == DMM_ENOMEM) (void)hipGetLastError();               // (it would be the next call's)
   return rc;
 }
@@ -600,6 +655,33 @@ void tile_groups(const Grid &G, LayerWork *W, Segment segment, Out out) {
       W->groups.push_back(r);
     }
 }
+int32_t interval_of(const std::vector<int64_t> &cuts, int64_t at) {   // the non-empty interval that holds `at`
+  return (int32_t)(std::upper_bound(cuts.begin(), cuts.end(), at) - cuts.begin()) - 1;
+}
+
+// On a copy of the left operand alone, whose row cuts then play no part (few rows, cut into blocks that would each bring in all of the right operand): C's
+// tiles, cut where B's columns are; a segment for every tile of B down them.  `whole`: C's cuts play no part either, its tiles are filled from scratch memory
+// afterwards.  (8 x 8192 x 28672 in 8 bits, A in 8 row blocks, B in 8 column blocks, C in 4 x 2: 255 us in place, 134 with LAYER_LEFT, 46 with LAYER_ROWS.)
+template <class Segment, class Out>
+void left_groups(const dmm_plan_t *P, bool whole, LayerWork *W, Segment segment, Out out) {
+  const Grid &B = P->B, &C = P->C;
+  const std::vector<int64_t> nc = whole ? merged_cuts({&B.cc}) : merged_cuts({&B.cc, &C.cc}), mc = whole ? std::vector<int64_t>{0, C.rows} : merged_cuts({&C.rc});
+  for (size_t y = 0; y + 1 < mc.size(); ++y)
+    for (size_t x = 0; x + 1 < nc.size(); ++x) {
+      const int32_t bj = interval_of(B.cc, nc[x]);
+      LayerGroup r;
+      std::memset(&r, 0, sizeof r);
+      r.m = mc[y + 1] - mc[y];
+      r.n = nc[x + 1] - nc[x];
+      if (r.m <= 0 || r.n <= 0) continue;
+      r.seg = W->segs.size();
+      for (int32_t bi = 0; bi < B.gr; ++bi)
+        if (B.rc[(size_t)bi + 1] > B.rc[(size_t)bi]) segment(bi, bj, mc[y], nc[x], r.n);
+      r.n_segs = W->segs.size() - r.seg;
+      out(bj, mc[y], nc[x], &r);
+      W->groups.push_back(r);
+    }
+}
 // A segment on copies: places of the operands' first element, whole steps of K.
 LayerSeg dense_segment(size_t a, int64_t a_pitch, size_t b, int64_t b_pitch, size_t b2, int64_t b2_pitch, int64_t steps) {
   LayerSeg s;
@@ -613,10 +695,6 @@ LayerSeg dense_segment(size_t a, int64_t a_pitch, size_t b, int64_t b_pitch, siz
   s.tail = 0;
   s.pad = 0;
   return s;
-}
-
-int32_t interval_of(const std::vector<int64_t> &cuts, int64_t at) {   // the non-empty interval that holds `at`
-  return (int32_t)(std::upper_bound(cuts.begin(), cuts.end(), at) - cuts.begin()) - 1;
 }
 
 // dA = dC B^T (summed over the pairs): A's tiles, cut where C's rows and B's rows are; both operands lie along n.
@@ -692,6 +770,7 @@ LayerWork gradients(const dmm_plan_t *P, bool input, const dmm_tiles *a, const d
   const Grid &A = P->A, &B = P->B, &C = P->C;
   LayerWork W;
   W.kind = input ? LAYER_NT : LAYER_TN;
+  W.rows = input ? A.rows : A.cols;
   W.c_es = input ? 2 : es;
   if (!copies) {
     if (input) input_gradient(P, dc, b, pairs, da, &W);
@@ -754,17 +833,45 @@ int i8_product(dmm_plan_t *P, int which, int act, const dmm_int_tiles *a, const 
   key.put(b, B, true);
   if (b2) key.put(b2, B, true);
   key.put(c, C.c * C.tiles_per_rep());
-  auto make = [&](int, LayerCopies *copies) {
+  auto make = [&](int, LayerDense dense, LayerCopies *copies) {
     LayerWork W;
     W.kind = b2 ? LAYER_I8_GATED : LAYER_I8;
     W.act = act;
     W.c_es = c_es;
+    W.rows = C.rows;
     auto result = [&](int32_t rep, int32_t ti, int32_t tj, int64_t m0, int64_t n0, LayerGroup *r) {
       const int64_t i = C.table_index(rep, ti, tj);
       r->c = corner(C, c, i, ti, tj, m0, n0, c_es);
       r->ldc = c->ld[i];
     };
-    if (copies) {
+    if (dense == LAYER_LEFT || dense == LAYER_ROWS) {
+      const LayerCopies::Axis along(B.rc, layer_step(W.kind));
+      const LayerCopies::Matrix ca = copies->matrix(A, a->codes, a->code_ld, 1, false, A.rows, along, false);
+      const size_t sa = copies->scales(A.rc, a->scales);
+      const LayerCopies::Matrix cc = dense == LAYER_ROWS ? copies->results(C, c, c_es) : LayerCopies::Matrix{0, 0};
+      left_groups(
+          P, dense == LAYER_ROWS, &W,
+          [&](int32_t bi, int32_t bj, int64_t m0, int64_t n0, int64_t) {
+            const int64_t i = B.table_index(0, bi, bj), bc = n0 - B.cc[(size_t)bj];
+            LayerSeg s;
+            s.a = (const char *)(uintptr_t)(ca.at + (size_t)(m0 * ca.pitch + along.place(B.rc[(size_t)bi])));
+            s.b = (const char *)b->codes[i] + bc * b->code_ld[i];
+            s.b2 = b2 ? (const char *)b2->codes[i] + bc * b2->code_ld[i] : nullptr;
+            s.a_pitch = (uint32_t)ca.pitch;
+            s.b_pitch = (uint32_t)b->code_ld[i];
+            s.b2_pitch = b2 ? (uint32_t)b2->code_ld[i] : 0;
+            put_segment(&W, s, B.rc[(size_t)bi + 1] - B.rc[(size_t)bi], 0);
+          },
+          [&](int32_t bj, int64_t m0, int64_t n0, LayerGroup *r) {
+            if (dense == LAYER_ROWS) r->c = (char *)(uintptr_t)(cc.at + (size_t)(n0 * c_es)), r->ldc = cc.pitch / c_es;
+            else result(0, interval_of(C.rc, m0), interval_of(C.cc, n0), m0, n0, r);
+            r->sa = (const float *)(uintptr_t)(sa + (size_t)m0 * 4);
+            r->sb = b->scales[bj] + (n0 - B.cc[(size_t)bj]);
+            r->sb2 = b2 ? b2->scales[bj] + (n0 - B.cc[(size_t)bj]) : nullptr;
+          });
+      return W;
+    }
+    if (dense == LAYER_BOTH) {
       const LayerCopies::Axis along({0, A.cols}, layer_step(W.kind));
       const int64_t k = along.total;
       const LayerCopies::Matrix ca = copies->matrix(A, a->codes, a->code_ld, 1, false, A.rows, along, true),
@@ -811,7 +918,7 @@ int i8_product(dmm_plan_t *P, int which, int act, const dmm_int_tiles *a, const 
         });
     return W;
   };
-  return run_layer(P, which, key.bytes, c->tiles, c->ld, reduce, stream, 1, make, [] { return DMM_OK; });
+  return run_layer(P, which, key.bytes, c->tiles, c->ld, reduce, stream, 1, true, make, [] { return DMM_OK; });
 }
 
 // dU = dH act(G), dG = dH U act'(G), tile by tile.
@@ -1076,11 +1183,27 @@ int dmm_gated_execute(dmm_plan_t *P, int activation, const dmm_tiles *a, const d
     key.put(gate, B.c * B.tiles_per_rep());
     key.put(up, B.c * B.tiles_per_rep());
     for (const dmm_tiles *t : {h, g, u}) key.put(t, C.tiles_per_rep());
-    auto make = [&](int, LayerCopies *copies) {
+    // the rows k0 to k1 of `n` columns of a tile of both weights, against what lies at `left`
+    auto weights = [&](LayerWork *W, int64_t i, int32_t bi, int32_t bj, int64_t k0, int64_t k1, int64_t n0, int64_t n, const char *left, int64_t pitch) {
+      LayerSeg s;
+      s.a = left;
+      s.b = corner(B, gate, i, bi, bj, k0, n0, 2);
+      s.b2 = corner(B, up, i, bi, bj, k0, n0, 2);
+      s.a_pitch = (uint32_t)pitch;
+      s.b_pitch = (uint32_t)(gate->ld[i] * 2);
+      s.b2_pitch = (uint32_t)(up->ld[i] * 2);
+      int64_t guard = 0;
+      for (const dmm_tiles *w : {gate, up})
+        guard = std::max(guard, rows_past_end(B.rc[(size_t)bi + 1] - B.rc[(size_t)bi], B.cc[(size_t)bj + 1] - B.cc[(size_t)bj], w->ld[i], k1 - B.rc[(size_t)bi],
+                                              n0 - B.cc[(size_t)bj], n));
+      put_segment(W, s, k1 - k0, guard);
+    };
+    auto make = [&](int, LayerDense dense, LayerCopies *copies) {
       LayerWork W;
       W.kind = LAYER_GATED;
       W.act = activation;
       W.c_es = 2;
+      W.rows = C.rows;
       auto result = [&](int32_t rep, int32_t ti, int32_t tj, int64_t m0, int64_t n0, LayerGroup *r) {
         const int64_t i = C.table_index(rep, ti, tj);
         r->c = corner(C, h, i, ti, tj, m0, n0, 2);
@@ -1088,7 +1211,30 @@ int dmm_gated_execute(dmm_plan_t *P, int activation, const dmm_tiles *a, const d
         if (g) r->g = corner(C, g, i, ti, tj, m0, n0, 2), r->ldg = g->ld[i];
         if (u) r->u = corner(C, u, i, ti, tj, m0, n0, 2), r->ldu = u->ld[i];
       };
-      if (copies) {
+      if (dense == LAYER_LEFT || dense == LAYER_ROWS) {
+        const bool whole = dense == LAYER_ROWS;
+        const LayerCopies::Axis along(B.rc, 64);
+        const LayerCopies::Matrix ca = copies->matrix(A, a->tiles, a->ld, 2, false, A.rows, along, false);
+        LayerCopies::Matrix out[3] = {};
+        const dmm_tiles *const results[3] = {h, g, u};
+        for (int x = 0; x < 3 && whole; ++x)
+          if (results[x]) out[x] = copies->results(C, results[x], 2);
+        left_groups(
+            P, whole, &W,
+            [&](int32_t bi, int32_t bj, int64_t m0, int64_t n0, int64_t n) {
+              weights(&W, B.table_index(0, bi, bj), bi, bj, B.rc[(size_t)bi], B.rc[(size_t)bi + 1], n0, n,
+                      (const char *)(uintptr_t)(ca.at + (size_t)(m0 * ca.pitch + along.place(B.rc[(size_t)bi]) * 2)), ca.pitch);
+            },
+            [&](int32_t, int64_t m0, int64_t n0, LayerGroup *r) {
+              if (!whole) return result(0, interval_of(C.rc, m0), interval_of(C.cc, n0), m0, n0, r);
+              auto at = [&](int x) { return (char *)(uintptr_t)(out[x].at + (size_t)n0 * 2); };
+              r->c = at(0), r->ldc = out[0].pitch / 2;
+              if (g) r->g = at(1), r->ldg = out[1].pitch / 2;
+              if (u) r->u = at(2), r->ldu = out[2].pitch / 2;
+            });
+        return W;
+      }
+      if (dense == LAYER_BOTH) {
         const LayerCopies::Axis along({0, A.cols}, 64), cols(C.cc, 64);
         const int64_t k = along.total;
         const LayerCopies::Matrix ca = copies->matrix(A, a->tiles, a->ld, 2, false, A.rows, along, true),
@@ -1107,23 +1253,12 @@ int dmm_gated_execute(dmm_plan_t *P, int activation, const dmm_tiles *a, const d
           P, &W,
           [&](const Group &gr, const dmm_task &t) {
             const int64_t ai = A.table_index(t.a_rep, t.a_ti, t.a_tj), bi = B.table_index(t.b_rep, t.b_ti, t.b_tj);
-            LayerSeg s;
-            s.a = corner(A, a, ai, t.a_ti, t.a_tj, gr.m0, t.k0, 2);
-            s.b = corner(B, gate, bi, t.b_ti, t.b_tj, t.k0, gr.n0, 2);
-            s.b2 = corner(B, up, bi, t.b_ti, t.b_tj, t.k0, gr.n0, 2);
-            s.a_pitch = (uint32_t)(a->ld[ai] * 2);
-            s.b_pitch = (uint32_t)(gate->ld[bi] * 2);
-            s.b2_pitch = (uint32_t)(up->ld[bi] * 2);
-            int64_t guard = 0;
-            for (const dmm_tiles *w : {gate, up})
-              guard = std::max(guard, rows_past_end(B.rc[(size_t)t.b_ti + 1] - B.rc[(size_t)t.b_ti], B.cc[(size_t)t.b_tj + 1] - B.cc[(size_t)t.b_tj], w->ld[bi],
-                                                    t.k1 - B.rc[(size_t)t.b_ti], gr.n0 - B.cc[(size_t)t.b_tj], gr.n1 - gr.n0));
-            put_segment(&W, s, t.k1 - t.k0, guard);
+            weights(&W, bi, t.b_ti, t.b_tj, t.k0, t.k1, gr.n0, gr.n1 - gr.n0, corner(A, a, ai, t.a_ti, t.a_tj, gr.m0, t.k0, 2), a->ld[ai] * 2);
           },
           [&](int32_t rep, int32_t ti, int32_t tj, int64_t m0, int64_t n0, const dmm_task *, LayerGroup *r) { result(rep, ti, tj, m0, n0, r); });
       return W;
     };
-    return run_layer(P, LAYER_GATED_EXECUTE, key.bytes, nullptr, nullptr, false, (hipStream_t)hip_stream, 1, make, [] { return DMM_OK; });
+    return run_layer(P, LAYER_GATED_EXECUTE, key.bytes, nullptr, nullptr, false, (hipStream_t)hip_stream, 1, true, make, [] { return DMM_OK; });
   } catch (const std::bad_alloc &) {
     return DMM_ENOMEM;
   }
@@ -1154,9 +1289,9 @@ int dmm_gated_backward(dmm_plan_t *P, int activation, const dmm_tiles *a, const 
     key.put(da, A.tiles_per_rep());
     const dmm_tiles *const bs[2] = {gate, up}, *const dcs[2] = {dg, du}, *const dbs[2] = {dgate, dup};
     const int first = da ? 0 : 1, last = dgate || dup ? 1 : 0;
-    auto make = [&](int x, LayerCopies *copies) { return gradients(P, first + x == 0, a, bs, dcs, 2, da, dbs, es, copies); };
+    auto make = [&](int x, LayerDense, LayerCopies *copies) { return gradients(P, first + x == 0, a, bs, dcs, 2, da, dbs, es, copies); };
     hipStream_t stream = (hipStream_t)hip_stream;
-    return run_layer(P, LAYER_GATED_BACKWARD, key.bytes, nullptr, nullptr, false, stream, std::max(0, last - first + 1), make,
+    return run_layer(P, LAYER_GATED_BACKWARD, key.bytes, nullptr, nullptr, false, stream, std::max(0, last - first + 1), false, make,
                      [&] { return slope(C, activation, g, u, dh, dg, du, stream); });
   } catch (const std::bad_alloc &) {
     return DMM_ENOMEM;
@@ -1184,8 +1319,8 @@ int dmm_execute_backward(dmm_plan_t *P, const dmm_tiles *a, const dmm_tiles *b, 
     key.put(db, B.tiles_per_rep());
     key.put(dc, C.tiles_per_rep());
     const int first = da ? 0 : 1;
-    auto make = [&](int x, LayerCopies *copies) { return gradients(P, first + x == 0, a, &b, &dc, 1, da, &db, es, copies); };
-    return run_layer(P, LAYER_EXECUTE_BACKWARD, key.bytes, nullptr, nullptr, false, (hipStream_t)hip_stream, (da != nullptr) + (db != nullptr), make, [] { return DMM_OK; });
+    auto make = [&](int x, LayerDense, LayerCopies *copies) { return gradients(P, first + x == 0, a, &b, &dc, 1, da, &db, es, copies); };
+    return run_layer(P, LAYER_EXECUTE_BACKWARD, key.bytes, nullptr, nullptr, false, (hipStream_t)hip_stream, (da != nullptr) + (db != nullptr), false, make, [] { return DMM_OK; });
   } catch (const std::bad_alloc &) {
     return DMM_ENOMEM;
   }

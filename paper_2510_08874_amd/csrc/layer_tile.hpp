@@ -332,21 +332,19 @@ struct LayerTileSums {
         *(__attribute__((address_space(3))) nt_i32x4 *)((nt_lptr)lds + to) = v;
       };
       __syncthreads();                                        // every wave is done with the stage
-      // (four at a time: registers)
+      // (four at a time beside 256 accumulators a lane, else all of them: each time is a wait for memory)
+      constexpr int MOST = MI * NI <= 4 ? SH::LOADS : 4;
 #pragma unroll
-      for (int of_b = 0; of_b < 2; ++of_b)
+      for (int y0 = 0; y0 < SH::LOADS; y0 += MOST) {
+        nt_i32x4 v[MOST];
 #pragma unroll
-        for (int y0 = 0; y0 < (of_b ? LB : LA); y0 += 4) {
-          constexpr int MOST = 4;
-          nt_i32x4 v[MOST];
+        for (int y = 0; y < MOST; ++y)
+          if (y0 + y < SH::LOADS) v[y] = y0 + y < LA ? some(false, y0 + y) : some(true, y0 + y - LA);
 #pragma unroll
-          for (int y = 0; y < MOST; ++y)
-            if (y0 + y < (of_b ? LB : LA)) v[y] = some(of_b, y0 + y);
-#pragma unroll
-          for (int y = 0; y < MOST; ++y)
-            if (y0 + y < (of_b ? LB : LA)) keep(of_b, y0 + y, v[y]);
-          __builtin_amdgcn_sched_barrier(0);
-        }
+        for (int y = 0; y < MOST; ++y)
+          if (y0 + y < SH::LOADS) y0 + y < LA ? keep(false, y0 + y, v[y]) : keep(true, y0 + y - LA, v[y]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
       __syncthreads();
       const int quarters = (s.tail * SH::ES + 31) / 32;
       nt_for<4>([&](auto hc) {

@@ -104,6 +104,8 @@ def descs(layout, m, k, n):
         return (D(m, k, [0, m], [0, k], 1, 1, replication=4), workloads.block_desc(k, n, 1, 4), workloads.block_desc(m, n, 1, 4)), 4
     if layout == "uneven":
         return (D(m, k, uneven(m, 3), uneven(k, 4), 3, 4), D(k, n, uneven(k, 3), uneven(n, 2), 3, 2), D(m, n, uneven(m, 2), uneven(n, 3), 2, 3)), 12
+    if layout == "row_col":
+        return (workloads.block_desc(m, k, 8, 1), D(k, n, uneven(k, 3), uneven(n, 2), 3, 2), workloads.block_desc(m, n, 4, 2)), 8
     assert layout == "replicated"
     return tuple(workloads.block_desc(r, c, 2, 2, replication=2) for r, c in ((m, k), (k, n), (m, n))), 8
 

@@ -19,7 +19,7 @@ binding = pytest.importorskip("paper_2510_08874_amd.binding")
 pytestmark = pytest.mark.gpu
 
 U, H = 2.0 ** -24, 2.0 ** -8
-LAYOUTS = ("whole", "blocks", "column", "uneven")
+LAYOUTS = ("whole", "blocks", "column", "uneven", "row_col")
 TINY = 2.0 ** -126                                             # (results below the normal range of fp32 and bf16)
 
 
@@ -120,7 +120,7 @@ def scales_of(n, seed, spread=8):
     return torch.from_numpy(np.exp2(np.random.default_rng(seed).uniform(-spread, spread, n)).astype(np.float32)).to("cuda")
 
 
-SIZES = [(1, 1, 1), (1, 127, 3), (2, 128, 130), (17, 129, 128), (33, 300, 257), (64, 1000, 64), (100, 640, 129), (130, 257, 131), (257, 1025, 300), (5, 9000, 70), (300, 5000, 500)]
+SIZES = [(1, 1, 1), (1, 127, 3), (2, 128, 130), (17, 129, 128), (33, 300, 257), (64, 1000, 64), (100, 640, 129), (130, 257, 131), (257, 1025, 300), (5, 9000, 70), (300, 5000, 500), (40, 3001, 6001), (9, 2000, 12001)]
 
 
 @pytest.mark.parametrize("layout,c_dtype", [(x, t) for x in LAYOUTS for t in ("f32", "bf16")] + [("replicated", "f32")])
@@ -177,7 +177,7 @@ def test_scales_far_apart():
 
 # ---- the gated block ------------------------------------------------------------------------------------
 
-GATED_SIZES = [(1, 1, 1), (1, 64, 3), (2, 65, 129), (17, 129, 128), (33, 200, 257), (64, 500, 64), (100, 320, 129), (130, 257, 131), (257, 513, 300), (5, 4500, 70), (300, 2500, 500)]
+GATED_SIZES = [(1, 1, 1), (1, 64, 3), (2, 65, 129), (17, 129, 128), (33, 200, 257), (64, 500, 64), (100, 320, 129), (130, 257, 131), (257, 513, 300), (5, 4500, 70), (300, 2500, 500), (40, 3001, 6001), (9, 2000, 12001)]
 
 
 def gated_error(g, u, eg, eu, name):

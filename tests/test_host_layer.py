@@ -29,7 +29,7 @@ class Space:
     """Made-up device buffers that end with a tile's last element, far from each other."""
 
     def __init__(self, aligned=False):
-        self.at, self.start, self.end, self.copies, self.aligned = 1 << 44, [], [], None, aligned
+        self.at, self.start, self.end, self.copies, self.results, self.aligned = 1 << 44, [], [], None, None, aligned
 
     def take(self, size, align):
         self.at += 0 if self.aligned else align                # (at multiples of the element's size, not of more)
@@ -55,8 +55,8 @@ class Space:
         return b.int_tiles(ptr, ld, [self.take(4 * (j - i), 4) if j > i else None for _ in range(d["replication"]) for i, j in zip(cuts, cuts[1:])])
 
     def inside(self, first, last, what):
-        """Bytes first ... last - 1 lie in one buffer (or in this call's copies)."""
-        if self.copies and self.copies[0] <= first and last <= self.copies[1]:
+        """Bytes first ... last - 1 lie in one buffer (or in this call's copies, or its results on their way)."""
+        if any(x and x[0] <= first and last <= x[1] for x in (self.copies, self.results)):
             return
         i = bisect.bisect_right(self.start, first) - 1
         assert i >= 0 and first >= self.start[i] and last <= self.end[i], f"{what}: bytes {first:#x} to {last:#x}, the buffer ends at {self.end[i]:#x}"
@@ -64,7 +64,7 @@ class Space:
 
 COPY = struct.Struct("<2Q2q4i")
 class Results(list):
-    """Regions of results; `copies`: the operands lie in copies."""
+    """Regions of results; `copies`: both operands lie in copies."""
     copies = False
 
 
@@ -101,7 +101,7 @@ def follow(rec, space, op, kind):
         v = ITEM.unpack(raw[x * ITEM.size:(x + 1) * ITEM.size])
         front, (c, ldc, g, u, ldg, ldu, sa, sb, sb2), (m_off, n_off, m_ext, n_ext, seg, n_segs, first, steps, tail_seg, n_tails, c_es, what) = v[:9], v[9:18], v[18:]
         k_sum, left, s, skip = 0, steps, 0, first
-        if steps and space.copies and space.copies[0] <= front[0] < space.copies[1]:
+        if steps and space.copies and space.copies[0] <= front[1] < space.copies[1]:
             out.copies = True
         while left > 0:
             rec_seg = front if s == 0 else seg_at(seg + s)
@@ -138,21 +138,29 @@ def follow(rec, space, op, kind):
 
 def follow_call(rec, space, at, kinds):
     """The launches of one call: [(corner, ld, bytes of an element, rows, columns, k)] of every kind."""
-    space.copies = None
+    space.copies, space.results, back, multiplied = None, None, [], False
     for op in rec.launches(at):
+        multiplied = multiplied or op[1] == "layer_gemm_kernel"
         if op[1] == "layer_copy_kernel":
             blocks, x, low, high = 0, 0, 1 << 63, 0
             while blocks < rec.so.rec_blocks(op[0]):
                 src, dst, src_pitch, dst_pitch, rows, size, first, _ = COPY.unpack(ctypes.string_at(op[3] + x * COPY.size, COPY.size))
                 assert first == blocks and rows > 0 and size > 0
-                if src:
+                if multiplied:
+                    back.append((src, dst, src_pitch, dst_pitch, rows, size))
+                elif src:
                     space.inside(src, src + (rows - 1) * src_pitch + size, "copied")
                 low, high = min(low, dst), max(high, dst + (rows - 1) * dst_pitch + size)
                 blocks += -(-(-(-size // 16) * rows) // 2048)
                 x += 1
             assert blocks == rec.so.rec_blocks(op[0])
+            if multiplied:
+                continue
             # (rows are filled up to 128 bytes, and so many lie behind the last: a read of eight columns may pass a row's end)
             space.copies = (low, -(-high // 128) * 128 + 128)
+    if back:
+        space.results = (min(o[0] for o in back), max(o[0] + (o[4] - 1) * o[2] + o[5] for o in back))
+        assert space.results[0] >= space.copies[1] - 128       # (behind the copies of operands)
     ops = [o for o in rec.launches(at) if o[1] in ("layer_gemm_kernel", "layer_join_kernel")]
     got, x = [], 0
     for kind in kinds:
@@ -176,6 +184,25 @@ def follow_call(rec, space, at, kinds):
             assert used == len(slots)
         got.append(out)
     assert x == len(ops)
+    if back:
+        # results in dense rows: their tiles do not meet, and what goes into the tiles is what they hold
+        (out,) = got
+        pitch = {o[1] * o[2] for o in out}
+        assert pitch == {o[2] for o in back} and len({o[5] for o in out}) == 1
+        at, pitch, es = min(o[0] for o in out), pitch.pop(), out[0][2]
+        placed = sorted((*reversed(divmod(o[0] - at, pitch)), o[3], o[4] * es) for o in out)
+        for i, (col, row, h, w) in enumerate(placed):
+            assert col + w <= pitch and not any(c < col + w and r < row + h and row < r + hh for c, r, hh, _ in placed[i + 1:])
+        rows, cols = max(r + h for _, r, h, _ in placed), max(c + w for c, _, _, w in placed)
+        assert sum(h * w for _, _, h, w in placed) == rows * cols
+        out, of = Results(), out
+        for src, dst, _, dst_pitch, h, size in back:
+            r, c = divmod(src - at, pitch)
+            if r < rows and c + size <= cols and r + h <= rows:    # (what is kept of G and U lies behind H)
+                out.append((dst, dst_pitch // es, es, h, size // es, of[0][5]))
+            else:
+                space.inside(dst, dst + (h - 1) * dst_pitch + size, "kept results")
+        got = [out]
     return got
 
 
@@ -203,13 +230,15 @@ def covers(space, out, ptr, ld, d, es, k, step, times=1, cuts=None, replicas=1):
 
 def layouts(rng, m, k, n):
     D, block, jitter = workloads.desc, workloads.block_desc, workloads.jittered_cuts
-    which = rng.choice(("whole", "blocks", "column", "uneven"))
+    which = rng.choice(("whole", "blocks", "column", "uneven", "row_col"))
     if which == "whole":
         return (D(m, k, [0, m], [0, k], 1, 1), D(k, n, [0, k], [0, n], 1, 1), D(m, n, [0, m], [0, n], 1, 1)), 1
     if which == "blocks":
         return (block(m, k, 2, 2), block(k, n, 2, 2), block(m, n, 2, 2)), 4
     if which == "column":
         return (D(m, k, [0, m], [0, k], 1, 1, replication=4), block(k, n, 1, 4), block(m, n, 1, 4)), 4
+    if which == "row_col":
+        return (block(m, k, 8, 1), block(k, n, 1, 8), block(m, n, 2, 4)), 8
     s = rng.randrange(1000)
     return (D(m, k, jitter(m, 3, s), jitter(k, 5, s + 1), 3, 5), D(k, n, jitter(k, 4, s + 2), jitter(n, 2, s + 3), 4, 2), D(m, n, jitter(m, 5, s + 4), jitter(n, 3, s + 5), 5, 3)), 15
 
@@ -349,6 +378,26 @@ def few_rows_run_on_few_rows(rec):
             assert [o[1] for o in ops] == ["layer_gemm_kernel"] and rows.get(rec.so.rec_lds(ops[0][0])) == want, (m, want, rec.so.rec_lds(ops[0][0]))
 
 
+def rows_in_blocks_are_joined_on_a_copy(rec):
+    """Few rows, cut into blocks each of which would bring in all of the weights: the rows alone are copied, C's tiles are written whole, or, where C is cut
+    into blocks of rows as well, from scratch memory."""
+    from paper_2510_08874_amd import binding as b
+    for m, k, n, blocks, back in ((8, 4096, 16384, 4, True), (64, 4096, 16380, 4, True), (61, 4099, 8192, 4, True), (64, 4096, 4100, 1, False)):
+        d = (workloads.block_desc(m, k, 8, 1), workloads.desc(k, n, [0, 1000, k], [0, n], 2, 1), workloads.block_desc(m, n, blocks, 8 // blocks))
+        plan, space = b.Plan(*d, 8), Space(True)
+        a, w, v = space.integers(d[0], "rows"), space.integers(d[1], "cols"), space.integers(d[1], "cols")
+        t = [space.tiles(x, 2)[0] for x in (d[0], d[1], d[1])]
+        h, g, u = (space.tiles(d[2], 2) for _ in range(3))
+        for kind, call in (("int", lambda: plan.execute_int(a, w, h[0], b.DMM_C_BF16, 0)), ("int_gated", lambda: plan.gated_int(b.DMM_GELU, a, w, v, h[0], 0)),
+                           ("gated", lambda: plan.gated(b.DMM_SILU, *t, h[0], None, None, 0)), ("gated", lambda: plan.gated(b.DMM_SILU, *t, h[0], g[0], u[0], 0)),
+                           ("gated", lambda: plan.gated(b.DMM_SILU, *t, h[0], None, u[0], 0))):
+            at = len(rec.ops())
+            call()
+            (out,) = follow_call(rec, space, at, [kind])
+            assert space.copies and not out.copies and bool(space.results) == back, (kind, m, k, n)
+            covers(space, out, h[1], h[2], d[2], 2, k, 64)
+
+
 def a_call_without_memory_for_copies_runs_on_the_operands(rec):
     from paper_2510_08874_amd import binding as b
     d = made("uneven", 1301, 1103, 907)
@@ -446,7 +495,7 @@ def many_rows_take_several_launches(rec):
         assert {o[1] for o in ops} == {"i8_whole_rows_kernel"} and sum(blocks) == m and max(blocks) * threads < 1 << 32, (m, n, blocks)
 
 
-SCENARIOS = [many_rows_take_several_launches, reads_and_writes_stay_inside, narrow_tiles, sizes_under_test_take_the_ways_they_are_meant_for, few_rows_run_on_few_rows,
+SCENARIOS = [many_rows_take_several_launches, rows_in_blocks_are_joined_on_a_copy, reads_and_writes_stay_inside, narrow_tiles, sizes_under_test_take_the_ways_they_are_meant_for, few_rows_run_on_few_rows,
              a_call_without_memory_for_copies_runs_on_the_operands, captures_take_what_is_there, partial_sums_and_copies_wait_for_each_other]
 
 
