@@ -457,11 +457,11 @@ void place_parts(std::vector<char> *h, const LayerLayout &L, char *buf, char *co
 }
 
 // The part of a call that all kinds have in common: the tables of the call before if they are of the same inputs (`key`), else new ones,
-// made from what `make` tells of each product (on the operands, or on copies); then `in_front`, the launches and, where `reduce` asks for it, the sum of
+// made from what `make` tells of each product (on the operands, or on copies; the first `lefts` products can be on copies of the left operand alone); then `in_front`, the launches and, where `reduce` asks for it, the sum of
 // C's replicas.
 template <class Make, class Front>
 int run_layer_on(dmm_plan_t *P, int which, const std::vector<char> &inputs, void *const *c_tiles, const int64_t *c_ld, bool reduce, hipStream_t stream, int products,
-              bool left, Make make, Front in_front) {
+              int lefts, Make make, Front in_front) {
   int rc;
   const bool capturing = is_capturing(stream), known = P->dev && P->dev->layer[which].cached;
   if (!known && (rc = materialize(P))) return rc;
@@ -492,7 +492,7 @@ int run_layer_on(dmm_plan_t *P, int which, const std::vector<char> &inputs, void
       choice[x] = choose_layer(work[x], cus);
       double best = choice[x].us;
       for (LayerDense d : {LAYER_BOTH, LAYER_LEFT, LAYER_ROWS}) {
-        if (P->C.c != 1 || (d != LAYER_BOTH && !left)) continue;
+        if (P->C.c != 1 || (d != LAYER_BOTH && x >= lefts)) continue;
         LayerCopies copies;
         const LayerWork then = make(x, d, &copies);
         const LayerChoice c = choose_layer(then, cus);
@@ -583,8 +583,8 @@ int run_layer_on(dmm_plan_t *P, int which, const std::vector<char> &inputs, void
 
 template <class Make, class Front>
 int run_layer(dmm_plan_t *P, int which, const std::vector<char> &inputs, void *const *c_tiles, const int64_t *c_ld, bool reduce, hipStream_t stream, int products,
-              bool left, Make make, Front in_front) {
-  const int rc = run_layer_on(P, which, inputs, c_tiles, c_ld, reduce, stream, products, left, make, in_front);
+              int lefts, Make make, Front in_front) {
+  const int rc = run_layer_on(P, which, inputs, c_tiles, c_ld, reduce, stream, products, lefts, make, in_front);
   if (rc == DMM_ENOMEM) (void)hipGetLastError();               // (it would be the next call's)
   return rc;
 }
@@ -766,13 +766,13 @@ void weight_gradient(const dmm_plan_t *P, const dmm_tiles *a, const dmm_tiles *d
 
 // The products behind both backward calls, from the operands or from copies of these: dA (`input`) or all dB, of `pairs` of dC and B.
 LayerWork gradients(const dmm_plan_t *P, bool input, const dmm_tiles *a, const dmm_tiles *const *b, const dmm_tiles *const *dc, int pairs, const dmm_tiles *da,
-                    const dmm_tiles *const *db, int es, LayerCopies *copies) {
+                    const dmm_tiles *const *db, int es, LayerDense dense, LayerCopies *copies) {
   const Grid &A = P->A, &B = P->B, &C = P->C;
   LayerWork W;
   W.kind = input ? LAYER_NT : LAYER_TN;
   W.rows = input ? A.rows : A.cols;
   W.c_es = input ? 2 : es;
-  if (!copies) {
+  if (dense == LAYER_IN_PLACE) {
     if (input) input_gradient(P, dc, b, pairs, da, &W);
     for (int p = 0; p < pairs && !input; ++p)
       if (db[p]) weight_gradient(P, a, dc[p], db[p], &W);
@@ -784,6 +784,41 @@ LayerWork gradients(const dmm_plan_t *P, bool input, const dmm_tiles *a, const d
   LayerCopies::Matrix cc[2], cb[2];
   for (int p = 0; p < pairs; ++p)
     if (input || db[p]) cc[p] = copies->matrix(C, dc[p]->tiles, dc[p]->ld, 2, false, m, cols, true);
+  if (dense != LAYER_BOTH) {
+    const bool whole = dense == LAYER_ROWS;
+    const LayerCopies::Matrix out = whole ? copies->results(A, da, 2) : LayerCopies::Matrix{0, 0};
+    const std::vector<int64_t> mc = whole ? std::vector<int64_t>{0, A.rows} : merged_cuts({&A.rc}), kc = whole ? merged_cuts({&B.rc}) : merged_cuts({&A.cc, &B.rc});
+    for (size_t y = 0; y + 1 < mc.size(); ++y)
+      for (size_t x = 0; x + 1 < kc.size(); ++x) {
+        const int32_t bi = interval_of(B.rc, kc[x]);
+        LayerGroup r;
+        std::memset(&r, 0, sizeof r);
+        r.m = mc[y + 1] - mc[y];
+        r.n = kc[x + 1] - kc[x];
+        if (r.m <= 0 || r.n <= 0) continue;
+        r.seg = W.segs.size();
+        for (int p = 0; p < pairs; ++p)
+          for (int32_t bj = 0; bj < B.gc; ++bj) {
+            if (B.cc[(size_t)bj + 1] == B.cc[(size_t)bj]) continue;
+            const int64_t i = B.table_index(0, bi, bj);
+            LayerSeg s = dense_segment(cc[p].at + (size_t)(mc[y] * cc[p].pitch + cols.place(B.cc[(size_t)bj]) * 2), cc[p].pitch, 0, b[p]->ld[i] * 2, 0, 0, 0);
+            s.b = corner(B, b[p], i, bi, bj, kc[x], B.cc[(size_t)bj], 2);
+            put_segment(&W, s, B.cc[(size_t)bj + 1] - B.cc[(size_t)bj], 0);
+          }
+        r.n_segs = W.segs.size() - r.seg;
+        if (whole) {
+          r.c = (char *)(uintptr_t)(out.at + (size_t)kc[x] * 2);
+          r.ldc = out.pitch / 2;
+        } else {
+          const int32_t ti = interval_of(A.rc, mc[y]), tj = interval_of(A.cc, kc[x]);
+          const int64_t i = A.table_index(0, ti, tj);
+          r.c = corner(A, da, i, ti, tj, mc[y], kc[x], 2);
+          r.ldc = da->ld[i];
+        }
+        W.groups.push_back(r);
+      }
+    return W;
+  }
   if (input) {
     for (int p = 0; p < pairs; ++p) cb[p] = copies->matrix(B, b[p]->tiles, b[p]->ld, 2, false, B.rows, cols, true);
     tile_groups(
@@ -918,7 +953,7 @@ int i8_product(dmm_plan_t *P, int which, int act, const dmm_int_tiles *a, const 
         });
     return W;
   };
-  return run_layer(P, which, key.bytes, c->tiles, c->ld, reduce, stream, 1, true, make, [] { return DMM_OK; });
+  return run_layer(P, which, key.bytes, c->tiles, c->ld, reduce, stream, 1, 1, make, [] { return DMM_OK; });
 }
 
 // dU = dH act(G), dG = dH U act'(G), tile by tile.
@@ -1258,7 +1293,7 @@ int dmm_gated_execute(dmm_plan_t *P, int activation, const dmm_tiles *a, const d
           [&](int32_t rep, int32_t ti, int32_t tj, int64_t m0, int64_t n0, const dmm_task *, LayerGroup *r) { result(rep, ti, tj, m0, n0, r); });
       return W;
     };
-    return run_layer(P, LAYER_GATED_EXECUTE, key.bytes, nullptr, nullptr, false, (hipStream_t)hip_stream, 1, true, make, [] { return DMM_OK; });
+    return run_layer(P, LAYER_GATED_EXECUTE, key.bytes, nullptr, nullptr, false, (hipStream_t)hip_stream, 1, 1, make, [] { return DMM_OK; });
   } catch (const std::bad_alloc &) {
     return DMM_ENOMEM;
   }
@@ -1289,9 +1324,9 @@ int dmm_gated_backward(dmm_plan_t *P, int activation, const dmm_tiles *a, const 
     key.put(da, A.tiles_per_rep());
     const dmm_tiles *const bs[2] = {gate, up}, *const dcs[2] = {dg, du}, *const dbs[2] = {dgate, dup};
     const int first = da ? 0 : 1, last = dgate || dup ? 1 : 0;
-    auto make = [&](int x, LayerDense, LayerCopies *copies) { return gradients(P, first + x == 0, a, bs, dcs, 2, da, dbs, es, copies); };
+    auto make = [&](int x, LayerDense dense, LayerCopies *copies) { return gradients(P, first + x == 0, a, bs, dcs, 2, da, dbs, es, dense, copies); };
     hipStream_t stream = (hipStream_t)hip_stream;
-    return run_layer(P, LAYER_GATED_BACKWARD, key.bytes, nullptr, nullptr, false, stream, std::max(0, last - first + 1), false, make,
+    return run_layer(P, LAYER_GATED_BACKWARD, key.bytes, nullptr, nullptr, false, stream, std::max(0, last - first + 1), da != nullptr, make,
                      [&] { return slope(C, activation, g, u, dh, dg, du, stream); });
   } catch (const std::bad_alloc &) {
     return DMM_ENOMEM;
@@ -1319,8 +1354,8 @@ int dmm_execute_backward(dmm_plan_t *P, const dmm_tiles *a, const dmm_tiles *b, 
     key.put(db, B.tiles_per_rep());
     key.put(dc, C.tiles_per_rep());
     const int first = da ? 0 : 1;
-    auto make = [&](int x, LayerDense, LayerCopies *copies) { return gradients(P, first + x == 0, a, &b, &dc, 1, da, &db, es, copies); };
-    return run_layer(P, LAYER_EXECUTE_BACKWARD, key.bytes, nullptr, nullptr, false, (hipStream_t)hip_stream, (da != nullptr) + (db != nullptr), false, make, [] { return DMM_OK; });
+    auto make = [&](int x, LayerDense dense, LayerCopies *copies) { return gradients(P, first + x == 0, a, &b, &dc, 1, da, &db, es, dense, copies); };
+    return run_layer(P, LAYER_EXECUTE_BACKWARD, key.bytes, nullptr, nullptr, false, (hipStream_t)hip_stream, (da != nullptr) + (db != nullptr), da != nullptr, make, [] { return DMM_OK; });
   } catch (const std::bad_alloc &) {
     return DMM_ENOMEM;
   }

@@ -138,7 +138,7 @@ def follow(rec, space, op, kind):
 
 def follow_call(rec, space, at, kinds):
     """The launches of one call: [(corner, ld, bytes of an element, rows, columns, k)] of every kind."""
-    space.copies, space.results, back, multiplied = None, None, [], False
+    space.copies, space.results, back, made, multiplied = None, None, [], [], False
     for op in rec.launches(at):
         multiplied = multiplied or op[1] == "layer_gemm_kernel"
         if op[1] == "layer_copy_kernel":
@@ -150,6 +150,8 @@ def follow_call(rec, space, at, kinds):
                     back.append((src, dst, src_pitch, dst_pitch, rows, size))
                 elif src:
                     space.inside(src, src + (rows - 1) * src_pitch + size, "copied")
+                if not multiplied:
+                    made.append((dst, dst + (rows - 1) * dst_pitch + size))
                 low, high = min(low, dst), max(high, dst + (rows - 1) * dst_pitch + size)
                 blocks += -(-(-(-size // 16) * rows) // 2048)
                 x += 1
@@ -160,7 +162,7 @@ def follow_call(rec, space, at, kinds):
             space.copies = (low, -(-high // 128) * 128 + 128)
     if back:
         space.results = (min(o[0] for o in back), max(o[0] + (o[4] - 1) * o[2] + o[5] for o in back))
-        assert space.results[0] >= space.copies[1] - 128       # (behind the copies of operands)
+        assert all(high <= space.results[0] or low >= space.results[1] for low, high in made)
     ops = [o for o in rec.launches(at) if o[1] in ("layer_gemm_kernel", "layer_join_kernel")]
     got, x = [], 0
     for kind in kinds:
@@ -184,25 +186,26 @@ def follow_call(rec, space, at, kinds):
             assert used == len(slots)
         got.append(out)
     assert x == len(ops)
-    if back:
+    for y, of in enumerate(got):
+        if not (back and of and space.results[0] <= of[0][0] < space.results[1]):
+            continue
         # results in dense rows: their tiles do not meet, and what goes into the tiles is what they hold
-        (out,) = got
-        pitch = {o[1] * o[2] for o in out}
-        assert pitch == {o[2] for o in back} and len({o[5] for o in out}) == 1
-        at, pitch, es = min(o[0] for o in out), pitch.pop(), out[0][2]
-        placed = sorted((*reversed(divmod(o[0] - at, pitch)), o[3], o[4] * es) for o in out)
+        pitch = {o[1] * o[2] for o in of}
+        assert pitch == {o[2] for o in back} and len({o[5] for o in of}) == 1
+        at, pitch, es = min(o[0] for o in of), pitch.pop(), of[0][2]
+        placed = sorted((*reversed(divmod(o[0] - at, pitch)), o[3], o[4] * es) for o in of)
         for i, (col, row, h, w) in enumerate(placed):
             assert col + w <= pitch and not any(c < col + w and r < row + h and row < r + hh for c, r, hh, _ in placed[i + 1:])
         rows, cols = max(r + h for _, r, h, _ in placed), max(c + w for c, _, _, w in placed)
         assert sum(h * w for _, _, h, w in placed) == rows * cols
-        out, of = Results(), out
+        out = Results()
         for src, dst, _, dst_pitch, h, size in back:
             r, c = divmod(src - at, pitch)
             if r < rows and c + size <= cols and r + h <= rows:    # (what is kept of G and U lies behind H)
                 out.append((dst, dst_pitch // es, es, h, size // es, of[0][5]))
             else:
                 space.inside(dst, dst + (h - 1) * dst_pitch + size, "kept results")
-        got = [out]
+        got[y] = out
     return got
 
 
@@ -396,6 +399,19 @@ def rows_in_blocks_are_joined_on_a_copy(rec):
             (out,) = follow_call(rec, space, at, [kind])
             assert space.copies and not out.copies and bool(space.results) == back, (kind, m, k, n)
             covers(space, out, h[1], h[2], d[2], 2, k, 64)
+    # a layer's gradients by few rows: dA alike, dB on copies of both its operands
+    for m, k, n, back in ((83, 4160, 16384, True), (96, 4099, 8192, False)):
+        d = (workloads.block_desc(m, k, 8 if back else 1, 1), workloads.desc(k, n, [0, 1000, k], [0, 3001, n], 2, 2), workloads.block_desc(m, n, 4, 2))
+        plan, space = b.Plan(*d, 8), Space()
+        a, w, v, h, g, u, dg, du, da = (space.tiles(x, 2) for x in (d[0], d[1], d[1], d[2], d[2], d[2], d[2], d[2], d[0]))
+        dw, dv = space.tiles(d[1], 4), space.tiles(d[1], 4)
+        at = len(rec.ops())
+        plan.gated_backward(b.DMM_SILU, a[0], w[0], v[0], g[0], u[0], h[0], dg[0], du[0], da[0], dw[0], dv[0], b.DMM_DB_F32, 0)
+        out = follow_call(rec, space, at, ["nt", "tn"])
+        assert space.copies and not out[0].copies and out[1].copies and bool(space.results) == back, (m, k, n)
+        covers(space, out[0], da[1], da[2], d[0], 2, n, 64, 2)
+        covers(space, those(space, out[1], dw), dw[1], dw[2], d[1], 4, m, 64)
+        covers(space, those(space, out[1], dv), dv[1], dv[2], d[1], 4, m, 64)
 
 
 def a_call_without_memory_for_copies_runs_on_the_operands(rec):
