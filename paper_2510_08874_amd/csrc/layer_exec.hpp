@@ -123,7 +123,8 @@ struct LayerChoice {
 // Which operands of a product are read from copies; LAYER_ROWS: the left one, and results go through scratch memory as well.
 enum LayerDense { LAYER_IN_PLACE, LAYER_BOTH, LAYER_LEFT, LAYER_ROWS };
 
-// Dense copies of operands whose rows are misaligned or finely cut: every row starts at a multiple of 128 bytes, K is one segment of whole steps,
+// Dense copies of operands whose rows are misaligned or finely cut (8-bit gated 2501 x 1999 x 1777 in 15 uneven blocks: 93 us in place, 42 with 10 for the
+// copies; gradients of 1999 x 2731 x 1021 87 and 52): every row starts at a multiple of 128 bytes, K is one segment of whole steps,
 // filled up with zeros.  Places are given out from 0 on; the buffer is known later.
 struct LayerCopies {
   std::vector<LayerCopy> jobs, back;   // in front of the product, behind it
@@ -242,8 +243,13 @@ constexpr size_t kLayerCopies = (size_t)1 << 30;               // of a call
 bool LayerCopies::possible() const { return fits && size <= kLayerCopies && blocks <= kLayerBlocks && back_blocks <= kLayerBlocks; }
 
 
-// By an estimate in us, from what a step (128 bytes of K) of a tile takes, measured as what more of K costs.  Where rows are not aligned to 16 bytes a step takes a
-// quarter more (integers: a third: 8191^3 direct 625 us, on copies 497; aligned 423), what is left of a segment as much as four steps.
+// The macro-tile, and into how many runs K is cut, with the shortest estimate in us, from measured steps (128 bytes of K): for every shape a step's time with
+// few workgroups and what it grows by until all CUs have one, and a tile's ends.  Where rows are not aligned to 16 bytes a step takes a quarter more (integers a
+// third: 8191^3 direct 625 us, on copies 497; aligned 423; gated 40 and 45 %), what is left of a segment 5 us whatever the shape.  Both sides of what it decides:
+//   gated, 8 bits, 2501 x 512 x 1777     two on a CU 14.3, 256 x 128 19.2          4096 x 4096 x 8192    265 and 237
+//   gated, bf16, 256 x 2048 x 2048       two on a CU 18.6, 128 x 128 24.6          1024 x 4096 x 4096    73 and 58
+//   8 bits, 2048^3                       128 x 128 13.4, 256 x 256 27.8            4096 x 4096 x 8192    136 and 117
+//   gated, bf16, 128 x 8192 x 4096       K in four runs 37, whole 64               1 x 8192 x 28672 in 8 bits: 43 and 36 (B is in a cache), whole
 LayerChoice choose_layer(const LayerWork &W, int cus) {
   const bool gated = layer_gated(W.kind);
   double cells = 0, k_steps = 0, k_tails = 0, b_once = 0;

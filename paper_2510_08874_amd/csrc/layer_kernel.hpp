@@ -1,5 +1,8 @@
 // Kernels of the layers around a product (gfx950, device code only): products of 8-bit integers with a scale for every row and
 // column, the gated block H = act(A Wg) * (A Wu), and the gradients of bf16 products, all on the macro-tiles of layer_tile.hpp.
+//
+// Sums, scales, activations and the product of both projections are fp32 (integers: int32 sums, converted once); a result is rounded once, on its
+// way out.  The activation is applied where the sums are: G and U of 8192 x 49152 would be 3.2 GB written and read again, 1.3 ms beside 14.6.
 #pragma once
 
 #include "dmm.h"
@@ -13,7 +16,6 @@ typedef __bf16 layer_bf16x2 __attribute__((ext_vector_type(2)));
 typedef float layer_f32x2 __attribute__((ext_vector_type(2)));
 typedef int layer_i32_any __attribute__((aligned(2)));        // (two bf16 at any address of one)
 __device__ __forceinline__ unsigned short layer_bf16(float v) { return __builtin_bit_cast(unsigned short, (__bf16)v); }
-__device__ __forceinline__ float layer_f32(unsigned short v) { return __builtin_bit_cast(float, (unsigned)v << 16); }
 
 // ---- activations ------------------------------------------------------------------------------------
 

@@ -88,6 +88,7 @@ __device__ __forceinline__ void layer_store8(char *row, int col, int w, const La
 
 // Tiles whose rows are misaligned or finely cut, into dense rows: 16 bytes a thread at a time, eight of them on their way together.  The last 16 bytes
 // of a row are moved as such, over some of those in front of them: a part of 16 bytes would be moved one by one, and every wave meets one.
+// Bound: HBM or the caches (21 MB of integers in 15 uneven blocks 10.2 us with the launch, 4.1 TB/s read and written).
 __global__ __launch_bounds__(256) void layer_copy_kernel(const LayerCopy *__restrict__ jobs, int n) {
   const LayerCopy j = jobs[layer_last(jobs, n, (int)blockIdx.x)];
   const unsigned across = (unsigned)(j.bytes + 15) / 16;      // chunks of a row
@@ -121,7 +122,8 @@ __global__ __launch_bounds__(256) void layer_copy_kernel(const LayerCopy *__rest
 }
 
 // dU = dH act(G), dG = dH U act'(G): a thread has four pieces of eight neighbouring elements, whatever rows they are of.  Every element is read and written
-// by one thread, in this order, so dG and dU may be G and U themselves.
+// by one thread, in this order, so dG and dU may be G and U themselves.  Bound: HBM (4096 x 8192: 335 MB in 62 us, 5.4 TB/s; 2501 x 1777 in 15 uneven blocks,
+// 44 MB with rows at any address, 17.7).
 __global__ __launch_bounds__(256) void layer_slope_kernel(SlopeArgs) {
   const auto &args = *(const SlopeArgs *)__builtin_amdgcn_kernarg_segment_ptr();
   constexpr int N = SLOPE_CHUNKS / 256;
@@ -164,6 +166,10 @@ __global__ __launch_bounds__(256) void layer_slope_kernel(SlopeArgs) {
 //
 // A row's (column's) scale is its largest magnitude over 127, rounded to fp32; an element is the integer nearest to 127 x / (largest
 // magnitude), both taken exactly, half-way values to the even one.  A row with an infinity or a NaN has the scale NaN.
+//
+// Bound: HBM.  A row's scale is known only when all of it has been read; along the rows a workgroup keeps what it has read in registers, along the columns the
+// matrix is read twice (4099 x 11003 fp32 in uneven blocks: magnitudes 47 us, 3.8 TB/s; integers 46, 4.9; values back 56, 4.0; scales cleared and finished
+// 4.8 each).
 
 // bits of |x|, which compare like the values (NaN above infinity)
 template <bool F32>
