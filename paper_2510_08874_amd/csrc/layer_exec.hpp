@@ -7,6 +7,7 @@ namespace dmm {
 namespace {
 
 constexpr int64_t kLayerBlocks = (1 << 24) - 1;                // workgroups of a launch: 2^32 threads are too many
+constexpr int kLayerManyRows = 1024;                           // rows that fill the device with small workgroups
 constexpr int64_t kLayerPitch = (int64_t)1 << 24;              // bytes from row to row
 constexpr int64_t kLayerRows = 0x7fff0000;                     // kernels count rows and columns in 32 bits, a workgroup's past the last among them
 constexpr int64_t kLayerSum = 131071;                          // products of two bytes that an int32 sum holds whatever they are
@@ -1097,7 +1098,7 @@ int i8_form(const Grid &G, int dtype, char *const *x, const int64_t *x_ld, const
   const int es = dtype == DMM_F32 ? 4 : 2;
   const bool f32 = es == 4;
   int rc;
-  if (!by_cols && G.gc <= I8_ROW_PIECES) {
+  if (!by_cols && G.gc <= I8_ROW_PIECES && G.cols <= kLayerRows) {
     for (int32_t rep = 0; rep < G.c; ++rep)
       for (int32_t ti = 0; ti < G.gr; ++ti) {
         I8RowArgs args;
@@ -1107,11 +1108,13 @@ int i8_form(const Grid &G, int dtype, char *const *x, const int64_t *x_ld, const
         args.scale = q->scales[(int64_t)rep * G.gr + ti];
         for (int32_t tj = 0; tj < G.gc; ++tj) {
           const int64_t w = G.cc[(size_t)tj + 1] - G.cc[(size_t)tj], i = G.table_index(rep, ti, tj);
-          if (w > 0) args.piece[args.n++] = {x[i], (char *)q->codes[i], x_ld[i] * es, q->code_ld[i], (int32_t)w, 0};
+          if (w <= 0) continue;
+          args.piece[args.n++] = {x[i], (char *)q->codes[i], x_ld[i] * es, q->code_ld[i], (int32_t)w, args.vectors};
+          args.vectors += (int32_t)((w + 7) / 8);
         }
-        int32_t widest = 0;
-        for (int32_t p = 0; p < args.n; ++p) widest = std::max(widest, args.piece[p].w);
-        const int threads = (int)std::min<int64_t>(I8_ROW_THREADS, up_to(std::max(widest, 512) / 8, 64));
+        // (few rows: a vector a thread; many: I8_ROW_KEPT, and more rows on a CU at a time)
+        const int per = args.h < kLayerManyRows ? 1 : I8_ROW_KEPT;
+        const int threads = (int)std::min<int64_t>(I8_ROW_THREADS, up_to(std::max(args.vectors / per, 1), 64));
         // (rows past the 2^32 threads that a launch can have go into the next)
         const int64_t all = args.h, most = ((int64_t)1 << 32) / threads - 1;
         for (int64_t at = 0; at < all; at += most) {

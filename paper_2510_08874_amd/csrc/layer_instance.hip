@@ -165,8 +165,8 @@ void i8_values_launch(const I8Args &args, int blocks, bool f32, bool cols, hipSt
 }
 void i8_whole_rows_launch(const I8RowArgs &args, int threads, bool f32, hipStream_t stream) {
   const dim3 grid((unsigned)args.h), block((unsigned)threads);
-  if (f32) i8_whole_rows_kernel<true><<<grid, block, 0, stream>>>(args);
-  else i8_whole_rows_kernel<false><<<grid, block, 0, stream>>>(args);
+  if (f32) args.n > 1 ? i8_whole_rows_kernel<true, true><<<grid, block, 0, stream>>>(args) : i8_whole_rows_kernel<true, false><<<grid, block, 0, stream>>>(args);
+  else args.n > 1 ? i8_whole_rows_kernel<false, true><<<grid, block, 0, stream>>>(args) : i8_whole_rows_kernel<false, false><<<grid, block, 0, stream>>>(args);
 }
 
 #endif

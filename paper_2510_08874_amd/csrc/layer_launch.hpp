@@ -147,12 +147,13 @@ struct I8RowPiece {
   const char *x;
   char *q;
   int64_t x_pitch, q_pitch;
-  int32_t w, pad;
+  int32_t w, first;              // columns; vectors of eight of the tiles in front
 };
-constexpr int I8_ROW_PIECES = 32, I8_ROW_THREADS = 1024, I8_ROW_KEPT = 2;   // eight elements of a row, so many a thread
+constexpr int I8_ROW_PIECES = 32, I8_ROW_THREADS = 1024, I8_ROW_KEPT = 4;
 struct I8RowArgs {
   float *scale;
   int32_t h, n;
+  int32_t vectors, pad;          // of all tiles
   I8RowPiece piece[I8_ROW_PIECES];
 };
 enum { I8_CLEAR, I8_FINISH };

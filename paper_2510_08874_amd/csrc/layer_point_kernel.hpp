@@ -230,6 +230,23 @@ __device__ __forceinline__ void i8_put(char *p, const unsigned *w, int n) {
       if (i < n) p[i] = (char)(w[i / 4] >> (8 * (i & 3)));
   }
 }
+// Eight integers of a row from column `col` on, zeros behind column w (a row's end as in layer_load8).
+__device__ __forceinline__ void i8_load8(const char *row, int col, int w, unsigned out[2]) {
+  uint64_t all = 0;
+  if (col + 8 <= w) {
+    __builtin_memcpy(&all, row + col, 8);
+  } else if (w >= 8) {
+    const int back = min(col + 8 - w, 8);
+    __builtin_memcpy(&all, row + w - 8, 8);
+    all = back < 8 ? all >> (8 * back) : 0;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (col + i < w) all |= (uint64_t)*(const unsigned char *)(row + col + i) << (8 * i);
+  }
+  out[0] = (unsigned)all;
+  out[1] = (unsigned)(all >> 32);
+}
 template <int N>
 __device__ __forceinline__ void i8_get(const char *p, unsigned *w, int n) {
 #pragma unroll
@@ -337,13 +354,21 @@ __global__ __launch_bounds__(256) void i8_rows_kernel(I8Args) {
   const I8Place place0 = i8_place<128, B::COLS>(T, block);
   const int col0 = place0.col0, row0 = place0.row0;
   const int col = col0 + threadIdx.x % B::ACROSS * 8, r0 = threadIdx.x / B::ACROSS;
+  if (col >= T.w) return;
+  LayerVec<F32> v[B::PASSES];
+  unsigned top[B::PASSES];
+#pragma unroll
+  for (int x = 0; x < B::PASSES; ++x) {
+    const int row = min(row0 + x * B::DOWN + r0, T.h - 1);    // (rows past the last read that one again: loads that wait for no branch)
+    v[x] = layer_load8<F32>(T.x + (int64_t)row * T.x_pitch, col, T.w);
+    top[x] = ((const unsigned *)T.scale)[row];
+  }
 #pragma unroll
   for (int x = 0; x < B::PASSES; ++x) {
     const int row = row0 + x * B::DOWN + r0;
-    if (row >= T.h || col >= T.w) continue;
-    const LayerVec<F32> v = layer_load8<F32>(T.x + (int64_t)row * T.x_pitch, col, T.w);
-    const I8Row r = i8_row(((const unsigned *)T.scale)[row]);
-    const unsigned w[2] = {i8_four(r, v.at(0), v.at(1), v.at(2), v.at(3)), i8_four(r, v.at(4), v.at(5), v.at(6), v.at(7))};
+    if (row >= T.h) break;
+    const I8Row r = i8_row(top[x]);
+    const unsigned w[2] = {i8_four(r, v[x].at(0), v[x].at(1), v[x].at(2), v[x].at(3)), i8_four(r, v[x].at(4), v[x].at(5), v[x].at(6), v[x].at(7))};
     i8_put<2>(T.q + (int64_t)row * T.q_pitch + col, w, T.w - col);
   }
 }
@@ -406,37 +431,46 @@ __global__ __launch_bounds__(256) void i8_cols_kernel(I8Args) {
   }
 }
 
-// The rows of a row of tiles, a workgroup each, scales and integers: what fits is kept between the two passes over a row.  (16 rows of 8192: 256 threads
-// with eight pieces each took 7 us, of which 2 went into turning 32 elements a thread into integers.)
-template <bool F32>
+// The rows of a row of tiles, a workgroup each, scales and integers.  The vectors of eight elements of all tiles are counted through, so that every thread has
+// its own on their way at once whatever the tiles' widths, and the first I8_ROW_KEPT of each thread stay in registers between the two passes over a row.  (16
+// rows of 8192: 256 threads with four vectors each 7 us, 1024 threads 4.3; 115 x 715 in eight tiles, and back, 22 us
+// one tile after the other, now 11.  4096 x 8192, and back: 36 us with 256 threads and four vectors each, 50 with 1024 and one.)
+// CUT: several tiles (without, the one tile's numbers stay in scalar registers).
+template <bool F32, bool CUT>
 __global__ __launch_bounds__(I8_ROW_THREADS) void i8_whole_rows_kernel(I8RowArgs) {
-  constexpr int KEPT = I8_ROW_KEPT, PIECES = 4;               // pieces of eight elements of each of the first tiles of the row that stay in registers
   __shared__ unsigned tops[I8_ROW_THREADS / 64];
+  __shared__ int firsts[I8_ROW_PIECES];
   const auto &args = *(const I8RowArgs *)__builtin_amdgcn_kernarg_segment_ptr();
   const int row = blockIdx.x, tid = threadIdx.x, threads = blockDim.x;
-  LayerVec<F32> kept[PIECES][KEPT];
+  if constexpr (CUT) {
+    if (tid < args.n) firsts[tid] = args.piece[tid].first;
+    __syncthreads();
+  }
+  // the tile of vector `at`
+  auto piece_of = [&](int at) -> const I8RowPiece & {
+    if constexpr (!CUT) return args.piece[0];
+    int lo = 0, hi = args.n - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (firsts[mid] <= at) lo = mid;
+      else hi = mid - 1;
+    }
+    return args.piece[lo];
+  };
+  auto load = [&](int at) {
+    const I8RowPiece &P = piece_of(at);
+    return layer_load8<F32>(P.x + (int64_t)row * P.x_pitch, (at - P.first) * 8, P.w);
+  };
+  LayerVec<F32> kept[I8_ROW_KEPT];
+#pragma unroll
+  for (int y = 0; y < I8_ROW_KEPT; ++y) {
+    kept[y] = LayerVec<F32>{};
+    if (y * threads + tid < args.vectors) kept[y] = load(y * threads + tid);
+  }
   unsigned m = 0;
 #pragma unroll
-  for (int p = 0; p < PIECES; ++p) {
-    if (p >= args.n) break;
-    const I8RowPiece &P = args.piece[p];
-#pragma unroll
-    for (int y = 0; y < KEPT; ++y) {
-      kept[p][y] = LayerVec<F32>{};
-      if ((y * threads + tid) * 8 < P.w) kept[p][y] = layer_load8<F32>(P.x + (int64_t)row * P.x_pitch, (y * threads + tid) * 8, P.w);
-    }
-  }
-#pragma unroll
-  for (int p = 0; p < PIECES; ++p) {
-    if (p >= args.n) break;
-#pragma unroll
-    for (int y = 0; y < KEPT; ++y) m = i8_abs_max(kept[p][y], m);
-  }
-  for (int p = 0; p < args.n; ++p) {
-    const I8RowPiece &P = args.piece[p];
-    for (int col = ((p < PIECES ? KEPT * threads : 0) + tid) * 8; col < P.w; col += threads * 8)
-      m = i8_abs_max(layer_load8<F32>(P.x + (int64_t)row * P.x_pitch, col, P.w), m);
-  }
+  for (int y = 0; y < I8_ROW_KEPT; ++y) m = i8_abs_max(kept[y], m);
+  for (int64_t at = I8_ROW_KEPT * threads + tid; at < args.vectors; at += threads) m = i8_abs_max(load((int)at), m);
   m = i8_wave_max(m);
   if ((tid & 63) == 0) tops[tid >> 6] = m;
   __syncthreads();
@@ -444,23 +478,16 @@ __global__ __launch_bounds__(I8_ROW_THREADS) void i8_whole_rows_kernel(I8RowArgs
   for (int x = 0; x < threads / 64; ++x) m = max(m, tops[x]);
   if (tid == 0) args.scale[row] = i8_scale(m);
   const I8Row r = i8_row(m);
-  auto codes = [&](const I8RowPiece &P, int col, const LayerVec<F32> &v) {
+  auto codes = [&](int at, const LayerVec<F32> &v) {
+    const I8RowPiece &P = piece_of(at);
+    const int col = (at - P.first) * 8;
     const unsigned w[2] = {i8_four(r, v.at(0), v.at(1), v.at(2), v.at(3)), i8_four(r, v.at(4), v.at(5), v.at(6), v.at(7))};
     i8_put<2>(P.q + (int64_t)row * P.q_pitch + col, w, P.w - col);
   };
 #pragma unroll
-  for (int p = 0; p < PIECES; ++p) {
-    if (p >= args.n) break;
-    const I8RowPiece &P = args.piece[p];
-#pragma unroll
-    for (int y = 0; y < KEPT; ++y)
-      if ((y * threads + tid) * 8 < P.w) codes(P, (y * threads + tid) * 8, kept[p][y]);
-  }
-  for (int p = 0; p < args.n; ++p) {
-    const I8RowPiece &P = args.piece[p];
-    for (int col = ((p < PIECES ? KEPT * threads : 0) + tid) * 8; col < P.w; col += threads * 8)
-      codes(P, col, layer_load8<F32>(P.x + (int64_t)row * P.x_pitch, col, P.w));
-  }
+  for (int y = 0; y < I8_ROW_KEPT; ++y)
+    if (y * threads + tid < args.vectors) codes(y * threads + tid, kept[y]);
+  for (int64_t at = I8_ROW_KEPT * threads + tid; at < args.vectors; at += threads) codes((int)at, load((int)at));
 }
 
 // Values, integer times scale, along the rows.
@@ -473,16 +500,21 @@ __global__ __launch_bounds__(256) void i8_row_values_kernel(I8Args) {
   const I8Place place0 = i8_place<128, B::COLS>(T, block);
   const int col = place0.col0 + threadIdx.x % B::ACROSS * 8, row0 = place0.row0 + threadIdx.x / B::ACROSS;
   if (col >= T.w) return;
+  unsigned w[B::PASSES][2];
+  float s[B::PASSES];
+#pragma unroll
+  for (int x = 0; x < B::PASSES; ++x) {
+    const int row = min(row0 + x * B::DOWN, T.h - 1);
+    i8_load8(T.q + (int64_t)row * T.q_pitch, col, T.w, w[x]);
+    s[x] = T.scale[row];
+  }
 #pragma unroll
   for (int x = 0; x < B::PASSES; ++x) {
     const int row = row0 + x * B::DOWN;
-    if (row >= T.h) continue;
-    unsigned w[2];
-    i8_get<2>(T.q + (int64_t)row * T.q_pitch + col, w, T.w - col);
-    const float s = T.scale[row];
+    if (row >= T.h) break;
     LayerVec<F32> v;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v.set(i, (float)(signed char)(w[i / 4] >> (8 * (i & 3))) * s);
+    for (int i = 0; i < 8; ++i) v.set(i, (float)(signed char)(w[x][i / 4] >> (8 * (i & 3))) * s[x]);
     layer_store8<F32>(T.x + (int64_t)row * T.x_pitch, col, T.w, v);
   }
 }

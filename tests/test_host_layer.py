@@ -502,7 +502,7 @@ def many_rows_take_several_launches(rec):
     """A launch has less than 2^32 threads, and no row is left out or quantised twice."""
     from paper_2510_08874_amd import binding as b
     rec.so.rec_blocks.restype = ctypes.c_uint
-    for m, n, threads in (((1 << 23) + 5, 8192, 1024), ((1 << 31) - (1 << 17), 1, 64), (1 << 22, 2000, 256)):
+    for m, n, threads in (((1 << 24) + 5, 8192, 256), ((1 << 22) + 5, 40000, 1024), ((1 << 31) - (1 << 17), 1, 64), (1 << 22, 2000, 64)):
         d, space = workloads.desc(m, n, [0, m], [0, n], 1, 1), Space(True)
         at = len(rec.ops())
         b.dmm_int_quantize(b.matrix_desc(d), b.DMM_BF16, space.tiles(d, 2)[0], rows=space.integers(d, "rows"))
