@@ -14,8 +14,8 @@ binding = pytest.importorskip("paper_2510_08874_amd.binding")
 pytestmark = pytest.mark.gpu
 BF16 = torch.bfloat16
 
-# whole tiles; cut along K; on copies
-SIZES = [("blocks", 512, 512, 768), ("whole", 40, 8192, 300), ("uneven", 1301, 1103, 907)]
+# whole tiles; cut along K; on copies; on copies of few rows alone, results on their way through scratch memory
+SIZES = [("blocks", 512, 512, 768), ("whole", 40, 8192, 300), ("uneven", 1301, 1103, 907), ("row_col", 9, 2000, 12001)]
 
 
 class Calls:
@@ -260,7 +260,7 @@ def test_empty_sides(m, k, n):
     assert bool((ga.whole() == n).all()) and bool((gw.whole() == m).all())
 
 
-@pytest.mark.parametrize("layout,m,k,n", [("whole", 70, 200, 90), ("uneven", 300, 257, 260), ("uneven", 1301, 1103, 907)], ids=str)
+@pytest.mark.parametrize("layout,m,k,n", [("whole", 70, 200, 90), ("uneven", 300, 257, 260), ("uneven", 1301, 1103, 907), ("row_col", 9, 2000, 12001)], ids=str)
 def test_infinities_and_nan_stay_in_their_rows_and_columns(layout, m, k, n):
     """Of the operands, whatever is filled up with zeros next to them."""
     (da, db, dc), ranks = descs(layout, m, k, n)

@@ -331,7 +331,8 @@ def sizes_under_test_take_the_ways_they_are_meant_for(rec):
     """The sizes of the GPU tests of calls: whole tiles as they lie, tiles cut along K, copies of the operands."""
     from paper_2510_08874_amd import binding as b
     for layout, m, k, n, kernels in (("blocks", 512, 512, 768, {"layer_gemm_kernel"}), ("whole", 40, 8192, 300, {"layer_gemm_kernel", "layer_join_kernel"}),
-                                     ("uneven", 1301, 1103, 907, {"layer_gemm_kernel", "layer_copy_kernel"})):
+                                     ("uneven", 1301, 1103, 907, {"layer_gemm_kernel", "layer_copy_kernel"}),
+                                     ("row_col", 9, 2000, 12001, {"layer_gemm_kernel", "layer_copy_kernel"})):
         d = made(layout, m, k, n)
         plan, space = b.Plan(*d, 12), Space(True)
         a, w, v = space.integers(d[0], "rows"), space.integers(d[1], "cols"), space.integers(d[1], "cols")
@@ -341,7 +342,10 @@ def sizes_under_test_take_the_ways_they_are_meant_for(rec):
                                (lambda: plan.gated(b.DMM_SILU, *t[:4], None, None, 0), kernels), (lambda: plan.execute_backward(t[0], t[1], t[3], t[7], t[8]), set())):
             at = len(rec.ops())
             call()
-            got = {o[1] for o in rec.launches(at)}
+            names = [o[1] for o in rec.launches(at)]
+            if layout == "row_col":                                # (results are copied behind the product, dA in front of dB)
+                assert names.count("layer_copy_kernel") == 2 and names[0] == names[-1] == "layer_copy_kernel", names
+            got = set(names)
             assert got >= at_least and (not at_least or "layer_copy_kernel" in at_least or "layer_copy_kernel" not in got), (layout, got)
 
 
@@ -357,6 +361,8 @@ def made(layout, m, k, n):
         return D(m, k, [0, m], [0, k], 1, 1), D(k, n, [0, k], [0, n], 1, 1), D(m, n, [0, m], [0, n], 1, 1)
     if layout == "blocks":
         return block(m, k, 2, 2), block(k, n, 2, 2), block(m, n, 2, 2)
+    if layout == "row_col":
+        return block(m, k, 8, 1), D(k, n, uneven(k, 3), uneven(n, 2), 3, 2), block(m, n, 4, 2)
     return D(m, k, uneven(m, 3), uneven(k, 4), 3, 4), D(k, n, uneven(k, 3), uneven(n, 2), 3, 2), D(m, n, uneven(m, 2), uneven(n, 3), 2, 3)
 
 
