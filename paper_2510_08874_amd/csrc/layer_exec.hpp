@@ -119,6 +119,8 @@ struct LayerChoice {
   int shape = LAYER_256;
   int64_t runs = 1;
   double us = 0;
+  // what an estimate of two products together needs: steps and tails of a tile's K, macro-tiles of 128 x 128, how long memory takes
+  double steps = 0, tails = 0, tiles = 0, memory = 0;
 };
 
 // Which operands of a product are read from copies; LAYER_ROWS: the left one, and results go through scratch memory as well.
@@ -273,6 +275,8 @@ LayerChoice choose_layer(const LayerWork &W, int cus) {
   }
   const double steps = cells > 0 ? std::max(1.0, k_steps / cells) : 1, tails = cells > 0 ? k_tails / cells : 0;
   LayerChoice best;
+  best.steps = steps;
+  best.tails = tails;
   double best_us = 0;
   for (int shape = 0; shape < LAYER_SHAPES; ++shape) {
     const int tm = kLayerTile[W.kind][shape].tm, tn = kLayerTile[W.kind][shape].tn;
@@ -288,6 +292,7 @@ LayerChoice choose_layer(const LayerWork &W, int cus) {
     const int places = shape == LAYER_TWO || (!gated && shape != LAYER_256) ? 2 * cus : cus;
     // B from memory; another row of tiles reads it from a cache (48 x 8192 x 28672 gated, integers: 85 us on tiles of 64 rows, 103 on those of 32)
     const double down = strips * (double)W.rows / std::max(cells, 1.0);
+    if (shape == LAYER_128) best.tiles = tiles;
     const double memory = 2.0 + b_once * (0.8 + 0.2 * down) / 5.4e6;
     for (int64_t runs = 1; runs <= 32; ++runs) {
       const double work = tiles * (double)runs, per = std::ceil(steps / (double)runs);
@@ -307,10 +312,27 @@ LayerChoice choose_layer(const LayerWork &W, int cus) {
       double us = std::max(whole * round(places) + round(work - whole * places), memory);
       if (runs > 1) us += 4.5 + 2.0 * work * tm * tn * (gated ? 2 : 1) * 4 / 3e6;
       // (of equal estimates, as where memory bounds all of them, the smaller tile's)
-      if (best_us == 0 || us < best_us || (us == best_us && shape != best.shape)) best_us = best.us = us, best.shape = shape, best.runs = runs;
+      if (best_us == 0 || us < best_us || (us == best_us && shape != best.shape)) best_us = best.us = us, best.shape = shape, best.runs = runs, best.memory = memory;
     }
   }
   return best;
+}
+
+// Both gradients in one launch of macro-tiles of 128 x 128, each with its own runs of K (what a product is asked for with does not change its bits).  Both sides,
+// gated backward: 2501 x 1999 x 1777 uneven 145 us in two launches, 126 in one; 2048^3 84 and 81; 1448 x 512 x 768 in row blocks 52 and 36; 4096^3 452 and 522.
+double pair_us(const LayerChoice *c, int cus) {
+  double n = 0, busy = 0, longest = 0, us = 0;
+  for (int x = 0; x < 2; ++x) n += c[x].tiles * (double)c[x].runs;
+  const double full = n / cus;
+  for (int x = 0; x < 2; ++x) {
+    const double per = std::ceil(c[x].steps / (double)c[x].runs), ends = kTail * c[x].tails / (double)c[x].runs, work = c[x].tiles * (double)c[x].runs;
+    busy += work * (0.45 * per + 2.0 + 0.4 * ends) / cus;
+    longest = std::max(longest, per * (full > 1 ? 0.8 : 0.5 + 0.16 * full) + 5.0 + ends);
+    if (c[x].runs > 1) us += 4.5 + 2.0 * work * 128 * 128 * 4 / 3e6;
+  }
+  // (rounds are not full: a third of the longest tile; a launch less, with its start and its last tiles)
+  const double rounds = full > 1 ? busy + 0.3 * (longest - 5.0) : longest;
+  return us - 7.0 + std::max({rounds, longest, c[0].memory + c[1].memory});
 }
 
 // Tables of one product, appended to `h`; partial sums in slots of M's buffer, which have addresses from 0 on until place_parts.
@@ -383,6 +405,7 @@ int lay_out(const LayerWork &W, const LayerChoice &choice, std::vector<char> *h,
                 it.steps = (int32_t)n_steps;
                 it.tail_seg = (int32_t)tail0;
                 it.n_tails = (int32_t)(tail - tail0);
+                it.kind = W.kind;
                 it.what = k == 0 ? LAYER_ZERO : LAYER_STORE;
                 if (runs > 1) {
                   const int64_t slot = first_slot + tile * runs;
@@ -463,6 +486,32 @@ void place_parts(std::vector<char> *h, const LayerLayout &L, char *buf, char *co
   }
 }
 
+// The tables of two products, one behind the other in `h`, as those of one launch: that with the longer tiles first.
+void merge_pair(std::vector<char> *h, LayerLayout *L, bool second_first) {
+  std::vector<char> all;
+  const int order[2] = {second_first ? 1 : 0, second_first ? 0 : 1};
+  auto put = [&](size_t from, size_t to) { all.insert(all.end(), h->data() + from, h->data() + to); };
+  const size_t n_segs = (L[order[0]].o_joins - L[order[0]].o_segs) / sizeof(LayerSeg);
+  for (LayerItem *it = (LayerItem *)(h->data() + L[order[1]].o_items), *end = it + L[order[1]].n_items; it < end; ++it) {
+    it->seg += (int32_t)n_segs;
+    it->tail_seg += (int32_t)n_segs;
+  }
+  LayerLayout both = L[0];
+  both.kind = LAYER_PAIR;
+  both.shape = LAYER_128;
+  both.n_items = L[0].n_items + L[1].n_items;
+  both.n_joins = L[0].n_joins + L[1].n_joins;
+  both.o_items = 0;
+  for (int x : order) put(L[x].o_items, L[x].o_segs);
+  both.o_segs = all.size();
+  for (int x : order) put(L[x].o_segs, L[x].o_joins);
+  both.o_joins = all.size();
+  for (int x : order) put(L[x].o_joins, L[x].o_joins + (size_t)L[x].n_joins * sizeof(LayerJoin));
+  h->swap(all);
+  L[0] = both;
+  L[1] = LayerLayout();
+}
+
 // The part of a call that all kinds have in common: the tables of the call before if they are of the same inputs (`key`), else new ones,
 // made from what `make` tells of each product (on the operands, or on copies; the first `lefts` products can be on copies of the left operand alone); then `in_front`, the launches and, where `reduce` asks for it, the sum of
 // C's replicas.
@@ -513,10 +562,13 @@ int run_layer_on(dmm_plan_t *P, int which, const std::vector<char> &inputs, void
     if ((rc = P->dev->uses.order(stream))) return rc;
     for (;;) {
       h.clear();
-      size_t scratch = 0;
-      for (int x = 0; x < products; ++x)
-        if ((rc = lay_out(work[x], choice[x], &h, &layout[x], &scratch))) return rc;
-      scratch = (scratch + 4095) / 4096 * 4096;
+      size_t parts[2] = {0, 0};                                // partial sums of each product
+      const bool pair = products == 2 && choice[0].tiles > 0 && choice[1].tiles > 0 && pair_us(choice, cus) < choice[0].us + choice[1].us;
+      for (int x = 0; x < products; ++x) {
+        if (pair) choice[x].shape = LAYER_128;
+        if ((rc = lay_out(work[x], choice[x], &h, &layout[x], &parts[x]))) return rc;
+      }
+      const size_t scratch = ((pair ? parts[0] + parts[1] : std::max(parts[0], parts[1])) + 4095) / 4096 * 4096;
       const size_t need = scratch + copies.size;
       if (need > M.cap) {
         if (M.buf) {
@@ -539,7 +591,8 @@ int run_layer_on(dmm_plan_t *P, int which, const std::vector<char> &inputs, void
         if (rc) return rc;
       }
       char *const at = copies.size ? M.buf + scratch : nullptr;
-      for (int x = 0; x < products; ++x) place_parts(&h, layout[x], M.buf, at, dense[x]);
+      for (int x = 0; x < products; ++x) place_parts(&h, layout[x], M.buf + (pair && x == 1 ? parts[0] : 0), at, dense[x]);
+      if (pair && layout[0].n_items && layout[1].n_items) merge_pair(&h, layout, choice[1].steps / (double)choice[1].runs > choice[0].steps / (double)choice[0].runs);
       for (LayerCopy &j : copies.jobs) j.dst = at + (uintptr_t)j.dst;
       for (LayerCopy &j : copies.back) j.src = at + (uintptr_t)j.src;
       break;

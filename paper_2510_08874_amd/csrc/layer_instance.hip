@@ -81,8 +81,27 @@ bool launch(hipEvent_t behind, int shape, int cus, const LayerItem *items, int n
 
 }  // namespace
 
+#if DMM_INSTANCE == 4
+namespace {
+using N128 = LayerShape<LAYER_NT, 128, 128, 2, 2>;
+using ND128 = LayerShape<LAYER_NT, 128, 128, 4, 2>;
+template <class SA, class SB>
+hipError_t allow_pair() {
+  return hipFuncSetAttribute((const void *)layer_pair_kernel<SA, SB>, hipFuncAttributeMaxDynamicSharedMemorySize, SA::LDS);
+}
+}  // namespace
+bool layer_launch_pair(hipEvent_t behind, int cus, const LayerItem *items, int n, const LayerSeg *segs, hipStream_t stream) {
+  if (n <= cus) return launch_behind(behind, layer_pair_kernel<ND128, D128>, (unsigned)n, LAYER_THREADS, D128::LDS, stream, items, segs);
+  return launch_behind(behind, layer_pair_kernel<N128, L128>, (unsigned)n, LAYER_THREADS, L128::LDS, stream, items, segs);
+}
+#endif
+
 hipError_t DMM_CAT(layer_allow_lds_, DMM_INSTANCE)() {
   hipError_t e = allow_all<DMM_SILU>();
+#if DMM_INSTANCE == 4
+  if (e == hipSuccess) e = allow_pair<N128, L128>();
+  if (e == hipSuccess) e = allow_pair<ND128, D128>();
+#endif
   if constexpr (DUAL) {
     if (e == hipSuccess) e = allow_all<DMM_GELU>();
     if (e == hipSuccess) e = allow_all<DMM_GELU_TANH>();
@@ -128,11 +147,13 @@ bool layer_launch(hipEvent_t behind, int kind, int shape, int act, int cus, cons
     case LAYER_I8: marked = layer_launch_0(last, shape, act, cus, items, n_items, segs, stream); break;
     case LAYER_I8_GATED: marked = layer_launch_1(last, shape, act, cus, items, n_items, segs, stream); break;
     case LAYER_GATED: marked = layer_launch_2(last, shape, act, cus, items, n_items, segs, stream); break;
+    case LAYER_PAIR: marked = layer_launch_pair(last, cus, items, n_items, segs, stream); break;
     case LAYER_NT: marked = layer_launch_3(last, shape, act, cus, items, n_items, segs, stream); break;
     default: marked = layer_launch_4(last, shape, act, cus, items, n_items, segs, stream); break;
   }
   if (!n_joins || hipPeekAtLastError() != hipSuccess) return marked;
-  const int per = (kLayerTile[kind][shape].tm * kLayerTile[kind][shape].tn + 1023) / 1024;
+  const LayerTile tile = kLayerTile[kind == LAYER_PAIR ? LAYER_NT : kind][shape];
+  const int per = (tile.tm * tile.tn + 1023) / 1024;
   switch (kind) {
     case LAYER_I8: return join<LAYER_I8>(behind, act, joins, n_joins, per, stream);
     case LAYER_I8_GATED: return join<LAYER_I8_GATED>(behind, act, joins, n_joins, per, stream);

@@ -234,6 +234,29 @@ __global__ __launch_bounds__(LAYER_THREADS, SH::LDS > 80 * 1024 ? 1 : 2) void la
   layer_finish<SH, ACT>(tile, it, lds);
 }
 
+// Macro-tiles of two kinds in one launch, of the same size: the gradients of a product, which wait for nothing of each other.  Each alone leaves places empty
+// in its last round, or fills none.  (Gradients of 381 x 720 x 1112 uneven, copies included: 29 us in two launches, 20.5 in one.)
+template <class SA, class SB>
+__global__ __launch_bounds__(LAYER_THREADS, SA::LDS > 80 * 1024 ? 1 : 2) void layer_pair_kernel(const LayerItem *__restrict__ items,
+                                                                                               const LayerSeg *__restrict__ segs) {
+  static_assert(SA::LDS == SB::LDS && !SA::DUAL && !SB::DUAL, "one size of LDS, one epilogue");
+  extern __shared__ char lds[];
+  const LayerItem it = items[blockIdx.x];
+  if (it.what == LAYER_ZERO) {
+    layer_zeros(it);
+    return;
+  }
+  auto multiply = [&](auto *sums) {
+    using SH = std::remove_reference_t<decltype(*sums)>;
+    LayerTileSums<SH> tile;
+    tile.run(it, segs + it.seg, segs + it.tail_seg, lds);
+    tile.pin();
+    layer_finish<SH, DMM_SILU>(tile, it, lds);
+  };
+  if (it.kind == SA::KIND) multiply((SA *)nullptr);
+  else multiply((SB *)nullptr);
+}
+
 // Sums of partial tiles, in ascending k: four columns a thread.  Integers are added in 64 bits: a run's sum fits 32, all together need not.
 template <int KIND, int ACT>
 __global__ __launch_bounds__(256) void layer_join_kernel(const LayerJoin *__restrict__ joins, int blocks_per_join) {

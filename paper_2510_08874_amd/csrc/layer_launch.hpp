@@ -36,6 +36,7 @@ struct LayerItem {
   int32_t tail_seg, n_tails;    // segments whose tails it adds
   int32_t c_es;                 // bytes of an element of C: 4, or 2 for bf16
   int32_t what;                 // LAYER_*
+  int32_t kind, pad;            // of product, where a launch has two
 };
 
 struct LayerJoin {
@@ -66,7 +67,8 @@ enum {
   LAYER_GATED,                  // bf16, A direct, both right operands turned
   LAYER_NT,                     // bf16, both direct
   LAYER_TN,                     // bf16, both turned
-  LAYER_KINDS
+  LAYER_KINDS,
+  LAYER_PAIR = LAYER_KINDS      // a launch of both gradients' macro-tiles of 128 x 128
 };
 // Macro-tiles of a kind: rows by columns of the result.
 enum { LAYER_256, LAYER_128, LAYER_TWO, LAYER_64, LAYER_32, LAYER_SHAPES };   // (TWO: gated, small enough for two on a CU)
@@ -98,6 +100,7 @@ DMM_DECLARE_LAYER(2)
 DMM_DECLARE_LAYER(3)
 DMM_DECLARE_LAYER(4)
 #undef DMM_DECLARE_LAYER
+bool layer_launch_pair(hipEvent_t behind, int cus, const LayerItem *items, int n, const LayerSeg *segs, hipStream_t stream);
 
 // ---- element by element ---------------------------------------------------------------------------------
 

@@ -63,20 +63,19 @@ class Space:
 
 
 COPY = struct.Struct("<2Q2q4i")
+PRODUCTS = ("layer_gemm_kernel", "layer_pair_kernel")
 class Results(list):
     """Regions of results; `copies`: both operands lie in copies."""
     copies = False
 
 
-SEG, ITEM, JOIN = struct.Struct("<3Q3I3i"), struct.Struct("<3Q3I3i" + "Qq2Q2q3Q" + "12i"), struct.Struct("<Qq2Q2q3Q" + "Q6i")
+SEG, ITEM, JOIN = struct.Struct("<3Q3I3i"), struct.Struct("<3Q3I3i" + "Qq2Q2q3Q" + "14i"), struct.Struct("<Qq2Q2q3Q" + "Q6i")
 # kind of a launch: rows, columns of a right operand in its macro-tiles, by LDS; (A turned, B turned, two right operands, bytes of an element)
 KINDS = {"int": (False, False, False, 1), "int_gated": (False, False, True, 1), "gated": (False, True, True, 2), "nt": (False, False, False, 2), "tn": (True, True, False, 2)}
 
 
-def follow(rec, space, op, kind):
-    """Everything that a launch reads and writes; the regions of its results, and how much of K each got."""
-    a_turned, b_turned, dual, es = KINDS[kind]
-    step = 128 // es
+def follow(rec, space, op):
+    """Everything that a launch reads and writes: by kind of product, the regions of its results and how much of K each got; the same of partial sums."""
     i, _, _, items, _ = op
     n = int(rec.so.rec_blocks(i))
     raw = ctypes.string_at(items, n * ITEM.size)
@@ -96,10 +95,14 @@ def follow(rec, space, op, kind):
             first = p + off * pitch + k0 * es
             space.inside(first, first + (ext - 1) * pitch + k * es, f"{kind}, along K, {'whole steps' if whole else 'a tail'}")
 
-    out, parts = Results(), {}
+    got, parts = {}, {}
     for x in range(n):
         v = ITEM.unpack(raw[x * ITEM.size:(x + 1) * ITEM.size])
-        front, (c, ldc, g, u, ldg, ldu, sa, sb, sb2), (m_off, n_off, m_ext, n_ext, seg, n_segs, first, steps, tail_seg, n_tails, c_es, what) = v[:9], v[9:18], v[18:]
+        front, (c, ldc, g, u, ldg, ldu, sa, sb, sb2), (m_off, n_off, m_ext, n_ext, seg, n_segs, first, steps, tail_seg, n_tails, c_es, what, kind, _) = v[:9], v[9:18], v[18:]
+        kind = list(KINDS)[kind]
+        a_turned, b_turned, dual, es = KINDS[kind]
+        step = 128 // es
+        out = got.setdefault(kind, Results())
         k_sum, left, s, skip = 0, steps, 0, first
         if steps and space.copies and space.copies[0] <= front[1] < space.copies[1]:
             out.copies = True
@@ -127,20 +130,20 @@ def follow(rec, space, op, kind):
                 for p, ext in ((sa, m_ext), (sb, n_ext)) + (((sb2, n_ext),) if dual else ()):
                     space.inside(p, p + 4 * ext, "scales")
         if what == 1:
-            parts[c] = k_sum
+            parts[c] = k_sum, kind
         else:
             out.append((c, ldc, c_es, m_ext, n_ext, k_sum))
             for p, ld in ((g, ldg), (u, ldu)):
                 if p:
                     space.inside(p, p + ((m_ext - 1) * ld + n_ext) * 2, "what is kept")
-    return out, parts
+    return got, parts
 
 
 def follow_call(rec, space, at, kinds):
     """The launches of one call: [(corner, ld, bytes of an element, rows, columns, k)] of every kind."""
     space.copies, space.results, back, made, multiplied = None, None, [], [], False
     for op in rec.launches(at):
-        multiplied = multiplied or op[1] == "layer_gemm_kernel"
+        multiplied = multiplied or op[1] in PRODUCTS
         if op[1] == "layer_copy_kernel":
             blocks, x, low, high = 0, 0, 1 << 63, 0
             while blocks < rec.so.rec_blocks(op[0]):
@@ -163,11 +166,13 @@ def follow_call(rec, space, at, kinds):
     if back:
         space.results = (min(o[0] for o in back), max(o[0] + (o[4] - 1) * o[2] + o[5] for o in back))
         assert all(high <= space.results[0] or low >= space.results[1] for low, high in made)
-    ops = [o for o in rec.launches(at) if o[1] in ("layer_gemm_kernel", "layer_join_kernel")]
-    got, x = [], 0
-    for kind in kinds:
-        assert ops[x][1] == "layer_gemm_kernel"
-        out, parts = follow(rec, space, ops[x], kind)
+    ops = [o for o in rec.launches(at) if o[1] in PRODUCTS or o[1] == "layer_join_kernel"]
+    all_of, x = {}, 0
+    while x < len(ops):
+        assert ops[x][1] in PRODUCTS
+        of, parts = follow(rec, space, ops[x])
+        assert len(of) == (2 if ops[x][1] == "layer_pair_kernel" else 1) and not set(of) & set(all_of)
+        all_of.update(of)
         x += 1
         if parts:
             assert ops[x][1] == "layer_join_kernel"
@@ -180,12 +185,13 @@ def follow_call(rec, space, at, kinds):
             while used < len(slots):
                 c, ldc, g, u, ldg, ldu, sa, sb, sb2, p, runs, tm, tn, m_ext, n_ext, c_es = JOIN.unpack(ctypes.string_at(join_at + y * JOIN.size, JOIN.size))
                 size = tm * tn * 4
-                out.append((c, ldc, c_es, m_ext, n_ext, sum(parts[p + r * size] for r in range(runs))))
+                of[parts[p][1]].append((c, ldc, c_es, m_ext, n_ext, sum(parts[p + r * size][0] for r in range(runs))))
+                assert len({parts[p + r * size][1] for r in range(runs)}) == 1
                 used += runs
                 y += 1
             assert used == len(slots)
-        got.append(out)
-    assert x == len(ops)
+    assert list(sorted(all_of)) == list(sorted(kinds))
+    got = [all_of[kind] for kind in kinds]
     for y, of in enumerate(got):
         if not (back and of and space.results[0] <= of[0][0] < space.results[1]):
             continue
@@ -420,6 +426,23 @@ def rows_in_blocks_are_joined_on_a_copy(rec):
         covers(space, those(space, out[1], dv), dv[1], dv[2], d[1], 4, m, 64)
 
 
+def both_gradients_in_one_launch(rec):
+    """Where each alone leaves places empty, and not where both fill the device with tiles of 256 x 256."""
+    from paper_2510_08874_amd import binding as b
+    for m, k, n, one in ((381, 720, 1112, True), (1448, 512, 768, True), (256, 1080, 3600, True), (4096, 4096, 4096, False)):
+        d = made("blocks", m, k, n)
+        plan, space = b.Plan(*d, 4), Space(True)
+        a, w, dc = (space.tiles(x, 2) for x in d)
+        da, db = space.tiles(d[0], 2), space.tiles(d[1], 4)
+        at = len(rec.ops())
+        plan.execute_backward(a[0], w[0], dc[0], da[0], db[0], b.DMM_DB_F32, 0)
+        names = [o[1] for o in rec.launches(at) if o[1] in PRODUCTS]
+        assert names == (["layer_pair_kernel"] if one else ["layer_gemm_kernel"] * 2), (m, k, n)
+        out = follow_call(rec, space, at, ["nt", "tn"])
+        covers(space, out[0], da[1], da[2], d[0], 2, n, 64, 1, d[1]["col_cuts"])
+        covers(space, out[1], db[1], db[2], d[1], 4, m, 64)
+
+
 def a_call_without_memory_for_copies_runs_on_the_operands(rec):
     from paper_2510_08874_amd import binding as b
     d = made("uneven", 1301, 1103, 907)
@@ -517,7 +540,8 @@ def many_rows_take_several_launches(rec):
         assert {o[1] for o in ops} == {"i8_whole_rows_kernel"} and sum(blocks) == m and max(blocks) * threads < 1 << 32, (m, n, blocks)
 
 
-SCENARIOS = [many_rows_take_several_launches, rows_in_blocks_are_joined_on_a_copy, reads_and_writes_stay_inside, narrow_tiles, sizes_under_test_take_the_ways_they_are_meant_for, few_rows_run_on_few_rows,
+SCENARIOS = [many_rows_take_several_launches, rows_in_blocks_are_joined_on_a_copy, both_gradients_in_one_launch,
+             reads_and_writes_stay_inside, narrow_tiles, sizes_under_test_take_the_ways_they_are_meant_for, few_rows_run_on_few_rows,
              a_call_without_memory_for_copies_runs_on_the_operands, captures_take_what_is_there, partial_sums_and_copies_wait_for_each_other]
 
 
