@@ -1145,8 +1145,8 @@ int over_scales(const Grid &G, const dmm_int_tiles *q, bool by_cols, int what, h
   return flush();
 }
 
-// One form.  Along the rows, a workgroup takes a whole row where it meets few tiles and rows are many or short; otherwise, and along the columns, the
-// largest magnitudes are collected block by block first.
+// One form.  Along the rows, a workgroup takes a whole row where it meets few tiles and rows are many or short; along the columns, a block where
+// there are no more rows than it has; otherwise the largest magnitudes are collected block by block first.
 int i8_form(const Grid &G, int dtype, char *const *x, const int64_t *x_ld, const dmm_int_tiles *q, bool by_cols, hipStream_t stream) {
   const int es = dtype == DMM_F32 ? 4 : 2;
   const bool f32 = es == 4;
@@ -1184,6 +1184,8 @@ int i8_form(const Grid &G, int dtype, char *const *x, const int64_t *x_ld, const
       }
     return DMM_OK;
   }
+  if (by_cols && merged_cuts({&G.rc}).size() == 2 && G.rows <= 128)
+    return over_i8_tiles(G, es, x, x_ld, q, true, 128, i8_block_cols(f32), [&](const I8Args &args, int blocks) { i8_whole_cols_launch(args, blocks, f32, stream); });
   if ((rc = over_scales(G, q, by_cols, I8_CLEAR, stream))) return rc;
   if ((rc = over_i8_tiles(G, es, x, x_ld, q, by_cols, 128, i8_block_cols(f32),
                           [&](const I8Args &args, int blocks) { i8_amax_launch(args, blocks, f32, by_cols, stream); })))

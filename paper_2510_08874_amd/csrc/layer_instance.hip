@@ -176,8 +176,13 @@ void i8_amax_launch(const I8Args &args, int blocks, bool f32, bool cols, hipStre
 }
 void i8_quantize_launch(const I8Args &args, int blocks, bool f32, bool cols, hipStream_t stream) {
   const dim3 grid((unsigned)blocks), block(256);
-  if (f32) cols ? i8_cols_kernel<true><<<grid, block, 0, stream>>>(args) : i8_rows_kernel<true><<<grid, block, 0, stream>>>(args);
-  else cols ? i8_cols_kernel<false><<<grid, block, 0, stream>>>(args) : i8_rows_kernel<false><<<grid, block, 0, stream>>>(args);
+  if (f32) cols ? i8_cols_kernel<true, false><<<grid, block, 0, stream>>>(args) : i8_rows_kernel<true><<<grid, block, 0, stream>>>(args);
+  else cols ? i8_cols_kernel<false, false><<<grid, block, 0, stream>>>(args) : i8_rows_kernel<false><<<grid, block, 0, stream>>>(args);
+}
+void i8_whole_cols_launch(const I8Args &args, int blocks, bool f32, hipStream_t stream) {
+  const dim3 grid((unsigned)blocks), block(256);
+  if (f32) i8_cols_kernel<true, true><<<grid, block, 0, stream>>>(args);
+  else i8_cols_kernel<false, true><<<grid, block, 0, stream>>>(args);
 }
 void i8_values_launch(const I8Args &args, int blocks, bool f32, bool cols, hipStream_t stream) {
   const dim3 grid((unsigned)blocks), block(256);

@@ -166,6 +166,7 @@ constexpr int i8_block_cols(bool f32) { return f32 ? 64 : 128; }
 void i8_amax_launch(const I8Args &args, int blocks, bool f32, bool cols, hipStream_t stream);
 void i8_quantize_launch(const I8Args &args, int blocks, bool f32, bool cols, hipStream_t stream);
 void i8_values_launch(const I8Args &args, int blocks, bool f32, bool cols, hipStream_t stream);
+void i8_whole_cols_launch(const I8Args &args, int blocks, bool f32, hipStream_t stream);   // columns of no more rows than a block has
 void i8_whole_rows_launch(const I8RowArgs &args, int threads, bool f32, hipStream_t stream);
 
 }  // namespace dmm
