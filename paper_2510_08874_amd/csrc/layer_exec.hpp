@@ -7,7 +7,7 @@ namespace dmm {
 namespace {
 
 constexpr int64_t kLayerBlocks = (1 << 24) - 1;                // workgroups of a launch: 2^32 threads are too many
-constexpr int kLayerManyRows = 1024;                           // rows that fill the device with small workgroups
+constexpr int64_t kLayerManyRows = 1024;                           // rows that fill the device with small workgroups
 constexpr int64_t kLayerPitch = (int64_t)1 << 24;              // bytes from row to row
 constexpr int64_t kLayerRows = 0x7fff0000;                     // kernels count rows and columns in 32 bits, a workgroup's past the last among them
 constexpr int64_t kLayerSum = 131071;                          // products of two bytes that an int32 sum holds whatever they are
@@ -1151,38 +1151,47 @@ int i8_form(const Grid &G, int dtype, char *const *x, const int64_t *x_ld, const
   const int es = dtype == DMM_F32 ? 4 : 2;
   const bool f32 = es == 4;
   int rc;
-  if (!by_cols && G.gc <= I8_ROW_PIECES && G.cols <= kLayerRows) {
+  if (!by_cols && G.gc <= I8_ROW_CUTS && G.cols <= kLayerRows) {
+    I8RowArgs args;
+    std::memset(&args, 0, sizeof args);
+    for (int32_t tj = 0; tj < G.gc; ++tj) {
+      const int64_t w = G.cc[(size_t)tj + 1] - G.cc[(size_t)tj];
+      args.n += w > 0;
+      args.vectors += (int32_t)((w + 7) / 8);
+    }
+    int64_t blocks = 0;
+    auto flush = [&]() -> int {
+      if (!blocks) return DMM_OK;
+      // (few rows: a vector a thread; many: I8_ROW_KEPT, and more rows on a CU at a time)
+      const int per = blocks < kLayerManyRows ? 1 : I8_ROW_KEPT;
+      i8_whole_rows_launch(args, (int)blocks, (int)std::min<int64_t>(I8_ROW_THREADS, up_to(std::max(args.vectors / per, 1), 64)), f32, stream);
+      args.groups = 0;
+      blocks = 0;
+      DMM_HIP(hipGetLastError());
+      return DMM_OK;
+    };
+    const int64_t most = ((int64_t)1 << 32) / I8_ROW_THREADS - 1;   // (a launch has less than 2^32 threads)
     for (int32_t rep = 0; rep < G.c; ++rep)
       for (int32_t ti = 0; ti < G.gr; ++ti) {
-        I8RowArgs args;
-        std::memset(&args, 0, sizeof args);
-        args.h = (int32_t)(G.rc[(size_t)ti + 1] - G.rc[(size_t)ti]);
-        if (args.h <= 0) continue;
-        args.scale = q->scales[(int64_t)rep * G.gr + ti];
-        for (int32_t tj = 0; tj < G.gc; ++tj) {
-          const int64_t w = G.cc[(size_t)tj + 1] - G.cc[(size_t)tj], i = G.table_index(rep, ti, tj);
-          if (w <= 0) continue;
-          args.piece[args.n++] = {x[i], (char *)q->codes[i], x_ld[i] * es, q->code_ld[i], (int32_t)w, args.vectors};
-          args.vectors += (int32_t)((w + 7) / 8);
-        }
-        // (few rows: a vector a thread; many: I8_ROW_KEPT, and more rows on a CU at a time)
-        const int per = args.h < kLayerManyRows ? 1 : I8_ROW_KEPT;
-        const int threads = (int)std::min<int64_t>(I8_ROW_THREADS, up_to(std::max(args.vectors / per, 1), 64));
-        // (rows past the 2^32 threads that a launch can have go into the next)
-        const int64_t all = args.h, most = ((int64_t)1 << 32) / threads - 1;
-        for (int64_t at = 0; at < all; at += most) {
-          I8RowArgs part = args;
-          part.h = (int32_t)std::min(all - at, most);
-          part.scale += at;
-          for (int32_t p = 0; p < part.n; ++p) {
-            part.piece[p].x += at * part.piece[p].x_pitch;
-            part.piece[p].q += at * part.piece[p].q_pitch;
+        const int64_t all = G.rc[(size_t)ti + 1] - G.rc[(size_t)ti];
+        for (int64_t at = 0; at < all;) {
+          if ((args.groups == I8_ROW_GROUPS || (args.groups + 1) * args.n > I8_ROW_PIECES || blocks == most) && (rc = flush())) return rc;
+          const int64_t h = std::min(all - at, most - blocks);
+          I8RowPiece *piece = args.piece + args.groups * args.n;
+          args.group[args.groups] = {q->scales[(int64_t)rep * G.gr + ti] + at, (int32_t)blocks, args.groups * args.n};
+          int32_t first = 0;
+          for (int32_t tj = 0; tj < G.gc; ++tj) {
+            const int64_t w = G.cc[(size_t)tj + 1] - G.cc[(size_t)tj], i = G.table_index(rep, ti, tj);
+            if (w <= 0) continue;
+            *piece++ = {x[i] + at * x_ld[i] * es, (char *)q->codes[i] + at * q->code_ld[i], x_ld[i] * es, q->code_ld[i], (int32_t)w, first};
+            first += (int32_t)((w + 7) / 8);
           }
-          i8_whole_rows_launch(part, threads, f32, stream);
-          DMM_HIP(hipGetLastError());
+          ++args.groups;
+          blocks += h;
+          at += h;
         }
       }
-    return DMM_OK;
+    return flush();
   }
   if (by_cols && merged_cuts({&G.rc}).size() == 2 && G.rows <= 128)
     return over_i8_tiles(G, es, x, x_ld, q, true, 128, i8_block_cols(f32), [&](const I8Args &args, int blocks) { i8_whole_cols_launch(args, blocks, f32, stream); });

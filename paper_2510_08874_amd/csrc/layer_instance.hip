@@ -189,10 +189,15 @@ void i8_values_launch(const I8Args &args, int blocks, bool f32, bool cols, hipSt
   if (f32) cols ? i8_col_values_kernel<true><<<grid, block, 0, stream>>>(args) : i8_row_values_kernel<true><<<grid, block, 0, stream>>>(args);
   else cols ? i8_col_values_kernel<false><<<grid, block, 0, stream>>>(args) : i8_row_values_kernel<false><<<grid, block, 0, stream>>>(args);
 }
-void i8_whole_rows_launch(const I8RowArgs &args, int threads, bool f32, hipStream_t stream) {
-  const dim3 grid((unsigned)args.h), block((unsigned)threads);
-  if (f32) args.n > 1 ? i8_whole_rows_kernel<true, true><<<grid, block, 0, stream>>>(args) : i8_whole_rows_kernel<true, false><<<grid, block, 0, stream>>>(args);
-  else args.n > 1 ? i8_whole_rows_kernel<false, true><<<grid, block, 0, stream>>>(args) : i8_whole_rows_kernel<false, false><<<grid, block, 0, stream>>>(args);
+template <bool F32>
+static void whole_rows(const I8RowArgs &args, const dim3 &grid, const dim3 &block, hipStream_t stream) {
+  if (args.groups > 1) args.n > 1 ? i8_whole_rows_kernel<F32, true, true><<<grid, block, 0, stream>>>(args) : i8_whole_rows_kernel<F32, false, true><<<grid, block, 0, stream>>>(args);
+  else args.n > 1 ? i8_whole_rows_kernel<F32, true, false><<<grid, block, 0, stream>>>(args) : i8_whole_rows_kernel<F32, false, false><<<grid, block, 0, stream>>>(args);
+}
+void i8_whole_rows_launch(const I8RowArgs &args, int blocks, int threads, bool f32, hipStream_t stream) {
+  const dim3 grid((unsigned)blocks), block((unsigned)threads);
+  if (f32) whole_rows<true>(args, grid, block, stream);
+  else whole_rows<false>(args, grid, block, stream);
 }
 
 #endif

@@ -145,18 +145,23 @@ struct I8ScaleArgs {
   int32_t n, pad;
   I8Scales piece[I8_PIECES];
 };
-// A row of tiles whose rows are quantised whole.
+// A tile of such a row of tiles.
 struct I8RowPiece {
   const char *x;
   char *q;
   int64_t x_pitch, q_pitch;
   int32_t w, first;              // columns; vectors of eight of the tiles in front
 };
-constexpr int I8_ROW_PIECES = 32, I8_ROW_THREADS = 1024, I8_ROW_KEPT = 4;
-struct I8RowArgs {
+// A row of tiles whose rows are quantised whole: its tiles are I8RowArgs::piece[first_piece ...], n of them.
+struct I8RowGroup {
   float *scale;
-  int32_t h, n;
-  int32_t vectors, pad;          // of all tiles
+  int32_t first_block, first_piece;
+};
+constexpr int I8_ROW_GROUPS = 24, I8_ROW_PIECES = 64, I8_ROW_CUTS = 32, I8_ROW_THREADS = 1024, I8_ROW_KEPT = 4;
+struct I8RowArgs {
+  int32_t groups, n;
+  int32_t vectors, pad;          // of a row
+  I8RowGroup group[I8_ROW_GROUPS];
   I8RowPiece piece[I8_ROW_PIECES];
 };
 enum { I8_CLEAR, I8_FINISH };
@@ -167,6 +172,6 @@ void i8_amax_launch(const I8Args &args, int blocks, bool f32, bool cols, hipStre
 void i8_quantize_launch(const I8Args &args, int blocks, bool f32, bool cols, hipStream_t stream);
 void i8_values_launch(const I8Args &args, int blocks, bool f32, bool cols, hipStream_t stream);
 void i8_whole_cols_launch(const I8Args &args, int blocks, bool f32, hipStream_t stream);   // columns of no more rows than a block has
-void i8_whole_rows_launch(const I8RowArgs &args, int threads, bool f32, hipStream_t stream);
+void i8_whole_rows_launch(const I8RowArgs &args, int blocks, int threads, bool f32, hipStream_t stream);
 
 }  // namespace dmm

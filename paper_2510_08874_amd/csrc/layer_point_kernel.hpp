@@ -445,31 +445,33 @@ __global__ __launch_bounds__(256) void i8_cols_kernel(I8Args) {
   }
 }
 
-// The rows of a row of tiles, a workgroup each, scales and integers.  The vectors of eight elements of all tiles are counted through, so that every thread has
+// Rows over all tiles that they are cut into, a workgroup each, scales and integers.  The vectors of eight elements of all tiles are counted through, so that every thread has
 // its own on their way at once whatever the tiles' widths, and the first I8_ROW_KEPT of each thread stay in registers between the two passes over a row.  (16
 // rows of 8192: 256 threads with four vectors each 7 us, 1024 threads 4.3; 115 x 715 in eight tiles, and back, 22 us
 // one tile after the other, now 11.  4096 x 8192, and back: 36 us with 256 threads and four vectors each, 50 with 1024 and one.)
-// CUT: several tiles (without, the one tile's numbers stay in scalar registers).
-template <bool F32, bool CUT>
+// CUT: several tiles side by side, MANY: several rows of tiles (without, there is no search, and the one tile's numbers stay in scalar registers).
+template <bool F32, bool CUT, bool MANY>
 __global__ __launch_bounds__(I8_ROW_THREADS) void i8_whole_rows_kernel(I8RowArgs) {
   __shared__ unsigned tops[I8_ROW_THREADS / 64];
-  __shared__ int firsts[I8_ROW_PIECES];
+  __shared__ int firsts[I8_ROW_CUTS];
   const auto &args = *(const I8RowArgs *)__builtin_amdgcn_kernarg_segment_ptr();
-  const int row = blockIdx.x, tid = threadIdx.x, threads = blockDim.x;
+  const I8RowGroup &group = args.group[MANY ? layer_last(args.group, args.groups, (int)blockIdx.x) : 0];
+  const I8RowPiece *const pieces = args.piece + (MANY ? group.first_piece : 0);
+  const int row = (int)blockIdx.x - (MANY ? group.first_block : 0), tid = threadIdx.x, threads = blockDim.x;
   if constexpr (CUT) {
-    if (tid < args.n) firsts[tid] = args.piece[tid].first;
+    if (tid < args.n) firsts[tid] = pieces[tid].first;
     __syncthreads();
   }
   // the tile of vector `at`
   auto piece_of = [&](int at) -> const I8RowPiece & {
-    if constexpr (!CUT) return args.piece[0];
+    if constexpr (!CUT) return pieces[0];
     int lo = 0, hi = args.n - 1;
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
       if (firsts[mid] <= at) lo = mid;
       else hi = mid - 1;
     }
-    return args.piece[lo];
+    return pieces[lo];
   };
   auto load = [&](int at) {
     const I8RowPiece &P = piece_of(at);
@@ -490,7 +492,7 @@ __global__ __launch_bounds__(I8_ROW_THREADS) void i8_whole_rows_kernel(I8RowArgs
   __syncthreads();
   m = 0;
   for (int x = 0; x < threads / 64; ++x) m = max(m, tops[x]);
-  if (tid == 0) args.scale[row] = i8_scale(m);
+  if (tid == 0) group.scale[row] = i8_scale(m);
   const I8Row r = i8_row(m);
   auto codes = [&](int at, const LayerVec<F32> &v) {
     const I8RowPiece &P = piece_of(at);

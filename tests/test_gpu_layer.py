@@ -51,7 +51,7 @@ def quantized(X, axis):
 
 
 GRIDS = [(1, 1, None), (1, 7, None), (3, 130, None), (5, 1000, (2, 3)), (129, 257, (3, 4)), (64, 16384, None), (33, 20001, (1, 2)), (257, 96, (4, 1)), (700, 513, (2, 40)),
-         (200, 4100, (3, 3)), (1500, 700, (1, 5)), (1030, 41001, (1, 3)), (40, 70001, None)]
+         (200, 4100, (3, 3)), (1500, 700, (1, 5)), (1030, 41001, (1, 3)), (40, 70001, None), (200, 300, (30, 2)), (90, 500, (5, 31))]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
