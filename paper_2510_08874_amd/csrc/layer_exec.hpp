@@ -242,7 +242,7 @@ struct LayerCopies {
   bool possible() const;
 };
 constexpr double kTail = 5;                                    // us, see choose_layer
-constexpr size_t kLayerCopies = (size_t)1 << 30;               // of a call
+constexpr size_t kLayerCopies = (size_t)1 << 30;               // of a product
 bool LayerCopies::possible() const { return fits && size <= kLayerCopies && blocks <= kLayerBlocks && back_blocks <= kLayerBlocks; }
 
 
