@@ -406,8 +406,8 @@ int dmm_int_dequantize(const dmm_matrix_desc *X, const dmm_int_tiles *q, int alo
  * parts, and one part may meet so many at most (DMM_ELIMIT where thousands of cuts of k leave nothing longer than 127).  Replicas of A and B are taken to be
  * copies of each other: which of them an element and its scale are read from is not said.
  * Operands whose rows are misaligned or finely cut may be copied to dense rows first, into the plan's scratch memory, and results may come through it (at most
- * 1 GiB for each product of a call; without so much the call runs on the operands).  Whether they are is decided from cuts, leading dimensions and addresses; integer sums do not depend on it, those of bf16 in the
- * calls below are rounded in another order on copies.
+ * 1 GiB for each product of a call; without so much the call runs on the operands).  Whether they are is decided from cuts, leading dimensions
+ * and addresses; integer sums do not depend on it, those of bf16 in the calls below are rounded in another order on copies.
  * Replicas of C, streams, ownership and captures as for dmm_mx_execute; the plan's tables and scratch memory for this entry point are its own.  (With
  * copies or partial sums a call waits for the plan's calls before it, on whichever stream.)  dmm_plan_last_execute, dmm_plan_last_kernels and
  * the elapsed times do not speak of these calls, of the gated block's or of the gradients'. */
