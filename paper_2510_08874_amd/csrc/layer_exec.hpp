@@ -101,11 +101,12 @@ void put_segment(LayerWork *W, LayerSeg s, int64_t len, int64_t guard) {
     s.tail = (int32_t)step;
     W->segs.push_back(s);
     if (tail == 0) return;
-    auto on = [&](const char *p, uint32_t pitch, bool turned) { return p ? p + (turned ? steps * step * (int64_t)pitch : steps * 128) : p; };
+    // (an operand on a copy is named by its place, which may be 0)
+    auto on = [&](const char *p, uint32_t pitch, bool turned) { return (const char *)((uintptr_t)p + (uintptr_t)(turned ? steps * step * (int64_t)pitch : steps * 128)); };
     const bool bt = W->kind == LAYER_TN || W->kind == LAYER_GATED;
     s.a = on(s.a, s.a_pitch, W->kind == LAYER_TN);
     s.b = on(s.b, s.b_pitch, bt);
-    s.b2 = on(s.b2, s.b2_pitch, bt);
+    if (layer_gated(W->kind)) s.b2 = on(s.b2, s.b2_pitch, bt);
     steps = 0;
   }
   s.steps = (int32_t)steps;

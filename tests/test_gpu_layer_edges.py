@@ -1,0 +1,32 @@
+"""GPU tests of the layers around a product at the edges of what their calls allow.  Limits as in test_gpu_layer.py."""
+import pytest
+
+import workloads
+from tests.layer_tiles import ACTS, Tiles, act, normal, stream
+from tests.test_gpu_layer import H, TINY, close, gated_error, sum_error
+
+torch = pytest.importorskip("torch")
+binding = pytest.importorskip("paper_2510_08874_amd.binding")
+pytestmark = pytest.mark.gpu
+BF16 = torch.bfloat16
+
+
+@pytest.mark.parametrize("name", list(ACTS))
+@pytest.mark.parametrize("m,blocks,k,n,last", [(8, 8, 4097, 8195, 3), (8, 1, 4098, 8194, 2), (8, 2, 4102, 8193, 1), (64, 8, 8193, 8195, 3)], ids=str)
+def test_narrow_tiles_of_weights_behind_a_copy_of_the_rows(m, blocks, k, n, last, name):
+    """The weights' last tile has one to three columns: rows that whole steps leave out are multiplied behind these, with the copy's columns there."""
+    da, db, dc = workloads.block_desc(m, k, 8, 1), workloads.desc(k, n, [0, k], [0, n - last, n], 1, 2), workloads.block_desc(m, n, blocks, 1)
+    plan = binding.Plan(da, db, dc, 8)
+    A, Wg, Wu = normal(m, k, 1), normal(k, n, 2, 2 * k ** -0.5), normal(k, n, 3, k ** -0.5)
+    g, u = A.double() @ Wg.double(), A.double() @ Wu.double()
+    eg, eu = sum_error(A.double(), Wg.double()), sum_error(A.double(), Wu.double())
+    want = act(g, name)[0] * u
+    a, wg, wu = (Tiles(d, BF16, x) for d, x in ((da, A), (db, Wg), (db, Wu)))
+    h, kg, ku = (Tiles(dc, BF16) for _ in range(3))
+    plan.gated(ACTS[name], *(t.table() for t in (a, wg, wu, h, kg, ku)), stream=stream())
+    torch.cuda.synchronize()
+    close(kg.whole(), g, H * g.abs() + (1 + H) * eg, "G")
+    close(ku.whole(), u, H * u.abs() + (1 + H) * eu, "U")
+    close(h.whole(), want, H * want.abs() + (1 + H) * gated_error(g, u, eg, eu, name) + TINY, "H")
+    for t in (h, kg, ku):
+        t.check_guards()
