@@ -3,6 +3,7 @@ in a process of its own.  Each address that a work table names, in a tile or in 
 operands of a product have to be at the same k, and every k of a result counts once."""
 import ctypes
 import os
+import random
 import subprocess
 import sys
 
@@ -15,7 +16,7 @@ if ROOT not in sys.path:
 
 import workloads  # noqa: E402
 from tests.test_host_calls import Recorder, recorder  # noqa: E402, F401
-from tests.test_host_layer import COPY, ITEM, JOIN, KINDS, PRODUCTS, SEG, Space, bounds  # noqa: E402
+from tests.test_host_layer import COPY, ITEM, JOIN, KINDS, PRODUCTS, SEG, Space, bounds, layouts, made  # noqa: E402
 
 ZERO = -1                                                      # where a copy was filled up
 STORE, PARTS, NOTHING = range(3)                               # what becomes of a macro-tile (NOTHING: zeros, there is no k)
@@ -271,6 +272,23 @@ def every_call(rec, d, ranks, more=0, aligned=False, integers=True, gated=True, 
     return out
 
 
+def operands_meet_at_the_same_k(rec):
+    """Random sizes, cuts and leading dimensions."""
+    rng = random.Random(23)
+    copied = 0
+    for turn in range(24):
+        m, k, n = (max(15, rng.choice((rng.randint(15, 300), rng.randint(15, 1200), 64 * rng.randint(1, 16)))) for _ in range(3))
+        if turn % 4 == 0:
+            m = rng.randint(15, 64)
+        d, ranks = layouts(rng, m, k, n)
+        copied += any(c.front for c in every_call(rec, d, ranks, rng.choice((0, 0, 1, 3, 8)), turn % 2 == 0))
+    assert copied > 5
+    every_call(rec, made("whole", 40, 140100, 30), 1, backward=False, gated=False)   # (integer sums in several runs)
+    every_call(rec, made("whole", 40, 8192, 300), 1)
+    every_call(rec, made("row_col", 9, 2000, 12001), 12)
+    every_call(rec, made("uneven", 1301, 1103, 907), 12)
+
+
 def narrow_tiles_of_weights_on_a_copy_of_the_rows(rec):
     """A weight's last tile has one to three columns, so that a read of eight runs over rows that whole steps do not have behind them, and these rows are
     multiplied behind the steps: with the left operand's columns there, in a copy as anywhere else."""
@@ -284,7 +302,7 @@ def narrow_tiles_of_weights_on_a_copy_of_the_rows(rec):
     assert took >= 8
 
 
-SCENARIOS = [narrow_tiles_of_weights_on_a_copy_of_the_rows]
+SCENARIOS = [operands_meet_at_the_same_k, narrow_tiles_of_weights_on_a_copy_of_the_rows]
 
 
 @pytest.mark.parametrize("scenario", [f.__name__ for f in SCENARIOS])
