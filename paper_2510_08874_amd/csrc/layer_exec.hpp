@@ -254,7 +254,8 @@ bool LayerCopies::possible() const { return fits && size <= kLayerCopies && bloc
 //   gated, bf16, 256 x 2048 x 2048       two on a CU 18.6, 128 x 128 24.6          1024 x 4096 x 4096    73 and 58
 //   8 bits, 2048^3                       128 x 128 13.4, 256 x 256 27.8            4096 x 4096 x 8192    136 and 117
 //   gated, bf16, 128 x 8192 x 4096       K in four runs 37, whole 64               1 x 8192 x 28672 in 8 bits: 43 and 36 (B is in a cache), whole
-LayerChoice choose_layer(const LayerWork &W, int cus) {
+// `fixed`: the runs are given, and a macro-tile is looked for.
+LayerChoice choose_layer(const LayerWork &W, int cus, int64_t fixed = 0) {
   const bool gated = layer_gated(W.kind);
   double cells = 0, k_steps = 0, k_tails = 0, b_once = 0;
   int64_t most = 0;
@@ -276,6 +277,7 @@ LayerChoice choose_layer(const LayerWork &W, int cus) {
   }
   const double steps = cells > 0 ? std::max(1.0, k_steps / cells) : 1, tails = cells > 0 ? k_tails / cells : 0;
   LayerChoice best;
+  best.runs = fixed ? fixed : 1;
   best.steps = steps;
   best.tails = tails;
   double best_us = 0;
@@ -295,9 +297,9 @@ LayerChoice choose_layer(const LayerWork &W, int cus) {
     const double down = strips * (double)W.rows / std::max(cells, 1.0);
     if (shape == LAYER_128) best.tiles = tiles;
     const double memory = 2.0 + b_once * (0.8 + 0.2 * down) / 5.4e6;
-    for (int64_t runs = 1; runs <= 32; ++runs) {
+    for (int64_t runs = fixed ? fixed : 1; runs <= (fixed ? fixed : 32); ++runs) {
       const double work = tiles * (double)runs, per = std::ceil(steps / (double)runs);
-      if (runs > 1 && (work > places || per < 3)) break;
+      if (!fixed && runs > 1 && (work > places || per < 3)) break;
       auto round = [&](double n) {
         if (n <= 0) return 0.0;
         const double full = n / cus, ends = kTail * tails / (double)runs;
@@ -515,10 +517,11 @@ void merge_pair(std::vector<char> *h, LayerLayout *L, bool second_first) {
 
 // The part of a call that all kinds have in common: the tables of the call before if they are of the same inputs (`key`), else new ones,
 // made from what `make` tells of each product (on the operands, or on copies; the first `lefts` products can be on copies of the left operand alone); then `in_front`, the launches and, where `reduce` asks for it, the sum of
-// C's replicas.
+// C's replicas.  `part`: the last product has one of two results that are cut alike.  Its runs of K, and whether it is on copies, are those that both
+// together are estimated to be best with (`make`'s last argument), so that its bits do not depend on the other's being asked for.
 template <class Make, class Front>
 int run_layer_on(dmm_plan_t *P, int which, const std::vector<char> &inputs, void *const *c_tiles, const int64_t *c_ld, bool reduce, hipStream_t stream, int products,
-              int lefts, Make make, Front in_front) {
+              int lefts, bool part, Make make, Front in_front) {
   int rc;
   const bool capturing = is_capturing(stream), known = P->dev && P->dev->layer[which].cached;
   if (!known && (rc = materialize(P))) return rc;
@@ -544,22 +547,27 @@ int run_layer_on(dmm_plan_t *P, int which, const std::vector<char> &inputs, void
     // does not change its bits)
     LayerWork work[2];
     LayerDense dense[2] = {LAYER_IN_PLACE, LAYER_IN_PLACE};
+    LayerCopies copies;
+    // what is laid out: on copies, or of a part
+    auto settle = [&](int x) {
+      const bool of_part = part && x == products - 1;
+      if (dense[x] || of_part) work[x] = make(x, dense[x], &copies, false);
+      if (of_part) choice[x] = choose_layer(work[x], cus, choice[x].runs);
+    };
     for (int x = 0; x < products; ++x) {
-      work[x] = make(x, LAYER_IN_PLACE, nullptr);
+      work[x] = make(x, LAYER_IN_PLACE, nullptr, true);
       choice[x] = choose_layer(work[x], cus);
       double best = choice[x].us;
       for (LayerDense d : {LAYER_BOTH, LAYER_LEFT, LAYER_ROWS}) {
         if (P->C.c != 1 || (d != LAYER_BOTH && x >= lefts)) continue;
-        LayerCopies copies;
-        const LayerWork then = make(x, d, &copies);
+        LayerCopies tried;
+        const LayerWork then = make(x, d, &tried, true);
         const LayerChoice c = choose_layer(then, cus);
-        if (c.us + copies.us() < best && copies.possible())
-          best = c.us + copies.us(), dense[x] = d, choice[x] = c;
+        if (c.us + tried.us() < best && tried.possible())
+          best = c.us + tried.us(), dense[x] = d, choice[x] = c;
       }
     }
-    LayerCopies copies;
-    for (int x = 0; x < products; ++x)
-      if (dense[x]) work[x] = make(x, dense[x], &copies);
+    for (int x = 0; x < products; ++x) settle(x);
     if ((rc = P->dev->uses.order(stream))) return rc;
     for (;;) {
       h.clear();
@@ -584,8 +592,9 @@ int run_layer_on(dmm_plan_t *P, int which, const std::vector<char> &inputs, void
           for (int x = 0; x < products; ++x) {
             if (!dense[x]) continue;
             dense[x] = LAYER_IN_PLACE;
-            work[x] = make(x, LAYER_IN_PLACE, nullptr);
+            work[x] = make(x, LAYER_IN_PLACE, nullptr, true);
             choice[x] = choose_layer(work[x], cus);
+            settle(x);
           }
           continue;
         }
@@ -644,8 +653,8 @@ int run_layer_on(dmm_plan_t *P, int which, const std::vector<char> &inputs, void
 
 template <class Make, class Front>
 int run_layer(dmm_plan_t *P, int which, const std::vector<char> &inputs, void *const *c_tiles, const int64_t *c_ld, bool reduce, hipStream_t stream, int products,
-              int lefts, Make make, Front in_front) {
-  const int rc = run_layer_on(P, which, inputs, c_tiles, c_ld, reduce, stream, products, lefts, make, in_front);
+              int lefts, bool part, Make make, Front in_front) {
+  const int rc = run_layer_on(P, which, inputs, c_tiles, c_ld, reduce, stream, products, lefts, part, make, in_front);
   if (rc == DMM_ENOMEM) (void)hipGetLastError();               // (it would be the next call's)
   return rc;
 }
@@ -929,7 +938,7 @@ int i8_product(dmm_plan_t *P, int which, int act, const dmm_int_tiles *a, const 
   key.put(b, B, true);
   if (b2) key.put(b2, B, true);
   key.put(c, C.c * C.tiles_per_rep());
-  auto make = [&](int, LayerDense dense, LayerCopies *copies) {
+  auto make = [&](int, LayerDense dense, LayerCopies *copies, bool) {
     LayerWork W;
     W.kind = b2 ? LAYER_I8_GATED : LAYER_I8;
     W.act = act;
@@ -1014,7 +1023,7 @@ int i8_product(dmm_plan_t *P, int which, int act, const dmm_int_tiles *a, const 
         });
     return W;
   };
-  return run_layer(P, which, key.bytes, c->tiles, c->ld, reduce, stream, 1, 1, make, [] { return DMM_OK; });
+  return run_layer(P, which, key.bytes, c->tiles, c->ld, reduce, stream, 1, 1, false, make, [] { return DMM_OK; });
 }
 
 // dU = dH act(G), dG = dH U act'(G), tile by tile.
@@ -1307,7 +1316,7 @@ int dmm_gated_execute(dmm_plan_t *P, int activation, const dmm_tiles *a, const d
                                               n0 - B.cc[(size_t)bj], n));
       put_segment(W, s, k1 - k0, guard);
     };
-    auto make = [&](int, LayerDense dense, LayerCopies *copies) {
+    auto make = [&](int, LayerDense dense, LayerCopies *copies, bool) {
       LayerWork W;
       W.kind = LAYER_GATED;
       W.act = activation;
@@ -1367,7 +1376,7 @@ int dmm_gated_execute(dmm_plan_t *P, int activation, const dmm_tiles *a, const d
           [&](int32_t rep, int32_t ti, int32_t tj, int64_t m0, int64_t n0, const dmm_task *, LayerGroup *r) { result(rep, ti, tj, m0, n0, r); });
       return W;
     };
-    return run_layer(P, LAYER_GATED_EXECUTE, key.bytes, nullptr, nullptr, false, (hipStream_t)hip_stream, 1, 1, make, [] { return DMM_OK; });
+    return run_layer(P, LAYER_GATED_EXECUTE, key.bytes, nullptr, nullptr, false, (hipStream_t)hip_stream, 1, 1, false, make, [] { return DMM_OK; });
   } catch (const std::bad_alloc &) {
     return DMM_ENOMEM;
   }
@@ -1396,11 +1405,13 @@ int dmm_gated_backward(dmm_plan_t *P, int activation, const dmm_tiles *a, const 
     for (const dmm_tiles *t : {da ? gate : nullptr, da ? up : nullptr, dgate, dup}) key.put(t, B.tiles_per_rep());
     for (const dmm_tiles *t : {dg, du}) key.put(t, C.tiles_per_rep());
     key.put(da, A.tiles_per_rep());
-    const dmm_tiles *const bs[2] = {gate, up}, *const dcs[2] = {dg, du}, *const dbs[2] = {dgate, dup};
+    const dmm_tiles *const bs[2] = {gate, up}, *const dcs[2] = {dg, du}, *const dbs[2] = {dgate, dup}, *const either[2] = {dgate ? dgate : dup, dup ? dup : dgate};
     const int first = da ? 0 : 1, last = dgate || dup ? 1 : 0;
-    auto make = [&](int x, LayerDense dense, LayerCopies *copies) { return gradients(P, first + x == 0, a, bs, dcs, 2, da, dbs, es, dense, copies); };
+    auto make = [&](int x, LayerDense dense, LayerCopies *copies, bool both) {
+      return gradients(P, first + x == 0, a, bs, dcs, 2, da, both ? either : dbs, es, dense, copies);
+    };
     hipStream_t stream = (hipStream_t)hip_stream;
-    return run_layer(P, LAYER_GATED_BACKWARD, key.bytes, nullptr, nullptr, false, stream, std::max(0, last - first + 1), da != nullptr, make,
+    return run_layer(P, LAYER_GATED_BACKWARD, key.bytes, nullptr, nullptr, false, stream, std::max(0, last - first + 1), da != nullptr, (dgate != nullptr) != (dup != nullptr), make,
                      [&] { return slope(C, activation, g, u, dh, dg, du, stream); });
   } catch (const std::bad_alloc &) {
     return DMM_ENOMEM;
@@ -1428,8 +1439,9 @@ int dmm_execute_backward(dmm_plan_t *P, const dmm_tiles *a, const dmm_tiles *b, 
     key.put(db, B.tiles_per_rep());
     key.put(dc, C.tiles_per_rep());
     const int first = da ? 0 : 1;
-    auto make = [&](int x, LayerDense dense, LayerCopies *copies) { return gradients(P, first + x == 0, a, &b, &dc, 1, da, &db, es, dense, copies); };
-    return run_layer(P, LAYER_EXECUTE_BACKWARD, key.bytes, nullptr, nullptr, false, (hipStream_t)hip_stream, (da != nullptr) + (db != nullptr), da != nullptr, make, [] { return DMM_OK; });
+    auto make = [&](int x, LayerDense dense, LayerCopies *copies, bool) { return gradients(P, first + x == 0, a, &b, &dc, 1, da, &db, es, dense, copies); };
+    return run_layer(P, LAYER_EXECUTE_BACKWARD, key.bytes, nullptr, nullptr, false, (hipStream_t)hip_stream, (da != nullptr) + (db != nullptr), da != nullptr, false, make,
+                     [] { return DMM_OK; });
   } catch (const std::bad_alloc &) {
     return DMM_ENOMEM;
   }

@@ -2,7 +2,7 @@
 import pytest
 
 import workloads
-from tests.layer_tiles import ACTS, Tiles, act, normal, stream
+from tests.layer_tiles import ACTS, Tiles, act, descs, normal, stream
 from tests.test_gpu_layer import H, TINY, close, gated_error, sum_error
 
 torch = pytest.importorskip("torch")
@@ -30,3 +30,25 @@ def test_narrow_tiles_of_weights_behind_a_copy_of_the_rows(m, blocks, k, n, last
     close(h.whole(), want, H * want.abs() + (1 + H) * gated_error(g, u, eg, eu, name) + TINY, "H")
     for t in (h, kg, ku):
         t.check_guards()
+
+
+@pytest.mark.parametrize("layout,m,k,n", [("whole", 4096, 1024, 1024), ("whole", 8192, 512, 768), ("whole", 8192, 1024, 3072), ("whole", 2048, 256, 512), ("whole", 1111, 300, 500),
+                                          ("blocks", 3000, 256, 384), ("uneven", 1301, 1103, 907), ("uneven", 2500, 300, 400), ("row_col", 83, 520, 4096)], ids=str)
+def test_gradients_do_not_depend_on_what_else_is_asked_for(layout, m, k, n):
+    """Bit for bit, whatever macro-tiles and launches the others bring with them.  The sums are cut along K."""
+    (da, db, dc), ranks = descs(layout, m, k, n)
+    plan = binding.Plan(da, db, dc, ranks)
+    a, wg, wu = (Tiles(d, BF16, normal(d["rows"], d["cols"], i, s)) for i, (d, s) in enumerate(((da, 1), (db, k ** -0.5), (db, k ** -0.5))))
+    g, u, dh = (Tiles(dc, BF16, normal(m, n, 5 + i)) for i in range(3))
+    dg, du = Tiles(dc, BF16), Tiles(dc, BF16)
+    want = None
+    for asked in ((1, 1, 1), (1, 0, 0), (0, 1, 0), (0, 0, 1), (1, 1, 0), (1, 0, 1), (0, 1, 1)):
+        out = [Tiles(da, BF16, replicas=1), Tiles(db, torch.float32, replicas=1), Tiles(db, torch.float32, replicas=1)]
+        plan.gated_backward(binding.DMM_SILU, *(t.table() for t in (a, wg, wu, g, u, dh, dg, du)), *(t.table() if x else None for x, t in zip(asked, out)),
+                            binding.DMM_DB_F32, stream())
+        torch.cuda.synchronize()
+        want = want or out
+        for x, t, w, what in zip(asked, out, want, ("dA", "dWg", "dWu")):
+            assert not x or torch.equal(t.whole(), w.whole()), (asked, what)
+    for t, y in ((want[1], dg), (want[2], du)):
+        close(t.whole(), a.whole().t() @ y.whole(), sum_error(a.whole().t(), y.whole()) + TINY, "a weight's gradient")

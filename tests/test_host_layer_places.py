@@ -80,6 +80,7 @@ class Call:
 
     def __init__(self, rec, space, at):
         self.rec, self.space, self.front, self.back = rec, space, [], []
+        self.sums = {}                                         # result, row, column -> k's of every partial sum, in the order they are added in
         ops, multiplied = rec.launches(at), False
         for op in ops:
             if op[1] == "layer_copy_kernel":
@@ -180,13 +181,13 @@ class Call:
             if what == PARTS:
                 parts[c] = corners
             else:
-                self.result(corners, c, ldc, c_es, g, ldg, u, ldu, scales)
+                self.result({at: [of] for at, of in corners.items()}, c, ldc, c_es, g, ldg, u, ldu, scales)
         slots, y = set(parts), 0
         while slots:
             c, ldc, g, u, ldg, ldu, sa, sb, sb2, p, runs, tm, tn, m_ext, n_ext, c_es = JOIN.unpack(ctypes.string_at(joins + y * JOIN.size, JOIN.size))
             all_of = [parts[p + r * tm * tn * 4] for r in range(runs)]
             slots -= {p + r * tm * tn * 4 for r in range(runs)}
-            corners = {at: [x for of in all_of for x in of[at]] for at in all_of[0]}
+            corners = {at: [of[at] for of in all_of] for at in all_of[0]}
             scales = self.scales(sa, sb, sb2, KINDS[kind][2], m_ext, n_ext) if KINDS[kind][3] == 1 else None
             self.result(corners, c, ldc, c_es, g, ldg, u, ldu, scales)
             y += 1
@@ -216,13 +217,14 @@ class Call:
         return names.pop(), int(r[0]), int(c[0])
 
     def result(self, corners, c, ldc, c_es, g, ldg, u, ldu, scales):
-        for (dm, dn), got in corners.items():
+        for (dm, dn), runs in corners.items():
             name, row, col = self.target(c + (dm * ldc + dn) * c_es, c_es)
             for p, ld, kept in ((g, ldg, "g"), (u, ldu, "u")):
                 if p and name == "h":
                     assert self.target(p + (dm * ld + dn) * 2, 2) == (kept, row, col)
             seen = {}
-            for pair, r, q, k in got:
+            self.sums[name, row, col] = [[(pair, tuple(k.tolist())) for pair, _, _, k in got] for got in runs]
+            for pair, r, q, k in (x for got in runs for x in got):
                 assert name in PAIRS[pair], (pair, name)
                 assert (r, q) == (row, col), ("the product of another row or column", pair, (r, q), (row, col))
                 seen.setdefault(pair, []).append(k)
@@ -302,7 +304,36 @@ def narrow_tiles_of_weights_on_a_copy_of_the_rows(rec):
     assert took >= 8
 
 
-SCENARIOS = [operands_meet_at_the_same_k, narrow_tiles_of_weights_on_a_copy_of_the_rows]
+def gradients_are_summed_alike_whatever_else_is_asked_for(rec):
+    """The k's of a gradient come in the same order and in the same partial sums, whichever of the others are asked for as well."""
+    from paper_2510_08874_amd import binding as b
+    rng = random.Random(5)
+    cases = [(made("whole", *x), 1, 0) for x in ((4096, 1024, 1024), (8192, 512, 768), (8192, 1024, 3072), (2048, 256, 512), (1111, 300, 500), (40, 300, 500), (9000, 130, 65))]
+    cases += [(made("uneven", 1301, 1103, 907), 12, 0), (made("uneven", 2500, 300, 400), 12, 1), (made("blocks", 3000, 256, 384), 4, 0)]
+    for _ in range(6):
+        cases.append((*layouts(rng, 64 * rng.randint(1, 40), 64 * rng.randint(1, 12), 64 * rng.randint(1, 12)), rng.choice((0, 1, 8))))
+    cut = 0
+    for d, ranks, more in cases:
+        da, db, dc = d
+        plan, s = b.Plan(*d, ranks), Ground(True)
+        a, w, v = s.bf("a", da, 2, more), s.bf("w", db, 2, more), s.bf("v", db, 2, more)
+        h, g, u = (s.bf("h", dc, 2, more) for _ in range(3))
+        ga, gw, gv = s.bf("ga", da, 2, more, 1), s.bf("gw", db, 4, more, 1), s.bf("gv", db, 4, more + 1, 1)
+        for of in ((0, 0), (0, 1), (1, 0)):                    # rows of dG and dU: as long as each other, or not
+            dg, du = s.bf("dg", dc, 2, more + of[0]), s.bf("du", dc, 2, more + of[1])
+            depth, got = dict(ga=db["cols"], gw=da["rows"], gv=da["rows"]), []
+            for x in ((ga, gw, gv), (ga, None, None), (None, gw, None), (None, None, gv), (ga, None, gv), (None, gw, gv)):
+                got.append(check(rec, s, lambda: plan.gated_backward(b.DMM_SILU, a, w, v, g, u, h, dg, du, *x, b.DMM_DB_F32, 0), depth).sums)
+            for one in got[1:]:
+                both = set(one) & set(got[0])
+                assert {name for name, _, _ in both} == {name for name, _, _ in one}
+                assert all(one[x] == got[0][x] for x in both), [(x, [len(r) for r in one[x]], [len(r) for r in got[0][x]]) for x in both if one[x] != got[0][x]][:3]
+            cut += any(len(runs) > 1 for (name, _, _), runs in got[0].items() if name != "ga")
+        plan.destroy()
+    assert cut > 5
+
+
+SCENARIOS = [gradients_are_summed_alike_whatever_else_is_asked_for, operands_meet_at_the_same_k, narrow_tiles_of_weights_on_a_copy_of_the_rows]
 
 
 @pytest.mark.parametrize("scenario", [f.__name__ for f in SCENARIOS])
