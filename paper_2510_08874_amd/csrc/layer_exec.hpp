@@ -574,8 +574,9 @@ int run_layer_on(dmm_plan_t *P, int which, const std::vector<char> &inputs, void
       size_t parts[2] = {0, 0};                                // partial sums of each product
       const bool pair = products == 2 && choice[0].tiles > 0 && choice[1].tiles > 0 && pair_us(choice, cus) < choice[0].us + choice[1].us;
       for (int x = 0; x < products; ++x) {
-        if (pair) choice[x].shape = LAYER_128;
-        if ((rc = lay_out(work[x], choice[x], &h, &layout[x], &parts[x]))) return rc;
+        LayerChoice as = choice[x];                            // (should there be no memory, what was chosen counts again)
+        if (pair) as.shape = LAYER_128;
+        if ((rc = lay_out(work[x], as, &h, &layout[x], &parts[x]))) return rc;
       }
       const size_t scratch = ((pair ? parts[0] + parts[1] : std::max(parts[0], parts[1])) + 4095) / 4096 * 4096;
       const size_t need = scratch + copies.size;

@@ -333,7 +333,39 @@ def gradients_are_summed_alike_whatever_else_is_asked_for(rec):
     assert cut > 5
 
 
-SCENARIOS = [gradients_are_summed_alike_whatever_else_is_asked_for, operands_meet_at_the_same_k, narrow_tiles_of_weights_on_a_copy_of_the_rows]
+def without_memory_for_copies_each_gradient_has_its_own_macro_tiles(rec):
+    """Both gradients in one launch on copies; without room for these, in two launches, on the tiles that each gets alone."""
+    from paper_2510_08874_amd import binding as b
+    D, block = workloads.desc, workloads.block_desc
+    rec.so.rec_lds.restype = ctypes.c_uint64
+    plans, two = [], 0                                         # (plans live on: buffers of others are not to be had again)
+    for m, k, n, a_rows, b_cols, c_cols, more in ((3712, 3073, 3649, 1, 3, 5, (0, 0, 0)), (3073, 2945, 3777, 8, 1, 1, (0, 8, 0)), (3841, 3456, 2944, 8, 1, 1, (1, 1, 0)),
+                                                  (2945, 3457, 3520, 1, 3, 5, (8, 0, 8))):
+        d, s = (block(m, k, a_rows, 1), block(k, n, 1, b_cols), block(m, n, 1, c_cols)), Ground(True)
+        a, w, dc = (s.bf(name, x, 2, y, 1) for name, x, y in zip(("a", "w", "dg"), d, more))
+        ga, gw = s.bf("ga", d[0], 2, 0, 1), s.bf("gw", d[1], 2, 0, 1)
+
+        def launches(room, x):
+            plans.append(b.Plan(*d, 8))
+            rec.so.rec_set_limit(rec.so.rec_live() + room)
+            at = len(rec.ops())
+            try:
+                plans[-1].execute_backward(a, w, dc, *x, 0, 0)
+            except b.DmmError as e:
+                assert e.kind == "ENOMEM"
+                return None
+            return [(o[1], int(rec.so.rec_lds(o[0])), int(rec.so.rec_blocks(o[0]))) for o in rec.launches(at)]
+
+        assert [x[0] for x in launches(1 << 40, (ga, gw))] == ["layer_copy_kernel", "layer_pair_kernel"]
+        for room in (5 << 20, 9 << 20, 17 << 20):
+            got, alone = launches(room, (ga, gw)), [launches(room, x) for x in ((ga, None), (None, gw))]
+            if got and all(alone) and [x[0] for x in got] == ["layer_gemm_kernel"] * 2:
+                assert got == alone[0] + alone[1], (m, k, n, got, alone)
+                two += 1
+    assert two >= 4
+
+
+SCENARIOS = [without_memory_for_copies_each_gradient_has_its_own_macro_tiles, gradients_are_summed_alike_whatever_else_is_asked_for, operands_meet_at_the_same_k, narrow_tiles_of_weights_on_a_copy_of_the_rows]
 
 
 @pytest.mark.parametrize("scenario", [f.__name__ for f in SCENARIOS])
