@@ -19,9 +19,12 @@ __device__ __forceinline__ unsigned short layer_bf16(float v) { return __builtin
 
 // ---- activations ------------------------------------------------------------------------------------
 
-// 16 / (1 + e^-x): the instruction for 1 / x gives zero instead of results below the normal range, and 1 / (1 + e^87.4) is one
-__device__ __forceinline__ float layer_sigmoid16(float x) {
-  return __builtin_amdgcn_rcpf(__builtin_fmaf(0.0625f, __builtin_amdgcn_exp2f(-1.442695041f * x), 0.0625f));
+// 256 / (1 + e^-x): the instruction for 1 / x gives zero instead of results below the normal range, and 1 / (1 + e^87.4) is one; e^88.8 is past the range, its
+// root is not.  (x / (1 + e^-x) then reaches down to the end of the normal range, x = -92.)
+constexpr float kSigmoidUnit = 1.f / 256;
+__device__ __forceinline__ float layer_sigmoid256(float x) {
+  const float root = __builtin_amdgcn_exp2f(-0.7213475204f * x);
+  return __builtin_amdgcn_rcpf(__builtin_fmaf(kSigmoidUnit * root, root, kSigmoidUnit));
 }
 constexpr float kTanhIn = 1.595769122f, kTanhCube = 0.044715f;   // 2 sqrt(2 / pi): (1 + tanh y) / 2 = 1 / (1 + e^-2y)
 
@@ -45,23 +48,23 @@ __device__ __forceinline__ float layer_normal(float g) {
 
 template <int ACT>
 __device__ __forceinline__ float layer_act(float g) {
-  if constexpr (ACT == DMM_SILU) return 0.0625f * g * layer_sigmoid16(g);
+  if constexpr (ACT == DMM_SILU) return kSigmoidUnit * g * layer_sigmoid256(g);
   if constexpr (ACT == DMM_GELU) return g * layer_normal(g);
-  return 0.0625f * g * layer_sigmoid16(kTanhIn * (g + kTanhCube * g * g * g));
+  return kSigmoidUnit * g * layer_sigmoid256(kTanhIn * (g + kTanhCube * g * g * g));
 }
 // act and its slope
 __device__ __forceinline__ void layer_slope(int act, float g, float *value, float *slope) {
   if (act == DMM_SILU) {
-    const float s16 = layer_sigmoid16(g), s = 0.0625f * s16;
-    *value = 0.0625f * g * s16;
-    *slope = s16 * (0.0625f * (1.f + g * (1.f - s)));
+    const float s256 = layer_sigmoid256(g), s = kSigmoidUnit * s256;
+    *value = kSigmoidUnit * g * s256;
+    *slope = s256 * (kSigmoidUnit * (1.f + g * (1.f - s)));
   } else if (act == DMM_GELU) {
     const float p = layer_normal(g);
     *value = g * p;
     *slope = p + g * 0.3989422804f * __builtin_amdgcn_exp2f(-0.7213475204f * g * g);
   } else {
-    const float s16 = layer_sigmoid16(kTanhIn * (g + kTanhCube * g * g * g)), s = 0.0625f * s16;
-    *value = 0.0625f * g * s16;
+    const float s256 = layer_sigmoid256(kTanhIn * (g + kTanhCube * g * g * g)), s = kSigmoidUnit * s256;
+    *value = kSigmoidUnit * g * s256;
     *slope = s + *value * (1.f - s) * kTanhIn * (1.f + 3.f * kTanhCube * g * g);
   }
 }

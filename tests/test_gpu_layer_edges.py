@@ -3,7 +3,7 @@ import pytest
 
 import workloads
 from tests.layer_tiles import ACTS, Tiles, act, descs, normal, stream
-from tests.test_gpu_layer import H, TINY, close, gated_error, sum_error
+from tests.test_gpu_layer import H, TINY, U, argument, close, gated_error, sum_error
 
 torch = pytest.importorskip("torch")
 binding = pytest.importorskip("paper_2510_08874_amd.binding")
@@ -52,3 +52,27 @@ def test_gradients_do_not_depend_on_what_else_is_asked_for(layout, m, k, n):
             assert not x or torch.equal(t.whole(), w.whole()), (asked, what)
     for t, y in ((want[1], dg), (want[2], du)):
         close(t.whole(), a.whole().t() @ y.whole(), sum_error(a.whole().t(), y.whole()) + TINY, "a weight's gradient")
+
+
+@pytest.mark.parametrize("name", list(ACTS))
+def test_activations_of_every_number(name):
+    """All finite bf16 numbers through the block (G = g, U = 1) and back (dH = 1): the function and its slope wherever these are.  Where the argument of the
+    exponential is past 200 nothing is left of that in 64 bits of fp32's range, so that its error counts no further."""
+    g = torch.arange(65536, device="cuda", dtype=torch.int32).to(torch.int16).view(BF16)
+    g = g[torch.isfinite(g)].reshape(-1, 1)
+    m = len(g)
+    (da, db, dc), ranks = descs("whole", m, 2, 1)
+    plan = binding.Plan(da, db, dc, ranks)
+    one = torch.ones(m, 1, dtype=BF16, device="cuda")
+    x, w, v, d = Tiles(da, BF16, torch.cat((g, one), 1)), Tiles(db, BF16, torch.eye(2)[:, :1]), Tiles(db, BF16, torch.eye(2)[:, 1:]), Tiles(dc, BF16, one)
+    h, kg, ku, dg, du = (Tiles(dc, BF16) for _ in range(5))
+    plan.gated(ACTS[name], *(t.table() for t in (x, w, v, h, kg, ku)), stream=stream())
+    plan.gated_backward(ACTS[name], None, None, None, *(t.table() for t in (kg, ku, d, dg, du)), stream=stream())
+    torch.cuda.synchronize()
+    G = g.double()
+    value, _ = act(G, name)
+    arg = argument(G, name).clamp(max=200)
+    assert torch.equal(kg.whole(), G) and bool((ku.whole() == 1).all())
+    limit = H * value.abs() + (1 + H) * value.abs() * (10 + 4 * arg) * U + TINY
+    close(h.whole(), value, limit, "H")
+    close(du.whole(), value, limit, "dU")
