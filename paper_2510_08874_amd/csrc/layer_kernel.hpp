@@ -65,7 +65,8 @@ __device__ __forceinline__ void layer_slope(int act, float g, float *value, floa
   } else {
     const float s256 = layer_sigmoid256(kTanhIn * (g + kTanhCube * g * g * g)), s = kSigmoidUnit * s256;
     *value = kSigmoidUnit * g * s256;
-    *slope = s + *value * (1.f - s) * kTanhIn * (1.f + 3.f * kTanhCube * g * g);
+    // (g^2 past the range times no slope would be NaN; from |g| = 20 on s is 0 or 1 and the product zero)
+    *slope = s + *value * (1.f - s) * kTanhIn * (1.f + 3.f * kTanhCube * __builtin_fminf(g * g, 1e30f));
   }
 }
 

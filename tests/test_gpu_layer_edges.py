@@ -70,9 +70,10 @@ def test_activations_of_every_number(name):
     plan.gated_backward(ACTS[name], None, None, None, *(t.table() for t in (kg, ku, d, dg, du)), stream=stream())
     torch.cuda.synchronize()
     G = g.double()
-    value, _ = act(G, name)
+    value, slope = act(G, name)
     arg = argument(G, name).clamp(max=200)
     assert torch.equal(kg.whole(), G) and bool((ku.whole() == 1).all())
     limit = H * value.abs() + (1 + H) * value.abs() * (10 + 4 * arg) * U + TINY
     close(h.whole(), value, limit, "H")
     close(du.whole(), value, limit, "dU")
+    close(dg.whole(), slope, H * slope.abs() + (1 + H) * 2 * (10 + 4 * arg) * U + TINY, "dG")
