@@ -37,7 +37,7 @@ int check_layer_tiles(const Grid &G, const dmm_tiles *t, int es) {
         if (G.rc[ti + 1] > G.rc[ti] && G.cc[tj + 1] > G.cc[tj] && t->ld[G.table_index(rep, ti, tj)] >= kLayerPitch / es) return DMM_ELD;
   return DMM_OK;
 }
-// One replica's, whatever the matrix has.
+// One replica's, whatever the matrix has.  (The copy takes host memory.)
 int check_layer_single(const Grid &G, const dmm_tiles *t, int es) {
   Grid one = G;
   one.c = 1;
@@ -1391,15 +1391,15 @@ int dmm_gated_backward(dmm_plan_t *P, int activation, const dmm_tiles *a, const 
   if ((da && (!gate || !up)) || ((dgate || dup) && !a)) return DMM_EINVAL;
   const Grid &A = P->A, &B = P->B, &C = P->C;
   const int es = (flags & DMM_DB_F32) ? 4 : 2;
-  int rc;
-  for (const dmm_tiles *t : {g, u, dh, dg, du})
-    if ((rc = check_layer_tiles(C, t, 2))) return rc;
-  if (da && ((rc = check_layer_tiles(B, gate, 2)) || (rc = check_layer_tiles(B, up, 2)) || (rc = check_layer_single(A, da, 2)))) return rc;
-  if ((dgate || dup) && (rc = check_layer_tiles(A, a, 2))) return rc;
-  if ((dgate && (rc = check_layer_single(B, dgate, es))) || (dup && (rc = check_layer_single(B, dup, es))) || (rc = check_sizes(P)) || (rc = check_slope(C)))
-    return rc;
   TraceRange whole("dmm_gated_backward");
   try {
+    int rc;
+    for (const dmm_tiles *t : {g, u, dh, dg, du})
+      if ((rc = check_layer_tiles(C, t, 2))) return rc;
+    if (da && ((rc = check_layer_tiles(B, gate, 2)) || (rc = check_layer_tiles(B, up, 2)) || (rc = check_layer_single(A, da, 2)))) return rc;
+    if ((dgate || dup) && (rc = check_layer_tiles(A, a, 2))) return rc;
+    if ((dgate && (rc = check_layer_single(B, dgate, es))) || (dup && (rc = check_layer_single(B, dup, es))) || (rc = check_sizes(P)) || (rc = check_slope(C)))
+      return rc;
     LayerKey key;
     key.put(&flags, sizeof flags);
     key.put(dgate || dup ? a : nullptr, A.tiles_per_rep());
@@ -1425,13 +1425,13 @@ int dmm_execute_backward(dmm_plan_t *P, const dmm_tiles *a, const dmm_tiles *b, 
   if (!P || !dc || (!da && !db) || (da && !b) || (db && !a) || (flags & ~DMM_DB_F32)) return DMM_EINVAL;
   const Grid &A = P->A, &B = P->B, &C = P->C;
   const int es = (flags & DMM_DB_F32) ? 4 : 2;
-  int rc;
-  if ((rc = check_layer_single(C, dc, 2))) return rc;
-  if (da && ((rc = check_layer_single(B, b, 2)) || (rc = check_layer_single(A, da, 2)))) return rc;
-  if (db && ((rc = check_layer_single(A, a, 2)) || (rc = check_layer_single(B, db, es)))) return rc;
-  if ((rc = check_sizes(P))) return rc;
   TraceRange whole("dmm_execute_backward");
   try {
+    int rc;
+    if ((rc = check_layer_single(C, dc, 2))) return rc;
+    if (da && ((rc = check_layer_single(B, b, 2)) || (rc = check_layer_single(A, da, 2)))) return rc;
+    if (db && ((rc = check_layer_single(A, a, 2)) || (rc = check_layer_single(B, db, es)))) return rc;
+    if ((rc = check_sizes(P))) return rc;
     LayerKey key;
     key.put(&flags, sizeof flags);
     key.put(db ? a : nullptr, A.tiles_per_rep());
