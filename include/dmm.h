@@ -439,7 +439,7 @@ int dmm_int_gated_execute(dmm_plan_t *p, int activation, const dmm_int_tiles *a,
  *   dg, du          dG = dH U act'(G), dU = dH act(G), bf16 tiles of the plan's C.  They may be the tiles of G and U.
  *   da              dA = dG Wg^T + dU Wu^T, bf16, or null
  *   dgate, dup      dWg = A^T dG, dWu = A^T dU, bf16 (fp32 with DMM_DB_F32), or null
- * dA, dWg and dWu are products of dG and dU as they are stored, in bf16.  They are overwritten, and have one replica (grid_rows * grid_cols tiles in
+ * dA, dWg and dWu are products of dG and dU as they are stored, in bf16.  They are overwritten, must not overlap what the call reads, and have one replica (grid_rows * grid_cols tiles in
  * the cuts of A and B), whatever the operands have; of these replica 0 is read.  a may be null without dgate and dup, the weights without da.  Bits of each result do
  * not depend on which others are asked for.  Copies, captures, streams and ownership as for dmm_gated_execute. */
 int dmm_gated_backward(dmm_plan_t *p, int activation, const dmm_tiles *a, const dmm_tiles *gate, const dmm_tiles *up, const dmm_tiles *g,
@@ -447,7 +447,7 @@ int dmm_gated_backward(dmm_plan_t *p, int activation, const dmm_tiles *a, const 
                        const dmm_tiles *dup, uint32_t flags, void *hip_stream);
 
 /* The gradients of C = A B in bf16: dA = dC B^T and dB = A^T dC (either may be null), from tiles in the cuts of the plan's A, B and C.  All tables
- * name one replica, whatever the plan has.  da is bf16, db bf16 (fp32 with DMM_DB_F32); both are overwritten.  a may be null without db, b
+ * name one replica, whatever the plan has.  da is bf16, db bf16 (fp32 with DMM_DB_F32); both are overwritten and must not overlap what the call reads.  a may be null without db, b
  * without da.  Rows lie less than 2^24 bytes apart (DMM_ELD).  Copies, captures, streams and ownership as for dmm_gated_execute. */
 int dmm_execute_backward(dmm_plan_t *p, const dmm_tiles *a, const dmm_tiles *b, const dmm_tiles *dc, const dmm_tiles *da, const dmm_tiles *db,
                          uint32_t flags, void *hip_stream);

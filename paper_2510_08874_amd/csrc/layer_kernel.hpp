@@ -28,8 +28,8 @@ __device__ __forceinline__ float layer_sigmoid256(float x) {
 }
 constexpr float kTanhIn = 1.595769122f, kTanhCube = 0.044715f;   // 2 sqrt(2 / pi): (1 + tanh y) / 2 = 1 / (1 + e^-2y)
 
-// The normal distribution's (1 + erf(g / sqrt 2)) / 2, to 5 units in the last place wherever it is (1 + erf would lose what is left of it where g
-// is negative): with x = |g| / sqrt 2 and t = 1 / (1 + x / 2), erfc(x) e^(x^2) / t is a smooth function of t, here by the polynomial of degree 8
+// The normal distribution's (1 + erf(g / sqrt 2)) / 2, to 5 units in the last place down to g = -2 and, where little is left of it, to 1.5 for every unit of the
+// exponential's argument g^2 / 2, which is rounded to fp32 (12 units at -4, 126 at -13; 1 + erf would lose it altogether): with x = |g| / sqrt 2 and t = 1 / (1 + x / 2), erfc(x) e^(x^2) / t is a smooth function of t, here by the polynomial of degree 8
 // whose largest relative error over x <= 14 is the least (2^-24; beyond, e^(-x^2) is zero).
 __device__ __forceinline__ float layer_normal(float g) {
   const float t = __builtin_amdgcn_rcpf(1.f + 0.3535533906f * __builtin_fabsf(g));

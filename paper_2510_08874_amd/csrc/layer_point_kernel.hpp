@@ -374,7 +374,7 @@ __global__ __launch_bounds__(256) void i8_rows_kernel(I8Args) {
 }
 
 // Integers along the columns: the block is left in LDS, where every thread finds 32 rows of one or two columns.  ALL: a block has all rows of its columns, and
-// finds their largest magnitudes there as well (one launch for four: 16 x 8192 bf16, and back, 23 us and 15).
+// finds their largest magnitudes there as well (one launch for four: 16 x 8192, and back, bf16 23 us and 15, fp32 20 and 9.6).
 template <bool F32, bool ALL>
 __global__ __launch_bounds__(256) void i8_cols_kernel(I8Args) {
   using B = I8Block<F32>;

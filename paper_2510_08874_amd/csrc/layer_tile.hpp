@@ -14,8 +14,8 @@
 // products of 4-bit operands, all fragments of a step are read in its first half and the quarter before; behind a barrier its stage is
 // filled again in the second half, a quarter before another barrier waits for the step behind it.
 //
-// Measured, whole products: integers 2.55 to 2.65 POP/s (16384 x 8192 x 28672), bf16 1.34 to 1.45 PFLOP/s gated (8192 x 12288 x 49152), 1.38 to 1.44
-// along K and across K (8192^3), where the library's largest product makes 1.41 and the pipes alone 1.77 to 1.81 from registers.  A step takes
+// Measured, whole products: integers 2.41 to 2.56 POP/s (16384 x 8192 x 28672), bf16 1.30 to 1.36 PFLOP/s gated (8192 x 12288 x 49152), 1.40
+// along K and across K (both gradients of 8192^3), where the library's largest product makes 1.41 and the pipes alone 1.77 to 1.81 from registers.  A step takes
 // 1.37 to 1.42 us of which matrix instructions are 1.19, a tile's ends (first stages, epilogue) 8 to 11 us of 64 steps' 90.
 //
 // Shapes, and what each is for:
